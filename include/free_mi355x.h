@@ -509,6 +509,68 @@ int32_t free_op_linear_ln(const void* z, const void* W, int32_t M, int32_t N, in
                           const float* c1, const float* c0, int64_t fold_stride, int32_t rows_per_sample,
                           int32_t gelu, void* out, void* stream);
 
+/* ---- operators of rotary, gated transformer blocks and of their training ------------------------------------------------
+ * Targets and drafters of newer design turn queries and keys by their position (in place of the sin-cos table that is added to
+ * the tokens) and have a gated feed-forward block; fitting a drafter needs gradients.  These calls stand beside free_op_ln_modulate,
+ * free_op_linear and free_op_attention and chain with them: layer norm, QKV layer, rotary positions on the q | k part of its rows,
+ * attention, output layer, layer norm, feed-forward block.
+ * All of them only enqueue on `stream`, allocate nothing and can be captured in a HIP graph (a workspace belongs to one call at a
+ * time: graphs that may run at once need one each).  Equal inputs give equal bits.  dtype, x_dtype: FREE_FP32 or FREE_BF16, the
+ * element type of the tensors it is said of.  No rows (M = 0, rows = 0) is not an error: nothing is written but the gradients
+ * of weights, which are zero.  Outputs must not overlap inputs except where said.  Infinite or NaN inputs give NaN where a sum or
+ * product of theirs does, and nowhere else.
+ *
+ * Layer norm, affine or modulated, over rows of D values:
+ *   xh = (x - mean) / sqrt(var + eps),  out = xh w_s + b_s,  s = row / rows_per_sample
+ * x [M, D] of x_dtype, out [M, D] of dtype; weight, bias fp32, sample s's at weight + s wb_stride (NULL: ones, zeros; with one
+ * sample, rows_per_sample >= M, the stride does not count); plus_one != 0: w_s is 1 + the weight given (adaLN's scale).  Biased variance,
+ * statistics fp32.  D <= 16384 (FREE_ERR_LIMIT).
+ * The gradient: dout [M, D] of dtype, dx [M, D] of x_dtype,
+ *   dx = (g - mean(g) - xh mean(g xh)) / sqrt(var + eps),  g = dout w_s,
+ *   dweight_s = sum over the sample's rows of dout xh,  dbias_s = sum of dout   (fp32, at + s grad_stride; both or neither NULL).
+ * Mean and variance are computed again from x: the forward pass keeps nothing.  dx may be dout or x if the types are equal.  Without
+ * dweight and dbias no workspace is needed.  Samples: at most 2^22 in the gradient (FREE_ERR_LIMIT). */
+int32_t free_op_layer_norm(const void* x, int32_t x_dtype, const float* weight, const float* bias, int32_t wb_stride, int32_t plus_one,
+                           float eps, int32_t M, int32_t D, int32_t rows_per_sample, int32_t dtype, void* out, void* stream);
+size_t free_layer_norm_backward_workspace_bytes(int32_t M, int32_t D, int32_t rows_per_sample);
+int32_t free_op_layer_norm_backward(const void* dout, int32_t dtype, const void* x, int32_t x_dtype, const float* weight,
+                                    int32_t w_stride, int32_t plus_one, float eps, int32_t M, int32_t D, int32_t rows_per_sample,
+                                    void* dx, float* dweight, float* dbias, int32_t grad_stride, void* workspace, size_t ws_bytes,
+                                    void* stream);
+
+/* Rotary positions over several axes (time, row, column, ...).  The dh values of a head are cut into one section of axis_dims[a] values
+ * ([host], even) per axis, in order, and a rest that is copied; pair i of axis a's section is turned by pos[., a] theta^(-2 i / axis_dims[a]):
+ *   (u, v) -> (u cos - v sin, u sin + v cos);  inverse != 0: by the opposite angle, which is the gradient's way back.
+ * FREE_ROPE_PAIRS: the section's values 2 i and 2 i + 1 are a pair; FREE_ROPE_HALVES: i and i + axis_dims[a] / 2.
+ * x: `rows` token rows of `heads` heads next to each other, x_stride values from row to row (the q | k part of packed q | k | v rows is
+ * 2 heads with the stride of the whole row); out likewise, and it may be x with the same stride.  pos [pos_rows, axes] int32, token row m
+ * at m % pos_rows (one grid for all states of a batch); any int32 is a position, and its angle is exact to 2^-30 turns.
+ * dh even and <= 256, 1 to 4 axes, theta >= 1.  At most 2^24 workgroups of 256 threads, a thread having up to four heads of one to four
+ * pairs (FREE_ERR_LIMIT). */
+#define FREE_ROPE_PAIRS  0
+#define FREE_ROPE_HALVES 1
+int32_t free_op_rope_axes(const void* x, int64_t x_stride, const int32_t* pos, int32_t pos_rows, int32_t rows, int32_t heads, int32_t dh,
+                          int32_t axes, const int32_t* axis_dims, double theta, int32_t pairing, int32_t inverse, int32_t dtype,
+                          void* out, int64_t out_stride, void* stream);
+
+/* Gated feed-forward block of M token rows of width D with F hidden values, all tensors of type dtype, contiguous and 16-byte aligned:
+ *   [g | u] = x w_in^T,  h = act(g) u,  out = h w_out^T;   w_in [2 F, D] (gate rows, then up rows), w_out [D, F]
+ * act: FREE_ACT_SILU or FREE_ACT_GELU (tanh form).  Any D and F; sums, g and u are fp32, h is rounded to dtype.
+ * saved (NULL: none): free_gated_ffn_saved_bytes bytes that the gradient's pass reads, of a layout of the library's own; they belong to
+ * these sizes and this x.
+ * The gradient: dx [M, D] and dw_in, dw_out of the weights' shapes, written, not added to; g's and u's gradients are rounded to dtype.
+ * `saved` and workspaces are 256-byte aligned (FREE_ERR_WORKSPACE).  free_gated_ffn_workspace_bytes(.., backward): of the forward call,
+ * or, backward != 0, enough for both. */
+#define FREE_ACT_SILU 0
+#define FREE_ACT_GELU 1
+size_t free_gated_ffn_saved_bytes(int32_t M, int32_t D, int32_t F, int32_t dtype);
+size_t free_gated_ffn_workspace_bytes(int32_t M, int32_t D, int32_t F, int32_t dtype, int32_t backward);
+int32_t free_op_gated_ffn(const void* x, const void* w_in, const void* w_out, int32_t M, int32_t D, int32_t F, int32_t dtype, int32_t act,
+                          void* out, void* saved, size_t saved_bytes, void* workspace, size_t ws_bytes, void* stream);
+int32_t free_op_gated_ffn_backward(const void* dout, const void* x, const void* w_in, const void* w_out, const void* saved,
+                                   size_t saved_bytes, int32_t M, int32_t D, int32_t F, int32_t dtype, int32_t act, void* dx, void* dw_in,
+                                   void* dw_out, void* workspace, size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

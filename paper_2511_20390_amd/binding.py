@@ -22,6 +22,8 @@ FREE_FP32, FREE_BF16 = 0, 1
 EPI_BIAS, EPI_BIAS_GELU, EPI_GATE_RESID = 0, 1, 2
 LN_FOLD_OFF, LN_FOLD_AUTO, LN_FOLD_REQUIRE = 0, 1, 2
 LN_SLOT_COLS = 128
+ROPE_PAIRS, ROPE_HALVES = 0, 1
+ACTS = {"silu": 0, "gelu": 1}
 MODES = {"fp32": FREE_FP32, "bf16": FREE_BF16}
 
 EXPORTED_SYMBOLS = [
@@ -36,6 +38,8 @@ EXPORTED_SYMBOLS = [
     "free_dit_set_ln_fold", "free_dit_ln_fold_active", "free_op_ln_fold_vectors", "free_op_linear_resid_prep",
     "free_op_linear_ln", "free_op_linear_f32", "free_op_attention_split",
     "free_profile_begin", "free_profile_end", "free_profile_category_name", "free_mfma_ceiling", "free_validate_inputs",
+    "free_op_layer_norm", "free_layer_norm_backward_workspace_bytes", "free_op_layer_norm_backward", "free_op_rope_axes",
+    "free_gated_ffn_saved_bytes", "free_gated_ffn_workspace_bytes", "free_op_gated_ffn", "free_op_gated_ffn_backward",
 ]
 PROF_NCAT = 12
 
@@ -156,6 +160,22 @@ def load():
     lib.free_mfma_ceiling.argtypes = [i32, vp, vp, vp]
     lib.free_profile_category_name.restype = C.c_char_p
     lib.free_profile_category_name.argtypes = [i32]
+    lib.free_op_layer_norm.restype = i32
+    lib.free_op_layer_norm.argtypes = [vp, i32, vp, vp, i32, i32, f32, i32, i32, i32, i32, vp, vp]
+    lib.free_layer_norm_backward_workspace_bytes.restype = sz
+    lib.free_layer_norm_backward_workspace_bytes.argtypes = [i32] * 3
+    lib.free_op_layer_norm_backward.restype = i32
+    lib.free_op_layer_norm_backward.argtypes = [vp, i32, vp, i32, vp, i32, i32, f32, i32, i32, i32, vp, vp, vp, i32, vp, sz, vp]
+    lib.free_op_rope_axes.restype = i32
+    lib.free_op_rope_axes.argtypes = [vp, i64, vp, i32, i32, i32, i32, i32, vp, C.c_double, i32, i32, i32, vp, i64, vp]
+    lib.free_gated_ffn_saved_bytes.restype = sz
+    lib.free_gated_ffn_saved_bytes.argtypes = [i32] * 4
+    lib.free_gated_ffn_workspace_bytes.restype = sz
+    lib.free_gated_ffn_workspace_bytes.argtypes = [i32] * 5
+    lib.free_op_gated_ffn.restype = i32
+    lib.free_op_gated_ffn.argtypes = [vp, vp, vp, i32, i32, i32, i32, i32, vp, vp, sz, vp, sz, vp]
+    lib.free_op_gated_ffn_backward.restype = i32
+    lib.free_op_gated_ffn_backward.argtypes = [vp] * 5 + [sz] + [i32] * 5 + [vp, vp, vp, vp, sz, vp]
     _lib = lib
     return lib
 
@@ -704,4 +724,191 @@ def op_ln_modulate(x, shift, scale, rows_per_sample: int, mode: str):
     out = torch.empty(M, D, dtype=torch.float32 if mode == "fp32" else torch.bfloat16, device=x.device)
     _check(load().free_op_ln_modulate(_ptr(x), _ptr(shift), _ptr(scale), shift.stride(0), M, D, rows_per_sample,
                                       MODES[mode], _ptr(out), _stream()), "free_op_ln_modulate")
+    return out
+
+
+# ---- operators of rotary, gated blocks and of their training ------------------------------------------------------
+def _mode_of(t, name):
+    """FREE_FP32 or FREE_BF16, by a tensor's element type."""
+    import torch
+    if t.dtype == torch.bfloat16:
+        return FREE_BF16
+    if t.dtype == torch.float32:
+        return FREE_FP32
+    raise FreeError(FREE_ERR_DTYPE, f"{name}: element type {t.dtype}, expected float32 or bfloat16")
+
+
+def _same_device(first, *others):
+    """The device the call runs on, whatever the current one is: that of its tensors, which have to agree."""
+    for t in others:
+        if t is not None and t.device != first.device:
+            raise FreeError(FREE_ERR_SHAPE, f"tensors on {first.device} and {t.device}")
+    return first.device
+
+
+def _enqueue(fn, where, device, *args):
+    """fn(*args, stream) on the current stream of `device`."""
+    import torch
+    if device.index == torch.cuda.current_device():
+        st = fn(*args, _stream())
+    else:
+        with torch.cuda.device(device):
+            st = fn(*args, _stream())
+    if st != FREE_OK:
+        raise FreeError(st, where)
+
+
+def _vectors(t, name, samples, D):
+    """Address and sample stride of per-sample vectors [samples, D] (one sample: [D] too), rows dense, any distance apart."""
+    import torch
+    if t is None:
+        return None, 0
+    if not t.is_cuda:
+        raise FreeError(FREE_ERR_NULL, f"{name}: not a device tensor")
+    if t.dtype != torch.float32:
+        raise FreeError(FREE_ERR_DTYPE, f"{name}: element type {t.dtype}, expected float32")
+    if tuple(t.shape) != (samples, D) and not (samples == 1 and tuple(t.shape) == (D,)):
+        raise FreeError(FREE_ERR_SHAPE, f"{name}: shape {tuple(t.shape)}, expected {(samples, D)}")
+    if D > 1 and t.stride(-1) != 1:
+        raise FreeError(FREE_ERR_SHAPE, f"{name}: values of a row are not next to each other")
+    return t.data_ptr(), D if samples == 1 else t.stride(0)
+
+
+def _norm_rows(x, rows_per_sample):
+    if x.dim() != 2:
+        raise FreeError(FREE_ERR_SHAPE, f"x: shape {tuple(x.shape)}, expected [rows, width]")
+    M, D = x.shape
+    rows = max(M, 1) if rows_per_sample is None else int(rows_per_sample)
+    if rows < 1:
+        raise FreeError(FREE_ERR_SHAPE, f"rows_per_sample: {rows}")
+    return M, D, rows, max(1, -(-M // rows))
+
+
+def op_layer_norm(x, weight=None, bias=None, mode: str = None, rows_per_sample: int = None, modulate: bool = False,
+                  eps: float = 1e-6, out=None):
+    """Layer norm of the rows of x [M, D] (float32 or bfloat16), affine (weight, bias [D]) or per sample ([samples, D], sample =
+    row // rows_per_sample); modulate: the weight is adaLN's scale, 1 + weight.  mode: element type of the result, x's by default."""
+    import torch
+    M, D, rows, samples = _norm_rows(x, rows_per_sample)
+    dtype = _mode_of(x, "x") if mode is None else MODES[mode]
+    kind = torch.bfloat16 if dtype == FREE_BF16 else torch.float32
+    w, ws = _vectors(weight, "weight", samples, D)
+    b, bs = _vectors(bias, "bias", samples, D)
+    if w is not None and b is not None and ws != bs:
+        raise FreeError(FREE_ERR_SHAPE, "weight and bias: different strides")
+    if out is None:
+        out = torch.empty(M, D, dtype=kind, device=x.device)
+    dev = _same_device(x, weight, bias, out)
+    _enqueue(load().free_op_layer_norm, "free_op_layer_norm", dev, _addr(x, x.dtype, "x"), _mode_of(x, "x"), w, b, ws or bs,
+             int(bool(modulate)), float(eps), M, D, rows, dtype, _addr(out, kind, "out", (M, D)))
+    return out
+
+
+def layer_norm_backward_workspace_bytes(M: int, D: int, rows_per_sample: int = None) -> int:
+    return load().free_layer_norm_backward_workspace_bytes(M, D, max(M, 1) if rows_per_sample is None else rows_per_sample)
+
+
+def op_layer_norm_backward(dout, x, weight=None, rows_per_sample: int = None, modulate: bool = False, eps: float = 1e-6,
+                           want_weight: bool = True, out=None, workspace=None):
+    """Gradient of op_layer_norm: (dx of x's type, dweight, dbias [samples, D] float32, None without want_weight).  out: the three to
+    write to."""
+    import torch
+    M, D, rows, samples = _norm_rows(x, rows_per_sample)
+    if out is None:
+        new = lambda: torch.empty(samples, D, dtype=torch.float32, device=x.device) if want_weight else None
+        out = (torch.empty_like(x), new(), new())
+    dx, dw, db = out
+    if want_weight and workspace is None:
+        workspace = torch.empty(layer_norm_backward_workspace_bytes(M, D, rows), dtype=torch.uint8, device=x.device)
+    w, ws = _vectors(weight, "weight", samples, D)
+    gw, gws = _vectors(dw, "dweight", samples, D)
+    gb, gbs = _vectors(db, "dbias", samples, D)
+    if gws != gbs:
+        raise FreeError(FREE_ERR_SHAPE, "dweight and dbias: different strides, or only one of them")
+    dev = _same_device(x, dout, weight, dx, dw, db, workspace)
+    _enqueue(load().free_op_layer_norm_backward, "free_op_layer_norm_backward", dev, _addr(dout, dout.dtype, "dout", (M, D)),
+             _mode_of(dout, "dout"), _addr(x, x.dtype, "x"), _mode_of(x, "x"), w, ws, int(bool(modulate)), float(eps), M, D, rows,
+             _addr(dx, x.dtype, "dx", (M, D)), gw, gb, gws, _addr(workspace, torch.uint8, "workspace", optional=True),
+             0 if workspace is None else workspace.numel())
+    return out
+
+
+def op_rope_axes(x, pos, heads: int, dh: int, axis_dims, theta: float = 10000.0, pairing: int = ROPE_PAIRS, inverse: bool = False,
+                 out=None):
+    """Rotary positions over len(axis_dims) axes.  x [rows, heads * dh], values of a row next to each other, rows any distance apart (the
+    q | k part of packed rows: heads = q's and k's); pos [pos_rows, axes] int32, row m at m % pos_rows.  out: a tensor like x, or x
+    itself; a new dense one by default."""
+    import torch
+    if x.dim() != 2 or pos.dim() != 2:
+        raise FreeError(FREE_ERR_SHAPE, f"x, pos: shapes {tuple(x.shape)}, {tuple(pos.shape)}, expected two axes each")
+    rows, width = x.shape
+    axes = len(axis_dims)
+    if width != heads * dh or pos.shape[1] != axes:
+        raise FreeError(FREE_ERR_SHAPE, f"x {tuple(x.shape)}, pos {tuple(pos.shape)}: expected {heads * dh} and {axes} columns")
+    if out is None:
+        out = torch.empty(rows, width, dtype=x.dtype, device=x.device)
+    if tuple(out.shape) != (rows, width) or out.dtype != x.dtype:
+        raise FreeError(FREE_ERR_SHAPE if out.dtype == x.dtype else FREE_ERR_DTYPE, f"out: {out.dtype} {tuple(out.shape)}, expected x's")
+    for t, name in ((x, "x"), (out, "out")):
+        if not t.is_cuda:
+            raise FreeError(FREE_ERR_NULL, f"{name}: not a device tensor")
+        if width > 1 and t.stride(1) != 1:
+            raise FreeError(FREE_ERR_SHAPE, f"{name}: values of a row are not next to each other")
+    dev = _same_device(x, pos, out)
+    dims = (C.c_int32 * max(axes, 1))(*axis_dims)
+    _enqueue(load().free_op_rope_axes, "free_op_rope_axes", dev, x.data_ptr(), x.stride(0), _addr(pos, torch.int32, "pos"), pos.shape[0],
+             rows, heads, dh, axes, dims, float(theta), int(pairing), int(bool(inverse)), _mode_of(x, "x"), out.data_ptr(), out.stride(0))
+    return out
+
+
+def gated_ffn_saved_bytes(M: int, D: int, F: int, mode: str) -> int:
+    """Bytes of what op_gated_ffn keeps for op_gated_ffn_backward."""
+    return load().free_gated_ffn_saved_bytes(M, D, F, MODES[mode])
+
+
+def gated_ffn_workspace_bytes(M: int, D: int, F: int, mode: str, backward: bool = False) -> int:
+    """Workspace of op_gated_ffn; with backward, of either pass."""
+    return load().free_gated_ffn_workspace_bytes(M, D, F, MODES[mode], int(bool(backward)))
+
+
+def _ffn_sizes(x, w_in, w_out):
+    if x.dim() != 2 or w_in.dim() != 2 or w_out.dim() != 2:
+        raise FreeError(FREE_ERR_SHAPE, "x, w_in, w_out: two axes each")
+    return x.shape[0], x.shape[1], w_out.shape[1], _mode_of(x, "x")
+
+
+def op_gated_ffn(x, w_in, w_out, act: str = "silu", saved=None, out=None, workspace=None):
+    """act(x w_gate^T) * (x w_up^T) w_out^T for x [M, D], w_in [2 F, D] (gate rows, then up rows), w_out [D, F], all float32 or all
+    bfloat16.  saved: None, or a uint8 tensor of gated_ffn_saved_bytes for op_gated_ffn_backward."""
+    import torch
+    M, D, F, dtype = _ffn_sizes(x, w_in, w_out)
+    u8 = torch.uint8
+    if out is None:
+        out = torch.empty(M, D, dtype=x.dtype, device=x.device)
+    if workspace is None:
+        workspace = torch.empty(load().free_gated_ffn_workspace_bytes(M, D, F, dtype, 0), dtype=u8, device=x.device)
+    dev = _same_device(x, w_in, w_out, saved, out, workspace)
+    _enqueue(load().free_op_gated_ffn, "free_op_gated_ffn", dev, _addr(x, x.dtype, "x"), _addr(w_in, x.dtype, "w_in", (2 * F, D)),
+             _addr(w_out, x.dtype, "w_out", (D, F)), M, D, F, dtype, ACTS[act], _addr(out, x.dtype, "out", (M, D)),
+             _addr(saved, u8, "saved", optional=True), 0 if saved is None else saved.numel(), _addr(workspace, u8, "workspace"),
+             workspace.numel())
+    return out
+
+
+def op_gated_ffn_backward(dout, x, w_in, w_out, saved, act: str = "silu", out=None, workspace=None):
+    """Gradient of op_gated_ffn, of which `saved` is: (dx, dw_in, dw_out).  out: the three to write to."""
+    import torch
+    M, D, F, dtype = _ffn_sizes(x, w_in, w_out)
+    u8 = torch.uint8
+    if out is None:
+        out = (torch.empty_like(x), torch.empty_like(w_in), torch.empty_like(w_out))
+    dx, dw_in, dw_out = out
+    if workspace is None:
+        workspace = torch.empty(load().free_gated_ffn_workspace_bytes(M, D, F, dtype, 1), dtype=u8, device=x.device)
+    dev = _same_device(x, dout, w_in, w_out, saved, dx, dw_in, dw_out, workspace)
+    _enqueue(load().free_op_gated_ffn_backward, "free_op_gated_ffn_backward", dev, _addr(dout, x.dtype, "dout", (M, D)),
+             _addr(x, x.dtype, "x"), _addr(w_in, x.dtype, "w_in", (2 * F, D)), _addr(w_out, x.dtype, "w_out", (D, F)),
+             _addr(saved, u8, "saved"), saved.numel(), M, D, F, dtype, ACTS[act], _addr(dx, x.dtype, "dx", (M, D)),
+             _addr(dw_in, x.dtype, "dw_in", (2 * F, D)), _addr(dw_out, x.dtype, "dw_out", (D, F)), _addr(workspace, u8, "workspace"),
+             workspace.numel())
     return out

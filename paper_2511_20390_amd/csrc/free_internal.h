@@ -330,4 +330,26 @@ bool mfma_attention_f32_supported(int32_t N, int32_t dh);
 int32_t launch_attention_mfma_f32(const float* qkv, int32_t B, int32_t N, int32_t heads, int32_t dh,
                                   float* out, hipStream_t s);
 
+// ---- operators of rotary, gated blocks and their gradients (norm.hip, rotary.hip, ffn.hip) ----------------------------------
+// The arguments are those of the entry points in the public header, checked by them (block_abi.hip).
+bool norm_covers(int32_t D);
+size_t norm_backward_workspace_bytes(int32_t M, int32_t D, int32_t rows_per_sample);
+int32_t launch_norm_forward(const void* x, int32_t x_dtype, const float* weight, const float* bias, int32_t stride, bool plus_one,
+                            float eps, int32_t M, int32_t D, int32_t rows_per_sample, int32_t dtype, void* out, hipStream_t s);
+int32_t launch_norm_backward(const void* dout, int32_t dtype, const void* x, int32_t x_dtype, const float* weight, int32_t stride,
+                             bool plus_one, float eps, int32_t M, int32_t D, int32_t rows_per_sample, void* dx, float* dweight,
+                             float* dbias, int32_t grad_stride, void* ws, hipStream_t s);
+bool rope_covers(int32_t dh, int32_t axes, const int32_t* dims);
+int32_t launch_rope(const void* x, int64_t x_stride, const int32_t* pos, int32_t pos_rows, int32_t rows, int32_t heads, int32_t dh,
+                    int32_t axes, const int32_t* dims, double theta, bool adjacent, bool inverse, int32_t dtype, void* out,
+                    int64_t out_stride, hipStream_t s);
+bool ffn_covers(int32_t M, int32_t D, int32_t F, int32_t dtype);
+size_t ffn_saved_bytes(int32_t M, int32_t D, int32_t F, int32_t dtype);
+size_t ffn_workspace_bytes(int32_t M, int32_t D, int32_t F, int32_t dtype, bool backward);
+// saved: nullptr, or where the gradient's pass finds what it needs
+int32_t launch_ffn_forward(const void* x, const void* w_in, const void* w_out, int32_t M, int32_t D, int32_t F, int32_t dtype, int32_t act,
+                           void* out, void* saved, void* ws, hipStream_t s);
+int32_t launch_ffn_backward(const void* dout, const void* x, const void* w_in, const void* w_out, const void* saved, int32_t M, int32_t D,
+                            int32_t F, int32_t dtype, int32_t act, void* dx, void* dw_in, void* dw_out, void* ws, hipStream_t s);
+
 }  // namespace freemi
