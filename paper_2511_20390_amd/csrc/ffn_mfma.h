@@ -1,0 +1,36 @@
+// The bf16 matrix products of the gated feed-forward block (ffn_mfma.hip), for ffn.hip.  Sizes but the number of token rows are multiples of
+// 64, pointers 16-byte aligned, leading dimensions multiples of 8.
+#pragma once
+
+#include "free_internal.h"
+
+namespace freemi {
+
+// what a product is: the layout of its operands and its epilogue
+enum FfnKind {
+    FFN_GATE,          // out = act(g) u of X [M, K] and W [2 N, K]
+    FFN_GATE_KEEP,     // and g, u kept in gu
+    FFN_GATE_GRAD,     // out [M, 2 N] = [dg | du] of dh = X [M, K] by W [K, N], with the kept gu
+    FFN_ROWS,          // out = X [M, K] by W [N, K]
+    FFN_ROWS_BY_K,     // out = X [M, K] by W [K, N]
+    FFN_K_BY_K,        // out = X [K, M] by W [K, N]
+    FFN_STORE,         // (epilogues of the kernel alone: plain, and parts of K)
+    FFN_PART
+};
+
+struct FfnProduct {
+    FfnKind kind;
+    const bf16_t *X, *W;
+    int64_t ldx, ldw;
+    int32_t M, N, K;
+    bf16_t* out;
+    int64_t ldo;
+    float* gu = nullptr;             // [M / 32 rounded up][N / 32][2][1024]
+    int32_t act = 0;
+    bool gated() const { return kind == FFN_GATE || kind == FFN_GATE_KEEP; }
+};
+
+// one launch for n products (1, or 2 of the same kind)
+int32_t launch_ffn_products(const FfnProduct* p, int n, hipStream_t s);
+
+}  // namespace freemi

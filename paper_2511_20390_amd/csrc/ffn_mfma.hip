@@ -1,0 +1,486 @@
+// The products of the gated feed-forward block and of its gradient in bf16 on the matrix cores, fp32 accumulation:
+//   C[m, n] = sum over k of X(m, k) W(n, k)
+// with X and W each either row-major (k next to each other) or K-major (rows of k, m or n next to each other):
+//   [g | u] = x w_in^T                          rows, rows       h = act(g) u in the epilogue, and g, u kept
+//   y  = h w_out^T                              rows, rows
+//   dh = dy w_out                               rows, K-major    [dg | du] in the epilogue, from the kept g, u
+//   dx = [dg | du] w_in                         rows, K-major
+//   dw_in = [dg | du]^T x,  dw_out = dy^T h     K-major, K-major both in one launch
+// so that no operand is transposed in memory first: a transposed copy of every factor of the gradient would move 6 M D + 14 M F + 12 D F
+// bytes more.
+//
+// The K loop is that of gemm_pipe.hip (slices of 64 k in two LDS stages, loads global -> LDS, quarter steps).  What a K-major operand
+// changes: a slice is 64 rows of 128 or 256 values, and the fragments come through ds_read_b64_tr_b16, which gives lane i of 16 the i-th
+// column of a 4 x 16 block whose 4-value pieces the 16 lanes address.  A read of 32 lanes covers 4 k x 32 columns, four rows of 64
+// bytes at the same place of rows 256 or 512 bytes long; 16-byte chunk (b4 b3 b2 b1 b0) of row k is kept at place (b4, b1, b2 ^ k1, b3 ^
+// k0, b0) instead, which puts the 32 lanes on 64 different banks.
+// The last slice of a K-major operand ends where the tensor does: the buffer descriptor gives zeros from there on.  Columns past the
+// end of a row hold the next row's values and end in columns of C that are not written.
+#include <algorithm>
+
+#include "free_internal.h"
+#include "ffn_mfma.h"
+#include "gemm_dma.h"
+
+namespace freemi {
+
+namespace {
+
+typedef short s16x4_t __attribute__((ext_vector_type(4)));
+
+struct Problem {
+    const bf16_t *X, *W;
+    int64_t ldx, ldw;            // values from row to row (K-major: from k to k)
+    int32_t M, N, K;             // N: of the hidden values for the gated epilogues
+    int32_t tiles_m, tiles_n, group_m;
+    int32_t splits, split_slices;
+    bf16_t* out;                 // [M, N], ldo values from row to row; gated gradient: dg, du n_gate values further
+    float* part;                 // sums over a part of K: [splits][32 x 32 block][lane][16]
+    float* gu;                   // kept g, u: [32 x 32 block][2][4][lane][4]
+    int64_t ldo;
+    int32_t act;
+};
+
+struct Launch {
+    Problem p[2];
+    int32_t first1;              // workgroups of p[0]
+};
+
+// act(v), act'(v) with the hardware's exponential and reciprocal (1 ulp each): both activations are v s with s = 1 / (1 + 2^-t),
+// t = v log2(e) for SiLU and v (a + b v^2) for the tanh form of GELU
+__device__ __forceinline__ void act_fast(float v, int act, float* f, float* df) {
+    constexpr float kLog2e = 1.4426950408889634f, kA = 2.0f * 0.7978845608028654f, kB = kA * 0.044715f;
+    const float v2 = v * v;
+    const float t = act == FREE_ACT_SILU ? -v * kLog2e : -v * fmaf(v2, kB * kLog2e, kA * kLog2e);
+    const float s = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(t));
+    const float slope = act == FREE_ACT_SILU ? v : v * fmaf(v2, 3.0f * kB, kA);      // v dt / dv
+    *f = v * s;
+    // s (1 - s): where slope is infinite s is 0 or 1 exactly
+    *df = s == 0.f || s == 1.f ? s : fmaf(s * (1.0f - s), slope, s);
+}
+
+template <int EPI>
+constexpr bool kGated = EPI == FFN_GATE || EPI == FFN_GATE_KEEP;
+
+template <int BM, int BN, int WGM, int WGN, bool XK, bool WK, int EPI>
+__global__ __launch_bounds__(512) void ffn_product_kernel(Launch la) {
+    constexpr int NW = 8;
+    static_assert(WGM * WGN == NW && BN / WGN == 64, "eight wavefronts of 64 columns");
+    constexpr int TM = BM / WGM / 32, TN = 2, MF = TM * TN;
+    constexpr int LA = BM / 64, NL = (BM + BN) / 64, D2 = NL / 2, D3 = NL - D2;
+    constexpr int kStageBytes = (BM + BN) * kRowBytes;
+    constexpr int XU = XK ? 2 : 1, WU = WK ? 2 : 1;              // reads per fragment
+    constexpr int RU = XU * TM + WU * TN;                        // reads of a k-step
+    static_assert(!XK || BM == 128 || BM == 256, "rows of a K-major slice");
+    static_assert(!WK || BN == 128 || BN == 256, "rows of a K-major slice");
+    static_assert(!kGated<EPI> || !WK, "gate and up rows are interleaved row by row");
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+
+    const bool second = static_cast<int>(blockIdx.x) >= la.first1;
+    const Problem& a = second ? la.p[1] : la.p[0];
+    const int pid = second ? blockIdx.x - la.first1 : blockIdx.x;
+    const int tiles = a.tiles_m * a.tiles_n;
+    const int split = pid / tiles;
+    int tile_m, tile_n;
+    tile_coords(a.group_m, pid % tiles, a.tiles_m, a.tiles_n, &tile_m, &tile_n);
+    constexpr int kCols = kGated<EPI> ? BN / 2 : BN;             // columns of C per tile
+    const int m0 = tile_m * BM, n0 = tile_n * kCols;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    constexpr int kHalfN = WGN / 2;
+    const int wm = (wave & 3) / kHalfN, wn = (wave >> 2) * kHalfN + (wave & 3) % kHalfN;
+    const int all_slices = (a.K + BK - 1) / BK;
+    const int kt0 = split * a.split_slices;
+    const int nk = (kt0 + a.split_slices < all_slices ? a.split_slices : all_slices - kt0);
+
+    // ---- loads, blocks of 1 KB: w, w + 8, ... per wavefront.  Row-major: 8 rows of 64 k, chunks swizzled as in gemm_pipe.hip.  K-major:
+    // 1024 / row bytes rows of k.
+    const int ldx2 = static_cast<int>(a.ldx) * 2, ldw2 = static_cast<int>(a.ldw) * 2;
+    const auto major_offset = [&](int row_bytes, int ld2) {
+        const int per = 64 / (1024 / row_bytes);                 // lanes per row of k
+        const int k = lane / per + (row_bytes == 512 ? 2 * (wave & 1) : 0), p = lane % per;
+        const int c = (p & 0x11) | ((p >> 3 & 1) << 1) | ((p >> 2 & 1) ^ (k >> 1 & 1)) << 2 | ((p >> 1 & 1) ^ (k & 1)) << 3;
+        return (lane / per) * ld2 + c * 16;
+    };
+    const auto minor_offset = [&](int ld2) { return (lane >> 3) * ld2 + (((lane & 7) ^ (((wave & 1) << 2) | (lane >> 4))) << 4); };
+    const int xoff = XK ? major_offset(BM * 2, ldx2) : minor_offset(ldx2);
+    const int woff = WK ? major_offset(BN * 2, ldw2) : minor_offset(ldw2);
+    constexpr int XB = XK ? 1024 / (BM * 2) : 8, WB = WK ? 1024 / (BN * 2) : 8;       // memory rows per block
+    const uint32_t lds_base = lds_address(lds);
+    // gated: tile row r holds a gate row of the hidden value n0 + 32 (r / 64) + r % 32 where r % 64 < 32, else the up row; wavefronts
+    // 0 to 3 load the gate rows of a group of 64, 4 to 7 the up rows
+    const int64_t w_first = kGated<EPI> ? static_cast<int64_t>(wave < 4 ? 0 : a.N) + n0 + (wave & 3) * 8 : n0;
+    const int64_t w_rows = kGated<EPI> ? 2 * static_cast<int64_t>(a.N) : a.N;
+    u32x4_t xsrd, wsrd;
+    if constexpr (!XK) xsrd = make_rsrc(a.X + m0 * a.ldx, (a.M - m0) * a.ldx * 2);
+    if constexpr (!WK) wsrd = make_rsrc(a.W + w_first * a.ldw, (w_rows - w_first) * a.ldw * 2);
+    // descriptors of a slice of a K-major operand, from its first k on: the offsets inside stay small whatever K is
+    const auto aim = [&](int kt) {
+        const int64_t k = static_cast<int64_t>(kt) * BK;
+        if constexpr (XK) xsrd = make_rsrc(a.X + k * a.ldx + m0, ((a.K - k) * a.ldx - m0) * 2);
+        if constexpr (WK) wsrd = make_rsrc(a.W + k * a.ldw + n0, ((a.K - k) * a.ldw - n0) * 2);
+    };
+    const auto dma = [&](int kt, int stage, int i) {
+        const uint32_t dst = lds_base + stage * kStageBytes + wave * 1024;
+        if (i < LA) {
+            dma_1k(dst + i * NW * 1024, xoff, xsrd, (wave + i * NW) * XB * ldx2 + (XK ? 0 : kt * kRowBytes));
+        } else {
+            const int j = i - LA;
+            const int row = kGated<EPI> ? j * 32 : (wave + j * NW) * WB;
+            dma_1k(dst + BM * kRowBytes + j * NW * 1024, woff, wsrd, row * ldw2 + (WK ? 0 : kt * kRowBytes));
+        }
+    };
+
+    // ---- fragments of k-step ks
+    const int l32 = lane & 31, lhi = lane >> 5;
+    const int sw = (l32 >> 1) & 7;
+    const int kq = (lane & 15) >> 2;                             // the row of k, of four, that this lane addresses
+    const auto major_place = [&](int tile) {                     // of its 8 bytes, in a row of k: columns 32 tile + 16 (lane / 16 % 2) + 4 (lane % 4)
+        const int t0 = tile & 1, t1 = tile >> 1 & 1, t2 = tile >> 2;
+        const int p = (lane >> 1 & 1) | (t1 ^ (kq & 1)) << 1 | (t0 ^ (kq >> 1)) << 2 | (lane >> 4 & 1) << 3 | t2 << 4;
+        return p * 16 + (lane & 1) * 8;
+    };
+    int xat[TM], wat[TN];
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+        xat[i] = XK ? (lhi * 8 + kq) * BM * 2 + major_place(wm * TM + i) : (wm * TM * 32 + l32 + i * 32) * kRowBytes;
+#pragma unroll
+    for (int j = 0; j < TN; ++j)
+        wat[j] = BM * kRowBytes + (WK ? (lhi * 8 + kq) * BN * 2 + major_place(wn * TN + j) : (wn * TN * 32 + l32 + j * 32) * kRowBytes);
+    u32x2_t f[4][TM + TN][2];
+    const auto read_half = [&](const char* at) {
+        return __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)at));
+    };
+    const auto read = [&](int stage, int ks, int r) {            // r-th of the RU reads
+        const char* base = lds + stage * kStageBytes;
+        const int minor = (((ks << 1) | lhi) ^ sw) << 4;
+        if (r < XU * TM) {
+            const int i = r / XU;
+            if constexpr (XK) {
+                f[ks][i][r % 2] = read_half(base + xat[i] + (ks * 16 + (r % 2) * 4) * BM * 2);
+            } else {
+                const u32x4_t v = *reinterpret_cast<const u32x4_t*>(base + xat[i] + minor);
+                f[ks][i][0] = u32x2_t{v[0], v[1]};
+                f[ks][i][1] = u32x2_t{v[2], v[3]};
+            }
+        } else {
+            const int q = r - XU * TM, j = q / WU;
+            if constexpr (WK) {
+                f[ks][TM + j][q % 2] = read_half(base + wat[j] + (ks * 16 + (q % 2) * 4) * BN * 2);
+            } else {
+                const u32x4_t v = *reinterpret_cast<const u32x4_t*>(base + wat[j] + minor);
+                f[ks][TM + j][0] = u32x2_t{v[0], v[1]};
+                f[ks][TM + j][1] = u32x2_t{v[2], v[3]};
+            }
+        }
+    };
+    f32x16_t acc[TM][TN];
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+    const auto frag = [&](int ks, int r) {
+        return __builtin_bit_cast(bf16x8_t, u32x4_t{f[ks][r][0][0], f[ks][r][0][1], f[ks][r][1][0], f[ks][r][1][1]});
+    };
+    const auto mma = [&](int ks, int t) {
+        const int i = t / TN, j = t % TN;
+        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag(ks, TM + j), frag(ks, i), acc[i][j], 0, 0, 0);
+    };
+    // a quarter: the products of k-step ks with nd loads and nr fragment reads spread between them
+    const auto quarter = [&](auto ks_c, auto nd_c, auto nr_c, auto&& load, auto&& fetch) {
+        constexpr int ks = decltype(ks_c)::value, nd = decltype(nd_c)::value, nr = decltype(nr_c)::value;
+#pragma unroll
+        for (int t = 0; t < MF; ++t) {
+#pragma unroll
+            for (int d = t * nd / MF; d < (t + 1) * nd / MF; ++d) load(d);
+#pragma unroll
+            for (int r = t * nr / MF; r < (t + 1) * nr / MF; ++r) fetch(r);
+            mma(ks, t);
+            if constexpr (nd > 0) {
+                if ((t + 1) * nd / MF != t * nd / MF) __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+        if constexpr (nd == 0) {
+#pragma unroll
+            for (int t = 0; t < MF; ++t) {
+                __builtin_amdgcn_sched_group_barrier(kMfma, 1, 0);
+                if ((t + 1) * nr / MF != t * nr / MF) __builtin_amdgcn_sched_group_barrier(kDsRd, (nr + MF - 1) / MF, 0);
+            }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    const auto slice = [&](int kt, auto on, auto more1, auto more2) {   // slices kt + 1, kt + 2 exist; kt counts from this part's first
+        constexpr bool kOn = decltype(on)::value, m1 = decltype(more1)::value, m2 = decltype(more2)::value;
+        constexpr int nd2 = m2 ? D2 : 0, nd3 = m2 ? D3 : 0;
+        const int s = kt & 1, o = s ^ 1;
+        if constexpr (m2) aim(kt0 + kt + 2);
+        const auto load2 = [&](int d) { dma(kt0 + kt + 2, s, d); };
+        const auto load3 = [&](int d) { dma(kt0 + kt + 2, s, D2 + d); };
+        if constexpr (kOn) {
+            const auto none = [](int) {};
+            using std::integral_constant;
+            quarter(integral_constant<int, 0>{}, integral_constant<int, 0>{}, integral_constant<int, 2 * RU>{}, none,
+                    [&](int r) { read(s, 1 + r / RU, r % RU); });
+            quarter(integral_constant<int, 1>{}, integral_constant<int, 0>{}, integral_constant<int, RU>{}, none,
+                    [&](int r) { read(s, 3, r); });
+            if constexpr (m2) wait_lds_barrier();
+            quarter(integral_constant<int, 2>{}, integral_constant<int, nd2>{}, integral_constant<int, 0>{}, load2, none);
+            if constexpr (m1) wait_vm_barrier<nd2>();
+            quarter(integral_constant<int, 3>{}, integral_constant<int, nd3>{}, integral_constant<int, m1 ? RU : 0>{}, load3,
+                    [&](int r) { read(o, 0, r); });
+        } else {
+            if constexpr (m2) wait_lds_barrier();
+#pragma unroll
+            for (int d = 0; d < nd2; ++d) load2(d);
+            if constexpr (m1) wait_vm_barrier<nd2>();
+#pragma unroll
+            for (int d = 0; d < nd3; ++d) load3(d);
+        }
+    };
+    const std::true_type yes{};
+    const std::false_type no{};
+
+    aim(kt0);
+#pragma unroll
+    for (int i = 0; i < NL; ++i) dma(kt0, 0, i);
+    if (nk > 1) {
+        aim(kt0 + 1);
+#pragma unroll
+        for (int i = 0; i < NL; ++i) dma(kt0 + 1, 1, i);
+        wait_vm_barrier<NL>();
+    } else {
+        wait_vm_barrier<0>();
+    }
+    const int gn_wave = n0 + wn * (kGated<EPI> ? 32 : 64);       // this wavefront's first column of C
+    const bool mine = gn_wave < a.N && m0 + wm * TM * 32 < a.M;
+    const auto k_loop = [&](auto on) {
+        if constexpr (decltype(on)::value) {
+#pragma unroll
+            for (int r = 0; r < RU; ++r) read(0, 0, r);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        int kt = 0;
+        for (; kt + 2 < nk; ++kt) slice(kt, on, yes, yes);
+        if (kt + 1 < nk) {
+            slice(kt, on, yes, no);
+            ++kt;
+        }
+        slice(kt, on, no, no);
+    };
+    if (mine) k_loop(yes);
+    else k_loop(no);
+
+    // ---- epilogue: register e of acc[i][j] in lane l is row 32 i + l % 32, column 32 j + 8 (e / 4) + 4 (l / 32) + e % 4 of the wavefront's
+    // part.  bf16 goes through a private piece of the idle stages, so that whole rows are written.
+    __syncthreads();
+    if (!mine) return;
+    constexpr int OC = kGated<EPI> ? 1 : TN;                     // 32-column blocks of an output row
+    constexpr int CH = OC * 4, kStageRow = (CH + 1) * 16;
+    static_assert(NW * 32 * kStageRow <= 2 * kStageBytes, "output staging must fit in the K-loop stages");
+    char* const stage = lds + wave * 32 * kStageRow;
+    // 16 values of a 32 x 32 block -> row l32 of the staging rows, chunks 4 j ..
+    const auto put = [&](int j, const auto& v) {
+#pragma unroll
+        for (int e8 = 0; e8 < 2; ++e8) {
+            const uint32_t lo0 = pack2(v[8 * e8], v[8 * e8 + 1]), lo1 = pack2(v[8 * e8 + 2], v[8 * e8 + 3]);
+            const uint32_t hi0 = pack2(v[8 * e8 + 4], v[8 * e8 + 5]), hi1 = pack2(v[8 * e8 + 6], v[8 * e8 + 7]);
+            const u32x2_t s0 = __builtin_amdgcn_permlane32_swap(lo0, hi0, false, false);
+            const u32x2_t s1 = __builtin_amdgcn_permlane32_swap(lo1, hi1, false, false);
+            *reinterpret_cast<u32x4_t*>(stage + l32 * kStageRow + ((4 * j + 2 * e8 + lhi) << 4)) = u32x4_t{s0[0], s1[0], s0[1], s1[1]};
+        }
+    };
+    const auto flush = [&](int i, bf16_t* out) {                 // the staged 32 rows -> out[row][gn_wave ..]
+        const int gm0 = m0 + (wm * TM + i) * 32;
+#pragma unroll
+        for (int q = 0; q < 32 * CH / 64; ++q) {
+            const int c = q * 64 + lane, row = c / CH, ch = c % CH;
+            const u32x4_t o = *reinterpret_cast<const u32x4_t*>(stage + row * kStageRow + (ch << 4));
+            if (gm0 + row < a.M && gn_wave + ch * 8 < a.N)
+                *reinterpret_cast<u32x4_t*>(out + static_cast<int64_t>(gm0 + row) * a.ldo + gn_wave + ch * 8) = o;
+        }
+    };
+    const int blocks_n = (a.N + 31) / 32;
+    if constexpr (EPI == FFN_PART) {
+        const int64_t blocks = static_cast<int64_t>((a.M + 31) / 32) * blocks_n;
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+            for (int j = 0; j < TN; ++j) {
+                const int mb = m0 / 32 + wm * TM + i, nb = gn_wave / 32 + j;
+                if (mb * 32 >= a.M || nb >= blocks_n) continue;
+                float* p = a.part + (split * blocks + static_cast<int64_t>(mb) * blocks_n + nb) * 1024 + lane * 4;
+#pragma unroll
+                for (int e4 = 0; e4 < 4; ++e4)
+                    *reinterpret_cast<f32x4_t*>(p + e4 * 256) = f32x4_t{acc[i][j][4 * e4], acc[i][j][4 * e4 + 1], acc[i][j][4 * e4 + 2], acc[i][j][4 * e4 + 3]};
+            }
+    } else if constexpr (kGated<EPI>) {
+#pragma unroll
+        for (int i = 0; i < TM; ++i) {
+            if constexpr (EPI == FFN_GATE_KEEP) {
+                const int mb = m0 / 32 + wm * TM + i;
+                if (mb * 32 < a.M) {
+                    float* p = a.gu + (static_cast<int64_t>(mb) * blocks_n + gn_wave / 32) * 2048 + lane * 4;
+#pragma unroll
+                    for (int j = 0; j < 2; ++j)
+#pragma unroll
+                        for (int e4 = 0; e4 < 4; ++e4)
+                            *reinterpret_cast<f32x4_t*>(p + j * 1024 + e4 * 256) =
+                                f32x4_t{acc[i][j][4 * e4], acc[i][j][4 * e4 + 1], acc[i][j][4 * e4 + 2], acc[i][j][4 * e4 + 3]};
+                }
+            }
+            float h[16];
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                float f, df;
+                act_fast(acc[i][0][e], a.act, &f, &df);
+                h[e] = f * acc[i][1][e];
+            }
+            put(0, h);
+            flush(i, a.out);
+        }
+    } else if constexpr (EPI == FFN_GATE_GRAD) {
+#pragma unroll
+        for (int i = 0; i < TM; ++i) {
+            const int mb = m0 / 32 + wm * TM + i;
+            float du[TN][16];
+#pragma unroll
+            for (int j = 0; j < TN; ++j) {
+                const int nb = gn_wave / 32 + j;
+                f32x4_t g[4], u[4];
+                if (mb * 32 < a.M && nb < blocks_n) {
+                    const float* p = a.gu + (static_cast<int64_t>(mb) * blocks_n + nb) * 2048 + lane * 4;
+#pragma unroll
+                    for (int e4 = 0; e4 < 4; ++e4) {
+                        g[e4] = *reinterpret_cast<const f32x4_t*>(p + e4 * 256);
+                        u[e4] = *reinterpret_cast<const f32x4_t*>(p + 1024 + e4 * 256);
+                    }
+                }
+                float dg[16];
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    float f, df;
+                    act_fast(g[e / 4][e % 4], a.act, &f, &df);
+                    du[j][e] = acc[i][j][e] * f;
+                    dg[e] = acc[i][j][e] * u[e / 4][e % 4] * df;
+                }
+                put(j, dg);
+            }
+            flush(i, a.out);
+#pragma unroll
+            for (int j = 0; j < TN; ++j) put(j, du[j]);
+            flush(i, a.out + a.N);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < TM; ++i) {
+#pragma unroll
+            for (int j = 0; j < TN; ++j) put(j, acc[i][j]);
+            flush(i, a.out);
+        }
+    }
+}
+
+// C = the parts, added in order: a wavefront per 32 x 32 block
+__global__ __launch_bounds__(256) void ffn_join_kernel(const float* part, int32_t splits, int32_t M, int32_t N, bf16_t* out) {
+    const int blocks_n = (N + 31) / 32;
+    const int64_t blocks = static_cast<int64_t>((M + 31) / 32) * blocks_n;
+    const int64_t block = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
+    if (block >= blocks) return;
+    const int lane = threadIdx.x & 63;
+    const int mb = static_cast<int>(block / blocks_n), nb = static_cast<int>(block % blocks_n);
+    const float* p = part + block * 1024 + lane * 4;
+    f32x4_t s[4];
+#pragma unroll
+    for (int e4 = 0; e4 < 4; ++e4) s[e4] = *reinterpret_cast<const f32x4_t*>(p + e4 * 256);
+    for (int k = 1; k < splits; ++k) {
+        p += blocks * 1024;
+#pragma unroll
+        for (int e4 = 0; e4 < 4; ++e4) s[e4] += *reinterpret_cast<const f32x4_t*>(p + e4 * 256);
+    }
+    const int m = mb * 32 + (lane & 31);
+    if (m >= M) return;
+#pragma unroll
+    for (int e4 = 0; e4 < 4; ++e4) {
+        const int n = nb * 32 + 8 * e4 + 4 * (lane >> 5);
+        *reinterpret_cast<u32x2_t*>(out + static_cast<int64_t>(m) * N + n) = u32x2_t{pack2(s[e4][0], s[e4][1]), pack2(s[e4][2], s[e4][3])};
+    }
+}
+
+struct Tile {
+    int bm, bn;
+};
+
+template <int BM, int BN, int WGM, int WGN, bool XK, bool WK, int EPI>
+int32_t launch_kernel(const Launch& la, int blocks, hipStream_t s) {
+    auto kern = ffn_product_kernel<BM, BN, WGM, WGN, XK, WK, EPI>;
+    const size_t lds = 2 * static_cast<size_t>(BM + BN) * kRowBytes;
+    static LdsLimit limit;
+    if (!limit.allow(reinterpret_cast<const void*>(kern), lds)) return FREE_ERR_HIP;
+    hipLaunchKernelGGL(kern, dim3(blocks), dim3(512), lds, s, la);
+    return launch_ok() ? FREE_OK : FREE_ERR_HIP;
+}
+
+template <bool XK, bool WK, int EPI>
+int32_t launch_tile(const Tile& t, const Launch& la, int blocks, hipStream_t s) {
+    if (t.bm == 256) return launch_kernel<256, 256, 2, 4, XK, WK, EPI>(la, blocks, s);
+    if (t.bn == 256) return launch_kernel<128, 256, 2, 4, XK, WK, EPI>(la, blocks, s);
+    return launch_kernel<128, 128, 4, 2, XK, WK, EPI>(la, blocks, s);
+}
+
+Tile tile_of(const FfnProduct* p, int n) {
+    // the largest tile that still gives every compute unit one
+    for (const Tile t : {Tile{256, 256}, Tile{128, 256}}) {
+        int64_t tiles = 0;
+        for (int i = 0; i < n; ++i) {
+            const int cols = p[i].gated() ? t.bn / 2 : t.bn;
+            tiles += static_cast<int64_t>((p[i].M + t.bm - 1) / t.bm) * ((p[i].N + cols - 1) / cols);
+        }
+        if (tiles >= device_cus() * 3 / 4) return t;
+    }
+    return Tile{128, 128};
+}
+
+}  // namespace
+
+int32_t launch_ffn_products(const FfnProduct* p, int n, hipStream_t s) {
+    const Tile t = tile_of(p, n);
+    Launch la{};
+    int64_t blocks = 0;
+    for (int i = 0; i < n; ++i) {
+        Problem& q = la.p[i];
+        q.X = p[i].X;
+        q.W = p[i].W;
+        q.ldx = p[i].ldx;
+        q.ldw = p[i].ldw;
+        q.M = p[i].M;
+        q.N = p[i].N;
+        q.K = p[i].K;
+        const int cols = p[i].gated() ? t.bn / 2 : t.bn;
+        q.tiles_m = (q.M + t.bm - 1) / t.bm;
+        q.tiles_n = (q.N + cols - 1) / cols;
+        q.group_m = 8;
+        q.splits = 1;
+        q.split_slices = (q.K + BK - 1) / BK;
+        q.out = p[i].out;
+        q.ldo = p[i].ldo;
+        q.gu = p[i].gu;
+        q.act = p[i].act;
+        if (i == 1) la.first1 = static_cast<int32_t>(blocks);
+        blocks += static_cast<int64_t>(q.tiles_m) * q.tiles_n;
+    }
+    if (n == 1) la.first1 = 0x7fffffff;
+    if (blocks > (1 << 22)) return FREE_ERR_LIMIT;
+    const int b = static_cast<int>(blocks);
+    switch (p[0].kind) {
+        case FFN_GATE: return launch_tile<false, false, FFN_GATE>(t, la, b, s);
+        case FFN_GATE_KEEP: return launch_tile<false, false, FFN_GATE_KEEP>(t, la, b, s);
+        case FFN_GATE_GRAD: return launch_tile<false, true, FFN_GATE_GRAD>(t, la, b, s);
+        case FFN_ROWS: return launch_tile<false, false, FFN_STORE>(t, la, b, s);
+        case FFN_ROWS_BY_K: return launch_tile<false, true, FFN_STORE>(t, la, b, s);
+        case FFN_K_BY_K: return launch_tile<true, true, FFN_STORE>(t, la, b, s);
+        default: return FREE_ERR_RANGE;
+    }
+}
+
+}  // namespace freemi
