@@ -33,4 +33,9 @@ struct FfnProduct {
 // one launch for n products (1, or 2 of the same kind)
 int32_t launch_ffn_products(const FfnProduct* p, int n, hipStream_t s);
 
+// ffn_rows.hip: y of up to kFfnFewRows token rows, any D and F, in two launches; h: room for [M, F]
+constexpr int32_t kFfnFewRows = 64;
+template <typename T>
+int32_t launch_ffn_rows(const T* x, const T* w_in, const T* w_out, int32_t M, int32_t D, int32_t F, int32_t act, T* h, T* out, hipStream_t s);
+
 }  // namespace freemi
