@@ -4,13 +4,18 @@
 // with s = row / rows_per_sample (one sample: the affine layer norm) and w_s the given weight, or 1 + it (adaLN's scale).
 //
 // Both passes are bound by HBM: forward reads x and writes y, backward reads x and dy and writes dx.  So a row is read once and stays
-// in registers: 1 to 16 wavefronts hold it, mean and variance are taken from the registers one after the other (centred, so that
-// nothing cancels), and the gradient's two sums likewise; nothing but the inputs is needed again, so no statistics are kept between
-// the passes.  All sums and statistics are fp32.
+// in registers, over 1 to 8 wavefronts; nothing but the inputs is needed again, so no statistics are kept between the passes.
+// Variance and products with xh are summed around a mean, so that nothing cancels: every wavefront takes the mean of its own values
+// first, without waiting for the others, and sums around that; then the wavefronts of a row exchange all their sums at once - one
+// barrier per row - and each moves them to the row's mean:
+//     sum (x - mean)^2   = sum over wavefronts of  S2_w + n_w (mean_w - mean)^2
+//     sum g (x - mean)   = sum over wavefronts of  GX_w + (mean_w - mean) G_w
+// All sums and statistics are fp32.
 //
-// The weight's gradient sums over rows.  A workgroup walks the rows of one sample with a stride and adds dy xh and dy to registers, per
-// column; at its end its wavefronts add theirs through LDS, in order, and write one partial row; a second launch adds the partial rows
-// of a sample in a fixed order (no atomics: equal inputs give equal bits).  A sample that one workgroup walks is written directly.
+// The weight's gradient sums over rows.  A workgroup walks the rows of one sample with a stride, the next row's loads under way while
+// it computes, and adds dy xh and dy to registers, per column; at its end its wavefronts add theirs through LDS, in order, and write
+// one partial row; a second launch adds the partial rows of a sample in a fixed order (no atomics: equal inputs give equal bits).  A sample
+// that one workgroup walks is written directly.
 #include <algorithm>
 
 #include "free_internal.h"
@@ -21,6 +26,8 @@ namespace freemi {
 namespace {
 
 constexpr int kThreads = 256;
+// wavefronts of a workgroup of the backward pass whose rows take WPR of them
+constexpr int back_waves(int wpr) { return wpr > 4 ? wpr : 4; }
 
 struct NormArgs {
     const void *x, *dy;
@@ -38,46 +45,90 @@ struct NormGrad {
     int32_t chunks, stride;
 };
 
+// VE values as they lie in memory.  No alignment is asked of rows (a row of odd width starts anywhere): the memory pipe takes wide
+// accesses at any address.  kTail: the last piece of a row may have fewer, `left` of them; what is missing reads as zero.
 template <typename T, int VE>
-__device__ __forceinline__ void load_chunk(const T* p, float (&v)[VE]) {
-    if constexpr (VE == 1) {
-        v[0] = load_f(p);
-    } else if constexpr (sizeof(T) == 4) {
-        const float4 f = *reinterpret_cast<const float4*>(p);
-        v[0] = f.x; v[1] = f.y; v[2] = f.z; v[3] = f.w;
-    } else {
-        const uint2 u = *reinterpret_cast<const uint2*>(p);
-        v[0] = __uint_as_float(u.x << 16); v[1] = __uint_as_float(u.x & 0xffff0000u);
-        v[2] = __uint_as_float(u.y << 16); v[3] = __uint_as_float(u.y & 0xffff0000u);
+struct Piece {
+    uint32_t u[VE * sizeof(T) / 4];
+    template <bool kTail>
+    __device__ __forceinline__ void load(const T* p, int left) {
+        if (!kTail || left >= VE) {
+            __builtin_memcpy(u, p, sizeof(u));
+        } else {
+            T t[VE];
+#pragma unroll
+            for (int e = 0; e < VE; ++e) t[e] = e < left ? p[e] : T{};
+            __builtin_memcpy(u, t, sizeof(u));
+        }
+    }
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (uint32_t& w : u) w = 0;
+    }
+    __device__ __forceinline__ float at(int e) const {
+        if constexpr (sizeof(T) == 4) return __uint_as_float(u[e]);
+        else return __uint_as_float(e % 2 == 0 ? u[e / 2] << 16 : u[e / 2] & 0xffff0000u);
+    }
+};
+
+template <bool kTail, int VE>
+__device__ __forceinline__ void load_vector(const float* p, int left, float (&v)[VE]) {
+#pragma unroll
+    for (int k = 0; k < VE; k += 4) {
+        Piece<float, 4> q;
+        q.load<kTail>(p + k, left - k);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[k + e] = q.at(e);
     }
 }
 
-template <typename T, int VE>
-__device__ __forceinline__ void store_chunk(T* p, const float (&v)[VE]) {
-    if constexpr (VE == 1) store_f(p, v[0]);
-    else if constexpr (sizeof(T) == 4) *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
-    else *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16_pair(v[0], v[1]), pack_bf16_pair(v[2], v[3]));
-}
-
-// The sum over the WPR wavefronts of a row, in every lane.  slot: WPR floats of LDS.  A kernel uses two or more slots in turn: between
-// the read of one and its next write lies the barrier of another.
-template <int WPR>
-__device__ __forceinline__ float row_sum(float v, float* slot, int wave_in_row) {
-    v = wave_sum(v);
-    if constexpr (WPR == 1) return v;
-    if ((threadIdx.x & 63) == 0) slot[wave_in_row] = v;
-    __syncthreads();
-    float s = slot[0];
+template <bool kTail, typename T, int VE>
+__device__ __forceinline__ void store_piece(T* p, int left, const float (&v)[VE]) {
+    uint32_t u[VE * sizeof(T) / 4];
 #pragma unroll
-    for (int w = 1; w < WPR; ++w) s += slot[w];
-    return s;
+    for (int k = 0; k < VE * static_cast<int>(sizeof(T)) / 4; ++k) {
+        if constexpr (sizeof(T) == 4) u[k] = __float_as_uint(v[k]);
+        else u[k] = pack_bf16_pair(v[2 * k], v[2 * k + 1]);
+    }
+    if (!kTail || left >= VE) {
+        __builtin_memcpy(p, u, sizeof(u));
+    } else {
+        T t[VE];
+        __builtin_memcpy(t, u, sizeof(u));
+#pragma unroll
+        for (int e = 0; e < VE; ++e)
+            if (e < left) p[e] = t[e];
+    }
 }
 
-// Weight (nullable) of a chunk.  Requested ahead of the sums it waits for nothing but the cache.
-template <int VE>
-__device__ __forceinline__ void load_weight(const float* w, float plus, int at, float (&v)[VE]) {
+// where a lane's pieces of a row lie: piece c at first + c * kStep
+template <int VE, int NV, int WPR>
+struct Place {
+    static constexpr int kStep = WPR * 64 * VE;
+    int first, D;
+    float values;                // of the row in this wavefront
+    __device__ __forceinline__ Place(int wave_in_row, int D_) : first((wave_in_row * 64 + (threadIdx.x & 63)) * VE), D(D_) {
+        values = static_cast<float>(count(wave_in_row));
+    }
+    __device__ __forceinline__ int at(int c) const { return first + c * kStep; }
+    __device__ __forceinline__ bool has(int c) const { return at(c) < D; }
+    __device__ __forceinline__ int left(int c) const { return D - at(c); }
+    __device__ __forceinline__ int count(int w) const {          // values of the row in wavefront w
+        int n = 0;
+#pragma unroll
+        for (int c = 0; c < NV; ++c) {
+            const int k = D - (w * 64 * VE + c * kStep);
+            n += k < 0 ? 0 : k > 64 * VE ? 64 * VE : k;
+        }
+        return n;
+    }
+};
+
+// a weight (nullable) of a piece
+template <bool kTail, int VE>
+__device__ __forceinline__ void load_weight(const float* w, float plus, int at, int left, float (&v)[VE]) {
     if (w) {
-        load_chunk<float, VE>(w + at, v);
+        load_vector<kTail, VE>(w + at, left, v);
 #pragma unroll
         for (int e = 0; e < VE; ++e) v[e] += plus;
     } else {
@@ -86,46 +137,63 @@ __device__ __forceinline__ void load_weight(const float* w, float plus, int at, 
     }
 }
 
-// One row per group of WPR wavefronts, NV chunks of VE values per lane.
-template <typename XT, typename OT, int VE, int NV, int WPR>
-__global__ __launch_bounds__(WPR > 4 ? WPR * 64 : kThreads) void norm_forward_kernel(NormArgs a) {
-    constexpr int kGroups = WPR > 4 ? 1 : 4 / WPR;
-    __shared__ float red[kGroups][2][WPR];
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+// Rows of WPR wavefronts, NV pieces of VE values per lane
+template <typename XT, typename OT, int VE, int NV, int WPR, bool kTail>
+__global__ __launch_bounds__(kThreads) void norm_forward_kernel(NormArgs a) {
+    constexpr int kGroups = 4 / WPR;
+    __shared__ float2 red[2][kGroups][WPR];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int group = wave / WPR, wave_in_row = wave % WPR;
-    constexpr int kStep = WPR * 64 * VE;
-    const int first = (wave_in_row * 64 + lane) * VE;
-    // every wavefront takes part in every pass (barriers in row_sum)
-    for (int64_t base = static_cast<int64_t>(blockIdx.x) * kGroups; base < a.M; base += static_cast<int64_t>(gridDim.x) * kGroups) {
+    const Place<VE, NV, WPR> at(wave_in_row, a.D);
+    int parity = 0;
+    // every wavefront takes part in every pass (barriers)
+    for (int64_t base = static_cast<int64_t>(blockIdx.x) * kGroups; base < a.M; base += static_cast<int64_t>(gridDim.x) * kGroups, parity ^= 1) {
         const bool on = base + group < a.M;
         const int64_t row = on ? base + group : base;
         const XT* x = static_cast<const XT*>(a.x) + row * a.D;
-        float v[NV][VE];
-        float s = 0.f;
+        Piece<XT, VE> raw[NV];
 #pragma unroll
         for (int c = 0; c < NV; ++c) {
-            const int at = first + c * kStep;
-            if (at < a.D) {
-                load_chunk<XT, VE>(x + at, v[c]);
-            } else {
-#pragma unroll
-                for (int e = 0; e < VE; ++e) v[c][e] = 0.f;
-            }
-#pragma unroll
-            for (int e = 0; e < VE; ++e) s += v[c][e];
+            if (at.has(c)) raw[c].template load<kTail>(x + at.at(c), at.left(c));
+            else raw[c].clear();
         }
-        const float mean = row_sum<WPR>(s, red[group][0], wave_in_row) / a.D;       // (a quotient: rows of one value have no variance)
-        float q = 0.f;
+        float v[NV][VE], s = 0.f;
 #pragma unroll
-        for (int c = 0; c < NV; ++c) {
-            const int at = first + c * kStep;
+        for (int c = 0; c < NV; ++c)
 #pragma unroll
             for (int e = 0; e < VE; ++e) {
-                v[c][e] = at < a.D ? v[c][e] - mean : 0.f;
-                q = fmaf(v[c][e], v[c][e], q);
+                v[c][e] = raw[c].at(e);
+                s += v[c][e];
             }
+        s = wave_sum(s);
+        float mean = at.values > 0.f ? s / at.values : 0.f;       // (quotients: rows of one value have no variance)
+        float q = 0.f;
+#pragma unroll
+        for (int c = 0; c < NV; ++c)
+#pragma unroll
+            for (int e = 0; e < VE; ++e) {
+                v[c][e] -= mean;
+                const float d = at.has(c) && (!kTail || e < at.left(c)) ? v[c][e] : 0.f;
+                q = fmaf(d, d, q);
+            }
+        q = wave_sum(q);
+        float shift = 0.f;                                        // the wavefront's mean, off the row's
+        if constexpr (WPR > 1) {
+            if ((threadIdx.x & 63) == 0) red[parity][group][wave_in_row] = make_float2(s, q);
+            __syncthreads();
+            float total = 0.f, sq = 0.f;
+#pragma unroll
+            for (int w = 0; w < WPR; ++w) total += red[parity][group][w].x;
+            const float row_mean = total / a.D;
+#pragma unroll
+            for (int w = 0; w < WPR; ++w) {
+                const float n = static_cast<float>(at.count(w)), d = n > 0.f ? red[parity][group][w].x / n - row_mean : 0.f;
+                sq += fmaf(n * d, d, red[parity][group][w].y);
+            }
+            shift = mean - row_mean;
+            q = sq;
         }
-        const float r = 1.0f / sqrtf(row_sum<WPR>(q, red[group][1], wave_in_row) * a.inv_d + a.eps);
+        const float r = 1.0f / sqrtf(q * a.inv_d + a.eps);
         if (!on) continue;
         const int64_t sample = row / a.rows_per_sample;
         const float* w = a.weight ? a.weight + sample * a.stride : nullptr;
@@ -133,109 +201,153 @@ __global__ __launch_bounds__(WPR > 4 ? WPR * 64 : kThreads) void norm_forward_ke
         OT* out = static_cast<OT*>(a.out) + row * a.D;
 #pragma unroll
         for (int c = 0; c < NV; ++c) {
-            const int at = first + c * kStep;
-            if (at >= a.D) continue;
+            if (!at.has(c)) continue;
             float wv[VE], bv[VE], o[VE];
-            load_weight<VE>(w, a.plus, at, wv);
+            load_weight<kTail, VE>(w, a.plus, at.at(c), at.left(c), wv);
             if (b) {
-                load_chunk<float, VE>(b + at, bv);
+                load_vector<kTail, VE>(b + at.at(c), at.left(c), bv);
             } else {
 #pragma unroll
                 for (int e = 0; e < VE; ++e) bv[e] = 0.f;
             }
 #pragma unroll
-            for (int e = 0; e < VE; ++e) o[e] = fmaf(v[c][e] * r, wv[e], bv[e]);
-            store_chunk<OT, VE>(out + at, o);
+            for (int e = 0; e < VE; ++e) o[e] = fmaf((v[c][e] + shift) * r, wv[e], bv[e]);
+            store_piece<kTail, OT, VE>(out + at.at(c), at.left(c), o);
         }
     }
 }
 
 // Workgroup (sample, chunk): rows chunk * groups + group, + chunks * groups, ... of the sample.
-template <typename XT, typename OT, int VE, int NV, int WPR>
-__global__ __launch_bounds__(WPR > 4 ? WPR * 64 : kThreads) void norm_backward_kernel(NormArgs a, NormGrad gr, int32_t chunks) {
-    constexpr int kGroups = WPR > 4 ? 1 : 4 / WPR;
-    __shared__ float red[kGroups][4][WPR];
+template <typename XT, typename OT, int VE, int NV, int WPR, bool kTail>
+__global__ __launch_bounds__(back_waves(WPR) * 64) void norm_backward_kernel(NormArgs a, NormGrad gr, int32_t chunks) {
+    constexpr int kGroups = back_waves(WPR) / WPR;
+    constexpr bool kHoldWeight = NV * VE <= 20;           // as registers allow; otherwise read again for every row, from the L1
+    __shared__ float4 red[2][kGroups][WPR];
     extern __shared__ float cols[];                       // [2][D]: column sums of the workgroup (kGroups > 1)
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int group = wave / WPR, wave_in_row = wave % WPR;
     const int sample = blockIdx.x / chunks, chunk = blockIdx.x % chunks;
     const int64_t row0 = static_cast<int64_t>(sample) * a.rows_per_sample;
-    const int rows = static_cast<int>(row0 + a.rows_per_sample < a.M ? a.rows_per_sample : a.M - row0);
+    const int64_t rows = row0 + a.rows_per_sample < a.M ? a.rows_per_sample : a.M - row0;
     const float* w = a.weight ? a.weight + static_cast<int64_t>(sample) * a.stride : nullptr;
-    const int first = (wave_in_row * 64 + lane) * VE;
-    constexpr int kStep = WPR * 64 * VE;
-    float dw[NV][VE], db[NV][VE];
+    const Place<VE, NV, WPR> at(wave_in_row, a.D);
+    float dw[NV][VE], db[NV][VE], held[kHoldWeight ? NV : 1][VE];
 #pragma unroll
     for (int c = 0; c < NV; ++c)
 #pragma unroll
         for (int e = 0; e < VE; ++e) dw[c][e] = db[c][e] = 0.f;
-    for (int64_t base = chunk * kGroups; base < rows; base += chunks * kGroups) {
-        const bool on = base + group < rows;
-        const int64_t row = row0 + (on ? base + group : base);
-        const XT* x = static_cast<const XT*>(a.x) + row * a.D;
-        const OT* dy = static_cast<const OT*>(a.dy) + row * a.D;
-        float v[NV][VE], g[NV][VE];
-        float s = 0.f;
+    if constexpr (kHoldWeight) {
 #pragma unroll
         for (int c = 0; c < NV; ++c) {
-            const int at = first + c * kStep;
-            if (at < a.D) {
-                load_chunk<XT, VE>(x + at, v[c]);
-                load_chunk<OT, VE>(dy + at, g[c]);
+            if (at.has(c)) {
+                load_weight<kTail, VE>(w, a.plus, at.at(c), at.left(c), held[c]);
             } else {
 #pragma unroll
-                for (int e = 0; e < VE; ++e) v[c][e] = g[c][e] = 0.f;
+                for (int e = 0; e < VE; ++e) held[c][e] = 0.f;
             }
         }
+    }
+    Piece<XT, VE> xr[NV];
+    Piece<OT, VE> gradr[NV];
+    const auto request = [&](int64_t base) {              // this group's row of a pass, the pass's first where there is none
+        const int64_t row = row0 + (base + group < rows ? base + group : base);
+        const XT* x = static_cast<const XT*>(a.x) + row * a.D;
+        const OT* dy = static_cast<const OT*>(a.dy) + row * a.D;
+#pragma unroll
+        for (int c = 0; c < NV; ++c) {
+            if (at.has(c)) {
+                xr[c].template load<kTail>(x + at.at(c), at.left(c));
+                gradr[c].template load<kTail>(dy + at.at(c), at.left(c));
+            } else {
+                xr[c].clear();
+                gradr[c].clear();
+            }
+        }
+    };
+    const int64_t step = static_cast<int64_t>(chunks) * kGroups;
+    const int64_t start = static_cast<int64_t>(chunk) * kGroups;
+    if (start < rows) request(start);
+    int parity = 0;
+    for (int64_t base = start; base < rows; base += step, parity ^= 1) {
+        const bool on = base + group < rows;
+        float v[NV][VE], g[NV][VE], s = 0.f;
 #pragma unroll
         for (int c = 0; c < NV; ++c)
 #pragma unroll
-            for (int e = 0; e < VE; ++e) s += v[c][e];
-        const float mean = row_sum<WPR>(s, red[group][0], wave_in_row) / a.D;       // (a quotient: rows of one value have no variance)
-        float q = 0.f;
+            for (int e = 0; e < VE; ++e) {
+                v[c][e] = xr[c].at(e);
+                g[c][e] = gradr[c].at(e);
+                s += v[c][e];
+            }
+        if (base + step < rows) request(base + step);
+        s = wave_sum(s);
+        const float mean = at.values > 0.f ? s / at.values : 0.f;
+        float q = 0.f, sg = 0.f, sgx = 0.f;
 #pragma unroll
         for (int c = 0; c < NV; ++c) {
-            const int at = first + c * kStep;
+            float wv[VE];
+            if constexpr (kHoldWeight) {
+#pragma unroll
+                for (int e = 0; e < VE; ++e) wv[e] = held[c][e];
+            } else if (at.has(c)) {
+                load_weight<kTail, VE>(w, a.plus, at.at(c), at.left(c), wv);
+            } else {
+#pragma unroll
+                for (int e = 0; e < VE; ++e) wv[e] = 0.f;
+            }
 #pragma unroll
             for (int e = 0; e < VE; ++e) {
-                v[c][e] = at < a.D ? v[c][e] - mean : 0.f;
+                v[c][e] = at.has(c) && (!kTail || e < at.left(c)) ? v[c][e] - mean : 0.f;
                 q = fmaf(v[c][e], v[c][e], q);
+                const float gw = g[c][e] * wv[e];
+                sg += gw;
+                sgx = fmaf(gw, v[c][e], sgx);
             }
         }
-        const float r = 1.0f / sqrtf(row_sum<WPR>(q, red[group][1], wave_in_row) * a.inv_d + a.eps);
-        float s1 = 0.f, s2 = 0.f;
+        q = wave_sum(q);
+        sg = wave_sum(sg);
+        sgx = wave_sum(sgx);
+        float shift = 0.f;
+        if constexpr (WPR > 1) {
+            if ((threadIdx.x & 63) == 0) red[parity][group][wave_in_row] = make_float4(s, q, sg, sgx);
+            __syncthreads();
+            float total = 0.f;
+#pragma unroll
+            for (int k = 0; k < WPR; ++k) total += red[parity][group][k].x;
+            const float row_mean = total / a.D;
+            q = sg = sgx = 0.f;
+#pragma unroll
+            for (int k = 0; k < WPR; ++k) {
+                const float4 p = red[parity][group][k];
+                const float n = static_cast<float>(at.count(k)), d = n > 0.f ? p.x / n - row_mean : 0.f;
+                q += fmaf(n * d, d, p.y);
+                sg += p.z;
+                sgx += fmaf(d, p.z, p.w);
+            }
+            shift = mean - row_mean;
+        }
+        const float r = 1.0f / sqrtf(q * a.inv_d + a.eps);
+        const float m1 = sg * a.inv_d, m2 = r * sgx * a.inv_d;
+        if (!on) continue;
+        XT* dx = static_cast<XT*>(a.out) + (row0 + base + group) * a.D;
 #pragma unroll
         for (int c = 0; c < NV; ++c) {
-            const int at = first + c * kStep;
-            if (at < a.D) {
-                float wv[VE];
-                load_weight<VE>(w, a.plus, at, wv);
+            if (!at.has(c)) continue;
+            float wv[VE], o[VE];
+            if constexpr (kHoldWeight) {
 #pragma unroll
-                for (int e = 0; e < VE; ++e) {
-                    v[c][e] *= r;
-                    if (on) {
-                        dw[c][e] = fmaf(g[c][e], v[c][e], dw[c][e]);
-                        db[c][e] += g[c][e];
-                    }
-                    g[c][e] *= wv[e];
-                    s1 += g[c][e];
-                    s2 = fmaf(g[c][e], v[c][e], s2);
-                }
+                for (int e = 0; e < VE; ++e) wv[e] = held[c][e];
+            } else {
+                load_weight<kTail, VE>(w, a.plus, at.at(c), at.left(c), wv);
             }
-        }
-        const float m1 = row_sum<WPR>(s1, red[group][2], wave_in_row) * a.inv_d;
-        const float m2 = row_sum<WPR>(s2, red[group][3], wave_in_row) * a.inv_d;
-        if (on) {
-            XT* dx = static_cast<XT*>(a.out) + row * a.D;
 #pragma unroll
-            for (int c = 0; c < NV; ++c) {
-                const int at = first + c * kStep;
-                if (at >= a.D) continue;
-                float o[VE];
-#pragma unroll
-                for (int e = 0; e < VE; ++e) o[e] = r * (g[c][e] - m1 - v[c][e] * m2);
-                store_chunk<XT, VE>(dx + at, o);
+            for (int e = 0; e < VE; ++e) {
+                const float xh = (v[c][e] + shift) * r;
+                dw[c][e] = fmaf(g[c][e], xh, dw[c][e]);
+                db[c][e] += g[c][e];
+                o[e] = r * (g[c][e] * wv[e] - m1 - xh * m2);
             }
+            store_piece<kTail, XT, VE>(dx + at.at(c), at.left(c), o);
         }
     }
     if (gr.dw == nullptr) return;
@@ -248,17 +360,17 @@ __global__ __launch_bounds__(WPR > 4 ? WPR * 64 : kThreads) void norm_backward_k
             if (group != k) continue;
 #pragma unroll
             for (int c = 0; c < NV; ++c) {
-                const int at = first + c * kStep;
-                if (at >= a.D) continue;
 #pragma unroll
                 for (int e = 0; e < VE; ++e) {
+                    const int i = at.at(c) + e;
+                    if (i >= a.D) continue;
                     if (k > 0) {
-                        dw[c][e] += cols[at + e];
-                        db[c][e] += cols[a.D + at + e];
+                        dw[c][e] += cols[i];
+                        db[c][e] += cols[a.D + i];
                     }
                     if (k < kGroups - 1) {
-                        cols[at + e] = dw[c][e];
-                        cols[a.D + at + e] = db[c][e];
+                        cols[i] = dw[c][e];
+                        cols[a.D + i] = db[c][e];
                     }
                 }
             }
@@ -267,31 +379,44 @@ __global__ __launch_bounds__(WPR > 4 ? WPR * 64 : kThreads) void norm_backward_k
     }
 #pragma unroll
     for (int c = 0; c < NV; ++c) {
-        const int at = first + c * kStep;
-        if (at >= a.D) continue;
-#pragma unroll
-        for (int e = 0; e < VE; ++e) {
-            pw[at + e] = dw[c][e];
-            pb[at + e] = db[c][e];
-        }
+        if (!at.has(c)) continue;
+        store_piece<kTail, float, VE>(pw + at.at(c), at.left(c), dw[c]);
+        store_piece<kTail, float, VE>(pb + at.at(c), at.left(c), db[c]);
     }
 }
 
-// dw, db [sample] = the partial rows of its chunks, added: 64 columns x 16 threads per workgroup, each thread every 16th chunk.
-constexpr int kJoinRows = 16;
-__global__ __launch_bounds__(64 * kJoinRows) void norm_join_kernel(NormGrad gr, int32_t D) {
+// dw, db [sample] = the partial rows of its chunks, added: 64 columns per workgroup, 16 lanes of four columns, 64 threads per column that
+// take every 64th chunk each, then 16 that add four of those, then one.
+constexpr int kJoinRows = 64;
+__global__ __launch_bounds__(16 * kJoinRows) void norm_join_kernel(NormGrad gr, int32_t D) {
     __shared__ float red[kJoinRows][64];
-    const int col = blockIdx.x * 64 + threadIdx.x % 64, k = threadIdx.x / 64, which = blockIdx.y;
+    const int x = threadIdx.x % 16, k = threadIdx.x / 16, which = blockIdx.y;
     const int64_t sample = blockIdx.z;
-    float s = 0.f;
-    if (col < D)
-        for (int c = k; c < gr.chunks; c += kJoinRows) s += gr.part[((sample * gr.chunks + c) * 2 + which) * D + col];
-    red[k][threadIdx.x % 64] = s;
-    __syncthreads();
-    if (k != 0 || col >= D) return;
+    const int col = blockIdx.x * 64 + x * 4, left = D - col;
+    float s[4] = {0.f, 0.f, 0.f, 0.f};
+    if (left > 0) {
+        const float* p = gr.part + (sample * gr.chunks * 2 + which) * D + col;
+#pragma unroll 4
+        for (int c = k; c < gr.chunks; c += kJoinRows) {
+            Piece<float, 4> q;
+            q.load<true>(p + static_cast<int64_t>(c) * 2 * D, left);
 #pragma unroll
-    for (int j = 1; j < kJoinRows; ++j) s += red[j][threadIdx.x];
-    (which == 0 ? gr.dw : gr.db)[sample * gr.stride + col] = s;
+            for (int e = 0; e < 4; ++e) s[e] += q.at(e);
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) red[k][x * 4 + e] = s[e];
+    __syncthreads();
+    const int c = threadIdx.x % 64, r = threadIdx.x / 64;
+    const float part = ((red[r][c] + red[r + 16][c]) + red[r + 32][c]) + red[r + 48][c];
+    __syncthreads();
+    red[r][c] = part;
+    __syncthreads();
+    if (r != 0 || blockIdx.x * 64 + c >= D) return;
+    float total = red[0][c];
+#pragma unroll
+    for (int j = 1; j < 16; ++j) total += red[j][c];
+    (which == 0 ? gr.dw : gr.db)[sample * gr.stride + blockIdx.x * 64 + c] = total;
 }
 
 __global__ __launch_bounds__(kThreads) void norm_zero_kernel(NormGrad gr, int32_t D) {
@@ -299,81 +424,88 @@ __global__ __launch_bounds__(kThreads) void norm_zero_kernel(NormGrad gr, int32_
     if (col < D) gr.dw[col] = gr.db[col] = 0.f;
 }
 
-// Values per lane: the smallest row layout that holds D.  A lane holds up to 32 values in the backward pass (x, dy and two column sums
-// of each are 128 registers), so wider rows take more wavefronts.
+// The layouts of a row: pieces of 16 bytes of the wider of the two types (VE values), NV per lane, over WPR wavefronts.  Forward: one
+// wavefront up to 4096 values (64 registers), no exchange between wavefronts.  Backward: x, dy and the two column sums of every value are
+// in registers, so 20 to 32 values per lane.
 struct Layout {
-    int ve, nv, wpr;
+    int nv, wpr;
 };
-Layout layout_of(int32_t D, bool vec) {
-    const int per_wave = (D + 63) / 64;
-    if (vec) {
-        const int n = (D / 4 + 63) / 64;                              // 16-byte chunks per lane of one wavefront
-        if (n <= 1) return {4, 1, 1};
-        if (n <= 2) return {4, 2, 1};
-        if (n <= 5) return {4, 5, 1};
-        if (n <= 10) return {4, 5, 2};
-        if (n <= 20) return {4, 5, 4};
-        if (n <= 32) return {4, 8, 4};
-        return {4, 8, 8};
-    }
-    if (per_wave <= 8) return {1, 8, 1};
-    if (per_wave <= 32) return {1, 16, 2};
-    if (per_wave <= 64) return {1, 16, 4};
-    if (per_wave <= 128) return {1, 16, 8};
-    return {1, 16, 16};
-}
-constexpr int kMaxWidth = 64 * 16 * 16;
+constexpr int kMaxWidth = 16384;
 constexpr int kMaxBlocks = 1 << 22;                                    // grids of less than 2^32 threads
 
-#define FREE_NORM_LAYOUTS(CASE) \
-    CASE(4, 1, 1) CASE(4, 2, 1) CASE(4, 5, 1) CASE(4, 5, 2) CASE(4, 5, 4) CASE(4, 8, 4) CASE(4, 8, 8) \
-    CASE(1, 8, 1) CASE(1, 16, 2) CASE(1, 16, 4) CASE(1, 16, 8) CASE(1, 16, 16)
+#define FREE_NORM_FORWARD_4(CASE) CASE(4, 1, 1) CASE(4, 2, 1) CASE(4, 3, 1) CASE(4, 5, 1) CASE(4, 8, 1) CASE(4, 16, 1) CASE(4, 16, 4)
+#define FREE_NORM_FORWARD_8(CASE) CASE(8, 1, 1) CASE(8, 2, 1) CASE(8, 3, 1) CASE(8, 4, 1) CASE(8, 8, 1) CASE(8, 8, 4)
+#define FREE_NORM_BACKWARD_4(CASE) CASE(4, 1, 1) CASE(4, 2, 1) CASE(4, 3, 1) CASE(4, 5, 1) CASE(4, 4, 2) CASE(4, 5, 2) CASE(4, 4, 4) CASE(4, 5, 4) CASE(4, 8, 4) CASE(4, 8, 8)
+#define FREE_NORM_BACKWARD_8(CASE) CASE(8, 1, 1) CASE(8, 2, 1) CASE(8, 2, 2) CASE(8, 2, 4) CASE(8, 2, 8) CASE(8, 4, 8)
+
+// the first of the list that holds D
+#define FREE_FIRST(VE, NV, WPR) if (64 * VE * NV * WPR >= D) return Layout{NV, WPR};
+Layout forward_layout(int ve, int32_t D) {
+    if (ve == 8) { FREE_NORM_FORWARD_8(FREE_FIRST) } else { FREE_NORM_FORWARD_4(FREE_FIRST) }
+    return {0, 0};
+}
+Layout backward_layout(int ve, int32_t D) {
+    if (ve == 8) { FREE_NORM_BACKWARD_8(FREE_FIRST) } else { FREE_NORM_BACKWARD_4(FREE_FIRST) }
+    return {0, 0};
+}
+#undef FREE_FIRST
 
 template <typename XT, typename OT>
-int32_t forward_of(const NormArgs& a, const Layout& l, hipStream_t s) {
-    const int groups = l.wpr > 4 ? 1 : 4 / l.wpr, threads = l.wpr > 4 ? l.wpr * 64 : kThreads;
-    const int blocks = static_cast<int>(std::min<int64_t>((static_cast<int64_t>(a.M) + groups - 1) / groups, kMaxBlocks));
-#define FREE_CASE(VE, NV, WPR)                                                                                              \
-    if (l.ve == VE && l.nv == NV && l.wpr == WPR) {                                                                         \
-        hipLaunchKernelGGL((norm_forward_kernel<XT, OT, VE, NV, WPR>), dim3(blocks), dim3(threads), 0, s, a);               \
-        return launch_ok() ? FREE_OK : FREE_ERR_HIP;                                                                        \
+constexpr int kPiece = sizeof(XT) == 2 && sizeof(OT) == 2 ? 8 : 4;
+
+template <typename XT, typename OT>
+int32_t forward_of(const NormArgs& a, hipStream_t s) {
+    constexpr int VEC = kPiece<XT, OT>;
+    const Layout l = forward_layout(VEC, a.D);
+    const int groups = 4 / l.wpr;
+    const dim3 grid(static_cast<uint32_t>(std::min<int64_t>((static_cast<int64_t>(a.M) + groups - 1) / groups, kMaxBlocks))), block(kThreads);
+#define FREE_CASE(VE, NV, WPR)                                                                                                       \
+    if (l.nv == NV && l.wpr == WPR) {                                                                                                \
+        if (a.D % VE == 0) hipLaunchKernelGGL((norm_forward_kernel<XT, OT, VE, NV, WPR, false>), grid, block, 0, s, a);              \
+        else hipLaunchKernelGGL((norm_forward_kernel<XT, OT, VE, NV, WPR, true>), grid, block, 0, s, a);                             \
+        return launch_ok() ? FREE_OK : FREE_ERR_HIP;                                                                                 \
     }
-    FREE_NORM_LAYOUTS(FREE_CASE)
+    if constexpr (VEC == 8) { FREE_NORM_FORWARD_8(FREE_CASE) } else { FREE_NORM_FORWARD_4(FREE_CASE) }
 #undef FREE_CASE
     return FREE_ERR_SHAPE;
 }
 
 template <typename XT, typename OT>
-int32_t backward_of(const NormArgs& a, const NormGrad& gr, int samples, const Layout& l, hipStream_t s) {
-    const int threads = l.wpr > 4 ? l.wpr * 64 : kThreads;
-    const size_t lds = l.wpr >= 4 || gr.dw == nullptr ? 0 : static_cast<size_t>(2) * a.D * sizeof(float);
-#define FREE_CASE(VE, NV, WPR)                                                                                              \
-    if (l.ve == VE && l.nv == NV && l.wpr == WPR) {                                                                         \
-        hipLaunchKernelGGL((norm_backward_kernel<XT, OT, VE, NV, WPR>), dim3(samples * gr.chunks), dim3(threads), lds, s, a, gr, \
-                           gr.chunks);                                                                                      \
-        return launch_ok() ? FREE_OK : FREE_ERR_HIP;                                                                        \
+int32_t backward_of(const NormArgs& a, const NormGrad& gr, int samples, hipStream_t s) {
+    constexpr int VEC = kPiece<XT, OT>;
+    const Layout l = backward_layout(VEC, a.D);
+    const size_t lds = l.wpr == back_waves(l.wpr) || gr.dw == nullptr ? 0 : static_cast<size_t>(2) * a.D * sizeof(float);
+    const dim3 grid(samples * gr.chunks), block(back_waves(l.wpr) * 64);
+#define FREE_CASE(VE, NV, WPR)                                                                                                       \
+    if (l.nv == NV && l.wpr == WPR) {                                                                                                \
+        if (a.D % VE == 0) hipLaunchKernelGGL((norm_backward_kernel<XT, OT, VE, NV, WPR, false>), grid, block, lds, s, a, gr, gr.chunks); \
+        else hipLaunchKernelGGL((norm_backward_kernel<XT, OT, VE, NV, WPR, true>), grid, block, lds, s, a, gr, gr.chunks);           \
+        return launch_ok() ? FREE_OK : FREE_ERR_HIP;                                                                                 \
     }
-    FREE_NORM_LAYOUTS(FREE_CASE)
+    if constexpr (VEC == 8) { FREE_NORM_BACKWARD_8(FREE_CASE) } else { FREE_NORM_BACKWARD_4(FREE_CASE) }
 #undef FREE_CASE
     return FREE_ERR_SHAPE;
 }
 
-bool aligned(const void* p, int bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
-
-// whether rows can be read and written four values at a time
-bool vector_ok(const void* x, int xb, const void* o, int ob, const float* w, const float* b, int32_t stride, int32_t D) {
-    return D % 4 == 0 && stride % 4 == 0 && aligned(x, 4 * xb) && aligned(o, 4 * ob) && aligned(w, 16) && aligned(b, 16);
-}
-
-// Workgroups per sample in the backward pass.  Each writes a partial row of the weight's gradient and adds to what the second launch
-// reads, so no more than keep the chip busy, and none for fewer than eight rows of a group.
+// Workgroups per sample in the backward pass.  A group of wavefronts takes `passes` rows; all workgroups should run at once or in full
+// rounds (two on every compute unit), since each ends with sums over its wavefronts and a partial row of the weight's gradient that the
+// second launch reads: together some three passes.
 int chunks_of(int32_t M, int32_t D, int32_t rows_per_sample) {
     const int64_t samples = (static_cast<int64_t>(M) + rows_per_sample - 1) / rows_per_sample;
-    const int groups = std::max(1, 4 / layout_of(D, D % 4 == 0).wpr);
-    const int64_t rows = std::min<int64_t>(M, rows_per_sample);
-    const int64_t most = (rows + 8 * groups - 1) / (8 * groups);
-    const int64_t want = (1024 + samples - 1) / samples;
-    return static_cast<int>(std::max<int64_t>(1, std::min(most, want)));
+    const int wpr = backward_layout(4, D).wpr, groups = back_waves(wpr) / wpr;
+    const int64_t rows = std::min<int64_t>(M, rows_per_sample), slots = 2 * 256;
+    int64_t best = 1, best_cost = INT64_MAX;
+    for (int64_t passes = 1; passes <= 64; ++passes) {
+        const int64_t chunks = std::min<int64_t>((rows + passes * groups - 1) / (passes * groups), std::max<int64_t>(1, 2 * slots / samples));
+        const int64_t real = (rows + chunks * groups - 1) / (chunks * groups);
+        const int64_t cost = (samples * chunks + slots - 1) / slots * (real + 3);
+        if (cost < best_cost) {
+            best_cost = cost;
+            best = chunks;
+        }
+        if (chunks == 1) break;
+    }
+    return static_cast<int>(best);
 }
 
 }  // namespace
@@ -391,10 +523,8 @@ int32_t launch_norm_forward(const void* x, int32_t x_dtype, const float* weight,
                             float eps, int32_t M, int32_t D, int32_t rows_per_sample, int32_t dtype, void* out, hipStream_t s) {
     if (M == 0) return FREE_OK;
     const NormArgs a{x, nullptr, weight, bias, stride, plus_one ? 1.f : 0.f, eps, 1.0f / static_cast<float>(D), M, D, rows_per_sample, out};
-    const int xb = x_dtype == FREE_BF16 ? 2 : 4, ob = dtype == FREE_BF16 ? 2 : 4;
-    const Layout l = layout_of(D, vector_ok(x, xb, out, ob, weight, bias, stride, D));
-    if (xb == 4) return ob == 4 ? forward_of<float, float>(a, l, s) : forward_of<float, bf16_t>(a, l, s);
-    return ob == 4 ? forward_of<bf16_t, float>(a, l, s) : forward_of<bf16_t, bf16_t>(a, l, s);
+    if (x_dtype == FREE_FP32) return dtype == FREE_FP32 ? forward_of<float, float>(a, s) : forward_of<float, bf16_t>(a, s);
+    return dtype == FREE_FP32 ? forward_of<bf16_t, float>(a, s) : forward_of<bf16_t, bf16_t>(a, s);
 }
 
 int32_t launch_norm_backward(const void* dout, int32_t dtype, const void* x, int32_t x_dtype, const float* weight, int32_t stride,
@@ -410,14 +540,11 @@ int32_t launch_norm_backward(const void* dout, int32_t dtype, const void* x, int
     if (samples > kMaxBlocks) return FREE_ERR_LIMIT;
     gr.chunks = chunks_of(M, D, rows_per_sample);
     const NormArgs a{x, dout, weight, nullptr, stride, plus_one ? 1.f : 0.f, eps, 1.0f / static_cast<float>(D), M, D, rows_per_sample, dx};
-    const int xb = x_dtype == FREE_BF16 ? 2 : 4, ob = dtype == FREE_BF16 ? 2 : 4;
-    const bool vec = vector_ok(x, xb, dout, ob, weight, nullptr, weight ? stride : 0, D) && aligned(dx, 4 * xb);
-    const Layout l = layout_of(D, vec);
     int32_t st;
-    if (xb == 4) st = ob == 4 ? backward_of<float, float>(a, gr, samples, l, s) : backward_of<float, bf16_t>(a, gr, samples, l, s);
-    else st = ob == 4 ? backward_of<bf16_t, float>(a, gr, samples, l, s) : backward_of<bf16_t, bf16_t>(a, gr, samples, l, s);
+    if (x_dtype == FREE_FP32) st = dtype == FREE_FP32 ? backward_of<float, float>(a, gr, samples, s) : backward_of<float, bf16_t>(a, gr, samples, s);
+    else st = dtype == FREE_FP32 ? backward_of<bf16_t, float>(a, gr, samples, s) : backward_of<bf16_t, bf16_t>(a, gr, samples, s);
     if (st != FREE_OK || gr.chunks == 1 || dweight == nullptr) return st;
-    hipLaunchKernelGGL(norm_join_kernel, dim3((D + 63) / 64, 2, samples), dim3(64 * kJoinRows), 0, s, gr, D);
+    hipLaunchKernelGGL(norm_join_kernel, dim3((D + 63) / 64, 2, samples), dim3(16 * kJoinRows), 0, s, gr, D);
     return launch_ok() ? FREE_OK : FREE_ERR_HIP;
 }
 
