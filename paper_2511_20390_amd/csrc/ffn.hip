@@ -144,6 +144,27 @@ struct Carve {
     }
 };
 
+// bf16: the products of the two passes
+struct ForwardProducts {
+    FfnProduct up, down;
+    ForwardProducts(const Sizes& z, const bf16_t* x, const bf16_t* w_in, const bf16_t* w_out, int32_t act, bf16_t* y, float* gu, bf16_t* h, bool keep)
+        : up{keep ? FFN_GATE_KEEP : FFN_GATE, x, w_in, z.Dp, z.Dp, z.M, z.Fp, z.Dp, h, z.Fp, gu, act},
+          down{FFN_ROWS, h, w_out, z.Fp, z.Fp, z.M, z.Dp, z.Fp, y, z.Dp} {}
+    size_t room() const { return std::max(ffn_products_part_bytes(&up, 1), ffn_products_part_bytes(&down, 1)); }
+};
+
+struct BackwardProducts {
+    FfnProduct gate, rows, weights[2];
+    BackwardProducts(const Sizes& z, const bf16_t* dy, const bf16_t* x, const bf16_t* w_in, const bf16_t* w_out, float* gu, const bf16_t* h,
+                     int32_t act, bf16_t* dgu, bf16_t* dx, bf16_t* dw_in, bf16_t* dw_out)
+        : gate{FFN_GATE_GRAD, dy, w_out, z.Dp, z.Fp, z.M, z.Fp, z.Dp, dgu, 2 * z.Fp, gu, act},
+          rows{FFN_ROWS_BY_K, dgu, w_in, 2 * z.Fp, z.Dp, z.M, z.Dp, 2 * z.Fp, dx, z.Dp},
+          weights{{FFN_K_BY_K, dgu, x, 2 * z.Fp, z.Dp, 2 * z.Fp, z.Dp, z.M, dw_in, z.Dp}, {FFN_K_BY_K, dy, h, z.Dp, z.Fp, z.Dp, z.Fp, z.M, dw_out, z.Fp}} {}
+    size_t room() const {
+        return std::max({ffn_products_part_bytes(&gate, 1), ffn_products_part_bytes(&rows, 1), ffn_products_part_bytes(weights, 2)});
+    }
+};
+
 template <typename T>
 struct Saved {
     float* gu;
@@ -160,13 +181,14 @@ struct Saved {
 template <typename T>
 struct ForwardSpace {
     T *x, *w_in, *w_out, *y, *h;
-    float *gu, *zero;
+    float *gu, *room;            // room: bf16 the parts of a product, fp32 a bias of zeros
     size_t bytes;
     ForwardSpace(const Sizes& z, char* base) {
         Carve c{base};
         gu = c.take<float>(z.es == 4 ? z.gu_bytes() : 0);
         h = c.take<T>(z.act_bytes(z.Fp));
-        zero = c.take<float>(z.es == 4 ? sizeof(float) * std::max(2 * z.Fp, z.Dp) : 0);
+        room = c.take<float>(z.es == 4 ? sizeof(float) * std::max(2 * z.Fp, z.Dp)
+                                       : ForwardProducts(z, nullptr, nullptr, nullptr, 0, nullptr, nullptr, nullptr, false).room());
         x = w_in = w_out = y = nullptr;
         if (z.padded) {
             x = c.take<T>(z.act_bytes(z.Dp));
@@ -181,15 +203,16 @@ struct ForwardSpace {
 template <typename T>
 struct BackwardSpace {
     T *dgu, *x, *dy, *w_in, *w_out, *dx, *dw_in, *dw_out;
-    float *dh, *zero, *t1, *t2;
+    float *dh, *room, *t1, *t2;
     size_t bytes;
     BackwardSpace(const Sizes& z, char* base) {
         Carve c{base};
         dgu = c.take<T>(z.act_bytes(2 * z.Fp));
-        dh = zero = t1 = t2 = nullptr;
+        dh = t1 = t2 = nullptr;
+        room = c.take<float>(z.es == 4 ? sizeof(float) * std::max(2 * z.Fp, z.Dp)
+                                       : BackwardProducts(z, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, 0, nullptr, nullptr, nullptr, nullptr).room());
         if (z.es == 4) {
             dh = c.take<float>(z.act_bytes(z.Fp));
-            zero = c.take<float>(sizeof(float) * std::max(2 * z.Fp, z.Dp));
             // transposed factors: a weight, or two of rows Mk
             t1 = c.take<float>(std::max(z.weight_bytes(2), static_cast<size_t>(z.Mk) * std::max(2 * z.Fp, z.Dp) * 4));
             t2 = c.take<float>(static_cast<size_t>(z.Mk) * std::max(z.Fp, z.Dp) * 4);
@@ -227,11 +250,10 @@ int32_t product_f32(const float* X, const float* W, const float* zero, int32_t M
 }
 
 int32_t products_forward(const Sizes& z, const bf16_t* x, const bf16_t* w_in, const bf16_t* w_out, int32_t act, bf16_t* y, float* gu,
-                         bf16_t* h, bool keep, float*, hipStream_t s) {
-    const FfnProduct up{keep ? FFN_GATE_KEEP : FFN_GATE, x, w_in, z.Dp, z.Dp, z.M, z.Fp, z.Dp, h, z.Fp, gu, act};
-    FREE_STEP(launch_ffn_products(&up, 1, s));
-    const FfnProduct down{FFN_ROWS, h, w_out, z.Fp, z.Fp, z.M, z.Dp, z.Fp, y, z.Dp};
-    return launch_ffn_products(&down, 1, s);
+                         bf16_t* h, bool keep, float* room, hipStream_t s) {
+    const ForwardProducts p(z, x, w_in, w_out, act, y, gu, h, keep);
+    FREE_STEP(launch_ffn_products(&p.up, 1, room, s));
+    return launch_ffn_products(&p.down, 1, room, s);
 }
 
 int32_t products_forward(const Sizes& z, const float* x, const float* w_in, const float* w_out, int32_t act, float* y, float* gu, float* h,
@@ -246,33 +268,29 @@ int32_t products_forward(const Sizes& z, const float* x, const float* w_in, cons
 
 int32_t products_backward(const Sizes& z, const bf16_t* dy, const bf16_t* x, const bf16_t* w_in, const bf16_t* w_out, const Saved<bf16_t>& kept,
                           int32_t act, const BackwardSpace<bf16_t>& w, bf16_t* dx, bf16_t* dw_in, bf16_t* dw_out, hipStream_t s) {
-    const int32_t F2 = 2 * z.Fp;
-    const FfnProduct gate{FFN_GATE_GRAD, dy, w_out, z.Dp, z.Fp, z.M, z.Fp, z.Dp, w.dgu, F2, kept.gu, act};
-    FREE_STEP(launch_ffn_products(&gate, 1, s));
-    const FfnProduct rows{FFN_ROWS_BY_K, w.dgu, w_in, F2, z.Dp, z.M, z.Dp, F2, dx, z.Dp};
-    FREE_STEP(launch_ffn_products(&rows, 1, s));
-    const FfnProduct weights[2] = {{FFN_K_BY_K, w.dgu, x, F2, z.Dp, F2, z.Dp, z.M, dw_in, z.Dp},
-                                   {FFN_K_BY_K, dy, kept.h, z.Dp, z.Fp, z.Dp, z.Fp, z.M, dw_out, z.Fp}};
-    return launch_ffn_products(weights, 2, s);
+    const BackwardProducts p(z, dy, x, w_in, w_out, kept.gu, kept.h, act, w.dgu, dx, dw_in, dw_out);
+    FREE_STEP(launch_ffn_products(&p.gate, 1, w.room, s));
+    FREE_STEP(launch_ffn_products(&p.rows, 1, w.room, s));
+    return launch_ffn_products(p.weights, 2, w.room, s);
 }
 
 int32_t products_backward(const Sizes& z, const float* dy, const float* x, const float* w_in, const float* w_out, const Saved<float>& kept,
                           int32_t act, const BackwardSpace<float>& w, float* dx, float* dw_in, float* dw_out, hipStream_t s) {
     const int32_t F2 = 2 * z.Fp;
-    FREE_STEP(fit(x, 0, 0, w.zero, 1, std::max(F2, z.Dp), s));
+    FREE_STEP(fit(x, 0, 0, w.room, 1, std::max(F2, z.Dp), s));
     FREE_STEP(transpose(w_out, z.Dp, z.Fp, w.t1, z.Dp, s));
-    FREE_STEP(product_f32(dy, w.t1, w.zero, z.M, z.Fp, z.Dp, w.dh, s));
+    FREE_STEP(product_f32(dy, w.t1, w.room, z.M, z.Fp, z.Dp, w.dh, s));
     const int64_t total4 = static_cast<int64_t>(z.M) * z.Fp / 4;
     hipLaunchKernelGGL(ffn_gate_grad_kernel, dim3(grid_of(total4)), dim3(kThreads), 0, s, kept.gu, w.dh, total4, z.Fp, act, w.dgu);
     if (!launch_ok()) return FREE_ERR_HIP;
     FREE_STEP(transpose(w_in, F2, z.Dp, w.t1, F2, s));
-    FREE_STEP(product_f32(w.dgu, w.t1, w.zero, z.M, z.Dp, F2, dx, s));
+    FREE_STEP(product_f32(w.dgu, w.t1, w.room, z.M, z.Dp, F2, dx, s));
     FREE_STEP(transpose(w.dgu, z.M, F2, w.t1, z.Mk, s));
     FREE_STEP(transpose(x, z.M, z.Dp, w.t2, z.Mk, s));
-    FREE_STEP(product_f32(w.t1, w.t2, w.zero, F2, z.Dp, z.Mk, dw_in, s));
+    FREE_STEP(product_f32(w.t1, w.t2, w.room, F2, z.Dp, z.Mk, dw_in, s));
     FREE_STEP(transpose(dy, z.M, z.Dp, w.t1, z.Mk, s));
     FREE_STEP(transpose(kept.h, z.M, z.Fp, w.t2, z.Mk, s));
-    return product_f32(w.t1, w.t2, w.zero, z.Dp, z.Fp, z.Mk, dw_out, s);
+    return product_f32(w.t1, w.t2, w.room, z.Dp, z.Fp, z.Mk, dw_out, s);
 }
 
 template <typename T>
@@ -295,7 +313,7 @@ int32_t forward_of(const Sizes& z, const T* x, const T* w_in, const T* w_out, in
         w_out = w.w_out;
         y = w.y;
     }
-    FREE_STEP(products_forward(z, x, w_in, w_out, act, y, gu, h, saved != nullptr, w.zero, s));
+    FREE_STEP(products_forward(z, x, w_in, w_out, act, y, gu, h, saved != nullptr, w.room, s));
     return z.padded ? fit(y, z.M, z.Dp, out, z.M, z.D, s) : FREE_OK;
 }
 

@@ -30,8 +30,10 @@ struct FfnProduct {
     bool gated() const { return kind == FFN_GATE || kind == FFN_GATE_KEEP; }
 };
 
-// one launch for n products (1, or 2 of the same kind)
-int32_t launch_ffn_products(const FfnProduct* p, int n, hipStream_t s);
+// One launch for n products (1, or 2 FFN_K_BY_K), or, where their sums over K are cut in parts, one more for each that joins them; part: room of
+// ffn_products_part_bytes (by the sizes alone).
+size_t ffn_products_part_bytes(const FfnProduct* p, int n);
+int32_t launch_ffn_products(const FfnProduct* p, int n, float* part, hipStream_t s);
 
 // ffn_rows.hip: y of up to kFfnFewRows token rows, any D and F, in two launches; h: room for [M, F]
 constexpr int32_t kFfnFewRows = 64;

@@ -33,9 +33,9 @@ struct Problem {
     int64_t ldx, ldw;            // values from row to row (K-major: from k to k)
     int32_t M, N, K;             // N: of the hidden values for the gated epilogues
     int32_t tiles_m, tiles_n, group_m;
-    int32_t splits, split_slices;
+    int32_t split_slices;        // slices of a part of K (all, or those of one of several)
     bf16_t* out;                 // [M, N], ldo values from row to row; gated gradient: dg, du n_gate values further
-    float* part;                 // sums over a part of K: [splits][32 x 32 block][lane][16]
+    float* part;                 // sums over a part of K: [part][32 x 32 block][4][lane][4]
     float* gu;                   // kept g, u: [32 x 32 block][2][4][lane][4]
     int64_t ldo;
     int32_t act;
@@ -381,29 +381,72 @@ __global__ __launch_bounds__(512) void ffn_product_kernel(Launch la) {
     }
 }
 
-// C = the parts, added in order: a wavefront per 32 x 32 block
-__global__ __launch_bounds__(256) void ffn_join_kernel(const float* part, int32_t splits, int32_t M, int32_t N, bf16_t* out) {
-    const int blocks_n = (N + 31) / 32;
-    const int64_t blocks = static_cast<int64_t>((M + 31) / 32) * blocks_n;
-    const int64_t block = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
-    if (block >= blocks) return;
+// The parts of a product's sums over K, added in order, and the epilogue they were left without; a wavefront per 32 x 32 block of the
+// result.  Blocks of g | u: block_n and block_n + N / 32.
+struct Join {
+    const float* part;
+    float* gu;
+    bf16_t* out;
+    int64_t ldo;
+    int32_t M, N, splits, act;       // N: hidden values for the gated kinds
+};
+
+template <FfnKind kKind>
+__global__ __launch_bounds__(256) void ffn_join_kernel(Join a) {
+    constexpr bool kGate = kKind == FFN_GATE || kKind == FFN_GATE_KEEP, kGrad = kKind == FFN_GATE_GRAD;
+    const int blocks_n = a.N / 32, part_n = kGate ? 2 * blocks_n : blocks_n;
+    const int64_t rows = (a.M + 31) / 32, block = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
+    if (block >= rows * blocks_n) return;
     const int lane = threadIdx.x & 63;
     const int mb = static_cast<int>(block / blocks_n), nb = static_cast<int>(block % blocks_n);
-    const float* p = part + block * 1024 + lane * 4;
-    f32x4_t s[4];
+    constexpr int B = kGate ? 2 : 1;
+    f32x4_t s[B][4];
 #pragma unroll
-    for (int e4 = 0; e4 < 4; ++e4) s[e4] = *reinterpret_cast<const f32x4_t*>(p + e4 * 256);
-    for (int k = 1; k < splits; ++k) {
-        p += blocks * 1024;
+    for (int b = 0; b < B; ++b) {
+        const float* p = a.part + (static_cast<int64_t>(mb) * part_n + nb + b * blocks_n) * 1024 + lane * 4;
 #pragma unroll
-        for (int e4 = 0; e4 < 4; ++e4) s[e4] += *reinterpret_cast<const f32x4_t*>(p + e4 * 256);
+        for (int e4 = 0; e4 < 4; ++e4) s[b][e4] = *reinterpret_cast<const f32x4_t*>(p + e4 * 256);
+#pragma unroll 3
+        for (int k = 1; k < a.splits; ++k)
+#pragma unroll
+            for (int e4 = 0; e4 < 4; ++e4) s[b][e4] += *reinterpret_cast<const f32x4_t*>(p + k * rows * part_n * 1024 + e4 * 256);
     }
+    float* const gu = a.gu + (static_cast<int64_t>(mb) * blocks_n + nb) * 2048 + lane * 4;
     const int m = mb * 32 + (lane & 31);
-    if (m >= M) return;
+    bf16_t* const out = a.out + m * a.ldo + nb * 32 + 4 * (lane >> 5);
+    const auto store = [&](bf16_t* p, const f32x4_t& v) {
+        if (m < a.M) *reinterpret_cast<u32x2_t*>(p) = u32x2_t{pack2(v[0], v[1]), pack2(v[2], v[3])};
+    };
 #pragma unroll
     for (int e4 = 0; e4 < 4; ++e4) {
-        const int n = nb * 32 + 8 * e4 + 4 * (lane >> 5);
-        *reinterpret_cast<u32x2_t*>(out + static_cast<int64_t>(m) * N + n) = u32x2_t{pack2(s[e4][0], s[e4][1]), pack2(s[e4][2], s[e4][3])};
+        if constexpr (kGate) {
+            if constexpr (kKind == FFN_GATE_KEEP) {
+                *reinterpret_cast<f32x4_t*>(gu + e4 * 256) = s[0][e4];
+                *reinterpret_cast<f32x4_t*>(gu + 1024 + e4 * 256) = s[1][e4];
+            }
+            f32x4_t h;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                float f, df;
+                act_fast(s[0][e4][c], a.act, &f, &df);
+                h[c] = f * s[1][e4][c];
+            }
+            store(out + 8 * e4, h);
+        } else if constexpr (kGrad) {
+            const f32x4_t g = *reinterpret_cast<const f32x4_t*>(gu + e4 * 256), u = *reinterpret_cast<const f32x4_t*>(gu + 1024 + e4 * 256);
+            f32x4_t dg, du;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                float f, df;
+                act_fast(g[c], a.act, &f, &df);
+                du[c] = s[0][e4][c] * f;
+                dg[c] = s[0][e4][c] * u[c] * df;
+            }
+            store(out + 8 * e4, dg);
+            store(out + 8 * e4 + a.N, du);
+        } else {
+            store(out + 8 * e4, s[0][e4]);
+        }
     }
 }
 
@@ -428,23 +471,97 @@ int32_t launch_tile(const Tile& t, const Launch& la, int blocks, hipStream_t s) 
     return launch_kernel<128, 128, 4, 2, XK, WK, EPI>(la, blocks, s);
 }
 
-Tile tile_of(const FfnProduct* p, int n) {
-    // the largest tile that still gives every compute unit one
-    for (const Tile t : {Tile{256, 256}, Tile{128, 256}}) {
-        int64_t tiles = 0;
+// What a launch takes: tile, and per product the parts that its sums over K are cut in
+struct Plan {
+    Tile tile;
+    int splits[2];
+};
+
+int slices_of(int32_t K) { return std::max(1, (K + BK - 1) / BK); }
+int parts_of(int slices, int splits) { return (slices + (slices + splits - 1) / splits - 1) / ((slices + splits - 1) / splits); }
+
+int64_t tiles_of(const FfnProduct& p, const Tile& t, bool parts) {
+    // (parts of g | u are those of one matrix of 2 N rows: gate and up meet in the join)
+    const int64_t cols = p.gated() ? (parts ? 2 * static_cast<int64_t>(p.N) : p.N) : p.N;
+    const int per = p.gated() && !parts ? t.bn / 2 : t.bn;
+    return static_cast<int64_t>((p.M + t.bm - 1) / t.bm) * ((cols + per - 1) / per);
+}
+
+size_t part_bytes(const FfnProduct& p, int splits) {
+    return splits == 1 ? 0 : static_cast<size_t>(splits) * ((p.M + 31) / 32) * (p.N / 32) * (p.gated() ? 2 : 1) * 4096;
+}
+
+// Times of a workgroup, us: a launch; a slice of 64 k with all compute units at work, and with nothing in the way but its loads' latency;
+// the epilogue by what it does; slices of K-major operands against those of rows.  Fitted to 930 launches (70 to 12288 rows, widths 384 /
+// 768 / 1152 / 2048 / 4096 with 1536 to 10240 hidden values, the three tiles, K in 1 to 24 parts, every kind of product): the plan chosen
+// by them takes 1.0 % longer than the fastest one on average, 14 % at most.  What it decides, us: 12288 x 1152 x 4608, gate and up, 256 x
+// 256 tiles 257, 128 x 128 322; 4096 x 1152 x 4608, the gated gradient, 256 x 256 100, 128 x 128 - a workgroup's epilogue beside another's
+// products - 79; 128 x 1152 x 4608, the down product, K whole 46, in 12 parts 9 and 7 for the join.
+struct TileTime {
+    Tile tile;
+    double launch, slice, alone, store, gate, grad, part, one_k_major, both_k_major;
+    int resident;                    // workgroups per compute unit
+};
+constexpr TileTime kTileTimes[] = {{{256, 256}, 0.46, 1.15, 0.58, 7.6, 8.8, 16.0, 10.5, 1.05, 1.06, 1},
+                                   {{128, 256}, 1.35, 0.89, 0.53, 4.8, 3.6, 9.5, 6.3, 0.82, 0.83, 1},
+                                   {{128, 128}, 3.25, 0.58, 0.49, 1.9, 6.7, 6.9, 4.0, 0.64, 1.01, 2}};
+constexpr int kUnits = 256;          // compute units; not asked of the device, as a workspace's size must not depend on which is current
+constexpr int kMinPart = 4;          // slices of a part of K
+
+Plan plan_of(const FfnProduct* p, int n) {
+    Plan best{{128, 128}, {1, 1}};
+    double best_time = 0.0;
+    const FfnKind kind = p[0].kind;
+    for (const int splits : {1, 2, 3, 4, 6, 8, 12, 16, 24}) {
+        Plan plan{{0, 0}, {1, 1}};
+        double join = 0.0;
+        int slices = 0;
         for (int i = 0; i < n; ++i) {
-            const int cols = p[i].gated() ? t.bn / 2 : t.bn;
-            tiles += static_cast<int64_t>((p[i].M + t.bm - 1) / t.bm) * ((p[i].N + cols - 1) / cols);
+            const int all = slices_of(p[i].K);
+            plan.splits[i] = parts_of(all, std::min(splits, all));
+            slices = std::max(slices, (all + plan.splits[i] - 1) / plan.splits[i]);
+            if (splits > 1) join += 4.8 + 0.27 * plan.splits[i] + 0.18e-6 * static_cast<double>(part_bytes(p[i], plan.splits[i]));
         }
-        if (tiles >= device_cus() * 3 / 4) return t;
+        if (splits > 1 && slices < kMinPart) break;
+        for (const TileTime& t : kTileTimes) {
+            int64_t work = 0;
+            for (int i = 0; i < n; ++i) work += tiles_of(p[i], t.tile, splits > 1) * plan.splits[i];
+            const double slice = t.slice * (kind == FFN_K_BY_K ? t.both_k_major : kind == FFN_ROWS_BY_K || kind == FFN_GATE_GRAD ? t.one_k_major : 1.0);
+            const double end = splits > 1 ? t.part : p[0].gated() ? t.gate : kind == FFN_GATE_GRAD ? t.grad : t.store;
+            const int64_t rounds = work / (kUnits * t.resident), rest = work % (kUnits * t.resident), share = (rest + kUnits - 1) / kUnits;
+            double time = t.launch + join + rounds * (slices * std::max(t.alone, slice * t.resident) + end);
+            if (rest > 0) time += slices * std::max(t.alone, slice * share) + end * share / t.resident;
+            if (best_time == 0.0 || time < best_time) {
+                best_time = time;
+                best = plan;
+                best.tile = t.tile;
+            }
+        }
     }
-    return Tile{128, 128};
+    return best;
+}
+
+template <FfnKind kKind>
+int32_t launch_join(const FfnProduct& p, const float* part, int splits, hipStream_t s) {
+    const int64_t blocks = static_cast<int64_t>((p.M + 31) / 32) * (p.N / 32);
+    hipLaunchKernelGGL(ffn_join_kernel<kKind>, dim3(static_cast<uint32_t>((blocks + 3) / 4)), dim3(256), 0, s,
+                       Join{part, p.gu, p.out, p.ldo, p.M, p.N, splits, p.act});
+    return launch_ok() ? FREE_OK : FREE_ERR_HIP;
 }
 
 }  // namespace
 
-int32_t launch_ffn_products(const FfnProduct* p, int n, hipStream_t s) {
-    const Tile t = tile_of(p, n);
+size_t ffn_products_part_bytes(const FfnProduct* p, int n) {
+    const Plan plan = plan_of(p, n);
+    if (n == 1 || (plan.splits[0] == 1 && plan.splits[1] == 1)) return part_bytes(p[0], plan.splits[0]);
+    return static_cast<size_t>(plan.splits[0]) * (p[0].M / 32) * (p[0].N / 32) * 4096 +
+           static_cast<size_t>(plan.splits[1]) * (p[1].M / 32) * (p[1].N / 32) * 4096;
+}
+
+int32_t launch_ffn_products(const FfnProduct* p, int n, float* part, hipStream_t s) {
+    const Plan plan = plan_of(p, n);
+    const Tile t = plan.tile;
+    const bool parts = plan.splits[0] > 1 || (n == 2 && plan.splits[1] > 1);
     Launch la{};
     int64_t blocks = 0;
     for (int i = 0; i < n; ++i) {
@@ -454,33 +571,58 @@ int32_t launch_ffn_products(const FfnProduct* p, int n, hipStream_t s) {
         q.ldx = p[i].ldx;
         q.ldw = p[i].ldw;
         q.M = p[i].M;
-        q.N = p[i].N;
+        q.N = p[i].gated() && parts ? 2 * p[i].N : p[i].N;
         q.K = p[i].K;
-        const int cols = p[i].gated() ? t.bn / 2 : t.bn;
+        const int cols = p[i].gated() && !parts ? t.bn / 2 : t.bn;
         q.tiles_m = (q.M + t.bm - 1) / t.bm;
         q.tiles_n = (q.N + cols - 1) / cols;
         q.group_m = 8;
-        q.splits = 1;
-        q.split_slices = (q.K + BK - 1) / BK;
+        q.split_slices = (slices_of(q.K) + plan.splits[i] - 1) / plan.splits[i];
         q.out = p[i].out;
         q.ldo = p[i].ldo;
         q.gu = p[i].gu;
         q.act = p[i].act;
+        if (parts) {
+            q.part = part;
+            part += static_cast<int64_t>(plan.splits[i]) * ((q.M + 31) / 32) * (q.N / 32) * 1024;
+        }
         if (i == 1) la.first1 = static_cast<int32_t>(blocks);
-        blocks += static_cast<int64_t>(q.tiles_m) * q.tiles_n;
+        blocks += static_cast<int64_t>(q.tiles_m) * q.tiles_n * plan.splits[i];
     }
     if (n == 1) la.first1 = 0x7fffffff;
     if (blocks > (1 << 22)) return FREE_ERR_LIMIT;
     const int b = static_cast<int>(blocks);
+    if (!parts) {
+        switch (p[0].kind) {
+            case FFN_GATE: return launch_tile<false, false, FFN_GATE>(t, la, b, s);
+            case FFN_GATE_KEEP: return launch_tile<false, false, FFN_GATE_KEEP>(t, la, b, s);
+            case FFN_GATE_GRAD: return launch_tile<false, true, FFN_GATE_GRAD>(t, la, b, s);
+            case FFN_ROWS: return launch_tile<false, false, FFN_STORE>(t, la, b, s);
+            case FFN_ROWS_BY_K: return launch_tile<false, true, FFN_STORE>(t, la, b, s);
+            case FFN_K_BY_K: return launch_tile<true, true, FFN_STORE>(t, la, b, s);
+            default: return FREE_ERR_RANGE;
+        }
+    }
+    int32_t st;
     switch (p[0].kind) {
-        case FFN_GATE: return launch_tile<false, false, FFN_GATE>(t, la, b, s);
-        case FFN_GATE_KEEP: return launch_tile<false, false, FFN_GATE_KEEP>(t, la, b, s);
-        case FFN_GATE_GRAD: return launch_tile<false, true, FFN_GATE_GRAD>(t, la, b, s);
-        case FFN_ROWS: return launch_tile<false, false, FFN_STORE>(t, la, b, s);
-        case FFN_ROWS_BY_K: return launch_tile<false, true, FFN_STORE>(t, la, b, s);
-        case FFN_K_BY_K: return launch_tile<true, true, FFN_STORE>(t, la, b, s);
+        case FFN_GATE:
+        case FFN_GATE_KEEP:
+        case FFN_ROWS: st = launch_tile<false, false, FFN_PART>(t, la, b, s); break;
+        case FFN_GATE_GRAD:
+        case FFN_ROWS_BY_K: st = launch_tile<false, true, FFN_PART>(t, la, b, s); break;
+        case FFN_K_BY_K: st = launch_tile<true, true, FFN_PART>(t, la, b, s); break;
         default: return FREE_ERR_RANGE;
     }
+    for (int i = 0; i < n && st == FREE_OK; ++i) {
+        const float* from = la.p[i].part;
+        switch (p[i].kind) {
+            case FFN_GATE: st = launch_join<FFN_GATE>(p[i], from, plan.splits[i], s); break;
+            case FFN_GATE_KEEP: st = launch_join<FFN_GATE_KEEP>(p[i], from, plan.splits[i], s); break;
+            case FFN_GATE_GRAD: st = launch_join<FFN_GATE_GRAD>(p[i], from, plan.splits[i], s); break;
+            default: st = launch_join<FFN_ROWS>(p[i], from, plan.splits[i], s); break;
+        }
+    }
+    return st;
 }
 
 }  // namespace freemi
