@@ -303,7 +303,7 @@ int32_t forward_of(const Sizes& z, const T* x, const T* w_in, const T* w_out, in
         gu = k.gu;
         h = k.h;
     }
-    if (!saved && z.M <= kFfnFewRows) return launch_ffn_rows(x, w_in, w_out, z.M, z.D, z.F, act, h, out, s);
+    if (!saved && ffn_rows_pay(z.M, z.D, z.F, z.es == 2 ? FREE_BF16 : FREE_FP32)) return launch_ffn_rows(x, w_in, w_out, z.M, z.D, z.F, act, h, out, s);
     T* y = out;
     if (z.padded) {
         FREE_STEP(fit(x, z.M, z.D, w.x, z.M, z.Dp, s));

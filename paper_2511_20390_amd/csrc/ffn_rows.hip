@@ -1,12 +1,16 @@
 // The two products of the gated feed-forward block for few token rows (a token that is being sampled, a handful of states): bound by
 // reading the weights once, 2 F D and D F values, whatever the rows are.
 //
-// A workgroup owns 16 weight rows (gated: 16 gate rows and the 16 up rows of the same hidden values) and its wavefronts share K: step
-// s of 128 bytes per row goes to wavefront s % wavefronts, so that a workgroup reads runs of a kilobyte and more of every row.  Weights
-// go from memory to the registers of the matrix instruction directly - they are used once, LDS would only delay them -: lane l holds 32
-// bytes of weight row l % 16 at 32 (l / 16) of the step and the same k of token l % 16; which of a step's k meet in an instruction does
-// not matter to the sum.  bf16: v_mfma_f32_16x16x32_bf16; fp32: v_mfma_f32_16x16x4_f32, exact products, fp32 sums.  The wavefronts' sums
-// are added through LDS in order, and the activation is applied there.
+// A workgroup owns R = 16 or 8 weight rows (gated: of either matrix, the same hidden values) and its 8 wavefronts share K, step by step of
+// 128 bytes per row, so that a workgroup reads runs of a kilobyte of every row.  Weights go from memory to the registers of the matrix
+// instruction directly: they are used once, LDS would only delay them.  A row's step is 8 pieces of 16 bytes, and 16 lanes meet two of
+// them with their 16 tokens: with R = 16 lane l has both of weight row l % 16; with R = 8 it has one of row l % 8, and the instruction for the
+// other finds its rows 8 lanes away.  Which of a step's k meet in an instruction does not matter to the sum.  bf16:
+// v_mfma_f32_16x16x32_bf16; fp32: v_mfma_f32_16x16x4_f32, exact products, fp32 sums.  The wavefronts' sums are added through LDS in
+// order, and the activation is applied there.
+// R = 8 spreads the weights over twice the workgroups (a compute unit takes some 46 KB/us from memory) and reads 128 bytes of a row per
+// instruction instead of 64, but loads the tokens once more per weight.  us with 16 rows in both launches, with 8 in both, with 8 for gate
+// and up alone: bf16, one row, 1152 x 4608 15.7, 13.3, 15.2; 4096 x 10240 52.9, 46.4, 45.5; 16 rows 19.8, 18.2, 20.0; 60.9, 73.0, 64.5.
 // Any D, F and number of rows: rows past the end are read as the last one and not written, a row's last step is read value by value
 // where it is not whole, and rows that are not 16-byte aligned cost the memory pipe more, no copies.
 #include <algorithm>
@@ -21,9 +25,7 @@ namespace {
 
 typedef float f32x4a_t __attribute__((ext_vector_type(4)));
 
-constexpr int kRowsPerGroup = 16;
-constexpr int kStepBytes = 128;
-constexpr int kUnroll = 4;
+constexpr int kWaves = 8;
 
 struct RowArgs {
     const void *x, *w;
@@ -31,20 +33,18 @@ struct RowArgs {
     int32_t M, N, K, act;
 };
 
+// 16 bytes; left: values of the row from p on, maybe none
 template <typename T>
-__device__ __forceinline__ void load_piece(const T* p, int left, u32x4_t (&v)[2], bool whole) {
+__device__ __forceinline__ void load_piece(const T* p, int left, u32x4_t& v, bool whole) {
     constexpr int E = 16 / sizeof(T);
-    if (whole) {
-        __builtin_memcpy(&v[0], p, 16);
-        __builtin_memcpy(&v[1], p + E, 16);
+    if (whole || left >= E) {
+        __builtin_memcpy(&v, p, 16);
         return;
     }
-    // (left: values of the row from p on, maybe none)
-    T t[2 * E];
+    T t[E];
 #pragma unroll
-    for (int e = 0; e < 2 * E; ++e) t[e] = e < left ? p[e] : T{};
-    __builtin_memcpy(&v[0], t, 16);
-    __builtin_memcpy(&v[1], t + E, 16);
+    for (int e = 0; e < E; ++e) t[e] = e < left ? p[e] : T{};
+    __builtin_memcpy(&v, t, 16);
 }
 
 template <typename T>
@@ -63,24 +63,26 @@ __device__ __forceinline__ float gate_of(float g, int act) {
     return 0.5f * g * (1.0f + tanhf(0.7978845608028654f * (g + 0.044715f * g * g * g)));
 }
 
-// kEdge: rows or their ends may not be whole pieces
-template <typename T, int MT, int WAVES, bool kGated, bool kEdge>
-__global__ __launch_bounds__(WAVES * 64) void ffn_rows_kernel(RowArgs a) {
+// kEdge: rows' last steps may not be whole
+template <typename T, int R, int MT, bool kGated, bool kEdge>
+__global__ __launch_bounds__(kWaves * 64) void ffn_rows_kernel(RowArgs a) {
     constexpr int NB = kGated ? 2 : 1;                           // weight matrices
-    constexpr int kStep = kStepBytes / sizeof(T);
-    __shared__ f32x4a_t red[WAVES][NB * MT][64];
+    constexpr int P = 2, H = R / 8;                              // pieces of a step for 16 lanes; of them in one lane
+    constexpr int E = 16 / sizeof(T), kStep = 4 * P * E;         // values
+    constexpr int U = 4;                                         // steps in flight per wavefront
+    __shared__ f32x4a_t red[kWaves][NB * MT][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int n0 = blockIdx.x * kRowsPerGroup;
-    const int r16 = lane & 15, part = (lane >> 4) * (kStep / 4);
-    const int n = n0 + r16 < a.N ? n0 + r16 : a.N - 1;
+    const int n0 = blockIdx.x * R, quad = lane >> 4, r16 = lane & 15;
+    const int n = n0 + r16 % R < a.N ? n0 + r16 % R : a.N - 1;
+    const int w_at = (quad * P + r16 / R * H) * E, x_at = quad * P * E;
     const T* w[NB];
 #pragma unroll
-    for (int b = 0; b < NB; ++b) w[b] = static_cast<const T*>(a.w) + (static_cast<int64_t>(b) * a.N + n) * a.K + part;
+    for (int b = 0; b < NB; ++b) w[b] = static_cast<const T*>(a.w) + (static_cast<int64_t>(b) * a.N + n) * a.K + w_at;
     const T* x[MT];
 #pragma unroll
     for (int t = 0; t < MT; ++t) {
         const int m = t * 16 + r16;
-        x[t] = static_cast<const T*>(a.x) + static_cast<int64_t>(m < a.M ? m : a.M - 1) * a.K + part;
+        x[t] = static_cast<const T*>(a.x) + static_cast<int64_t>(m < a.M ? m : a.M - 1) * a.K + x_at;
     }
     f32x4a_t acc[NB][MT];
 #pragma unroll
@@ -88,29 +90,42 @@ __global__ __launch_bounds__(WAVES * 64) void ffn_rows_kernel(RowArgs a) {
 #pragma unroll
         for (int t = 0; t < MT; ++t) acc[b][t] = f32x4a_t{0.f, 0.f, 0.f, 0.f};
     const int steps = (a.K + kStep - 1) / kStep;
-    for (int s0 = wave; s0 < steps; s0 += WAVES * kUnroll) {
-        u32x4_t wv[kUnroll][NB][2], xv[kUnroll][MT][2];
+    for (int s0 = wave; s0 < steps; s0 += kWaves * U) {
+        u32x4_t wv[U][NB][H], xv[U][MT][P];
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u) {
-            const int s = s0 + u * WAVES;
+        for (int u = 0; u < U; ++u) {
+            const int s = s0 + u * kWaves;
             if (s >= steps) continue;
             const int64_t k = static_cast<int64_t>(s) * kStep;
             const bool whole = !kEdge || k + kStep <= a.K;
-            const int left = static_cast<int>(a.K - k) - part;
+            const int left = static_cast<int>(a.K - k);
 #pragma unroll
-            for (int b = 0; b < NB; ++b) load_piece(w[b] + k, left, wv[u][b], whole);
+            for (int b = 0; b < NB; ++b)
 #pragma unroll
-            for (int t = 0; t < MT; ++t) load_piece(x[t] + k, left, xv[u][t], whole);
+                for (int h = 0; h < H; ++h) load_piece(w[b] + k + h * E, left - w_at - h * E, wv[u][b][h], whole);
+#pragma unroll
+            for (int t = 0; t < MT; ++t)
+#pragma unroll
+                for (int p = 0; p < P; ++p) load_piece(x[t] + k + p * E, left - x_at - p * E, xv[u][t][p], whole);
         }
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u) {
-            if (s0 + u * WAVES >= steps) continue;
+        for (int u = 0; u < U; ++u) {
+            if (s0 + u * kWaves >= steps) continue;
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
+            for (int b = 0; b < NB; ++b)
 #pragma unroll
-                for (int b = 0; b < NB; ++b)
+                for (int h = 0; h < H; ++h) {
+                    const u32x4_t v = wv[u][b][h];
 #pragma unroll
-                    for (int t = 0; t < MT; ++t) multiply<T>(wv[u][b][h], xv[u][t][h], acc[b][t]);
+                    for (int t = 0; t < MT; ++t) multiply<T>(v, xv[u][t][h], acc[b][t]);
+                    if constexpr (R == 8) {
+                        u32x4_t other;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) other[e] = lane_xor<8>(static_cast<uint32_t>(v[e]));
+#pragma unroll
+                        for (int t = 0; t < MT; ++t) multiply<T>(other, xv[u][t][1], acc[b][t]);
+                    }
+                }
         }
     }
 #pragma unroll
@@ -118,9 +133,9 @@ __global__ __launch_bounds__(WAVES * 64) void ffn_rows_kernel(RowArgs a) {
 #pragma unroll
         for (int t = 0; t < MT; ++t) red[wave][b * MT + t][lane] = acc[b][t];
     __syncthreads();
-    // value i of a tile: token i / 16, weight row i % 16; it stands in lane token + 16 (row / 4), register row % 4
-    for (int i = threadIdx.x; i < MT * 256; i += WAVES * 64) {
-        const int t = i >> 8, token = i >> 4 & 15, row = i & 15, from = token + 16 * (row >> 2);
+    // value i of a tile: token i / R, weight row i % R; it stands in lane token + 16 (row / 4), register row % 4
+    for (int i = threadIdx.x; i < MT * 16 * R; i += kWaves * 64) {
+        const int t = i / (16 * R), token = i / R % 16, row = i % R, from = token + 16 * (row >> 2);
         const int m = t * 16 + token;
         if (m >= a.M || n0 + row >= a.N) continue;
         float v[NB];
@@ -128,26 +143,27 @@ __global__ __launch_bounds__(WAVES * 64) void ffn_rows_kernel(RowArgs a) {
         for (int b = 0; b < NB; ++b) {
             v[b] = red[0][b * MT + t][from][row & 3];
 #pragma unroll
-            for (int k = 1; k < WAVES; ++k) v[b] += red[k][b * MT + t][from][row & 3];
+            for (int k = 1; k < kWaves; ++k) v[b] += red[k][b * MT + t][from][row & 3];
         }
         if constexpr (kGated) v[0] = gate_of(v[0], a.act) * v[1];
         store_f(static_cast<T*>(a.out) + static_cast<int64_t>(m) * a.N + n0 + row, v[0]);
     }
 }
 
-template <typename T, int MT, int WAVES, bool kGated>
+template <typename T, int R, int MT, bool kGated>
 int32_t launch_edge(const RowArgs& a, hipStream_t s) {
-    const dim3 grid((a.N + kRowsPerGroup - 1) / kRowsPerGroup), block(WAVES * 64);
-    if (a.K % (kStepBytes / sizeof(T)) == 0) hipLaunchKernelGGL((ffn_rows_kernel<T, MT, WAVES, kGated, false>), grid, block, 0, s, a);
-    else hipLaunchKernelGGL((ffn_rows_kernel<T, MT, WAVES, kGated, true>), grid, block, 0, s, a);
+    constexpr int kStep = 128 / sizeof(T);
+    const dim3 grid((a.N + R - 1) / R), block(kWaves * 64);
+    if (a.K % kStep == 0) hipLaunchKernelGGL((ffn_rows_kernel<T, R, MT, kGated, false>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((ffn_rows_kernel<T, R, MT, kGated, true>), grid, block, 0, s, a);
     return launch_ok() ? FREE_OK : FREE_ERR_HIP;
 }
 
 template <typename T, bool kGated>
 int32_t launch_rows(const RowArgs& a, hipStream_t s) {
-    if (a.M <= 16) return launch_edge<T, 1, 8, kGated>(a, s);
-    if (a.M <= 32) return launch_edge<T, 2, 8, kGated>(a, s);
-    return launch_edge<T, 4, 8, kGated>(a, s);
+    // 8 weight rows where groups of 16 would leave compute units without one, and for gate and up of few tokens
+    if (a.N < 16 * 256 || (kGated && a.M <= 8)) return a.M <= 16 ? launch_edge<T, 8, 1, kGated>(a, s) : launch_edge<T, 8, 2, kGated>(a, s);
+    return a.M <= 16 ? launch_edge<T, 16, 1, kGated>(a, s) : launch_edge<T, 16, 2, kGated>(a, s);
 }
 
 }  // namespace
@@ -157,6 +173,12 @@ int32_t launch_ffn_rows(const T* x, const T* w_in, const T* w_out, int32_t M, in
     const int32_t st = launch_rows<T, true>(RowArgs{x, w_in, h, M, F, D, act}, s);
     return st != FREE_OK ? st : launch_rows<T, false>(RowArgs{h, w_out, out, M, D, F, act}, s);
 }
+// Against the tiles of ffn_mfma.hip and gemm_f32.hip, us: bf16 17 to 32 rows, 384 x 1536 9 against 15, 1152 x 4608 25.5 against 25.7, 4096 x
+// 10240 63 to 80 against 65; fp32 32 rows, 1152 x 4608 50 against 88, 4096 x 10240 191 against 238 (48 rows 286 against 259).
+bool ffn_rows_pay(int32_t M, int32_t D, int32_t F, int32_t dtype) {
+    return M <= 16 || (M <= 32 && (dtype == FREE_FP32 || static_cast<int64_t>(D) * F <= 1 << 22));
+}
+
 template int32_t launch_ffn_rows(const bf16_t*, const bf16_t*, const bf16_t*, int32_t, int32_t, int32_t, int32_t, bf16_t*, bf16_t*, hipStream_t);
 template int32_t launch_ffn_rows(const float*, const float*, const float*, int32_t, int32_t, int32_t, int32_t, float*, float*, hipStream_t);
 
