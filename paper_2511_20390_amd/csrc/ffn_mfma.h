@@ -1,4 +1,4 @@
-// The bf16 matrix products of the gated feed-forward block (ffn_mfma.hip), for ffn.hip.  Sizes but the number of token rows are multiples of
+// The matrix products of the gated feed-forward block (ffn_mfma.hip; fp32: gemm_f32.hip), for ffn.hip.  Sizes but the number of token rows are multiples of
 // 64, pointers 16-byte aligned, leading dimensions multiples of 8.
 #pragma once
 
@@ -18,22 +18,26 @@ enum FfnKind {
     FFN_PART
 };
 
+template <typename T>                // bf16_t or float
 struct FfnProduct {
     FfnKind kind;
-    const bf16_t *X, *W;
+    const T *X, *W;
     int64_t ldx, ldw;
     int32_t M, N, K;
-    bf16_t* out;
+    T* out;
     int64_t ldo;
-    float* gu = nullptr;             // [M / 32 rounded up][N / 32][2][1024]
+    float* gu = nullptr;             // [g | u] as 32 x 32 blocks: [M / 32 rounded up][2 N / 32][4][lane][4]
     int32_t act = 0;
     bool gated() const { return kind == FFN_GATE || kind == FFN_GATE_KEEP; }
 };
 
-// One launch for n products (1, or 2 FFN_K_BY_K), or, where their sums over K are cut in parts, one more for each that joins them; part: room of
-// ffn_products_part_bytes (by the sizes alone).
-size_t ffn_products_part_bytes(const FfnProduct* p, int n);
-int32_t launch_ffn_products(const FfnProduct* p, int n, float* part, hipStream_t s);
+// bf16: one launch for n products (1, or 2 FFN_K_BY_K), or, where their sums over K are cut in parts, one more for each that joins them.
+// fp32: a launch for each, and one more where parts are joined or an activation is applied.  part: room of ffn_products_part_bytes (by the
+// sizes alone).
+size_t ffn_products_part_bytes(const FfnProduct<bf16_t>* p, int n);
+size_t ffn_products_part_bytes(const FfnProduct<float>* p, int n);
+int32_t launch_ffn_products(const FfnProduct<bf16_t>* p, int n, float* part, hipStream_t s);
+int32_t launch_ffn_products(const FfnProduct<float>* p, int n, float* part, hipStream_t s);
 
 // ffn_rows.hip: y of up to 32 token rows, any D and F, in two launches; h: room for [M, F].  ffn_rows_pay: where that is the faster way.
 bool ffn_rows_pay(int32_t M, int32_t D, int32_t F, int32_t dtype);

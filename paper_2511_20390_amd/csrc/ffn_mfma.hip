@@ -36,7 +36,7 @@ struct Problem {
     int32_t split_slices;        // slices of a part of K (all, or those of one of several)
     bf16_t* out;                 // [M, N], ldo values from row to row; gated gradient: dg, du n_gate values further
     float* part;                 // sums over a part of K: [part][32 x 32 block][4][lane][4]
-    float* gu;                   // kept g, u: [32 x 32 block][2][4][lane][4]
+    float* gu;                   // kept [g | u], in blocks likewise
     int64_t ldo;
     int32_t act;
 };
@@ -320,12 +320,12 @@ __global__ __launch_bounds__(512) void ffn_product_kernel(Launch la) {
             if constexpr (EPI == FFN_GATE_KEEP) {
                 const int mb = m0 / 32 + wm * TM + i;
                 if (mb * 32 < a.M) {
-                    float* p = a.gu + (static_cast<int64_t>(mb) * blocks_n + gn_wave / 32) * 2048 + lane * 4;
+                    float* p = a.gu + (static_cast<int64_t>(mb) * 2 * blocks_n + gn_wave / 32) * 1024 + lane * 4;
 #pragma unroll
                     for (int j = 0; j < 2; ++j)
 #pragma unroll
                         for (int e4 = 0; e4 < 4; ++e4)
-                            *reinterpret_cast<f32x4_t*>(p + j * 1024 + e4 * 256) =
+                            *reinterpret_cast<f32x4_t*>(p + static_cast<int64_t>(j) * blocks_n * 1024 + e4 * 256) =
                                 f32x4_t{acc[i][j][4 * e4], acc[i][j][4 * e4 + 1], acc[i][j][4 * e4 + 2], acc[i][j][4 * e4 + 3]};
                 }
             }
@@ -349,11 +349,11 @@ __global__ __launch_bounds__(512) void ffn_product_kernel(Launch la) {
                 const int nb = gn_wave / 32 + j;
                 f32x4_t g[4], u[4];
                 if (mb * 32 < a.M && nb < blocks_n) {
-                    const float* p = a.gu + (static_cast<int64_t>(mb) * blocks_n + nb) * 2048 + lane * 4;
+                    const float* p = a.gu + (static_cast<int64_t>(mb) * 2 * blocks_n + nb) * 1024 + lane * 4;
 #pragma unroll
                     for (int e4 = 0; e4 < 4; ++e4) {
                         g[e4] = *reinterpret_cast<const f32x4_t*>(p + e4 * 256);
-                        u[e4] = *reinterpret_cast<const f32x4_t*>(p + 1024 + e4 * 256);
+                        u[e4] = *reinterpret_cast<const f32x4_t*>(p + static_cast<int64_t>(blocks_n) * 1024 + e4 * 256);
                     }
                 }
                 float dg[16];
@@ -383,16 +383,32 @@ __global__ __launch_bounds__(512) void ffn_product_kernel(Launch la) {
 
 // The parts of a product's sums over K, added in order, and the epilogue they were left without; a wavefront per 32 x 32 block of the
 // result.  Blocks of g | u: block_n and block_n + N / 32.
+template <typename T>
 struct Join {
     const float* part;
     float* gu;
-    bf16_t* out;
+    T* out;
     int64_t ldo;
     int32_t M, N, splits, act;       // N: hidden values for the gated kinds
 };
 
-template <FfnKind kKind>
-__global__ __launch_bounds__(256) void ffn_join_kernel(Join a) {
+// fp32: the library's exponential and tanh in place of the hardware's
+__device__ __forceinline__ void act_exact(float v, int act, float* f, float* df) {
+    if (act == FREE_ACT_SILU) {
+        const float s = 1.0f / (1.0f + expf(-v));
+        *f = v * s;
+        *df = s == 0.f || s == 1.f ? s : s * (1.0f + v * (1.0f - s));
+    } else {
+        const float k = 0.7978845608028654f;
+        const float v2 = v * v, t = tanhf(k * (v + 0.044715f * v2 * v));
+        *f = 0.5f * v * (1.0f + t);
+        // (1 - t^2) times what grows with v^3: 0 where t is one to the last bit
+        *df = fabsf(t) == 1.f ? 0.5f * (1.0f + t) : 0.5f * (1.0f + t) + 0.5f * v * (1.0f - t * t) * k * (1.0f + 3.0f * 0.044715f * v2);
+    }
+}
+
+template <FfnKind kKind, typename T>
+__global__ __launch_bounds__(256) void ffn_join_kernel(Join<T> a) {
     constexpr bool kGate = kKind == FFN_GATE || kKind == FFN_GATE_KEEP, kGrad = kKind == FFN_GATE_GRAD;
     const int blocks_n = a.N / 32, part_n = kGate ? 2 * blocks_n : blocks_n;
     const int64_t rows = (a.M + 31) / 32, block = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
@@ -411,34 +427,41 @@ __global__ __launch_bounds__(256) void ffn_join_kernel(Join a) {
 #pragma unroll
             for (int e4 = 0; e4 < 4; ++e4) s[b][e4] += *reinterpret_cast<const f32x4_t*>(p + k * rows * part_n * 1024 + e4 * 256);
     }
-    float* const gu = a.gu + (static_cast<int64_t>(mb) * blocks_n + nb) * 2048 + lane * 4;
+    float* const gu = a.gu + (static_cast<int64_t>(mb) * 2 * blocks_n + nb) * 1024 + lane * 4;
+    float* const up = gu + static_cast<int64_t>(blocks_n) * 1024;
     const int m = mb * 32 + (lane & 31);
-    bf16_t* const out = a.out + m * a.ldo + nb * 32 + 4 * (lane >> 5);
-    const auto store = [&](bf16_t* p, const f32x4_t& v) {
-        if (m < a.M) *reinterpret_cast<u32x2_t*>(p) = u32x2_t{pack2(v[0], v[1]), pack2(v[2], v[3])};
+    T* const out = a.out + m * a.ldo + nb * 32 + 4 * (lane >> 5);
+    const auto store = [&](T* p, const f32x4_t& v) {
+        if (m >= a.M) return;
+        if constexpr (sizeof(T) == 4) *reinterpret_cast<f32x4_t*>(p) = v;
+        else *reinterpret_cast<u32x2_t*>(p) = u32x2_t{pack2(v[0], v[1]), pack2(v[2], v[3])};
+    };
+    const auto activate = [&](float v, float* f, float* df) {
+        if constexpr (sizeof(T) == 4) act_exact(v, a.act, f, df);
+        else act_fast(v, a.act, f, df);
     };
 #pragma unroll
     for (int e4 = 0; e4 < 4; ++e4) {
         if constexpr (kGate) {
             if constexpr (kKind == FFN_GATE_KEEP) {
                 *reinterpret_cast<f32x4_t*>(gu + e4 * 256) = s[0][e4];
-                *reinterpret_cast<f32x4_t*>(gu + 1024 + e4 * 256) = s[1][e4];
+                *reinterpret_cast<f32x4_t*>(up + e4 * 256) = s[1][e4];
             }
             f32x4_t h;
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
                 float f, df;
-                act_fast(s[0][e4][c], a.act, &f, &df);
+                activate(s[0][e4][c], &f, &df);
                 h[c] = f * s[1][e4][c];
             }
             store(out + 8 * e4, h);
         } else if constexpr (kGrad) {
-            const f32x4_t g = *reinterpret_cast<const f32x4_t*>(gu + e4 * 256), u = *reinterpret_cast<const f32x4_t*>(gu + 1024 + e4 * 256);
+            const f32x4_t g = *reinterpret_cast<const f32x4_t*>(gu + e4 * 256), u = *reinterpret_cast<const f32x4_t*>(up + e4 * 256);
             f32x4_t dg, du;
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
                 float f, df;
-                act_fast(g[c], a.act, &f, &df);
+                activate(g[c], &f, &df);
                 du[c] = s[0][e4][c] * f;
                 dg[c] = s[0][e4][c] * u[c] * df;
             }
@@ -480,15 +503,17 @@ struct Plan {
 int slices_of(int32_t K) { return std::max(1, (K + BK - 1) / BK); }
 int parts_of(int slices, int splits) { return (slices + (slices + splits - 1) / splits - 1) / ((slices + splits - 1) / splits); }
 
-int64_t tiles_of(const FfnProduct& p, const Tile& t, bool parts) {
+template <typename T>
+int64_t tiles_of(const FfnProduct<T>& p, const Tile& t, bool parts) {
     // (parts of g | u are those of one matrix of 2 N rows: gate and up meet in the join)
     const int64_t cols = p.gated() ? (parts ? 2 * static_cast<int64_t>(p.N) : p.N) : p.N;
     const int per = p.gated() && !parts ? t.bn / 2 : t.bn;
     return static_cast<int64_t>((p.M + t.bm - 1) / t.bm) * ((cols + per - 1) / per);
 }
 
-size_t part_bytes(const FfnProduct& p, int splits) {
-    return splits == 1 ? 0 : static_cast<size_t>(splits) * ((p.M + 31) / 32) * (p.N / 32) * (p.gated() ? 2 : 1) * 4096;
+template <typename T>
+size_t part_bytes(const FfnProduct<T>& p, int splits) {
+    return splits == 0 ? 0 : static_cast<size_t>(splits) * ((p.M + 31) / 32) * (p.N / 32) * (p.gated() ? 2 : 1) * 4096;
 }
 
 // Times of a workgroup, us: a launch; a slice of 64 k with all compute units at work, and with nothing in the way but its loads' latency;
@@ -508,7 +533,7 @@ constexpr TileTime kTileTimes[] = {{{256, 256}, 0.46, 1.15, 0.58, 7.6, 8.8, 16.0
 constexpr int kUnits = 256;          // compute units; not asked of the device, as a workspace's size must not depend on which is current
 constexpr int kMinPart = 4;          // slices of a part of K
 
-Plan plan_of(const FfnProduct* p, int n) {
+Plan plan_of(const FfnProduct<bf16_t>* p, int n) {
     Plan best{{128, 128}, {1, 1}};
     double best_time = 0.0;
     const FfnKind kind = p[0].kind;
@@ -541,24 +566,92 @@ Plan plan_of(const FfnProduct* p, int n) {
     return best;
 }
 
-template <FfnKind kKind>
-int32_t launch_join(const FfnProduct& p, const float* part, int splits, hipStream_t s) {
+template <FfnKind kKind, typename T>
+int32_t launch_join_kernel(const FfnProduct<T>& p, const float* part, int splits, hipStream_t s) {
     const int64_t blocks = static_cast<int64_t>((p.M + 31) / 32) * (p.N / 32);
-    hipLaunchKernelGGL(ffn_join_kernel<kKind>, dim3(static_cast<uint32_t>((blocks + 3) / 4)), dim3(256), 0, s,
-                       Join{part, p.gu, p.out, p.ldo, p.M, p.N, splits, p.act});
+    hipLaunchKernelGGL((ffn_join_kernel<kKind, T>), dim3(static_cast<uint32_t>((blocks + 3) / 4)), dim3(256), 0, s,
+                       Join<T>{part, p.gu, p.out, p.ldo, p.M, p.N, splits, p.act});
     return launch_ok() ? FREE_OK : FREE_ERR_HIP;
 }
 
-}  // namespace
-
-size_t ffn_products_part_bytes(const FfnProduct* p, int n) {
-    const Plan plan = plan_of(p, n);
-    if (n == 1 || (plan.splits[0] == 1 && plan.splits[1] == 1)) return part_bytes(p[0], plan.splits[0]);
-    return static_cast<size_t>(plan.splits[0]) * (p[0].M / 32) * (p[0].N / 32) * 4096 +
-           static_cast<size_t>(plan.splits[1]) * (p[1].M / 32) * (p[1].N / 32) * 4096;
+template <typename T>
+int32_t launch_join(const FfnProduct<T>& p, FfnKind kind, const float* part, int splits, hipStream_t s) {
+    switch (kind) {
+        case FFN_GATE: return launch_join_kernel<FFN_GATE>(p, part, splits, s);
+        case FFN_GATE_KEEP: return launch_join_kernel<FFN_GATE_KEEP>(p, part, splits, s);
+        case FFN_GATE_GRAD: return launch_join_kernel<FFN_GATE_GRAD>(p, part, splits, s);
+        default: return launch_join_kernel<FFN_ROWS>(p, part, splits, s);
+    }
 }
 
-int32_t launch_ffn_products(const FfnProduct* p, int n, float* part, hipStream_t s) {
+// fp32: tile and parts by the times of gemm_f32.hip's tiles
+struct PlanF32 {
+    bool large;
+    int splits;
+};
+constexpr int kSliceF32 = 32, kMinPartF32 = 8;
+
+bool join_anyway(FfnKind k) { return k == FFN_GATE || k == FFN_GATE_KEEP || k == FFN_GATE_GRAD; }
+
+PlanF32 plan_of(const FfnProduct<float>& p) {
+    PlanF32 best{false, 1};
+    double best_time = 0.0;
+    const int all = std::max(1, (p.K + kSliceF32 - 1) / kSliceF32);
+    const int64_t cols = p.gated() ? 2 * static_cast<int64_t>(p.N) : p.N;
+    for (const int want : {1, 2, 3, 4, 6, 8, 12, 16}) {
+        const int splits = parts_of(all, std::min(want, all)), slices = (all + splits - 1) / splits;
+        if (want > 1 && slices < kMinPartF32) break;
+        for (const bool large : {false, true}) {
+            const int b = large ? 128 : 64;
+            const int64_t work = static_cast<int64_t>((p.M + b - 1) / b) * ((cols + b - 1) / b) * splits;
+            double time = product_f32_time(large, work, slices);
+            if (splits > 1) time += (join_anyway(p.kind) ? 0.0 : 4.8) + 0.27 * splits + 0.18e-6 * static_cast<double>(part_bytes(p, splits));
+            if (best_time == 0.0 || time < best_time) {
+                best_time = time;
+                best = PlanF32{large, splits};
+            }
+        }
+    }
+    return best;
+}
+
+// parts in `part`, not in the place of the result (one part of a kept [g | u] is what is kept)
+bool needs_room(const FfnProduct<float>& p, int splits) { return splits > 1 || p.kind == FFN_GATE || p.kind == FFN_GATE_GRAD; }
+
+}  // namespace
+
+size_t ffn_products_part_bytes(const FfnProduct<bf16_t>* p, int n) {
+    const Plan plan = plan_of(p, n);
+    if (plan.splits[0] == 1 && (n == 1 || plan.splits[1] == 1)) return 0;
+    return part_bytes(p[0], plan.splits[0]) + (n == 2 ? part_bytes(p[1], plan.splits[1]) : 0);
+}
+
+size_t ffn_products_part_bytes(const FfnProduct<float>* p, int n) {
+    size_t most = 0;
+    for (int i = 0; i < n; ++i) {
+        const int splits = plan_of(p[i]).splits;
+        if (needs_room(p[i], splits)) most = std::max(most, part_bytes(p[i], splits));
+    }
+    return most;
+}
+
+int32_t launch_ffn_products(const FfnProduct<float>* p, int n, float* part, hipStream_t s) {
+    for (int i = 0; i < n; ++i) {
+        const FfnProduct<float>& q = p[i];
+        const PlanF32 plan = plan_of(q);
+        const bool blocks = plan.splits > 1 || join_anyway(q.kind);
+        float* const to = !blocks ? q.out : needs_room(q, plan.splits) ? part : q.gu;
+        const bool x_by_k = q.kind == FFN_K_BY_K, w_by_k = x_by_k || q.kind == FFN_ROWS_BY_K || q.kind == FFN_GATE_GRAD;
+        int32_t st = launch_product_f32(x_by_k, w_by_k, plan.large, q.X, q.ldx, q.W, q.ldw, q.M, q.gated() ? 2 * q.N : q.N, q.K, plan.splits,
+                                        blocks, to, s);
+        // (what is kept already is not written again)
+        if (st == FREE_OK && blocks) st = launch_join(q, to == q.gu ? FFN_GATE : q.kind, to, plan.splits, s);
+        if (st != FREE_OK) return st;
+    }
+    return FREE_OK;
+}
+
+int32_t launch_ffn_products(const FfnProduct<bf16_t>* p, int n, float* part, hipStream_t s) {
     const Plan plan = plan_of(p, n);
     const Tile t = plan.tile;
     const bool parts = plan.splits[0] > 1 || (n == 2 && plan.splits[1] > 1);
@@ -614,13 +707,7 @@ int32_t launch_ffn_products(const FfnProduct* p, int n, float* part, hipStream_t
         default: return FREE_ERR_RANGE;
     }
     for (int i = 0; i < n && st == FREE_OK; ++i) {
-        const float* from = la.p[i].part;
-        switch (p[i].kind) {
-            case FFN_GATE: st = launch_join<FFN_GATE>(p[i], from, plan.splits[i], s); break;
-            case FFN_GATE_KEEP: st = launch_join<FFN_GATE_KEEP>(p[i], from, plan.splits[i], s); break;
-            case FFN_GATE_GRAD: st = launch_join<FFN_GATE_GRAD>(p[i], from, plan.splits[i], s); break;
-            default: st = launch_join<FFN_ROWS>(p[i], from, plan.splits[i], s); break;
-        }
+        st = launch_join(p[i], p[i].kind, la.p[i].part, plan.splits[i], s);
     }
     return st;
 }

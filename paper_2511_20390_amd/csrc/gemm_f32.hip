@@ -59,11 +59,22 @@ __device__ __forceinline__ void unrolled(F&& f, std::integer_sequence<int, I...>
     (f(std::integral_constant<int, I>{}), ...);
 }
 
-template <int BM, int BN, int SETS, int EPI>
+// Plain products without a bias, for ffn.hip: the result row by row, or sums over parts of K as 32 x 32 blocks in the accumulators' order.
+// An operand may be K-major (XK, WK: rows of k): a thread's four k of a row are then four loads of a lane's column each, 64 columns next
+// to each other, and the last slice ends where the matrix does.
+constexpr int FREE_EPI_STORE = 8;
+constexpr bool plain_product(int epi) { return epi == FREE_EPI_STORE || epi == FREE_EPI_PARTIAL; }
+struct PlainOperands {
+    int64_t ldx = 0, ldw = 0;                // K-major: values from k to k
+    int32_t part_slices = 0;
+};
+
+template <int BM, int BN, int SETS, int EPI, bool XK = false, bool WK = false>
 __global__ __launch_bounds__(kWaves * 64) void gemm_f32_kernel(
     const float* __restrict__ X, const float* __restrict__ W, const float* __restrict__ bias, int32_t M, int32_t N, int32_t K,
     int32_t tiles_m, int32_t tiles_n, int32_t group_m, int32_t vec_ok, float* __restrict__ out, float* __restrict__ resid,
-    RowVec gate) {
+    RowVec gate, PlainOperands plain) {
+    constexpr bool kParts = EPI == FREE_EPI_PARTIAL;
     constexpr int NW = kWaves, NT = NW * 64;
     constexpr int TM = BM / 64, TN = BN / 64;                           // 32 x 32 blocks of a wavefront
     constexpr int kRows = BM + BN, kPlane = kRows * kPlaneRow, kStage = 3 * kPlane;
@@ -72,12 +83,15 @@ __global__ __launch_bounds__(kWaves * 64) void gemm_f32_kernel(
     extern __shared__ __attribute__((aligned(16))) char lds[];
 
     int tile_m, tile_n;
-    tile_coords(group_m, blockIdx.x, tiles_m, tiles_n, &tile_m, &tile_n);
+    const int split = kParts ? blockIdx.x / (tiles_m * tiles_n) : 0;
+    tile_coords(group_m, kParts ? blockIdx.x % (tiles_m * tiles_n) : blockIdx.x, tiles_m, tiles_n, &tile_m, &tile_n);
     const int m0 = tile_m * BM, n0 = tile_n * BN;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int ks = wave >> 2, wm = (wave >> 1) & 1, wn = wave & 1;
     const int l32 = lane & 31, lhi = lane >> 5;
-    const int nk = K / kSlice;
+    const int all_slices = XK || WK ? (K + kSlice - 1) / kSlice : K / kSlice;
+    const int kt0 = kParts ? split * plain.part_slices : 0;             // this part's first slice; kt counts from there
+    const int nk = kParts ? std::min(plain.part_slices, all_slices - kt0) : all_slices;
 
     // ---- loads: group i of this thread is row 8 (i NW + wave) + lane / 8 of the tile (X rows, then W rows), values
     // 4 (lane % 8) .. + 3 of the slice: the lanes walk whole lines.  Rows past the end of a matrix read as zero; a slice past the end
@@ -89,14 +103,31 @@ __global__ __launch_bounds__(kWaves * 64) void gemm_f32_kernel(
         const_cast<float*>(W + static_cast<int64_t>(n0) * K), 0, static_cast<int>(std::min<int64_t>(w_left, 0x7fffffff)), 0x00020000);
     const int voff = (lane >> 3) * K * 4 + (lane & 7) * 16;
     f32x4_t reg[SETS][UP];                                              // slice k goes through set k % SETS
+    // K-major: group i is column 64 i + lane (of X, or of W), values 4 wave .. + 3 of the slice; past the end of the matrix zero.  The
+    // descriptor starts at the slice: offsets stay small whatever K is.
+    auto fetch_column = [&](const float* base, int64_t ld, int first, int kt, f32x4_t& v, int i) {
+        const int64_t k = static_cast<int64_t>(kt0 + kt) * kSlice, left = ((K - k) * ld - first) * 4;
+        const __amdgpu_buffer_rsrc_t srd = __builtin_amdgcn_make_buffer_rsrc(
+            const_cast<float*>(base + (left > 0 ? k * ld + first : 0)), 0, static_cast<int>(left < 0 ? 0 : std::min<int64_t>(left, 0x7fffffff)), 0x00020000);
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+            v[c] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(srd, (64 * i + lane) * 4, (4 * wave + c) * static_cast<int>(ld) * 4, 0));
+    };
     auto fetch = [&](int kt, auto set_c, int i) {
         constexpr int set = decltype(set_c)::value;
-        const int soff = 8 * ((i < UX ? i : i - UX) * NW + wave) * K * 4 + kt * kRowBytes;
+        if constexpr (XK) {
+            if (i < UX) return fetch_column(X, plain.ldx, m0, kt, reg[set][i], i);
+        }
+        if constexpr (WK) {
+            if (i >= UX) return fetch_column(W, plain.ldw, n0, kt, reg[set][i], i - UX);
+        }
+        const int soff = 8 * ((i < UX ? i : i - UX) * NW + wave) * K * 4 + (kt0 + kt) * kRowBytes;
         const u32x4_t v = __builtin_amdgcn_raw_buffer_load_b128(i < UX ? xsrd : wsrd, voff, soff, 0);
         reg[set][i] = __builtin_bit_cast(f32x4_t, v);
     };
     // (row / 4) % 4 of this lane's rows is 2 (wave % 2) + lane / 32
     const int st_off = (8 * wave + (lane >> 3)) * kPlaneRow + ((((lane >> 1) & 3) ^ (((wave & 1) << 1) | (lane >> 5))) << 4) + ((lane & 1) << 3);
+    [[maybe_unused]] const int st_column = lane * kPlaneRow + (((wave >> 1) ^ ((lane >> 2) & 3)) << 4) + ((wave & 1) << 3);
     u32x2_t part[3];
     // half c of the cutting of group i; the second one stores it to its stage and requests the group of slice kt + SETS
     auto stash = [&](int kt, auto set_c, int i, int c) {
@@ -106,7 +137,7 @@ __global__ __launch_bounds__(kWaves * 64) void gemm_f32_kernel(
 #pragma unroll
         for (int p = 0; p < 3; ++p) part[p][c] = two[p];
         if (c == 0) return;
-        char* dst = lds + (kt & 1) * kStage + 8 * i * NW * kPlaneRow + st_off;
+        char* dst = lds + (kt & 1) * kStage + 8 * i * NW * kPlaneRow + ((i < UX ? XK : WK) ? st_column : st_off);
 #pragma unroll
         for (int p = 0; p < 3; ++p) *reinterpret_cast<u32x2_t*>(dst + p * kPlane) = part[p];
         fetch(kt + SETS, set_c, i);
@@ -255,8 +286,21 @@ __global__ __launch_bounds__(kWaves * 64) void gemm_f32_kernel(
                 f32x16_t acc;
 #pragma unroll
                 for (int e = 0; e < 16; ++e) acc[e] = 0.f;
-                for (int k = 0; k < K; k += 8) {
-                    const f32x4_t xv = *reinterpret_cast<const f32x4_t*>(xr + k), wv = *reinterpret_cast<const f32x4_t*>(wr + k);
+                const int k_end = kParts ? std::min(K, (kt0 + nk) * kSlice) : K;
+                for (int k = kt0 * kSlice; k < k_end; k += 8) {
+                    f32x4_t xv, wv;
+                    if constexpr (XK) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) xv[e] = k + 4 * lhi + e < K ? X[static_cast<int64_t>(k + 4 * lhi + e) * plain.ldx + gm] : 0.f;
+                    } else {
+                        xv = *reinterpret_cast<const f32x4_t*>(xr + k);
+                    }
+                    if constexpr (WK) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) wv[e] = k + 4 * lhi + e < K ? W[static_cast<int64_t>(k + 4 * lhi + e) * plain.ldw + gn] : 0.f;
+                    } else {
+                        wv = *reinterpret_cast<const f32x4_t*>(wr + k);
+                    }
 #pragma unroll
                     for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(wv[e], xv[e], acc, 0, 0, 0);
                 }
@@ -269,6 +313,25 @@ __global__ __launch_bounds__(kWaves * 64) void gemm_f32_kernel(
 #pragma unroll
                             for (int e = 0; e < 16; ++e) hi[a][b][e] = needs(hi[a][b][e]) ? acc[e] : hi[a][b][e];
             }
+    }
+    if constexpr (plain_product(EPI)) {
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+            for (int j = 0; j < TN; ++j) {
+                const int gm0 = m0 + (wm * TM + i) * 32, gn0 = n0 + (wn * TN + j) * 32;
+                if (gm0 >= M || gn0 >= N) continue;
+                const int64_t blocks_m = (M + 31) / 32, blocks_n = (N + 31) / 32;
+                float* block = out + ((split * blocks_m + gm0 / 32) * blocks_n + gn0 / 32) * 1024 + lane * 4;
+                float* row = out + static_cast<int64_t>(gm0 + l32) * N + gn0 + 4 * lhi;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const f32x4_t v = {hi[i][j][4 * q], hi[i][j][4 * q + 1], hi[i][j][4 * q + 2], hi[i][j][4 * q + 3]};
+                    if constexpr (kParts) *reinterpret_cast<f32x4_t*>(block + q * 256) = v;
+                    else if (gm0 + l32 < M && gn0 + 8 * q + 4 * lhi < N) *reinterpret_cast<f32x4_t*>(row + 8 * q) = v;
+                }
+            }
+        return;
     }
     float ln_scale[TM];                                                 // (used by the folded-LayerNorm epilogues only)
 #pragma unroll
@@ -298,7 +361,7 @@ int32_t launch_one(const Args& a) {
     // tile order as in gemm_pipe.hip; with few rows all row tiles of a column, so that a weight panel is fetched by one XCD
     int group_m = total <= 2 * device_cus() ? tiles_m : BM > BN ? 4 : 8;
     hipLaunchKernelGGL(kern, dim3(total), dim3(kWaves * 64), lds, a.s, a.X, a.W, a.bias, a.M, a.N, a.K, tiles_m, tiles_n, group_m,
-                       vec ? 1 : 0, a.out, a.resid, a.gate);
+                       vec ? 1 : 0, a.out, a.resid, a.gate, PlainOperands{});
     return launch_ok() ? FREE_OK : FREE_ERR_HIP;
 }
 
@@ -312,7 +375,49 @@ int32_t launch_tile(const Args& a, int32_t epi) {
     }
 }
 
+template <int B, int SETS, int EPI, bool XK, bool WK>
+int32_t launch_plain(const float* X, const float* W, int32_t M, int32_t N, int32_t K, const PlainOperands& o, int parts, float* out, hipStream_t s) {
+    const int tiles_m = (M + B - 1) / B, tiles_n = (N + B - 1) / B, total = tiles_m * tiles_n;
+    const size_t lds = 4 * static_cast<size_t>(B) * 3 * kPlaneRow;
+    auto kern = gemm_f32_kernel<B, B, SETS, EPI, XK, WK>;
+    static LdsLimit limit;
+    if (!limit.allow(reinterpret_cast<const void*>(kern), lds)) return FREE_ERR_HIP;
+    const int group_m = total <= 2 * device_cus() ? tiles_m : 8;
+    hipLaunchKernelGGL(kern, dim3(total * parts), dim3(kWaves * 64), lds, s, X, W, nullptr, M, N, K, tiles_m, tiles_n, group_m, 1, out, nullptr,
+                       RowVec{nullptr, 0, 1}, o);
+    return launch_ok() ? FREE_OK : FREE_ERR_HIP;
+}
+
+template <bool XK, bool WK>
+int32_t launch_layout(bool large, const float* X, const float* W, int32_t M, int32_t N, int32_t K, const PlainOperands& o, int parts, bool blocks,
+                      float* out, hipStream_t s) {
+    if (blocks)
+        return large ? launch_plain<128, 2, FREE_EPI_PARTIAL, XK, WK>(X, W, M, N, K, o, parts, out, s)
+                     : launch_plain<64, 4, FREE_EPI_PARTIAL, XK, WK>(X, W, M, N, K, o, parts, out, s);
+    return large ? launch_plain<128, 2, FREE_EPI_STORE, XK, WK>(X, W, M, N, K, o, 1, out, s)
+                 : launch_plain<64, 4, FREE_EPI_STORE, XK, WK>(X, W, M, N, K, o, 1, out, s);
+}
+
+// us of a launch of `work` tiles of 64 x 64 or 128 x 128 and nk slices each on `cus` compute units; see launch_linear_f32
+double tile_time(bool large, double work, double nk, double cus) {
+    const double rounds = std::ceil(work / cus);
+    return large ? rounds * (7.5 + 1.455 * nk) : 4.4 + nk * (rounds <= 1.0 ? 0.526 : 0.499 * rounds);
+}
+
 }  // namespace
+
+double product_f32_time(bool large, int64_t work, int32_t slices) { return tile_time(large, static_cast<double>(work), slices, 256.0); }
+
+int32_t launch_product_f32(bool x_by_k, bool w_by_k, bool large, const float* X, int64_t ldx, const float* W, int64_t ldw, int32_t M, int32_t N,
+                           int32_t K, int32_t parts, bool blocks, float* out, hipStream_t s) {
+    PlainOperands o;
+    o.ldx = ldx;
+    o.ldw = ldw;
+    o.part_slices = ((K + kSlice - 1) / kSlice + parts - 1) / parts;
+    if (x_by_k) return launch_layout<true, true>(large, X, W, M, N, K, o, parts, blocks, out, s);
+    return w_by_k ? launch_layout<false, true>(large, X, W, M, N, K, o, parts, blocks, out, s)
+                  : launch_layout<false, false>(large, X, W, M, N, K, o, parts, blocks, out, s);
+}
 
 bool linear_f32_covers(const float* X, const float* W, int32_t M, int32_t N, int32_t K) {
     // whole slices of 16-byte aligned rows; 32-bit byte offsets inside a tile and three slices past the end of its rows
@@ -333,9 +438,8 @@ int32_t launch_linear_f32(const float* X, const float* W, const float* bias, int
     if (!linear_f32_covers(X, W, M, N, K)) return FREE_ERR_SHAPE;
     const Args a{X, W, bias, M, N, K, out, resid, gate, s};
     const double cus = std::max(1, device_cus() / std::max(1, cu_share)), nk = K / kSlice;
-    const auto rounds = [&](int b) { return std::ceil(static_cast<double>((M + b - 1) / b) * ((N + b - 1) / b) / cus); };
-    const double n64 = rounds(64), t64 = 4.4 + nk * (n64 <= 1.0 ? 0.526 : 0.499 * n64), t128 = rounds(128) * (7.5 + 1.455 * nk);
-    return t64 <= t128 ? launch_tile<64, 64, 4>(a, epi) : launch_tile<128, 128, 2>(a, epi);
+    const auto time = [&](int b) { return tile_time(b == 128, static_cast<double>((M + b - 1) / b) * ((N + b - 1) / b), nk, cus); };
+    return time(64) <= time(128) ? launch_tile<64, 64, 4>(a, epi) : launch_tile<128, 128, 2>(a, epi);
 }
 
 }  // namespace freemi
