@@ -22,25 +22,40 @@ namespace {
 
 constexpr int kThreads = 256;
 
-// dst [rows_to, cols_to] = src [rows, cols], cropped or filled with zeros; elements of 2 or 4 bytes
+// dst [rows_to, cols_to] = src [rows, cols], cropped or filled with zeros; elements of 2 or 4 bytes.  A thread has 16 bytes of a row, at
+// whatever address; rows over blockIdx.y.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void ffn_fit_kernel(const T* src, int32_t rows, int32_t cols, T* dst, int32_t rows_to, int32_t cols_to) {
-    const int64_t total = static_cast<int64_t>(rows_to) * cols_to;
-    for (int64_t i = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x; i < total; i += static_cast<int64_t>(gridDim.x) * kThreads) {
-        const int64_t r = i / cols_to, c = i - r * cols_to;
-        dst[i] = r < rows && c < cols ? src[r * cols + c] : T(0);
+    constexpr int E = 16 / sizeof(T);
+    const int c = (blockIdx.x * kThreads + threadIdx.x) * E;
+    if (c >= cols_to) return;
+    for (int64_t r = blockIdx.y; r < rows_to; r += gridDim.y) {
+        const T* from = src + r * cols + c;
+        T* to = dst + r * cols_to + c;
+        const int n = r < rows ? cols - c : 0, m = cols_to - c;  // values there are, and are wanted, from c on
+        T v[E];
+        if (n >= E) {
+            __builtin_memcpy(v, from, 16);
+        } else {
+#pragma unroll
+            for (int e = 0; e < E; ++e) v[e] = e < n ? from[e] : T(0);
+        }
+        if (m >= E) {
+            __builtin_memcpy(to, v, 16);
+        } else {
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                if (e < m) to[e] = v[e];
+        }
     }
 }
-
-constexpr int kMaxBlocks = 1 << 16;
-
-int grid_of(int64_t items) { return static_cast<int>(std::max<int64_t>(1, std::min<int64_t>((items + kThreads - 1) / kThreads, kMaxBlocks))); }
 
 template <typename T>
 int32_t fit(const T* src, int32_t rows, int32_t cols, T* dst, int32_t rows_to, int32_t cols_to, hipStream_t s) {
     using U = typename std::conditional<sizeof(T) == 2, uint16_t, uint32_t>::type;
-    hipLaunchKernelGGL(ffn_fit_kernel<U>, dim3(grid_of(static_cast<int64_t>(rows_to) * cols_to)), dim3(kThreads), 0, s, reinterpret_cast<const U*>(src),
-                       rows, cols, reinterpret_cast<U*>(dst), rows_to, cols_to);
+    const dim3 grid((cols_to + kThreads * 16 / sizeof(T) - 1) / (kThreads * 16 / sizeof(T)), std::min(rows_to, 65535));
+    hipLaunchKernelGGL(ffn_fit_kernel<U>, grid, dim3(kThreads), 0, s, reinterpret_cast<const U*>(src), rows, cols, reinterpret_cast<U*>(dst), rows_to,
+                       cols_to);
     return launch_ok() ? FREE_OK : FREE_ERR_HIP;
 }
 
