@@ -728,29 +728,37 @@ def op_ln_modulate(x, shift, scale, rows_per_sample: int, mode: str):
 
 
 # ---- operators of rotary, gated blocks and of their training ------------------------------------------------------
+_ELEMENTS = {}                      # torch element type -> FREE_FP32 / FREE_BF16
+
+
 def _mode_of(t, name):
     """FREE_FP32 or FREE_BF16, by a tensor's element type."""
-    import torch
-    if t.dtype == torch.bfloat16:
-        return FREE_BF16
-    if t.dtype == torch.float32:
-        return FREE_FP32
-    raise FreeError(FREE_ERR_DTYPE, f"{name}: element type {t.dtype}, expected float32 or bfloat16")
+    mode = _ELEMENTS.get(t.dtype)
+    if mode is None:
+        if not _ELEMENTS:
+            import torch
+            _ELEMENTS.update({torch.float32: FREE_FP32, torch.bfloat16: FREE_BF16})
+            return _mode_of(t, name)
+        raise FreeError(FREE_ERR_DTYPE, f"{name}: element type {t.dtype}, expected float32 or bfloat16")
+    return mode
 
 
 def _same_device(first, *others):
-    """The device the call runs on, whatever the current one is: that of its tensors, which have to agree."""
+    """Index of the device the call runs on, whatever the current one is: that of its tensors, which have to agree."""
+    index = first.get_device()
     for t in others:
-        if t is not None and t.device != first.device:
+        if t is not None and t.get_device() != index:
             raise FreeError(FREE_ERR_SHAPE, f"tensors on {first.device} and {t.device}")
-    return first.device
+    return index
 
 
 def _enqueue(fn, where, device, *args):
-    """fn(*args, stream) on the current stream of `device`."""
+    """fn(*args, stream) on the current stream of the device of that index.  (A call on a few rows is bound by its submission: 9.5 us of
+    which 4 are the library's and the runtime's; the bare handle as in _stream, one look at the current device.)"""
     import torch
-    if device.index == torch.cuda.current_device():
-        st = fn(*args, _stream())
+    if device == torch.cuda.current_device():
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        st = fn(*args, _stream() if raw is None else raw(device))
     else:
         with torch.cuda.device(device):
             st = fn(*args, _stream())
@@ -760,14 +768,13 @@ def _enqueue(fn, where, device, *args):
 
 def _vectors(t, name, samples, D):
     """Address and sample stride of per-sample vectors [samples, D] (one sample: [D] too), rows dense, any distance apart."""
-    import torch
     if t is None:
         return None, 0
     if not t.is_cuda:
         raise FreeError(FREE_ERR_NULL, f"{name}: not a device tensor")
-    if t.dtype != torch.float32:
+    if _mode_of(t, name) != FREE_FP32:
         raise FreeError(FREE_ERR_DTYPE, f"{name}: element type {t.dtype}, expected float32")
-    if tuple(t.shape) != (samples, D) and not (samples == 1 and tuple(t.shape) == (D,)):
+    if t.shape != (samples, D) and not (samples == 1 and t.shape == (D,)):
         raise FreeError(FREE_ERR_SHAPE, f"{name}: shape {tuple(t.shape)}, expected {(samples, D)}")
     if D > 1 and t.stride(-1) != 1:
         raise FreeError(FREE_ERR_SHAPE, f"{name}: values of a row are not next to each other")
@@ -833,6 +840,9 @@ def op_layer_norm_backward(dout, x, weight=None, rows_per_sample: int = None, mo
     return out
 
 
+_DIMS = [C.c_int32 * max(n, 1) for n in range(5)]
+
+
 def op_rope_axes(x, pos, heads: int, dh: int, axis_dims, theta: float = 10000.0, pairing: int = ROPE_PAIRS, inverse: bool = False,
                  out=None):
     """Rotary positions over len(axis_dims) axes.  x [rows, heads * dh], values of a row next to each other, rows any distance apart (the
@@ -855,7 +865,7 @@ def op_rope_axes(x, pos, heads: int, dh: int, axis_dims, theta: float = 10000.0,
         if width > 1 and t.stride(1) != 1:
             raise FreeError(FREE_ERR_SHAPE, f"{name}: values of a row are not next to each other")
     dev = _same_device(x, pos, out)
-    dims = (C.c_int32 * max(axes, 1))(*axis_dims)
+    dims = _DIMS[axes](*axis_dims) if axes < len(_DIMS) else (C.c_int32 * axes)(*axis_dims)
     _enqueue(load().free_op_rope_axes, "free_op_rope_axes", dev, x.data_ptr(), x.stride(0), _addr(pos, torch.int32, "pos"), pos.shape[0],
              rows, heads, dh, axes, dims, float(theta), int(pairing), int(bool(inverse)), _mode_of(x, "x"), out.data_ptr(), out.stride(0))
     return out

@@ -101,7 +101,7 @@ int32_t free_op_gated_ffn(const void* x, const void* w_in, const void* w_out, in
     if (!x || !w_in || !w_out || !out) return FREE_ERR_NULL;
     if (!aligned(x, 16) || !aligned(w_in, 16) || !aligned(w_out, 16) || !aligned(out, 16)) return FREE_ERR_SHAPE;
     if (saved && (!aligned(saved, 256) || saved_bytes < ffn_saved_bytes(M, D, F, dtype))) return FREE_ERR_WORKSPACE;
-    st = check_workspace(workspace, ws_bytes, ffn_workspace_bytes(M, D, F, dtype, false));
+    st = check_workspace(workspace, ws_bytes, ffn_forward_bytes(M, D, F, dtype, saved != nullptr));
     if (st != FREE_OK) return st;
     return launch_ffn_forward(x, w_in, w_out, M, D, F, dtype, act, out, saved, workspace, static_cast<hipStream_t>(stream));
 }

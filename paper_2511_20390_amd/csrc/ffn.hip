@@ -187,8 +187,12 @@ int32_t products_backward(const Sizes& z, const T* dy, const T* x, const T* w_in
     return launch_ffn_products(p.weights, 2, w.room, s);
 }
 
+// the way of few rows, which keeps nothing and needs room for h alone
+bool few_rows(const Sizes& z, bool keep) { return !keep && ffn_rows_pay(z.M, z.D, z.F, z.es == 2 ? FREE_BF16 : FREE_FP32); }
+
 template <typename T>
 int32_t forward_of(const Sizes& z, const T* x, const T* w_in, const T* w_out, int32_t act, T* out, char* saved, char* ws, hipStream_t s) {
+    if (few_rows(z, saved != nullptr)) return launch_ffn_rows(x, w_in, w_out, z.M, z.D, z.F, act, reinterpret_cast<T*>(ws), out, s);
     const ForwardSpace<T> w(z, ws);
     float* gu = nullptr;
     T* h = w.h;
@@ -197,7 +201,6 @@ int32_t forward_of(const Sizes& z, const T* x, const T* w_in, const T* w_out, in
         gu = k.gu;
         h = k.h;
     }
-    if (!saved && ffn_rows_pay(z.M, z.D, z.F, z.es == 2 ? FREE_BF16 : FREE_FP32)) return launch_ffn_rows(x, w_in, w_out, z.M, z.D, z.F, act, h, out, s);
     T* y = out;
     if (z.padded) {
         FREE_STEP(fit(x, z.M, z.D, w.x, z.M, z.Dp, s));
@@ -254,6 +257,11 @@ size_t ffn_workspace_bytes(int32_t M, int32_t D, int32_t F, int32_t dtype, bool 
     const size_t f = z.es == 2 ? ForwardSpace<bf16_t>(z, nullptr).bytes : ForwardSpace<float>(z, nullptr).bytes;
     const size_t b = z.es == 2 ? BackwardSpace<bf16_t>(z, nullptr).bytes : BackwardSpace<float>(z, nullptr).bytes;
     return backward ? std::max(f, b) : f;
+}
+
+size_t ffn_forward_bytes(int32_t M, int32_t D, int32_t F, int32_t dtype, bool keep) {
+    const Sizes z(M, D, F, dtype);
+    return few_rows(z, keep) ? z.act_bytes(z.F) : ffn_workspace_bytes(M, D, F, dtype, false);
 }
 
 int32_t launch_ffn_forward(const void* x, const void* w_in, const void* w_out, int32_t M, int32_t D, int32_t F, int32_t dtype, int32_t act,

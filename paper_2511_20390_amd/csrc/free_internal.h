@@ -353,6 +353,8 @@ int32_t launch_rope(const void* x, int64_t x_stride, const int32_t* pos, int32_t
 bool ffn_covers(int32_t M, int32_t D, int32_t F, int32_t dtype);
 size_t ffn_saved_bytes(int32_t M, int32_t D, int32_t F, int32_t dtype);
 size_t ffn_workspace_bytes(int32_t M, int32_t D, int32_t F, int32_t dtype, bool backward);
+// what a forward call that keeps its state, or does not, uses of that workspace
+size_t ffn_forward_bytes(int32_t M, int32_t D, int32_t F, int32_t dtype, bool keep);
 // saved: nullptr, or where the gradient's pass finds what it needs
 int32_t launch_ffn_forward(const void* x, const void* w_in, const void* w_out, int32_t M, int32_t D, int32_t F, int32_t dtype, int32_t act,
                            void* out, void* saved, void* ws, hipStream_t s);
