@@ -515,12 +515,12 @@ int32_t backward_of(const NormArgs& a, const NormGrad& gr, int samples, hipStrea
 }
 
 // Workgroups per sample in the backward pass.  A group of wavefronts takes `passes` rows; all workgroups should run at once or in full
-// rounds (two on every compute unit), since each ends with sums over its wavefronts and a partial row of the weight's gradient that the
+// rounds (two on every compute unit, of eight wavefronts one), since each ends with sums over its wavefronts and a partial row of the weight's gradient that the
 // second launch reads: together some three passes.
 int chunks_of(int32_t M, int32_t D, int32_t rows_per_sample) {
     const int64_t samples = (static_cast<int64_t>(M) + rows_per_sample - 1) / rows_per_sample;
     const int lanes = backward_layout(4, D).lanes, groups = back_threads(lanes) / lanes;
-    const int64_t rows = std::min<int64_t>(M, rows_per_sample), slots = 2 * 256;
+    const int64_t rows = std::min<int64_t>(M, rows_per_sample), slots = back_threads(lanes) > 256 ? 256 : 2 * 256;
     int64_t best = 1, best_cost = INT64_MAX;
     for (int64_t passes = 1; passes <= 64; ++passes) {
         const int64_t chunks = std::min<int64_t>((rows + passes * groups - 1) / (passes * groups), std::max<int64_t>(1, 2 * slots / samples));
