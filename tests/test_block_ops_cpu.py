@@ -120,4 +120,33 @@ def test_binding_refusals():
         with pytest.raises(b.FreeError) as e:
             call()
         assert e.value.status == status, k
-    assert torch.zeros(1).sum() == 0
+
+
+def test_calls_go_to_the_device_of_their_tensors(monkeypatch):
+    """The device and the stream of a call are its tensors', whichever device is current; tensors on two devices are refused."""
+    import contextlib
+    import types
+    torch = pytest.importorskip("torch")
+    seen = []
+    current = [0]
+
+    @contextlib.contextmanager
+    def device(index):
+        before, current[0] = current[0], index
+        yield
+        current[0] = before
+
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: current[0])
+    monkeypatch.setattr(torch.cuda, "device", device)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda dev: 40 + dev, raising=False)
+    fn = lambda *a: seen.append((current[0], a)) or 0
+    b._enqueue(fn, "call", 0, 1, 2)
+    b._enqueue(fn, "call", 3, 1, 2)
+    assert seen == [(0, (1, 2, 40)), (3, (1, 2, 43))] and current[0] == 0
+    on = lambda index: types.SimpleNamespace(get_device=lambda: index, device=f"cuda:{index}")
+    assert b._same_device(on(2), None, on(2)) == 2
+    with pytest.raises(b.FreeError) as e:
+        b._same_device(on(2), on(0))
+    assert e.value.status == b.FREE_ERR_SHAPE
+    with pytest.raises(b.FreeError):
+        b._enqueue(lambda *a: b.FREE_ERR_SHAPE, "call", 0)

@@ -129,6 +129,29 @@ def test_norm_strided_vectors_and_odd_addresses():
             assert (grads[:, rest] == 7.0).all()
 
 
+@pytest.mark.parametrize("M,D,rows", [(1, 5, 1), (300, 130, 300), (300, 1152, 25), (67, 1001, 67), (90, 4100, 90)])
+def test_norm_what_buffers_held(M, D, rows):
+    """A workspace that starts as NaN, and memory behind every output left as it was."""
+    import torch
+    from paper_2511_20390_amd import binding as b
+    g = _gen(19, M, D)
+    n = -(-M // rows)
+    for dt in (torch.float32, torch.bfloat16):
+        x, dy, w, bias = _rnd(g, M, D, dtype=dt), _rnd(g, M, D, dtype=dt), _rnd(g, n, D), _rnd(g, n, D)
+        results = []
+        for fill in (0, 255):
+            ws = torch.full((b.layer_norm_backward_workspace_bytes(M, D, rows),), fill, dtype=torch.uint8, device="cuda")
+            room = [torch.full((k * D + 64,), 7.0, dtype=t, device="cuda") for k, t in ((M, dt), (M, dt), (n, torch.float32), (n, torch.float32))]
+            outs = [r[:-64].view(-1, D) for r in room]
+            b.op_layer_norm(x, w, bias, rows_per_sample=rows, out=outs[0])
+            b.op_layer_norm_backward(dy, x, w, rows_per_sample=rows, out=outs[1:], workspace=ws)
+            for r in room:
+                assert (r[-64:] == 7.0).all()
+            results.append(outs)
+        for a, e in zip(*results):
+            assert torch.equal(a, e) and torch.isfinite(a).all()
+
+
 def test_norm_gradient_in_place():
     import torch
     from paper_2511_20390_amd import binding as b
@@ -346,6 +369,89 @@ def test_ffn_sizes_in_use(M, D, F, act, dtype):
     _ffn_case(M, D, F, act, dtype)
 
 
+# every tile of every product of the two passes, with K whole and in parts: (256 x 256, 128 x 256) down 4100, 9000; in parts 6000, 2060; dx
+# 9000, 6000; in parts 3001, 1500; weights 200 (256), 9000 and 6000 in parts; the gated gradient on 256 x 256 2060; gate and up in parts 33;
+# ragged rows in all of them
+@pytest.mark.parametrize("M,D,F", [(4100, 2048, 1024), (9000, 512, 512), (6000, 320, 6400), (2060, 1152, 4608), (9000, 1536, 2048),
+                                   (6000, 1152, 4608), (3001, 1152, 4608), (1500, 1152, 4608), (200, 1536, 2048), (9000, 256, 1024),
+                                   (6000, 768, 2048), (2060, 320, 6400), (33, 2048, 1024)])
+def test_ffn_tiles(M, D, F):
+    _ffn_case(M, D, F, "silu", "bf16")
+
+
+@pytest.mark.parametrize("M,D,F", [(40, 256, 4096), (600, 1152, 1152), (3000, 128, 512), (2500, 768, 1536), (130, 1024, 64)])
+def test_ffn_tiles_fp32(M, D, F):
+    """64 x 64 and 128 x 128 tiles, K whole and in parts."""
+    _ffn_case(M, D, F, "gelu", "fp32")
+
+
+@pytest.mark.parametrize("scale", [1e-22, 1e-12, 1e15])
+def test_ffn_fp32_scales(scale):
+    """Gradients far below 2^-64, where the three-part products are computed again in fp32, and far above one."""
+    import torch
+    from paper_2511_20390_amd import binding as b
+    from tests import block_ops_util as u
+    g = _gen(16)
+    for M, D, F in ((70, 128, 192), (333, 96, 100), (1000, 384, 512)):
+        x, w_in, w_out = _rnd(g, M, D), _rnd(g, 2 * F, D, std=D ** -0.5), _rnd(g, D, F, std=F ** -0.5)
+        dy = _rnd(g, M, D, std=scale)
+        saved = torch.empty(b.gated_ffn_saved_bytes(M, D, F, "fp32"), dtype=torch.uint8, device="cuda")
+        out = b.op_gated_ffn(x, w_in, w_out, saved=saved)
+        got = (out, *b.op_gated_ffn_backward(dy, x, w_in, w_out, saved))
+        for k, r, name in zip(got, u.ffn_reference(x, w_in, w_out, "silu", dy), ("out", "dx", "dw_in", "dw_out")):
+            u.check(k, r, f"scale {scale} {name}")
+
+
+def test_ffn_gradient_not_finite_rows_stay_alone():
+    """dx has a row per token; what a token's infinite gradient reaches in the weights' gradients is not finite either."""
+    import torch
+    from paper_2511_20390_amd import binding as b
+    g = _gen(17)
+    for dtype in ("bf16", "fp32"):
+        dt = _t(dtype)
+        M, D, F = 90, 128, 192
+        x, w_in, w_out = _rnd(g, M, D, dtype=dt), _rnd(g, 2 * F, D, std=0.1, dtype=dt), _rnd(g, D, F, std=0.1, dtype=dt)
+        dy = _rnd(g, M, D, dtype=dt)
+        saved = torch.empty(b.gated_ffn_saved_bytes(M, D, F, dtype), dtype=torch.uint8, device="cuda")
+        b.op_gated_ffn(x, w_in, w_out, saved=saved)
+        clean = b.op_gated_ffn_backward(dy, x, w_in, w_out, saved)
+        dy[41, 3] = float("inf")
+        dx, dw_in, dw_out = b.op_gated_ffn_backward(dy, x, w_in, w_out, saved)
+        keep = torch.arange(M, device="cuda") != 41
+        assert torch.equal(dx[keep], clean[0][keep]) and not torch.isfinite(dx[41]).any()
+        assert not torch.isfinite(dw_in).any() and not torch.isfinite(dw_out[3]).any()
+        rest = torch.arange(D, device="cuda") != 3
+        assert torch.equal(dw_out[rest], clean[2][rest])
+
+
+@pytest.mark.parametrize("M", [1, 20, 33, 500])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_ffn_what_buffers_held(M, dtype):
+    """Workspaces and kept state that start as NaN, and memory behind every output left as it was; even and padded widths."""
+    import torch
+    from paper_2511_20390_amd import binding as b
+    g = _gen(18, M)
+    dt = _t(dtype)
+    for D, F in ((128, 192), (72, 1100), (33, 65)):
+        x, w_in, w_out = _rnd(g, M, D, dtype=dt), _rnd(g, 2 * F, D, std=0.1, dtype=dt), _rnd(g, D, F, std=0.1, dtype=dt)
+        dy = _rnd(g, M, D, dtype=dt)
+        results = []
+        for fill in (0, 255):
+            byte = lambda n: torch.full((n,), fill, dtype=torch.uint8, device="cuda")
+            ws, saved = byte(b.gated_ffn_workspace_bytes(M, D, F, dtype, True)), byte(b.gated_ffn_saved_bytes(M, D, F, dtype))
+            small = byte(b.gated_ffn_workspace_bytes(M, D, F, dtype))
+            room = [torch.full((n + 64,), 7.0, dtype=dt, device="cuda") for n in (M * D, M * D, M * D, 2 * F * D, D * F)]
+            outs = [r[:r.numel() - 64].view(s) for r, s in zip(room, ((M, D), (M, D), (M, D), (2 * F, D), (D, F)))]
+            b.op_gated_ffn(x, w_in, w_out, out=outs[0], workspace=small)
+            b.op_gated_ffn(x, w_in, w_out, out=outs[1], saved=saved, workspace=small)
+            b.op_gated_ffn_backward(dy, x, w_in, w_out, saved, out=outs[2:], workspace=ws)
+            for r in room:
+                assert (r[-64:] == 7.0).all()
+            results.append(outs)
+        for a, e in zip(*results):
+            assert torch.equal(a, e) and torch.isfinite(a).all()
+
+
 def test_ffn_extreme_gates():
     """Gates far out on both sides: the activation is 0 or the gate, its slope 0 or 1, and nothing is NaN."""
     import torch
@@ -540,6 +646,24 @@ def test_block_in_a_graph(mode):
         torch.cuda.synchronize()
         for a, e in zip(got, block.run()):
             assert torch.equal(a, e), k
+
+
+def test_two_streams_at_once():
+    """Calls in flight on two streams, each with buffers of its own."""
+    import torch
+    blocks = [_Block("bf16", B=8, F=1024, seed=k) for k in range(2)]
+    refs = [k.run() for k in blocks]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in blocks]
+    got = []
+    for _ in range(3):
+        for block, s in zip(blocks, streams):
+            with torch.cuda.stream(s):
+                got.append(block.run())
+    torch.cuda.synchronize()
+    for k, r in enumerate(got):
+        for a, e in zip(r, refs[k % 2]):
+            assert torch.equal(a, e)
 
 
 def test_on_a_side_stream():
