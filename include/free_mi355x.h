@@ -517,8 +517,8 @@ int32_t free_op_linear_ln(const void* z, const void* W, int32_t M, int32_t N, in
  * All of them only enqueue on `stream`, allocate nothing and can be captured in a HIP graph (a workspace belongs to one call at a
  * time: graphs that may run at once need one each).  Equal inputs give equal bits.  dtype, x_dtype: FREE_FP32 or FREE_BF16, the
  * element type of the tensors it is said of.  No rows (M = 0, rows = 0) is not an error: nothing is written but the gradients
- * of weights, which are zero.  Outputs must not overlap inputs except where said.  Infinite or NaN inputs give NaN where a sum or
- * product of theirs does, and nowhere else.
+ * of weights, which are zero.  Outputs must not overlap inputs except where said.  Infinite or NaN inputs make the results that depend
+ * on them infinite or NaN, and no others.
  *
  * Layer norm, affine or modulated, over rows of D values:
  *   xh = (x - mean) / sqrt(var + eps),  out = xh w_s + b_s,  s = row / rows_per_sample
@@ -546,7 +546,7 @@ int32_t free_op_layer_norm_backward(const void* dout, int32_t dtype, const void*
  * 2 heads with the stride of the whole row); out likewise, and it may be x with the same stride.  pos [pos_rows, axes] int32, token row m
  * at m % pos_rows (one grid for all states of a batch); any int32 is a position, and its angle is exact to 2^-30 turns.
  * dh even and <= 256, 1 to 4 axes, theta >= 1.  At most 2^24 workgroups of 256 threads, a thread having up to four heads of one to four
- * pairs (FREE_ERR_LIMIT). */
+ * pairs, and 2^30 threads for one row (FREE_ERR_LIMIT). */
 #define FREE_ROPE_PAIRS  0
 #define FREE_ROPE_HALVES 1
 int32_t free_op_rope_axes(const void* x, int64_t x_stride, const int32_t* pos, int32_t pos_rows, int32_t rows, int32_t heads, int32_t dh,
@@ -555,7 +555,10 @@ int32_t free_op_rope_axes(const void* x, int64_t x_stride, const int32_t* pos, i
 
 /* Gated feed-forward block of M token rows of width D with F hidden values, all tensors of type dtype, contiguous and 16-byte aligned:
  *   [g | u] = x w_in^T,  h = act(g) u,  out = h w_out^T;   w_in [2 F, D] (gate rows, then up rows), w_out [D, F]
- * act: FREE_ACT_SILU or FREE_ACT_GELU (tanh form).  Any D and F; sums, g and u are fp32, h is rounded to dtype.
+ * act: FREE_ACT_SILU or FREE_ACT_GELU (tanh form).  Sums, g and u are fp32, h is rounded to dtype.  Any widths up to 2^20; those that are
+ * not multiples of 64 go through padded copies in the workspace where there are more than 32 rows.  M F, M D and 2 F D: at most 2^35 (bf16) or 2^33 (fp32)
+ * (FREE_ERR_LIMIT).  How sums are cut depends on M, D, F and on whether state is kept, so results of calls that differ in these may differ
+ * in their last bits.
  * saved (NULL: none): free_gated_ffn_saved_bytes bytes that the gradient's pass reads, of a layout of the library's own; they belong to
  * these sizes and this x.
  * The gradient: dx [M, D] and dw_in, dw_out of the weights' shapes, written, not added to; g's and u's gradients are rounded to dtype.

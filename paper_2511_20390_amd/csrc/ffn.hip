@@ -238,13 +238,12 @@ int32_t backward_of(const Sizes& z, const T* dout, const T* x, const T* w_in, co
 
 }  // namespace
 
-// 32-bit byte offsets inside a tile of 256 rows, 32-bit column numbers of [g | u], grids of less than 2^32 threads
+// 32-bit byte offsets inside a tile of 256 rows, 32-bit column numbers of [g | u], grids of less than 2^32 threads (fp32: of tiles a quarter
+// as large)
 bool ffn_covers(int32_t M, int32_t D, int32_t F, int32_t dtype) {
-    constexpr int32_t kMost = 1 << 20;
-    (void)dtype;
-    if (D > kMost || F > kMost) return false;
+    if (D > 1 << 20 || F > 1 << 20) return false;
     const int64_t m = (static_cast<int64_t>(M) + 127) / 128, d = (D + 127) / 128, f = (F + 63) / 64;
-    return std::max({m * f, m * d, 2 * f * d}) <= 1 << 22;
+    return std::max({m * f, m * d, 2 * f * d}) <= (dtype == FREE_FP32 ? 1 << 20 : 1 << 22);
 }
 
 size_t ffn_saved_bytes(int32_t M, int32_t D, int32_t F, int32_t dtype) {

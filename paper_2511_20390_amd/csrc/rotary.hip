@@ -164,8 +164,10 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a, RopeTable ta
 template <typename T, int V, bool kAdjacent>
 int32_t launch_of(RopeArgs a, const RopeTable& tab, hipStream_t s) {
     a.units = a.dh / 2 / V;
-    a.slots = (a.heads + kHeads - 1) / kHeads;
-    const int64_t blocks = (static_cast<int64_t>(a.rows) * a.units * a.slots + kThreads - 1) / kThreads;
+    a.slots = a.heads / kHeads + (a.heads % kHeads != 0);
+    const int64_t per_row = static_cast<int64_t>(a.units) * a.slots;
+    if (per_row > (1 << 30)) return FREE_ERR_LIMIT;
+    const int64_t blocks = (a.rows * per_row + kThreads - 1) / kThreads;
     if (blocks > (1 << 24) - 1) return FREE_ERR_LIMIT;             // a grid has less than 2^32 threads
     hipLaunchKernelGGL((rope_kernel<T, V, kAdjacent>), dim3(static_cast<uint32_t>(blocks)), dim3(kThreads), 0, s, a, tab);
     return launch_ok() ? FREE_OK : FREE_ERR_HIP;

@@ -62,6 +62,7 @@ def test_rope_refusals(lib):
     assert call(xs=127) == call(os_=127) == b.FREE_ERR_SHAPE
     assert call(xs=256) == b.FREE_ERR_SHAPE                        # in place with another stride
     assert call(rows=2**31 - 1, heads=1 << 10, xs=1 << 20, os_=1 << 20) == b.FREE_ERR_LIMIT
+    assert call(rows=1, heads=2**31 - 1) == b.FREE_ERR_LIMIT
     assert call(rows=0, x=None, pos=None, out=None) == b.FREE_OK
 
 
@@ -80,7 +81,8 @@ def test_ffn_refusals(lib):
         assert call(act=2) == b.FREE_ERR_RANGE
         assert call(M=-1) == call(D=0) == call(F=0) == b.FREE_ERR_SHAPE
         assert call(ws=None) == call(ws=C.c_void_p(4112)) == call(n=64) == b.FREE_ERR_WORKSPACE
-        assert call(F=2**31 - 1) == call(D=2**31 - 1) == b.FREE_ERR_LIMIT
+        assert call(F=2**31 - 1) == call(D=2**31 - 1) == call(M=2**31 - 1, F=1 << 15) == b.FREE_ERR_LIMIT
+        assert call(M=1 << 20, F=1 << 14, t=0) == b.FREE_ERR_LIMIT
     assert fwd(x=C.c_void_p(4104)) == fwd(out=C.c_void_p(4104)) == b.FREE_ERR_SHAPE
     assert fwd(saved=ONE, sb=64) == fwd(saved=C.c_void_p(4112), sb=BIG) == b.FREE_ERR_WORKSPACE
     assert bwd(saved=None) == bwd(sb=64) == bwd(saved=C.c_void_p(4112)) == b.FREE_ERR_WORKSPACE
