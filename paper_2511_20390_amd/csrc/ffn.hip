@@ -7,8 +7,9 @@
 // error of their own to dg and du, three roundings on the way to a gradient in place of two.  h, dg and du are rounded to the type of the
 // block once, as operands of the next product.
 //
-// The products want widths that are multiples of 64 (16-byte rows, whole slices of K).  Other widths go through zero-padded copies in
-// the workspace, results through a cropping copy: zeros in D add nothing to a sum, zero rows of w_in give h = 0.
+// The products want widths that are multiples of 8 (bf16: 16-byte rows) or of 64 (fp32: whole slices of K).  Other widths go through
+// zero-padded copies in the workspace, results through a cropping copy: zeros in D add nothing to a sum, zero rows of w_in give h = 0.
+// (bf16, 1000 rows of 1152, forward and gradient, us: 2743 hidden values, padded, 177; 2736, not padded, 121; 2752 121.)
 // bf16: ffn_mfma.hip; fp32: the products of three bf16 parts per value of gemm_f32.hip.  Both read operands in either layout.  Few rows:
 // ffn_rows.hip.
 #include <algorithm>
@@ -65,11 +66,18 @@ int32_t up_to(int32_t v, int32_t step) { return (v + step - 1) / step * step; }
 struct Sizes {
     int32_t M, D, F;                 // as given
     int32_t Dp, Fp;                  // as the products have them
+    int32_t H;                       // values of a row of h, dg, du
     size_t es;
     bool padded;
-    Sizes(int32_t m, int32_t d, int32_t f, int32_t dtype)
-        : M(m), D(d), F(f), Dp(up_to(d, 64)), Fp(up_to(f, 64)), es(dtype == FREE_BF16 ? 2 : 4), padded(Dp != d || Fp != f) {}
-    size_t gu_bytes() const { return static_cast<size_t>(up_to(M, 32)) * 2 * Fp * sizeof(float); }
+    Sizes(int32_t m, int32_t d, int32_t f, int32_t dtype) : M(m), D(d), F(f), Dp(d), Fp(f), H(up_to(f, 64)), es(dtype == FREE_BF16 ? 2 : 4) {
+        const int32_t step = es == 2 ? 8 : 64;
+        padded = d % step != 0 || f % step != 0;
+        if (padded) {
+            Dp = up_to(d, 64);
+            Fp = H;
+        }
+    }
+    size_t gu_bytes() const { return static_cast<size_t>(up_to(M, 32)) * 2 * H * sizeof(float); }
     size_t act_bytes(int32_t width) const { return static_cast<size_t>(M) * width * es; }
     size_t weight_bytes(int32_t n) const { return static_cast<size_t>(n) * Dp * Fp * es; }
 };
@@ -90,8 +98,8 @@ template <typename T>
 struct ForwardProducts {
     FfnProduct<T> up, down;
     ForwardProducts(const Sizes& z, const T* x, const T* w_in, const T* w_out, int32_t act, T* y, float* gu, T* h, bool keep)
-        : up{keep ? FFN_GATE_KEEP : FFN_GATE, x, w_in, z.Dp, z.Dp, z.M, z.Fp, z.Dp, h, z.Fp, gu, act},
-          down{FFN_ROWS, h, w_out, z.Fp, z.Fp, z.M, z.Dp, z.Fp, y, z.Dp} {}
+        : up{keep ? FFN_GATE_KEEP : FFN_GATE, x, w_in, z.Dp, z.Dp, z.M, z.Fp, z.Dp, h, z.H, gu, act, z.H},
+          down{FFN_ROWS, h, w_out, z.H, z.Fp, z.M, z.Dp, z.Fp, y, z.Dp} {}
     size_t room() const { return std::max(ffn_products_part_bytes(&up, 1), ffn_products_part_bytes(&down, 1)); }
 };
 
@@ -100,9 +108,10 @@ struct BackwardProducts {
     FfnProduct<T> gate, rows, weights[2];
     BackwardProducts(const Sizes& z, const T* dy, const T* x, const T* w_in, const T* w_out, float* gu, const T* h, int32_t act, T* dgu, T* dx,
                      T* dw_in, T* dw_out)
-        : gate{FFN_GATE_GRAD, dy, w_out, z.Dp, z.Fp, z.M, z.Fp, z.Dp, dgu, 2 * z.Fp, gu, act},
-          rows{FFN_ROWS_BY_K, dgu, w_in, 2 * z.Fp, z.Dp, z.M, z.Dp, 2 * z.Fp, dx, z.Dp},
-          weights{{FFN_K_BY_K, dgu, x, 2 * z.Fp, z.Dp, 2 * z.Fp, z.Dp, z.M, dw_in, z.Dp}, {FFN_K_BY_K, dy, h, z.Dp, z.Fp, z.Dp, z.Fp, z.M, dw_out, z.Fp}} {}
+        : gate{FFN_GATE_GRAD, dy, w_out, z.Dp, z.Fp, z.M, z.Fp, z.Dp, dgu, 2 * z.H, gu, act, z.H},
+          rows{FFN_ROWS_BY_K, dgu, w_in, 2 * z.H, z.Dp, z.M, z.Dp, 2 * z.H, dx, z.Dp, nullptr, 0, 0, z.H, z.Fp},
+          weights{{FFN_K_BY_K, dgu, x, 2 * z.H, z.Dp, 2 * z.H, z.Dp, z.M, dw_in, z.Dp, nullptr, 0, 0, z.H, z.Fp},
+                  {FFN_K_BY_K, dy, h, z.Dp, z.H, z.Dp, z.Fp, z.M, dw_out, z.Fp}} {}
     size_t room() const {
         return std::max({ffn_products_part_bytes(&gate, 1), ffn_products_part_bytes(&rows, 1), ffn_products_part_bytes(weights, 2)});
     }
@@ -116,7 +125,7 @@ struct Saved {
     Saved(const Sizes& z, char* base) {
         Carve c{base};
         gu = c.take<float>(z.gu_bytes());
-        h = c.take<T>(z.act_bytes(z.Fp));
+        h = c.take<T>(z.act_bytes(z.H));
         bytes = c.at + 256;
     }
 };
@@ -128,7 +137,7 @@ struct ForwardSpace {
     size_t bytes;
     ForwardSpace(const Sizes& z, char* base) {
         Carve c{base};
-        h = c.take<T>(z.act_bytes(z.Fp));
+        h = c.take<T>(z.act_bytes(z.H));
         const auto room_of = [&](bool keep) { return ForwardProducts<T>(z, nullptr, nullptr, nullptr, 0, nullptr, nullptr, nullptr, keep).room(); };
         room = c.take<float>(std::max(room_of(false), room_of(true)));
         x = w_in = w_out = y = nullptr;
@@ -149,7 +158,7 @@ struct BackwardSpace {
     size_t bytes;
     BackwardSpace(const Sizes& z, char* base) {
         Carve c{base};
-        dgu = c.take<T>(z.act_bytes(2 * z.Fp));
+        dgu = c.take<T>(z.act_bytes(2 * z.H));
         room = c.take<float>(BackwardProducts<T>(z, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, 0, nullptr, nullptr, nullptr, nullptr).room());
         x = dy = w_in = w_out = dx = dw_in = dw_out = nullptr;
         if (z.padded) {

@@ -1,5 +1,5 @@
-// The matrix products of the gated feed-forward block (ffn_mfma.hip; fp32: gemm_f32.hip), for ffn.hip.  Sizes but the number of token rows are multiples of
-// 64, pointers 16-byte aligned, leading dimensions multiples of 8.
+// The matrix products of the gated feed-forward block (ffn_mfma.hip; fp32: gemm_f32.hip), for ffn.hip.  bf16: widths and leading
+// dimensions are multiples of 8; fp32: of 64, and rows dense.  Pointers are 16-byte aligned.
 #pragma once
 
 #include "free_internal.h"
@@ -26,8 +26,14 @@ struct FfnProduct {
     int32_t M, N, K;
     T* out;
     int64_t ldo;
-    float* gu = nullptr;             // [g | u] as 32 x 32 blocks: [M / 32 rounded up][2 N / 32][4][lane][4]
+    float* gu = nullptr;             // [g | u] as 32 x 32 blocks: [M / 32 rounded up][2 H / 32][4][lane][4]
     int32_t act = 0;
+    // H, N rounded up to a multiple of 64, for the gated kinds: what `out` has columns for, zeros past N (the gradient: du at H)
+    int32_t hidden = 0;
+    // dg and du as rows of C (FFN_K_BY_K) or of W (FFN_ROWS_BY_K): index fold + i of [dg | du] is row fold_to + i, indexes from fold_to to
+    // fold are none
+    int32_t fold = 0, fold_to = 0;
+    int32_t cols() const { return hidden > 0 ? hidden : N; }
     bool gated() const { return kind == FFN_GATE || kind == FFN_GATE_KEEP; }
 };
 

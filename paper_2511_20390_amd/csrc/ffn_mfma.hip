@@ -15,7 +15,10 @@
 // bytes at the same place of rows 256 or 512 bytes long; 16-byte chunk (b4 b3 b2 b1 b0) of row k is kept at place (b4, b1, b2 ^ k1, b3 ^
 // k0, b0) instead, which puts the 32 lanes on 64 different banks.
 // The last slice of a K-major operand ends where the tensor does: the buffer descriptor gives zeros from there on.  Columns past the
-// end of a row hold the next row's values and end in columns of C that are not written.
+// end of a row hold the next row's values and end in columns of C that are not written.  Of a row-major operand whose rows are not whole
+// slices the fragments past the end are cleared in registers, in the last slice.  So widths need to be multiples of 8 only (16-byte
+// rows); the hidden values' own tensors (h, dg, du and what is kept) have rows of H values, F rounded up to whole slices, zeros at the end, and an
+// index of [dg | du] past H is one of w_in's rows past F: `fold`.
 #include <algorithm>
 
 #include "free_internal.h"
@@ -32,9 +35,10 @@ struct Problem {
     const bf16_t *X, *W;
     int64_t ldx, ldw;            // values from row to row (K-major: from k to k)
     int32_t M, N, K;             // N: of the hidden values for the gated epilogues
+    int32_t cols, fold, fold_to; // see FfnProduct
     int32_t tiles_m, tiles_n, group_m;
     int32_t split_slices;        // slices of a part of K (all, or those of one of several)
-    bf16_t* out;                 // [M, N], ldo values from row to row; gated gradient: dg, du n_gate values further
+    bf16_t* out;                 // [M, cols], ldo values from row to row; gated gradient: dg, du `cols` further
     float* part;                 // sums over a part of K: [part][32 x 32 block][4][lane][4]
     float* gu;                   // kept [g | u], in blocks likewise
     int64_t ldo;
@@ -62,7 +66,9 @@ __device__ __forceinline__ void act_fast(float v, int act, float* f, float* df) 
 template <int EPI>
 constexpr bool kGated = EPI == FFN_GATE || EPI == FFN_GATE_KEEP;
 
-template <int BM, int BN, int WGM, int WGN, bool XK, bool WK, int EPI>
+// kRagged: rows of a row-major operand are not whole slices of K, or `cols` is more than N (an instance of its own: what it does in the
+// last slice and in the epilogue costs products of few slices 3 %)
+template <int BM, int BN, int WGM, int WGN, bool XK, bool WK, int EPI, bool kRagged>
 __global__ __launch_bounds__(512) void ffn_product_kernel(Launch la) {
     constexpr int NW = 8;
     static_assert(WGM * WGN == NW && BN / WGN == 64, "eight wavefronts of 64 columns");
@@ -117,7 +123,12 @@ __global__ __launch_bounds__(512) void ffn_product_kernel(Launch la) {
     const auto aim = [&](int kt) {
         const int64_t k = static_cast<int64_t>(kt) * BK;
         if constexpr (XK) xsrd = make_rsrc(a.X + k * a.ldx + m0, ((a.K - k) * a.ldx - m0) * 2);
-        if constexpr (WK) wsrd = make_rsrc(a.W + k * a.ldw + n0, ((a.K - k) * a.ldw - n0) * 2);
+        if constexpr (WK) {
+            const bool folded = !XK && a.fold > 0 && k >= a.fold;         // (of two K-major operands it is X's rows that fold)
+            const int64_t row = folded ? k - a.fold + a.fold_to : k;
+            const int64_t end = XK || a.fold == 0 ? a.K : folded ? 2 * static_cast<int64_t>(a.fold_to) : a.fold_to;
+            wsrd = make_rsrc(a.W + row * a.ldw + n0, ((end - row) * a.ldw - n0) * 2);
+        }
     };
     const auto dma = [&](int kt, int stage, int i) {
         const uint32_t dst = lds_base + stage * kStageBytes + wave * 1024;
@@ -210,6 +221,19 @@ __global__ __launch_bounds__(512) void ffn_product_kernel(Launch la) {
         }
         __builtin_amdgcn_sched_barrier(0);
     };
+    // the last slice of K: fragments of row-major operands past the end of a row
+    const auto clear = [&](int kt, int ks) {
+        if constexpr (kRagged) {
+            if ((a.K - (kt0 + kt) * BK) >= BK) return;
+            const bool ok = ks * 16 + lhi * 8 < a.K - (kt0 + kt) * BK;
+#pragma unroll
+            for (int r = XK ? TM : 0; r < (WK ? TM : TM + TN); ++r)
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) f[ks][r][h][e] = ok ? f[ks][r][h][e] : 0u;
+        }
+    };
     const auto slice = [&](int kt, auto on, auto more1, auto more2) {   // slices kt + 1, kt + 2 exist; kt counts from this part's first
         constexpr bool kOn = decltype(on)::value, m1 = decltype(more1)::value, m2 = decltype(more2)::value;
         constexpr int nd2 = m2 ? D2 : 0, nd3 = m2 ? D3 : 0;
@@ -220,13 +244,17 @@ __global__ __launch_bounds__(512) void ffn_product_kernel(Launch la) {
         if constexpr (kOn) {
             const auto none = [](int) {};
             using std::integral_constant;
+            if constexpr (!m1) clear(kt, 0);
             quarter(integral_constant<int, 0>{}, integral_constant<int, 0>{}, integral_constant<int, 2 * RU>{}, none,
                     [&](int r) { read(s, 1 + r / RU, r % RU); });
+            if constexpr (!m1) clear(kt, 1);
             quarter(integral_constant<int, 1>{}, integral_constant<int, 0>{}, integral_constant<int, RU>{}, none,
                     [&](int r) { read(s, 3, r); });
             if constexpr (m2) wait_lds_barrier();
+            if constexpr (!m1) clear(kt, 2);
             quarter(integral_constant<int, 2>{}, integral_constant<int, nd2>{}, integral_constant<int, 0>{}, load2, none);
             if constexpr (m1) wait_vm_barrier<nd2>();
+            if constexpr (!m1) clear(kt, 3);
             quarter(integral_constant<int, 3>{}, integral_constant<int, nd3>{}, integral_constant<int, m1 ? RU : 0>{}, load3,
                     [&](int r) { read(o, 0, r); });
         } else {
@@ -253,7 +281,7 @@ __global__ __launch_bounds__(512) void ffn_product_kernel(Launch la) {
         wait_vm_barrier<0>();
     }
     const int gn_wave = n0 + wn * (kGated<EPI> ? 32 : 64);       // this wavefront's first column of C
-    const bool mine = gn_wave < a.N && m0 + wm * TM * 32 < a.M;
+    const bool mine = gn_wave < a.cols && m0 + wm * TM * 32 < a.M;
     const auto k_loop = [&](auto on) {
         if constexpr (decltype(on)::value) {
 #pragma unroll
@@ -291,16 +319,22 @@ __global__ __launch_bounds__(512) void ffn_product_kernel(Launch la) {
         }
     };
     const auto flush = [&](int i, bf16_t* out) {                 // the staged 32 rows -> out[row][gn_wave ..]
-        const int gm0 = m0 + (wm * TM + i) * 32;
+        int gm0 = m0 + (wm * TM + i) * 32, rows = a.M;
+        if constexpr (XK) {                                      // (a fold is at a multiple of 64)
+            if (a.fold > 0) {
+                rows = gm0 < a.fold ? a.fold_to : 2 * a.fold_to;
+                gm0 = gm0 < a.fold ? gm0 : gm0 - a.fold + a.fold_to;
+            }
+        }
 #pragma unroll
         for (int q = 0; q < 32 * CH / 64; ++q) {
             const int c = q * 64 + lane, row = c / CH, ch = c % CH;
             const u32x4_t o = *reinterpret_cast<const u32x4_t*>(stage + row * kStageRow + (ch << 4));
-            if (gm0 + row < a.M && gn_wave + ch * 8 < a.N)
+            if (gm0 + row < rows && gn_wave + ch * 8 < a.cols)
                 *reinterpret_cast<u32x4_t*>(out + static_cast<int64_t>(gm0 + row) * a.ldo + gn_wave + ch * 8) = o;
         }
     };
-    const int blocks_n = (a.N + 31) / 32;
+    const int blocks_n = (a.cols + 31) / 32;
     if constexpr (EPI == FFN_PART) {
         const int64_t blocks = static_cast<int64_t>((a.M + 31) / 32) * blocks_n;
 #pragma unroll
@@ -334,7 +368,7 @@ __global__ __launch_bounds__(512) void ffn_product_kernel(Launch la) {
             for (int e = 0; e < 16; ++e) {
                 float f, df;
                 act_fast(acc[i][0][e], a.act, &f, &df);
-                h[e] = f * acc[i][1][e];
+                h[e] = !kRagged || gn_wave + 8 * (e / 4) < a.N ? f * acc[i][1][e] : 0.f;
             }
             put(0, h);
             flush(i, a.out);
@@ -361,15 +395,16 @@ __global__ __launch_bounds__(512) void ffn_product_kernel(Launch la) {
                 for (int e = 0; e < 16; ++e) {
                     float f, df;
                     act_fast(g[e / 4][e % 4], a.act, &f, &df);
-                    du[j][e] = acc[i][j][e] * f;
-                    dg[e] = acc[i][j][e] * u[e / 4][e % 4] * df;
+                    const bool there = !kRagged || gn_wave + 32 * j + 8 * (e / 4) < a.N;
+                    du[j][e] = there ? acc[i][j][e] * f : 0.f;
+                    dg[e] = there ? acc[i][j][e] * u[e / 4][e % 4] * df : 0.f;
                 }
                 put(j, dg);
             }
             flush(i, a.out);
 #pragma unroll
             for (int j = 0; j < TN; ++j) put(j, du[j]);
-            flush(i, a.out + a.N);
+            flush(i, a.out + a.cols);
         }
     } else {
 #pragma unroll
@@ -382,14 +417,16 @@ __global__ __launch_bounds__(512) void ffn_product_kernel(Launch la) {
 }
 
 // The parts of a product's sums over K, added in order, and the epilogue they were left without; a wavefront per 32 x 32 block of the
-// result.  Blocks of g | u: block_n and block_n + N / 32.
+// result
 template <typename T>
 struct Join {
-    const float* part;
+    const float* part;               // [splits][M / 32][part_n], and u's blocks `up` floats behind g's
+    int64_t up;
+    int32_t part_n;
     float* gu;
     T* out;
     int64_t ldo;
-    int32_t M, N, splits, act;       // N: hidden values for the gated kinds
+    int32_t M, N, cols, fold, fold_to, splits, act;       // N: hidden values for the gated kinds
 };
 
 // fp32: the library's exponential and tanh in place of the hardware's
@@ -410,7 +447,7 @@ __device__ __forceinline__ void act_exact(float v, int act, float* f, float* df)
 template <FfnKind kKind, typename T>
 __global__ __launch_bounds__(256) void ffn_join_kernel(Join<T> a) {
     constexpr bool kGate = kKind == FFN_GATE || kKind == FFN_GATE_KEEP, kGrad = kKind == FFN_GATE_GRAD;
-    const int blocks_n = a.N / 32, part_n = kGate ? 2 * blocks_n : blocks_n;
+    const int blocks_n = (a.cols + 31) / 32;
     const int64_t rows = (a.M + 31) / 32, block = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
     if (block >= rows * blocks_n) return;
     const int lane = threadIdx.x & 63;
@@ -419,20 +456,24 @@ __global__ __launch_bounds__(256) void ffn_join_kernel(Join<T> a) {
     f32x4_t s[B][4];
 #pragma unroll
     for (int b = 0; b < B; ++b) {
-        const float* p = a.part + (static_cast<int64_t>(mb) * part_n + nb + b * blocks_n) * 1024 + lane * 4;
+        const float* p = a.part + b * a.up + (static_cast<int64_t>(mb) * a.part_n + nb) * 1024 + lane * 4;
 #pragma unroll
         for (int e4 = 0; e4 < 4; ++e4) s[b][e4] = *reinterpret_cast<const f32x4_t*>(p + e4 * 256);
 #pragma unroll 3
         for (int k = 1; k < a.splits; ++k)
 #pragma unroll
-            for (int e4 = 0; e4 < 4; ++e4) s[b][e4] += *reinterpret_cast<const f32x4_t*>(p + k * rows * part_n * 1024 + e4 * 256);
+            for (int e4 = 0; e4 < 4; ++e4) s[b][e4] += *reinterpret_cast<const f32x4_t*>(p + k * rows * a.part_n * 1024 + e4 * 256);
     }
     float* const gu = a.gu + (static_cast<int64_t>(mb) * 2 * blocks_n + nb) * 1024 + lane * 4;
     float* const up = gu + static_cast<int64_t>(blocks_n) * 1024;
-    const int m = mb * 32 + (lane & 31);
+    int m = mb * 32 + (lane & 31), m_end = a.M;
+    if (kKind == FFN_ROWS && a.fold > 0) {
+        m_end = m < a.fold ? a.fold_to : 2 * a.fold_to;
+        m = m < a.fold ? m : m - a.fold + a.fold_to;
+    }
     T* const out = a.out + m * a.ldo + nb * 32 + 4 * (lane >> 5);
     const auto store = [&](T* p, const f32x4_t& v) {
-        if (m >= a.M) return;
+        if (m >= m_end) return;
         if constexpr (sizeof(T) == 4) *reinterpret_cast<f32x4_t*>(p) = v;
         else *reinterpret_cast<u32x2_t*>(p) = u32x2_t{pack2(v[0], v[1]), pack2(v[2], v[3])};
     };
@@ -442,6 +483,7 @@ __global__ __launch_bounds__(256) void ffn_join_kernel(Join<T> a) {
     };
 #pragma unroll
     for (int e4 = 0; e4 < 4; ++e4) {
+        const bool there = nb * 32 + 8 * e4 < a.N;               // (N: a multiple of 8)
         if constexpr (kGate) {
             if constexpr (kKind == FFN_GATE_KEEP) {
                 *reinterpret_cast<f32x4_t*>(gu + e4 * 256) = s[0][e4];
@@ -452,7 +494,7 @@ __global__ __launch_bounds__(256) void ffn_join_kernel(Join<T> a) {
             for (int c = 0; c < 4; ++c) {
                 float f, df;
                 activate(s[0][e4][c], &f, &df);
-                h[c] = f * s[1][e4][c];
+                h[c] = there ? f * s[1][e4][c] : 0.f;
             }
             store(out + 8 * e4, h);
         } else if constexpr (kGrad) {
@@ -462,12 +504,12 @@ __global__ __launch_bounds__(256) void ffn_join_kernel(Join<T> a) {
             for (int c = 0; c < 4; ++c) {
                 float f, df;
                 activate(g[c], &f, &df);
-                du[c] = s[0][e4][c] * f;
-                dg[c] = s[0][e4][c] * u[c] * df;
+                du[c] = there ? s[0][e4][c] * f : 0.f;
+                dg[c] = there ? s[0][e4][c] * u[c] * df : 0.f;
             }
             store(out + 8 * e4, dg);
-            store(out + 8 * e4 + a.N, du);
-        } else {
+            store(out + 8 * e4 + a.cols, du);
+        } else if (there) {
             store(out + 8 * e4, s[0][e4]);
         }
     }
@@ -477,9 +519,9 @@ struct Tile {
     int bm, bn;
 };
 
-template <int BM, int BN, int WGM, int WGN, bool XK, bool WK, int EPI>
+template <int BM, int BN, int WGM, int WGN, bool XK, bool WK, int EPI, bool kRagged>
 int32_t launch_kernel(const Launch& la, int blocks, hipStream_t s) {
-    auto kern = ffn_product_kernel<BM, BN, WGM, WGN, XK, WK, EPI>;
+    auto kern = ffn_product_kernel<BM, BN, WGM, WGN, XK, WK, EPI, kRagged>;
     const size_t lds = 2 * static_cast<size_t>(BM + BN) * kRowBytes;
     static LdsLimit limit;
     if (!limit.allow(reinterpret_cast<const void*>(kern), lds)) return FREE_ERR_HIP;
@@ -487,11 +529,21 @@ int32_t launch_kernel(const Launch& la, int blocks, hipStream_t s) {
     return launch_ok() ? FREE_OK : FREE_ERR_HIP;
 }
 
+template <bool XK, bool WK, int EPI, bool kRagged>
+int32_t launch_size(const Tile& t, const Launch& la, int blocks, hipStream_t s) {
+    if (t.bm == 256) return launch_kernel<256, 256, 2, 4, XK, WK, EPI, kRagged>(la, blocks, s);
+    if (t.bn == 256) return launch_kernel<128, 256, 2, 4, XK, WK, EPI, kRagged>(la, blocks, s);
+    return launch_kernel<128, 128, 4, 2, XK, WK, EPI, kRagged>(la, blocks, s);
+}
+
 template <bool XK, bool WK, int EPI>
 int32_t launch_tile(const Tile& t, const Launch& la, int blocks, hipStream_t s) {
-    if (t.bm == 256) return launch_kernel<256, 256, 2, 4, XK, WK, EPI>(la, blocks, s);
-    if (t.bn == 256) return launch_kernel<128, 256, 2, 4, XK, WK, EPI>(la, blocks, s);
-    return launch_kernel<128, 128, 4, 2, XK, WK, EPI>(la, blocks, s);
+    // (K-major X, and rows by K-major but for the gated gradient, whose K is D: their K is the token rows, or whole slices of [dg | du])
+    if constexpr (!XK && !(WK && EPI == FFN_STORE)) {
+        const Problem& q = la.p[0];
+        if (q.K % BK != 0 || q.cols != q.N) return launch_size<XK, WK, EPI, true>(t, la, blocks, s);
+    }
+    return launch_size<XK, WK, EPI, false>(t, la, blocks, s);
 }
 
 // What a launch takes: tile, and per product the parts that its sums over K are cut in
@@ -505,15 +557,14 @@ int parts_of(int slices, int splits) { return (slices + (slices + splits - 1) / 
 
 template <typename T>
 int64_t tiles_of(const FfnProduct<T>& p, const Tile& t, bool parts) {
-    // (parts of g | u are those of one matrix of 2 N rows: gate and up meet in the join)
-    const int64_t cols = p.gated() ? (parts ? 2 * static_cast<int64_t>(p.N) : p.N) : p.N;
+    // (in parts gate and up are two products that meet in the join)
     const int per = p.gated() && !parts ? t.bn / 2 : t.bn;
-    return static_cast<int64_t>((p.M + t.bm - 1) / t.bm) * ((cols + per - 1) / per);
+    return static_cast<int64_t>((p.M + t.bm - 1) / t.bm) * ((p.cols() + per - 1) / per) * (p.gated() && parts ? 2 : 1);
 }
 
 template <typename T>
 size_t part_bytes(const FfnProduct<T>& p, int splits) {
-    return splits == 0 ? 0 : static_cast<size_t>(splits) * ((p.M + 31) / 32) * (p.N / 32) * (p.gated() ? 2 : 1) * 4096;
+    return splits == 0 ? 0 : static_cast<size_t>(splits) * ((p.M + 31) / 32) * ((p.cols() + 31) / 32) * (p.gated() ? 2 : 1) * 4096;
 }
 
 // Times of a workgroup, us: a launch; a slice of 64 k with all compute units at work, and with nothing in the way but its loads' latency;
@@ -568,9 +619,12 @@ Plan plan_of(const FfnProduct<bf16_t>* p, int n) {
 
 template <FfnKind kKind, typename T>
 int32_t launch_join_kernel(const FfnProduct<T>& p, const float* part, int splits, hipStream_t s) {
-    const int64_t blocks = static_cast<int64_t>((p.M + 31) / 32) * (p.N / 32);
-    hipLaunchKernelGGL((ffn_join_kernel<kKind, T>), dim3(static_cast<uint32_t>((blocks + 3) / 4)), dim3(256), 0, s,
-                       Join<T>{part, p.gu, p.out, p.ldo, p.M, p.N, splits, p.act});
+    const int64_t rows = (p.M + 31) / 32, cols = (p.cols() + 31) / 32, blocks = rows * cols;
+    // g's and u's parts: fp32 those of one matrix [g | u], bf16 all of g's, then all of u's
+    const bool one = sizeof(T) == 4 && p.gated();
+    const Join<T> j{part,  one ? cols * 1024 : splits * blocks * 1024, static_cast<int32_t>(one ? 2 * cols : cols),
+                    p.gu,  p.out, p.ldo, p.M, p.N, p.cols(), p.kind == FFN_K_BY_K ? p.fold : 0, p.fold_to, splits, p.act};
+    hipLaunchKernelGGL((ffn_join_kernel<kKind, T>), dim3(static_cast<uint32_t>((blocks + 3) / 4)), dim3(256), 0, s, j);
     return launch_ok() ? FREE_OK : FREE_ERR_HIP;
 }
 
@@ -597,7 +651,7 @@ PlanF32 plan_of(const FfnProduct<float>& p) {
     PlanF32 best{false, 1};
     double best_time = 0.0;
     const int all = std::max(1, (p.K + kSliceF32 - 1) / kSliceF32);
-    const int64_t cols = p.gated() ? 2 * static_cast<int64_t>(p.N) : p.N;
+    const int64_t cols = p.gated() ? 2 * static_cast<int64_t>(p.N) : p.N;                // (N: multiples of 64)
     for (const int want : {1, 2, 3, 4, 6, 8, 12, 16}) {
         const int splits = parts_of(all, std::min(want, all)), slices = (all + splits - 1) / splits;
         if (want > 1 && slices < kMinPartF32) break;
@@ -657,32 +711,41 @@ int32_t launch_ffn_products(const FfnProduct<bf16_t>* p, int n, float* part, hip
     const bool parts = plan.splits[0] > 1 || (n == 2 && plan.splits[1] > 1);
     Launch la{};
     int64_t blocks = 0;
-    for (int i = 0; i < n; ++i) {
-        Problem& q = la.p[i];
-        q.X = p[i].X;
-        q.W = p[i].W;
-        q.ldx = p[i].ldx;
-        q.ldw = p[i].ldw;
-        q.M = p[i].M;
-        q.N = p[i].gated() && parts ? 2 * p[i].N : p[i].N;
-        q.K = p[i].K;
-        const int cols = p[i].gated() && !parts ? t.bn / 2 : t.bn;
+    int count = 0;
+    const auto add = [&](const FfnProduct<bf16_t>& from, int splits, const bf16_t* W) {
+        Problem& q = la.p[count];
+        q.X = from.X;
+        q.W = W;
+        q.ldx = from.ldx;
+        q.ldw = from.ldw;
+        q.M = from.M;
+        q.N = from.N;
+        q.K = from.K;
+        q.cols = from.cols();
+        q.fold = from.fold;
+        q.fold_to = from.fold_to;
+        const int cols = from.gated() && !parts ? t.bn / 2 : t.bn;
         q.tiles_m = (q.M + t.bm - 1) / t.bm;
-        q.tiles_n = (q.N + cols - 1) / cols;
+        q.tiles_n = (q.cols + cols - 1) / cols;
         q.group_m = 8;
-        q.split_slices = (slices_of(q.K) + plan.splits[i] - 1) / plan.splits[i];
-        q.out = p[i].out;
-        q.ldo = p[i].ldo;
-        q.gu = p[i].gu;
-        q.act = p[i].act;
+        q.split_slices = (slices_of(q.K) + splits - 1) / splits;
+        q.out = from.out;
+        q.ldo = from.ldo;
+        q.gu = from.gu;
+        q.act = from.act;
         if (parts) {
             q.part = part;
-            part += static_cast<int64_t>(plan.splits[i]) * ((q.M + 31) / 32) * (q.N / 32) * 1024;
+            part += static_cast<int64_t>(splits) * ((q.M + 31) / 32) * ((q.cols + 31) / 32) * 1024;
         }
-        if (i == 1) la.first1 = static_cast<int32_t>(blocks);
-        blocks += static_cast<int64_t>(q.tiles_m) * q.tiles_n * plan.splits[i];
+        if (count == 1) la.first1 = static_cast<int32_t>(blocks);
+        blocks += static_cast<int64_t>(q.tiles_m) * q.tiles_n * splits;
+        ++count;
+    };
+    for (int i = 0; i < n; ++i) {
+        add(p[i], plan.splits[i], p[i].W);
+        if (p[i].gated() && parts) add(p[i], plan.splits[i], p[i].W + static_cast<int64_t>(p[i].N) * p[i].ldw);
     }
-    if (n == 1) la.first1 = 0x7fffffff;
+    if (count == 1) la.first1 = 0x7fffffff;
     if (blocks > (1 << 22)) return FREE_ERR_LIMIT;
     const int b = static_cast<int>(blocks);
     if (!parts) {

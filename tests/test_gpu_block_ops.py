@@ -379,6 +379,34 @@ def test_ffn_tiles(M, D, F):
     _ffn_case(M, D, F, "silu", "bf16")
 
 
+# widths that are multiples of 8 and not of a slice: ragged K of every product, the seam of [dg | du], K whole and in parts
+@pytest.mark.parametrize("M,D,F", [(33, 72, 40), (100, 8, 8), (70, 136, 2000), (257, 1000, 72), (300, 1160, 2744), (1001, 200, 1000), (40, 1096, 4104),
+                                   (2100, 1144, 4616), (6000, 328, 1544), (9000, 264, 1032)])
+def test_ffn_ragged_slices(M, D, F):
+    _ffn_case(M, D, F, "silu", "bf16")
+
+
+def test_ffn_not_finite_weights():
+    """What an infinite weight next to a ragged row's end reaches: the gate value it belongs to, not its neighbour's column."""
+    import torch
+    from paper_2511_20390_amd import binding as b
+    g = _gen(21)
+    M, D, F = 50, 72, 136
+    dt = torch.bfloat16
+    x, w_in, w_out = _rnd(g, M, D, dtype=dt), _rnd(g, 2 * F, D, std=0.1, dtype=dt), _rnd(g, D, F, std=0.1, dtype=dt)
+    clean = b.op_gated_ffn(x, w_in, w_out)
+    w_out[6, 0] = float("inf")                             # read behind the end of row 5
+    got = b.op_gated_ffn(x, w_in, w_out)
+    keep = torch.arange(D, device="cuda") != 6
+    assert torch.equal(got[:, keep], clean[:, keep]) and not torch.isfinite(got[:, 6]).any()
+    # one infinite input: its row alone, though the row before is read into it
+    w_out[6, 0] = 0.1
+    x[7, 0] = float("nan")
+    clean, got = b.op_gated_ffn(x.nan_to_num(0.0), w_in, w_out), b.op_gated_ffn(x, w_in, w_out)
+    rows = torch.arange(M, device="cuda") != 7
+    assert torch.equal(got[rows], clean[rows]) and torch.isnan(got[7]).all()
+
+
 @pytest.mark.parametrize("M,D,F", [(40, 256, 4096), (600, 1152, 1152), (3000, 128, 512), (2500, 768, 1536), (130, 1024, 64)])
 def test_ffn_tiles_fp32(M, D, F):
     """64 x 64 and 128 x 128 tiles, K whole and in parts."""
