@@ -47,7 +47,8 @@ struct Problem {
 
 struct Launch {
     Problem p[2];
-    int32_t first1;              // workgroups of p[0]
+    int32_t first1;              // tiles (and parts of K) of p[0]
+    int32_t total;               // of both
 };
 
 // act(v), act'(v) with the hardware's exponential and reciprocal (1 ulp each): both activations are v s with s = 1 / (1 + 2^-t),
@@ -62,6 +63,12 @@ __device__ __forceinline__ void act_fast(float v, int act, float* f, float* df) 
     // s (1 - s): where slope is infinite s is 0 or 1 exactly
     *df = s == 0.f || s == 1.f ? s : fmaf(s * (1.0f - s), slope, s);
 }
+
+// Whether a workgroup does several tiles (LDS for the stages and for the epilogue, one workgroup per compute unit): launches of one product
+// in whole sums, the others having few tiles, whose epilogue is short of neither registers (the gated gradient would spill 150) nor
+// patience: the next tile's first slice is counted as arrived only once the epilogue's stores are, so that keeping g and u would cost
+// more (12288 x 1152 x 4608 forward and gradient 1274 -> 1284 us) than it saves.  Forward of these rows 342 -> 334 us, 4096 x 4096 x 10240 777 -> 767.
+constexpr bool ffn_rounds(int bm, int bn, bool xk, int epi) { return bm * bn > 128 * 128 && !xk && (epi == FFN_GATE || epi == FFN_STORE); }
 
 template <int EPI>
 constexpr bool kGated = EPI == FFN_GATE || EPI == FFN_GATE_KEEP;
@@ -82,25 +89,22 @@ __global__ __launch_bounds__(512) void ffn_product_kernel(Launch la) {
     static_assert(!kGated<EPI> || !WK, "gate and up rows are interleaved row by row");
     extern __shared__ __attribute__((aligned(16))) char lds[];
 
-    const bool second = static_cast<int>(blockIdx.x) >= la.first1;
-    const Problem& a = second ? la.p[1] : la.p[0];
-    const int pid = second ? blockIdx.x - la.first1 : blockIdx.x;
-    const int tiles = a.tiles_m * a.tiles_n;
-    const int split = pid / tiles;
-    int tile_m, tile_n;
-    tile_coords(a.group_m, pid % tiles, a.tiles_m, a.tiles_n, &tile_m, &tile_n);
     constexpr int kCols = kGated<EPI> ? BN / 2 : BN;             // columns of C per tile
-    const int m0 = tile_m * BM, n0 = tile_n * kCols;
+    // A tile that has its compute unit to itself is one of several that a workgroup does: the next one's first two slices are requested
+    // before the epilogue, which has its own piece of LDS.
+    constexpr bool kRounds = ffn_rounds(BM, BN, XK, EPI);
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     constexpr int kHalfN = WGN / 2;
     const int wm = (wave & 3) / kHalfN, wn = (wave >> 2) * kHalfN + (wave & 3) % kHalfN;
-    const int all_slices = (a.K + BK - 1) / BK;
-    const int kt0 = split * a.split_slices;
-    const int nk = (kt0 + a.split_slices < all_slices ? a.split_slices : all_slices - kt0);
+    const bool second = !kRounds && static_cast<int>(blockIdx.x) >= la.first1;
+    const Problem& a = second ? la.p[1] : la.p[0];
+    const int ldx2 = static_cast<int>(a.ldx) * 2, ldw2 = static_cast<int>(a.ldw) * 2;
+    // the tile at work (its epilogue goes by copies)
+    int m0, n0, split, kt0, nk;
+    u32x4_t xsrd, wsrd;
 
     // ---- loads, blocks of 1 KB: w, w + 8, ... per wavefront.  Row-major: 8 rows of 64 k, chunks swizzled as in gemm_pipe.hip.  K-major:
     // 1024 / row bytes rows of k.
-    const int ldx2 = static_cast<int>(a.ldx) * 2, ldw2 = static_cast<int>(a.ldw) * 2;
     const auto major_offset = [&](int row_bytes, int ld2) {
         const int per = 64 / (1024 / row_bytes);                 // lanes per row of k
         const int k = lane / per + (row_bytes == 512 ? 2 * (wave & 1) : 0), p = lane % per;
@@ -108,17 +112,28 @@ __global__ __launch_bounds__(512) void ffn_product_kernel(Launch la) {
         return (lane / per) * ld2 + c * 16;
     };
     const auto minor_offset = [&](int ld2) { return (lane >> 3) * ld2 + (((lane & 7) ^ (((wave & 1) << 2) | (lane >> 4))) << 4); };
-    const int xoff = XK ? major_offset(BM * 2, ldx2) : minor_offset(ldx2);
-    const int woff = WK ? major_offset(BN * 2, ldw2) : minor_offset(ldw2);
     constexpr int XB = XK ? 1024 / (BM * 2) : 8, WB = WK ? 1024 / (BN * 2) : 8;       // memory rows per block
     const uint32_t lds_base = lds_address(lds);
     // gated: tile row r holds a gate row of the hidden value n0 + 32 (r / 64) + r % 32 where r % 64 < 32, else the up row; wavefronts
     // 0 to 3 load the gate rows of a group of 64, 4 to 7 the up rows
-    const int64_t w_first = kGated<EPI> ? static_cast<int64_t>(wave < 4 ? 0 : a.N) + n0 + (wave & 3) * 8 : n0;
-    const int64_t w_rows = kGated<EPI> ? 2 * static_cast<int64_t>(a.N) : a.N;
-    u32x4_t xsrd, wsrd;
-    if constexpr (!XK) xsrd = make_rsrc(a.X + m0 * a.ldx, (a.M - m0) * a.ldx * 2);
-    if constexpr (!WK) wsrd = make_rsrc(a.W + w_first * a.ldw, (w_rows - w_first) * a.ldw * 2);
+    const int xoff = XK ? major_offset(BM * 2, ldx2) : minor_offset(ldx2);
+    const int woff = WK ? major_offset(BN * 2, ldw2) : minor_offset(ldw2);
+    const auto set_tile = [&](int id) {
+        const int pid = second ? id - la.first1 : id;
+        const int tiles = a.tiles_m * a.tiles_n;
+        int tile_m, tile_n;
+        split = pid / tiles;
+        tile_coords(a.group_m, pid % tiles, a.tiles_m, a.tiles_n, &tile_m, &tile_n);
+        m0 = tile_m * BM;
+        n0 = tile_n * kCols;
+        const int all_slices = (a.K + BK - 1) / BK;
+        kt0 = split * a.split_slices;
+        nk = (kt0 + a.split_slices < all_slices ? a.split_slices : all_slices - kt0);
+        const int64_t w_first = kGated<EPI> ? static_cast<int64_t>(wave < 4 ? 0 : a.N) + n0 + (wave & 3) * 8 : n0;
+        const int64_t w_rows = kGated<EPI> ? 2 * static_cast<int64_t>(a.N) : a.N;
+        if constexpr (!XK) xsrd = make_rsrc(a.X + m0 * a.ldx, (a.M - m0) * a.ldx * 2);
+        if constexpr (!WK) wsrd = make_rsrc(a.W + w_first * a.ldw, (w_rows - w_first) * a.ldw * 2);
+    };
     // descriptors of a slice of a K-major operand, from its first k on: the offsets inside stay small whatever K is
     const auto aim = [&](int kt) {
         const int64_t k = static_cast<int64_t>(kt) * BK;
@@ -185,12 +200,6 @@ __global__ __launch_bounds__(512) void ffn_product_kernel(Launch la) {
         }
     };
     f32x16_t acc[TM][TN];
-#pragma unroll
-    for (int i = 0; i < TM; ++i)
-#pragma unroll
-        for (int j = 0; j < TN; ++j)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
     const auto frag = [&](int ks, int r) {
         return __builtin_bit_cast(bf16x8_t, u32x4_t{f[ks][r][0][0], f[ks][r][0][1], f[ks][r][1][0], f[ks][r][1][1]});
     };
@@ -269,19 +278,16 @@ __global__ __launch_bounds__(512) void ffn_product_kernel(Launch la) {
     const std::true_type yes{};
     const std::false_type no{};
 
-    aim(kt0);
+    const auto first_slices = [&]() {
+        aim(kt0);
 #pragma unroll
-    for (int i = 0; i < NL; ++i) dma(kt0, 0, i);
-    if (nk > 1) {
-        aim(kt0 + 1);
+        for (int i = 0; i < NL; ++i) dma(kt0, 0, i);
+        if (nk > 1) {
+            aim(kt0 + 1);
 #pragma unroll
-        for (int i = 0; i < NL; ++i) dma(kt0 + 1, 1, i);
-        wait_vm_barrier<NL>();
-    } else {
-        wait_vm_barrier<0>();
-    }
-    const int gn_wave = n0 + wn * (kGated<EPI> ? 32 : 64);       // this wavefront's first column of C
-    const bool mine = gn_wave < a.cols && m0 + wm * TM * 32 < a.M;
+            for (int i = 0; i < NL; ++i) dma(kt0 + 1, 1, i);
+        }
+    };
     const auto k_loop = [&](auto on) {
         if constexpr (decltype(on)::value) {
 #pragma unroll
@@ -296,123 +302,148 @@ __global__ __launch_bounds__(512) void ffn_product_kernel(Launch la) {
         }
         slice(kt, on, no, no);
     };
-    if (mine) k_loop(yes);
-    else k_loop(no);
-
-    // ---- epilogue: register e of acc[i][j] in lane l is row 32 i + l % 32, column 32 j + 8 (e / 4) + 4 (l / 32) + e % 4 of the wavefront's
-    // part.  bf16 goes through a private piece of the idle stages, so that whole rows are written.
-    __syncthreads();
-    if (!mine) return;
-    constexpr int OC = kGated<EPI> ? 1 : TN;                     // 32-column blocks of an output row
-    constexpr int CH = OC * 4, kStageRow = (CH + 1) * 16;
-    static_assert(NW * 32 * kStageRow <= 2 * kStageBytes, "output staging must fit in the K-loop stages");
-    char* const stage = lds + wave * 32 * kStageRow;
-    // 16 values of a 32 x 32 block -> row l32 of the staging rows, chunks 4 j ..
-    const auto put = [&](int j, const auto& v) {
-#pragma unroll
-        for (int e8 = 0; e8 < 2; ++e8) {
-            const uint32_t lo0 = pack2(v[8 * e8], v[8 * e8 + 1]), lo1 = pack2(v[8 * e8 + 2], v[8 * e8 + 3]);
-            const uint32_t hi0 = pack2(v[8 * e8 + 4], v[8 * e8 + 5]), hi1 = pack2(v[8 * e8 + 6], v[8 * e8 + 7]);
-            const u32x2_t s0 = __builtin_amdgcn_permlane32_swap(lo0, hi0, false, false);
-            const u32x2_t s1 = __builtin_amdgcn_permlane32_swap(lo1, hi1, false, false);
-            *reinterpret_cast<u32x4_t*>(stage + l32 * kStageRow + ((4 * j + 2 * e8 + lhi) << 4)) = u32x4_t{s0[0], s1[0], s0[1], s1[1]};
-        }
-    };
-    const auto flush = [&](int i, bf16_t* out) {                 // the staged 32 rows -> out[row][gn_wave ..]
-        int gm0 = m0 + (wm * TM + i) * 32, rows = a.M;
-        if constexpr (XK) {                                      // (a fold is at a multiple of 64)
-            if (a.fold > 0) {
-                rows = gm0 < a.fold ? a.fold_to : 2 * a.fold_to;
-                gm0 = gm0 < a.fold ? gm0 : gm0 - a.fold + a.fold_to;
-            }
-        }
-#pragma unroll
-        for (int q = 0; q < 32 * CH / 64; ++q) {
-            const int c = q * 64 + lane, row = c / CH, ch = c % CH;
-            const u32x4_t o = *reinterpret_cast<const u32x4_t*>(stage + row * kStageRow + (ch << 4));
-            if (gm0 + row < rows && gn_wave + ch * 8 < a.cols)
-                *reinterpret_cast<u32x4_t*>(out + static_cast<int64_t>(gm0 + row) * a.ldo + gn_wave + ch * 8) = o;
-        }
-    };
-    const int blocks_n = (a.cols + 31) / 32;
-    if constexpr (EPI == FFN_PART) {
-        const int64_t blocks = static_cast<int64_t>((a.M + 31) / 32) * blocks_n;
+    int id = blockIdx.x;
+    set_tile(id);
+    first_slices();
+    for (;;) {
 #pragma unroll
         for (int i = 0; i < TM; ++i)
 #pragma unroll
-            for (int j = 0; j < TN; ++j) {
-                const int mb = m0 / 32 + wm * TM + i, nb = gn_wave / 32 + j;
-                if (mb * 32 >= a.M || nb >= blocks_n) continue;
-                float* p = a.part + (split * blocks + static_cast<int64_t>(mb) * blocks_n + nb) * 1024 + lane * 4;
+            for (int j = 0; j < TN; ++j)
 #pragma unroll
-                for (int e4 = 0; e4 < 4; ++e4)
-                    *reinterpret_cast<f32x4_t*>(p + e4 * 256) = f32x4_t{acc[i][j][4 * e4], acc[i][j][4 * e4 + 1], acc[i][j][4 * e4 + 2], acc[i][j][4 * e4 + 3]};
-            }
-    } else if constexpr (kGated<EPI>) {
-#pragma unroll
-        for (int i = 0; i < TM; ++i) {
-            if constexpr (EPI == FFN_GATE_KEEP) {
-                const int mb = m0 / 32 + wm * TM + i;
-                if (mb * 32 < a.M) {
-                    float* p = a.gu + (static_cast<int64_t>(mb) * 2 * blocks_n + gn_wave / 32) * 1024 + lane * 4;
-#pragma unroll
-                    for (int j = 0; j < 2; ++j)
-#pragma unroll
-                        for (int e4 = 0; e4 < 4; ++e4)
-                            *reinterpret_cast<f32x4_t*>(p + static_cast<int64_t>(j) * blocks_n * 1024 + e4 * 256) =
-                                f32x4_t{acc[i][j][4 * e4], acc[i][j][4 * e4 + 1], acc[i][j][4 * e4 + 2], acc[i][j][4 * e4 + 3]};
-                }
-            }
-            float h[16];
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                float f, df;
-                act_fast(acc[i][0][e], a.act, &f, &df);
-                h[e] = !kRagged || gn_wave + 8 * (e / 4) < a.N ? f * acc[i][1][e] : 0.f;
-            }
-            put(0, h);
-            flush(i, a.out);
+                for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+        // the first slice has arrived (loads return in order, and the epilogue's stores behind them only make this wait longer)
+        if (nk > 1) wait_vm_barrier<NL>();
+        else wait_vm_barrier<0>();
+        const int e_m0 = m0, e_split = split, e_col = n0 + wn * (kGated<EPI> ? 32 : 64);       // first row; this wavefront's first column of C
+        const bool mine = e_col < a.cols && e_m0 + wm * TM * 32 < a.M;
+        if (mine) k_loop(yes);
+        else k_loop(no);
+        wait_lds_barrier();
+        id += gridDim.x;
+        const bool more = kRounds && id < la.total;
+        if (more) {
+            set_tile(id);
+            first_slices();
         }
-    } else if constexpr (EPI == FFN_GATE_GRAD) {
+
+        // ---- epilogue: register e of acc[i][j] in lane l is row 32 i + l % 32, column 32 j + 8 (e / 4) + 4 (l / 32) + e % 4 of the
+        // wavefront's part.  bf16 goes through a private piece of LDS, so that whole rows are written.
+        if (mine) {
+            constexpr int OC = kGated<EPI> ? 1 : TN;                     // 32-column blocks of an output row
+            constexpr int CH = OC * 4;
+            char* const stage = lds + (kRounds ? 2 * kStageBytes : 0) + wave * 32 * CH * 16;
+            static_assert(kRounds || NW * 32 * CH * 16 <= 2 * kStageBytes, "output staging must fit in the K-loop stages");
+            const auto place = [&](int row, int chunk) { return stage + (row * CH + (chunk ^ (row & (CH - 1)))) * 16; };
+            // 16 values of a 32 x 32 block -> row l32 of the staging rows, chunks 4 j ..
+            const auto put = [&](int j, const auto& v) {
 #pragma unroll
-        for (int i = 0; i < TM; ++i) {
-            const int mb = m0 / 32 + wm * TM + i;
-            float du[TN][16];
-#pragma unroll
-            for (int j = 0; j < TN; ++j) {
-                const int nb = gn_wave / 32 + j;
-                f32x4_t g[4], u[4];
-                if (mb * 32 < a.M && nb < blocks_n) {
-                    const float* p = a.gu + (static_cast<int64_t>(mb) * 2 * blocks_n + nb) * 1024 + lane * 4;
-#pragma unroll
-                    for (int e4 = 0; e4 < 4; ++e4) {
-                        g[e4] = *reinterpret_cast<const f32x4_t*>(p + e4 * 256);
-                        u[e4] = *reinterpret_cast<const f32x4_t*>(p + static_cast<int64_t>(blocks_n) * 1024 + e4 * 256);
+                for (int e8 = 0; e8 < 2; ++e8) {
+                    const uint32_t lo0 = pack2(v[8 * e8], v[8 * e8 + 1]), lo1 = pack2(v[8 * e8 + 2], v[8 * e8 + 3]);
+                    const uint32_t hi0 = pack2(v[8 * e8 + 4], v[8 * e8 + 5]), hi1 = pack2(v[8 * e8 + 6], v[8 * e8 + 7]);
+                    const u32x2_t s0 = __builtin_amdgcn_permlane32_swap(lo0, hi0, false, false);
+                    const u32x2_t s1 = __builtin_amdgcn_permlane32_swap(lo1, hi1, false, false);
+                    *reinterpret_cast<u32x4_t*>(place(l32, 4 * j + 2 * e8 + lhi)) = u32x4_t{s0[0], s1[0], s0[1], s1[1]};
+                }
+            };
+            const auto flush = [&](int i, bf16_t* out) {                 // the staged 32 rows -> out[row][e_col ..]
+                int gm0 = e_m0 + (wm * TM + i) * 32, rows = a.M;
+                if constexpr (XK) {                                      // (a fold is at a multiple of 64)
+                    if (a.fold > 0) {
+                        rows = gm0 < a.fold ? a.fold_to : 2 * a.fold_to;
+                        gm0 = gm0 < a.fold ? gm0 : gm0 - a.fold + a.fold_to;
                     }
                 }
-                float dg[16];
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    float f, df;
-                    act_fast(g[e / 4][e % 4], a.act, &f, &df);
-                    const bool there = !kRagged || gn_wave + 32 * j + 8 * (e / 4) < a.N;
-                    du[j][e] = there ? acc[i][j][e] * f : 0.f;
-                    dg[e] = there ? acc[i][j][e] * u[e / 4][e % 4] * df : 0.f;
+                for (int q = 0; q < 32 * CH / 64; ++q) {
+                    const int c = q * 64 + lane, row = c / CH, ch = c % CH;
+                    const u32x4_t o = *reinterpret_cast<const u32x4_t*>(place(row, ch));
+                    if (gm0 + row < rows && e_col + ch * 8 < a.cols)
+                        *reinterpret_cast<u32x4_t*>(out + static_cast<int64_t>(gm0 + row) * a.ldo + e_col + ch * 8) = o;
                 }
-                put(j, dg);
+            };
+            const int blocks_n = (a.cols + 31) / 32;
+            if constexpr (EPI == FFN_PART) {
+                const int64_t blocks = static_cast<int64_t>((a.M + 31) / 32) * blocks_n;
+#pragma unroll
+                for (int i = 0; i < TM; ++i)
+#pragma unroll
+                    for (int j = 0; j < TN; ++j) {
+                        const int mb = e_m0 / 32 + wm * TM + i, nb = e_col / 32 + j;
+                        if (mb * 32 >= a.M || nb >= blocks_n) continue;
+                        float* p = a.part + (e_split * blocks + static_cast<int64_t>(mb) * blocks_n + nb) * 1024 + lane * 4;
+#pragma unroll
+                        for (int e4 = 0; e4 < 4; ++e4)
+                            *reinterpret_cast<f32x4_t*>(p + e4 * 256) = f32x4_t{acc[i][j][4 * e4], acc[i][j][4 * e4 + 1], acc[i][j][4 * e4 + 2], acc[i][j][4 * e4 + 3]};
+                    }
+            } else if constexpr (kGated<EPI>) {
+#pragma unroll
+                for (int i = 0; i < TM; ++i) {
+                    if constexpr (EPI == FFN_GATE_KEEP) {
+                        const int mb = e_m0 / 32 + wm * TM + i;
+                        if (mb * 32 < a.M) {
+                            float* p = a.gu + (static_cast<int64_t>(mb) * 2 * blocks_n + e_col / 32) * 1024 + lane * 4;
+#pragma unroll
+                            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                                for (int e4 = 0; e4 < 4; ++e4)
+                                    *reinterpret_cast<f32x4_t*>(p + static_cast<int64_t>(j) * blocks_n * 1024 + e4 * 256) =
+                                        f32x4_t{acc[i][j][4 * e4], acc[i][j][4 * e4 + 1], acc[i][j][4 * e4 + 2], acc[i][j][4 * e4 + 3]};
+                        }
+                    }
+                    float h[16];
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        float f, df;
+                        act_fast(acc[i][0][e], a.act, &f, &df);
+                        h[e] = !kRagged || e_col + 8 * (e / 4) < a.N ? f * acc[i][1][e] : 0.f;
+                    }
+                    put(0, h);
+                    flush(i, a.out);
+                }
+            } else if constexpr (EPI == FFN_GATE_GRAD) {
+#pragma unroll
+                for (int i = 0; i < TM; ++i) {
+                    const int mb = e_m0 / 32 + wm * TM + i;
+                    float du[TN][16];
+#pragma unroll
+                    for (int j = 0; j < TN; ++j) {
+                        const int nb = e_col / 32 + j;
+                        f32x4_t g[4], u[4];
+                        if (mb * 32 < a.M && nb < blocks_n) {
+                            const float* p = a.gu + (static_cast<int64_t>(mb) * 2 * blocks_n + nb) * 1024 + lane * 4;
+#pragma unroll
+                            for (int e4 = 0; e4 < 4; ++e4) {
+                                g[e4] = *reinterpret_cast<const f32x4_t*>(p + e4 * 256);
+                                u[e4] = *reinterpret_cast<const f32x4_t*>(p + static_cast<int64_t>(blocks_n) * 1024 + e4 * 256);
+                            }
+                        }
+                        float dg[16];
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) {
+                            float f, df;
+                            act_fast(g[e / 4][e % 4], a.act, &f, &df);
+                            const bool there = !kRagged || e_col + 32 * j + 8 * (e / 4) < a.N;
+                            du[j][e] = there ? acc[i][j][e] * f : 0.f;
+                            dg[e] = there ? acc[i][j][e] * u[e / 4][e % 4] * df : 0.f;
+                        }
+                        put(j, dg);
+                    }
+                    flush(i, a.out);
+#pragma unroll
+                    for (int j = 0; j < TN; ++j) put(j, du[j]);
+                    flush(i, a.out + a.cols);
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < TM; ++i) {
+#pragma unroll
+                    for (int j = 0; j < TN; ++j) put(j, acc[i][j]);
+                    flush(i, a.out);
+                }
             }
-            flush(i, a.out);
-#pragma unroll
-            for (int j = 0; j < TN; ++j) put(j, du[j]);
-            flush(i, a.out + a.cols);
         }
-    } else {
-#pragma unroll
-        for (int i = 0; i < TM; ++i) {
-#pragma unroll
-            for (int j = 0; j < TN; ++j) put(j, acc[i][j]);
-            flush(i, a.out);
-        }
+        if (!more) break;
     }
 }
 
@@ -522,10 +553,11 @@ struct Tile {
 template <int BM, int BN, int WGM, int WGN, bool XK, bool WK, int EPI, bool kRagged>
 int32_t launch_kernel(const Launch& la, int blocks, hipStream_t s) {
     auto kern = ffn_product_kernel<BM, BN, WGM, WGN, XK, WK, EPI, kRagged>;
-    const size_t lds = 2 * static_cast<size_t>(BM + BN) * kRowBytes;
+    constexpr bool rounds = ffn_rounds(BM, BN, XK, EPI);
+    const size_t lds = 2 * static_cast<size_t>(BM + BN) * kRowBytes + (rounds ? 8 * 32 * (kGated<EPI> ? 64 : 128) : 0);
     static LdsLimit limit;
     if (!limit.allow(reinterpret_cast<const void*>(kern), lds)) return FREE_ERR_HIP;
-    hipLaunchKernelGGL(kern, dim3(blocks), dim3(512), lds, s, la);
+    hipLaunchKernelGGL(kern, dim3(rounds ? std::min(blocks, device_cus()) : blocks), dim3(512), lds, s, la);
     return launch_ok() ? FREE_OK : FREE_ERR_HIP;
 }
 
@@ -747,7 +779,7 @@ int32_t launch_ffn_products(const FfnProduct<bf16_t>* p, int n, float* part, hip
     }
     if (count == 1) la.first1 = 0x7fffffff;
     if (blocks > (1 << 22)) return FREE_ERR_LIMIT;
-    const int b = static_cast<int>(blocks);
+    const int b = la.total = static_cast<int>(blocks);
     if (!parts) {
         switch (p[0].kind) {
             case FFN_GATE: return launch_tile<false, false, FFN_GATE>(t, la, b, s);
