@@ -37,9 +37,8 @@ struct FfnProduct {
     bool gated() const { return kind == FFN_GATE || kind == FFN_GATE_KEEP; }
 };
 
-// bf16: one launch for n products (1, or 2 FFN_K_BY_K), or, where their sums over K are cut in parts, one more for each that joins them.
-// fp32: a launch for each, and one more where parts are joined or an activation is applied.  part: room of ffn_products_part_bytes (by the
-// sizes alone).
+// One launch for n products (1, or 2 FFN_K_BY_K), and one more for each whose sums over K are cut in parts, or, fp32, to which an activation is
+// applied.  part: room of ffn_products_part_bytes (by the sizes alone).
 size_t ffn_products_part_bytes(const FfnProduct<bf16_t>* p, int n);
 size_t ffn_products_part_bytes(const FfnProduct<float>* p, int n);
 int32_t launch_ffn_products(const FfnProduct<bf16_t>* p, int n, float* part, hipStream_t s);

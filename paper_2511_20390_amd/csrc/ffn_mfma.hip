@@ -679,19 +679,23 @@ constexpr int kSliceF32 = 32, kMinPartF32 = 8;
 
 bool join_anyway(FfnKind k) { return k == FFN_GATE || k == FFN_GATE_KEEP || k == FFN_GATE_GRAD; }
 
-PlanF32 plan_of(const FfnProduct<float>& p) {
+PlanF32 plan_of(const FfnProduct<float>* p, int n) {
     PlanF32 best{false, 1};
     double best_time = 0.0;
-    const int all = std::max(1, (p.K + kSliceF32 - 1) / kSliceF32);
-    const int64_t cols = p.gated() ? 2 * static_cast<int64_t>(p.N) : p.N;                // (N: multiples of 64)
+    const int all = std::max(1, (p[0].K + kSliceF32 - 1) / kSliceF32);
     for (const int want : {1, 2, 3, 4, 6, 8, 12, 16}) {
         const int splits = parts_of(all, std::min(want, all)), slices = (all + splits - 1) / splits;
         if (want > 1 && slices < kMinPartF32) break;
         for (const bool large : {false, true}) {
             const int b = large ? 128 : 64;
-            const int64_t work = static_cast<int64_t>((p.M + b - 1) / b) * ((cols + b - 1) / b) * splits;
-            double time = product_f32_time(large, work, slices);
-            if (splits > 1) time += (join_anyway(p.kind) ? 0.0 : 4.8) + 0.27 * splits + 0.18e-6 * static_cast<double>(part_bytes(p, splits));
+            int64_t work = 0;
+            double join = 0.0;
+            for (int i = 0; i < n; ++i) {
+                const int64_t cols = p[i].gated() ? 2 * static_cast<int64_t>(p[i].N) : p[i].N;        // (N: multiples of 64)
+                work += static_cast<int64_t>((p[i].M + b - 1) / b) * ((cols + b - 1) / b) * splits;
+                if (splits > 1) join += (join_anyway(p[i].kind) ? 0.0 : 4.8) + 0.27 * splits + 0.18e-6 * static_cast<double>(part_bytes(p[i], splits));
+            }
+            const double time = product_f32_time(large, work, slices) + join;
             if (best_time == 0.0 || time < best_time) {
                 best_time = time;
                 best = PlanF32{large, splits};
@@ -713,28 +717,32 @@ size_t ffn_products_part_bytes(const FfnProduct<bf16_t>* p, int n) {
 }
 
 size_t ffn_products_part_bytes(const FfnProduct<float>* p, int n) {
-    size_t most = 0;
-    for (int i = 0; i < n; ++i) {
-        const int splits = plan_of(p[i]).splits;
-        if (needs_room(p[i], splits)) most = std::max(most, part_bytes(p[i], splits));
-    }
-    return most;
+    const int splits = plan_of(p, n).splits;
+    size_t bytes = 0;
+    for (int i = 0; i < n; ++i)
+        if (needs_room(p[i], splits)) bytes += part_bytes(p[i], splits);
+    return bytes;
 }
 
 int32_t launch_ffn_products(const FfnProduct<float>* p, int n, float* part, hipStream_t s) {
+    const PlanF32 plan = plan_of(p, n);
+    const bool blocks = plan.splits > 1 || join_anyway(p[0].kind);
+    const bool x_by_k = p[0].kind == FFN_K_BY_K, w_by_k = x_by_k || p[0].kind == FFN_ROWS_BY_K || p[0].kind == FFN_GATE_GRAD;
+    ProductF32 q[2];
     for (int i = 0; i < n; ++i) {
-        const FfnProduct<float>& q = p[i];
-        const PlanF32 plan = plan_of(q);
-        const bool blocks = plan.splits > 1 || join_anyway(q.kind);
-        float* const to = !blocks ? q.out : needs_room(q, plan.splits) ? part : q.gu;
-        const bool x_by_k = q.kind == FFN_K_BY_K, w_by_k = x_by_k || q.kind == FFN_ROWS_BY_K || q.kind == FFN_GATE_GRAD;
-        int32_t st = launch_product_f32(x_by_k, w_by_k, plan.large, q.X, q.ldx, q.W, q.ldw, q.M, q.gated() ? 2 * q.N : q.N, q.K, plan.splits,
-                                        blocks, to, s);
-        // (what is kept already is not written again)
-        if (st == FREE_OK && blocks) st = launch_join(q, to == q.gu ? FFN_GATE : q.kind, to, plan.splits, s);
-        if (st != FREE_OK) return st;
+        q[i] = ProductF32{p[i].X, p[i].W, p[i].ldx, p[i].ldw, p[i].M, p[i].gated() ? 2 * p[i].N : p[i].N, p[i].K, p[i].out};
+        if (!blocks) continue;
+        q[i].out = p[i].gu;
+        if (needs_room(p[i], plan.splits)) {
+            q[i].out = part;
+            part += part_bytes(p[i], plan.splits) / sizeof(float);
+        }
     }
-    return FREE_OK;
+    int32_t st = launch_products_f32(x_by_k, w_by_k, plan.large, q, n, plan.splits, blocks, s);
+    // (what is kept already is not written again)
+    for (int i = 0; i < n && st == FREE_OK && blocks; ++i)
+        st = launch_join(p[i], q[i].out == p[i].gu ? FFN_GATE : p[i].kind, q[i].out, plan.splits, s);
+    return st;
 }
 
 int32_t launch_ffn_products(const FfnProduct<bf16_t>* p, int n, float* part, hipStream_t s) {

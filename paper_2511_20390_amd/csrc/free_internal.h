@@ -309,11 +309,16 @@ int32_t launch_linear_f32(const float* X, const float* W, const float* bias, int
                           float* out, float* resid, RowVec gate, hipStream_t s, int cu_share = 1);
 // The same products plain, without bias, of operands that may be K-major (x_by_k: X [K, M], W [K, N], ldx / ldw values from k to k; w_by_k:
 // W [K, N]); row-major ones have rows of K values, K % 32 == 0.  N % 4 == 0, 16-byte aligned.  blocks: sums over `parts` parts of K as blocks
-// of 32 x 32, [part][M / 32][N / 32][4][lane][4]; otherwise the result's rows, parts 1.  large: 128 x 128 tiles, else 64 x 64; the time such
-// a launch takes, us, for a number of tiles and of slices of 32 k.
+// of 32 x 32, [part][M / 32][N / 32][4][lane][4]; otherwise the result's rows, parts 1.  large: 128 x 128 tiles, else 64 x 64.  n: one
+// product, or with x_by_k two of one K.  product_f32_time: the time a launch takes, us, for a number of tiles and of slices of 32 k.
+struct ProductF32 {
+    const float *X, *W;
+    int64_t ldx, ldw;
+    int32_t M, N, K;
+    float* out;
+};
 double product_f32_time(bool large, int64_t work, int32_t slices);
-int32_t launch_product_f32(bool x_by_k, bool w_by_k, bool large, const float* X, int64_t ldx, const float* W, int64_t ldw, int32_t M, int32_t N,
-                           int32_t K, int32_t parts, bool blocks, float* out, hipStream_t s);
+int32_t launch_products_f32(bool x_by_k, bool w_by_k, bool large, const ProductF32* p, int n, int32_t parts, bool blocks, hipStream_t s);
 // shapes the folded-LayerNorm epilogues cover: M rows of width D normalised, rows_per_sample tokens per sample
 bool mfma_ln_fold_supported(int32_t M, int32_t D, int32_t rows_per_sample);
 // the same kernel on fp32 operands (v_mfma_f32_32x32x2_f32), fp32 output

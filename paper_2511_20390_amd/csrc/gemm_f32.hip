@@ -64,17 +64,29 @@ __device__ __forceinline__ void unrolled(F&& f, std::integer_sequence<int, I...>
 // to each other, and the last slice ends where the matrix does.
 constexpr int FREE_EPI_STORE = 8;
 constexpr bool plain_product(int epi) { return epi == FREE_EPI_STORE || epi == FREE_EPI_PARTIAL; }
+// Two products of one K (the two weights' gradients) can share a launch: few tiles each, they fill the chip together.
 struct PlainOperands {
     int64_t ldx = 0, ldw = 0;                // K-major: values from k to k
     int32_t part_slices = 0;
+    int32_t first1 = 0x7fffffff;             // workgroups of the first product; the second one's operands and tiles:
+    ProductF32 second{};
+    int32_t tiles_m1 = 0, tiles_n1 = 0;
 };
 
 template <int BM, int BN, int SETS, int EPI, bool XK = false, bool WK = false>
 __global__ __launch_bounds__(kWaves * 64) void gemm_f32_kernel(
-    const float* __restrict__ X, const float* __restrict__ W, const float* __restrict__ bias, int32_t M, int32_t N, int32_t K,
-    int32_t tiles_m, int32_t tiles_n, int32_t group_m, int32_t vec_ok, float* __restrict__ out, float* __restrict__ resid,
+    const float* __restrict__ X0, const float* __restrict__ W0, const float* __restrict__ bias, int32_t M0, int32_t N0, int32_t K,
+    int32_t tiles_m0, int32_t tiles_n0, int32_t group_m, int32_t vec_ok, float* __restrict__ out0, float* __restrict__ resid,
     RowVec gate, PlainOperands plain) {
     constexpr bool kParts = EPI == FREE_EPI_PARTIAL;
+    const bool second = XK && static_cast<int>(blockIdx.x) >= plain.first1;
+    const float* __restrict__ X = second ? plain.second.X : X0;
+    const float* __restrict__ W = second ? plain.second.W : W0;
+    float* __restrict__ out = second ? plain.second.out : out0;
+    const int32_t M = second ? plain.second.M : M0, N = second ? plain.second.N : N0;
+    const int32_t tiles_m = second ? plain.tiles_m1 : tiles_m0, tiles_n = second ? plain.tiles_n1 : tiles_n0;
+    const int64_t ldx = second ? plain.second.ldx : plain.ldx, ldw = second ? plain.second.ldw : plain.ldw;
+    const int pid = second ? blockIdx.x - plain.first1 : blockIdx.x;
     constexpr int NW = kWaves, NT = NW * 64;
     constexpr int TM = BM / 64, TN = BN / 64;                           // 32 x 32 blocks of a wavefront
     constexpr int kRows = BM + BN, kPlane = kRows * kPlaneRow, kStage = 3 * kPlane;
@@ -83,8 +95,8 @@ __global__ __launch_bounds__(kWaves * 64) void gemm_f32_kernel(
     extern __shared__ __attribute__((aligned(16))) char lds[];
 
     int tile_m, tile_n;
-    const int split = kParts ? blockIdx.x / (tiles_m * tiles_n) : 0;
-    tile_coords(group_m, kParts ? blockIdx.x % (tiles_m * tiles_n) : blockIdx.x, tiles_m, tiles_n, &tile_m, &tile_n);
+    const int split = kParts ? pid / (tiles_m * tiles_n) : 0;
+    tile_coords(group_m, kParts ? pid % (tiles_m * tiles_n) : pid, tiles_m, tiles_n, &tile_m, &tile_n);
     const int m0 = tile_m * BM, n0 = tile_n * BN;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int ks = wave >> 2, wm = (wave >> 1) & 1, wn = wave & 1;
@@ -116,10 +128,10 @@ __global__ __launch_bounds__(kWaves * 64) void gemm_f32_kernel(
     auto fetch = [&](int kt, auto set_c, int i) {
         constexpr int set = decltype(set_c)::value;
         if constexpr (XK) {
-            if (i < UX) return fetch_column(X, plain.ldx, m0, kt, reg[set][i], i);
+            if (i < UX) return fetch_column(X, ldx, m0, kt, reg[set][i], i);
         }
         if constexpr (WK) {
-            if (i >= UX) return fetch_column(W, plain.ldw, n0, kt, reg[set][i], i - UX);
+            if (i >= UX) return fetch_column(W, ldw, n0, kt, reg[set][i], i - UX);
         }
         const int soff = 8 * ((i < UX ? i : i - UX) * NW + wave) * K * 4 + (kt0 + kt) * kRowBytes;
         const u32x4_t v = __builtin_amdgcn_raw_buffer_load_b128(i < UX ? xsrd : wsrd, voff, soff, 0);
@@ -291,13 +303,13 @@ __global__ __launch_bounds__(kWaves * 64) void gemm_f32_kernel(
                     f32x4_t xv, wv;
                     if constexpr (XK) {
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) xv[e] = k + 4 * lhi + e < K ? X[static_cast<int64_t>(k + 4 * lhi + e) * plain.ldx + gm] : 0.f;
+                        for (int e = 0; e < 4; ++e) xv[e] = k + 4 * lhi + e < K ? X[static_cast<int64_t>(k + 4 * lhi + e) * ldx + gm] : 0.f;
                     } else {
                         xv = *reinterpret_cast<const f32x4_t*>(xr + k);
                     }
                     if constexpr (WK) {
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) wv[e] = k + 4 * lhi + e < K ? W[static_cast<int64_t>(k + 4 * lhi + e) * plain.ldw + gn] : 0.f;
+                        for (int e = 0; e < 4; ++e) wv[e] = k + 4 * lhi + e < K ? W[static_cast<int64_t>(k + 4 * lhi + e) * ldw + gn] : 0.f;
                     } else {
                         wv = *reinterpret_cast<const f32x4_t*>(wr + k);
                     }
@@ -376,26 +388,35 @@ int32_t launch_tile(const Args& a, int32_t epi) {
 }
 
 template <int B, int SETS, int EPI, bool XK, bool WK>
-int32_t launch_plain(const float* X, const float* W, int32_t M, int32_t N, int32_t K, const PlainOperands& o, int parts, float* out, hipStream_t s) {
-    const int tiles_m = (M + B - 1) / B, tiles_n = (N + B - 1) / B, total = tiles_m * tiles_n;
+int32_t launch_plain(const ProductF32* p, int n, int parts, hipStream_t s) {
+    const auto tiles = [](int32_t v) { return (v + B - 1) / B; };
+    const int tiles_m = tiles(p[0].M), tiles_n = tiles(p[0].N);
+    PlainOperands o;
+    o.ldx = p[0].ldx;
+    o.ldw = p[0].ldw;
+    o.part_slices = ((p[0].K + kSlice - 1) / kSlice + parts - 1) / parts;
+    int total = tiles_m * tiles_n * parts;
+    if (n == 2) {
+        o.first1 = total;
+        o.second = p[1];
+        o.tiles_m1 = tiles(p[1].M);
+        o.tiles_n1 = tiles(p[1].N);
+        total += o.tiles_m1 * o.tiles_n1 * parts;
+    }
     const size_t lds = 4 * static_cast<size_t>(B) * 3 * kPlaneRow;
     auto kern = gemm_f32_kernel<B, B, SETS, EPI, XK, WK>;
     static LdsLimit limit;
     if (!limit.allow(reinterpret_cast<const void*>(kern), lds)) return FREE_ERR_HIP;
-    const int group_m = total <= 2 * device_cus() ? tiles_m : 8;
-    hipLaunchKernelGGL(kern, dim3(total * parts), dim3(kWaves * 64), lds, s, X, W, nullptr, M, N, K, tiles_m, tiles_n, group_m, 1, out, nullptr,
-                       RowVec{nullptr, 0, 1}, o);
+    const int group_m = tiles_m * tiles_n <= 2 * device_cus() ? tiles_m : 8;
+    hipLaunchKernelGGL(kern, dim3(total), dim3(kWaves * 64), lds, s, p[0].X, p[0].W, nullptr, p[0].M, p[0].N, p[0].K, tiles_m, tiles_n, group_m, 1,
+                       p[0].out, nullptr, RowVec{nullptr, 0, 1}, o);
     return launch_ok() ? FREE_OK : FREE_ERR_HIP;
 }
 
 template <bool XK, bool WK>
-int32_t launch_layout(bool large, const float* X, const float* W, int32_t M, int32_t N, int32_t K, const PlainOperands& o, int parts, bool blocks,
-                      float* out, hipStream_t s) {
-    if (blocks)
-        return large ? launch_plain<128, 2, FREE_EPI_PARTIAL, XK, WK>(X, W, M, N, K, o, parts, out, s)
-                     : launch_plain<64, 4, FREE_EPI_PARTIAL, XK, WK>(X, W, M, N, K, o, parts, out, s);
-    return large ? launch_plain<128, 2, FREE_EPI_STORE, XK, WK>(X, W, M, N, K, o, 1, out, s)
-                 : launch_plain<64, 4, FREE_EPI_STORE, XK, WK>(X, W, M, N, K, o, 1, out, s);
+int32_t launch_layout(bool large, const ProductF32* p, int n, int parts, bool blocks, hipStream_t s) {
+    if (blocks) return large ? launch_plain<128, 2, FREE_EPI_PARTIAL, XK, WK>(p, n, parts, s) : launch_plain<64, 4, FREE_EPI_PARTIAL, XK, WK>(p, n, parts, s);
+    return large ? launch_plain<128, 2, FREE_EPI_STORE, XK, WK>(p, n, 1, s) : launch_plain<64, 4, FREE_EPI_STORE, XK, WK>(p, n, 1, s);
 }
 
 // us of a launch of `work` tiles of 64 x 64 or 128 x 128 and nk slices each on `cus` compute units; see launch_linear_f32
@@ -408,15 +429,9 @@ double tile_time(bool large, double work, double nk, double cus) {
 
 double product_f32_time(bool large, int64_t work, int32_t slices) { return tile_time(large, static_cast<double>(work), slices, 256.0); }
 
-int32_t launch_product_f32(bool x_by_k, bool w_by_k, bool large, const float* X, int64_t ldx, const float* W, int64_t ldw, int32_t M, int32_t N,
-                           int32_t K, int32_t parts, bool blocks, float* out, hipStream_t s) {
-    PlainOperands o;
-    o.ldx = ldx;
-    o.ldw = ldw;
-    o.part_slices = ((K + kSlice - 1) / kSlice + parts - 1) / parts;
-    if (x_by_k) return launch_layout<true, true>(large, X, W, M, N, K, o, parts, blocks, out, s);
-    return w_by_k ? launch_layout<false, true>(large, X, W, M, N, K, o, parts, blocks, out, s)
-                  : launch_layout<false, false>(large, X, W, M, N, K, o, parts, blocks, out, s);
+int32_t launch_products_f32(bool x_by_k, bool w_by_k, bool large, const ProductF32* p, int n, int32_t parts, bool blocks, hipStream_t s) {
+    if (x_by_k) return launch_layout<true, true>(large, p, n, parts, blocks, s);
+    return w_by_k ? launch_layout<false, true>(large, p, 1, parts, blocks, s) : launch_layout<false, false>(large, p, 1, parts, blocks, s);
 }
 
 bool linear_f32_covers(const float* X, const float* W, int32_t M, int32_t N, int32_t K) {
