@@ -197,7 +197,7 @@ int32_t products_backward(const Sizes& z, const T* dy, const T* x, const T* w_in
 }
 
 // the way of few rows, which keeps nothing and needs room for h alone
-bool few_rows(const Sizes& z, bool keep) { return !keep && ffn_rows_pay(z.M, z.D, z.F, z.es == 2 ? FREE_BF16 : FREE_FP32); }
+bool few_rows(const Sizes& z, bool keep) { return !keep && ffn_rows_pay(z.M, z.D, z.F, z.padded); }
 
 template <typename T>
 int32_t forward_of(const Sizes& z, const T* x, const T* w_in, const T* w_out, int32_t act, T* out, char* saved, char* ws, hipStream_t s) {

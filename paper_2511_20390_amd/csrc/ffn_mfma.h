@@ -45,7 +45,7 @@ int32_t launch_ffn_products(const FfnProduct<bf16_t>* p, int n, float* part, hip
 int32_t launch_ffn_products(const FfnProduct<float>* p, int n, float* part, hipStream_t s);
 
 // ffn_rows.hip: y of up to 32 token rows, any D and F, in two launches; h: room for [M, F].  ffn_rows_pay: where that is the faster way.
-bool ffn_rows_pay(int32_t M, int32_t D, int32_t F, int32_t dtype);
+bool ffn_rows_pay(int32_t M, int32_t D, int32_t F, bool tiles_padded);
 template <typename T>
 int32_t launch_ffn_rows(const T* x, const T* w_in, const T* w_out, int32_t M, int32_t D, int32_t F, int32_t act, T* h, T* out, hipStream_t s);
 

@@ -173,10 +173,12 @@ int32_t launch_ffn_rows(const T* x, const T* w_in, const T* w_out, int32_t M, in
     const int32_t st = launch_rows<T, true>(RowArgs{x, w_in, h, M, F, D, act}, s);
     return st != FREE_OK ? st : launch_rows<T, false>(RowArgs{h, w_out, out, M, D, F, act}, s);
 }
-// Against the tiles of ffn_mfma.hip and gemm_f32.hip, us: bf16 17 to 32 rows, 384 x 1536 9 against 15, 1152 x 4608 25.5 against 25.7, 4096 x
-// 10240 63 to 80 against 65; fp32 32 rows, 1152 x 4608 50 against 88, 4096 x 10240 191 against 238 (48 rows 286 against 259).
-bool ffn_rows_pay(int32_t M, int32_t D, int32_t F, int32_t dtype) {
-    return M <= 16 || (M <= 32 && (dtype == FREE_FP32 || static_cast<int64_t>(D) * F <= 1 << 22));
+// Against the tiles of ffn_mfma.hip and gemm_f32.hip, us.  16 rows: bf16 384 x 1536 7.5 against 15, 1152 x 4608 18.3 against 26, 4096 x 10240
+// 60.9 against 64.7; fp32 10.9 against 24, 31.9 against 38, 128 against 143.  32 rows: bf16 9.5 against 15.3, 27.0 against 26.9, 64.4 against 65.7
+// (17 rows of 4096 x 10240 63.9 against 65.0); fp32 15.5 against 24, 49.8 against 38.8, 191 against 147.  Where the tiles would need
+// padded copies of the weights, three times their bytes, 32 rows always.
+bool ffn_rows_pay(int32_t M, int32_t D, int32_t F, bool tiles_padded) {
+    return M <= 16 || (M <= 32 && (tiles_padded || static_cast<int64_t>(D) * F <= 1 << 22));
 }
 
 template int32_t launch_ffn_rows(const bf16_t*, const bf16_t*, const bf16_t*, int32_t, int32_t, int32_t, int32_t, bf16_t*, bf16_t*, hipStream_t);
