@@ -17,6 +17,10 @@
 // it computes, and adds dy xh and dy to registers, per column; at its end its wavefronts add theirs through LDS, in order, and write
 // one partial row; a second launch adds the partial rows of a sample in a fixed order (no atomics: equal inputs give equal bits).  A sample
 // that one workgroup walks is written directly.
+//
+// us, in a row of launches on inputs from memory (at the 5.1 TB/s of a large copy): forward 12288 x 1152 fp32 -> bf16 19.0 (16.7), 16384 x
+// 4096 bf16 49 (53), 32768 x 768 bf16 20.5 (19.8); gradient with its second launch 35.1 (27.8), 87 (79), 40 (29.7), and 4096 x 8192 fp32 69 (66),
+// 1531 x 1001 fp32 17.4 (3.6: two launches and their round trips).
 #include <algorithm>
 
 #include "free_internal.h"

@@ -8,7 +8,9 @@
 // turns, where an fp32 product of position and frequency is off by a turn from 2^24 on.  Of it the leading 32 bits go to sincospi.
 //
 // Bound by HBM (every value read and written once).  A thread holds V pairs of a token and computes their sines and cosines once for
-// up to kHeads heads, whose loads are all in flight before the first is turned.
+// up to kHeads heads, whose loads are all in flight before the first is turned.  32760 tokens of 48 heads of 128 in bf16: 154 us, 5.2 TB/s
+// read and written (a copy of 1 GiB: 5.1); fp32, 15640 tokens of 24 heads of 64, halves of the sections 24 values apart, 37.5 us, 5.1 TB/s;
+// 256 tokens of 32 heads of 72, 4.6 us, of which an empty launch takes half.
 #include <algorithm>
 #include <cmath>
 
