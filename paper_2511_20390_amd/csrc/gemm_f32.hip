@@ -64,7 +64,8 @@ __device__ __forceinline__ void unrolled(F&& f, std::integer_sequence<int, I...>
 // to each other, and the last slice ends where the matrix does.
 constexpr int FREE_EPI_STORE = 8;
 constexpr bool plain_product(int epi) { return epi == FREE_EPI_STORE || epi == FREE_EPI_PARTIAL; }
-// Two products of one K (the two weights' gradients) can share a launch: few tiles each, they fill the chip together.
+// Two products of one K (the two weights' gradients) can share a launch: few tiles each, they fill the chip together (1000 rows, 384 x 1536: 28 +
+// 5 + 25 us in two launches and a join, 41 in one).
 struct PlainOperands {
     int64_t ldx = 0, ldw = 0;                // K-major: values from k to k
     int32_t part_slices = 0;
