@@ -206,6 +206,29 @@ def test_norm_far_rows():
     u.check(db[None], ref[3], "far dbias")
 
 
+def test_norm_many_rows():
+    """More rows than a grid's workgroups take at once."""
+    import torch
+    from paper_2511_20390_amd import binding as b
+    from tests import block_ops_util as u
+    M, D = 70_000_003, 3
+    g = _gen(22)
+    x = torch.zeros(M, D, dtype=torch.bfloat16, device="cuda")
+    at = torch.tensor([0, 1, 67_108_863, 67_108_864, 67_108_865, M - 1], device="cuda")
+    x[at] = _rnd(g, 6, D, dtype=torch.bfloat16)
+    w, bias = _rnd(g, D), _rnd(g, D)
+    out = b.op_layer_norm(x, w, bias)
+    ref = u.norm_reference(x[at], w, bias, 6, False, 1e-6, x[at])
+    u.check(out[at], ref[0], "many rows")
+    rest = torch.ones(M, dtype=torch.bool, device="cuda")
+    rest[at] = False
+    assert (out[rest] == bias.to(torch.bfloat16)).all()
+    dx, dw, db = b.op_layer_norm_backward(x, x, w)
+    u.check(dx[at], ref[1], "many rows dx")
+    u.check(dw, ref[2], "many rows dweight")
+    u.check(db, ref[3], "many rows dbias")
+
+
 # ---- rotary positions ------------------------------------------------------------------------------------------------
 ROPE = [(72, [36, 36]), (128, [16, 56, 56]), (128, [128]), (64, [8, 24, 24]), (2, [2]), (6, [2, 2, 2]), (40, [4, 6, 8, 10]), (16, [0, 8]),
         (256, [64, 96, 96]), (34, [16, 16]), (20, [10])]
