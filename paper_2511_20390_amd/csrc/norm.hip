@@ -238,7 +238,7 @@ __global__ __launch_bounds__(back_threads(LANES)) void norm_backward_kernel(Norm
     constexpr int kGroups = back_threads(LANES) / LANES, WPR = LANES / 64;
     constexpr bool kHoldWeight = NV * VE <= 20;           // as registers allow; otherwise read again for every row, from the L1
     __shared__ float4 red[2][kGroups][WPR > 1 ? WPR : 1];
-    extern __shared__ float cols[];                       // [2][D]: column sums of the workgroup (kGroups > 1)
+    extern __shared__ __attribute__((aligned(16))) float cols[];          // [2][NV VE LANES]: column sums of the workgroup (kGroups > 1)
     const int wave_in_row = threadIdx.x % LANES / 64;
     const int group = LANES < 64 ? threadIdx.x / LANES : __builtin_amdgcn_readfirstlane(threadIdx.x / LANES);
     const int sample = blockIdx.x / chunks, chunk = blockIdx.x % chunks;
@@ -385,21 +385,21 @@ __global__ __launch_bounds__(back_threads(LANES)) void norm_backward_kernel(Norm
             __syncthreads();
             if (turn != k) continue;
 #pragma unroll
-            for (int c = 0; c < NV; ++c) {
+            for (int c = 0; c < NV; ++c)
 #pragma unroll
-                for (int e = 0; e < VE; ++e) {
-                    const int i = at.at(c) + e;
-                    if (i >= a.D) continue;
+                for (int e = 0; e < VE; e += 4) {                 // (whole pieces, past the end of a row too)
+                    float4* w4 = reinterpret_cast<float4*>(cols + at.at(c) + e);
+                    float4* b4 = reinterpret_cast<float4*>(cols + NV * VE * LANES + at.at(c) + e);
                     if (k > 0) {
-                        dw[c][e] += cols[i];
-                        db[c][e] += cols[a.D + i];
+                        const float4 p = *w4, q = *b4;
+                        dw[c][e] += p.x; dw[c][e + 1] += p.y; dw[c][e + 2] += p.z; dw[c][e + 3] += p.w;
+                        db[c][e] += q.x; db[c][e + 1] += q.y; db[c][e + 2] += q.z; db[c][e + 3] += q.w;
                     }
                     if (k < kLast - 1) {
-                        cols[i] = dw[c][e];
-                        cols[a.D + i] = db[c][e];
+                        *w4 = make_float4(dw[c][e], dw[c][e + 1], dw[c][e + 2], dw[c][e + 3]);
+                        *b4 = make_float4(db[c][e], db[c][e + 1], db[c][e + 2], db[c][e + 3]);
                     }
                 }
-            }
         }
         if (turn != kLast - 1) return;
     }
@@ -505,7 +505,7 @@ int32_t backward_of(const NormArgs& a, const NormGrad& gr, int samples, hipStrea
     constexpr int VEC = kPiece<XT, OT>;
     const Layout l = backward_layout(VEC, a.D);
     const int threads = back_threads(l.lanes);
-    const size_t lds = l.lanes == threads || gr.dw == nullptr ? 0 : static_cast<size_t>(2) * a.D * sizeof(float);
+    const size_t lds = l.lanes == threads || gr.dw == nullptr ? 0 : static_cast<size_t>(2) * VEC * l.nv * l.lanes * sizeof(float);
     const dim3 grid(samples * gr.chunks), block(threads);
 #define FREE_CASE(VE, NV, LANES)                                                                                                     \
     if (l.nv == NV && l.lanes == LANES) {                                                                                            \
