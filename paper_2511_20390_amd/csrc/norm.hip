@@ -4,7 +4,7 @@
 // with s = row / rows_per_sample (one sample: the affine layer norm) and w_s the given weight, or 1 + it (adaLN's scale).
 //
 // Both passes are bound by HBM: forward reads x and writes y, backward reads x and dy and writes dx.  So a row is read once and stays
-// in registers, over 16 lanes (rows of up to 256 values: 100000 x 130 bf16, forward 40 -> 20 us, gradient 110 -> 48 against a wavefront each) or 1 to 8
+// in registers, over 16 lanes (rows of up to 256 values: 100000 x 130 bf16, forward 40 -> 20 us, gradient 110 -> 46 against a wavefront each) or 1 to 8
 // wavefronts; nothing but the inputs is needed again, so no statistics are kept between the passes.
 // Variance and products with xh are summed around a mean, so that nothing cancels: every wavefront takes the mean of its own values
 // first, without waiting for the others, and sums around that; then the wavefronts of a row exchange all their sums at once - one
@@ -19,8 +19,8 @@
 // that one workgroup walks is written directly.
 //
 // us, in a row of launches on inputs from memory (at the 5.1 TB/s of a large copy): forward 12288 x 1152 fp32 -> bf16 19.0 (16.7), 16384 x
-// 4096 bf16 49 (53), 32768 x 768 bf16 20.5 (19.8); gradient with its second launch 35.1 (27.8), 87 (79), 40 (29.7), and 4096 x 8192 fp32 69 (66),
-// 1531 x 1001 fp32 17.4 (3.6: two launches and their round trips).
+// 4096 bf16 49 (53), 32768 x 768 bf16 20.5 (19.8); gradient with its second launch 32.0 (27.8), 86 (79), 37 (29.7), and 4096 x 8192 fp32 69 (66),
+// 1531 x 1001 fp32 14.2 (3.6: two launches and their round trips).
 #include <algorithm>
 
 #include "free_internal.h"
@@ -236,7 +236,10 @@ __global__ __launch_bounds__(kThreads) void norm_forward_kernel(NormArgs a) {
 template <typename XT, typename OT, int VE, int NV, int LANES, bool kTail>
 __global__ __launch_bounds__(back_threads(LANES)) void norm_backward_kernel(NormArgs a, NormGrad gr, int32_t chunks) {
     constexpr int kGroups = back_threads(LANES) / LANES, WPR = LANES / 64;
-    constexpr bool kHoldWeight = NV * VE <= 20;           // as registers allow; otherwise read again for every row, from the L1
+    // The weight is held in registers: read again for every row its loads would wait behind the next row's (12288 x 1152 35 -> 47 us).  32
+    // values per lane leave no registers for the next row's beside it (4096 x 12288 bf16 75 us, with the next row's loads
+    // and without the weight 98).
+    constexpr bool kAhead = NV * VE <= 20;
     __shared__ float4 red[2][kGroups][WPR > 1 ? WPR : 1];
     extern __shared__ __attribute__((aligned(16))) float cols[];          // [2][NV VE LANES]: column sums of the workgroup (kGroups > 1)
     const int wave_in_row = threadIdx.x % LANES / 64;
@@ -246,20 +249,18 @@ __global__ __launch_bounds__(back_threads(LANES)) void norm_backward_kernel(Norm
     const int64_t rows = row0 + a.rows_per_sample < a.M ? a.rows_per_sample : a.M - row0;
     const float* w = a.weight ? a.weight + static_cast<int64_t>(sample) * a.stride : nullptr;
     const Place<VE, NV, LANES> at(a.D);
-    float dw[NV][VE], db[NV][VE], held[kHoldWeight ? NV : 1][VE];
+    float dw[NV][VE], db[NV][VE], held[NV][VE];
 #pragma unroll
     for (int c = 0; c < NV; ++c)
 #pragma unroll
         for (int e = 0; e < VE; ++e) dw[c][e] = db[c][e] = 0.f;
-    if constexpr (kHoldWeight) {
 #pragma unroll
-        for (int c = 0; c < NV; ++c) {
-            if (at.has(c)) {
-                load_weight<kTail, VE>(w, a.plus, at.at(c), at.left(c), held[c]);
-            } else {
+    for (int c = 0; c < NV; ++c) {
+        if (at.has(c)) {
+            load_weight<kTail, VE>(w, a.plus, at.at(c), at.left(c), held[c]);
+        } else {
 #pragma unroll
-                for (int e = 0; e < VE; ++e) held[c][e] = 0.f;
-            }
+            for (int e = 0; e < VE; ++e) held[c][e] = 0.f;
         }
     }
     Piece<XT, VE> xr[NV];
@@ -281,11 +282,12 @@ __global__ __launch_bounds__(back_threads(LANES)) void norm_backward_kernel(Norm
     };
     const int64_t step = static_cast<int64_t>(chunks) * kGroups;
     const int64_t start = static_cast<int64_t>(chunk) * kGroups;
-    if (start < rows) request(start);
+    if (kAhead && start < rows) request(start);
     int parity = 0;
     for (int64_t base = start; base < rows; base += step, parity ^= 1) {
         const bool on = base + group < rows;
         float v[NV][VE], g[NV][VE], s = 0.f;
+        if constexpr (!kAhead) request(base);
 #pragma unroll
         for (int c = 0; c < NV; ++c)
 #pragma unroll
@@ -294,27 +296,17 @@ __global__ __launch_bounds__(back_threads(LANES)) void norm_backward_kernel(Norm
                 g[c][e] = gradr[c].at(e);
                 s += v[c][e];
             }
-        if (base + step < rows) request(base + step);
+        if (kAhead && base + step < rows) request(base + step);
         s = lanes_sum<LANES>(s);
         const float mean = at.values > 0.f ? s / at.values : 0.f;
         float q = 0.f, sg = 0.f, sgx = 0.f;
 #pragma unroll
         for (int c = 0; c < NV; ++c) {
-            float wv[VE];
-            if constexpr (kHoldWeight) {
-#pragma unroll
-                for (int e = 0; e < VE; ++e) wv[e] = held[c][e];
-            } else if (at.has(c)) {
-                load_weight<kTail, VE>(w, a.plus, at.at(c), at.left(c), wv);
-            } else {
-#pragma unroll
-                for (int e = 0; e < VE; ++e) wv[e] = 0.f;
-            }
 #pragma unroll
             for (int e = 0; e < VE; ++e) {
                 v[c][e] = at.has(c) && (!kTail || e < at.left(c)) ? v[c][e] - mean : 0.f;
                 q = fmaf(v[c][e], v[c][e], q);
-                const float gw = g[c][e] * wv[e];
+                const float gw = g[c][e] * held[c][e];
                 sg += gw;
                 sgx = fmaf(gw, v[c][e], sgx);
             }
@@ -348,19 +340,13 @@ __global__ __launch_bounds__(back_threads(LANES)) void norm_backward_kernel(Norm
 #pragma unroll
         for (int c = 0; c < NV; ++c) {
             if (!at.has(c)) continue;
-            float wv[VE], o[VE];
-            if constexpr (kHoldWeight) {
-#pragma unroll
-                for (int e = 0; e < VE; ++e) wv[e] = held[c][e];
-            } else {
-                load_weight<kTail, VE>(w, a.plus, at.at(c), at.left(c), wv);
-            }
+            float o[VE];
 #pragma unroll
             for (int e = 0; e < VE; ++e) {
                 const float xh = (v[c][e] + shift) * r;
                 dw[c][e] = fmaf(g[c][e], xh, dw[c][e]);
                 db[c][e] += g[c][e];
-                o[e] = r * (g[c][e] * wv[e] - m1 - xh * m2);
+                o[e] = r * (g[c][e] * held[c][e] - m1 - xh * m2);
             }
             store_piece<kTail, XT, VE>(dx + at.at(c), at.left(c), o);
         }
