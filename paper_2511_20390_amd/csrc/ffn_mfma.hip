@@ -26,8 +26,9 @@
 // The library's product of 8192^3 reaches 1325 on that card.
 #include <algorithm>
 
-#include "free_internal.h"
+#include "ffn_act.h"
 #include "ffn_mfma.h"
+#include "free_internal.h"
 #include "gemm_dma.h"
 
 namespace freemi {
@@ -55,19 +56,6 @@ struct Launch {
     int32_t first1;              // tiles (and parts of K) of p[0]
     int32_t total;               // of both
 };
-
-// act(v), act'(v) with the hardware's exponential and reciprocal (1 ulp each): both activations are v s with s = 1 / (1 + 2^-t),
-// t = v log2(e) for SiLU and v (a + b v^2) for the tanh form of GELU
-__device__ __forceinline__ void act_fast(float v, int act, float* f, float* df) {
-    constexpr float kLog2e = 1.4426950408889634f, kA = 2.0f * 0.7978845608028654f, kB = kA * 0.044715f;
-    const float v2 = v * v;
-    const float t = act == FREE_ACT_SILU ? -v * kLog2e : -v * fmaf(v2, kB * kLog2e, kA * kLog2e);
-    const float s = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(t));
-    const float slope = act == FREE_ACT_SILU ? v : v * fmaf(v2, 3.0f * kB, kA);      // v dt / dv
-    *f = v * s;
-    // s (1 - s): where slope is infinite s is 0 or 1 exactly
-    *df = s == 0.f || s == 1.f ? s : fmaf(s * (1.0f - s), slope, s);
-}
 
 // Whether a workgroup does several tiles (LDS for the stages and for the epilogue, one workgroup per compute unit): launches of one product
 // in whole sums, the others having few tiles, whose epilogue is short of neither registers (the gated gradient would spill 150) nor
@@ -465,21 +453,6 @@ struct Join {
     int32_t M, N, cols, fold, fold_to, splits, act;       // N: hidden values for the gated kinds
 };
 
-// fp32: the library's exponential and tanh in place of the hardware's
-__device__ __forceinline__ void act_exact(float v, int act, float* f, float* df) {
-    if (act == FREE_ACT_SILU) {
-        const float s = 1.0f / (1.0f + expf(-v));
-        *f = v * s;
-        *df = s == 0.f || s == 1.f ? s : s * (1.0f + v * (1.0f - s));
-    } else {
-        const float k = 0.7978845608028654f;
-        const float v2 = v * v, t = tanhf(k * (v + 0.044715f * v2 * v));
-        *f = 0.5f * v * (1.0f + t);
-        // (1 - t^2) times what grows with v^3: 0 where t is one to the last bit
-        *df = fabsf(t) == 1.f ? 0.5f * (1.0f + t) : 0.5f * (1.0f + t) + 0.5f * v * (1.0f - t * t) * k * (1.0f + 3.0f * 0.044715f * v2);
-    }
-}
-
 template <FfnKind kKind, typename T>
 __global__ __launch_bounds__(256) void ffn_join_kernel(Join<T> a) {
     constexpr bool kGate = kKind == FFN_GATE || kKind == FFN_GATE_KEEP, kGrad = kKind == FFN_GATE_GRAD;
@@ -682,7 +655,8 @@ struct PlanF32 {
 };
 constexpr int kSliceF32 = 32, kMinPartF32 = 8;
 
-bool join_anyway(FfnKind k) { return k == FFN_GATE || k == FFN_GATE_KEEP || k == FFN_GATE_GRAD; }
+// a second launch whatever the parts: gate and up are in different tiles
+bool join_anyway(FfnKind k) { return k == FFN_GATE || k == FFN_GATE_KEEP; }
 
 PlanF32 plan_of(const FfnProduct<float>* p, int n) {
     PlanF32 best{false, 1};
@@ -711,7 +685,7 @@ PlanF32 plan_of(const FfnProduct<float>* p, int n) {
 }
 
 // parts in `part`, not in the place of the result (one part of a kept [g | u] is what is kept)
-bool needs_room(const FfnProduct<float>& p, int splits) { return splits > 1 || p.kind == FFN_GATE || p.kind == FFN_GATE_GRAD; }
+bool needs_room(const FfnProduct<float>& p, int splits) { return splits > 1 || p.kind == FFN_GATE; }
 
 }  // namespace
 
@@ -731,6 +705,10 @@ size_t ffn_products_part_bytes(const FfnProduct<float>* p, int n) {
 
 int32_t launch_ffn_products(const FfnProduct<float>* p, int n, float* part, hipStream_t s) {
     const PlanF32 plan = plan_of(p, n);
+    if (p[0].kind == FFN_GATE_GRAD && plan.splits == 1) {
+        const ProductF32 q{p[0].X, p[0].W, p[0].ldx, p[0].ldw, p[0].M, p[0].N, p[0].K, p[0].out};
+        return launch_gated_grad_f32(plan.large, q, p[0].gu, p[0].act, s);
+    }
     const bool blocks = plan.splits > 1 || join_anyway(p[0].kind);
     const bool x_by_k = p[0].kind == FFN_K_BY_K, w_by_k = x_by_k || p[0].kind == FFN_ROWS_BY_K || p[0].kind == FFN_GATE_GRAD;
     ProductF32 q[2];

@@ -317,6 +317,8 @@ struct ProductF32 {
     int32_t M, N, K;
     float* out;
 };
+// the gated gradient [dg | du], rows of 2 N values, of dh = X W (w_by_k) and the kept [g | u] (ffn_mfma.h); N % 64 == 0
+int32_t launch_gated_grad_f32(bool large, const ProductF32& p, const float* gu, int32_t act, hipStream_t s);
 double product_f32_time(bool large, int64_t work, int32_t slices);
 int32_t launch_products_f32(bool x_by_k, bool w_by_k, bool large, const ProductF32* p, int n, int32_t parts, bool blocks, hipStream_t s);
 // shapes the folded-LayerNorm epilogues cover: M rows of width D normalised, rows_per_sample tokens per sample
