@@ -583,17 +583,19 @@ size_t part_bytes(const FfnProduct<T>& p, int splits) {
 // Times of a workgroup, us: a launch; a slice of 64 k with all compute units at work, and with nothing in the way but its loads' latency;
 // the epilogue by what it does; slices of K-major operands against those of rows.  Fitted to 930 launches (70 to 12288 rows, widths 384 /
 // 768 / 1152 / 2048 / 4096 with 1536 to 10240 hidden values, the three tiles, K in 1 to 24 parts, every kind of product): the plan chosen
-// by them takes 1.0 % longer than the fastest one on average, 14 % at most.  What it decides, us: 12288 x 1152 x 4608, gate and up, 256 x
+// by them takes 1.0 % longer than the fastest one on average, 14 % at most.  The gated gradient has a factor of its own for K-major slices: its
+// two resident 128 x 128 tiles are slower in long launches than products without its reads (4096 x 4096 x 10240, backward pass 1802 us, with 256 x 256
+// tiles 1755; 44 sizes of 300 to 12288 rows: 0.2 % longer than the fastest tile on average).  What it decides, us: 12288 x 1152 x 4608, gate and up, 256 x
 // 256 tiles 257, 128 x 128 322; 4096 x 1152 x 4608, the gated gradient, 256 x 256 100, 128 x 128 - a workgroup's epilogue beside another's
 // products - 79; 128 x 1152 x 4608, the down product, K whole 46, in 12 parts 9 and 7 for the join.
 struct TileTime {
     Tile tile;
-    double launch, slice, alone, store, gate, grad, part, one_k_major, both_k_major;
+    double launch, slice, alone, store, gate, grad, part, one_k_major, grad_k_major, both_k_major;
     int resident;                    // workgroups per compute unit
 };
-constexpr TileTime kTileTimes[] = {{{256, 256}, 0.46, 1.15, 0.58, 7.6, 8.8, 16.0, 10.5, 1.05, 1.06, 1},
-                                   {{128, 256}, 1.35, 0.89, 0.53, 4.8, 3.6, 9.5, 6.3, 0.82, 0.83, 1},
-                                   {{128, 128}, 3.25, 0.58, 0.49, 1.9, 6.7, 6.9, 4.0, 0.64, 1.01, 2}};
+constexpr TileTime kTileTimes[] = {{{256, 256}, 0.46, 1.15, 0.58, 7.6, 8.8, 16.0, 10.5, 1.05, 1.05, 1.06, 1},
+                                   {{128, 256}, 1.35, 0.89, 0.53, 4.8, 3.6, 9.5, 6.3, 0.82, 0.82, 0.83, 1},
+                                   {{128, 128}, 3.25, 0.58, 0.49, 1.9, 6.7, 6.9, 4.0, 0.64, 0.72, 1.01, 2}};
 constexpr int kUnits = 256;          // compute units; not asked of the device, as a workspace's size must not depend on which is current
 constexpr int kMinPart = 4;          // slices of a part of K
 
@@ -615,7 +617,7 @@ Plan plan_of(const FfnProduct<bf16_t>* p, int n) {
         for (const TileTime& t : kTileTimes) {
             int64_t work = 0;
             for (int i = 0; i < n; ++i) work += tiles_of(p[i], t.tile, splits > 1) * plan.splits[i];
-            const double slice = t.slice * (kind == FFN_K_BY_K ? t.both_k_major : kind == FFN_ROWS_BY_K || kind == FFN_GATE_GRAD ? t.one_k_major : 1.0);
+            const double slice = t.slice * (kind == FFN_K_BY_K ? t.both_k_major : kind == FFN_GATE_GRAD ? t.grad_k_major : kind == FFN_ROWS_BY_K ? t.one_k_major : 1.0);
             const double end = splits > 1 ? t.part : p[0].gated() ? t.gate : kind == FFN_GATE_GRAD ? t.grad : t.store;
             const int64_t rounds = work / (kUnits * t.resident), rest = work % (kUnits * t.resident), share = (rest + kUnits - 1) / kUnits;
             double time = t.launch + join + rounds * (slices * std::max(t.alone, slice * t.resident) + end);
