@@ -22,7 +22,7 @@
 //
 // Bound by the matrix pipe at the clock that the power limit leaves (1.7 GHz in the long launches; busy 0.65 to 0.78 of the cycles; LDS bank
 // conflicts 1 % of its cycles).  Medians: 12288 x 1152 x 4608, gate and up 230 us (1137 TFLOP/s), down 117 (1119); 4096 x 4096 x 10240, gate and up with
-// both kept 550 (1250), down 276 (1244), gated gradient 425 (809: 0.8 GB of g, u, dg and du besides), dx 605 (1135), both weights 809 (1274).
+// both kept 550 (1250), down 276 (1244), gated gradient 389 (883: 0.5 GB of g, u, dg and du besides), dx 605 (1135), both weights 809 (1274).
 // The library's product of 8192^3 reaches 1325 on that card.
 #include <algorithm>
 
