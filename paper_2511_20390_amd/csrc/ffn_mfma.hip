@@ -122,10 +122,9 @@ __global__ __launch_bounds__(512) void ffn_product_kernel(Launch la) {
         const int all_slices = (a.K + BK - 1) / BK;
         kt0 = split * a.split_slices;
         nk = (kt0 + a.split_slices < all_slices ? a.split_slices : all_slices - kt0);
-        const int64_t w_first = kGated<EPI> ? static_cast<int64_t>(wave < 4 ? 0 : a.N) + n0 + (wave & 3) * 8 : n0;
-        const int64_t w_rows = kGated<EPI> ? 2 * static_cast<int64_t>(a.N) : a.N;
+        const RowRange w_rows = kGated<EPI> ? gated_rows(wave, a.N, n0) : RowRange{n0, a.N - n0};
         if constexpr (!XK) xsrd = make_rsrc(a.X + m0 * a.ldx, (a.M - m0) * a.ldx * 2);
-        if constexpr (!WK) wsrd = make_rsrc(a.W + w_first * a.ldw, (w_rows - w_first) * a.ldw * 2);
+        if constexpr (!WK) wsrd = make_rsrc(a.W + w_rows.first * a.ldw, w_rows.count * a.ldw * 2);
     };
     // descriptors of a slice of a K-major operand, from its first k on: the offsets inside stay small whatever K is
     const auto aim = [&](int kt) {

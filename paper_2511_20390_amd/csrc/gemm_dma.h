@@ -2,6 +2,7 @@
 // (gemm_pipe.hip).  Device code.
 #pragma once
 
+#include "buffer_range.h"
 #include "gemm_tile.h"
 
 namespace freemi {
@@ -35,8 +36,7 @@ __device__ __forceinline__ void wait_lds_barrier() {
 template <typename T>
 __device__ __forceinline__ u32x4_t make_rsrc(const T* base, int64_t bytes) {
     const uint64_t a = reinterpret_cast<uint64_t>(base);
-    return u32x4_t{static_cast<uint32_t>(a), static_cast<uint32_t>(a >> 32) & 0xffffu,
-                   static_cast<uint32_t>(bytes < 0x7fffffff ? bytes : 0x7fffffff), 0x00020000u};
+    return u32x4_t{static_cast<uint32_t>(a), static_cast<uint32_t>(a >> 32) & 0xffffu, range_bytes(bytes), 0x00020000u};
 }
 
 __device__ __forceinline__ uint32_t lds_address(const char* p) {

@@ -1,0 +1,65 @@
+"""What the operators of rotary, gated blocks read and keep at the ends of their tensors, at the largest sums and at the farthest
+positions."""
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+
+def _gen(*seed):
+    import torch
+    return torch.Generator(device="cuda").manual_seed(sum((i + 1) * s for i, s in enumerate(seed)) + 41)
+
+
+def _rnd(g, *shape, std=1.0, dtype=None):
+    import torch
+    v = torch.randn(*shape, generator=g, device="cuda") * std
+    return v if dtype is None else v.to(dtype)
+
+
+def _fenced(t, rows, fill):
+    """t as a view into a larger buffer, `rows` rows of `fill` behind it."""
+    import torch
+    room = torch.full((t.shape[0] + rows, t.shape[1]), fill, dtype=t.dtype, device=t.device)
+    room[:t.shape[0]] = t
+    return room[:t.shape[0]]
+
+
+def _kept(saved, M, F):
+    """g and u of the kept state [M, H] each, H = F rounded up to 64: blocks of 32 x 32, [M / 32][2 H / 32][4][lane][4], lane l's values being
+    row l % 32, columns 8 q + 4 (l / 32) + 0 .. 3 of a block."""
+    import torch
+    H, blocks_m = -(-F // 64) * 64, -(-M // 32)
+    n = blocks_m * 32 * 2 * H
+    v = saved[:4 * n].view(torch.float32).view(blocks_m, 2 * H // 32, 4, 2, 32, 4)          # mb, nb, q, lane / 32, lane % 32, c
+    v = v.permute(0, 4, 1, 2, 3, 5).reshape(blocks_m * 32, 2 * H)[:M]
+    return v[:, :H], v[:, H:]
+
+
+# hidden values of which the last tile has 8, 16, 24 or 40, and fewer in all than one tile; the three tiles, K whole; K in parts (33, 40 rows);
+# fp32, whose other widths go through padded copies
+@pytest.mark.parametrize("M,D,F,dtype", [(100, 8, 8, "bf16"), (100, 8, 16, "bf16"), (50, 72, 136, "bf16"), (50, 72, 144, "bf16"), (50, 72, 152, "bf16"),
+                                         (2100, 1144, 4616, "bf16"), (2100, 1144, 4624, "bf16"), (6000, 328, 1544, "bf16"), (6000, 328, 1552, "bf16"),
+                                         (9000, 264, 1032, "bf16"), (9000, 264, 1040, "bf16"), (9000, 256, 1064, "bf16"), (33, 2048, 1032, "bf16"),
+                                         (40, 1096, 4104, "bf16"), (70, 96, 136, "fp32"), (12, 72, 136, "bf16"), (3, 75, 133, "bf16"), (12, 64, 136, "fp32")])
+def test_ffn_reads_nothing_behind_its_operands(M, D, F, dtype):
+    """Memory behind every operand NaN or one: the same results to the bit, and what is kept past the hidden values zero."""
+    import torch
+    from paper_2511_20390_amd import binding as b
+    g = _gen(M, D, F)
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    x, w_in, w_out, dy = _rnd(g, M, D, dtype=dt), _rnd(g, 2 * F, D, std=D ** -0.5, dtype=dt), _rnd(g, D, F, std=F ** -0.5, dtype=dt), _rnd(g, M, D, dtype=dt)
+    results = []
+    for fill in (1.0, float("nan")):
+        fx, fi, fo, fy = (_fenced(t, 512, fill) for t in (x, w_in, w_out, dy))
+        saved = torch.full((b.gated_ffn_saved_bytes(M, D, F, dtype),), 255, dtype=torch.uint8, device="cuda")
+        plain = b.op_gated_ffn(fx, fi, fo)
+        out = b.op_gated_ffn(fx, fi, fo, saved=saved)
+        results.append((plain, out, *b.op_gated_ffn_backward(fy, fx, fi, fo, saved)))
+        kept = _kept(saved, M, F)
+        for t, w, name in zip(kept, (w_in[:F], w_in[F:]), "gu"):
+            assert not t[:, F:].any(), f"{name} past the hidden values"
+            ref = x.double() @ w.double().T
+            # a sum of D products, a rounding each; fp32 operands: cut into three parts, 2^-24 of a product more
+            assert ((t[:, :F] - ref).abs() <= (D + 16) * 2.0 ** -24 * (x.double().abs() @ w.double().abs().T)).all(), name
+    for a, e in zip(*results):
+        assert torch.isfinite(a).all() and torch.equal(a, e)
