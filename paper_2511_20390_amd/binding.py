@@ -743,6 +743,13 @@ def _mode_of(t, name):
     return mode
 
 
+def _int32(*sizes):
+    """Sizes the library takes as 32-bit integers; ctypes would cut a larger one to its low 32 bits, which may be a size as good as any."""
+    for n in sizes:
+        if n >> 31 not in (0, -1):
+            raise FreeError(FREE_ERR_LIMIT, f"sizes {sizes}: more than 31 bits")
+
+
 def _same_device(first, *others):
     """Index of the device the call runs on, whatever the current one is: that of its tensors, which have to agree."""
     index = first.get_device()
@@ -778,14 +785,19 @@ def _vectors(t, name, samples, D):
         raise FreeError(FREE_ERR_SHAPE, f"{name}: shape {tuple(t.shape)}, expected {(samples, D)}")
     if D > 1 and t.stride(-1) != 1:
         raise FreeError(FREE_ERR_SHAPE, f"{name}: values of a row are not next to each other")
-    return t.data_ptr(), D if samples == 1 else t.stride(0)
+    if samples == 1:
+        return t.data_ptr(), D
+    _int32(t.stride(0))
+    return t.data_ptr(), t.stride(0)
 
 
 def _norm_rows(x, rows_per_sample):
     if x.dim() != 2:
         raise FreeError(FREE_ERR_SHAPE, f"x: shape {tuple(x.shape)}, expected [rows, width]")
     M, D = x.shape
-    rows = max(M, 1) if rows_per_sample is None else int(rows_per_sample)
+    _int32(M, D)
+    # (more rows per sample than rows are one sample, whatever the number)
+    rows = max(M, 1) if rows_per_sample is None else min(int(rows_per_sample), max(M, 1))
     if rows < 1:
         raise FreeError(FREE_ERR_SHAPE, f"rows_per_sample: {rows}")
     return M, D, rows, max(1, -(-M // rows))
@@ -812,7 +824,8 @@ def op_layer_norm(x, weight=None, bias=None, mode: str = None, rows_per_sample: 
 
 
 def layer_norm_backward_workspace_bytes(M: int, D: int, rows_per_sample: int = None) -> int:
-    return load().free_layer_norm_backward_workspace_bytes(M, D, max(M, 1) if rows_per_sample is None else rows_per_sample)
+    _int32(M, D)
+    return load().free_layer_norm_backward_workspace_bytes(M, D, max(M, 1) if rows_per_sample is None else min(rows_per_sample, max(M, 1)))
 
 
 def op_layer_norm_backward(dout, x, weight=None, rows_per_sample: int = None, modulate: bool = False, eps: float = 1e-6,
@@ -855,6 +868,7 @@ def op_rope_axes(x, pos, heads: int, dh: int, axis_dims, theta: float = 10000.0,
     axes = len(axis_dims)
     if width != heads * dh or pos.shape[1] != axes:
         raise FreeError(FREE_ERR_SHAPE, f"x {tuple(x.shape)}, pos {tuple(pos.shape)}: expected {heads * dh} and {axes} columns")
+    _int32(rows, width, pos.shape[0], *axis_dims)                  # (heads and dh are factors of the width)
     if out is None:
         out = torch.empty(rows, width, dtype=x.dtype, device=x.device)
     if tuple(out.shape) != (rows, width) or out.dtype != x.dtype:
@@ -873,17 +887,20 @@ def op_rope_axes(x, pos, heads: int, dh: int, axis_dims, theta: float = 10000.0,
 
 def gated_ffn_saved_bytes(M: int, D: int, F: int, mode: str) -> int:
     """Bytes of what op_gated_ffn keeps for op_gated_ffn_backward."""
+    _int32(M, D, F)
     return load().free_gated_ffn_saved_bytes(M, D, F, MODES[mode])
 
 
 def gated_ffn_workspace_bytes(M: int, D: int, F: int, mode: str, backward: bool = False) -> int:
     """Workspace of op_gated_ffn; with backward, of either pass."""
+    _int32(M, D, F)
     return load().free_gated_ffn_workspace_bytes(M, D, F, MODES[mode], int(bool(backward)))
 
 
 def _ffn_sizes(x, w_in, w_out):
     if x.dim() != 2 or w_in.dim() != 2 or w_out.dim() != 2:
         raise FreeError(FREE_ERR_SHAPE, "x, w_in, w_out: two axes each")
+    _int32(x.shape[0], x.shape[1], w_out.shape[1])
     return x.shape[0], x.shape[1], w_out.shape[1], _mode_of(x, "x")
 
 
