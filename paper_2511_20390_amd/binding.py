@@ -868,7 +868,7 @@ def op_rope_axes(x, pos, heads: int, dh: int, axis_dims, theta: float = 10000.0,
     axes = len(axis_dims)
     if width != heads * dh or pos.shape[1] != axes:
         raise FreeError(FREE_ERR_SHAPE, f"x {tuple(x.shape)}, pos {tuple(pos.shape)}: expected {heads * dh} and {axes} columns")
-    _int32(rows, width, pos.shape[0], *axis_dims)                  # (heads and dh are factors of the width)
+    _int32(rows, heads, dh, pos.shape[0], *axis_dims)
     if out is None:
         out = torch.empty(rows, width, dtype=x.dtype, device=x.device)
     if tuple(out.shape) != (rows, width) or out.dtype != x.dtype:

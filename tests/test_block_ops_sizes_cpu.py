@@ -39,6 +39,14 @@ def test_arguments_of_more_bits():
         _refused(call)
 
 
+def test_rows_of_more_values():
+    """A row may have more than 2^32 values where heads and their widths are numbers of 32 bits (what fails next: it has no storage)."""
+    with pytest.raises(b.FreeError) as e:
+        b.op_rope_axes(_meta(1, 1 << 32), _meta(1, 1, dtype="int32"), 1 << 25, 128, [128])
+    assert e.value.status == b.FREE_ERR_NULL
+    _refused(lambda: b.op_rope_axes(_meta(1, FAR + 60), _meta(1, 1, dtype="int32"), 1, FAR + 60, [64]))
+
+
 def test_strides_of_more_bits():
     """Vectors of a sample four billion values behind those of the one before."""
     import types
