@@ -544,7 +544,8 @@ int32_t free_op_layer_norm_backward(const void* dout, int32_t dtype, const void*
  * FREE_ROPE_PAIRS: the section's values 2 i and 2 i + 1 are a pair; FREE_ROPE_HALVES: i and i + axis_dims[a] / 2.
  * x: `rows` token rows of `heads` heads next to each other, x_stride values from row to row (the q | k part of packed q | k | v rows is
  * 2 heads with the stride of the whole row); out likewise, and it may be x with the same stride.  pos [pos_rows, axes] int32, token row m
- * at m % pos_rows (one grid for all states of a batch); any int32 is a position, and its angle is exact to 2^-30 turns.
+ * at m % pos_rows (one grid for all states of a batch); any int32 is a position, and the angle whose sine and cosine are taken is off by
+ * less than 2^-25 turns (1.9e-7 rad), however far the position.
  * dh even and <= 256, 1 to 4 axes, theta >= 1.  At most 2^24 workgroups of 256 threads, a thread having up to four heads of one to four
  * pairs, and 2^30 threads for one row (FREE_ERR_LIMIT). */
 #define FREE_ROPE_PAIRS  0

@@ -4,8 +4,10 @@
 // the inverse (the gradient's way back) by the opposite angle; the rest is copied.
 //
 // Angles are kept in turns, as 64-bit fixed point: the frequency is F = round(2^64 theta^(-2 i / d) / 2 pi), at most 2^64 / 2 pi, and
-// pos F modulo 2^64 is the angle modulo one turn, exactly but for the rounding of F - positions up to 2^31 are off by less than 2^-30
-// turns, where an fp32 product of position and frequency is off by a turn from 2^24 on.  Of it the leading 32 bits go to sincospi.
+// pos F modulo 2^64 is the angle modulo one turn, exactly but for F's own error, the rounding's and that of the product of factors it comes
+// from (against 60 digits, theta from 1 to 1e9 and up to 256 values: 8 units at most).  So positions up to 2^31 are off by less than 2^-29
+// turns, where an fp32 product of position and frequency is off by a turn from 2^24 on.  Of it the leading 32 bits go to sincospi, rounded
+// to an fp32 number: up to 2^-26 turns, as for any fp32 angle of up to half a turn.
 //
 // Bound by HBM (every value read and written once).  A thread holds V pairs of a token and computes their sines and cosines once for
 // up to kHeads heads, whose loads are all in flight before the first is turned.  32760 tokens of 48 heads of 128 in bf16: 154 us, 5.2 TB/s

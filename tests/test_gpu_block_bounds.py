@@ -63,3 +63,32 @@ def test_ffn_reads_nothing_behind_its_operands(M, D, F, dtype):
             assert ((t[:, :F] - ref).abs() <= (D + 16) * 2.0 ** -24 * (x.double().abs() @ w.double().abs().T)).all(), name
     for a, e in zip(*results):
         assert torch.isfinite(a).all() and torch.equal(a, e)
+
+
+@pytest.mark.parametrize("theta,d", [(1.0, 8), (1.5, 256), (2.0, 64), (100.0, 36), (1e4, 128), (5e5, 64), (1e9, 20)])
+@pytest.mark.parametrize("inverse", [False, True])
+def test_rope_angles(theta, d, inverse):
+    """The pair (1, 0) becomes (cos, sin) of its angle, here against angles of 60 digits: off by less than 2^-25 turns at any position, where
+    64-bit products of position and frequency would be off by more themselves."""
+    import math
+    from decimal import Decimal, getcontext
+
+    import torch
+    from paper_2511_20390_amd import binding as b
+    getcontext().prec = 60
+    turn = 2 * Decimal("3.14159265358979323846264338327950288419716939937510582097494459")
+    g = _gen(int(theta), d)
+    pos = [0, 1, -1, 5000, 2**24 + 1, -2**30 - 7, 2**31 - 1, -2**31] + torch.randint(-2**31, 2**31 - 1, (40,), generator=g, device="cuda").tolist()
+    want = torch.empty(len(pos), d, dtype=torch.float64)
+    for i in range(d // 2):
+        f = Decimal(theta) ** (Decimal(-2 * i) / Decimal(d)) / turn
+        for m, p in enumerate(pos):
+            t = p * f
+            a = float(t - t.to_integral_value()) * 2 * math.pi * (-1 if inverse else 1)
+            want[m, 2 * i], want[m, 2 * i + 1] = math.cos(a), math.sin(a)
+    x = torch.zeros(len(pos), d, device="cuda")
+    x[:, 0::2] = 1.0
+    got = b.op_rope_axes(x, torch.tensor(pos, dtype=torch.int32, device="cuda")[:, None].contiguous(), 1, d, [d], theta=theta, inverse=inverse)
+    # the angle, and sine and cosine themselves: two steps of fp32 at one
+    bound = 2 * math.pi * 2.0 ** -25 + 2 * 2.0 ** -23
+    assert (got.double().cpu() - want).abs().max().item() <= bound
