@@ -557,9 +557,9 @@ int32_t free_op_rope_axes(const void* x, int64_t x_stride, const int32_t* pos, i
 /* Gated feed-forward block of M token rows of width D with F hidden values, all tensors of type dtype, contiguous and 16-byte aligned:
  *   [g | u] = x w_in^T,  h = act(g) u,  out = h w_out^T;   w_in [2 F, D] (gate rows, then up rows), w_out [D, F]
  * act: FREE_ACT_SILU or FREE_ACT_GELU (tanh form).  Sums, g and u are fp32, h is rounded to dtype.  Any widths up to 2^20; those that are
- * not multiples of 64 go through padded copies in the workspace where there are more than 32 rows.  M F, M D and 2 F D: at most 2^35 (bf16) or 2^33 (fp32)
- * (FREE_ERR_LIMIT).  How sums are cut depends on M, D, F and on whether state is kept, so results of calls that differ in these may differ
- * in their last bits.
+ * not multiples of 8 (bf16) or 64 (fp32) go through padded copies in the workspace, but for forward calls of at most 32 rows that keep
+ * nothing.  M F, M D and 2 F D: at most 2^35 (bf16) or 2^33 (fp32) (FREE_ERR_LIMIT).  How sums are cut depends on M, D, F and on whether
+ * state is kept, so results of calls that differ in these may differ in their last bits.
  * saved (NULL: none): free_gated_ffn_saved_bytes bytes that the gradient's pass reads, of a layout of the library's own; they belong to
  * these sizes and this x.
  * The gradient: dx [M, D] and dw_in, dw_out of the weights' shapes, written, not added to; g's and u's gradients are rounded to dtype.

@@ -64,3 +64,16 @@ def test_any_number_of_rows_per_sample(rows):
     assert b.layer_norm_backward_workspace_bytes(8, 64, rows) == b.layer_norm_backward_workspace_bytes(8, 64)
     assert b._norm_rows(_meta(0, 64), rows) == (0, 64, 1, 1)
     assert b._norm_rows(_meta(8, 64), 3) == (8, 64, 3, 3)
+
+
+@pytest.mark.parametrize("mode,step,size", [("bf16", 8, 2), ("fp32", 64, 4)])
+def test_which_widths_are_copied(mode, step, size):
+    """Room for padded copies of the weights is asked for where a width is no multiple of 8 (bf16) or 64 (fp32), and nowhere else."""
+    for D, F in ((1152, 2688), (1152, 2688 + step), (1152 + step, 2688), (1152 + step, 2688 + 3 * step)):
+        copies = 3 * D * F * size
+        for backward in (False, True):
+            room = lambda *widths: b.gated_ffn_workspace_bytes(40, *widths, mode, backward)
+            least = 40 * F * size * (2 if backward else 1)                   # h, or its two gradients
+            assert room(D, F) < least + copies
+            for widths in ((D, F + step // 2), (D + 1, F), (D + step // 2, F - 1)):
+                assert room(*widths) > least + copies * (1.9 if backward else 0.99)
