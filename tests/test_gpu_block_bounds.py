@@ -92,3 +92,43 @@ def test_rope_angles(theta, d, inverse):
     # the angle, and sine and cosine themselves: two steps of fp32 at one
     bound = 2 * math.pi * 2.0 ** -25 + 2 * 2.0 ** -23
     assert (got.double().cpu() - want).abs().max().item() <= bound
+
+
+@pytest.mark.parametrize("M,D,x_dtype,out_dtype", [(3_000_001, 24, "bfloat16", "bfloat16"), (4_000_003, 3, "float32", "float32"),
+                                                   (1_500_000, 130, "bfloat16", "bfloat16"), (250_001, 1152, "float32", "bfloat16")])
+def test_norm_long_column_sums(M, D, x_dtype, out_dtype):
+    """The weight's gradient over millions of rows, all of them in it, and with a mean, so that the sums grow."""
+    import torch
+    from paper_2511_20390_amd import binding as b
+    from tests import block_ops_util as u
+    g = _gen(M, D)
+    x = (_rnd(g, M, D) + 0.3).to(getattr(torch, x_dtype))
+    dy = (_rnd(g, M, D) * 0.5 + 0.5 + 0.25 * x.float().sign()).to(getattr(torch, out_dtype))
+    w = _rnd(g, D)
+    dx, dw, db = b.op_layer_norm_backward(dy, x, w)
+    # the definition in plain sums (the general reference adds every row to its sample's with atomics: minutes for so many)
+    x, dy, w = x.double(), dy.double(), w.double()
+    xc = x - x.mean(1, keepdim=True)
+    r = 1.0 / torch.sqrt((xc * xc).mean(1, keepdim=True) + 1e-6)
+    xh = xc * r
+    gw = dy * w
+    ref_dx = r * (gw - gw.mean(1, keepdim=True) - xh * (gw * xh).mean(1, keepdim=True))
+    ref_dw, ref_db, size_w, size_b = (dy * xh).sum(0), dy.sum(0), (dy * xh).abs().sum(0), dy.abs().sum(0)
+    # of a row: 64 roundings in a chain at most, in its mean, its deviation and the two means of the gradient
+    e_xh = 64 * u.U * ((x.abs().mean(1, keepdim=True) + x.abs()) * r + xh.abs())
+    e_dx = r * (64 * u.U * 2 * (gw.abs() + gw.abs().mean(1, keepdim=True) + xh.abs() * (gw * xh).abs().mean(1, keepdim=True)) +
+                xh.abs() * (gw.abs() * e_xh).mean(1, keepdim=True) + e_xh * (gw * xh).mean(1, keepdim=True).abs())
+    u.check(dx, (ref_dx, e_dx), "dx")
+    # The chain of additions of a column: the rows of a group (a workgroup has 16 of 16 lanes, or four wavefronts, two where 8-value pieces
+    # leave no more: 2 at least), the groups of a workgroup, the partial rows of a thread of the second launch, four of these, sixteen.
+    # Workgroups: by the workspace, a partial row of 2 D values each.
+    chunks = (b.layer_norm_backward_workspace_bytes(M, D) - 256) // (8 * D)
+    groups = 16 if D <= 256 else 2
+    chain = -(-M // (chunks * groups)) + 16 + -(-chunks // 64) + 4 + 16
+    u.check(dw[0], (ref_dw, chain * u.U * size_w + (dy.abs() * e_xh).sum(0)), "dweight")
+    u.check(db[0], (ref_db, chain * u.U * size_b), "dbias")
+    # Roundings of both signs: a partial sum is off by U / sqrt(3) of itself at every addition, n of them that grow evenly to a column's sum
+    # S add to U S sqrt(n) / 3; those of the groups and columns are independent.  xh's own errors average out over the rows likewise.  All
+    # columns together stay below eight times that.
+    for got, ref, size in ((dw[0], ref_dw, size_w), (db[0], ref_db, size_b)):
+        assert (got.double() - ref).norm() <= 8 * u.U * (1 + chain ** 0.5 / 3) * size.norm()
