@@ -19,7 +19,7 @@ int main() {
                     const RowRange r = gated_rows(wave, N, n0);
                     const int begin = wave < 4 ? 0 : N, end = begin + N;
                     if (r.count < 0 || r.first < begin || r.first + r.count > end) {
-                        std::printf("N %d n0 %d wave %d: rows %lld + %lld of %d .. %d\n", N, n0, wave, (long long)r.first, (long long)r.count, begin, end);
+                        std::printf("N %d n0 %d wave %d: rows %d + %d of %d .. %d\n", N, n0, wave, r.first, r.count, begin, end);
                         return 3;
                     }
                     for (int j = 0; j < cols / 32; ++j)
