@@ -795,7 +795,8 @@ def _norm_rows(x, rows_per_sample):
     if x.dim() != 2:
         raise FreeError(FREE_ERR_SHAPE, f"x: shape {tuple(x.shape)}, expected [rows, width]")
     M, D = x.shape
-    _int32(M, D)
+    if (M | D) >> 31:
+        _int32(M, D)
     # (more rows per sample than rows are one sample, whatever the number)
     rows = max(M, 1) if rows_per_sample is None else min(int(rows_per_sample), max(M, 1))
     if rows < 1:
@@ -869,11 +870,14 @@ def op_rope_axes(x, pos, heads: int, dh: int, axis_dims, theta: float = 10000.0,
     if width != heads * dh or pos.shape[1] != axes:
         raise FreeError(FREE_ERR_SHAPE, f"x {tuple(x.shape)}, pos {tuple(pos.shape)}: expected {heads * dh} and {axes} columns")
     _int32(rows, heads, dh, pos.shape[0], *axis_dims)
+    strided = ((x, "x"),)
     if out is None:
         out = torch.empty(rows, width, dtype=x.dtype, device=x.device)
-    if tuple(out.shape) != (rows, width) or out.dtype != x.dtype:
+    elif tuple(out.shape) != (rows, width) or out.dtype != x.dtype:
         raise FreeError(FREE_ERR_SHAPE if out.dtype == x.dtype else FREE_ERR_DTYPE, f"out: {out.dtype} {tuple(out.shape)}, expected x's")
-    for t, name in ((x, "x"), (out, "out")):
+    else:
+        strided = ((x, "x"), (out, "out"))
+    for t, name in strided:
         if not t.is_cuda:
             raise FreeError(FREE_ERR_NULL, f"{name}: not a device tensor")
         if width > 1 and t.stride(1) != 1:
@@ -900,8 +904,10 @@ def gated_ffn_workspace_bytes(M: int, D: int, F: int, mode: str, backward: bool 
 def _ffn_sizes(x, w_in, w_out):
     if x.dim() != 2 or w_in.dim() != 2 or w_out.dim() != 2:
         raise FreeError(FREE_ERR_SHAPE, "x, w_in, w_out: two axes each")
-    _int32(x.shape[0], x.shape[1], w_out.shape[1])
-    return x.shape[0], x.shape[1], w_out.shape[1], _mode_of(x, "x")
+    (M, D), F = x.shape, w_out.shape[1]
+    if (M | D | F) >> 31:
+        _int32(M, D, F)
+    return M, D, F, _mode_of(x, "x")
 
 
 def op_gated_ffn(x, w_in, w_out, act: str = "silu", saved=None, out=None, workspace=None):
