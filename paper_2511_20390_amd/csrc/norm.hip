@@ -508,8 +508,8 @@ int32_t backward_of(const NormArgs& a, const NormGrad& gr, int samples, hipStrea
 // rounds (two on every compute unit, of eight wavefronts one), since each ends with sums over its wavefronts and a partial row of the weight's
 // gradient that the second launch reads: together some three passes.  Groups and workgroups are counted as the layout of 4-value pieces has
 // them, whatever the types: the size of the workspace, which is asked for without them, holds for all.  bf16 rows in 8-value pieces may
-// have twice or half as many groups (1152 values two for four, 4097 to 5120 in workgroups of four wavefronts for eight); the rows are walked with
-// the stride of the layout that is launched, so this moves the balance only.
+// have half as many groups (1025 to 1280 values two for four, 2049 to 2560 one for two) or workgroups of eight wavefronts for four (4097 to 5120);
+// the rows are walked with the stride of the layout that is launched, so this moves the balance only.
 int chunks_of(int32_t M, int32_t D, int32_t rows_per_sample) {
     const int64_t samples = (static_cast<int64_t>(M) + rows_per_sample - 1) / rows_per_sample;
     const int lanes = backward_layout(4, D).lanes, groups = back_threads(lanes) / lanes;
