@@ -575,6 +575,40 @@ int32_t free_op_gated_ffn_backward(const void* dout, const void* x, const void* 
                                    size_t saved_bytes, int32_t M, int32_t D, int32_t F, int32_t dtype, int32_t act, void* dx, void* dw_in,
                                    void* dw_out, void* workspace, size_t ws_bytes, void* stream);
 
+/* ---- operators of blocks that are conditioned on an encoder's states and carry adapters ------------------------------------
+ * Targets and drafters that follow a text or a picture read an encoder's states in every block, and what a request has of its own beside
+ * the shared weights are low-rank adapters of the linear layers.  These calls stand beside free_op_attention and free_op_linear: query
+ * layer, cross attention, output layer, each layer with its adapters.  What is said above of streams, graphs, workspaces, equal bits, empty
+ * problems, overlaps and of infinite or NaN values holds here too.
+ *
+ * Cross attention: B samples, each of Nq query rows and Nk key / value rows,
+ *   out = softmax over the keys that count (scale q k^T) v     per sample and head
+ * q, out: B Nq rows of `heads` heads of dh values next to each other, sample after sample; k, v: B Nk rows of kv_heads heads; heads is a
+ * multiple of kv_heads, and query head h reads key head h / (heads / kv_heads).  Every tensor has a distance of its own from row to row
+ * (*_stride, in values; k and v may be the halves of packed rows), and no alignment is asked of it; rows that are 16-byte aligned, with dh a
+ * multiple of 16 bytes, are read faster.  Samples that share an encoder's states (the states of a pack) are one sample of more queries.
+ * key_len (NULL: Nk): int32 [B], the keys of a sample that count, values outside 0 .. Nk taken as the nearest; key_mask (NULL: all):
+ * [B, Nk] bytes, zero for a key that does not count.  What stands in keys that do not count, NaN included, has no influence.  A sample
+ * without keys has out zero.
+ * lse (NULL: not wanted): fp32 [B, heads, Nq], the logarithm of the sum of exp(scale q k^T), -inf without keys; the gradient reads it.
+ * Scores, probabilities' sums and results are summed in fp32; probabilities are rounded to dtype as operands of the second product.
+ * The gradient, of the same inputs, out and lse: dq like q, dk and dv like k and v (each with its distance from row to row), written, not
+ * added to, zero for keys that do not count; probabilities and the scores' gradient are rounded to dtype as operands of the products.
+ * How sums are cut depends on the sizes alone.  1 <= dh <= 128, strides up to 2^22 values, Nq heads / kv_heads below 2^31 - 128,
+ * B kv_heads below 2^24, at most 2^31 - 1 workgroups of 32 query or key rows of a (sample, key head) (FREE_ERR_LIMIT). */
+size_t free_cross_attention_workspace_bytes(int32_t B, int32_t Nq, int32_t Nk, int32_t heads, int32_t kv_heads, int32_t dh, int32_t dtype,
+                                            int32_t backward);
+int32_t free_op_cross_attention(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                                const int32_t* key_len, const uint8_t* key_mask, int32_t B, int32_t Nq, int32_t Nk, int32_t heads,
+                                int32_t kv_heads, int32_t dh, float scale, int32_t dtype, void* out, int64_t out_stride, float* lse,
+                                void* workspace, size_t ws_bytes, void* stream);
+int32_t free_op_cross_attention_backward(const void* dout, int64_t dout_stride, const void* q, int64_t q_stride, const void* k,
+                                         int64_t k_stride, const void* v, int64_t v_stride, const void* out, int64_t out_stride,
+                                         const float* lse, const int32_t* key_len, const uint8_t* key_mask, int32_t B, int32_t Nq,
+                                         int32_t Nk, int32_t heads, int32_t kv_heads, int32_t dh, float scale, int32_t dtype, void* dq,
+                                         int64_t dq_stride, void* dk, int64_t dk_stride, void* dv, int64_t dv_stride, void* workspace,
+                                         size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -40,6 +40,7 @@ EXPORTED_SYMBOLS = [
     "free_profile_begin", "free_profile_end", "free_profile_category_name", "free_mfma_ceiling", "free_validate_inputs",
     "free_op_layer_norm", "free_layer_norm_backward_workspace_bytes", "free_op_layer_norm_backward", "free_op_rope_axes",
     "free_gated_ffn_saved_bytes", "free_gated_ffn_workspace_bytes", "free_op_gated_ffn", "free_op_gated_ffn_backward",
+    "free_cross_attention_workspace_bytes", "free_op_cross_attention", "free_op_cross_attention_backward",
 ]
 PROF_NCAT = 12
 
@@ -176,6 +177,12 @@ def load():
     lib.free_op_gated_ffn.argtypes = [vp, vp, vp, i32, i32, i32, i32, i32, vp, vp, sz, vp, sz, vp]
     lib.free_op_gated_ffn_backward.restype = i32
     lib.free_op_gated_ffn_backward.argtypes = [vp] * 5 + [sz] + [i32] * 5 + [vp, vp, vp, vp, sz, vp]
+    lib.free_cross_attention_workspace_bytes.restype = sz
+    lib.free_cross_attention_workspace_bytes.argtypes = [i32] * 8
+    lib.free_op_cross_attention.restype = i32
+    lib.free_op_cross_attention.argtypes = [vp, i64] * 3 + [vp, vp] + [i32] * 6 + [f32, i32, vp, i64, vp, vp, sz, vp]
+    lib.free_op_cross_attention_backward.restype = i32
+    lib.free_op_cross_attention_backward.argtypes = [vp, i64] * 5 + [vp] * 3 + [i32] * 6 + [f32, i32] + [vp, i64] * 3 + [vp, sz, vp]
     _lib = lib
     return lib
 
@@ -945,3 +952,91 @@ def op_gated_ffn_backward(dout, x, w_in, w_out, saved, act: str = "silu", out=No
              _addr(dw_in, x.dtype, "dw_in", (2 * F, D)), _addr(dw_out, x.dtype, "dw_out", (D, F)), _addr(workspace, u8, "workspace"),
              workspace.numel())
     return out
+
+
+# ---- operators of blocks that are conditioned on an encoder's states and carry adapters -----------------------------
+def cross_attention_workspace_bytes(B: int, Nq: int, Nk: int, heads: int, kv_heads: int, dh: int, mode: str, backward: bool = False) -> int:
+    """Workspace of op_cross_attention; with backward, of either pass."""
+    _int32(B, Nq, Nk, heads, kv_heads, dh)
+    return load().free_cross_attention_workspace_bytes(B, Nq, Nk, heads, kv_heads, dh, MODES[mode], int(bool(backward)))
+
+
+def _rows(t, name, rows, width, dtype):
+    """Address and row distance of [rows, width], values of a row next to each other, rows any distance apart."""
+    if not t.is_cuda:
+        raise FreeError(FREE_ERR_NULL, f"{name}: not a device tensor")
+    if t.dtype != dtype:
+        raise FreeError(FREE_ERR_DTYPE, f"{name}: element type {t.dtype}, expected {dtype}")
+    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != width:
+        raise FreeError(FREE_ERR_SHAPE, f"{name}: shape {tuple(t.shape)}, expected {(rows, width)}")
+    step, inner = t.stride()
+    if width > 1 and inner != 1:
+        raise FreeError(FREE_ERR_SHAPE, f"{name}: values of a row are not next to each other")
+    return t.data_ptr(), step
+
+
+def _cross_sizes(q, k, B, heads, kv_heads, dh, scale):
+    if q.dim() != 2 or k.dim() != 2 or B < 1 or q.shape[0] % B or k.shape[0] % B:
+        raise FreeError(FREE_ERR_SHAPE, f"q, k: shapes {tuple(q.shape)}, {tuple(k.shape)}, expected rows of {B} samples")
+    Nq, Nk = q.shape[0] // B, k.shape[0] // B
+    kv_heads = heads if kv_heads is None else kv_heads
+    if (B | Nq | Nk | heads | kv_heads | dh) >> 31:
+        _int32(B, Nq, Nk, heads, kv_heads, dh)
+    if dh < 1:
+        raise FreeError(FREE_ERR_SHAPE, f"dh: {dh}")
+    return Nq, Nk, kv_heads, float(dh) ** -0.5 if scale is None else float(scale)
+
+
+def _keys(key_len, key_mask, B, Nk):
+    """Addresses of the lengths [B] int32 and of the mask [B, Nk], uint8 or bool."""
+    import torch
+    n = _addr(key_len, torch.int32, "key_len", (B,), optional=True)
+    if key_mask is None:
+        return n, None
+    return n, _addr(key_mask, torch.bool if key_mask.dtype == torch.bool else torch.uint8, "key_mask", (B, Nk))
+
+
+def op_cross_attention(q, k, v, B: int, heads: int, dh: int, kv_heads: int = None, key_len=None, key_mask=None, scale: float = None, lse=None,
+                       out=None, workspace=None):
+    """Attention of q [B * Nq, heads * dh] to k, v [B * Nk, kv_heads * dh] (float32 or bfloat16; rows any distance apart).  key_len [B] int32
+    and key_mask [B, Nk] say which keys of a sample count; without any its rows are zero.  scale: 1 / sqrt(dh) by default.  lse: a float32
+    [B, heads, Nq] tensor to write the logarithms of the sums to, which op_cross_attention_backward reads."""
+    import torch
+    Nq, Nk, kv_heads, scale = _cross_sizes(q, k, B, heads, kv_heads, dh, scale)
+    mode, dt, width, kv = _mode_of(q, "q"), q.dtype, heads * dh, kv_heads * dh
+    qa, ka, va = _rows(q, "q", B * Nq, width, dt), _rows(k, "k", B * Nk, kv, dt), _rows(v, "v", B * Nk, kv, dt)
+    keys = _keys(key_len, key_mask, B, Nk)
+    lse_at = _addr(lse, torch.float32, "lse", (B, heads, Nq), optional=True)
+    if out is None:
+        out = torch.empty(B * Nq, width, dtype=dt, device=q.device)
+    if workspace is None:
+        workspace = torch.empty(load().free_cross_attention_workspace_bytes(B, Nq, Nk, heads, kv_heads, dh, mode, 0), dtype=torch.uint8, device=q.device)
+    dev = _same_device(q, k, v, key_len, key_mask, lse, out, workspace)
+    _enqueue(load().free_op_cross_attention, "free_op_cross_attention", dev, *qa, *ka, *va, *keys, B, Nq, Nk, heads, kv_heads, dh, scale, mode,
+             *_rows(out, "out", B * Nq, width, dt), lse_at, _addr(workspace, torch.uint8, "workspace"), workspace.numel())
+    return out
+
+
+def op_cross_attention_backward(dout, q, k, v, out, lse, B: int, heads: int, dh: int, kv_heads: int = None, key_len=None, key_mask=None,
+                                scale: float = None, grads=None, workspace=None):
+    """Gradient of op_cross_attention, of whose result and lse `out` and `lse` are: (dq, dk, dv).  grads: the three to write to, rows any
+    distance apart."""
+    import torch
+    Nq, Nk, kv_heads, scale = _cross_sizes(q, k, B, heads, kv_heads, dh, scale)
+    mode, dt, width, kv = _mode_of(q, "q"), q.dtype, heads * dh, kv_heads * dh
+    if grads is None:
+        new = lambda rows, n: torch.empty(rows, n, dtype=dt, device=q.device)
+        grads = (new(B * Nq, width), new(B * Nk, kv), new(B * Nk, kv))
+    dq, dk, dv = grads
+    wide = [x for t, name in ((dout, "dout"), (q, "q")) for x in _rows(t, name, B * Nq, width, dt)]
+    wide += [x for t, name in ((k, "k"), (v, "v")) for x in _rows(t, name, B * Nk, kv, dt)]
+    wide += _rows(out, "out", B * Nq, width, dt)
+    keys = _keys(key_len, key_mask, B, Nk)
+    lse_at = _addr(lse, torch.float32, "lse", (B, heads, Nq))
+    written = [*_rows(dq, "dq", B * Nq, width, dt), *_rows(dk, "dk", B * Nk, kv, dt), *_rows(dv, "dv", B * Nk, kv, dt)]
+    if workspace is None:
+        workspace = torch.empty(load().free_cross_attention_workspace_bytes(B, Nq, Nk, heads, kv_heads, dh, mode, 1), dtype=torch.uint8, device=q.device)
+    dev = _same_device(q, dout, k, v, out, lse, key_len, key_mask, dq, dk, dv, workspace)
+    _enqueue(load().free_op_cross_attention_backward, "free_op_cross_attention_backward", dev, *wide, lse_at, *keys, B, Nq, Nk, heads, kv_heads, dh,
+             scale, mode, *written, _addr(workspace, torch.uint8, "workspace"), workspace.numel())
+    return grads

@@ -1,0 +1,555 @@
+// Cross attention to an encoder's states of another length: per sample and head
+//   out = softmax(scale q k^T over the keys that count) v,   lse = log sum exp(scale q k^T)
+// with a length and a mask per sample over its keys, heads in groups that share keys and values, rows any distance apart; bf16 and fp32.
+// One pass over the keys with a running maximum and sum in fp32 (cross_attn.h has the layout of the products).  Keys that do not count are
+// not only given no weight: their scores are replaced and their values read as zero, so that nothing they hold, NaN included, gets through.  A
+// sample without keys: out zero, lse -inf.
+//
+// The queries of a group of heads are rows of one problem (row r: token r / group, head r % group), so that keys and values are read once for
+// all of them.  Two kernels:
+//  * many rows: a workgroup has 128 or 64 of them and passes tiles of keys through LDS in two stages;
+//  * up to 32 rows (a single query, a few learned ones): bound by reading keys and values once.  Every wavefront streams key tiles of its own,
+//    K straight into the matrix instructions, V through a private piece of LDS; partial results (maximum, sum, out) are joined in order.
+// Where rows alone leave compute units idle the keys are cut in parts, each a workgroup's, and a second launch joins them.
+#include <algorithm>
+#include <cmath>
+#include <type_traits>
+
+#include "cross_attn.h"
+
+namespace freemi {
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kFewRows = 32;
+constexpr float kLazy = 8.0f;                     // log2 by which a maximum may grow before the sums are rescaled
+constexpr float kNoScore = -3.402823466e38f;      // a part's maximum where it has keys and all their scores are -inf
+
+// What a launch does: parts of the keys, tiles of a part; partial results [part][pair][row]
+struct Parts {
+    int32_t parts, tiles;
+    float *o, *ml;                                // [..][dh] sums, [..][2] maximum (of the scaled scores, log2) and sum
+};
+
+template <typename T>
+constexpr int kTileKeys = sizeof(T) == 2 ? 64 : 32;
+
+__device__ __forceinline__ int attended(const CrossArgs& a, int b) {
+    if (!a.key_len) return a.Nk;
+    const int n = a.key_len[b];
+    return n < 0 ? 0 : n < a.Nk ? n : a.Nk;
+}
+
+// The end of a row: out and lse, or a part's sums.  m: the maximum that l and o are relative to (log2 of the scaled scores).
+template <typename T, bool kVec, int DT>
+__device__ __forceinline__ void write_row(const CrossArgs& a, const Parts& pt, int part, int64_t pair, int b, int kvh, int64_t r, int g, float m, float l,
+                                          bool any, const xf32x16_t (&o)[DT]) {
+    const int group = a.heads / a.kv_heads;
+    const int64_t rows = static_cast<int64_t>(a.Nq) * group;
+    if (pt.parts > 1) {
+        const int64_t at = (part * static_cast<int64_t>(a.B) * a.kv_heads + pair) * rows + r;
+        float* dst = pt.o + at * a.dh;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+            for (int e4 = 0; e4 < 4; ++e4)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int d = 32 * dt + 8 * e4 + 4 * g + i;
+                    if (d < a.dh) dst[d] = o[dt][4 * e4 + i];
+                }
+        if (g == 0) {
+            pt.ml[2 * at] = any && m == -INFINITY ? kNoScore : m;
+            pt.ml[2 * at + 1] = l;
+        }
+        return;
+    }
+    const int64_t token = r / group;
+    const int head = kvh * group + static_cast<int>(r - token * group);
+    const float inv = any ? 1.0f / l : 0.f;
+    T* dst = static_cast<T*>(a.out) + (static_cast<int64_t>(b) * a.Nq + token) * a.out_stride + static_cast<int64_t>(head) * a.dh;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int e4 = 0; e4 < 4; ++e4)
+            store4<T, kVec>(dst, 32 * dt + 8 * e4 + 4 * g, a.dh, o[dt][4 * e4] * inv, o[dt][4 * e4 + 1] * inv, o[dt][4 * e4 + 2] * inv,
+                            o[dt][4 * e4 + 3] * inv);
+    if (a.lse && g == 0) a.lse[(static_cast<int64_t>(b) * a.heads + head) * a.Nq + token] = any ? (m + __builtin_log2f(l)) * kLn2 : -INFINITY;
+}
+
+// One online-softmax step of a query column: scores in st (KB blocks of 16 registers, those that do not count at -inf) -> probabilities in
+// place; m, l and o follow.
+template <int KB, int DT>
+__device__ __forceinline__ void softmax_step(xf32x16_t (&st)[KB], float scale_log2, float& m_ref, float& l, xf32x16_t (&o)[DT]) {
+    float mx = st[0][0];
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) mx = fmaxf(mx, st[kb][e]);
+    mx = max_lane_xor32(mx);
+    // the reference follows the maximum lazily: sums are rescaled once it has grown by a factor of 2^kLazy (true for the first scores)
+    if (__builtin_expect(__any((mx - m_ref) * scale_log2 > kLazy), 0)) {
+        const float m_new = fmaxf(m_ref, mx);
+        const float alpha = m_new == m_ref ? 1.0f : __builtin_amdgcn_exp2f((m_ref - m_new) * scale_log2);
+        l *= alpha;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) o[dt][e] *= alpha;
+        m_ref = m_new;
+    }
+    const float mb = m_ref == -INFINITY ? 0.f : m_ref * scale_log2;       // (no score yet: probabilities of zero, not NaN)
+    float sum = 0.f;
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            st[kb][e] = __builtin_amdgcn_exp2f(fmaf(st[kb][e], scale_log2, -mb));
+            sum += st[kb][e];
+        }
+    l += sum;
+}
+
+// o += V^T P^T for one 32-key block: v at the block's first key, rows VROW bytes apart
+template <typename T, int DT, int VROW>
+__device__ __forceinline__ void add_values(const char* v, int lane, const xf32x16_t& p, xf32x16_t (&o)[DT]) {
+    const int l32 = lane & 31, g = lane >> 5;
+    if constexpr (sizeof(T) == 2) {
+        const char* at = v + (8 * g + ((lane & 15) >> 2)) * VROW + (16 * ((lane >> 4) & 1) + 4 * (lane & 3)) * 2;
+#pragma unroll
+        for (int hh = 0; hh < 2; ++hh) {
+            const xu32x4_t pk = pack8({p[8 * hh], p[8 * hh + 1], p[8 * hh + 2], p[8 * hh + 3], p[8 * hh + 4], p[8 * hh + 5], p[8 * hh + 6], p[8 * hh + 7]});
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt)
+                chunk_product<T>(transposed_chunk(at + hh * 16 * VROW + dt * 64, at + (hh * 16 + 4) * VROW + dt * 64), pk, o[dt]);
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) {
+                const float x = *reinterpret_cast<const float*>(v + register_row<T>(e, g) * VROW + (32 * dt + l32) * 4);
+                o[dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, p[e], o[dt], 0, 0, 0);
+            }
+    }
+}
+
+// bytes from a key's row of K to the next in LDS: an odd number of chunks (reads of 16 bytes from 16 rows on different banks)
+template <typename T, int DP>
+constexpr int kKeyRow = (HeadShape<T, DP>::CH | 1) * 16;
+// ... of V: bf16, 4 rows x 64 bytes of a transposing read on different banks; fp32, rows four apart on the other 32 banks
+template <typename T, int DP>
+constexpr int kValueRow = sizeof(T) == 4 ? (DP + 8) * 4 : DP <= 32 ? 64 : DP <= 96 ? 192 : 320;
+
+// KS wavefronts share the keys of a block of 32 queries
+template <typename T, int DP, int KS, bool kVec>
+__global__ __launch_bounds__(kThreads, (sizeof(T) == 2 && DP <= 80 && KS == 1) ? 3 : 2) void cross_many_kernel(CrossArgs a, Parts pt, int32_t q_tiles) {
+    using H = HeadShape<T, DP>;
+    constexpr int E = H::E, CH = H::CH, KSTEPS = H::KSTEPS, DT = H::DT;
+    constexpr int BKV = kTileKeys<T>, KBT = BKV / 32, KB = KBT / KS;      // keys of a tile, blocks of it, blocks per wavefront
+    constexpr int KROW = kKeyRow<T, DP>, VROW = kValueRow<T, DP>;
+    constexpr int kK = BKV * KROW, kV = BKV * VROW + (sizeof(T) == 4 ? 128 : 0);
+    constexpr int BQ = 128 / KS, NLD = (BKV * CH + kThreads - 1) / kThreads;
+    static_assert(KB >= 1, "a block of keys for each wavefront");
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    char* const sK = lds;
+    char* const sV = lds + 2 * kK;
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int l32 = lane & 31, g = lane >> 5;
+    const int qw = wave / KS, kb0 = wave % KS * KB;
+    const int pairs = a.B * a.kv_heads, group = a.heads / a.kv_heads;
+    // the query tiles of a (sample, head) re-read its keys: all on one XCD, next to each other
+    const int per_part = pairs * q_tiles;
+    const int part = blockIdx.x / per_part, id = blockIdx.x % per_part;
+    const bool by_xcd = pairs % kXcds == 0;
+    const int pair = by_xcd ? id % kXcds + kXcds * (id / (kXcds * q_tiles)) : id / q_tiles;
+    const int q_tile = by_xcd ? id / kXcds % q_tiles : id % q_tiles;
+    const int kvh = pair % a.kv_heads, b = pair / a.kv_heads;
+    const int64_t rows = static_cast<int64_t>(a.Nq) * group;
+    const int64_t row = static_cast<int64_t>(q_tile) * BQ + qw * 32 + l32;
+    const int len = attended(a, b);
+    const int t0 = part * pt.tiles, t1 = min(t0 + pt.tiles, (len + BKV - 1) / BKV);
+
+    const T* const kp = static_cast<const T*>(a.k) + static_cast<int64_t>(b) * a.Nk * a.k_stride + static_cast<int64_t>(kvh) * a.dh;
+    const T* const vp = static_cast<const T*>(a.v) + static_cast<int64_t>(b) * a.Nk * a.v_stride + static_cast<int64_t>(kvh) * a.dh;
+    const uint8_t* const mask = a.key_mask ? a.key_mask + static_cast<int64_t>(b) * a.Nk : nullptr;
+    const int k_row = static_cast<int>(a.k_stride) * static_cast<int>(sizeof(T)), v_row = static_cast<int>(a.v_stride) * static_cast<int>(sizeof(T));
+    xu32x4_t kreg[NLD], vreg[NLD];
+    uint32_t mask_next = 1;
+    const auto fetch = [&](int t) {
+        const int64_t kv0 = static_cast<int64_t>(t) * BKV;
+        const auto kb = rows_buffer(kp + kv0 * a.k_stride, len - kv0, a.k_stride, a.dh), vb = rows_buffer(vp + kv0 * a.v_stride, len - kv0, a.v_stride, a.dh);
+#pragma unroll
+        for (int i = 0; i < NLD; ++i) {
+            const int idx = tid + kThreads * i, r = idx / CH, c = idx % CH;
+            if (idx < BKV * CH) {
+                kreg[i] = buffer_chunk<T, kVec>(kb, r * k_row + c * 16, c, a.dh);
+                vreg[i] = buffer_chunk<T, kVec>(vb, r * v_row + c * 16, c, a.dh);
+            }
+        }
+        if (mask) mask_next = kv0 + lane < len ? mask[kv0 + lane] : 0;
+    };
+    const auto valid_of = [&](int t) {               // of the tile fetched last
+        const uint64_t v = keys_below(min(len - t * BKV, BKV));
+        return mask ? v & __ballot(mask_next != 0) : v;
+    };
+    const auto stash = [&](int stage, uint64_t valid) {
+#pragma unroll
+        for (int i = 0; i < NLD; ++i) {
+            const int idx = tid + kThreads * i, r = idx / CH, c = idx % CH;
+            if (idx < BKV * CH) {
+                *reinterpret_cast<xu32x4_t*>(sK + stage * kK + r * KROW + c * 16) = kreg[i];
+                if (mask && !(valid >> r & 1)) vreg[i] = xu32x4_t{0, 0, 0, 0};
+                *reinterpret_cast<xu32x4_t*>(sV + stage * kV + r * VROW + c * 16) = vreg[i];
+            }
+        }
+    };
+    if (t0 < t1) fetch(t0);
+
+    const int64_t q_row = row < rows ? row : rows - 1, q_token = q_row / group;
+    const int q_head = kvh * group + static_cast<int>(q_row - q_token * group);
+    const T* const qp = static_cast<const T*>(a.q) + (static_cast<int64_t>(b) * a.Nq + q_token) * a.q_stride + static_cast<int64_t>(q_head) * a.dh;
+    xu32x4_t qf[KSTEPS];
+#pragma unroll
+    for (int ks = 0; ks < KSTEPS; ++ks) qf[ks] = row_chunk<T, kVec>(qp, 2 * ks + g, a.dh);
+
+    xf32x16_t o[DT];
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) clear_tile(o[dt]);
+    float m_ref = -INFINITY, l = 0.f;
+    const float scale_log2 = a.scale * kLog2e;
+    uint64_t valid = 0;
+    bool any = false;
+    if (t0 < t1) {
+        valid = valid_of(t0);
+        stash(0, valid);
+        if (t0 + 1 < t1) fetch(t0 + 1);
+    }
+    __syncthreads();
+    const int key_at = block_row<T>(l32);
+    for (int t = t0; t < t1; ++t) {
+        const int stage = (t - t0) & 1;
+        xf32x16_t st[KB];
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) clear_tile(st[kb]);
+        __builtin_amdgcn_s_setprio(2);
+#pragma unroll
+        for (int ks = 0; ks < KSTEPS; ++ks)
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb)
+                chunk_product<T>(*reinterpret_cast<const xu32x4_t*>(sK + stage * kK + ((kb0 + kb) * 32 + key_at) * KROW + (2 * ks + g) * 16), qf[ks], st[kb]);
+        __builtin_amdgcn_s_setprio(0);
+        uint64_t valid_next = 0;
+        if (t + 1 < t1) {
+            valid_next = valid_of(t + 1);
+            stash(stage ^ 1, valid_next);
+            if (t + 2 < t1) fetch(t + 2);
+        }
+        any |= valid != 0;
+        const uint64_t full = BKV == 64 ? ~0ull : 0xffffffffull;
+        if ((valid & full) != full) {
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb) {
+                const uint32_t bits = static_cast<uint32_t>(valid >> (32 * (kb0 + kb))) >> (sizeof(T) == 2 ? 8 * g : 4 * g);
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    if (!(bits >> register_row<T>(e, 0) & 1)) st[kb][e] = -INFINITY;
+            }
+        }
+        softmax_step<KB, DT>(st, scale_log2, m_ref, l, o);
+        __builtin_amdgcn_s_setprio(2);
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) add_values<T, DT, VROW>(sV + stage * kV + (kb0 + kb) * 32 * VROW, lane, st[kb], o);
+        __builtin_amdgcn_s_setprio(0);
+        valid = valid_next;
+        __syncthreads();                             // the other stage is complete, this one free
+    }
+    l = add_lane_xor<32>(l);
+    if constexpr (KS == 2) {
+        // the second half of the keys hands its sums to the first
+        static_assert(2 * DT * 4096 + 2 * 512 <= 2 * kK + 2 * kV, "the partial results must fit in the stages");
+        float* const ml = reinterpret_cast<float*>(lds) + qw * 128 + lane;
+        char* const so = lds + 1024 + qw * DT * 4096 + lane * 16;
+        if (kb0 > 0) {
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+                for (int e4 = 0; e4 < 4; ++e4)
+                    *reinterpret_cast<xf32x4_t*>(so + (dt * 4 + e4) * 1024) = xf32x4_t{o[dt][4 * e4], o[dt][4 * e4 + 1], o[dt][4 * e4 + 2], o[dt][4 * e4 + 3]};
+            ml[0] = m_ref;
+            ml[64] = l;
+        }
+        __syncthreads();
+        if (kb0 > 0) return;
+        const float m1 = ml[0], m = fmaxf(m_ref, m1);
+        const float a0 = m == m_ref ? 1.0f : __builtin_amdgcn_exp2f((m_ref - m) * scale_log2), a1 = m == m1 ? 1.0f : __builtin_amdgcn_exp2f((m1 - m) * scale_log2);
+        l = a0 * l + a1 * ml[64];
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+            for (int e4 = 0; e4 < 4; ++e4) {
+                const xf32x4_t v = *reinterpret_cast<const xf32x4_t*>(so + (dt * 4 + e4) * 1024);
+#pragma unroll
+                for (int c = 0; c < 4; ++c) o[dt][4 * e4 + c] = a0 * o[dt][4 * e4 + c] + a1 * v[c];
+            }
+        m_ref = m;
+    }
+    if (row >= rows) return;
+    write_row<T, kVec, DT>(a, pt, part, pair, b, kvh, row, g, m_ref * scale_log2, l, any, o);
+}
+
+// Up to 32 rows per (sample, head): workgroup (part, pair), its four wavefronts take the part's key tiles of 32 in turn
+template <typename T, int DP, bool kVec>
+__global__ __launch_bounds__(kThreads, 1) void cross_few_kernel(CrossArgs a, Parts pt) {
+    using H = HeadShape<T, DP>;
+    constexpr int E = H::E, CH = H::CH, KSTEPS = H::KSTEPS, DT = H::DT;
+    constexpr int VROW = kValueRow<T, DP>, kWaveV = 32 * VROW + (sizeof(T) == 4 ? 128 : 0), NV = CH / 2;
+    constexpr int kWaveLds = kWaveV > DT * 4096 + 512 ? kWaveV : DT * 4096 + 512;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int l32 = lane & 31, g = lane >> 5;
+    const int pairs = a.B * a.kv_heads, group = a.heads / a.kv_heads;
+    const int part = blockIdx.x / pairs, pair = blockIdx.x % pairs;
+    const int kvh = pair % a.kv_heads, b = pair / a.kv_heads;
+    const int rows = a.Nq * group, row = l32;
+    const int len = attended(a, b);
+    const int t0 = part * pt.tiles + wave, t1 = min((part + 1) * pt.tiles, (len + 31) / 32);
+    const T* const kp = static_cast<const T*>(a.k) + static_cast<int64_t>(b) * a.Nk * a.k_stride + static_cast<int64_t>(kvh) * a.dh;
+    const T* const vp = static_cast<const T*>(a.v) + static_cast<int64_t>(b) * a.Nk * a.v_stride + static_cast<int64_t>(kvh) * a.dh;
+    const uint8_t* const mask = a.key_mask ? a.key_mask + static_cast<int64_t>(b) * a.Nk : nullptr;
+    const int k_row = static_cast<int>(a.k_stride) * static_cast<int>(sizeof(T)), v_row = static_cast<int>(a.v_stride) * static_cast<int>(sizeof(T));
+    char* const sV = lds + wave * kWaveLds;
+    const int key_at = block_row<T>(l32);
+
+    xu32x4_t kf[KSTEPS], vf[NV];
+    uint32_t mask_next = 1;
+    const auto fetch = [&](int t) {
+        const int64_t kv0 = static_cast<int64_t>(t) * 32;
+        const auto kb = rows_buffer(kp + kv0 * a.k_stride, len - kv0, a.k_stride, a.dh), vb = rows_buffer(vp + kv0 * a.v_stride, len - kv0, a.v_stride, a.dh);
+#pragma unroll
+        for (int ks = 0; ks < KSTEPS; ++ks) kf[ks] = buffer_chunk<T, kVec>(kb, key_at * k_row + (2 * ks + g) * 16, 2 * ks + g, a.dh);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int idx = lane + 64 * i, r = idx / CH, c = idx % CH;
+            vf[i] = buffer_chunk<T, kVec>(vb, r * v_row + c * 16, c, a.dh);
+        }
+        if (mask) mask_next = l32 < len - kv0 ? mask[kv0 + l32] : 0;
+    };
+    if (t0 < t1) fetch(t0);
+    const int q_row = row < rows ? row : rows - 1, q_token = q_row / group;
+    const T* const qp = static_cast<const T*>(a.q) + (static_cast<int64_t>(b) * a.Nq + q_token) * a.q_stride +
+                        static_cast<int64_t>(kvh * group + q_row - q_token * group) * a.dh;
+    xu32x4_t qf[KSTEPS];
+#pragma unroll
+    for (int ks = 0; ks < KSTEPS; ++ks) qf[ks] = row_chunk<T, kVec>(qp, 2 * ks + g, a.dh);
+    xf32x16_t o[DT];
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) clear_tile(o[dt]);
+    float m_ref = -INFINITY, l = 0.f;
+    const float scale_log2 = a.scale * kLog2e;
+    bool any = false;
+    for (int t = t0; t < t1; t += 4) {
+        uint64_t valid = keys_below(min(len - t * 32, 32));
+        if (mask) valid &= __ballot(mask_next != 0);
+        any |= valid != 0;
+        xf32x16_t st[1];
+        clear_tile(st[0]);
+#pragma unroll
+        for (int ks = 0; ks < KSTEPS; ++ks) chunk_product<T>(kf[ks], qf[ks], st[0]);
+        // (a wavefront's LDS accesses keep their order; the fences keep the compiler's)
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int idx = lane + 64 * i, r = idx / CH, c = idx % CH;
+            if (mask && !(valid >> r & 1)) vf[i] = xu32x4_t{0, 0, 0, 0};
+            *reinterpret_cast<xu32x4_t*>(sV + r * VROW + c * 16) = vf[i];
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        if (t + 4 < t1) fetch(t + 4);
+        if ((valid & 0xffffffffull) != 0xffffffffull) {
+            const uint32_t bits = static_cast<uint32_t>(valid) >> (sizeof(T) == 2 ? 8 * g : 4 * g);
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+                if (!(bits >> register_row<T>(e, 0) & 1)) st[0][e] = -INFINITY;
+        }
+        softmax_step<1, DT>(st, scale_log2, m_ref, l, o);
+        add_values<T, DT, VROW>(sV, lane, st[0], o);
+    }
+    l = add_lane_xor<32>(l);
+    // the wavefronts' sums, in order
+    __shared__ int seen[4];
+    if (lane == 0) seen[wave] = any;
+    float* const ml = reinterpret_cast<float*>(lds + wave * kWaveLds + DT * 4096);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    if (wave > 0) {
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+            for (int e4 = 0; e4 < 4; ++e4)
+                *reinterpret_cast<xf32x4_t*>(sV + (dt * 4 + e4) * 1024 + lane * 16) = xf32x4_t{o[dt][4 * e4], o[dt][4 * e4 + 1], o[dt][4 * e4 + 2], o[dt][4 * e4 + 3]};
+        if (g == 0) {
+            ml[l32] = m_ref;
+            ml[32 + l32] = l;
+        }
+    }
+    __syncthreads();
+    if (wave > 0) return;
+    float m = m_ref;
+#pragma unroll
+    for (int w = 1; w < 4; ++w) {
+        any |= seen[w] != 0;
+        m = fmaxf(m, reinterpret_cast<const float*>(lds + w * kWaveLds + DT * 4096)[l32]);
+    }
+    const auto factor = [&](float from) { return from == m ? 1.0f : __builtin_amdgcn_exp2f((from - m) * scale_log2); };
+    const float a0 = factor(m_ref);
+    l *= a0;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[dt][e] *= a0;
+    for (int w = 1; w < 4; ++w) {
+        const float* const wml = reinterpret_cast<const float*>(lds + w * kWaveLds + DT * 4096);
+        const float aw = factor(wml[l32]);
+        l += aw * wml[32 + l32];
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+            for (int e4 = 0; e4 < 4; ++e4) {
+                const xf32x4_t v = *reinterpret_cast<const xf32x4_t*>(lds + w * kWaveLds + (dt * 4 + e4) * 1024 + lane * 16);
+#pragma unroll
+                for (int c = 0; c < 4; ++c) o[dt][4 * e4 + c] += aw * v[c];
+            }
+    }
+    if (row >= rows) return;
+    write_row<T, kVec, DT>(a, pt, part, pair, b, kvh, row, g, m * scale_log2, l, any, o);
+}
+
+// The parts of a row's sums, added in order: a thread per value of out
+template <typename T>
+__global__ __launch_bounds__(kThreads) void cross_join_kernel(CrossArgs a, Parts pt) {
+    const int group = a.heads / a.kv_heads;
+    const int64_t per_pair = static_cast<int64_t>(a.Nq) * group, all = static_cast<int64_t>(a.B) * a.kv_heads * per_pair;
+    const int64_t i = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x;
+    if (i >= all * a.dh) return;
+    const int64_t at = i / a.dh, pair = at / per_pair, r = at % per_pair, token = r / group;
+    const int d = static_cast<int>(i % a.dh), b = static_cast<int>(pair / a.kv_heads), head = static_cast<int>(pair % a.kv_heads * group + r % group);
+    float m = -INFINITY;
+    for (int p = 0; p < pt.parts; ++p) m = fmaxf(m, pt.ml[2 * (p * all + at)]);
+    float l = 0.f, o = 0.f;
+    if (m != -INFINITY) {
+        for (int p = 0; p < pt.parts; ++p) {
+            const float mp = pt.ml[2 * (p * all + at)];
+            if (mp == -INFINITY) continue;
+            const float w = mp == m ? 1.0f : __builtin_amdgcn_exp2f(mp - m);
+            l += w * pt.ml[2 * (p * all + at) + 1];
+            o += w * pt.o[(p * all + at) * a.dh + d];
+        }
+    }
+    store_f(static_cast<T*>(a.out) + (static_cast<int64_t>(b) * a.Nq + token) * a.out_stride + static_cast<int64_t>(head) * a.dh + d, m == -INFINITY ? 0.f : o * (1.0f / l));
+    if (a.lse && d == 0) a.lse[(static_cast<int64_t>(b) * a.heads + head) * a.Nq + token] = m == -INFINITY ? m : (m + __builtin_log2f(l)) * kLn2;
+}
+
+// How a problem is cut; by its sizes alone (a workspace's size must not depend on the device)
+struct Plan {
+    bool few;
+    int ks;                                       // wavefronts that share a query block's keys (many rows)
+    int32_t parts, tiles;                         // tiles: of 32 keys (few), else kTileKeys
+    int64_t q_tiles;
+};
+constexpr int kUnits = 256;
+
+Plan plan_of(int32_t B, int32_t Nq, int32_t Nk, int32_t heads, int32_t kv_heads, int32_t dtype) {
+    const int64_t pairs = static_cast<int64_t>(B) * kv_heads, rows = static_cast<int64_t>(Nq) * (heads / kv_heads);
+    Plan p{};
+    p.few = rows <= kFewRows;
+    const int tile = p.few ? 32 : dtype == FREE_BF16 ? 64 : 32;
+    const int64_t tiles = std::max<int64_t>(1, (static_cast<int64_t>(Nk) + tile - 1) / tile);
+    p.ks = 1;
+    p.q_tiles = 1;
+    if (!p.few) {
+        p.q_tiles = (rows + 127) / 128;
+        if (dtype == FREE_BF16 && pairs * p.q_tiles <= 2 * kUnits) {
+            p.ks = 2;
+            p.q_tiles = (rows + 63) / 64;
+        }
+    }
+    const int64_t work = pairs * p.q_tiles, least = p.few ? 8 : 4, want = p.few ? 4 * kUnits : 2 * kUnits;      // tiles of a part; workgroups
+    int64_t parts = 1;
+    if (work < want) parts = std::max<int64_t>(1, std::min(want / std::max<int64_t>(work, 1), tiles / least));
+    parts = std::min<int64_t>(parts, 64);
+    p.tiles = static_cast<int32_t>((tiles + parts - 1) / parts);
+    p.parts = static_cast<int32_t>((tiles + p.tiles - 1) / p.tiles);
+    return p;
+}
+
+template <typename T, int DP, bool kVec>
+int32_t launch_shape(const CrossArgs& a, const Plan& p, const Parts& pt, hipStream_t s) {
+    const int64_t blocks = static_cast<int64_t>(a.B) * a.kv_heads * p.q_tiles * p.parts;
+    if (blocks > 0x7fffffff) return FREE_ERR_LIMIT;
+    constexpr int DT = HeadShape<T, DP>::DT;
+    if (p.few) {
+        const size_t lds = 4 * std::max<size_t>(32 * kValueRow<T, DP> + (sizeof(T) == 4 ? 128 : 0), DT * 4096 + 512);
+        auto kern = cross_few_kernel<T, DP, kVec>;
+        static LdsLimit limit;
+        if (!limit.allow(reinterpret_cast<const void*>(kern), lds)) return FREE_ERR_HIP;
+        hipLaunchKernelGGL(kern, dim3(static_cast<uint32_t>(blocks)), dim3(kThreads), lds, s, a, pt);
+        return launch_ok() ? FREE_OK : FREE_ERR_HIP;
+    }
+    const size_t lds = 2 * kTileKeys<T> * static_cast<size_t>(kKeyRow<T, DP> + kValueRow<T, DP>) + (sizeof(T) == 4 ? 256 : 0);
+    const auto launch = [&](auto ks) {
+        auto kern = cross_many_kernel<T, DP, decltype(ks)::value, kVec>;
+        static LdsLimit limit;
+        if (!limit.allow(reinterpret_cast<const void*>(kern), lds)) return FREE_ERR_HIP;
+        hipLaunchKernelGGL(kern, dim3(static_cast<uint32_t>(blocks)), dim3(kThreads), lds, s, a, pt, static_cast<int32_t>(p.q_tiles));
+        return launch_ok() ? FREE_OK : FREE_ERR_HIP;
+    };
+    if constexpr (sizeof(T) == 2) {
+        if (p.ks == 2) return launch(std::integral_constant<int, 2>{});
+    }
+    return launch(std::integral_constant<int, 1>{});
+}
+
+template <typename T, bool kVec>
+int32_t launch_width(const CrossArgs& a, const Plan& p, const Parts& pt, hipStream_t s) {
+    if (a.dh <= 32) return launch_shape<T, 32, kVec>(a, p, pt, s);
+    if (a.dh <= 64) return launch_shape<T, 64, kVec>(a, p, pt, s);
+    if (a.dh <= 80) return launch_shape<T, 80, kVec>(a, p, pt, s);
+    if (a.dh <= 96) return launch_shape<T, 96, kVec>(a, p, pt, s);
+    return launch_shape<T, 128, kVec>(a, p, pt, s);
+}
+
+size_t up256(size_t n) { return (n + 255) / 256 * 256; }
+
+template <typename T>
+int32_t launch_type(const CrossArgs& a, const Plan& p, const Parts& pt, hipStream_t s) {
+    const auto al = [](const void* x, int64_t stride) { return (reinterpret_cast<uintptr_t>(x) & 15u) == 0 && stride % static_cast<int64_t>(16 / sizeof(T)) == 0; };
+    const bool vec = a.dh % static_cast<int>(16 / sizeof(T)) == 0 && al(a.q, a.q_stride) && al(a.k, a.k_stride) && al(a.v, a.v_stride) && al(a.out, a.out_stride);
+    const int32_t st = vec ? launch_width<T, true>(a, p, pt, s) : launch_width<T, false>(a, p, pt, s);
+    if (st != FREE_OK || p.parts == 1) return st;
+    const int64_t values = static_cast<int64_t>(a.B) * a.Nq * a.heads * a.dh;
+    hipLaunchKernelGGL(cross_join_kernel<T>, dim3(static_cast<uint32_t>((values + kThreads - 1) / kThreads)), dim3(kThreads), 0, s, a, pt);
+    return launch_ok() ? FREE_OK : FREE_ERR_HIP;
+}
+
+}  // namespace
+
+size_t cross_forward_bytes(int32_t B, int32_t Nq, int32_t Nk, int32_t heads, int32_t kv_heads, int32_t dh, int32_t dtype) {
+    const Plan p = plan_of(B, Nq, Nk, heads, kv_heads, dtype);
+    if (p.parts == 1) return 256;
+    const size_t rows = static_cast<size_t>(B) * Nq * heads * p.parts;
+    return up256(rows * dh * sizeof(float)) + up256(rows * 2 * sizeof(float));
+}
+
+int32_t launch_cross_forward(const CrossArgs& a, int32_t dtype, void* ws, hipStream_t s) {
+    const Plan p = plan_of(a.B, a.Nq, a.Nk, a.heads, a.kv_heads, dtype);
+    Parts pt{p.parts, p.tiles, nullptr, nullptr};
+    if (p.parts > 1) {
+        pt.o = static_cast<float*>(ws);
+        pt.ml = reinterpret_cast<float*>(static_cast<char*>(ws) + up256(static_cast<size_t>(a.B) * a.Nq * a.heads * p.parts * a.dh * sizeof(float)));
+    }
+    return dtype == FREE_BF16 ? launch_type<bf16_t>(a, p, pt, s) : launch_type<float>(a, p, pt, s);
+}
+
+}  // namespace freemi
