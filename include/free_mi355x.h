@@ -609,6 +609,28 @@ int32_t free_op_cross_attention_backward(const void* dout, int64_t dout_stride, 
                                          int64_t dq_stride, void* dk, int64_t dk_stride, void* dv, int64_t dv_stride, void* workspace,
                                          size_t ws_bytes, void* stream);
 
+/* A shared projection of M token rows with the low-rank adapters of many requests: row m belongs to sample m / rows_per_sample, which has
+ * adapter a = adapter[sample], or none where that is not one of 0 .. n - 1 (-1, say),
+ *   out = x W^T + bias + t B_a^T,   t = scale_a x A_a^T
+ * x [M, K], W [N, K], A [n, r, K], B [n, N, r], out [M, N], all of type dtype, contiguous; x, W, out (dout, dx) 16-byte aligned; bias fp32 [N] or
+ * NULL; scale fp32 [n] or NULL (ones); adapter int32 [samples], in any order.  Adapters of lower rank are filled up with zeros.  Sums are fp32,
+ * t is rounded to dtype as operand of the second product.  Any K and N up to 2^20; those that are not multiples of 8 (bf16) or 64 (fp32) go through
+ * padded copies in the workspace, but for forward calls of at most 32 rows.  r <= 128, n <= 16384, M K and M N at most 2^36 (bf16) or 2^34 (fp32),
+ * (K + N) r n at most 2^36 (FREE_ERR_LIMIT).
+ * saved (NULL: none): free_linear_adapters_saved_bytes bytes, 256-byte aligned, that keep t for the gradient.
+ * The gradient, W, bias and scale being fixed:
+ *   dx = dout W + u A_a,   u = scale_a dout B_a,   dA_a = sum over the adapter's rows of u^T x,   dB_a = sum of dout^T t
+ * written, not added to; u is rounded to dtype.  Adapters without rows have zeros. */
+size_t free_linear_adapters_saved_bytes(int32_t M, int32_t r, int32_t dtype);
+size_t free_linear_adapters_workspace_bytes(int32_t M, int32_t K, int32_t N, int32_t r, int32_t n, int32_t dtype, int32_t backward);
+int32_t free_op_linear_adapters(const void* x, const void* W, const float* bias, const void* A, const void* B, const float* scale,
+                                const int32_t* adapter, int32_t rows_per_sample, int32_t M, int32_t K, int32_t N, int32_t r, int32_t n,
+                                int32_t dtype, void* out, void* saved, size_t saved_bytes, void* workspace, size_t ws_bytes, void* stream);
+int32_t free_op_linear_adapters_backward(const void* dout, const void* x, const void* W, const void* A, const void* B, const float* scale,
+                                         const int32_t* adapter, int32_t rows_per_sample, const void* saved, size_t saved_bytes, int32_t M,
+                                         int32_t K, int32_t N, int32_t r, int32_t n, int32_t dtype, void* dx, void* dA, void* dB,
+                                         void* workspace, size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -41,6 +41,7 @@ EXPORTED_SYMBOLS = [
     "free_op_layer_norm", "free_layer_norm_backward_workspace_bytes", "free_op_layer_norm_backward", "free_op_rope_axes",
     "free_gated_ffn_saved_bytes", "free_gated_ffn_workspace_bytes", "free_op_gated_ffn", "free_op_gated_ffn_backward",
     "free_cross_attention_workspace_bytes", "free_op_cross_attention", "free_op_cross_attention_backward",
+    "free_linear_adapters_saved_bytes", "free_linear_adapters_workspace_bytes", "free_op_linear_adapters", "free_op_linear_adapters_backward",
 ]
 PROF_NCAT = 12
 
@@ -183,6 +184,14 @@ def load():
     lib.free_op_cross_attention.argtypes = [vp, i64] * 3 + [vp, vp] + [i32] * 6 + [f32, i32, vp, i64, vp, vp, sz, vp]
     lib.free_op_cross_attention_backward.restype = i32
     lib.free_op_cross_attention_backward.argtypes = [vp, i64] * 5 + [vp] * 3 + [i32] * 6 + [f32, i32] + [vp, i64] * 3 + [vp, sz, vp]
+    lib.free_linear_adapters_saved_bytes.restype = sz
+    lib.free_linear_adapters_saved_bytes.argtypes = [i32] * 3
+    lib.free_linear_adapters_workspace_bytes.restype = sz
+    lib.free_linear_adapters_workspace_bytes.argtypes = [i32] * 7
+    lib.free_op_linear_adapters.restype = i32
+    lib.free_op_linear_adapters.argtypes = [vp] * 7 + [i32] * 7 + [vp, vp, sz, vp, sz, vp]
+    lib.free_op_linear_adapters_backward.restype = i32
+    lib.free_op_linear_adapters_backward.argtypes = [vp] * 7 + [i32, vp, sz] + [i32] * 6 + [vp] * 4 + [sz, vp]
     _lib = lib
     return lib
 
@@ -1040,3 +1049,66 @@ def op_cross_attention_backward(dout, q, k, v, out, lse, B: int, heads: int, dh:
     _enqueue(load().free_op_cross_attention_backward, "free_op_cross_attention_backward", dev, *wide, lse_at, *keys, B, Nq, Nk, heads, kv_heads, dh,
              scale, mode, *written, _addr(workspace, torch.uint8, "workspace"), workspace.numel())
     return grads
+
+
+def linear_adapters_saved_bytes(M: int, r: int, mode: str) -> int:
+    """Bytes of what op_linear_adapters keeps for op_linear_adapters_backward."""
+    _int32(M, r)
+    return load().free_linear_adapters_saved_bytes(M, r, MODES[mode])
+
+
+def linear_adapters_workspace_bytes(M: int, K: int, N: int, r: int, n: int, mode: str, backward: bool = False) -> int:
+    """Workspace of op_linear_adapters with n adapters; with backward, of either pass."""
+    _int32(M, K, N, r, n)
+    return load().free_linear_adapters_workspace_bytes(M, K, N, r, n, MODES[mode], int(bool(backward)))
+
+
+def _adapter_sizes(x, W, A, B, adapter, rows_per_sample):
+    if x.dim() != 2 or W.dim() != 2 or A.dim() != 3 or B.dim() != 3:
+        raise FreeError(FREE_ERR_SHAPE, "x, W: two axes each, A, B: three")
+    (M, K), N, (n, r) = x.shape, W.shape[0], A.shape[:2]
+    if (M | K | N | n | r) >> 31:
+        _int32(M, K, N, n, r)
+    # (more rows per sample than rows are one sample, whatever the number)
+    rows = max(M, 1) if rows_per_sample is None else min(int(rows_per_sample), max(M, 1))
+    if rows < 1:
+        raise FreeError(FREE_ERR_SHAPE, f"rows_per_sample: {rows}")
+    dt = x.dtype
+    return M, K, N, r, n, rows, _mode_of(x, "x"), (_addr(x, dt, "x"), _addr(W, dt, "W", (N, K))), (_addr(A, dt, "A", (n, r, K)), _addr(B, dt, "B", (n, N, r)))
+
+
+def op_linear_adapters(x, W, bias, A, B, adapter, scale=None, rows_per_sample: int = None, saved=None, out=None, workspace=None):
+    """x W^T + bias + scale[a] (x A[a]^T) B[a]^T for x [M, K], W [N, K], A [n, r, K], B [n, N, r], all float32 or all bfloat16, with a = adapter[row //
+    rows_per_sample] (int32; not one of the n, -1 say: no adapter).  bias [N], scale [n]: float32 or None.  saved: None, or a uint8 tensor of
+    linear_adapters_saved_bytes for op_linear_adapters_backward."""
+    import torch
+    M, K, N, r, n, rows, mode, xw, ab = _adapter_sizes(x, W, A, B, adapter, rows_per_sample)
+    u8 = torch.uint8
+    if out is None:
+        out = torch.empty(M, N, dtype=x.dtype, device=x.device)
+    if workspace is None:
+        workspace = torch.empty(load().free_linear_adapters_workspace_bytes(M, K, N, r, n, mode, 0), dtype=u8, device=x.device)
+    dev = _same_device(x, W, bias, A, B, adapter, scale, saved, out, workspace)
+    _enqueue(load().free_op_linear_adapters, "free_op_linear_adapters", dev, *xw, _addr(bias, torch.float32, "bias", (N,), optional=True), *ab,
+             _addr(scale, torch.float32, "scale", (n,), optional=True), _addr(adapter, torch.int32, "adapter", (-(-M // rows),)), rows, M, K, N, r, n, mode,
+             _addr(out, x.dtype, "out", (M, N)), _addr(saved, u8, "saved", optional=True), 0 if saved is None else saved.numel(),
+             _addr(workspace, u8, "workspace"), workspace.numel())
+    return out
+
+
+def op_linear_adapters_backward(dout, x, W, A, B, adapter, saved, scale=None, rows_per_sample: int = None, out=None, workspace=None):
+    """Gradient of op_linear_adapters, of which `saved` is, by x and the adapters: (dx, dA, dB).  out: the three to write to."""
+    import torch
+    M, K, N, r, n, rows, mode, xw, ab = _adapter_sizes(x, W, A, B, adapter, rows_per_sample)
+    u8, dt = torch.uint8, x.dtype
+    if out is None:
+        out = (torch.empty_like(x), torch.empty_like(A), torch.empty_like(B))
+    dx, dA, dB = out
+    if workspace is None:
+        workspace = torch.empty(load().free_linear_adapters_workspace_bytes(M, K, N, r, n, mode, 1), dtype=u8, device=x.device)
+    dev = _same_device(x, dout, W, A, B, adapter, scale, saved, dx, dA, dB, workspace)
+    _enqueue(load().free_op_linear_adapters_backward, "free_op_linear_adapters_backward", dev, _addr(dout, dt, "dout", (M, N)), *xw, *ab,
+             _addr(scale, torch.float32, "scale", (n,), optional=True), _addr(adapter, torch.int32, "adapter", (-(-M // rows),)), rows,
+             _addr(saved, u8, "saved"), saved.numel(), M, K, N, r, n, mode, _addr(dx, dt, "dx", (M, K)), _addr(dA, dt, "dA", (n, r, K)),
+             _addr(dB, dt, "dB", (n, N, r)), _addr(workspace, u8, "workspace"), workspace.numel())
+    return out

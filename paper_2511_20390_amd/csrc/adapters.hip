@@ -1,0 +1,620 @@
+// A shared projection with the low-rank adapters of many requests beside it, and the gradient that fits adapters.  Row m belongs to request
+// m / rows_per_sample, which has adapter a of n (or none):
+//   t = s_a x A_a^T [M, r],   out = x W^T + bias + t B_a^T
+//   u = s_a dout B_a [M, r],  dx = dout W + u A_a,   dA_a = sum over the adapter's rows of u^T x,   dB_a = sum of dout^T t
+// (s: a scale per adapter; W is shared and keeps still).  Requests come in any order: wherever a kernel has a block of rows, it takes the
+// adapters of these rows one after the other, with the other rows masked.
+//  * t and u: x (dout) is read once, 16 or 32 rows per workgroup whose wavefronts share K; rounded to the type of the product they are
+//    operands of, like the hidden values of the gated block.
+//  * out and dx: the products of ffn_mfma.hip, whose sums begin with bias and adapter (bf16), or a second pass over the result (fp32, where
+//    the product takes ten times as long); up to 32 rows ffn_rows.hip.
+//  * dA and dB: 128 columns of x or dout by all ranks per workgroup, over the rows of one adapter, in parts that a second launch adds in
+//    order.  Rows of other adapters are not read.
+// For the gradient B and A are needed the other way round ([rank][N], [K][rank]): copies of that layout go into the workspace, ranks filled up
+// with zeros; they are r (N + K) values per adapter against the N K of the weights.
+#include <algorithm>
+
+#include "cross_attn.h"
+#include "ffn_mfma.h"
+#include "free_internal.h"
+#include "row_pieces.h"
+
+namespace freemi {
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kDownWaves = 8;
+constexpr int kTileRows = 64;                    // token rows of a tile of the weights' gradients
+constexpr int kMasks = 512;                      // tiles whose rows are looked over at once
+
+int32_t up_to(int32_t v, int32_t step) { return (v + step - 1) / step * step; }
+
+// ---- t, u
+struct DownArgs {
+    const void *x, *w;                           // x [M, K]; w [adapter][w_rows][K]
+    const int32_t* adapter;
+    const float* scale;                          // nullable
+    void* out;                                   // [M][t_row], zeros from r on
+    int32_t M, K, n_adapters, w_rows, r, t_row, rows_per_sample;
+};
+
+// Workgroup (block of 16 MT rows, j, 16 RT ranks): the j-th adapter of the block's rows, in the order they come
+template <typename T, int MT, int RT, bool kEdge>
+__global__ __launch_bounds__(kDownWaves * 64) void adapter_down_kernel(DownArgs a) {
+    constexpr int P = 2, E = 16 / sizeof(T), kStep = 4 * P * E, U = MT * RT > 2 ? 2 : 4;
+    __shared__ f32x4a_t red[kDownWaves][RT * MT][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int m0 = blockIdx.x * 16 * MT, rank0 = blockIdx.z * 16 * RT, quad = lane >> 4, r16 = lane & 15;
+    int of = -1;                                 // lane: row m0 + lane's adapter
+    if (lane < 16 * MT && m0 + lane < a.M) {
+        const int id = a.adapter[(m0 + lane) / a.rows_per_sample];
+        of = id >= 0 && id < a.n_adapters ? id : -1;
+    }
+    int which = -1;
+    uint64_t left = __ballot(of >= 0);
+    for (int j = 0; left != 0; ++j) {
+        which = __builtin_amdgcn_readlane(of, __builtin_ctzll(left));
+        if (j == static_cast<int>(blockIdx.y)) break;
+        left &= ~__ballot(of == which);
+    }
+    if (left == 0) return;
+    const uint64_t mine = __ballot(of == which);
+    const int at = quad * P * E;
+    const T* w[RT];
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+        const int rank = rank0 + t * 16 + r16;
+        w[t] = static_cast<const T*>(a.w) + (static_cast<int64_t>(which) * a.w_rows + (rank < a.r ? rank : a.r - 1)) * a.K + at;
+    }
+    const T* x[MT];
+#pragma unroll
+    for (int t = 0; t < MT; ++t) {
+        const int m = m0 + t * 16 + r16;
+        x[t] = static_cast<const T*>(a.x) + static_cast<int64_t>(m < a.M ? m : a.M - 1) * a.K + at;
+    }
+    f32x4a_t acc[RT][MT];
+#pragma unroll
+    for (int b = 0; b < RT; ++b)
+#pragma unroll
+        for (int t = 0; t < MT; ++t) acc[b][t] = f32x4a_t{0.f, 0.f, 0.f, 0.f};
+    const int steps = (a.K + kStep - 1) / kStep;
+    for (int s0 = wave; s0 < steps; s0 += kDownWaves * U) {
+        u32x4_t wv[U][RT][P], xv[U][MT][P];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int s = s0 + u * kDownWaves;
+            if (s >= steps) continue;
+            const int64_t k = static_cast<int64_t>(s) * kStep;
+            const bool whole = !kEdge || k + kStep <= a.K;
+            const int rest = static_cast<int>(a.K - k) - at;
+#pragma unroll
+            for (int t = 0; t < MT; ++t)
+#pragma unroll
+                for (int p = 0; p < P; ++p) load_piece(x[t] + k + p * E, rest - p * E, xv[u][t][p], whole);
+#pragma unroll
+            for (int b = 0; b < RT; ++b)
+#pragma unroll
+                for (int p = 0; p < P; ++p) load_piece(w[b] + k + p * E, rest - p * E, wv[u][b][p], whole);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (s0 + u * kDownWaves >= steps) continue;
+#pragma unroll
+            for (int p = 0; p < P; ++p)
+#pragma unroll
+                for (int b = 0; b < RT; ++b)
+#pragma unroll
+                    for (int t = 0; t < MT; ++t) multiply<T>(wv[u][b][p], xv[u][t][p], acc[b][t]);
+        }
+    }
+#pragma unroll
+    for (int b = 0; b < RT; ++b)
+#pragma unroll
+        for (int t = 0; t < MT; ++t) red[wave][b * MT + t][lane] = acc[b][t];
+    __syncthreads();
+    const float scale = a.scale ? a.scale[which] : 1.0f;
+    // value i: token i / (16 RT), rank i % (16 RT); it stands in lane token + 16 (rank / 4), register rank % 4
+    for (int i = threadIdx.x; i < MT * 16 * RT * 16; i += kDownWaves * 64) {
+        const int row = i / (16 * RT), c = i % (16 * RT), t = row / 16, b = c / 16, from = row % 16 + 16 * (c % 16 / 4);
+        if (!(mine >> row & 1) || rank0 + c >= a.t_row) continue;
+        float v = red[0][b * MT + t][from][c & 3];
+#pragma unroll
+        for (int k = 1; k < kDownWaves; ++k) v += red[k][b * MT + t][from][c & 3];
+        store_f(static_cast<T*>(a.out) + static_cast<int64_t>(m0 + row) * a.t_row + rank0 + c, rank0 + c < a.r ? v * scale : 0.f);
+    }
+}
+
+template <typename T, int MT, int RT>
+int32_t launch_down_shape(const DownArgs& a, hipStream_t s) {
+    const int32_t block = 16 * MT, rows = std::min(block, a.M);
+    // adapters that a block of rows can have
+    int32_t most = a.rows_per_sample >= a.M || a.rows_per_sample % block == 0 ? 1 : std::min(rows, (rows - 1) / a.rows_per_sample + 2);
+    most = std::min(most, a.n_adapters);
+    const dim3 grid((a.M + block - 1) / block, most, (a.t_row + 16 * RT - 1) / (16 * RT));
+    constexpr int kStep = 128 / sizeof(T);
+    if (a.K % kStep == 0) hipLaunchKernelGGL((adapter_down_kernel<T, MT, RT, false>), grid, dim3(kDownWaves * 64), 0, s, a);
+    else hipLaunchKernelGGL((adapter_down_kernel<T, MT, RT, true>), grid, dim3(kDownWaves * 64), 0, s, a);
+    return launch_ok() ? FREE_OK : FREE_ERR_HIP;
+}
+
+template <typename T, int MT>
+int32_t launch_down_ranks(const DownArgs& a, hipStream_t s) {
+    if (a.t_row <= 16) return launch_down_shape<T, MT, 1>(a, s);
+    if (a.t_row <= 32) return launch_down_shape<T, MT, 2>(a, s);
+    return launch_down_shape<T, MT, 4>(a, s);
+}
+
+template <typename T>
+int32_t launch_down(const DownArgs& a, hipStream_t s) {
+    return a.M <= 16 * 256 ? launch_down_ranks<T, 1>(a, s) : launch_down_ranks<T, 2>(a, s);
+}
+
+// ---- A and B the other way round
+struct TurnJob {
+    const void* src;                             // [n][rows][cols]
+    void* dst;                                   // [n][cols_to][rows_to]
+    int32_t rows, cols, rows_to, cols_to;
+};
+
+template <typename T>
+__global__ __launch_bounds__(kThreads) void adapter_turn_kernel(TurnJob j0, TurnJob j1, int32_t n) {
+    __shared__ T tile[32][33];
+    const bool second = static_cast<int>(blockIdx.z) >= n;
+    const TurnJob& j = second ? j1 : j0;
+    const int which = second ? blockIdx.z - n : blockIdx.z;
+    const int tiles_r = (j.rows_to + 31) / 32, tiles_c = (j.cols_to + 31) / 32;
+    const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5;
+    const T* const src = static_cast<const T*>(j.src) + static_cast<int64_t>(which) * j.rows * j.cols;
+    T* const dst = static_cast<T*>(j.dst) + static_cast<int64_t>(which) * j.rows_to * j.cols_to;
+    for (int id = blockIdx.x; id < tiles_r * tiles_c; id += gridDim.x) {
+        const int r0 = id / tiles_c * 32, c0 = id % tiles_c * 32;
+#pragma unroll
+        for (int i = 0; i < 32; i += 8) {
+            const int r = r0 + ty + i, c = c0 + tx;
+            tile[ty + i][tx] = r < j.rows && c < j.cols ? src[static_cast<int64_t>(r) * j.cols + c] : T{};
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 32; i += 8) {
+            const int c = c0 + ty + i, r = r0 + tx;
+            if (c < j.cols_to && r < j.rows_to) dst[static_cast<int64_t>(c) * j.rows_to + r] = tile[tx][ty + i];
+        }
+        __syncthreads();
+    }
+}
+
+// ---- fp32: out = y + bias + t B^T; a wavefront has 32 x 32 values
+__global__ __launch_bounds__(kThreads) void adapter_up_kernel(const float* y, int64_t ldy, AdapterTerm ad, int32_t M, float* out) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l32 = lane & 31, g = lane >> 5;
+    const int n0 = (blockIdx.x * 4 + wave) * 32, N = ad.cols;
+    if (n0 >= N) return;
+    const bool whole = ad.b_row % 4 == 0 && (reinterpret_cast<uintptr_t>(ad.b) & 15u) == 0;
+    for (int64_t m0 = static_cast<int64_t>(blockIdx.y) * 32; m0 < M; m0 += static_cast<int64_t>(gridDim.y) * 32) {
+        const int m = static_cast<int>(m0) + l32;
+        xf32x16_t acc;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            const int n = n0 + 8 * (e >> 2) + 4 * g + (e & 3);
+            acc[e] = m < M && n < N ? y[m * ldy + n] + (ad.bias ? ad.bias[n] : 0.f) : 0.f;
+        }
+        int of = m < M ? ad.of_row(m) : -1;
+        for (uint64_t left = __ballot(of >= 0); left != 0; left = __ballot(of >= 0)) {
+            const int which = __builtin_amdgcn_readlane(of, __builtin_ctzll(left));
+            const int n = n0 + l32 < N ? n0 + l32 : N - 1;
+            const float* const b = static_cast<const float*>(ad.b) + (static_cast<int64_t>(which) * N + n) * ad.b_row;
+            const float* const t = static_cast<const float*>(ad.t) + static_cast<int64_t>(m < M ? m : M - 1) * ad.t_row;
+            for (int k0 = 0; k0 < ad.r; k0 += 8) {
+                const int k = k0 + 4 * g;
+                xu32x4_t tv = {0, 0, 0, 0}, bv = {0, 0, 0, 0};
+                if (of == which) tv = *reinterpret_cast<const xu32x4_t*>(t + k);
+                if (whole) {
+                    if (k < ad.r) bv = *reinterpret_cast<const xu32x4_t*>(b + k);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) bv[e] = k + e < ad.r ? __float_as_uint(b[k + e]) : 0u;
+                }
+                chunk_product<float>(bv, tv, acc);
+            }
+            of = of == which ? -1 : of;
+        }
+        if (m < M) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const int n = n0 + 8 * (e >> 2) + 4 * g + (e & 3);
+                if (n < N) out[static_cast<int64_t>(m) * N + n] = acc[e];
+            }
+        }
+    }
+}
+
+// ---- dA, dB
+struct SumArgs {
+    const void* wide[2];                         // x, dout: [M][ld]
+    const void* thin[2];                         // u, t: [M][t_row]
+    int64_t ld[2];
+    int32_t cols[2];                             // K, N
+    int32_t tiles[2];                            // of 128 columns
+    void* out[2];                                // dA [n][r][K], dB [n][N][r]
+    float* part;                                 // parts > 1: [part][adapter][K + N][t_row]
+    const int32_t* adapter;
+    int32_t M, n_adapters, r, t_row, rows_per_sample, parts, part_tiles;
+};
+
+__device__ __forceinline__ int turned_chunk(int row, int c) { return c ^ ((row & 3) << 2 | (row >> 2 & 3)); }     // 256-byte rows: Tile::at of cross_attn_grad.hip
+
+// RB: blocks of 32 ranks.  Workgroup (columns, adapter, part): a wavefront has 32 columns.
+template <typename T, int RB>
+__global__ __launch_bounds__(kThreads) void adapter_sum_kernel(SumArgs a) {
+    constexpr int kPitch = 256, kLoads = kTileRows * 16 / kThreads;
+    __shared__ uint64_t masks[kMasks];
+    extern __shared__ __attribute__((aligned(16))) char lds[];          // bf16: [stage][wide, thin] tiles of 64 rows x 256 bytes
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, g = lane >> 5;
+    const int col_tiles = a.tiles[0] + a.tiles[1];
+    const int ct = blockIdx.x % col_tiles, which = blockIdx.x / col_tiles % a.n_adapters, part = blockIdx.x / col_tiles / a.n_adapters;
+    const bool second = ct >= a.tiles[0];
+    const T* const wide = static_cast<const T*>(second ? a.wide[1] : a.wide[0]);
+    const T* const thin = static_cast<const T*>(second ? a.thin[1] : a.thin[0]);
+    const int64_t ld = second ? a.ld[1] : a.ld[0];
+    const int cols = second ? a.cols[1] : a.cols[0], c0 = (second ? ct - a.tiles[0] : ct) * 128;
+    const int tiles = (a.M + kTileRows - 1) / kTileRows, first = part * a.part_tiles, last = min(first + a.part_tiles, tiles);
+    xf32x16_t acc[RB];
+#pragma unroll
+    for (int b = 0; b < RB; ++b) clear_tile(acc[b]);
+    for (int base = first; base < last; base += kMasks) {
+        // which rows of the tiles are this adapter's
+        const int count = min(last - base, kMasks);
+        if (base > first) __syncthreads();
+        for (int i = wave; i < count; i += 4) {
+            const int64_t m = static_cast<int64_t>(base + i) * kTileRows + lane;
+            const uint64_t bits = __ballot(m < a.M && a.adapter[(m < a.M ? m : 0) / a.rows_per_sample] == which);
+            if (lane == 0) masks[i] = bits;
+        }
+        __syncthreads();
+        const auto next = [&](int i) {
+            while (i < count && masks[i] == 0) ++i;
+            return i;
+        };
+        if constexpr (sizeof(T) == 2) {
+            u32x4_t wv[kLoads], tv[kLoads];
+            const auto fetch = [&](int i) {
+                const uint64_t bits = masks[i];
+                const int64_t m0 = static_cast<int64_t>(base + i) * kTileRows;
+#pragma unroll
+                for (int k = 0; k < kLoads; ++k) {
+                    const int row = (tid + k * kThreads) / 16, c = (tid + k * kThreads) % 16;
+                    wv[k] = tv[k] = u32x4_t{0, 0, 0, 0};
+                    if (bits >> row & 1) {
+                        if (c0 + c * 8 < cols) wv[k] = *reinterpret_cast<const u32x4_t*>(wide + (m0 + row) * ld + c0 + c * 8);
+                        if (c * 8 < a.t_row) tv[k] = *reinterpret_cast<const u32x4_t*>(thin + (m0 + row) * a.t_row + c * 8);
+                    }
+                }
+            };
+            const auto stash = [&](int stage) {
+#pragma unroll
+                for (int k = 0; k < kLoads; ++k) {
+                    const int row = (tid + k * kThreads) / 16, c = (tid + k * kThreads) % 16;
+                    char* const to = lds + stage * 2 * kTileRows * kPitch + row * kPitch + (turned_chunk(row, c) << 4);
+                    *reinterpret_cast<u32x4_t*>(to) = wv[k];
+                    if (c * 8 < RB * 32) *reinterpret_cast<u32x4_t*>(to + kTileRows * kPitch) = tv[k];
+                }
+            };
+            // transposing reads: 8 consecutive rows of a column per lane (cross_attn.h)
+            const int row = 8 * g + ((lane & 15) >> 2), in_c = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1), in = 8 * (lane & 1);
+            const auto column = [&](const char* tile, int ks, int block) {
+                const char* const p = tile + ks * 16 * kPitch + in;
+                return transposed_chunk(p + row * kPitch + (turned_chunk(row, 4 * block + in_c) << 4),
+                                        p + (row + 4) * kPitch + (turned_chunk(row + 4, 4 * block + in_c) << 4));
+            };
+            int i = next(0), stage = 0;
+            if (i < count) fetch(i);
+            while (i < count) {
+                stash(stage);
+                i = next(i + 1);
+                if (i < count) fetch(i);
+                __syncthreads();
+                const char* const tile = lds + stage * 2 * kTileRows * kPitch;
+#pragma unroll
+                for (int ks = 0; ks < kTileRows / 16; ++ks) {
+                    const xu32x4_t w = column(tile, ks, wave);
+#pragma unroll
+                    for (int b = 0; b < RB; ++b) chunk_product<T>(w, column(tile + kTileRows * kPitch, ks, b), acc[b]);
+                }
+                stage ^= 1;
+            }
+        } else {
+            const int col = c0 + wave * 32 + l32;
+            for (int i = next(0); i < count; i = next(i + 1)) {
+                const uint64_t bits = masks[i];
+                const int64_t m0 = static_cast<int64_t>(base + i) * kTileRows;
+#pragma unroll 8
+                for (int k = 0; k < kTileRows / 2; ++k) {
+                    const int row = 2 * k + g;
+                    const bool on = bits >> row & 1;
+                    const float w = on && col < cols ? wide[(m0 + row) * ld + col] : 0.f;
+#pragma unroll
+                    for (int b = 0; b < RB; ++b) {
+                        const float t = on && b * 32 + l32 < a.t_row ? thin[(m0 + row) * a.t_row + b * 32 + l32] : 0.f;
+                        acc[b] = __builtin_amdgcn_mfma_f32_32x32x2f32(w, t, acc[b], 0, 0, 0);
+                    }
+                }
+            }
+        }
+    }
+    // register e: column 8 (e / 4) + 4 g + e % 4 of the wavefront's, rank 32 b + l32
+#pragma unroll
+    for (int b = 0; b < RB; ++b) {
+        const int rank = b * 32 + l32;
+        if (rank >= a.r) continue;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            const int col = c0 + wave * 32 + 8 * (e >> 2) + 4 * g + (e & 3);
+            if (col >= cols) continue;
+            if (a.parts > 1) {
+                const int64_t at = (static_cast<int64_t>(part) * a.n_adapters + which) * (a.cols[0] + a.cols[1]) + (second ? a.cols[0] : 0) + col;
+                a.part[at * a.t_row + rank] = acc[b][e];
+            } else if (second) {
+                store_f(static_cast<T*>(a.out[1]) + (static_cast<int64_t>(which) * cols + col) * a.r + rank, acc[b][e]);
+            } else {
+                store_f(static_cast<T*>(a.out[0]) + (static_cast<int64_t>(which) * a.r + rank) * cols + col, acc[b][e]);
+            }
+        }
+    }
+}
+
+// the parts, added in order: a thread per value, in the order of the results
+template <typename T>
+__global__ __launch_bounds__(kThreads) void adapter_join_kernel(SumArgs a) {
+    const int64_t per = static_cast<int64_t>(a.cols[0] + a.cols[1]) * a.r, all = per * a.n_adapters, na = static_cast<int64_t>(a.cols[0]) * a.r * a.n_adapters;
+    const int64_t i = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x;
+    if (i >= all) return;
+    const bool second = i >= na;
+    const int64_t j = second ? i - na : i;
+    int64_t which, col;
+    int rank;
+    if (second) {
+        rank = static_cast<int>(j % a.r);
+        which = j / a.r / a.cols[1];
+        col = a.cols[0] + j / a.r % a.cols[1];
+    } else {
+        col = j % a.cols[0];
+        which = j / a.cols[0] / a.r;
+        rank = static_cast<int>(j / a.cols[0] % a.r);
+    }
+    const int64_t step = static_cast<int64_t>(a.n_adapters) * (a.cols[0] + a.cols[1]) * a.t_row;
+    const float* p = a.part + (which * (a.cols[0] + a.cols[1]) + col) * a.t_row + rank;
+    float v = p[0];
+    for (int k = 1; k < a.parts; ++k) v += p[k * step];
+    store_f(static_cast<T*>(second ? a.out[1] : a.out[0]) + j, v);
+}
+
+template <typename T>
+__global__ __launch_bounds__(kThreads) void adapter_clear_kernel(T* p, int64_t n) {
+    for (int64_t i = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x; i < n; i += static_cast<int64_t>(gridDim.x) * kThreads) p[i] = T{};
+}
+
+// ---- sizes, workspaces, launches
+struct Sizes {
+    int32_t M, K, N, r, n;
+    int32_t Kp, Np;                              // as the products have them
+    int32_t t_row;
+    size_t es;
+    bool padded;
+    Sizes(int32_t m, int32_t k, int32_t nn, int32_t rank, int32_t adapters, int32_t dtype)
+        : M(m), K(k), N(nn), r(rank), n(adapters), Kp(k), Np(nn), t_row(up_to(rank, 16)), es(dtype == FREE_BF16 ? 2 : 4) {
+        const int32_t step = es == 2 ? 8 : 64;
+        padded = k % step != 0 || nn % step != 0;
+        if (padded) {
+            Kp = up_to(k, 64);
+            Np = up_to(nn, 64);
+        }
+    }
+    bool few() const { return ffn_rows_pay(M, K, N, padded); }
+    size_t thin_bytes() const { return static_cast<size_t>(M) * t_row * es; }
+};
+
+struct Carve {
+    char* base;
+    size_t at = 0;
+    template <typename T>
+    T* take(size_t bytes) {
+        T* p = reinterpret_cast<T*>(base + at);
+        at += (bytes + 255) / 256 * 256;
+        return p;
+    }
+};
+
+template <typename T>
+FfnProduct<T> forward_product(const Sizes& z, const T* x, const T* w, T* y) {
+    return FfnProduct<T>{FFN_ROWS, x, w, z.Kp, z.Kp, z.M, z.Np, z.Kp, y, z.Np};
+}
+
+template <typename T>
+FfnProduct<T> backward_product(const Sizes& z, const T* dout, const T* w, T* dx) {
+    return FfnProduct<T>{FFN_ROWS_BY_K, dout, w, z.Np, z.Kp, z.M, z.Kp, z.Np, dx, z.Kp};
+}
+
+template <typename T>
+struct ForwardSpace {
+    T *t, *x, *w, *y;
+    float* room;
+    size_t bytes;
+    ForwardSpace(const Sizes& z, char* base) {
+        Carve c{base};
+        t = c.take<T>(z.thin_bytes());
+        x = w = y = nullptr;
+        room = nullptr;
+        if (!z.few()) {
+            const FfnProduct<T> p = forward_product<T>(z, nullptr, nullptr, nullptr);
+            room = c.take<float>(ffn_products_part_bytes(&p, 1));
+            if (z.padded) {
+                x = c.take<T>(static_cast<size_t>(z.M) * z.Kp * sizeof(T));
+                w = c.take<T>(static_cast<size_t>(z.Np) * z.Kp * sizeof(T));
+                y = c.take<T>(static_cast<size_t>(z.M) * z.Np * sizeof(T));
+            }
+        }
+        bytes = c.at + 256;
+    }
+};
+
+// Parts of the rows of the weights' gradients: workgroups for the chip, at least 4 tiles of 64 rows each.
+struct SumPlan {
+    int32_t parts, part_tiles;
+    explicit SumPlan(const Sizes& z) {
+        const int64_t tiles = std::max<int64_t>(1, (static_cast<int64_t>(z.M) + kTileRows - 1) / kTileRows);
+        const int64_t groups = (static_cast<int64_t>(z.K + 127) / 128 + (z.N + 127) / 128) * z.n;
+        const int64_t want = std::max<int64_t>(1, std::min({(1024 + groups - 1) / groups, tiles / 4, static_cast<int64_t>(32)}));
+        part_tiles = static_cast<int32_t>((tiles + want - 1) / want);
+        parts = static_cast<int32_t>((tiles + part_tiles - 1) / part_tiles);
+    }
+};
+
+template <typename T>
+struct BackwardSpace {
+    T *u, *bt, *at, *x, *w, *dout, *dx;
+    float *room, *part;
+    size_t bytes;
+    BackwardSpace(const Sizes& z, char* base) {
+        Carve c{base};
+        u = c.take<T>(z.thin_bytes());
+        bt = c.take<T>(static_cast<size_t>(z.n) * z.t_row * z.Np * sizeof(T));
+        at = c.take<T>(static_cast<size_t>(z.n) * z.K * z.t_row * sizeof(T));
+        const SumPlan sum(z);
+        part = c.take<float>(sum.parts > 1 ? static_cast<size_t>(sum.parts) * z.n * (z.K + z.N) * z.t_row * sizeof(float) : 0);
+        const FfnProduct<T> p = backward_product<T>(z, nullptr, nullptr, nullptr);
+        room = c.take<float>(ffn_products_part_bytes(&p, 1));
+        x = w = dout = dx = nullptr;
+        if (z.padded) {
+            x = c.take<T>(static_cast<size_t>(z.M) * z.Kp * sizeof(T));
+            w = c.take<T>(static_cast<size_t>(z.Np) * z.Kp * sizeof(T));
+            dout = c.take<T>(static_cast<size_t>(z.M) * z.Np * sizeof(T));
+            dx = c.take<T>(static_cast<size_t>(z.M) * z.Kp * sizeof(T));
+        }
+        bytes = c.at + 256;
+    }
+};
+
+#define FREE_STEP(call)                     \
+    do {                                    \
+        const int32_t st_ = (call);         \
+        if (st_ != FREE_OK) return st_;     \
+    } while (0)
+
+// product and what it gets besides, into out [M, term.cols]; y: where the product's own rows go if they are wider
+template <typename T>
+int32_t product_with(FfnProduct<T> p, const AdapterTerm& term, bool padded, T* out, float* room, hipStream_t s) {
+    if constexpr (sizeof(T) == 2) {
+        p.adapters = &term;
+        FREE_STEP(launch_ffn_products(&p, 1, room, s));
+        return padded ? launch_fit<T>(p.out, p.M, p.N, out, p.M, term.cols, s) : FREE_OK;
+    } else {
+        FREE_STEP(launch_ffn_products(&p, 1, room, s));
+        const dim3 grid((term.cols + 127) / 128, std::min((p.M + 31) / 32, 65535));
+        hipLaunchKernelGGL(adapter_up_kernel, grid, dim3(kThreads), 0, s, p.out, p.ldo, term, p.M, out);
+        return launch_ok() ? FREE_OK : FREE_ERR_HIP;
+    }
+}
+
+template <typename T>
+int32_t forward_of(const Sizes& z, const AdapterArgs& a, char* ws, hipStream_t s) {
+    const ForwardSpace<T> w(z, ws);
+    T* const t = a.saved ? static_cast<T*>(a.saved) : w.t;
+    const T *x = static_cast<const T*>(a.x), *weight = static_cast<const T*>(a.w);
+    T* const out = static_cast<T*>(a.out);
+    FREE_STEP(launch_down<T>(DownArgs{x, a.a, a.adapter, a.scale, t, z.M, z.K, z.n, z.r, z.r, z.t_row, a.rows_per_sample}, s));
+    const AdapterTerm term{t, a.b, a.adapter, a.bias, z.n, z.r, z.t_row, z.r, z.N, a.rows_per_sample};
+    if (z.few()) return launch_adapter_rows<T>(x, weight, z.M, z.N, z.K, term, out, s);
+    if (z.padded) {
+        FREE_STEP(launch_fit<T>(x, z.M, z.K, w.x, z.M, z.Kp, s));
+        FREE_STEP(launch_fit<T>(weight, z.N, z.K, w.w, z.Np, z.Kp, s));
+        x = w.x;
+        weight = w.w;
+    }
+    return product_with<T>(forward_product<T>(z, x, weight, z.padded ? w.y : out), term, z.padded, out, w.room, s);
+}
+
+template <typename T, int RB>
+int32_t launch_sum(const SumArgs& a, hipStream_t s) {
+    const int64_t blocks = static_cast<int64_t>(a.tiles[0] + a.tiles[1]) * a.n_adapters * a.parts;
+    if (blocks > 0x7fffffff) return FREE_ERR_LIMIT;
+    const size_t lds = sizeof(T) == 2 ? 4 * kTileRows * 256 : 0;
+    auto kern = adapter_sum_kernel<T, RB>;
+    static LdsLimit limit;
+    if (!limit.allow(reinterpret_cast<const void*>(kern), lds)) return FREE_ERR_HIP;
+    hipLaunchKernelGGL(kern, dim3(static_cast<uint32_t>(blocks)), dim3(kThreads), lds, s, a);
+    if (!launch_ok()) return FREE_ERR_HIP;
+    if (a.parts == 1) return FREE_OK;
+    const int64_t values = static_cast<int64_t>(a.cols[0] + a.cols[1]) * a.r * a.n_adapters;
+    hipLaunchKernelGGL(adapter_join_kernel<T>, dim3(static_cast<uint32_t>((values + kThreads - 1) / kThreads)), dim3(kThreads), 0, s, a);
+    return launch_ok() ? FREE_OK : FREE_ERR_HIP;
+}
+
+template <typename T>
+int32_t clear(void* p, int64_t n, hipStream_t s) {
+    const int64_t blocks = std::min<int64_t>((n + kThreads - 1) / kThreads, 4096);
+    hipLaunchKernelGGL(adapter_clear_kernel<T>, dim3(static_cast<uint32_t>(blocks)), dim3(kThreads), 0, s, static_cast<T*>(p), n);
+    return launch_ok() ? FREE_OK : FREE_ERR_HIP;
+}
+
+template <typename T>
+int32_t backward_of(const Sizes& z, const AdapterArgs& a, char* ws, hipStream_t s) {
+    if (z.M == 0) {                                      // empty sums
+        FREE_STEP(clear<T>(a.da, static_cast<int64_t>(z.n) * z.r * z.K, s));
+        return clear<T>(a.db, static_cast<int64_t>(z.n) * z.r * z.N, s);
+    }
+    const BackwardSpace<T> w(z, ws);
+    const T *x = static_cast<const T*>(a.x), *weight = static_cast<const T*>(a.w), *dout = static_cast<const T*>(a.dout);
+    T* const dx = static_cast<T*>(a.dx);
+    if (z.padded) {
+        FREE_STEP(launch_fit<T>(x, z.M, z.K, w.x, z.M, z.Kp, s));
+        FREE_STEP(launch_fit<T>(weight, z.N, z.K, w.w, z.Np, z.Kp, s));
+        FREE_STEP(launch_fit<T>(dout, z.M, z.N, w.dout, z.M, z.Np, s));
+        x = w.x;
+        weight = w.w;
+        dout = w.dout;
+    }
+    const TurnJob jb{a.b, w.bt, z.N, z.r, z.Np, z.t_row}, ja{a.a, w.at, z.r, z.K, z.t_row, z.K};
+    const auto tiles = [](const TurnJob& j) { return static_cast<int64_t>((j.rows_to + 31) / 32) * ((j.cols_to + 31) / 32); };
+    hipLaunchKernelGGL(adapter_turn_kernel<T>, dim3(static_cast<uint32_t>(std::min<int64_t>(std::max(tiles(ja), tiles(jb)), 65536)), 1, 2 * z.n), dim3(kThreads), 0, s,
+                       jb, ja, z.n);
+    if (!launch_ok()) return FREE_ERR_HIP;
+    FREE_STEP(launch_down<T>(DownArgs{dout, w.bt, a.adapter, a.scale, w.u, z.M, z.Np, z.n, z.t_row, z.r, z.t_row, a.rows_per_sample}, s));
+    const AdapterTerm term{w.u, w.at, a.adapter, nullptr, z.n, z.t_row, z.t_row, z.t_row, z.K, a.rows_per_sample};
+    FREE_STEP(product_with<T>(backward_product<T>(z, dout, weight, z.padded ? w.dx : dx), term, z.padded, dx, w.room, s));
+    const SumPlan plan(z);
+    const SumArgs sum{{x, dout}, {w.u, a.saved}, {z.Kp, z.Np}, {z.K, z.N}, {(z.K + 127) / 128, (z.N + 127) / 128}, {a.da, a.db}, w.part, a.adapter, z.M, z.n, z.r,
+                      z.t_row, a.rows_per_sample, plan.parts, plan.part_tiles};
+    if (z.t_row <= 32) return launch_sum<T, 1>(sum, s);
+    if (z.t_row <= 64) return launch_sum<T, 2>(sum, s);
+    return launch_sum<T, 4>(sum, s);
+}
+
+}  // namespace
+
+// 32-bit byte offsets inside a tile of 256 rows, grids of less than 2^32 threads
+bool adapters_cover(int32_t M, int32_t K, int32_t N, int32_t r, int32_t n, int32_t dtype) {
+    if (K > 1 << 20 || N > 1 << 20 || r > 128 || n > 16384) return false;
+    const int64_t m = (static_cast<int64_t>(M) + 127) / 128, k = (K + 127) / 128, c = (N + 127) / 128;
+    return std::max(m * k, m * c) <= (dtype == FREE_FP32 ? 1 << 20 : 1 << 22) && (static_cast<int64_t>(K) + N) * r * n <= int64_t{1} << 36;
+}
+
+size_t adapters_saved_bytes(int32_t M, int32_t r, int32_t dtype) { return static_cast<size_t>(M) * up_to(r, 16) * (dtype == FREE_BF16 ? 2 : 4) + 256; }
+
+size_t adapters_workspace_bytes(int32_t M, int32_t K, int32_t N, int32_t r, int32_t n, int32_t dtype, bool backward) {
+    const Sizes z(M, K, N, r, n, dtype);
+    const size_t f = z.es == 2 ? ForwardSpace<bf16_t>(z, nullptr).bytes : ForwardSpace<float>(z, nullptr).bytes;
+    const size_t b = z.es == 2 ? BackwardSpace<bf16_t>(z, nullptr).bytes : BackwardSpace<float>(z, nullptr).bytes;
+    return (backward ? std::max(f, b) : f) / 256 * 256 + 256;
+}
+
+int32_t launch_adapters_forward(const AdapterArgs& a, int32_t M, int32_t K, int32_t N, int32_t r, int32_t n, int32_t dtype, void* ws, hipStream_t s) {
+    const Sizes z(M, K, N, r, n, dtype);
+    return dtype == FREE_BF16 ? forward_of<bf16_t>(z, a, static_cast<char*>(ws), s) : forward_of<float>(z, a, static_cast<char*>(ws), s);
+}
+
+int32_t launch_adapters_backward(const AdapterArgs& a, int32_t M, int32_t K, int32_t N, int32_t r, int32_t n, int32_t dtype, void* ws, hipStream_t s) {
+    const Sizes z(M, K, N, r, n, dtype);
+    return dtype == FREE_BF16 ? backward_of<bf16_t>(z, a, static_cast<char*>(ws), s) : backward_of<float>(z, a, static_cast<char*>(ws), s);
+}
+
+}  // namespace freemi

@@ -1,4 +1,5 @@
-// C ABI of the operators of conditioned blocks: checks of the arguments, then the launches of cross_attn.hip and cross_attn_grad.hip.
+// C ABI of the operators of conditioned blocks: checks of the arguments, then the launches of cross_attn.hip, cross_attn_grad.hip and
+// adapters.hip.
 #include <algorithm>
 #include <cmath>
 
@@ -140,6 +141,51 @@ int32_t free_op_cross_attention_backward(const void* dout, int64_t dout_stride, 
     a.dv = dv;
     a.dv_stride = dv_stride;
     return launch_cross_backward(a, dtype, workspace, static_cast<hipStream_t>(stream));
+}
+
+static int32_t check_adapters(int32_t M, int32_t K, int32_t N, int32_t r, int32_t n, int32_t rows_per_sample, int32_t dtype) {
+    if (!known(dtype)) return FREE_ERR_DTYPE;
+    if (M < 0 || K < 1 || N < 1 || r < 1 || n < 1 || rows_per_sample < 1) return FREE_ERR_SHAPE;
+    return adapters_cover(M, K, N, r, n, dtype) ? FREE_OK : FREE_ERR_LIMIT;
+}
+
+size_t free_linear_adapters_saved_bytes(int32_t M, int32_t r, int32_t dtype) {
+    return check_adapters(M, 1, 1, r, 1, 1, dtype) == FREE_OK ? adapters_saved_bytes(M, r, dtype) : 0;
+}
+
+size_t free_linear_adapters_workspace_bytes(int32_t M, int32_t K, int32_t N, int32_t r, int32_t n, int32_t dtype, int32_t backward) {
+    return check_adapters(M, K, N, r, n, 1, dtype) == FREE_OK ? adapters_workspace_bytes(M, K, N, r, n, dtype, backward != 0) : 0;
+}
+
+int32_t free_op_linear_adapters(const void* x, const void* W, const float* bias, const void* A, const void* B, const float* scale,
+                                const int32_t* adapter, int32_t rows_per_sample, int32_t M, int32_t K, int32_t N, int32_t r, int32_t n,
+                                int32_t dtype, void* out, void* saved, size_t saved_bytes, void* workspace, size_t ws_bytes, void* stream) {
+    FREE_CHECK(check_adapters(M, K, N, r, n, rows_per_sample, dtype));
+    if (M == 0) return FREE_OK;
+    if (!x || !W || !A || !B || !adapter || !out) return FREE_ERR_NULL;
+    if (!aligned(x, 16) || !aligned(W, 16) || !aligned(out, 16) || !element_aligned(A, dtype) || !element_aligned(B, dtype) || !aligned(bias, 4) ||
+        !aligned(scale, 4) || !aligned(adapter, 4))
+        return FREE_ERR_SHAPE;
+    if (saved && (!aligned(saved, 256) || saved_bytes < adapters_saved_bytes(M, r, dtype))) return FREE_ERR_WORKSPACE;
+    FREE_CHECK(check_workspace(workspace, ws_bytes, adapters_workspace_bytes(M, K, N, r, n, dtype, false)));
+    AdapterArgs a{x, W, A, B, bias, scale, adapter, rows_per_sample, saved, out, nullptr, nullptr, nullptr, nullptr};
+    return launch_adapters_forward(a, M, K, N, r, n, dtype, workspace, static_cast<hipStream_t>(stream));
+}
+
+int32_t free_op_linear_adapters_backward(const void* dout, const void* x, const void* W, const void* A, const void* B, const float* scale,
+                                         const int32_t* adapter, int32_t rows_per_sample, const void* saved, size_t saved_bytes, int32_t M,
+                                         int32_t K, int32_t N, int32_t r, int32_t n, int32_t dtype, void* dx, void* dA, void* dB,
+                                         void* workspace, size_t ws_bytes, void* stream) {
+    FREE_CHECK(check_adapters(M, K, N, r, n, rows_per_sample, dtype));
+    if (!W || !A || !B || !dA || !dB || (M > 0 && (!dout || !x || !dx || !adapter))) return FREE_ERR_NULL;
+    if (!aligned(dout, 16) || !aligned(x, 16) || !aligned(W, 16) || !aligned(dx, 16)) return FREE_ERR_SHAPE;
+    for (const void* p : {A, B, static_cast<const void*>(dA), static_cast<const void*>(dB)})
+        if (!element_aligned(p, dtype)) return FREE_ERR_SHAPE;
+    if (!aligned(scale, 4) || !aligned(adapter, 4)) return FREE_ERR_SHAPE;
+    if (M > 0 && (!saved || !aligned(saved, 256) || saved_bytes < adapters_saved_bytes(M, r, dtype))) return FREE_ERR_WORKSPACE;
+    FREE_CHECK(check_workspace(workspace, ws_bytes, adapters_workspace_bytes(M, K, N, r, n, dtype, true)));
+    AdapterArgs a{x, W, A, B, nullptr, scale, adapter, rows_per_sample, const_cast<void*>(saved), nullptr, dout, dx, dA, dB};
+    return launch_adapters_backward(a, M, K, N, r, n, dtype, workspace, static_cast<hipStream_t>(stream));
 }
 
 }  // extern "C"

@@ -52,14 +52,21 @@ __global__ __launch_bounds__(kThreads) void ffn_fit_kernel(const T* src, int32_t
     }
 }
 
+}  // namespace
+
 template <typename T>
-int32_t fit(const T* src, int32_t rows, int32_t cols, T* dst, int32_t rows_to, int32_t cols_to, hipStream_t s) {
+int32_t launch_fit(const T* src, int32_t rows, int32_t cols, T* dst, int32_t rows_to, int32_t cols_to, hipStream_t s) {
     using U = typename std::conditional<sizeof(T) == 2, uint16_t, uint32_t>::type;
     const dim3 grid((cols_to + kThreads * 16 / sizeof(T) - 1) / (kThreads * 16 / sizeof(T)), std::min(rows_to, 65535));
     hipLaunchKernelGGL(ffn_fit_kernel<U>, grid, dim3(kThreads), 0, s, reinterpret_cast<const U*>(src), rows, cols, reinterpret_cast<U*>(dst), rows_to,
                        cols_to);
     return launch_ok() ? FREE_OK : FREE_ERR_HIP;
 }
+
+template int32_t launch_fit(const bf16_t*, int32_t, int32_t, bf16_t*, int32_t, int32_t, hipStream_t);
+template int32_t launch_fit(const float*, int32_t, int32_t, float*, int32_t, int32_t, hipStream_t);
+
+namespace {
 
 int32_t up_to(int32_t v, int32_t step) { return (v + step - 1) / step * step; }
 
@@ -183,9 +190,9 @@ struct BackwardSpace {
 
 template <typename T>
 int32_t pad_weights(const Sizes& z, const T* w_in, const T* w_out, T* w_in_p, T* w_out_p, hipStream_t s) {
-    FREE_STEP(fit(w_in, z.F, z.D, w_in_p, z.Fp, z.Dp, s));
-    FREE_STEP(fit(w_in + static_cast<size_t>(z.F) * z.D, z.F, z.D, w_in_p + static_cast<size_t>(z.Fp) * z.Dp, z.Fp, z.Dp, s));
-    return fit(w_out, z.D, z.F, w_out_p, z.Dp, z.Fp, s);
+    FREE_STEP(launch_fit(w_in, z.F, z.D, w_in_p, z.Fp, z.Dp, s));
+    FREE_STEP(launch_fit(w_in + static_cast<size_t>(z.F) * z.D, z.F, z.D, w_in_p + static_cast<size_t>(z.Fp) * z.Dp, z.Fp, z.Dp, s));
+    return launch_fit(w_out, z.D, z.F, w_out_p, z.Dp, z.Fp, s);
 }
 
 template <typename T>
@@ -213,7 +220,7 @@ int32_t forward_of(const Sizes& z, const T* x, const T* w_in, const T* w_out, in
     }
     T* y = out;
     if (z.padded) {
-        FREE_STEP(fit(x, z.M, z.D, w.x, z.M, z.Dp, s));
+        FREE_STEP(launch_fit(x, z.M, z.D, w.x, z.M, z.Dp, s));
         FREE_STEP(pad_weights(z, w_in, w_out, w.w_in, w.w_out, s));
         x = w.x;
         w_in = w.w_in;
@@ -223,27 +230,27 @@ int32_t forward_of(const Sizes& z, const T* x, const T* w_in, const T* w_out, in
     const ForwardProducts<T> p(z, x, w_in, w_out, act, y, gu, h, saved != nullptr);
     FREE_STEP(launch_ffn_products(&p.up, 1, w.room, s));
     FREE_STEP(launch_ffn_products(&p.down, 1, w.room, s));
-    return z.padded ? fit(y, z.M, z.Dp, out, z.M, z.D, s) : FREE_OK;
+    return z.padded ? launch_fit(y, z.M, z.Dp, out, z.M, z.D, s) : FREE_OK;
 }
 
 template <typename T>
 int32_t backward_of(const Sizes& z, const T* dout, const T* x, const T* w_in, const T* w_out, char* saved, int32_t act, T* dx, T* dw_in, T* dw_out,
                     char* ws, hipStream_t s) {
     if (z.M == 0) {                                      // empty sums
-        FREE_STEP(fit(w_in, 0, 0, dw_in, 2 * z.F, z.D, s));
-        return fit(w_out, 0, 0, dw_out, z.D, z.F, s);
+        FREE_STEP(launch_fit(w_in, 0, 0, dw_in, 2 * z.F, z.D, s));
+        return launch_fit(w_out, 0, 0, dw_out, z.D, z.F, s);
     }
     const BackwardSpace<T> w(z, ws);
     const Saved<T> kept(z, saved);
     if (!z.padded) return products_backward(z, dout, x, w_in, w_out, kept, act, w, dx, dw_in, dw_out, s);
-    FREE_STEP(fit(x, z.M, z.D, w.x, z.M, z.Dp, s));
-    FREE_STEP(fit(dout, z.M, z.D, w.dy, z.M, z.Dp, s));
+    FREE_STEP(launch_fit(x, z.M, z.D, w.x, z.M, z.Dp, s));
+    FREE_STEP(launch_fit(dout, z.M, z.D, w.dy, z.M, z.Dp, s));
     FREE_STEP(pad_weights(z, w_in, w_out, w.w_in, w.w_out, s));
     FREE_STEP(products_backward(z, w.dy, w.x, w.w_in, w.w_out, kept, act, w, w.dx, w.dw_in, w.dw_out, s));
-    FREE_STEP(fit(w.dx, z.M, z.Dp, dx, z.M, z.D, s));
-    FREE_STEP(fit(w.dw_in, z.Fp, z.Dp, dw_in, z.F, z.D, s));
-    FREE_STEP(fit(w.dw_in + static_cast<size_t>(z.Fp) * z.Dp, z.Fp, z.Dp, dw_in + static_cast<size_t>(z.F) * z.D, z.F, z.D, s));
-    return fit(w.dw_out, z.Dp, z.Fp, dw_out, z.D, z.F, s);
+    FREE_STEP(launch_fit(w.dx, z.M, z.Dp, dx, z.M, z.D, s));
+    FREE_STEP(launch_fit(w.dw_in, z.Fp, z.Dp, dw_in, z.F, z.D, s));
+    FREE_STEP(launch_fit(w.dw_in + static_cast<size_t>(z.Fp) * z.Dp, z.Fp, z.Dp, dw_in + static_cast<size_t>(z.F) * z.D, z.F, z.D, s));
+    return launch_fit(w.dw_out, z.Dp, z.Fp, dw_out, z.D, z.F, s);
 }
 
 }  // namespace

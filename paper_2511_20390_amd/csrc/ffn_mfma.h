@@ -18,6 +18,21 @@ enum FfnKind {
     FFN_PART
 };
 
+// What the rows of a product with adapters get besides: bias[n] + sum over ranks of t[m, rank] b_a[n, rank], a = adapter[m / rows_per_sample]
+// (none of n_adapters: the bias alone).  t: rows of t_row values, zeros past r, 16-byte aligned; b: [adapter][cols][b_row], any alignment.
+struct AdapterTerm {
+    const void *t, *b;
+    const int32_t* adapter;
+    const float* bias;               // nullable
+    int32_t n_adapters, r, t_row, b_row, cols, rows_per_sample;
+#if defined(__HIPCC__)
+    __device__ __forceinline__ int of_row(int m) const {
+        const int a = adapter[m / rows_per_sample];
+        return a >= 0 && a < n_adapters ? a : -1;
+    }
+#endif
+};
+
 template <typename T>                // bf16_t or float
 struct FfnProduct {
     FfnKind kind;
@@ -34,6 +49,7 @@ struct FfnProduct {
     // fold are none
     int32_t fold = 0, fold_to = 0;
     int32_t cols() const { return hidden > 0 ? hidden : N; }
+    const AdapterTerm* adapters = nullptr;                       // FFN_ROWS, FFN_ROWS_BY_K of bf16
     bool gated() const { return kind == FFN_GATE || kind == FFN_GATE_KEEP; }
 };
 
@@ -46,6 +62,12 @@ int32_t launch_ffn_products(const FfnProduct<float>* p, int n, float* part, hipS
 
 // ffn_rows.hip: y of up to 32 token rows, any D and F, in two launches; h: room for [M, F].  ffn_rows_pay: where that is the faster way.
 bool ffn_rows_pay(int32_t M, int32_t D, int32_t F, bool tiles_padded);
+// the rows of x w^T with adapters likewise
+template <typename T>
+int32_t launch_adapter_rows(const T* x, const T* w, int32_t M, int32_t N, int32_t K, const AdapterTerm& adapters, T* out, hipStream_t s);
+// ffn.hip: dst [rows_to, cols_to] = src [rows, cols], cropped or filled with zeros
+template <typename T>
+int32_t launch_fit(const T* src, int32_t rows, int32_t cols, T* dst, int32_t rows_to, int32_t cols_to, hipStream_t s);
 template <typename T>
 int32_t launch_ffn_rows(const T* x, const T* w_in, const T* w_out, int32_t M, int32_t D, int32_t F, int32_t act, T* h, T* out, hipStream_t s);
 

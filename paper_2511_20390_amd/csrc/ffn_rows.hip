@@ -17,13 +17,11 @@
 #include <type_traits>
 
 #include "ffn_mfma.h"
-#include "gemm_tile.h"
+#include "row_pieces.h"
 
 namespace freemi {
 
 namespace {
-
-typedef float f32x4a_t __attribute__((ext_vector_type(4)));
 
 constexpr int kWaves = 8;
 
@@ -31,40 +29,17 @@ struct RowArgs {
     const void *x, *w;
     void* out;
     int32_t M, N, K, act;
+    AdapterTerm adapters{};          // kAdapt
 };
-
-// 16 bytes; left: values of the row from p on, maybe none
-template <typename T>
-__device__ __forceinline__ void load_piece(const T* p, int left, u32x4_t& v, bool whole) {
-    constexpr int E = 16 / sizeof(T);
-    if (whole || left >= E) {
-        __builtin_memcpy(&v, p, 16);
-        return;
-    }
-    T t[E];
-#pragma unroll
-    for (int e = 0; e < E; ++e) t[e] = e < left ? p[e] : T{};
-    __builtin_memcpy(&v, t, 16);
-}
-
-template <typename T>
-__device__ __forceinline__ void multiply(const u32x4_t& w, const u32x4_t& x, f32x4a_t& acc) {
-    if constexpr (sizeof(T) == 2) {
-        acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, w), __builtin_bit_cast(bf16x8_t, x), acc, 0, 0, 0);
-    } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(w[e]), __uint_as_float(x[e]), acc, 0, 0, 0);
-    }
-}
 
 __device__ __forceinline__ float gate_of(float g, int act) {
     if (act == FREE_ACT_SILU) return g / (1.0f + expf(-g));
     return 0.5f * g * (1.0f + tanhf(0.7978845608028654f * (g + 0.044715f * g * g * g)));
 }
 
-// kEdge: rows' last steps may not be whole
-template <typename T, int R, int MT, bool kGated, bool kEdge>
+// kEdge: rows' last steps may not be whole.  kAdapt: a bias and the rows' adapters are added, summed before the weights arrive: a thread has
+// at most two values.
+template <typename T, int R, int MT, bool kGated, bool kEdge, bool kAdapt>
 __global__ __launch_bounds__(kWaves * 64) void ffn_rows_kernel(RowArgs a) {
     constexpr int NB = kGated ? 2 : 1;                           // weight matrices
     constexpr int P = 2, H = R / 8;                              // pieces of a step for 16 lanes; of them in one lane
@@ -83,6 +58,15 @@ __global__ __launch_bounds__(kWaves * 64) void ffn_rows_kernel(RowArgs a) {
     for (int t = 0; t < MT; ++t) {
         const int m = t * 16 + r16;
         x[t] = static_cast<const T*>(a.x) + static_cast<int64_t>(m < a.M ? m : a.M - 1) * a.K + x_at;
+    }
+    constexpr int kValues = (MT * 16 * R + kWaves * 64 - 1) / (kWaves * 64);
+    [[maybe_unused]] float extra[kValues];
+    if constexpr (kAdapt) {
+#pragma unroll
+        for (int c = 0; c < kValues; ++c) {
+            const int i = threadIdx.x + c * kWaves * 64, m = i / (16 * R) * 16 + i / R % 16, col = n0 + i % R;
+            extra[c] = i < MT * 16 * R && m < a.M && col < a.N ? adapter_value<T>(a.adapters, m, col) : 0.f;
+        }
     }
     f32x4a_t acc[NB][MT];
 #pragma unroll
@@ -134,7 +118,10 @@ __global__ __launch_bounds__(kWaves * 64) void ffn_rows_kernel(RowArgs a) {
         for (int t = 0; t < MT; ++t) red[wave][b * MT + t][lane] = acc[b][t];
     __syncthreads();
     // value i of a tile: token i / R, weight row i % R; it stands in lane token + 16 (row / 4), register row % 4
-    for (int i = threadIdx.x; i < MT * 16 * R; i += kWaves * 64) {
+#pragma unroll
+    for (int c = 0; c < kValues; ++c) {
+        const int i = threadIdx.x + c * kWaves * 64;
+        if (i >= MT * 16 * R) break;
         const int t = i / (16 * R), token = i / R % 16, row = i % R, from = token + 16 * (row >> 2);
         const int m = t * 16 + token;
         if (m >= a.M || n0 + row >= a.N) continue;
@@ -146,24 +133,25 @@ __global__ __launch_bounds__(kWaves * 64) void ffn_rows_kernel(RowArgs a) {
             for (int k = 1; k < kWaves; ++k) v[b] += red[k][b * MT + t][from][row & 3];
         }
         if constexpr (kGated) v[0] = gate_of(v[0], a.act) * v[1];
+        if constexpr (kAdapt) v[0] += extra[c];
         store_f(static_cast<T*>(a.out) + static_cast<int64_t>(m) * a.N + n0 + row, v[0]);
     }
 }
 
-template <typename T, int R, int MT, bool kGated>
+template <typename T, int R, int MT, bool kGated, bool kAdapt>
 int32_t launch_edge(const RowArgs& a, hipStream_t s) {
     constexpr int kStep = 128 / sizeof(T);
     const dim3 grid((a.N + R - 1) / R), block(kWaves * 64);
-    if (a.K % kStep == 0) hipLaunchKernelGGL((ffn_rows_kernel<T, R, MT, kGated, false>), grid, block, 0, s, a);
-    else hipLaunchKernelGGL((ffn_rows_kernel<T, R, MT, kGated, true>), grid, block, 0, s, a);
+    if (a.K % kStep == 0) hipLaunchKernelGGL((ffn_rows_kernel<T, R, MT, kGated, false, kAdapt>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((ffn_rows_kernel<T, R, MT, kGated, true, kAdapt>), grid, block, 0, s, a);
     return launch_ok() ? FREE_OK : FREE_ERR_HIP;
 }
 
-template <typename T, bool kGated>
+template <typename T, bool kGated, bool kAdapt = false>
 int32_t launch_rows(const RowArgs& a, hipStream_t s) {
     // 8 weight rows where groups of 16 would leave compute units without one, and for gate and up of few tokens
-    if (a.N < 16 * 256 || (kGated && a.M <= 8)) return a.M <= 16 ? launch_edge<T, 8, 1, kGated>(a, s) : launch_edge<T, 8, 2, kGated>(a, s);
-    return a.M <= 16 ? launch_edge<T, 16, 1, kGated>(a, s) : launch_edge<T, 16, 2, kGated>(a, s);
+    if (a.N < 16 * 256 || (kGated && a.M <= 8)) return a.M <= 16 ? launch_edge<T, 8, 1, kGated, kAdapt>(a, s) : launch_edge<T, 8, 2, kGated, kAdapt>(a, s);
+    return a.M <= 16 ? launch_edge<T, 16, 1, kGated, kAdapt>(a, s) : launch_edge<T, 16, 2, kGated, kAdapt>(a, s);
 }
 
 }  // namespace
@@ -181,6 +169,13 @@ bool ffn_rows_pay(int32_t M, int32_t D, int32_t F, bool tiles_padded) {
     return M <= 16 || (M <= 32 && (tiles_padded || static_cast<int64_t>(D) * F <= 1 << 22));
 }
 
+template <typename T>
+int32_t launch_adapter_rows(const T* x, const T* w, int32_t M, int32_t N, int32_t K, const AdapterTerm& adapters, T* out, hipStream_t s) {
+    return launch_rows<T, false, true>(RowArgs{x, w, out, M, N, K, 0, adapters}, s);
+}
+
+template int32_t launch_adapter_rows(const bf16_t*, const bf16_t*, int32_t, int32_t, int32_t, const AdapterTerm&, bf16_t*, hipStream_t);
+template int32_t launch_adapter_rows(const float*, const float*, int32_t, int32_t, int32_t, const AdapterTerm&, float*, hipStream_t);
 template int32_t launch_ffn_rows(const bf16_t*, const bf16_t*, const bf16_t*, int32_t, int32_t, int32_t, int32_t, bf16_t*, bf16_t*, hipStream_t);
 template int32_t launch_ffn_rows(const float*, const float*, const float*, int32_t, int32_t, int32_t, int32_t, float*, float*, hipStream_t);
 

@@ -368,4 +368,21 @@ int32_t launch_ffn_forward(const void* x, const void* w_in, const void* w_out, i
 int32_t launch_ffn_backward(const void* dout, const void* x, const void* w_in, const void* w_out, const void* saved, int32_t M, int32_t D,
                             int32_t F, int32_t dtype, int32_t act, void* dx, void* dw_in, void* dw_out, void* ws, hipStream_t s);
 
+// ---- a projection with the adapters of many requests (adapters.hip) ----------------------------------------------------------
+struct AdapterArgs {
+    const void *x, *w, *a, *b;                   // [M, K], [N, K], [n, r, K], [n, N, r]
+    const float *bias, *scale;                   // nullable: [N], [n]
+    const int32_t* adapter;                      // [samples]
+    int32_t rows_per_sample;
+    void* saved;                                 // t; the forward pass: nullable
+    void* out;
+    const void* dout;
+    void *dx, *da, *db;
+};
+bool adapters_cover(int32_t M, int32_t K, int32_t N, int32_t r, int32_t n, int32_t dtype);
+size_t adapters_saved_bytes(int32_t M, int32_t r, int32_t dtype);
+size_t adapters_workspace_bytes(int32_t M, int32_t K, int32_t N, int32_t r, int32_t n, int32_t dtype, bool backward);
+int32_t launch_adapters_forward(const AdapterArgs& a, int32_t M, int32_t K, int32_t N, int32_t r, int32_t n, int32_t dtype, void* ws, hipStream_t s);
+int32_t launch_adapters_backward(const AdapterArgs& a, int32_t M, int32_t K, int32_t N, int32_t r, int32_t n, int32_t dtype, void* ws, hipStream_t s);
+
 }  // namespace freemi

@@ -72,3 +72,39 @@ def keys_that_count(B, Nk, key_len, key_mask, device):
     if key_mask is not None:
         keys &= key_mask != 0
     return keys
+
+
+def adapters_reference(x, w, bias, a, b, adapter, scale, rows, dout=None):
+    """[(out, bound)], and with dout also of dx, dA, dB, without the rounding to the results' type."""
+    h = half_step(x.dtype) if x.dtype != torch.float32 else U
+    x, w, a, b = x.double(), w.double(), a.double(), b.double()
+    M, K = x.shape
+    n, r, N = a.shape[0], a.shape[1], w.shape[0]
+    s = torch.ones(n, dtype=torch.float64, device=x.device) if scale is None else scale.double()
+    which = adapter.long()[torch.arange(M, device=x.device) // rows]
+    total = lambda k: (k + 16) * U
+    out, e_out = x @ w.T, total(K + r) * (x.abs() @ w.abs().T)
+    if bias is not None:
+        out, e_out = out + bias.double(), e_out + total(K + r) * bias.double().abs()
+    if dout is not None:
+        g = dout.double()
+        dx, e_dx = g @ w, total(N + r) * (g.abs() @ w.abs())
+        da, db, e_da, e_db = torch.zeros_like(a), torch.zeros_like(b), torch.zeros_like(a), torch.zeros_like(b)
+    for i in range(n):
+        at = (which == i).nonzero()[:, 0]
+        if at.numel() == 0:
+            continue
+        # a sum, a factor, and the rounding to the operand's type
+        thin = lambda v, m, k: (s[i] * (v @ m), s[i].abs() * (total(k) + h) * (1 + h) * (v.abs() @ m.abs()) + 2.0 ** -126)
+        t, e_t = thin(x[at], a[i].T, K)
+        out[at] += t @ b[i].T
+        e_out[at] += (e_t + total(K + r) * (t.abs() + e_t)) @ b[i].abs().T
+        if dout is None:
+            continue
+        u, e_u = thin(g[at], b[i], N)
+        dx[at] += u @ a[i]
+        e_dx[at] += (e_u + total(N + r) * (u.abs() + e_u)) @ a[i].abs()
+        m = at.numel()
+        da[i], e_da[i] = u.T @ x[at], (e_u + total(m + 64) * (u.abs() + e_u)).T @ x[at].abs()
+        db[i], e_db[i] = g[at].T @ t, g[at].abs().T @ (e_t + total(m + 64) * (t.abs() + e_t))
+    return [(out, e_out)] if dout is None else [(out, e_out), (dx, e_dx), (da, e_da), (db, e_db)]

@@ -67,3 +67,48 @@ def test_cross_attention_workspaces(lib):
                 assert n <= 4096 + 4 * B * (64 * (Nq * heads + 2 * Nk * kv) * (dh + 2) + 8192 * dh)
     with pytest.raises(b.FreeError):
         b.cross_attention_workspace_bytes(1 << 32, 1, 1, 1, 1, 8, "bf16")
+
+
+def _adapt(lib, x=ONE, w=ONE, bias=ONE, a=ONE, bb=ONE, scale=ONE, which=ONE, rows=4, M=8, K=64, N=64, r=8, n=2, t=1, out=ONE, saved=None, sb=0, ws=ONE, bytes_=BIG):
+    return lib.free_op_linear_adapters(x, w, bias, a, bb, scale, which, rows, M, K, N, r, n, t, out, saved, sb, ws, bytes_, None)
+
+
+def _adapt_back(lib, g=ONE, x=ONE, w=ONE, a=ONE, bb=ONE, scale=ONE, which=ONE, rows=4, M=8, K=64, N=64, r=8, n=2, t=1, dx=ONE, da=ONE, db=ONE, saved=ONE, sb=BIG,
+                ws=ONE, bytes_=BIG):
+    return lib.free_op_linear_adapters_backward(g, x, w, a, bb, scale, which, rows, saved, sb, M, K, N, r, n, t, dx, da, db, ws, bytes_, None)
+
+
+@pytest.mark.parametrize("call", [_adapt, _adapt_back])
+def test_linear_adapters_refusals(lib, call):
+    back = call is _adapt_back
+    for name in ("x", "w", "a", "bb", "which") + (("g", "dx", "da", "db") if back else ("out",)):
+        assert call(lib, **{name: None}) == b.FREE_ERR_NULL, name
+        assert call(lib, **{name: ODD}) == b.FREE_ERR_SHAPE, name
+    for name in ("x", "w") + (("g", "dx") if back else ("out",)):
+        assert call(lib, **{name: C.c_void_p(4104)}) == b.FREE_ERR_SHAPE, name
+    assert call(lib, scale=ODD) == b.FREE_ERR_SHAPE
+    if not back:
+        assert call(lib, bias=ODD) == b.FREE_ERR_SHAPE
+    assert call(lib, t=2) == call(lib, t=-1) == b.FREE_ERR_DTYPE
+    assert call(lib, M=-1) == call(lib, K=0) == call(lib, N=0) == call(lib, r=0) == call(lib, n=0) == call(lib, rows=0) == b.FREE_ERR_SHAPE
+    assert call(lib, r=129) == call(lib, n=16385) == call(lib, K=(1 << 20) + 1) == call(lib, N=(1 << 20) + 1) == b.FREE_ERR_LIMIT
+    assert call(lib, M=2**31 - 1, K=1 << 20) == call(lib, M=2**31 - 1, N=1 << 20) == call(lib, K=1 << 20, N=1 << 20, r=128, n=16384) == b.FREE_ERR_LIMIT
+    assert call(lib, ws=None) == call(lib, ws=C.c_void_p(4100)) == call(lib, bytes_=0) == b.FREE_ERR_WORKSPACE
+    assert call(lib, saved=C.c_void_p(4100), sb=BIG) == call(lib, saved=ONE, sb=100) == b.FREE_ERR_WORKSPACE
+    if back:
+        assert call(lib, saved=None) == b.FREE_ERR_WORKSPACE
+    else:
+        assert call(lib, M=0, x=None, w=None, out=None, ws=None) == b.FREE_OK
+
+
+def test_linear_adapters_workspaces(lib):
+    size = lib.free_linear_adapters_workspace_bytes
+    assert size(8, 64, 64, 129, 2, 1, 0) == size(-1, 64, 64, 8, 2, 1, 0) == size(8, 0, 64, 8, 2, 1, 1) == size(8, 64, 64, 8, 2, 7, 1) == 0
+    assert lib.free_linear_adapters_saved_bytes(8, 129, 1) == lib.free_linear_adapters_saved_bytes(-1, 8, 1) == 0
+    for t in (0, 1):
+        for back in (0, 1):
+            for M, K, N, r, n in [(0, 64, 64, 8, 2), (1, 1, 1, 1, 1), (8, 4096, 4096, 16, 8), (12288, 1152, 1152, 16, 4), (1000, 1001, 77, 33, 2)]:
+                got = size(M, K, N, r, n, t, back)
+                assert got > 0 and got % 256 == 0
+    with pytest.raises(b.FreeError):
+        b.linear_adapters_workspace_bytes(1 << 32, 64, 64, 8, 2, "bf16")
