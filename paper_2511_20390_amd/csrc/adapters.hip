@@ -6,14 +6,15 @@
 // adapters of these rows one after the other, with the other rows masked.
 //  * t and u: x (dout) is read once, 16 or 32 rows per workgroup whose wavefronts share K; rounded to the type of the product they are
 //    operands of, like the hidden values of the gated block.
-//  * out and dx: the products of ffn_mfma.hip, whose sums begin with bias and adapter (bf16), or a second pass over the result (fp32, where
-//    the product takes ten times as long); up to 32 rows ffn_rows.hip.
+//  * out and dx: the kernels and tiles of the linear layers, whose sums begin with the adapters' (bf16, adapter_term.h), or a second pass over
+//    the result (fp32, where the product takes ten times as long); up to 32 rows of out ffn_rows.hip.
 //  * dA and dB: 128 columns of x or dout by all ranks per workgroup, over the rows of one adapter, in parts that a second launch adds in
 //    order.  Rows of other adapters are not read.
-// For the gradient B and A are needed the other way round ([rank][N], [K][rank]): copies of that layout go into the workspace, ranks filled up
-// with zeros; they are r (N + K) values per adapter against the N K of the weights.
+// For the gradient W, B and A are needed the other way round ([K][N], [rank][N], [K][rank]): copies of that layout go into the workspace, filled
+// up with zeros to whole slices. 
 #include <algorithm>
 
+#include "adapter_term.h"
 #include "cross_attn.h"
 #include "ffn_mfma.h"
 #include "free_internal.h"
@@ -37,15 +38,20 @@ struct DownArgs {
     const float* scale;                          // nullable
     void* out;                                   // [M][t_row], zeros from r on
     int32_t M, K, n_adapters, w_rows, r, t_row, rows_per_sample;
+    float* zeros = nullptr;                      // nullable: zero_n values to clear, a bias for the product behind
+    int32_t zero_n = 0;
 };
 
 // Workgroup (block of 16 MT rows, j, 16 RT ranks): the j-th adapter of the block's rows, in the order they come
 template <typename T, int MT, int RT, bool kEdge>
 __global__ __launch_bounds__(kDownWaves * 64) void adapter_down_kernel(DownArgs a) {
-    constexpr int P = 2, E = 16 / sizeof(T), kStep = 4 * P * E, U = MT * RT > 2 ? 2 : 4;
+    constexpr int P = 2, E = 16 / sizeof(T), kStep = 4 * P * E, U = MT * RT == 1 ? 8 : MT * RT == 2 ? 4 : 2;      // steps in flight
     __shared__ f32x4a_t red[kDownWaves][RT * MT][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int m0 = blockIdx.x * 16 * MT, rank0 = blockIdx.z * 16 * RT, quad = lane >> 4, r16 = lane & 15;
+    // blocks of rows next to each other on one XCD: its L2 has the adapters of few requests to hold
+    const int m0 = xcd_tile(blockIdx.x, gridDim.x) * 16 * MT, rank0 = blockIdx.z * 16 * RT, quad = lane >> 4, r16 = lane & 15;
+    if (a.zeros && blockIdx.y == 0 && blockIdx.z == 0)
+        for (int i = blockIdx.x * kDownWaves * 64 + threadIdx.x; i < a.zero_n; i += gridDim.x * kDownWaves * 64) a.zeros[i] = 0.f;
     int of = -1;                                 // lane: row m0 + lane's adapter
     if (lane < 16 * MT && m0 + lane < a.M) {
         const int id = a.adapter[(m0 + lane) / a.rows_per_sample];
@@ -60,7 +66,8 @@ __global__ __launch_bounds__(kDownWaves * 64) void adapter_down_kernel(DownArgs 
     }
     if (left == 0) return;
     const uint64_t mine = __ballot(of == which);
-    const int at = quad * P * E;
+    const float scale = a.scale ? a.scale[which] : 1.0f;
+    const int at = quad * E;                     // of a step's 128 bytes: piece p is 64 p bytes on, so that 4 lanes read 64 bytes
     const T* w[RT];
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
@@ -91,11 +98,11 @@ __global__ __launch_bounds__(kDownWaves * 64) void adapter_down_kernel(DownArgs 
 #pragma unroll
             for (int t = 0; t < MT; ++t)
 #pragma unroll
-                for (int p = 0; p < P; ++p) load_piece(x[t] + k + p * E, rest - p * E, xv[u][t][p], whole);
+                for (int p = 0; p < P; ++p) load_piece(x[t] + k + p * 4 * E, rest - p * 4 * E, xv[u][t][p], whole);
 #pragma unroll
             for (int b = 0; b < RT; ++b)
 #pragma unroll
-                for (int p = 0; p < P; ++p) load_piece(w[b] + k + p * E, rest - p * E, wv[u][b][p], whole);
+                for (int p = 0; p < P; ++p) load_piece(w[b] + k + p * 4 * E, rest - p * 4 * E, wv[u][b][p], whole);
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -113,7 +120,6 @@ __global__ __launch_bounds__(kDownWaves * 64) void adapter_down_kernel(DownArgs 
 #pragma unroll
         for (int t = 0; t < MT; ++t) red[wave][b * MT + t][lane] = acc[b][t];
     __syncthreads();
-    const float scale = a.scale ? a.scale[which] : 1.0f;
     // value i: token i / (16 RT), rank i % (16 RT); it stands in lane token + 16 (rank / 4), register rank % 4
     for (int i = threadIdx.x; i < MT * 16 * RT * 16; i += kDownWaves * 64) {
         const int row = i / (16 * RT), c = i % (16 * RT), t = row / 16, b = c / 16, from = row % 16 + 16 * (c % 16 / 4);
@@ -147,45 +153,63 @@ int32_t launch_down_ranks(const DownArgs& a, hipStream_t s) {
 
 template <typename T>
 int32_t launch_down(const DownArgs& a, hipStream_t s) {
-    return a.M <= 16 * 256 ? launch_down_ranks<T, 1>(a, s) : launch_down_ranks<T, 2>(a, s);
+    return a.M <= 16 * 128 ? launch_down_ranks<T, 1>(a, s) : launch_down_ranks<T, 2>(a, s);
 }
 
-// ---- A and B the other way round
+// ---- W, B and A the other way round
 struct TurnJob {
     const void* src;                             // [n][rows][cols]
-    void* dst;                                   // [n][cols_to][rows_to]
-    int32_t rows, cols, rows_to, cols_to;
+    void* dst;                                   // [n][cols_to][rows_to], zeros past cols and rows
+    int32_t rows, cols, rows_to, cols_to, n;
+    int32_t tiles;                               // of 64 x 64, of all n
+};
+struct TurnJobs {
+    TurnJob job[3];
 };
 
+// A tile of 64 x 64 values through LDS, 16 bytes per thread in and out, at any address
 template <typename T>
-__global__ __launch_bounds__(kThreads) void adapter_turn_kernel(TurnJob j0, TurnJob j1, int32_t n) {
-    __shared__ T tile[32][33];
-    const bool second = static_cast<int>(blockIdx.z) >= n;
-    const TurnJob& j = second ? j1 : j0;
-    const int which = second ? blockIdx.z - n : blockIdx.z;
-    const int tiles_r = (j.rows_to + 31) / 32, tiles_c = (j.cols_to + 31) / 32;
-    const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5;
+__global__ __launch_bounds__(kThreads) void adapter_turn_kernel(TurnJobs jobs) {
+    constexpr int E = 16 / sizeof(T), C = 64 / E;
+    __shared__ T tile[64][64 + 2];
+    int id = blockIdx.x, k = 0;
+    while (k < 2 && id >= jobs.job[k].tiles) id -= jobs.job[k++].tiles;
+    const TurnJob& j = jobs.job[k];
+    const int tiles_r = (j.rows_to + 63) / 64, tiles_c = (j.cols_to + 63) / 64, which = id / (tiles_r * tiles_c), at = id % (tiles_r * tiles_c);
+    const int r0 = at / tiles_c * 64, c0 = at % tiles_c * 64;
     const T* const src = static_cast<const T*>(j.src) + static_cast<int64_t>(which) * j.rows * j.cols;
     T* const dst = static_cast<T*>(j.dst) + static_cast<int64_t>(which) * j.rows_to * j.cols_to;
-    for (int id = blockIdx.x; id < tiles_r * tiles_c; id += gridDim.x) {
-        const int r0 = id / tiles_c * 32, c0 = id % tiles_c * 32;
 #pragma unroll
-        for (int i = 0; i < 32; i += 8) {
-            const int r = r0 + ty + i, c = c0 + tx;
-            tile[ty + i][tx] = r < j.rows && c < j.cols ? src[static_cast<int64_t>(r) * j.cols + c] : T{};
-        }
-        __syncthreads();
+    for (int i = threadIdx.x; i < 64 * C; i += kThreads) {
+        const int r = r0 + i / C, c = c0 + i % C * E;
+        u32x4_t v = {0, 0, 0, 0};
+        if (r < j.rows) load_piece(src + static_cast<int64_t>(r) * j.cols + c, j.cols - c, v, false);
+        T t[E];
+        __builtin_memcpy(t, &v, 16);
 #pragma unroll
-        for (int i = 0; i < 32; i += 8) {
-            const int c = c0 + ty + i, r = r0 + tx;
-            if (c < j.cols_to && r < j.rows_to) dst[static_cast<int64_t>(c) * j.rows_to + r] = tile[tx][ty + i];
+        for (int e = 0; e < E; ++e) tile[i / C][i % C * E + e] = t[e];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = threadIdx.x; i < 64 * C; i += kThreads) {
+        const int c = c0 + i / C, r = r0 + i % C * E;
+        if (c >= j.cols_to || r >= j.rows_to) continue;
+        T t[E];
+#pragma unroll
+        for (int e = 0; e < E; ++e) t[e] = tile[i % C * E + e][i / C];
+        T* const to = dst + static_cast<int64_t>(c) * j.rows_to + r;
+        if (r + E <= j.rows_to) {
+            __builtin_memcpy(to, t, 16);
+        } else {
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                if (r + e < j.rows_to) to[e] = t[e];
         }
-        __syncthreads();
     }
 }
 
-// ---- fp32: out = y + bias + t B^T; a wavefront has 32 x 32 values
-__global__ __launch_bounds__(kThreads) void adapter_up_kernel(const float* y, int64_t ldy, AdapterTerm ad, int32_t M, float* out) {
+// ---- fp32: out += t B^T; a wavefront has 32 x 32 values
+__global__ __launch_bounds__(kThreads) void adapter_up_kernel(AdapterTerm ad, int32_t M, float* out) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l32 = lane & 31, g = lane >> 5;
     const int n0 = (blockIdx.x * 4 + wave) * 32, N = ad.cols;
     if (n0 >= N) return;
@@ -196,7 +220,7 @@ __global__ __launch_bounds__(kThreads) void adapter_up_kernel(const float* y, in
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
             const int n = n0 + 8 * (e >> 2) + 4 * g + (e & 3);
-            acc[e] = m < M && n < N ? y[m * ldy + n] + (ad.bias ? ad.bias[n] : 0.f) : 0.f;
+            acc[e] = m < M && n < N ? out[static_cast<int64_t>(m) * N + n] : 0.f;
         }
         int of = m < M ? ad.of_row(m) : -1;
         for (uint64_t left = __ballot(of >= 0); left != 0; left = __ballot(of >= 0)) {
@@ -236,19 +260,28 @@ struct SumArgs {
     int32_t cols[2];                             // K, N
     int32_t tiles[2];                            // of 128 columns
     void* out[2];                                // dA [n][r][K], dB [n][N][r]
-    float* part;                                 // parts > 1: [part][adapter][K + N][t_row]
+    float* part;                                 // parts > 1: per part the values of both results, in their order
     const int32_t* adapter;
     int32_t M, n_adapters, r, t_row, rows_per_sample, parts, part_tiles;
 };
 
-__device__ __forceinline__ int turned_chunk(int row, int c) { return c ^ ((row & 3) << 2 | (row >> 2 & 3)); }     // 256-byte rows: Tile::at of cross_attn_grad.hip
+// Where chunk c of a row is, so that neither the stores nor the transposing reads of 4 rows x 64 bytes share banks.  Rows of 256, 128 or 64
+// bytes (whose four rows are next to each other).
+template <int kPitch>
+__device__ __forceinline__ int chunk_place(int row, int c) {
+    const int turn = kPitch == 256 ? (row & 3) << 2 | (row >> 2 & 3) : kPitch == 128 ? (row >> 1 & 1) << 2 | (row >> 2 & 3) : 0;
+    return row * kPitch + ((c ^ turn) << 4);
+}
+
+// bytes of a stage of adapter_sum_kernel: tiles of 64 rows of 128 columns, and of the ranks
+constexpr int sum_stage(int rb) { return kTileRows * (256 + rb * 64); }
 
 // RB: blocks of 32 ranks.  Workgroup (columns, adapter, part): a wavefront has 32 columns.
 template <typename T, int RB>
 __global__ __launch_bounds__(kThreads) void adapter_sum_kernel(SumArgs a) {
-    constexpr int kPitch = 256, kLoads = kTileRows * 16 / kThreads;
+    constexpr int kThinPitch = RB * 64, kThinChunks = RB * 4, kLoads = kTileRows * 16 / kThreads, kThinLoads = kTileRows * kThinChunks / kThreads;
     __shared__ uint64_t masks[kMasks];
-    extern __shared__ __attribute__((aligned(16))) char lds[];          // bf16: [stage][wide, thin] tiles of 64 rows x 256 bytes
+    extern __shared__ __attribute__((aligned(16))) char lds[];          // bf16: [stage][wide, thin]
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, g = lane >> 5;
     const int col_tiles = a.tiles[0] + a.tiles[1];
     const int ct = blockIdx.x % col_tiles, which = blockIdx.x / col_tiles % a.n_adapters, part = blockIdx.x / col_tiles / a.n_adapters;
@@ -276,35 +309,38 @@ __global__ __launch_bounds__(kThreads) void adapter_sum_kernel(SumArgs a) {
             return i;
         };
         if constexpr (sizeof(T) == 2) {
-            u32x4_t wv[kLoads], tv[kLoads];
+            u32x4_t wv[kLoads], tv[kThinLoads];
             const auto fetch = [&](int i) {
                 const uint64_t bits = masks[i];
                 const int64_t m0 = static_cast<int64_t>(base + i) * kTileRows;
 #pragma unroll
                 for (int k = 0; k < kLoads; ++k) {
                     const int row = (tid + k * kThreads) / 16, c = (tid + k * kThreads) % 16;
-                    wv[k] = tv[k] = u32x4_t{0, 0, 0, 0};
-                    if (bits >> row & 1) {
-                        if (c0 + c * 8 < cols) wv[k] = *reinterpret_cast<const u32x4_t*>(wide + (m0 + row) * ld + c0 + c * 8);
-                        if (c * 8 < a.t_row) tv[k] = *reinterpret_cast<const u32x4_t*>(thin + (m0 + row) * a.t_row + c * 8);
-                    }
+                    wv[k] = u32x4_t{0, 0, 0, 0};
+                    if ((bits >> row & 1) && c0 + c * 8 < cols) wv[k] = *reinterpret_cast<const u32x4_t*>(wide + (m0 + row) * ld + c0 + c * 8);
+                }
+#pragma unroll
+                for (int k = 0; k < kThinLoads; ++k) {
+                    const int row = (tid + k * kThreads) / kThinChunks, c = (tid + k * kThreads) % kThinChunks;
+                    tv[k] = u32x4_t{0, 0, 0, 0};
+                    if ((bits >> row & 1) && c * 8 < a.t_row) tv[k] = *reinterpret_cast<const u32x4_t*>(thin + (m0 + row) * a.t_row + c * 8);
                 }
             };
             const auto stash = [&](int stage) {
+                char* const to = lds + stage * sum_stage(RB);
 #pragma unroll
-                for (int k = 0; k < kLoads; ++k) {
-                    const int row = (tid + k * kThreads) / 16, c = (tid + k * kThreads) % 16;
-                    char* const to = lds + stage * 2 * kTileRows * kPitch + row * kPitch + (turned_chunk(row, c) << 4);
-                    *reinterpret_cast<u32x4_t*>(to) = wv[k];
-                    if (c * 8 < RB * 32) *reinterpret_cast<u32x4_t*>(to + kTileRows * kPitch) = tv[k];
-                }
+                for (int k = 0; k < kLoads; ++k)
+                    *reinterpret_cast<u32x4_t*>(to + chunk_place<256>((tid + k * kThreads) / 16, (tid + k * kThreads) % 16)) = wv[k];
+#pragma unroll
+                for (int k = 0; k < kThinLoads; ++k)
+                    *reinterpret_cast<u32x4_t*>(to + kTileRows * 256 + chunk_place<kThinPitch>((tid + k * kThreads) / kThinChunks, (tid + k * kThreads) % kThinChunks)) = tv[k];
             };
             // transposing reads: 8 consecutive rows of a column per lane (cross_attn.h)
             const int row = 8 * g + ((lane & 15) >> 2), in_c = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1), in = 8 * (lane & 1);
-            const auto column = [&](const char* tile, int ks, int block) {
+            const auto column = [&](const char* tile, auto pitch, int ks, int block) {
+                constexpr int kPitch = decltype(pitch)::value;
                 const char* const p = tile + ks * 16 * kPitch + in;
-                return transposed_chunk(p + row * kPitch + (turned_chunk(row, 4 * block + in_c) << 4),
-                                        p + (row + 4) * kPitch + (turned_chunk(row + 4, 4 * block + in_c) << 4));
+                return transposed_chunk(p + chunk_place<kPitch>(row, 4 * block + in_c), p + chunk_place<kPitch>(row + 4, 4 * block + in_c));
             };
             int i = next(0), stage = 0;
             if (i < count) fetch(i);
@@ -313,21 +349,24 @@ __global__ __launch_bounds__(kThreads) void adapter_sum_kernel(SumArgs a) {
                 i = next(i + 1);
                 if (i < count) fetch(i);
                 __syncthreads();
-                const char* const tile = lds + stage * 2 * kTileRows * kPitch;
+                const char* const tile = lds + stage * sum_stage(RB);
+                const std::integral_constant<int, 256> wide_pitch{};
+                const std::integral_constant<int, kThinPitch> thin_pitch{};
 #pragma unroll
                 for (int ks = 0; ks < kTileRows / 16; ++ks) {
-                    const xu32x4_t w = column(tile, ks, wave);
+                    const xu32x4_t w = column(tile, wide_pitch, ks, wave);
 #pragma unroll
-                    for (int b = 0; b < RB; ++b) chunk_product<T>(w, column(tile + kTileRows * kPitch, ks, b), acc[b]);
+                    for (int b = 0; b < RB; ++b) chunk_product<T>(w, column(tile + kTileRows * 256, thin_pitch, ks, b), acc[b]);
                 }
                 stage ^= 1;
             }
         } else {
+            constexpr int kPairs = RB == 1 ? 32 : 16;            // row pairs whose loads are in flight together
             const int col = c0 + wave * 32 + l32;
             for (int i = next(0); i < count; i = next(i + 1)) {
                 const uint64_t bits = masks[i];
                 const int64_t m0 = static_cast<int64_t>(base + i) * kTileRows;
-#pragma unroll 8
+#pragma unroll kPairs
                 for (int k = 0; k < kTileRows / 2; ++k) {
                     const int row = 2 * k + g;
                     const bool on = bits >> row & 1;
@@ -342,50 +381,38 @@ __global__ __launch_bounds__(kThreads) void adapter_sum_kernel(SumArgs a) {
         }
     }
     // register e: column 8 (e / 4) + 4 g + e % 4 of the wavefront's, rank 32 b + l32
+    const int64_t values = static_cast<int64_t>(a.cols[0] + a.cols[1]) * a.r * a.n_adapters;
+    const int64_t first_value = second ? static_cast<int64_t>(a.cols[0]) * a.r * a.n_adapters : 0;
 #pragma unroll
     for (int b = 0; b < RB; ++b) {
         const int rank = b * 32 + l32;
         if (rank >= a.r) continue;
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            const int col = c0 + wave * 32 + 8 * (e >> 2) + 4 * g + (e & 3);
-            if (col >= cols) continue;
-            if (a.parts > 1) {
-                const int64_t at = (static_cast<int64_t>(part) * a.n_adapters + which) * (a.cols[0] + a.cols[1]) + (second ? a.cols[0] : 0) + col;
-                a.part[at * a.t_row + rank] = acc[b][e];
-            } else if (second) {
-                store_f(static_cast<T*>(a.out[1]) + (static_cast<int64_t>(which) * cols + col) * a.r + rank, acc[b][e]);
-            } else {
-                store_f(static_cast<T*>(a.out[0]) + (static_cast<int64_t>(which) * a.r + rank) * cols + col, acc[b][e]);
+        for (int e4 = 0; e4 < 4; ++e4) {
+            const int col = c0 + wave * 32 + 8 * e4 + 4 * g;
+            const float v[4] = {acc[b][4 * e4], acc[b][4 * e4 + 1], acc[b][4 * e4 + 2], acc[b][4 * e4 + 3]};
+            const int64_t at = second ? (static_cast<int64_t>(which) * cols + col) * a.r + rank : (static_cast<int64_t>(which) * a.r + rank) * cols + col;
+            const int64_t step = second ? a.r : 1;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                if (col + c >= cols) continue;
+                if (a.parts > 1) a.part[part * values + first_value + at + c * step] = v[c];
+                else store_f(static_cast<T*>(second ? a.out[1] : a.out[0]) + at + c * step, v[c]);
             }
         }
     }
 }
 
-// the parts, added in order: a thread per value, in the order of the results
+// the parts, added in order: a thread per value
 template <typename T>
 __global__ __launch_bounds__(kThreads) void adapter_join_kernel(SumArgs a) {
-    const int64_t per = static_cast<int64_t>(a.cols[0] + a.cols[1]) * a.r, all = per * a.n_adapters, na = static_cast<int64_t>(a.cols[0]) * a.r * a.n_adapters;
+    const int64_t values = static_cast<int64_t>(a.cols[0] + a.cols[1]) * a.r * a.n_adapters, first = static_cast<int64_t>(a.cols[0]) * a.r * a.n_adapters;
     const int64_t i = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x;
-    if (i >= all) return;
-    const bool second = i >= na;
-    const int64_t j = second ? i - na : i;
-    int64_t which, col;
-    int rank;
-    if (second) {
-        rank = static_cast<int>(j % a.r);
-        which = j / a.r / a.cols[1];
-        col = a.cols[0] + j / a.r % a.cols[1];
-    } else {
-        col = j % a.cols[0];
-        which = j / a.cols[0] / a.r;
-        rank = static_cast<int>(j / a.cols[0] % a.r);
-    }
-    const int64_t step = static_cast<int64_t>(a.n_adapters) * (a.cols[0] + a.cols[1]) * a.t_row;
-    const float* p = a.part + (which * (a.cols[0] + a.cols[1]) + col) * a.t_row + rank;
-    float v = p[0];
-    for (int k = 1; k < a.parts; ++k) v += p[k * step];
-    store_f(static_cast<T*>(second ? a.out[1] : a.out[0]) + j, v);
+    if (i >= values) return;
+    float v = a.part[i];
+#pragma unroll 4
+    for (int k = 1; k < a.parts; ++k) v += a.part[k * values + i];
+    store_f(i < first ? static_cast<T*>(a.out[0]) + i : static_cast<T*>(a.out[1]) + (i - first), v);
 }
 
 template <typename T>
@@ -396,20 +423,16 @@ __global__ __launch_bounds__(kThreads) void adapter_clear_kernel(T* p, int64_t n
 // ---- sizes, workspaces, launches
 struct Sizes {
     int32_t M, K, N, r, n;
-    int32_t Kp, Np;                              // as the products have them
+    int32_t Kp, Np;                              // K and N in whole slices of a sum
     int32_t t_row;
     size_t es;
-    bool padded;
     Sizes(int32_t m, int32_t k, int32_t nn, int32_t rank, int32_t adapters, int32_t dtype)
-        : M(m), K(k), N(nn), r(rank), n(adapters), Kp(k), Np(nn), t_row(up_to(rank, 16)), es(dtype == FREE_BF16 ? 2 : 4) {
-        const int32_t step = es == 2 ? 8 : 64;
-        padded = k % step != 0 || nn % step != 0;
-        if (padded) {
-            Kp = up_to(k, 64);
-            Np = up_to(nn, 64);
-        }
+        : M(m), K(k), N(nn), r(rank), n(adapters), t_row(up_to(rank, 16)), es(dtype == FREE_BF16 ? 2 : 4) {
+        const int32_t slice = es == 2 ? 64 : 32;
+        Kp = up_to(k, slice);
+        Np = up_to(nn, slice);
     }
-    bool few() const { return ffn_rows_pay(M, K, N, padded); }
+    bool few() const { return ffn_rows_pay(M, K, N, K != Kp); }
     size_t thin_bytes() const { return static_cast<size_t>(M) * t_row * es; }
 };
 
@@ -425,33 +448,18 @@ struct Carve {
 };
 
 template <typename T>
-FfnProduct<T> forward_product(const Sizes& z, const T* x, const T* w, T* y) {
-    return FfnProduct<T>{FFN_ROWS, x, w, z.Kp, z.Kp, z.M, z.Np, z.Kp, y, z.Np};
-}
-
-template <typename T>
-FfnProduct<T> backward_product(const Sizes& z, const T* dout, const T* w, T* dx) {
-    return FfnProduct<T>{FFN_ROWS_BY_K, dout, w, z.Np, z.Kp, z.M, z.Kp, z.Np, dx, z.Kp};
-}
-
-template <typename T>
 struct ForwardSpace {
-    T *t, *x, *w, *y;
-    float* room;
+    T *t, *x, *w;
+    float* zeros;                                // in place of a bias
     size_t bytes;
     ForwardSpace(const Sizes& z, char* base) {
         Carve c{base};
         t = c.take<T>(z.thin_bytes());
-        x = w = y = nullptr;
-        room = nullptr;
-        if (!z.few()) {
-            const FfnProduct<T> p = forward_product<T>(z, nullptr, nullptr, nullptr);
-            room = c.take<float>(ffn_products_part_bytes(&p, 1));
-            if (z.padded) {
-                x = c.take<T>(static_cast<size_t>(z.M) * z.Kp * sizeof(T));
-                w = c.take<T>(static_cast<size_t>(z.Np) * z.Kp * sizeof(T));
-                y = c.take<T>(static_cast<size_t>(z.M) * z.Np * sizeof(T));
-            }
+        zeros = c.take<float>(static_cast<size_t>(z.N) * sizeof(float));
+        x = w = nullptr;
+        if (!z.few() && z.K != z.Kp) {
+            x = c.take<T>(static_cast<size_t>(z.M) * z.Kp * sizeof(T));
+            w = c.take<T>(static_cast<size_t>(z.N) * z.Kp * sizeof(T));
         }
         bytes = c.at + 256;
     }
@@ -471,25 +479,22 @@ struct SumPlan {
 
 template <typename T>
 struct BackwardSpace {
-    T *u, *bt, *at, *x, *w, *dout, *dx;
-    float *room, *part;
+    T *u, *wt, *bt, *at, *x, *dout;
+    float *zeros, *part;
     size_t bytes;
     BackwardSpace(const Sizes& z, char* base) {
         Carve c{base};
         u = c.take<T>(z.thin_bytes());
+        wt = c.take<T>(static_cast<size_t>(z.K) * z.Np * sizeof(T));
         bt = c.take<T>(static_cast<size_t>(z.n) * z.t_row * z.Np * sizeof(T));
         at = c.take<T>(static_cast<size_t>(z.n) * z.K * z.t_row * sizeof(T));
+        zeros = c.take<float>(static_cast<size_t>(z.K) * sizeof(float));
         const SumPlan sum(z);
-        part = c.take<float>(sum.parts > 1 ? static_cast<size_t>(sum.parts) * z.n * (z.K + z.N) * z.t_row * sizeof(float) : 0);
-        const FfnProduct<T> p = backward_product<T>(z, nullptr, nullptr, nullptr);
-        room = c.take<float>(ffn_products_part_bytes(&p, 1));
-        x = w = dout = dx = nullptr;
-        if (z.padded) {
-            x = c.take<T>(static_cast<size_t>(z.M) * z.Kp * sizeof(T));
-            w = c.take<T>(static_cast<size_t>(z.Np) * z.Kp * sizeof(T));
-            dout = c.take<T>(static_cast<size_t>(z.M) * z.Np * sizeof(T));
-            dx = c.take<T>(static_cast<size_t>(z.M) * z.Kp * sizeof(T));
-        }
+        part = c.take<float>(sum.parts > 1 ? static_cast<size_t>(sum.parts) * z.n * (z.K + z.N) * z.r * sizeof(float) : 0);
+        x = dout = nullptr;
+        // (rows of x in 16-byte pieces for dA; rows of dout in whole slices for dx)
+        if (z.K % (16 / sizeof(T)) != 0) x = c.take<T>(static_cast<size_t>(z.M) * z.Kp * sizeof(T));
+        if (z.N != z.Np) dout = c.take<T>(static_cast<size_t>(z.M) * z.Np * sizeof(T));
         bytes = c.at + 256;
     }
 };
@@ -500,17 +505,15 @@ struct BackwardSpace {
         if (st_ != FREE_OK) return st_;     \
     } while (0)
 
-// product and what it gets besides, into out [M, term.cols]; y: where the product's own rows go if they are wider
+// out [M, term.cols] = x w^T + bias and the adapters', K whole slices
 template <typename T>
-int32_t product_with(FfnProduct<T> p, const AdapterTerm& term, bool padded, T* out, float* room, hipStream_t s) {
+int32_t linear_with(const T* x, const T* w, const float* bias, int32_t M, int32_t K, const AdapterTerm& term, T* out, hipStream_t s) {
     if constexpr (sizeof(T) == 2) {
-        p.adapters = &term;
-        FREE_STEP(launch_ffn_products(&p, 1, room, s));
-        return padded ? launch_fit<T>(p.out, p.M, p.N, out, p.M, term.cols, s) : FREE_OK;
+        return launch_linear_adapters(x, w, bias, M, term.cols, K, out, term, s);
     } else {
-        FREE_STEP(launch_ffn_products(&p, 1, room, s));
-        const dim3 grid((term.cols + 127) / 128, std::min((p.M + 31) / 32, 65535));
-        hipLaunchKernelGGL(adapter_up_kernel, grid, dim3(kThreads), 0, s, p.out, p.ldo, term, p.M, out);
+        FREE_STEP(launch_linear_f32(x, w, bias, M, term.cols, K, FREE_EPI_BIAS, out, nullptr, RowVec{nullptr, 0, 1}, s));
+        const dim3 grid((term.cols + 127) / 128, std::min((M + 31) / 32, 65535));
+        hipLaunchKernelGGL(adapter_up_kernel, grid, dim3(kThreads), 0, s, term, M, out);
         return launch_ok() ? FREE_OK : FREE_ERR_HIP;
     }
 }
@@ -521,23 +524,28 @@ int32_t forward_of(const Sizes& z, const AdapterArgs& a, char* ws, hipStream_t s
     T* const t = a.saved ? static_cast<T*>(a.saved) : w.t;
     const T *x = static_cast<const T*>(a.x), *weight = static_cast<const T*>(a.w);
     T* const out = static_cast<T*>(a.out);
-    FREE_STEP(launch_down<T>(DownArgs{x, a.a, a.adapter, a.scale, t, z.M, z.K, z.n, z.r, z.r, z.t_row, a.rows_per_sample}, s));
+    DownArgs down{x, a.a, a.adapter, a.scale, t, z.M, z.K, z.n, z.r, z.r, z.t_row, a.rows_per_sample};
+    if (!a.bias && !z.few()) {
+        down.zeros = w.zeros;
+        down.zero_n = z.N;
+    }
+    FREE_STEP(launch_down<T>(down, s));
     const AdapterTerm term{t, a.b, a.adapter, a.bias, z.n, z.r, z.t_row, z.r, z.N, a.rows_per_sample};
     if (z.few()) return launch_adapter_rows<T>(x, weight, z.M, z.N, z.K, term, out, s);
-    if (z.padded) {
+    if (z.K != z.Kp) {
         FREE_STEP(launch_fit<T>(x, z.M, z.K, w.x, z.M, z.Kp, s));
-        FREE_STEP(launch_fit<T>(weight, z.N, z.K, w.w, z.Np, z.Kp, s));
+        FREE_STEP(launch_fit<T>(weight, z.N, z.K, w.w, z.N, z.Kp, s));
         x = w.x;
         weight = w.w;
     }
-    return product_with<T>(forward_product<T>(z, x, weight, z.padded ? w.y : out), term, z.padded, out, w.room, s);
+    return linear_with<T>(x, weight, a.bias ? a.bias : w.zeros, z.M, z.Kp, term, out, s);
 }
 
 template <typename T, int RB>
 int32_t launch_sum(const SumArgs& a, hipStream_t s) {
     const int64_t blocks = static_cast<int64_t>(a.tiles[0] + a.tiles[1]) * a.n_adapters * a.parts;
     if (blocks > 0x7fffffff) return FREE_ERR_LIMIT;
-    const size_t lds = sizeof(T) == 2 ? 4 * kTileRows * 256 : 0;
+    const size_t lds = sizeof(T) == 2 ? 2 * sum_stage(RB) : 0;
     auto kern = adapter_sum_kernel<T, RB>;
     static LdsLimit limit;
     if (!limit.allow(reinterpret_cast<const void*>(kern), lds)) return FREE_ERR_HIP;
@@ -563,27 +571,32 @@ int32_t backward_of(const Sizes& z, const AdapterArgs& a, char* ws, hipStream_t 
         return clear<T>(a.db, static_cast<int64_t>(z.n) * z.r * z.N, s);
     }
     const BackwardSpace<T> w(z, ws);
-    const T *x = static_cast<const T*>(a.x), *weight = static_cast<const T*>(a.w), *dout = static_cast<const T*>(a.dout);
-    T* const dx = static_cast<T*>(a.dx);
-    if (z.padded) {
+    const T *x = static_cast<const T*>(a.x), *dout = static_cast<const T*>(a.dout);
+    if (w.x) {
         FREE_STEP(launch_fit<T>(x, z.M, z.K, w.x, z.M, z.Kp, s));
-        FREE_STEP(launch_fit<T>(weight, z.N, z.K, w.w, z.Np, z.Kp, s));
-        FREE_STEP(launch_fit<T>(dout, z.M, z.N, w.dout, z.M, z.Np, s));
         x = w.x;
-        weight = w.w;
+    }
+    if (w.dout) {
+        FREE_STEP(launch_fit<T>(dout, z.M, z.N, w.dout, z.M, z.Np, s));
         dout = w.dout;
     }
-    const TurnJob jb{a.b, w.bt, z.N, z.r, z.Np, z.t_row}, ja{a.a, w.at, z.r, z.K, z.t_row, z.K};
-    const auto tiles = [](const TurnJob& j) { return static_cast<int64_t>((j.rows_to + 31) / 32) * ((j.cols_to + 31) / 32); };
-    hipLaunchKernelGGL(adapter_turn_kernel<T>, dim3(static_cast<uint32_t>(std::min<int64_t>(std::max(tiles(ja), tiles(jb)), 65536)), 1, 2 * z.n), dim3(kThreads), 0, s,
-                       jb, ja, z.n);
+    TurnJobs jobs{{{a.w, w.wt, z.N, z.K, z.Np, z.K, 1, 0}, {a.b, w.bt, z.N, z.r, z.Np, z.t_row, z.n, 0}, {a.a, w.at, z.r, z.K, z.t_row, z.K, z.n, 0}}};
+    int64_t tiles = 0;
+    for (TurnJob& j : jobs.job) {
+        const int64_t n = static_cast<int64_t>((j.rows_to + 63) / 64) * ((j.cols_to + 63) / 64) * j.n;
+        tiles += n;
+        if (tiles > 0x7fffffff) return FREE_ERR_LIMIT;
+        j.tiles = static_cast<int32_t>(n);
+    }
+    hipLaunchKernelGGL(adapter_turn_kernel<T>, dim3(static_cast<uint32_t>(tiles)), dim3(kThreads), 0, s, jobs);
     if (!launch_ok()) return FREE_ERR_HIP;
-    FREE_STEP(launch_down<T>(DownArgs{dout, w.bt, a.adapter, a.scale, w.u, z.M, z.Np, z.n, z.t_row, z.r, z.t_row, a.rows_per_sample}, s));
+    DownArgs down{dout, w.bt, a.adapter, a.scale, w.u, z.M, z.Np, z.n, z.t_row, z.r, z.t_row, a.rows_per_sample, w.zeros, z.K};
+    FREE_STEP(launch_down<T>(down, s));
     const AdapterTerm term{w.u, w.at, a.adapter, nullptr, z.n, z.t_row, z.t_row, z.t_row, z.K, a.rows_per_sample};
-    FREE_STEP(product_with<T>(backward_product<T>(z, dout, weight, z.padded ? w.dx : dx), term, z.padded, dx, w.room, s));
+    FREE_STEP(linear_with<T>(dout, w.wt, w.zeros, z.M, z.Np, term, static_cast<T*>(a.dx), s));
     const SumPlan plan(z);
-    const SumArgs sum{{x, dout}, {w.u, a.saved}, {z.Kp, z.Np}, {z.K, z.N}, {(z.K + 127) / 128, (z.N + 127) / 128}, {a.da, a.db}, w.part, a.adapter, z.M, z.n, z.r,
-                      z.t_row, a.rows_per_sample, plan.parts, plan.part_tiles};
+    const SumArgs sum{{x, dout}, {w.u, a.saved}, {w.x ? z.Kp : z.K, z.Np}, {z.K, z.N}, {(z.K + 127) / 128, (z.N + 127) / 128}, {a.da, a.db}, w.part, a.adapter, z.M,
+                      z.n, z.r, z.t_row, a.rows_per_sample, plan.parts, plan.part_tiles};
     if (z.t_row <= 32) return launch_sum<T, 1>(sum, s);
     if (z.t_row <= 64) return launch_sum<T, 2>(sum, s);
     return launch_sum<T, 4>(sum, s);
@@ -591,7 +604,7 @@ int32_t backward_of(const Sizes& z, const AdapterArgs& a, char* ws, hipStream_t 
 
 }  // namespace
 
-// 32-bit byte offsets inside a tile of 256 rows, grids of less than 2^32 threads
+// 32-bit byte offsets inside a tile of 384 rows, grids of less than 2^32 threads
 bool adapters_cover(int32_t M, int32_t K, int32_t N, int32_t r, int32_t n, int32_t dtype) {
     if (K > 1 << 20 || N > 1 << 20 || r > 128 || n > 16384) return false;
     const int64_t m = (static_cast<int64_t>(M) + 127) / 128, k = (K + 127) / 128, c = (N + 127) / 128;

@@ -302,7 +302,7 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 && DP <= 80 && KS == 1) ?
 
 // Up to 32 rows per (sample, head): workgroup (part, pair), its four wavefronts take the part's key tiles of 32 in turn
 template <typename T, int DP, bool kVec>
-__global__ __launch_bounds__(kThreads, 1) void cross_few_kernel(CrossArgs a, Parts pt) {
+__global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void cross_few_kernel(CrossArgs a, Parts pt) {
     using H = HeadShape<T, DP>;
     constexpr int E = H::E, CH = H::CH, KSTEPS = H::KSTEPS, DT = H::DT;
     constexpr int VROW = kValueRow<T, DP>, kWaveV = 32 * VROW + (sizeof(T) == 4 ? 128 : 0), NV = CH / 2;
@@ -426,29 +426,47 @@ __global__ __launch_bounds__(kThreads, 1) void cross_few_kernel(CrossArgs a, Par
     write_row<T, kVec, DT>(a, pt, part, pair, b, kvh, row, g, m * scale_log2, l, any, o);
 }
 
-// The parts of a row's sums, added in order: a thread per value of out
-template <typename T>
+// The parts of a row's sums, added in order: WPR wavefronts per row take them in turn, lane p having part p's maximum and sum (at most 64
+// parts)
+template <typename T, int WPR>
 __global__ __launch_bounds__(kThreads) void cross_join_kernel(CrossArgs a, Parts pt) {
-    const int group = a.heads / a.kv_heads;
+    __shared__ float sums[4][128];
+    const int group = a.heads / a.kv_heads, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, first = wave % WPR;
     const int64_t per_pair = static_cast<int64_t>(a.Nq) * group, all = static_cast<int64_t>(a.B) * a.kv_heads * per_pair;
-    const int64_t i = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x;
-    if (i >= all * a.dh) return;
-    const int64_t at = i / a.dh, pair = at / per_pair, r = at % per_pair, token = r / group;
-    const int d = static_cast<int>(i % a.dh), b = static_cast<int>(pair / a.kv_heads), head = static_cast<int>(pair % a.kv_heads * group + r % group);
-    float m = -INFINITY;
-    for (int p = 0; p < pt.parts; ++p) m = fmaxf(m, pt.ml[2 * (p * all + at)]);
-    float l = 0.f, o = 0.f;
-    if (m != -INFINITY) {
-        for (int p = 0; p < pt.parts; ++p) {
-            const float mp = pt.ml[2 * (p * all + at)];
-            if (mp == -INFINITY) continue;
-            const float w = mp == m ? 1.0f : __builtin_amdgcn_exp2f(mp - m);
-            l += w * pt.ml[2 * (p * all + at) + 1];
-            o += w * pt.o[(p * all + at) * a.dh + d];
-        }
+    const int64_t row = static_cast<int64_t>(blockIdx.x) * (4 / WPR) + wave / WPR, at = row < all ? row : all - 1;
+    const float mp = lane < pt.parts ? pt.ml[2 * (lane * all + at)] : -INFINITY, lp = lane < pt.parts ? pt.ml[2 * (lane * all + at) + 1] : 0.f;
+    float m = max_lane_xor32(mp);
+#pragma unroll
+    for (int x = 16; x > 0; x >>= 1) m = fmaxf(m, __shfl_xor(m, x, 64));
+    const float w = mp == -INFINITY ? 0.f : mp == m ? 1.0f : __builtin_amdgcn_exp2f(mp - m);
+    const float l = wave_sum(w == 0.f ? 0.f : w * lp);
+    float o[2] = {0.f, 0.f};
+    for (int p = first; p < pt.parts; p += WPR) {
+        const float wp = __shfl(w, p, 64);
+        const float* const from = pt.o + (p * all + at) * a.dh;
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+            if (lane + 64 * k < a.dh && wp != 0.f) o[k] = fmaf(wp, from[lane + 64 * k], o[k]);
     }
-    store_f(static_cast<T*>(a.out) + (static_cast<int64_t>(b) * a.Nq + token) * a.out_stride + static_cast<int64_t>(head) * a.dh + d, m == -INFINITY ? 0.f : o * (1.0f / l));
-    if (a.lse && d == 0) a.lse[(static_cast<int64_t>(b) * a.heads + head) * a.Nq + token] = m == -INFINITY ? m : (m + __builtin_log2f(l)) * kLn2;
+    if constexpr (WPR > 1) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) sums[wave][lane + 64 * k] = o[k];
+        __syncthreads();
+        if (wave > 0) return;
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int i = 1; i < WPR; ++i) o[k] += sums[i][lane + 64 * k];
+    }
+    if (row >= all) return;
+    const int64_t pair = at / per_pair, r = at - pair * per_pair, token = r / group;
+    const int b = static_cast<int>(pair / a.kv_heads), head = static_cast<int>(pair % a.kv_heads * group + (r - token * group));
+    T* const out = static_cast<T*>(a.out) + (static_cast<int64_t>(b) * a.Nq + token) * a.out_stride + static_cast<int64_t>(head) * a.dh;
+    const float inv = m == -INFINITY ? 0.f : 1.0f / l;
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+        if (lane + 64 * k < a.dh) store_f(out + lane + 64 * k, o[k] * inv);
+    if (a.lse && lane == 0) a.lse[(static_cast<int64_t>(b) * a.heads + head) * a.Nq + token] = m == -INFINITY ? m : (m + __builtin_log2f(l)) * kLn2;
 }
 
 // How a problem is cut; by its sizes alone (a workspace's size must not depend on the device)
@@ -475,7 +493,7 @@ Plan plan_of(int32_t B, int32_t Nq, int32_t Nk, int32_t heads, int32_t kv_heads,
             p.q_tiles = (rows + 63) / 64;
         }
     }
-    const int64_t work = pairs * p.q_tiles, least = p.few ? 8 : 4, want = p.few ? 4 * kUnits : 2 * kUnits;      // tiles of a part; workgroups
+    const int64_t work = pairs * p.q_tiles, least = p.few ? 8 : 4, want = 2 * kUnits;      // tiles of a part; workgroups
     int64_t parts = 1;
     if (work < want) parts = std::max<int64_t>(1, std::min(want / std::max<int64_t>(work, 1), tiles / least));
     parts = std::min<int64_t>(parts, 64);
@@ -528,8 +546,9 @@ int32_t launch_type(const CrossArgs& a, const Plan& p, const Parts& pt, hipStrea
     const bool vec = a.dh % static_cast<int>(16 / sizeof(T)) == 0 && al(a.q, a.q_stride) && al(a.k, a.k_stride) && al(a.v, a.v_stride) && al(a.out, a.out_stride);
     const int32_t st = vec ? launch_width<T, true>(a, p, pt, s) : launch_width<T, false>(a, p, pt, s);
     if (st != FREE_OK || p.parts == 1) return st;
-    const int64_t values = static_cast<int64_t>(a.B) * a.Nq * a.heads * a.dh;
-    hipLaunchKernelGGL(cross_join_kernel<T>, dim3(static_cast<uint32_t>((values + kThreads - 1) / kThreads)), dim3(kThreads), 0, s, a, pt);
+    const int64_t rows = static_cast<int64_t>(a.B) * a.Nq * a.heads;
+    if (p.parts > 8) hipLaunchKernelGGL((cross_join_kernel<T, 4>), dim3(static_cast<uint32_t>(rows)), dim3(kThreads), 0, s, a, pt);
+    else hipLaunchKernelGGL((cross_join_kernel<T, 1>), dim3(static_cast<uint32_t>((rows + 3) / 4)), dim3(kThreads), 0, s, a, pt);
     return launch_ok() ? FREE_OK : FREE_ERR_HIP;
 }
 

@@ -2,6 +2,7 @@
 // dimensions are multiples of 8; fp32: of 64, and rows dense.  Pointers are 16-byte aligned.
 #pragma once
 
+#include "adapter_term.h"
 #include "free_internal.h"
 
 namespace freemi {
@@ -16,21 +17,6 @@ enum FfnKind {
     FFN_K_BY_K,        // out = X [K, M] by W [K, N]
     FFN_STORE,         // (epilogues of the kernel alone: plain, and parts of K)
     FFN_PART
-};
-
-// What the rows of a product with adapters get besides: bias[n] + sum over ranks of t[m, rank] b_a[n, rank], a = adapter[m / rows_per_sample]
-// (none of n_adapters: the bias alone).  t: rows of t_row values, zeros past r, 16-byte aligned; b: [adapter][cols][b_row], any alignment.
-struct AdapterTerm {
-    const void *t, *b;
-    const int32_t* adapter;
-    const float* bias;               // nullable
-    int32_t n_adapters, r, t_row, b_row, cols, rows_per_sample;
-#if defined(__HIPCC__)
-    __device__ __forceinline__ int of_row(int m) const {
-        const int a = adapter[m / rows_per_sample];
-        return a >= 0 && a < n_adapters ? a : -1;
-    }
-#endif
 };
 
 template <typename T>                // bf16_t or float
@@ -49,7 +35,6 @@ struct FfnProduct {
     // fold are none
     int32_t fold = 0, fold_to = 0;
     int32_t cols() const { return hidden > 0 ? hidden : N; }
-    const AdapterTerm* adapters = nullptr;                       // FFN_ROWS, FFN_ROWS_BY_K of bf16
     bool gated() const { return kind == FFN_GATE || kind == FFN_GATE_KEEP; }
 };
 

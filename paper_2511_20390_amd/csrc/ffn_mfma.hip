@@ -55,7 +55,6 @@ struct Launch {
     Problem p[2];
     int32_t first1;              // tiles (and parts of K) of p[0]
     int32_t total;               // of both
-    AdapterTerm adapters;        // kAdapt (one product)
 };
 
 // Whether a workgroup does several tiles (LDS for the stages and for the epilogue, one workgroup per compute unit): launches of one product
@@ -67,12 +66,9 @@ constexpr bool ffn_rounds(int bm, int bn, bool xk, int epi) { return bm * bn > 1
 template <int EPI>
 constexpr bool kGated = EPI == FFN_GATE || EPI == FFN_GATE_KEEP;
 
-// kAdapt: the sums begin with the rows' bias and adapters (AdapterTerm) in place of zero, an adapter of the wavefront's rows after the
-// other - one where the rows are of one request - as k-steps of 16 ranks, the rows of others at zero.  The operands come straight from
-// memory behind the first slices' loads; a launch of its own over the finished result would read and write it once more, and round it twice.
 // kRagged: rows of a row-major operand are not whole slices of K, or `cols` is more than N (an instance of its own: what it does in the
 // last slice and in the epilogue costs products of few slices 3 %)
-template <int BM, int BN, int WGM, int WGN, bool XK, bool WK, int EPI, bool kRagged, bool kAdapt>
+template <int BM, int BN, int WGM, int WGN, bool XK, bool WK, int EPI, bool kRagged>
 __global__ __launch_bounds__(512) void ffn_product_kernel(Launch la) {
     constexpr int NW = 8;
     static_assert(WGM * WGN == NW && BN / WGN == 64, "eight wavefronts of 64 columns");
@@ -308,87 +304,11 @@ __global__ __launch_bounds__(512) void ffn_product_kernel(Launch la) {
             for (int j = 0; j < TN; ++j)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
-        const int e_m0 = m0, e_split = split, e_col = n0 + wn * (kGated<EPI> ? 32 : 64);       // first row; this wavefront's first column of C
-        const bool mine = e_col < a.cols && e_m0 + wm * TM * 32 < a.M;
-        if constexpr (kAdapt) {
-            static_assert(!XK && !kGated<EPI>, "rows as they are");
-            if (mine && e_split == 0) {
-                const AdapterTerm& ad = la.adapters;
-                if (ad.bias) {
-#pragma unroll
-                    for (int j = 0; j < TN; ++j)
-#pragma unroll
-                        for (int e4 = 0; e4 < 4; ++e4) {
-                            const int n = e_col + 32 * j + 8 * e4 + 4 * lhi;
-                            float v[4];
-                            if (n + 4 <= ad.cols) {
-                                __builtin_memcpy(v, ad.bias + n, 16);
-                            } else {
-#pragma unroll
-                                for (int c = 0; c < 4; ++c) v[c] = n + c < ad.cols ? ad.bias[n + c] : 0.f;
-                            }
-#pragma unroll
-                            for (int i = 0; i < TM; ++i)
-#pragma unroll
-                                for (int c = 0; c < 4; ++c) acc[i][j][4 * e4 + c] = v[c];
-                        }
-                }
-                int of[TM];                                      // the adapters of this lane's rows that are still to be added
-#pragma unroll
-                for (int i = 0; i < TM; ++i) {
-                    const int m = e_m0 + (wm * TM + i) * 32 + l32;
-                    of[i] = m < a.M ? ad.of_row(m) : -1;
-                }
-                const bool whole = ad.b_row % 8 == 0 && (reinterpret_cast<uintptr_t>(ad.b) & 15u) == 0;
-                for (;;) {
-                    int which = -1;                              // (of a row that has one)
-#pragma unroll
-                    for (int i = 0; i < TM; ++i) {
-                        const uint64_t left = __ballot(of[i] >= 0);
-                        which = left != 0 ? __builtin_amdgcn_readlane(of[i], __builtin_ctzll(left)) : which;
-                    }
-                    if (which < 0) break;
-                    const bf16_t* const b = static_cast<const bf16_t*>(ad.b) + static_cast<int64_t>(which) * ad.cols * ad.b_row;
-                    for (int k0 = 0; k0 < ad.r; k0 += 16) {
-                        const int k = k0 + lhi * 8;
-                        u32x4_t bv[TN], tv[TM];
-#pragma unroll
-                        for (int j = 0; j < TN; ++j) {
-                            const int n = e_col + 32 * j + l32;
-                            const bf16_t* const p = b + static_cast<int64_t>(n < ad.cols ? n : ad.cols - 1) * ad.b_row + k;
-                            bv[j] = u32x4_t{0, 0, 0, 0};
-                            if (whole) {
-                                if (k < ad.r) bv[j] = *reinterpret_cast<const u32x4_t*>(p);
-                            } else {
-                                bf16_t v[8];
-#pragma unroll
-                                for (int e = 0; e < 8; ++e) v[e] = k + e < ad.r ? p[e] : bf16_t{0};
-                                __builtin_memcpy(&bv[j], v, 16);
-                            }
-                        }
-#pragma unroll
-                        for (int i = 0; i < TM; ++i) {
-                            tv[i] = u32x4_t{0, 0, 0, 0};
-                            if (of[i] == which)
-                                tv[i] = *reinterpret_cast<const u32x4_t*>(static_cast<const bf16_t*>(ad.t) +
-                                                                          static_cast<int64_t>(e_m0 + (wm * TM + i) * 32 + l32) * ad.t_row + k);
-                        }
-#pragma unroll
-                        for (int i = 0; i < TM; ++i)
-#pragma unroll
-                            for (int j = 0; j < TN; ++j)
-                                acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, bv[j]),
-                                                                                    __builtin_bit_cast(bf16x8_t, tv[i]), acc[i][j], 0, 0, 0);
-                    }
-#pragma unroll
-                    for (int i = 0; i < TM; ++i) of[i] = of[i] == which ? -1 : of[i];
-                }
-            }
-            __builtin_amdgcn_sched_barrier(0);
-        }
         // the first slice has arrived (loads return in order, and the epilogue's stores behind them only make this wait longer)
         if (nk > 1) wait_vm_barrier<NL>();
         else wait_vm_barrier<0>();
+        const int e_m0 = m0, e_split = split, e_col = n0 + wn * (kGated<EPI> ? 32 : 64);       // first row; this wavefront's first column of C
+        const bool mine = e_col < a.cols && e_m0 + wm * TM * 32 < a.M;
         if (mine) k_loop(yes);
         else k_loop(no);
         wait_lds_barrier();
@@ -610,9 +530,9 @@ struct Tile {
     int bm, bn;
 };
 
-template <int BM, int BN, int WGM, int WGN, bool XK, bool WK, int EPI, bool kRagged, bool kAdapt>
+template <int BM, int BN, int WGM, int WGN, bool XK, bool WK, int EPI, bool kRagged>
 int32_t launch_kernel(const Launch& la, int blocks, hipStream_t s) {
-    auto kern = ffn_product_kernel<BM, BN, WGM, WGN, XK, WK, EPI, kRagged, kAdapt>;
+    auto kern = ffn_product_kernel<BM, BN, WGM, WGN, XK, WK, EPI, kRagged>;
     constexpr bool rounds = ffn_rounds(BM, BN, XK, EPI);
     const size_t lds = 2 * static_cast<size_t>(BM + BN) * kRowBytes + (rounds ? 8 * 32 * (kGated<EPI> ? 64 : 128) : 0);
     static LdsLimit limit;
@@ -621,22 +541,21 @@ int32_t launch_kernel(const Launch& la, int blocks, hipStream_t s) {
     return launch_ok() ? FREE_OK : FREE_ERR_HIP;
 }
 
-template <bool XK, bool WK, int EPI, bool kRagged, bool kAdapt>
+template <bool XK, bool WK, int EPI, bool kRagged>
 int32_t launch_size(const Tile& t, const Launch& la, int blocks, hipStream_t s) {
-    if (t.bm == 256) return launch_kernel<256, 256, 2, 4, XK, WK, EPI, kRagged, kAdapt>(la, blocks, s);
-    if (t.bn == 256) return launch_kernel<128, 256, 2, 4, XK, WK, EPI, kRagged, kAdapt>(la, blocks, s);
-    return launch_kernel<128, 128, 4, 2, XK, WK, EPI, kRagged, kAdapt>(la, blocks, s);
+    if (t.bm == 256) return launch_kernel<256, 256, 2, 4, XK, WK, EPI, kRagged>(la, blocks, s);
+    if (t.bn == 256) return launch_kernel<128, 256, 2, 4, XK, WK, EPI, kRagged>(la, blocks, s);
+    return launch_kernel<128, 128, 4, 2, XK, WK, EPI, kRagged>(la, blocks, s);
 }
 
-template <bool XK, bool WK, int EPI, bool kAdapt = false>
+template <bool XK, bool WK, int EPI>
 int32_t launch_tile(const Tile& t, const Launch& la, int blocks, hipStream_t s) {
-    // (K-major X, and rows by K-major but for the gated gradient, whose K is D, and adapters': their K is the token rows, or whole slices of
-    // [dg | du])
-    if constexpr (!XK && !(WK && EPI == FFN_STORE && !kAdapt)) {
+    // (K-major X, and rows by K-major but for the gated gradient, whose K is D: their K is the token rows, or whole slices of [dg | du])
+    if constexpr (!XK && !(WK && EPI == FFN_STORE)) {
         const Problem& q = la.p[0];
-        if (q.K % BK != 0 || q.cols != q.N) return launch_size<XK, WK, EPI, true, kAdapt>(t, la, blocks, s);
+        if (q.K % BK != 0 || q.cols != q.N) return launch_size<XK, WK, EPI, true>(t, la, blocks, s);
     }
-    return launch_size<XK, WK, EPI, false, kAdapt>(t, la, blocks, s);
+    return launch_size<XK, WK, EPI, false>(t, la, blocks, s);
 }
 
 // What a launch takes: tile, and per product the parts that its sums over K are cut in
@@ -856,13 +775,6 @@ int32_t launch_ffn_products(const FfnProduct<bf16_t>* p, int n, float* part, hip
     if (count == 1) la.first1 = 0x7fffffff;
     if (blocks > (1 << 22)) return FREE_ERR_LIMIT;
     const int b = la.total = static_cast<int>(blocks);
-    if (p[0].adapters) {
-        la.adapters = *p[0].adapters;
-        const bool by_k = p[0].kind == FFN_ROWS_BY_K;
-        if (!parts) return by_k ? launch_tile<false, true, FFN_STORE, true>(t, la, b, s) : launch_tile<false, false, FFN_STORE, true>(t, la, b, s);
-        const int32_t st = by_k ? launch_tile<false, true, FFN_PART, true>(t, la, b, s) : launch_tile<false, false, FFN_PART, true>(t, la, b, s);
-        return st != FREE_OK ? st : launch_join(p[0], p[0].kind, la.p[0].part, plan.splits[0], s);
-    }
     if (!parts) {
         switch (p[0].kind) {
             case FFN_GATE: return launch_tile<false, false, FFN_GATE>(t, la, b, s);

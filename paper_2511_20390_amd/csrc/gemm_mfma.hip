@@ -53,6 +53,7 @@
 #include <cstdlib>
 #include <type_traits>
 
+#include "adapter_term.h"
 #include "free_internal.h"
 #include "gemm_tile.h"
 
@@ -549,6 +550,14 @@ int32_t launch_linear_mfma(const bf16_t* X, const bf16_t* W, const float* bias, 
         case TILE_PIPE: return launch_linear_pipe(X, W, bias, M, N, K, epi, out, resid, gate, s, static_cast<PipeTile>(c.tile), ln);
         default: return launch_staged(static_cast<StagedTile>(c.tile), X, W, bias, M, N, K, epi, out, resid, gate, s);
     }
+}
+
+int32_t launch_linear_adapters(const bf16_t* X, const bf16_t* W, const float* bias, int32_t M, int32_t N, int32_t K, bf16_t* out, const AdapterTerm& term,
+                               hipStream_t s) {
+    if (!mfma_linear_supported(M, N, K) || K % BK != 0 || ((reinterpret_cast<uintptr_t>(X) | reinterpret_cast<uintptr_t>(W)) & 15u)) return FREE_ERR_SHAPE;
+    const Choice c = choose(M, N, K, 2, FREE_EPI_BIAS, linear_rows_covers(N, K, 2, bias, out, nullptr, RowVec{nullptr, 0, 1}), 1);
+    return c.family == TILE_ROWS ? launch_linear_rows_adapters(X, W, bias, M, N, K, out, s, static_cast<RowsTile>(c.tile), term)
+                                 : launch_linear_pipe_adapters(X, W, bias, M, N, K, out, s, static_cast<PipeTile>(c.tile), term);
 }
 
 // A part has at least twelve slices: below that a workgroup is all prologue and epilogue, and with one part less to wait for there

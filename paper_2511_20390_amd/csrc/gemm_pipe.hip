@@ -26,6 +26,7 @@
 // (12 x 1024 tokens: 14.01 -> 13.74 ms, 32 x 256 tokens: 10.20 -> 9.31 ms) gain accordingly less than single launches.
 #include <algorithm>
 
+#include "adapter_term.h"
 #include "free_internal.h"
 #include "gemm_dma.h"
 
@@ -37,7 +38,7 @@ template <int BM, int BN, int WGM, int WGN, int EPI>
 __global__ __launch_bounds__(WGM * WGN * 64) void gemm_pipe_kernel(
     const bf16_t* __restrict__ X, const bf16_t* __restrict__ W, const float* __restrict__ bias, int32_t M, int32_t N, int32_t K,
     int32_t tiles_m, int32_t tiles_n, int32_t group_m, int32_t vec_ok, bf16_t* __restrict__ out, float* __restrict__ resid,
-    RowVec gate, LnFold ln) {
+    RowVec gate, LnFold ln, AdaptersOf<EPI> adapters) {
     constexpr int ES = 2, NW = WGM * WGN;
     constexpr int TM = BM / WGM / 32, TN = BN / WGN / 32, FR = TM + TN, MF = TM * TN;
     constexpr int LA = BM / 8 / NW, NL = (BM + BN) / 8 / NW;      // 1 KB blocks per wavefront and slice: of X, of both
@@ -266,6 +267,11 @@ __global__ __launch_bounds__(WGM * WGN * 64) void gemm_pipe_kernel(
             }
         }
     }
+    if constexpr (EPI == FREE_EPI_ADAPT) {
+        if (n0 + wn * TN * 32 < N && m0 + wm * TM * 32 < M)
+            add_adapters<TM, TN>(adapters, m0 + wm * TM * 32 + l32, n0 + wn * TN * 32 + l32, lhi, M, acc);
+        __builtin_amdgcn_sched_barrier(0);
+    }
     if (nk > 1) wait_vm_barrier<NL>();
     else wait_vm_barrier<0>();
 
@@ -304,7 +310,7 @@ __global__ __launch_bounds__(WGM * WGN * 64) void gemm_pipe_kernel(
     constexpr int kSumBytes = kPrep ? BM * WGN * 2 * 4 : 0;
     static_assert(NW * kWaveStage + kSumBytes <= 2 * kStageBytes, "output staging must fit in the K-loop stages");
     float* row_sums = reinterpret_cast<float*>(lds + NW * kWaveStage);                   // kPrep: [BM][WGN][2]
-    write_tile<bf16_t, TM, TN, (kSeg ? FREE_EPI_GATE_RESID : EPI), (NW == 8 ? 4 : 0)>(acc, m0 + wm * TM * 32 + l32, n0 + wn * TN * 32, lane, M, N, vec_ok, bias,
+    write_tile<bf16_t, TM, TN, (kSeg ? FREE_EPI_GATE_RESID : EPI == FREE_EPI_ADAPT ? FREE_EPI_BIAS : EPI), (NW == 8 ? 4 : 0)>(acc, m0 + wm * TM * 32 + l32, n0 + wn * TN * 32, lane, M, N, vec_ok, bias,
                                                        out, resid, gate, lds + wave * kWaveStage, ln, ln_a,
                                                        row_sums + (wm * TM * 32 * WGN + wn) * 2, WGN * 2);
     if constexpr (kPrep) {
@@ -331,7 +337,7 @@ struct Args {
 };
 
 template <int BM, int BN, int WGM, int WGN, int EPI>
-int32_t launch_one(const Args& a, const LnFold& ln) {
+int32_t launch_one(const Args& a, const LnFold& ln, const AdaptersOf<EPI>& adapters = {}) {
     const int tiles_m = (a.M + BM - 1) / BM, tiles_n = (a.N + BN - 1) / BN;
     const size_t lds = 2 * static_cast<size_t>(BM + BN) * kRowBytes;
     auto kern = gemm_pipe_kernel<BM, BN, WGM, WGN, EPI>;
@@ -352,7 +358,7 @@ int32_t launch_one(const Args& a, const LnFold& ln) {
         group_m = std::max(1, (per_xcd + tiles_n / 2) / tiles_n);
     }
     hipLaunchKernelGGL(kern, dim3(total), dim3(WGM * WGN * 64), lds, a.s, a.X, a.W, a.bias, a.M, a.N, a.K, tiles_m, tiles_n,
-                       group_m, vec ? 1 : 0, a.out, a.resid, a.gate, ln);
+                       group_m, vec ? 1 : 0, a.out, a.resid, a.gate, ln, adapters);
     return launch_ok() ? FREE_OK : FREE_ERR_HIP;
 }
 
@@ -388,6 +394,22 @@ int32_t launch_linear_pipe(const bf16_t* X, const bf16_t* W, const float* bias, 
         case PIPE_192x128: return launch_tile<192, 128, 2, 4>(a, epi, f);
         case PIPE_160x128: return launch_tile<160, 128, 1, 4>(a, epi, f);
         case PIPE_128x128: return launch_tile<128, 128, 2, 4>(a, epi, f);
+    }
+    return FREE_ERR_RANGE;
+}
+
+int32_t launch_linear_pipe_adapters(const bf16_t* X, const bf16_t* W, const float* bias, int32_t M, int32_t N, int32_t K, bf16_t* out, hipStream_t s,
+                                    PipeTile tile, const AdapterTerm& term) {
+    const Args a{X, W, bias, M, N, K, out, nullptr, RowVec{nullptr, 0, 1}, s};
+    const LnFold f{};
+    switch (tile) {
+        case PIPE_256x256: return launch_one<256, 256, 2, 4, FREE_EPI_ADAPT>(a, f, term);
+        case PIPE_384x192: return launch_one<384, 192, 4, 2, FREE_EPI_ADAPT>(a, f, term);
+        case PIPE_256x192: return launch_one<256, 192, 4, 2, FREE_EPI_ADAPT>(a, f, term);
+        case PIPE_192x256: return launch_one<192, 256, 2, 4, FREE_EPI_ADAPT>(a, f, term);
+        case PIPE_192x128: return launch_one<192, 128, 2, 4, FREE_EPI_ADAPT>(a, f, term);
+        case PIPE_160x128: return launch_one<160, 128, 1, 4, FREE_EPI_ADAPT>(a, f, term);
+        case PIPE_128x128: return launch_one<128, 128, 2, 4, FREE_EPI_ADAPT>(a, f, term);
     }
     return FREE_ERR_RANGE;
 }

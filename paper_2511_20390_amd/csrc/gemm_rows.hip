@@ -24,6 +24,7 @@
 // what the small tiles buy is wavefronts: 512 rows 61, 59, 64, 217 -> 44, 26, 64, 89 (MLP-1 keeps its 96 x 128).
 #include <algorithm>
 
+#include "adapter_term.h"
 #include "free_internal.h"
 #include "gemm_dma.h"
 
@@ -34,7 +35,7 @@ namespace {
 template <typename T, int BM, int BN, int WGM, int WGN, int S, int EPI>
 __global__ __launch_bounds__(WGM * WGN * 64) void gemm_rows_kernel(
     const T* __restrict__ X, const T* __restrict__ W, const float* __restrict__ bias, int32_t M, int32_t N, int32_t K,
-    int32_t tiles_m, int32_t tiles_n, T* __restrict__ out, float* __restrict__ resid, RowVec gate, int32_t from_zero) {
+    int32_t tiles_m, int32_t tiles_n, T* __restrict__ out, float* __restrict__ resid, RowVec gate, int32_t from_zero, AdaptersOf<EPI> adapters) {
     constexpr bool kF32 = std::is_same<T, float>::value;
     constexpr bool kSeg = EPI == FREE_EPI_GATE_RESID_SEG, kResid = EPI == FREE_EPI_GATE_RESID || kSeg;
     constexpr bool kGelu = EPI == FREE_EPI_BIAS_GELU, kPart = EPI == FREE_EPI_PARTIAL;
@@ -169,6 +170,10 @@ __global__ __launch_bounds__(WGM * WGN * 64) void gemm_rows_kernel(
 #pragma unroll
     for (int p = 0; p < S; ++p)
         if (p < nk) issue(p, p, 0, NL);
+    if constexpr (EPI == FREE_EPI_ADAPT) {
+        if (n0 + wn * TN * 32 < N && m0 + wm * TM * 32 < M) add_adapters<TM, TN>(adapters, gm_lane, n0 + wn * TN * 32 + l32, lhi, M, acc);
+        __builtin_amdgcn_sched_barrier(0);
+    }
     arrive(std::min(nk - 1, S - 1));
 #pragma unroll
     for (int ks = 0; ks < 4; ++ks) load_frags(0, 0, ks);
@@ -337,7 +342,7 @@ struct Args {
 };
 
 template <typename T, int BM, int BN, int WGM, int WGN, int S, int EPI>
-int32_t launch_one(const Args<T>& a) {
+int32_t launch_one(const Args<T>& a, const AdaptersOf<EPI>& adapters = {}) {
     const int tiles_m = (a.M + BM - 1) / BM, tiles_n = (a.N + BN - 1) / BN;
     const size_t lds = S * static_cast<size_t>(BM + BN) * kRowBytes;
     auto kern = gemm_rows_kernel<T, BM, BN, WGM, WGN, S, EPI>;
@@ -345,7 +350,7 @@ int32_t launch_one(const Args<T>& a) {
     if (!limit.allow(reinterpret_cast<const void*>(kern), lds)) return FREE_ERR_HIP;
     constexpr int kParts = EPI == FREE_EPI_PARTIAL ? kSplitParts : 1;
     hipLaunchKernelGGL(kern, dim3(tiles_m * tiles_n * kParts), dim3(WGM * WGN * 64), lds, a.s, a.X, a.W, a.bias, a.M, a.N, a.K, tiles_m,
-                       tiles_n, a.out, a.resid, a.gate, a.from_zero ? 1 : 0);
+                       tiles_n, a.out, a.resid, a.gate, a.from_zero ? 1 : 0, adapters);
     return launch_ok() ? FREE_OK : FREE_ERR_HIP;
 }
 
@@ -394,6 +399,15 @@ int32_t launch_linear_rows(const bf16_t* X, const bf16_t* W, const float* bias, 
 int32_t launch_linear_rows(const float* X, const float* W, const float* bias, int32_t M, int32_t N, int32_t K, int32_t epi,
                            float* out, float* resid, RowVec gate, hipStream_t s, RowsTile tile) {
     return launch_rows(Args<float>{X, W, bias, M, N, K, out, resid, gate, s, false}, epi, tile);
+}
+
+int32_t launch_linear_rows_adapters(const bf16_t* X, const bf16_t* W, const float* bias, int32_t M, int32_t N, int32_t K, bf16_t* out, hipStream_t s,
+                                    RowsTile tile, const AdapterTerm& term) {
+    const Args<bf16_t> a{X, W, bias, M, N, K, out, nullptr, RowVec{nullptr, 0, 1}, s, false};
+    if (!linear_rows_covers(N, K, sizeof(bf16_t), bias, out, nullptr, a.gate)) return FREE_ERR_SHAPE;
+    if (tile == ROWS_64x64) return launch_one<bf16_t, 64, 64, 2, 2, 4, FREE_EPI_ADAPT>(a, term);
+    if (tile == ROWS_128x64) return launch_one<bf16_t, 128, 64, 2, 2, 3, FREE_EPI_ADAPT>(a, term);
+    return launch_one<bf16_t, 128, 128, 2, 4, 4, FREE_EPI_ADAPT>(a, term);
 }
 
 }  // namespace freemi
