@@ -594,7 +594,7 @@ int32_t free_op_gated_ffn_backward(const void* dout, const void* x, const void* 
  * Scores, probabilities' sums and results are summed in fp32; probabilities are rounded to dtype as operands of the second product.
  * The gradient, of the same inputs, out and lse: dq like q, dk and dv like k and v (each with its distance from row to row), written, not
  * added to, zero for keys that do not count; probabilities and the scores' gradient are rounded to dtype as operands of the products.
- * How sums are cut depends on the sizes alone.  1 <= dh <= 128, strides up to 2^22 values, Nq heads / kv_heads below 2^31 - 128,
+ * How sums are cut depends on the sizes alone.  2^-64 <= scale <= 2^64 (FREE_ERR_RANGE); 1 <= dh <= 128, strides up to 2^22 values, Nq heads / kv_heads below 2^31 - 128,
  * B kv_heads below 2^24, at most 2^31 - 1 workgroups of 32 query or key rows of a (sample, key head) (FREE_ERR_LIMIT). */
 size_t free_cross_attention_workspace_bytes(int32_t B, int32_t Nq, int32_t Nk, int32_t heads, int32_t kv_heads, int32_t dh, int32_t dtype,
                                             int32_t backward);

@@ -61,7 +61,7 @@ int32_t free_op_cross_attention(const void* q, int64_t q_stride, const void* k, 
                                 int32_t kv_heads, int32_t dh, float scale, int32_t dtype, void* out, int64_t out_stride, float* lse,
                                 void* workspace, size_t ws_bytes, void* stream) {
     FREE_CHECK(check_cross_sizes(B, Nq, Nk, heads, kv_heads, dh, dtype));
-    if (!(scale > 0.f) || !std::isfinite(scale)) return FREE_ERR_RANGE;
+    if (!(scale >= 0x1p-64f && scale <= 0x1p64f)) return FREE_ERR_RANGE;
     const int64_t nq = static_cast<int64_t>(B) * Nq, nk = static_cast<int64_t>(B) * Nk, wq = static_cast<int64_t>(heads) * dh, wk = static_cast<int64_t>(kv_heads) * dh;
     if (nq == 0) return FREE_OK;
     FREE_CHECK(check_rows(q, q_stride, nq, wq, dtype));
@@ -99,7 +99,7 @@ int32_t free_op_cross_attention_backward(const void* dout, int64_t dout_stride, 
                                          int64_t dq_stride, void* dk, int64_t dk_stride, void* dv, int64_t dv_stride, void* workspace,
                                          size_t ws_bytes, void* stream) {
     FREE_CHECK(check_cross_sizes(B, Nq, Nk, heads, kv_heads, dh, dtype));
-    if (!(scale > 0.f) || !std::isfinite(scale)) return FREE_ERR_RANGE;
+    if (!(scale >= 0x1p-64f && scale <= 0x1p64f)) return FREE_ERR_RANGE;
     const int64_t nq = static_cast<int64_t>(B) * Nq, nk = static_cast<int64_t>(B) * Nk, wq = static_cast<int64_t>(heads) * dh, wk = static_cast<int64_t>(kv_heads) * dh;
     if (nq == 0 && nk == 0) return FREE_OK;
     FREE_CHECK(check_rows(q, q_stride, nq, wq, dtype));

@@ -8,8 +8,9 @@
 // that the half-waves hold in a register).  A 16-byte chunk of a row is 8 values or 4, one instruction or four: the loops are the same.
 #pragma once
 
-#include "buffer_range.h"
-#include "free_internal.h"
+#include <type_traits>
+
+#include "gemm_dma.h"
 #include "lanes.h"
 
 namespace freemi {
@@ -156,8 +157,236 @@ __device__ __forceinline__ xu32x4_t transposed_chunk(const char* lo, const char*
     return __builtin_bit_cast(xu32x4_t, v);
 }
 
+// Loads that a loop's products use have arrived: without this the compiler waits for them in the loop, and there for every load that the loop
+// itself has requested since.
+template <int N>
+__device__ __forceinline__ void arrived(xu32x4_t (&v)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) asm volatile("" : "+v"(v[i]));
+}
+
+__device__ __forceinline__ int over_group(int row, int group) { return group == 1 ? row : row / group; }
+
 // which of the 64 (or, with 32 keys per tile, low 32) keys from kv0 on count
 __device__ __forceinline__ uint64_t keys_below(int left) { return left >= 64 ? ~0ull : left <= 0 ? 0ull : (1ull << left) - 1; }
+
+// ---- tiles of streamed rows in LDS.  A tile is read by rows (16 bytes of 32 rows: scores) and by columns (transposing reads of 4 rows x 64 bytes; fp32
+// 32 values of a row), and its chunks are at places that keep the lanes of either off each other's banks (64 banks, 16 chunks):
+//   rows of 4 or 12 chunks: 16 rows of one chunk c, four next to each other on every fourth place -> c ^ (row / 4 % 4)
+//   rows of 10: every second place, eight rows of them -> c ^ (row / 8 % 2)      rows of 8 and 16: likewise, and the four rows of a
+//   transposing read, which start at the same bank, on different groups of four places
+// fp32: rows of an odd number of chunks.
+template <typename T, int DP>
+struct Tile {
+    using H = HeadShape<T, DP>;
+    static constexpr int kRows = sizeof(T) == 2 ? 64 : 32;
+    static constexpr int CHP = sizeof(T) == 2 ? H::CH : H::CH | 1;                // chunks from row to row
+    static constexpr int kPitch = CHP * 16;
+    static constexpr int kBytes = kRows * kPitch + 128;  // (columns past a row's end are read, and dropped)
+    static_assert(sizeof(T) == 4 || CHP == 4 || CHP == 8 || CHP == 10 || CHP == 12 || CHP == 16, "a place for every chunk");
+    static __device__ __forceinline__ int turn(int row) {
+        if constexpr (sizeof(T) == 4) return 0;
+        else if constexpr (CHP == 16) return (row & 3) << 2 | (row >> 2 & 3);
+        else if constexpr (CHP == 8) return (row >> 1 & 1) << 2 | (row >> 2 & 3);
+        else if constexpr (CHP == 10) return row >> 3 & 1;
+        else return row >> 2 & 3;
+    }
+    static __device__ __forceinline__ int at(int row, int c) { return row * kPitch + ((c ^ turn(row)) << 4); }
+};
+
+constexpr int kStreamThreads = 256, kNowhere = 0x7fffffff;       // a byte offset behind every buffer: reads as zero
+
+// Brings tiles of one tensor's rows into LDS.  bf16 rows of whole chunks go there without registers in between (a lane's place in LDS is given,
+// so it fetches the chunk that belongs there); others through registers: request() ahead of a tile's products, deliver() behind them.
+template <typename T, int DP, bool kVec>
+struct TileStream {
+    using TL = Tile<T, DP>;
+    static constexpr bool kDirect = sizeof(T) == 2 && kVec;
+    static constexpr int E = TL::H::E, CH = TL::H::CH, kBlocks = TL::kRows * TL::kPitch / 1024, kWaves = kStreamThreads / 64;
+    static constexpr int N = kDirect ? (kBlocks + kWaves - 1) / kWaves : (TL::kRows * CH + kStreamThreads - 1) / kStreamThreads;
+    static_assert(!kDirect || TL::kRows * TL::kPitch % 1024 == 0, "whole blocks");
+    xu32x4_t reg[kDirect ? 1 : N];
+
+    // Row r of the tile is place(r) bytes behind base, whose buffer ends with the last row that there is.  valid: the rows that count, where
+    // `masked` (others read as zero).  lds: the tile.
+    template <typename Place>
+    __device__ __forceinline__ void request(const T* base, int64_t bytes, uint32_t lds, int wave, int lane, int dh, bool masked, uint64_t valid, Place&& place) {
+        if constexpr (kDirect) {
+            const u32x4_t rsrc = make_rsrc(base, bytes);
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const int block = wave + kWaves * i;
+                if (kBlocks % kWaves != 0 && block >= kBlocks) break;
+                const int slot = block * 64 + lane, row = slot / TL::CHP, c = (slot % TL::CHP) ^ TL::turn(row);
+                int off = c * E < dh ? place(row) + c * 16 : kNowhere;
+                if (masked) off = valid >> row & 1 ? off : kNowhere;
+                dma_1k(lds + block * 1024, off, rsrc, 0);
+            }
+        } else {
+            const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(base), 0, static_cast<int>(range_bytes(bytes)), 0x00020000);
+            const int tid = wave * 64 + lane;
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const int idx = tid + kStreamThreads * i, row = idx / CH, c = idx % CH;
+                if (idx < TL::kRows * CH) reg[i] = buffer_chunk<T, kVec>(rsrc, place(row) + c * 16, c, dh);
+            }
+        }
+    }
+    __device__ __forceinline__ void deliver(char* tile, int tid, bool masked, uint64_t valid) {
+        if constexpr (!kDirect) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const int idx = tid + kStreamThreads * i, row = idx / CH, c = idx % CH;
+                if (idx < TL::kRows * CH) {
+                    if (masked && !(valid >> row & 1)) reg[i] = xu32x4_t{0, 0, 0, 0};
+                    *reinterpret_cast<xu32x4_t*>(tile + TL::at(row, c)) = reg[i];
+                }
+            }
+        }
+    }
+    // everything requested and delivered is in LDS, for the whole workgroup
+    static __device__ __forceinline__ void settle() {
+        if constexpr (kDirect) wait_vm_barrier<0>();
+        else __syncthreads();
+    }
+};
+
+// The operands of a product are read from LDS ahead of the products before it: a wavefront that reads, waits and multiplies in turn spends
+// its time on the latency of LDS (dk and dv of 32760 queries to 512 keys of 16 heads of 128, 530 -> 385 us).  `fence` keeps the compiler from putting
+// the reads back behind the products.
+__device__ __forceinline__ void fence() { __builtin_amdgcn_sched_barrier(0); }
+
+// chunks of a row that are read together (fp32: its products take eight times as long per chunk)
+template <typename T, int DP>
+constexpr int kRowGroup = sizeof(T) == 4 ? 4 : HeadShape<T, DP>::KSTEPS <= 5 ? HeadShape<T, DP>::KSTEPS : HeadShape<T, DP>::KSTEPS / 2;
+
+// the row operands of the block of 32 rows from row0 on: a group of chunks from `first` on
+template <typename T, int DP>
+__device__ __forceinline__ void read_rows(const char* tile, int row0, int lane, int first, xu32x4_t (&f)[kRowGroup<T, DP>]) {
+    const int row = block_row<T>(lane & 31), g = lane >> 5;
+    const char* const base = tile + row0 * Tile<T, DP>::kPitch;
+#pragma unroll
+    for (int k = 0; k < kRowGroup<T, DP>; ++k)
+        if (first + k < HeadShape<T, DP>::KSTEPS) f[k] = *reinterpret_cast<const xu32x4_t*>(base + Tile<T, DP>::at(row, 2 * (first + k) + g));
+}
+
+// acc += block . own, with the first group of the block's rows in f
+template <typename T, int DP>
+__device__ __forceinline__ void row_products(const char* tile, int row0, int lane, xu32x4_t (&f)[kRowGroup<T, DP>],
+                                             const xu32x4_t (&own)[HeadShape<T, DP>::KSTEPS], xf32x16_t& acc) {
+    constexpr int G = kRowGroup<T, DP>, KSTEPS = HeadShape<T, DP>::KSTEPS;
+#pragma unroll
+    for (int first = 0; first < KSTEPS; first += G) {
+        xu32x4_t next[G];
+        if (first + G < KSTEPS) {
+            read_rows<T, DP>(tile, row0, lane, first + G, next);
+            fence();
+        }
+#pragma unroll
+        for (int k = 0; k < G; ++k)
+            if (first + k < KSTEPS) chunk_product<T>(f[k], own[first + k], acc);
+#pragma unroll
+        for (int k = 0; k < G; ++k) f[k] = next[k];
+    }
+}
+
+// Column operands of a block: bf16, for 16 of its rows and all columns; fp32, for two registers (two rows each)
+template <typename T, int DP>
+struct Columns {
+    using TL = Tile<T, DP>;
+    static constexpr int DT = HeadShape<T, DP>::DT;
+    static constexpr int kSteps = sizeof(T) == 2 ? 2 : 8;        // parts of a block
+    using Operand = std::conditional_t<sizeof(T) == 2, xu32x4_t, xu32x2_t>;
+    Operand f[DT];
+    __device__ __forceinline__ void read(const char* tile, int row0, int lane, int step) {
+        const int l32 = lane & 31, g = lane >> 5;
+        const char* const base = tile + row0 * TL::kPitch;
+        if constexpr (sizeof(T) == 2) {
+            const int row = 8 * g + ((lane & 15) >> 2), c = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1), in = 8 * (lane & 1);
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt)
+                f[dt] = transposed_chunk(base + step * 16 * TL::kPitch + TL::at(row, 4 * dt + c) + in, base + step * 16 * TL::kPitch + TL::at(row + 4, 4 * dt + c) + in);
+        } else {
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+                    f[dt][e] = *reinterpret_cast<const uint32_t*>(base + register_row<T>(2 * step + e, g) * TL::kPitch + (32 * dt + l32) * 4);
+        }
+    }
+    // o[d, column] += the part's rows times s, whose registers the part has
+    __device__ __forceinline__ void multiply(const xf32x16_t& s, int step, xf32x16_t (&o)[DT]) const {
+        if constexpr (sizeof(T) == 2) {
+            const int h = 8 * step;
+            const xu32x4_t pk = pack8({s[h], s[h + 1], s[h + 2], s[h + 3], s[h + 4], s[h + 5], s[h + 6], s[h + 7]});
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) chunk_product<T>(f[dt], pk, o[dt]);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+#pragma unroll
+                for (int dt = 0; dt < DT; ++dt) o[dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(f[dt][e]), s[2 * step + e], o[dt], 0, 0, 0);
+        }
+    }
+};
+
+// o[d, column] += sum over the 32 rows from row0 on of tile[row, d] s[row, column], the first part's operands in c
+template <typename T, int DP>
+__device__ __forceinline__ void column_products(const char* tile, int row0, int lane, Columns<T, DP>& c, const xf32x16_t& s,
+                                                xf32x16_t (&o)[HeadShape<T, DP>::DT]) {
+#pragma unroll
+    for (int step = 0; step < Columns<T, DP>::kSteps; ++step) {
+        Columns<T, DP> next;
+        if (step + 1 < Columns<T, DP>::kSteps) {
+            next.read(tile, row0, lane, step + 1);
+            fence();
+        }
+        c.multiply(s, step, o);
+        c = next;
+    }
+}
+
+// the keys of sample b that can count
+__device__ __forceinline__ int attended(const CrossArgs& a, int b) {
+    if (!a.key_len) return a.Nk;
+    const int n = a.key_len[b];
+    return n < 0 ? 0 : n < a.Nk ? n : a.Nk;
+}
+
+// Keys and values of a (sample, key head), tile by tile, and which of a tile's keys count.  The mask of a tile is requested a tile ahead of its rows.
+template <typename T, int DP, bool kVec>
+struct KeyStream {
+    using TL = Tile<T, DP>;
+    TileStream<T, DP, kVec> k, v;
+    const T *kp, *vp;
+    const uint8_t* mask;
+    int k_row, v_row, len, dh;
+    uint32_t mask_byte = 1;
+    __device__ __forceinline__ KeyStream(const CrossArgs& a, int b, int kvh)
+        : kp(static_cast<const T*>(a.k) + static_cast<int64_t>(b) * a.Nk * a.k_stride + static_cast<int64_t>(kvh) * a.dh),
+          vp(static_cast<const T*>(a.v) + static_cast<int64_t>(b) * a.Nk * a.v_stride + static_cast<int64_t>(kvh) * a.dh),
+          mask(a.key_mask ? a.key_mask + static_cast<int64_t>(b) * a.Nk : nullptr),
+          k_row(static_cast<int>(a.k_stride)), v_row(static_cast<int>(a.v_stride)), len(attended(a, b)), dh(a.dh) {}
+    __device__ __forceinline__ int tiles() const { return (len + TL::kRows - 1) / TL::kRows; }
+    __device__ __forceinline__ void request_mask(int t, int lane) {
+        if (mask) mask_byte = lane < len - t * TL::kRows ? mask[t * TL::kRows + lane] : 0;
+    }
+    // of the tile whose mask was requested last
+    __device__ __forceinline__ uint64_t valid_of(int t) const {
+        const uint64_t v = keys_below(min(len - t * TL::kRows, TL::kRows));
+        return mask ? v & __ballot(mask_byte != 0) : v;
+    }
+    __device__ __forceinline__ void request(int t, uint32_t tile_k, uint32_t tile_v, int wave, int lane, uint64_t valid) {
+        constexpr int ES = static_cast<int>(sizeof(T));
+        const int64_t first = static_cast<int64_t>(t) * TL::kRows, rows = len - first;
+        k.request(kp + first * k_row, ((rows - 1) * k_row + dh) * ES, tile_k, wave, lane, dh, mask != nullptr, valid, [&](int r) { return r * k_row * ES; });
+        v.request(vp + first * v_row, ((rows - 1) * v_row + dh) * ES, tile_v, wave, lane, dh, mask != nullptr, valid, [&](int r) { return r * v_row * ES; });
+    }
+    __device__ __forceinline__ void deliver(char* tile_k, char* tile_v, int tid, uint64_t valid) {
+        k.deliver(tile_k, tid, mask != nullptr, valid);
+        v.deliver(tile_v, tid, mask != nullptr, valid);
+    }
+};
 
 }  // namespace
 

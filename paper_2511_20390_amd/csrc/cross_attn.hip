@@ -21,7 +21,7 @@ namespace freemi {
 
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = kStreamThreads;
 constexpr int kFewRows = 32;
 constexpr float kLazy = 8.0f;                     // log2 by which a maximum may grow before the sums are rescaled
 constexpr float kNoScore = -3.402823466e38f;      // a part's maximum where it has keys and all their scores are -inf
@@ -32,18 +32,9 @@ struct Parts {
     float *o, *ml;                                // [..][dh] sums, [..][2] maximum (of the scaled scores, log2) and sum
 };
 
-template <typename T>
-constexpr int kTileKeys = sizeof(T) == 2 ? 64 : 32;
-
-__device__ __forceinline__ int attended(const CrossArgs& a, int b) {
-    if (!a.key_len) return a.Nk;
-    const int n = a.key_len[b];
-    return n < 0 ? 0 : n < a.Nk ? n : a.Nk;
-}
-
 // The end of a row: out and lse, or a part's sums.  m: the maximum that l and o are relative to (log2 of the scaled scores).
 template <typename T, bool kVec, int DT>
-__device__ __forceinline__ void write_row(const CrossArgs& a, const Parts& pt, int part, int64_t pair, int b, int kvh, int64_t r, int g, float m, float l,
+__device__ __forceinline__ void write_row(const CrossArgs& a, const Parts& pt, int part, int64_t pair, int b, int kvh, int r, int g, float m, float l,
                                           bool any, const xf32x16_t (&o)[DT]) {
     const int group = a.heads / a.kv_heads;
     const int64_t rows = static_cast<int64_t>(a.Nq) * group;
@@ -54,19 +45,14 @@ __device__ __forceinline__ void write_row(const CrossArgs& a, const Parts& pt, i
         for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
             for (int e4 = 0; e4 < 4; ++e4)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int d = 32 * dt + 8 * e4 + 4 * g + i;
-                    if (d < a.dh) dst[d] = o[dt][4 * e4 + i];
-                }
+                store4<float, kVec>(dst, 32 * dt + 8 * e4 + 4 * g, a.dh, o[dt][4 * e4], o[dt][4 * e4 + 1], o[dt][4 * e4 + 2], o[dt][4 * e4 + 3]);
         if (g == 0) {
             pt.ml[2 * at] = any && m == -INFINITY ? kNoScore : m;
             pt.ml[2 * at + 1] = l;
         }
         return;
     }
-    const int64_t token = r / group;
-    const int head = kvh * group + static_cast<int>(r - token * group);
+    const int token = over_group(r, group), head = kvh * group + r - token * group;
     const float inv = any ? 1.0f / l : 0.f;
     T* dst = static_cast<T*>(a.out) + (static_cast<int64_t>(b) * a.Nq + token) * a.out_stride + static_cast<int64_t>(head) * a.dh;
 #pragma unroll
@@ -135,26 +121,19 @@ __device__ __forceinline__ void add_values(const char* v, int lane, const xf32x1
     }
 }
 
-// bytes from a key's row of K to the next in LDS: an odd number of chunks (reads of 16 bytes from 16 rows on different banks)
-template <typename T, int DP>
-constexpr int kKeyRow = (HeadShape<T, DP>::CH | 1) * 16;
-// ... of V: bf16, 4 rows x 64 bytes of a transposing read on different banks; fp32, rows four apart on the other 32 banks
+// bytes from a value's row to the next (few rows): bf16, 4 rows x 64 bytes of a transposing read on different banks; fp32, rows four apart on the other 32 banks
 template <typename T, int DP>
 constexpr int kValueRow = sizeof(T) == 4 ? (DP + 8) * 4 : DP <= 32 ? 64 : DP <= 96 ? 192 : 320;
 
 // KS wavefronts share the keys of a block of 32 queries
 template <typename T, int DP, int KS, bool kVec>
-__global__ __launch_bounds__(kThreads, (sizeof(T) == 2 && DP <= 80 && KS == 1) ? 3 : 2) void cross_many_kernel(CrossArgs a, Parts pt, int32_t q_tiles) {
+__global__ __launch_bounds__(kThreads, (sizeof(T) == 2 && DP <= 64 && KS == 1 && kVec) ? 3 : 2) void cross_many_kernel(CrossArgs a, Parts pt, int32_t q_tiles) {
     using H = HeadShape<T, DP>;
-    constexpr int E = H::E, CH = H::CH, KSTEPS = H::KSTEPS, DT = H::DT;
-    constexpr int BKV = kTileKeys<T>, KBT = BKV / 32, KB = KBT / KS;      // keys of a tile, blocks of it, blocks per wavefront
-    constexpr int KROW = kKeyRow<T, DP>, VROW = kValueRow<T, DP>;
-    constexpr int kK = BKV * KROW, kV = BKV * VROW + (sizeof(T) == 4 ? 128 : 0);
-    constexpr int BQ = 128 / KS, NLD = (BKV * CH + kThreads - 1) / kThreads;
+    using TL = Tile<T, DP>;
+    constexpr int KSTEPS = H::KSTEPS, DT = H::DT;
+    constexpr int BKV = TL::kRows, KB = BKV / 32 / KS, BQ = 128 / KS;     // keys of a tile, 32-key blocks per wavefront, queries
     static_assert(KB >= 1, "a block of keys for each wavefront");
-    extern __shared__ __attribute__((aligned(16))) char lds[];
-    char* const sK = lds;
-    char* const sV = lds + 2 * kK;
+    extern __shared__ __attribute__((aligned(16))) char lds[];           // [stage][K, V]
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int l32 = lane & 31, g = lane >> 5;
@@ -167,89 +146,54 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 && DP <= 80 && KS == 1) ?
     const int pair = by_xcd ? id % kXcds + kXcds * (id / (kXcds * q_tiles)) : id / q_tiles;
     const int q_tile = by_xcd ? id / kXcds % q_tiles : id % q_tiles;
     const int kvh = pair % a.kv_heads, b = pair / a.kv_heads;
-    const int64_t rows = static_cast<int64_t>(a.Nq) * group;
-    const int64_t row = static_cast<int64_t>(q_tile) * BQ + qw * 32 + l32;
-    const int len = attended(a, b);
-    const int t0 = part * pt.tiles, t1 = min(t0 + pt.tiles, (len + BKV - 1) / BKV);
+    const int rows = a.Nq * group, row = q_tile * BQ + qw * 32 + l32;
+    KeyStream<T, DP, kVec> keys(a, b, kvh);
+    const int t0 = part * pt.tiles, t1 = min(t0 + pt.tiles, keys.tiles());
+    const uint32_t lds_base = lds_address(lds);
+    keys.request_mask(t0, lane);
+    uint64_t valid = keys.valid_of(t0);
+    if (t0 < t1) keys.request(t0, lds_base, lds_base + TL::kBytes, wave, lane, valid);
+    keys.request_mask(t0 + 1, lane);
 
-    const T* const kp = static_cast<const T*>(a.k) + static_cast<int64_t>(b) * a.Nk * a.k_stride + static_cast<int64_t>(kvh) * a.dh;
-    const T* const vp = static_cast<const T*>(a.v) + static_cast<int64_t>(b) * a.Nk * a.v_stride + static_cast<int64_t>(kvh) * a.dh;
-    const uint8_t* const mask = a.key_mask ? a.key_mask + static_cast<int64_t>(b) * a.Nk : nullptr;
-    const int k_row = static_cast<int>(a.k_stride) * static_cast<int>(sizeof(T)), v_row = static_cast<int>(a.v_stride) * static_cast<int>(sizeof(T));
-    xu32x4_t kreg[NLD], vreg[NLD];
-    uint32_t mask_next = 1;
-    const auto fetch = [&](int t) {
-        const int64_t kv0 = static_cast<int64_t>(t) * BKV;
-        const auto kb = rows_buffer(kp + kv0 * a.k_stride, len - kv0, a.k_stride, a.dh), vb = rows_buffer(vp + kv0 * a.v_stride, len - kv0, a.v_stride, a.dh);
-#pragma unroll
-        for (int i = 0; i < NLD; ++i) {
-            const int idx = tid + kThreads * i, r = idx / CH, c = idx % CH;
-            if (idx < BKV * CH) {
-                kreg[i] = buffer_chunk<T, kVec>(kb, r * k_row + c * 16, c, a.dh);
-                vreg[i] = buffer_chunk<T, kVec>(vb, r * v_row + c * 16, c, a.dh);
-            }
-        }
-        if (mask) mask_next = kv0 + lane < len ? mask[kv0 + lane] : 0;
-    };
-    const auto valid_of = [&](int t) {               // of the tile fetched last
-        const uint64_t v = keys_below(min(len - t * BKV, BKV));
-        return mask ? v & __ballot(mask_next != 0) : v;
-    };
-    const auto stash = [&](int stage, uint64_t valid) {
-#pragma unroll
-        for (int i = 0; i < NLD; ++i) {
-            const int idx = tid + kThreads * i, r = idx / CH, c = idx % CH;
-            if (idx < BKV * CH) {
-                *reinterpret_cast<xu32x4_t*>(sK + stage * kK + r * KROW + c * 16) = kreg[i];
-                if (mask && !(valid >> r & 1)) vreg[i] = xu32x4_t{0, 0, 0, 0};
-                *reinterpret_cast<xu32x4_t*>(sV + stage * kV + r * VROW + c * 16) = vreg[i];
-            }
-        }
-    };
-    if (t0 < t1) fetch(t0);
-
-    const int64_t q_row = row < rows ? row : rows - 1, q_token = q_row / group;
-    const int q_head = kvh * group + static_cast<int>(q_row - q_token * group);
+    const int q_row = row < rows ? row : rows - 1, q_token = over_group(q_row, group);
+    const int q_head = kvh * group + q_row - q_token * group;
     const T* const qp = static_cast<const T*>(a.q) + (static_cast<int64_t>(b) * a.Nq + q_token) * a.q_stride + static_cast<int64_t>(q_head) * a.dh;
     xu32x4_t qf[KSTEPS];
 #pragma unroll
     for (int ks = 0; ks < KSTEPS; ++ks) qf[ks] = row_chunk<T, kVec>(qp, 2 * ks + g, a.dh);
-
     xf32x16_t o[DT];
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) clear_tile(o[dt]);
     float m_ref = -INFINITY, l = 0.f;
     const float scale_log2 = a.scale * kLog2e;
-    uint64_t valid = 0;
     bool any = false;
-    if (t0 < t1) {
-        valid = valid_of(t0);
-        stash(0, valid);
-        if (t0 + 1 < t1) fetch(t0 + 1);
-    }
-    __syncthreads();
-    const int key_at = block_row<T>(l32);
+    if (t0 < t1) keys.deliver(lds, lds + TL::kBytes, tid, valid);
+    arrived(qf);
+    keys.k.settle();
     for (int t = t0; t < t1; ++t) {
-        const int stage = (t - t0) & 1;
-        xf32x16_t st[KB];
-#pragma unroll
-        for (int kb = 0; kb < KB; ++kb) clear_tile(st[kb]);
-        __builtin_amdgcn_s_setprio(2);
-#pragma unroll
-        for (int ks = 0; ks < KSTEPS; ++ks)
-#pragma unroll
-            for (int kb = 0; kb < KB; ++kb)
-                chunk_product<T>(*reinterpret_cast<const xu32x4_t*>(sK + stage * kK + ((kb0 + kb) * 32 + key_at) * KROW + (2 * ks + g) * 16), qf[ks], st[kb]);
-        __builtin_amdgcn_s_setprio(0);
-        uint64_t valid_next = 0;
+        const int stage = (t - t0) & 1, other = (stage ^ 1) * 2 * TL::kBytes;
+        const char *const sK = lds + stage * 2 * TL::kBytes, *const sV = sK + TL::kBytes;
+        const uint64_t valid_next = keys.valid_of(t + 1);
         if (t + 1 < t1) {
-            valid_next = valid_of(t + 1);
-            stash(stage ^ 1, valid_next);
-            if (t + 2 < t1) fetch(t + 2);
+            keys.request(t + 1, lds_base + other, lds_base + other + TL::kBytes, wave, lane, valid_next);
+            keys.request_mask(t + 2, lane);
         }
+        xf32x16_t st[KB];
+        xu32x4_t fk[KB][kRowGroup<T, DP>];
+        Columns<T, DP> cv;
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) {
+            clear_tile(st[kb]);
+            read_rows<T, DP>(sK, (kb0 + kb) * 32, lane, 0, fk[kb]);
+        }
+        fence();
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) row_products<T, DP>(sK, (kb0 + kb) * 32, lane, fk[kb], qf, st[kb]);
+        cv.read(sV, kb0 * 32, lane, 0);
+        fence();
         any |= valid != 0;
-        const uint64_t full = BKV == 64 ? ~0ull : 0xffffffffull;
-        if ((valid & full) != full) {
+        constexpr uint64_t kFull = BKV == 64 ? ~0ull : 0xffffffffull;
+        if (valid != kFull) {
 #pragma unroll
             for (int kb = 0; kb < KB; ++kb) {
                 const uint32_t bits = static_cast<uint32_t>(valid >> (32 * (kb0 + kb))) >> (sizeof(T) == 2 ? 8 * g : 4 * g);
@@ -259,17 +203,19 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 && DP <= 80 && KS == 1) ?
             }
         }
         softmax_step<KB, DT>(st, scale_log2, m_ref, l, o);
-        __builtin_amdgcn_s_setprio(2);
 #pragma unroll
-        for (int kb = 0; kb < KB; ++kb) add_values<T, DT, VROW>(sV + stage * kV + (kb0 + kb) * 32 * VROW, lane, st[kb], o);
-        __builtin_amdgcn_s_setprio(0);
+        for (int kb = 0; kb < KB; ++kb) {
+            column_products<T, DP>(sV, (kb0 + kb) * 32, lane, cv, st[kb], o);
+            if (kb + 1 < KB) cv.read(sV, (kb0 + kb + 1) * 32, lane, 0);
+        }
+        if (t + 1 < t1) keys.deliver(lds + other, lds + other + TL::kBytes, tid, valid_next);
         valid = valid_next;
-        __syncthreads();                             // the other stage is complete, this one free
+        keys.k.settle();
     }
     l = add_lane_xor<32>(l);
     if constexpr (KS == 2) {
         // the second half of the keys hands its sums to the first
-        static_assert(2 * DT * 4096 + 2 * 512 <= 2 * kK + 2 * kV, "the partial results must fit in the stages");
+        static_assert(2 * DT * 4096 + 2 * 512 <= 4 * TL::kBytes, "the partial results must fit in the stages");
         float* const ml = reinterpret_cast<float*>(lds) + qw * 128 + lane;
         char* const so = lds + 1024 + qw * DT * 4096 + lane * 16;
         if (kb0 > 0) {
@@ -350,6 +296,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void cross_few_ke
     float m_ref = -INFINITY, l = 0.f;
     const float scale_log2 = a.scale * kLog2e;
     bool any = false;
+    arrived(qf);
     for (int t = t0; t < t1; t += 4) {
         uint64_t valid = keys_below(min(len - t * 32, 32));
         if (mask) valid &= __ballot(mask_next != 0);
@@ -515,7 +462,7 @@ int32_t launch_shape(const CrossArgs& a, const Plan& p, const Parts& pt, hipStre
         hipLaunchKernelGGL(kern, dim3(static_cast<uint32_t>(blocks)), dim3(kThreads), lds, s, a, pt);
         return launch_ok() ? FREE_OK : FREE_ERR_HIP;
     }
-    const size_t lds = 2 * kTileKeys<T> * static_cast<size_t>(kKeyRow<T, DP> + kValueRow<T, DP>) + (sizeof(T) == 4 ? 256 : 0);
+    constexpr size_t lds = 4 * Tile<T, DP>::kBytes;
     const auto launch = [&](auto ks) {
         auto kern = cross_many_kernel<T, DP, decltype(ks)::value, kVec>;
         static LdsLimit limit;

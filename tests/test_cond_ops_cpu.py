@@ -43,7 +43,7 @@ def test_cross_attention_refusals(lib, call):
     assert call(lib, B=-1) == call(lib, Nq=-1) == call(lib, Nk=-1) == call(lib, heads=0) == call(lib, kv=0) == call(lib, dh=0) == b.FREE_ERR_SHAPE
     assert call(lib, heads=3) == call(lib, kv=4) == b.FREE_ERR_SHAPE
     assert call(lib, n=ODD) == b.FREE_ERR_SHAPE
-    for scale in (0.0, -1.0, float("nan"), float("inf")):
+    for scale in (0.0, -1.0, 2.0 ** -65, 2.0 ** 65, float("nan"), float("inf")):
         assert call(lib, scale=scale) == b.FREE_ERR_RANGE
     assert call(lib, dh=129) == call(lib, B=1 << 24) == call(lib, Nq=2**31 - 1) == call(lib, Nk=2**31 - 1) == b.FREE_ERR_LIMIT
     assert call(lib, B=1 << 23, kv=1, Nq=1 << 20) == call(lib, heads=1 << 18, kv=1 << 18) == b.FREE_ERR_LIMIT
