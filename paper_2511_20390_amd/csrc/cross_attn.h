@@ -270,8 +270,8 @@ __device__ __forceinline__ void read_rows(const char* tile, int row0, int lane, 
         if (first + k < HeadShape<T, DP>::KSTEPS) f[k] = *reinterpret_cast<const xu32x4_t*>(base + Tile<T, DP>::at(row, 2 * (first + k) + g));
 }
 
-// acc += block . own, with the first group of the block's rows in f
-template <typename T, int DP>
+// acc += block . own, with the first group of the block's rows in f.  kAhead: see fence; without it the compiler orders reads and products.
+template <typename T, int DP, bool kAhead = true>
 __device__ __forceinline__ void row_products(const char* tile, int row0, int lane, xu32x4_t (&f)[kRowGroup<T, DP>],
                                              const xu32x4_t (&own)[HeadShape<T, DP>::KSTEPS], xf32x16_t& acc) {
     constexpr int G = kRowGroup<T, DP>, KSTEPS = HeadShape<T, DP>::KSTEPS;
@@ -280,7 +280,7 @@ __device__ __forceinline__ void row_products(const char* tile, int row0, int lan
         xu32x4_t next[G];
         if (first + G < KSTEPS) {
             read_rows<T, DP>(tile, row0, lane, first + G, next);
-            fence();
+            if constexpr (kAhead) fence();
         }
 #pragma unroll
         for (int k = 0; k < G; ++k)
@@ -331,7 +331,7 @@ struct Columns {
 };
 
 // o[d, column] += sum over the 32 rows from row0 on of tile[row, d] s[row, column], the first part's operands in c
-template <typename T, int DP>
+template <typename T, int DP, bool kAhead = true>
 __device__ __forceinline__ void column_products(const char* tile, int row0, int lane, Columns<T, DP>& c, const xf32x16_t& s,
                                                 xf32x16_t (&o)[HeadShape<T, DP>::DT]) {
 #pragma unroll
@@ -339,7 +339,7 @@ __device__ __forceinline__ void column_products(const char* tile, int row0, int 
         Columns<T, DP> next;
         if (step + 1 < Columns<T, DP>::kSteps) {
             next.read(tile, row0, lane, step + 1);
-            fence();
+            if constexpr (kAhead) fence();
         }
         c.multiply(s, step, o);
         c = next;

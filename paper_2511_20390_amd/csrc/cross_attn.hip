@@ -127,12 +127,16 @@ constexpr int kValueRow = sizeof(T) == 4 ? (DP + 8) * 4 : DP <= 32 ? 64 : DP <= 
 
 // KS wavefronts share the keys of a block of 32 queries
 template <typename T, int DP, int KS, bool kVec>
-__global__ __launch_bounds__(kThreads, (sizeof(T) == 2 && DP <= 64 && KS == 1 && kVec) ? 3 : 2) void cross_many_kernel(CrossArgs a, Parts pt, int32_t q_tiles) {
+constexpr bool kThreeWaves = sizeof(T) == 2 && DP <= 80 && KS == 1 && kVec;
+
+template <typename T, int DP, int KS, bool kVec>
+__global__ __launch_bounds__(kThreads, (kThreeWaves<T, DP, KS, kVec> ? 3 : 2)) void cross_many_kernel(CrossArgs a, Parts pt, int32_t q_tiles) {
     using H = HeadShape<T, DP>;
     using TL = Tile<T, DP>;
     constexpr int KSTEPS = H::KSTEPS, DT = H::DT;
     constexpr int BKV = TL::kRows, KB = BKV / 32 / KS, BQ = 128 / KS;     // keys of a tile, 32-key blocks per wavefront, queries
     static_assert(KB >= 1, "a block of keys for each wavefront");
+    constexpr bool kAhead = !kThreeWaves<T, DP, KS, kVec>;
     extern __shared__ __attribute__((aligned(16))) char lds[];           // [stage][K, V]
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -186,11 +190,13 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 && DP <= 64 && KS == 1 &&
             clear_tile(st[kb]);
             read_rows<T, DP>(sK, (kb0 + kb) * 32, lane, 0, fk[kb]);
         }
-        fence();
+        if constexpr (kAhead) fence();
 #pragma unroll
-        for (int kb = 0; kb < KB; ++kb) row_products<T, DP>(sK, (kb0 + kb) * 32, lane, fk[kb], qf, st[kb]);
-        cv.read(sV, kb0 * 32, lane, 0);
-        fence();
+        for (int kb = 0; kb < KB; ++kb) row_products<T, DP, kAhead>(sK, (kb0 + kb) * 32, lane, fk[kb], qf, st[kb]);
+        if constexpr (kAhead) {
+            cv.read(sV, kb0 * 32, lane, 0);
+            fence();
+        }
         any |= valid != 0;
         constexpr uint64_t kFull = BKV == 64 ? ~0ull : 0xffffffffull;
         if (valid != kFull) {
@@ -205,8 +211,8 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 && DP <= 64 && KS == 1 &&
         softmax_step<KB, DT>(st, scale_log2, m_ref, l, o);
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb) {
-            column_products<T, DP>(sV, (kb0 + kb) * 32, lane, cv, st[kb], o);
-            if (kb + 1 < KB) cv.read(sV, (kb0 + kb + 1) * 32, lane, 0);
+            if (!kAhead || kb > 0) cv.read(sV, (kb0 + kb) * 32, lane, 0);
+            column_products<T, DP, kAhead>(sV, (kb0 + kb) * 32, lane, cv, st[kb], o);
         }
         if (t + 1 < t1) keys.deliver(lds + other, lds + other + TL::kBytes, tid, valid_next);
         valid = valid_next;
