@@ -143,6 +143,29 @@ __device__ __forceinline__ void store4(T* row, int d, int dh, float a, float b, 
     }
 }
 
+// A lane's column of 32 DT values (register e of tile dt: value 32 dt + 8 (e / 4) + 4 (lane / 32) + e % 4) times `factor` to its row, those before dh.
+// bf16: the half-waves, which have four values of eight each, exchange them, so that a store is 16 bytes per lane and 32 next to each other: the memory
+// pipe takes as long for 8 bytes of 32 rows.
+template <typename T, bool kVec, int DT>
+__device__ __forceinline__ void store_column(T* row, int dh, int g, const xf32x16_t (&v)[DT], float factor, bool on) {
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) {
+        if constexpr (sizeof(T) == 2 && kVec) {
+#pragma unroll
+            for (int e8 = 0; e8 < 2; ++e8) {
+                const auto pair = [&](int e) { return pack_bf16_pair(v[dt][8 * e8 + e] * factor, v[dt][8 * e8 + e + 1] * factor); };
+                const xu32x2_t s0 = __builtin_amdgcn_permlane32_swap(pair(0), pair(4), false, false), s1 = __builtin_amdgcn_permlane32_swap(pair(2), pair(6), false, false);
+                const int d = 32 * dt + 16 * e8 + 8 * g;
+                if (on && d < dh) *reinterpret_cast<xu32x4_t*>(row + d) = xu32x4_t{s0[0], s1[0], s0[1], s1[1]};
+            }
+        } else if (on) {
+#pragma unroll
+            for (int e4 = 0; e4 < 4; ++e4)
+                store4<T, kVec>(row, 32 * dt + 8 * e4 + 4 * g, dh, v[dt][4 * e4] * factor, v[dt][4 * e4 + 1] * factor, v[dt][4 * e4 + 2] * factor, v[dt][4 * e4 + 3] * factor);
+        }
+    }
+}
+
 // 8 registers of a tile of scores' row order as operands of the next product; fp32 uses the registers as they are
 __device__ __forceinline__ xu32x4_t pack8(const float (&p)[8]) {
     return xu32x4_t{pack_bf16_pair(p[0], p[1]), pack_bf16_pair(p[2], p[3]), pack_bf16_pair(p[4], p[5]), pack_bf16_pair(p[6], p[7])};
@@ -344,6 +367,38 @@ __device__ __forceinline__ void column_products(const char* tile, int row0, int 
         c.multiply(s, step, o);
         c = next;
     }
+}
+
+// Tiles of two tensors' rows (keys and values; queries and their gradients) one after the other in LDS, bf16 rows of whole chunks, NW wavefronts: block
+// of 1 KB w, w + NW, ... of both is wavefront w's, so that every wavefront has as many loads in flight and a wait counts tiles.
+template <int DP, int NW>
+struct PairRing {
+    using TL = Tile<bf16_t, DP>;
+    static constexpr int kBlocks = TL::kRows * TL::kPitch / 1024, kSecond = kBlocks * 1024, N = (2 * kBlocks + NW - 1) / NW, kTileBytes = N * NW * 1024;
+    int off[N];                      // of this lane's chunks in a tile, bytes behind the tile's first row
+    // place(second, r): where row r of a tile is
+    template <typename Place>
+    __device__ __forceinline__ void aim(int wave, int lane, int dh, Place&& place) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int block = wave + NW * i, second = block >= kBlocks ? 1 : 0, slot = (block - second * kBlocks) * 64 + lane;
+            const int row = slot / TL::CHP, c = (slot % TL::CHP) ^ TL::turn(row);
+            off[i] = block < 2 * kBlocks && c * 8 < dh ? place(second, row) + c * 16 : kNowhere;
+            asm volatile("" : "+v"(off[i]));     // (kept, not computed again for every tile)
+        }
+    }
+    __device__ __forceinline__ void request(const u32x4_t& first, const u32x4_t& second, uint32_t tile, int wave) const {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int block = wave + NW * i;
+            dma_1k(tile + block * 1024, off[i], block >= kBlocks ? second : first, 0);
+        }
+    }
+};
+
+// rows [first, first + rows) of a tensor as a buffer
+__device__ __forceinline__ u32x4_t rows_rsrc(const bf16_t* p, int64_t first, int64_t rows, int64_t stride, int width) {
+    return make_rsrc(p + first * stride, rows > 0 ? ((rows - 1) * stride + width) * 2 : 0);
 }
 
 // the keys of sample b that can count

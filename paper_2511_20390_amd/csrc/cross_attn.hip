@@ -32,36 +32,24 @@ struct Parts {
     float *o, *ml;                                // [..][dh] sums, [..][2] maximum (of the scaled scores, log2) and sum
 };
 
-// The end of a row: out and lse, or a part's sums.  m: the maximum that l and o are relative to (log2 of the scaled scores).
+// The end of a row (on: there is one): out and lse, or a part's sums.  m: the maximum that l and o are relative to (log2 of the scaled scores).
 template <typename T, bool kVec, int DT>
-__device__ __forceinline__ void write_row(const CrossArgs& a, const Parts& pt, int part, int64_t pair, int b, int kvh, int r, int g, float m, float l,
-                                          bool any, const xf32x16_t (&o)[DT]) {
+__device__ __forceinline__ void write_row(const CrossArgs& a, const Parts& pt, int part, int64_t pair, int b, int kvh, int r, int g, float m, float l, bool any,
+                                          const xf32x16_t (&o)[DT], bool on) {
     const int group = a.heads / a.kv_heads;
-    const int64_t rows = static_cast<int64_t>(a.Nq) * group;
     if (pt.parts > 1) {
-        const int64_t at = (part * static_cast<int64_t>(a.B) * a.kv_heads + pair) * rows + r;
-        float* dst = pt.o + at * a.dh;
-#pragma unroll
-        for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-            for (int e4 = 0; e4 < 4; ++e4)
-                store4<float, kVec>(dst, 32 * dt + 8 * e4 + 4 * g, a.dh, o[dt][4 * e4], o[dt][4 * e4 + 1], o[dt][4 * e4 + 2], o[dt][4 * e4 + 3]);
-        if (g == 0) {
+        const int64_t at = (part * static_cast<int64_t>(a.B) * a.kv_heads + pair) * a.Nq * group + r;
+        store_column<float, kVec, DT>(pt.o + at * a.dh, a.dh, g, o, 1.0f, on);
+        if (on && g == 0) {
             pt.ml[2 * at] = any && m == -INFINITY ? kNoScore : m;
             pt.ml[2 * at + 1] = l;
         }
         return;
     }
     const int token = over_group(r, group), head = kvh * group + r - token * group;
-    const float inv = any ? 1.0f / l : 0.f;
-    T* dst = static_cast<T*>(a.out) + (static_cast<int64_t>(b) * a.Nq + token) * a.out_stride + static_cast<int64_t>(head) * a.dh;
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-        for (int e4 = 0; e4 < 4; ++e4)
-            store4<T, kVec>(dst, 32 * dt + 8 * e4 + 4 * g, a.dh, o[dt][4 * e4] * inv, o[dt][4 * e4 + 1] * inv, o[dt][4 * e4 + 2] * inv,
-                            o[dt][4 * e4 + 3] * inv);
-    if (a.lse && g == 0) a.lse[(static_cast<int64_t>(b) * a.heads + head) * a.Nq + token] = any ? (m + __builtin_log2f(l)) * kLn2 : -INFINITY;
+    T* const dst = static_cast<T*>(a.out) + (static_cast<int64_t>(b) * a.Nq + token) * a.out_stride + static_cast<int64_t>(head) * a.dh;
+    store_column<T, kVec, DT>(dst, a.dh, g, o, any ? 1.0f / l : 0.f, on);
+    if (on && a.lse && g == 0) a.lse[(static_cast<int64_t>(b) * a.heads + head) * a.Nq + token] = any ? (m + __builtin_log2f(l)) * kLn2 : -INFINITY;
 }
 
 // One online-softmax step of a query column: scores in st (KB blocks of 16 registers, those that do not count at -inf) -> probabilities in
@@ -248,8 +236,171 @@ __global__ __launch_bounds__(kThreads, (kThreeWaves<T, DP, KS, kVec> ? 3 : 2)) v
             }
         m_ref = m;
     }
-    if (row >= rows) return;
-    write_row<T, kVec, DT>(a, pt, part, pair, b, kvh, row, g, m_ref * scale_log2, l, any, o);
+    write_row<T, kVec, DT>(a, pt, part, pair, b, kvh, row, g, m_ref * scale_log2, l, any, o, row < rows);
+}
+
+// bf16 of whole chunks, eight wavefronts of 32 queries at a time.
+// kResident: all keys and values of a (sample, key head) fit in LDS.  They are brought there once, and each wavefront takes one block of queries after
+// the other, without a barrier, the next block's queries requested ahead.  Otherwise tiles pass through a ring of kRing, two of them under way
+// while one is multiplied: requested one ahead, a tile arrives later than the products of another take.
+constexpr int kRing = 3, kRingWaves = 8, kMaxTiles = 16;
+constexpr int kLdsBytes = 160 * 1024 - 256;
+
+template <int DP>
+constexpr int ring_tiles() { return (kLdsBytes - 128) / PairRing<DP, kRingWaves>::kTileBytes; }
+
+template <int DP, bool kResident>
+__global__ __launch_bounds__(kRingWaves * 64, 2) void cross_ring_kernel(CrossArgs a, Parts pt, int32_t chunks, int32_t blocks_per_chunk) {
+    using T = bf16_t;
+    using H = HeadShape<T, DP>;
+    using TL = Tile<T, DP>;
+    using Ring = PairRing<DP, kRingWaves>;
+    constexpr int KSTEPS = H::KSTEPS, DT = H::DT, BKV = TL::kRows;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    __shared__ uint64_t masks[kMaxTiles];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, g = lane >> 5;
+    const int pairs = a.B * a.kv_heads, group = a.heads / a.kv_heads, per_part = pairs * chunks;
+    const int part = blockIdx.x / per_part, id = blockIdx.x % per_part;
+    const bool by_xcd = pairs % kXcds == 0;          // what reads the same keys on one XCD
+    const int pair = by_xcd ? id % kXcds + kXcds * (id / (kXcds * chunks)) : id / chunks;
+    const int chunk = by_xcd ? id / kXcds % chunks : id % chunks;
+    const int kvh = pair % a.kv_heads, b = pair / a.kv_heads;
+    const int rows = a.Nq * group, blocks = (rows + 31) / 32;
+    const int len = attended(a, b), tiles = (len + BKV - 1) / BKV, t0 = part * pt.tiles, t1 = min(t0 + pt.tiles, tiles);
+    const bf16_t* const kp = static_cast<const T*>(a.k) + static_cast<int64_t>(b) * a.Nk * a.k_stride + static_cast<int64_t>(kvh) * a.dh;
+    const bf16_t* const vp = static_cast<const T*>(a.v) + static_cast<int64_t>(b) * a.Nk * a.v_stride + static_cast<int64_t>(kvh) * a.dh;
+    const uint8_t* const mask = a.key_mask ? a.key_mask + static_cast<int64_t>(b) * a.Nk : nullptr;
+    const uint32_t lds_base = lds_address(lds);
+    Ring ring;
+    ring.aim(wave, lane, a.dh, [&](int second, int r) { return r * static_cast<int>(second ? a.v_stride : a.k_stride) * 2; });
+    const auto request = [&](int t, int slot) {
+        const int64_t first = static_cast<int64_t>(t) * BKV;
+        ring.request(rows_rsrc(kp, first, len - first, a.k_stride, a.dh), rows_rsrc(vp, first, len - first, a.v_stride, a.dh), lds_base + slot * Ring::kTileBytes, wave);
+    };
+    const auto mask_bits = [&](int t) {              // of tile t's keys; waits for memory
+        const int key = t * BKV + lane;
+        return __ballot(key < len && mask[key] != 0);
+    };
+    // the values of keys that do not count are replaced, in LDS: they are multiplied by zeros, and may be NaN
+    const auto drop_values = [&](char* tile, uint64_t valid) {
+        if (valid == ~0ull) return;
+        for (int r = wave; r < BKV; r += kRingWaves)
+            if (!(valid >> r & 1) && lane < TL::CHP) *reinterpret_cast<xu32x4_t*>(tile + Ring::kSecond + r * TL::kPitch + lane * 16) = xu32x4_t{0, 0, 0, 0};
+    };
+    const auto load_queries = [&](int block, xu32x4_t (&f)[KSTEPS]) {
+        const int r = min(block * 32 + l32, rows - 1), token = over_group(r, group), head = kvh * group + r - token * group;
+        const T* const p = static_cast<const T*>(a.q) + (static_cast<int64_t>(b) * a.Nq + token) * a.q_stride + static_cast<int64_t>(head) * a.dh;
+#pragma unroll
+        for (int ks = 0; ks < KSTEPS; ++ks) f[ks] = row_chunk<T, true>(p, 2 * ks + g, a.dh);
+    };
+    const float scale_log2 = a.scale * kLog2e;
+    xf32x16_t o[DT];
+    xu32x4_t qf[KSTEPS];
+    float m_ref, l;
+    const auto begin = [&]() {
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) clear_tile(o[dt]);
+        m_ref = -INFINITY;
+        l = 0.f;
+    };
+    const auto multiply = [&](const char* tile, uint64_t valid) {
+        const char* const values = tile + Ring::kSecond;
+        xf32x16_t st[2];
+        xu32x4_t fk[2][kRowGroup<T, DP>];
+        Columns<T, DP> cv;
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+            clear_tile(st[kb]);
+            read_rows<T, DP>(tile, kb * 32, lane, 0, fk[kb]);
+        }
+        fence();
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) row_products<T, DP>(tile, kb * 32, lane, fk[kb], qf, st[kb]);
+        cv.read(values, 0, lane, 0);
+        fence();
+        if (valid != ~0ull) {
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb) {
+                const uint32_t bits = static_cast<uint32_t>(valid >> (32 * kb)) >> (8 * g);
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    if (!(bits >> register_row<T>(e, 0) & 1)) st[kb][e] = -INFINITY;
+            }
+        }
+        softmax_step<2, DT>(st, scale_log2, m_ref, l, o);
+        column_products<T, DP>(values, 0, lane, cv, st[0], o);
+        cv.read(values, 32, lane, 0);
+        column_products<T, DP>(values, 32, lane, cv, st[1], o);
+    };
+    const auto finish = [&](int block, bool any) {
+        l = add_lane_xor<32>(l);
+        const int r = block * 32 + l32;
+        write_row<T, true, DT>(a, pt, part, pair, b, kvh, r, g, m_ref * scale_log2, l, any, o, r < rows);
+    };
+
+    if constexpr (kResident) {
+        for (int t = 0; t < tiles; ++t) request(t, t);
+        const int first = chunk * blocks_per_chunk, last = min(first + blocks_per_chunk, blocks);
+        if (first + wave < last) load_queries(first + wave, qf);
+        bool any = tiles > 0;
+        if (mask) {
+            for (int t = wave; t < tiles; t += kRingWaves) {
+                const uint64_t bits = mask_bits(t);
+                if (lane == 0) masks[t] = bits;
+            }
+        }
+        wait_vm_barrier<0>();
+        if (mask) {
+            any = false;
+            for (int t = 0; t < tiles; ++t) {
+                const uint64_t valid = masks[t];
+                any |= valid != 0;
+                drop_values(lds + t * Ring::kTileBytes, valid);
+            }
+            __syncthreads();
+        }
+        for (int block = first + wave; block < last; block += kRingWaves) {
+            xu32x4_t next[KSTEPS];
+            arrived(qf);
+            if (block + kRingWaves < last) load_queries(block + kRingWaves, next);
+            begin();
+            for (int t = 0; t < tiles; ++t) {
+                const uint64_t valid = mask ? masks[t] : keys_below(len - t * BKV);
+                multiply(lds + t * Ring::kTileBytes, valid);
+            }
+            finish(block, any);
+#pragma unroll
+            for (int ks = 0; ks < KSTEPS; ++ks) qf[ks] = next[ks];
+        }
+    } else {
+        const int block = min(chunk * kRingWaves + wave, blocks - 1);
+        const bool mine = chunk * kRingWaves + wave < blocks;
+#pragma unroll
+        for (int s = 0; s < kRing - 1; ++s)
+            if (t0 + s < t1) request(t0 + s, s);
+        load_queries(block, qf);
+        begin();
+        bool any = false;
+        arrived(qf);
+        int slot = 0, free_slot = kRing - 1;
+        for (int t = t0; t < t1; ++t) {
+            const uint64_t valid = mask ? mask_bits(t) : keys_below(len - t * BKV);
+            any |= valid != 0;
+            // tile t has arrived, and everybody is done with the one before it
+            if (t + kRing - 1 <= t1) wait_vm_barrier<(kRing - 2) * Ring::N>();
+            else wait_vm_barrier<0>();
+            char* const tile = lds + slot * Ring::kTileBytes;
+            if (mask && valid != ~0ull) {
+                drop_values(tile, valid);
+                __syncthreads();
+            }
+            if (t + kRing - 1 < t1) request(t + kRing - 1, free_slot);
+            multiply(tile, valid);
+            free_slot = slot;
+            slot = slot + 1 == kRing ? 0 : slot + 1;
+        }
+        finish(mine ? block : rows, any);
+    }
 }
 
 // Up to 32 rows per (sample, head): workgroup (part, pair), its four wavefronts take the part's key tiles of 32 in turn
@@ -375,8 +526,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void cross_few_ke
                 for (int c = 0; c < 4; ++c) o[dt][4 * e4 + c] += aw * v[c];
             }
     }
-    if (row >= rows) return;
-    write_row<T, kVec, DT>(a, pt, part, pair, b, kvh, row, g, m * scale_log2, l, any, o);
+    write_row<T, kVec, DT>(a, pt, part, pair, b, kvh, row, g, m * scale_log2, l, any, o, row < rows);
 }
 
 // The parts of a row's sums, added in order: WPR wavefronts per row take them in turn, lane p having part p's maximum and sum (at most 64
@@ -424,21 +574,41 @@ __global__ __launch_bounds__(kThreads) void cross_join_kernel(CrossArgs a, Parts
 
 // How a problem is cut; by its sizes alone (a workspace's size must not depend on the device)
 struct Plan {
-    bool few;
+    bool few, ring, resident;
     int ks;                                       // wavefronts that share a query block's keys (many rows)
-    int32_t parts, tiles;                         // tiles: of 32 keys (few), else kTileKeys
-    int64_t q_tiles;
+    int32_t parts, tiles;                         // tiles: of 32 keys (few rows, fp32) or 64
+    int64_t q_tiles;                              // workgroups of a (sample, key head) and part
+    int32_t blocks;                               // resident: 32-query blocks of each
 };
 constexpr int kUnits = 256;
 
-Plan plan_of(int32_t B, int32_t Nq, int32_t Nk, int32_t heads, int32_t kv_heads, int32_t dtype) {
+int tiles_that_fit(int32_t dh) {
+    return dh <= 32 ? ring_tiles<32>() : dh <= 64 ? ring_tiles<64>() : dh <= 80 ? ring_tiles<80>() : dh <= 96 ? ring_tiles<96>() : ring_tiles<128>();
+}
+
+Plan plan_of(int32_t B, int32_t Nq, int32_t Nk, int32_t heads, int32_t kv_heads, int32_t dh, int32_t dtype, bool ring_covers) {
     const int64_t pairs = static_cast<int64_t>(B) * kv_heads, rows = static_cast<int64_t>(Nq) * (heads / kv_heads);
     Plan p{};
     p.few = rows <= kFewRows;
-    const int tile = p.few ? 32 : dtype == FREE_BF16 ? 64 : 32;
-    const int64_t tiles = std::max<int64_t>(1, (static_cast<int64_t>(Nk) + tile - 1) / tile);
     p.ks = 1;
     p.q_tiles = 1;
+    const int tile = p.few || dtype == FREE_FP32 ? 32 : 64;
+    const int64_t tiles = std::max<int64_t>(1, (static_cast<int64_t>(Nk) + tile - 1) / tile);
+    const int64_t blocks = (rows + 31) / 32;
+    if (!p.few && dtype == FREE_BF16 && ring_covers && pairs * blocks >= kUnits * kRingWaves) {
+        p.ring = true;
+        p.resident = tiles <= std::min(tiles_that_fit(dh), kMaxTiles);
+        p.parts = 1;
+        p.tiles = static_cast<int32_t>(tiles);
+        p.q_tiles = (blocks + kRingWaves - 1) / kRingWaves;
+        if (p.resident) {
+            // one workgroup per compute unit
+            const int64_t want = std::max<int64_t>(1, kUnits / std::max<int64_t>(pairs, 1)), rounds = std::max<int64_t>(1, (p.q_tiles + want - 1) / want);
+            p.blocks = static_cast<int32_t>(rounds * kRingWaves);
+            p.q_tiles = (blocks + p.blocks - 1) / p.blocks;
+        }
+        return p;
+    }
     if (!p.few) {
         p.q_tiles = (rows + 127) / 128;
         if (dtype == FREE_BF16 && pairs * p.q_tiles <= 2 * kUnits) {
@@ -468,6 +638,19 @@ int32_t launch_shape(const CrossArgs& a, const Plan& p, const Parts& pt, hipStre
         hipLaunchKernelGGL(kern, dim3(static_cast<uint32_t>(blocks)), dim3(kThreads), lds, s, a, pt);
         return launch_ok() ? FREE_OK : FREE_ERR_HIP;
     }
+    if constexpr (sizeof(T) == 2 && kVec) {
+        if (p.ring) {
+            const size_t lds = static_cast<size_t>(p.resident ? p.tiles : kRing) * PairRing<DP, kRingWaves>::kTileBytes + 128;
+            const auto launch = [&](auto resident) {
+                auto kern = cross_ring_kernel<DP, decltype(resident)::value>;
+                static LdsLimit limit;
+                if (!limit.allow(reinterpret_cast<const void*>(kern), kLdsBytes)) return FREE_ERR_HIP;
+                hipLaunchKernelGGL(kern, dim3(static_cast<uint32_t>(blocks)), dim3(kRingWaves * 64), lds, s, a, pt, static_cast<int32_t>(p.q_tiles), p.blocks);
+                return launch_ok() ? FREE_OK : FREE_ERR_HIP;
+            };
+            return p.resident ? launch(std::true_type{}) : launch(std::false_type{});
+        }
+    }
     constexpr size_t lds = 4 * Tile<T, DP>::kBytes;
     const auto launch = [&](auto ks) {
         auto kern = cross_many_kernel<T, DP, decltype(ks)::value, kVec>;
@@ -494,9 +677,26 @@ int32_t launch_width(const CrossArgs& a, const Plan& p, const Parts& pt, hipStre
 size_t up256(size_t n) { return (n + 255) / 256 * 256; }
 
 template <typename T>
-int32_t launch_type(const CrossArgs& a, const Plan& p, const Parts& pt, hipStream_t s) {
+bool whole_chunks(const CrossArgs& a) {
     const auto al = [](const void* x, int64_t stride) { return (reinterpret_cast<uintptr_t>(x) & 15u) == 0 && stride % static_cast<int64_t>(16 / sizeof(T)) == 0; };
-    const bool vec = a.dh % static_cast<int>(16 / sizeof(T)) == 0 && al(a.q, a.q_stride) && al(a.k, a.k_stride) && al(a.v, a.v_stride) && al(a.out, a.out_stride);
+    return a.dh % static_cast<int>(16 / sizeof(T)) == 0 && al(a.q, a.q_stride) && al(a.k, a.k_stride) && al(a.v, a.v_stride) && al(a.out, a.out_stride);
+}
+
+size_t space_of(const Plan& p, int32_t B, int32_t Nq, int32_t heads, int32_t dh) {
+    if (p.parts == 1) return 256;
+    const size_t rows = static_cast<size_t>(B) * Nq * heads * p.parts;
+    return up256(rows * dh * sizeof(float)) + up256(rows * 2 * sizeof(float));
+}
+
+template <typename T>
+int32_t launch_type(const CrossArgs& a, void* ws, hipStream_t s) {
+    const bool vec = whole_chunks<T>(a);
+    const Plan p = plan_of(a.B, a.Nq, a.Nk, a.heads, a.kv_heads, a.dh, sizeof(T) == 2 ? FREE_BF16 : FREE_FP32, vec);
+    Parts pt{p.parts, p.tiles, nullptr, nullptr};
+    if (p.parts > 1) {
+        pt.o = static_cast<float*>(ws);
+        pt.ml = reinterpret_cast<float*>(static_cast<char*>(ws) + up256(static_cast<size_t>(a.B) * a.Nq * a.heads * p.parts * a.dh * sizeof(float)));
+    }
     const int32_t st = vec ? launch_width<T, true>(a, p, pt, s) : launch_width<T, false>(a, p, pt, s);
     if (st != FREE_OK || p.parts == 1) return st;
     const int64_t rows = static_cast<int64_t>(a.B) * a.Nq * a.heads;
@@ -508,20 +708,13 @@ int32_t launch_type(const CrossArgs& a, const Plan& p, const Parts& pt, hipStrea
 }  // namespace
 
 size_t cross_forward_bytes(int32_t B, int32_t Nq, int32_t Nk, int32_t heads, int32_t kv_heads, int32_t dh, int32_t dtype) {
-    const Plan p = plan_of(B, Nq, Nk, heads, kv_heads, dtype);
-    if (p.parts == 1) return 256;
-    const size_t rows = static_cast<size_t>(B) * Nq * heads * p.parts;
-    return up256(rows * dh * sizeof(float)) + up256(rows * 2 * sizeof(float));
+    // (whichever way the tensors' alignment leaves)
+    return std::max(space_of(plan_of(B, Nq, Nk, heads, kv_heads, dh, dtype, true), B, Nq, heads, dh),
+                    space_of(plan_of(B, Nq, Nk, heads, kv_heads, dh, dtype, false), B, Nq, heads, dh));
 }
 
 int32_t launch_cross_forward(const CrossArgs& a, int32_t dtype, void* ws, hipStream_t s) {
-    const Plan p = plan_of(a.B, a.Nq, a.Nk, a.heads, a.kv_heads, dtype);
-    Parts pt{p.parts, p.tiles, nullptr, nullptr};
-    if (p.parts > 1) {
-        pt.o = static_cast<float*>(ws);
-        pt.ml = reinterpret_cast<float*>(static_cast<char*>(ws) + up256(static_cast<size_t>(a.B) * a.Nq * a.heads * p.parts * a.dh * sizeof(float)));
-    }
-    return dtype == FREE_BF16 ? launch_type<bf16_t>(a, p, pt, s) : launch_type<float>(a, p, pt, s);
+    return dtype == FREE_BF16 ? launch_type<bf16_t>(a, ws, s) : launch_type<float>(a, ws, s);
 }
 
 }  // namespace freemi

@@ -115,23 +115,8 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 || DP <= 64) ? 2 : 1) voi
         valid = valid_next;
         keys.k.settle();
     }
-    if (row >= rows) return;
-    if (pt.parts > 1) {
-        float* const dst = pt.sum0 + ((part * static_cast<int64_t>(pairs) + pair) * rows + row) * a.dh;
-#pragma unroll
-        for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-            for (int e4 = 0; e4 < 4; ++e4)
-                store4<float, kVec>(dst, 32 * dt + 8 * e4 + 4 * g, a.dh, dq[dt][4 * e4], dq[dt][4 * e4 + 1], dq[dt][4 * e4 + 2], dq[dt][4 * e4 + 3]);
-        return;
-    }
-    T* const dst = static_cast<T*>(a.dq) + q_at * a.dq_stride + h_at;
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-        for (int e4 = 0; e4 < 4; ++e4)
-            store4<T, kVec>(dst, 32 * dt + 8 * e4 + 4 * g, a.dh, dq[dt][4 * e4] * a.scale, dq[dt][4 * e4 + 1] * a.scale, dq[dt][4 * e4 + 2] * a.scale,
-                            dq[dt][4 * e4 + 3] * a.scale);
+    if (pt.parts > 1) store_column<float, kVec, DT>(pt.sum0 + ((part * static_cast<int64_t>(pairs) + pair) * rows + row) * a.dh, a.dh, g, dq, 1.0f, row < rows);
+    else store_column<T, kVec, DT>(static_cast<T*>(a.dq) + q_at * a.dq_stride + h_at, a.dh, g, dq, a.scale, row < rows);
 }
 
 // ---- dk and dv.  KW wavefronts have 32 keys each; with KW 2 the two halves of a tile's rows go to two wavefronts, whose sums are parts of
@@ -264,7 +249,7 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 && DP <= 80) || DP <= 32 
         if (t + 1 < t1) deliver(stage ^ 1);
         queries.settle();
     }
-    if (key >= a.Nk) return;
+    const bool on = key < a.Nk;
     // (what a key that does not count has got are sums over zeros in place of it, not a gradient)
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt)
@@ -275,26 +260,12 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 && DP <= 80) || DP <= 32 
         }
     if (pt.parts > 1) {
         const int64_t at = (((part * QW + qw) * static_cast<int64_t>(pairs) + pair) * a.Nk + key) * a.dh;
-#pragma unroll
-        for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-            for (int e4 = 0; e4 < 4; ++e4) {
-                const int d = 32 * dt + 8 * e4 + 4 * g;
-                store4<float, kVec>(pt.sum0 + at, d, a.dh, dk[dt][4 * e4], dk[dt][4 * e4 + 1], dk[dt][4 * e4 + 2], dk[dt][4 * e4 + 3]);
-                store4<float, kVec>(pt.sum1 + at, d, a.dh, dv[dt][4 * e4], dv[dt][4 * e4 + 1], dv[dt][4 * e4 + 2], dv[dt][4 * e4 + 3]);
-            }
-        return;
+        store_column<float, kVec, DT>(pt.sum0 + at, a.dh, g, dk, 1.0f, on);
+        store_column<float, kVec, DT>(pt.sum1 + at, a.dh, g, dv, 1.0f, on);
+    } else {
+        store_column<T, kVec, DT>(static_cast<T*>(a.dk) + kv_at * a.dk_stride + h_at, a.dh, g, dk, a.scale, on);
+        store_column<T, kVec, DT>(static_cast<T*>(a.dv) + kv_at * a.dv_stride + h_at, a.dh, g, dv, 1.0f, on);
     }
-    T* const dkp = static_cast<T*>(a.dk) + kv_at * a.dk_stride + h_at;
-    T* const dvp = static_cast<T*>(a.dv) + kv_at * a.dv_stride + h_at;
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-        for (int e4 = 0; e4 < 4; ++e4) {
-            const int d = 32 * dt + 8 * e4 + 4 * g;
-            store4<T, kVec>(dkp, d, a.dh, dk[dt][4 * e4] * a.scale, dk[dt][4 * e4 + 1] * a.scale, dk[dt][4 * e4 + 2] * a.scale, dk[dt][4 * e4 + 3] * a.scale);
-            store4<T, kVec>(dvp, d, a.dh, dv[dt][4 * e4], dv[dt][4 * e4 + 1], dv[dt][4 * e4 + 2], dv[dt][4 * e4 + 3]);
-        }
 }
 
 // The parts of a sum [part][pair][row][dh], added in order, times `factor`: a thread per V values.  Row r of a pair is token r / group, head r % group

@@ -88,3 +88,15 @@ def test_odd_head_dimensions(dtype, dh):
 def test_sums_in_parts(dtype, B, Nq, Nk, heads, kv, dh):
     for keys in ("all", "holes"):
         compare(*problem(4, B, Nq, Nk, heads, kv, dh, dtype, keys), B, heads, kv, dh)
+
+
+@pytest.mark.parametrize("keys", ["all", "len", "holes"])
+@pytest.mark.parametrize("B,Nq,Nk,heads,kv,dh", [
+    (2, 2100, 130, 16, 16, 72),          # keys stay in LDS
+    (3, 1500, 383, 16, 16, 80), (1, 4100, 77, 32, 16, 64), (2, 1100, 250, 32, 32, 128), (4, 1030, 1000, 16, 16, 32), (2, 2100, 340, 16, 16, 96),
+    (1, 4200, 65, 16, 16, 40),
+    (1, 2100, 700, 32, 32, 64),          # keys pass through it
+    (2, 2049, 450, 16, 16, 72), (1, 1100, 513, 64, 8, 128), (2, 2100, 520, 16, 16, 96),
+])
+def test_many_queries(keys, B, Nq, Nk, heads, kv, dh):
+    compare(*problem(5, B, Nq, Nk, heads, kv, dh, torch.bfloat16, keys), B, heads, kv, dh)
