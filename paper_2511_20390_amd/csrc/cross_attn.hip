@@ -261,9 +261,10 @@ __global__ __launch_bounds__(kRingWaves * 64, 2) void cross_ring_kernel(CrossArg
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, g = lane >> 5;
     const int pairs = a.B * a.kv_heads, group = a.heads / a.kv_heads, per_part = pairs * chunks;
     const int part = blockIdx.x / per_part, id = blockIdx.x % per_part;
-    const bool by_xcd = pairs % kXcds == 0;          // what reads the same keys on one XCD
-    const int pair = by_xcd ? id % kXcds + kXcds * (id / (kXcds * chunks)) : id / chunks;
-    const int chunk = by_xcd ? id / kXcds % chunks : id % chunks;
+    // An XCD has heads that are next to each other, and the same queries of them at a time: rows of 144 bytes share lines.
+    const bool by_xcd = pairs % kXcds == 0;
+    const int per_xcd = by_xcd ? pairs / kXcds : pairs, place = by_xcd ? id / kXcds : id;
+    const int pair = (by_xcd ? id % kXcds * per_xcd : 0) + place % per_xcd, chunk = place / per_xcd;
     const int kvh = pair % a.kv_heads, b = pair / a.kv_heads;
     const int rows = a.Nq * group, blocks = (rows + 31) / 32;
     const int len = attended(a, b), tiles = (len + BKV - 1) / BKV, t0 = part * pt.tiles, t1 = min(t0 + pt.tiles, tiles);
