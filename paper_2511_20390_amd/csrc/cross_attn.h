@@ -8,6 +8,7 @@
 // that the half-waves hold in a register).  A 16-byte chunk of a row is 8 values or 4, one instruction or four: the loops are the same.
 #pragma once
 
+#include <algorithm>
 #include <type_traits>
 
 #include "gemm_dma.h"
@@ -396,6 +397,16 @@ struct PairRing {
     }
 };
 
+// Kernels with a PairRing: as many wavefronts, and tiles under way while one is multiplied: requested one ahead, a tile arrives later than the products of
+// another take.
+constexpr int kRing = 3, kRingWaves = 8, kMaxTiles = 16;
+constexpr int kLdsBytes = 160 * 1024 - 256;
+
+// 64 floats, one per lane, to LDS (dma_1k's comment)
+__device__ __forceinline__ void dma_floats(uint32_t lds_addr, int voff, u32x4_t rsrc) {
+    asm volatile("s_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" :: "{m0}"(lds_addr), "v"(voff), "s"(rsrc));
+}
+
 // rows [first, first + rows) of a tensor as a buffer
 __device__ __forceinline__ u32x4_t rows_rsrc(const bf16_t* p, int64_t first, int64_t rows, int64_t stride, int width) {
     return make_rsrc(p + first * stride, rows > 0 ? ((rows - 1) * stride + width) * 2 : 0);
@@ -407,6 +418,83 @@ __device__ __forceinline__ int attended(const CrossArgs& a, int b) {
     const int n = a.key_len[b];
     return n < 0 ? 0 : n < a.Nk ? n : a.Nk;
 }
+
+// Keys and values of a (sample, key head) for the kernels with a PairRing
+template <int DP>
+struct RingKeys {
+    using TL = Tile<bf16_t, DP>;
+    using Ring = PairRing<DP, kRingWaves>;
+    const bf16_t *kp, *vp;
+    const uint8_t* mask;
+    int64_t k_stride, v_stride;
+    int len, dh;
+    Ring ring;
+    __device__ __forceinline__ RingKeys(const CrossArgs& a, int b, int kvh, int wave, int lane)
+        : kp(static_cast<const bf16_t*>(a.k) + static_cast<int64_t>(b) * a.Nk * a.k_stride + static_cast<int64_t>(kvh) * a.dh),
+          vp(static_cast<const bf16_t*>(a.v) + static_cast<int64_t>(b) * a.Nk * a.v_stride + static_cast<int64_t>(kvh) * a.dh),
+          mask(a.key_mask ? a.key_mask + static_cast<int64_t>(b) * a.Nk : nullptr), k_stride(a.k_stride), v_stride(a.v_stride), len(attended(a, b)), dh(a.dh) {
+        ring.aim(wave, lane, dh, [&](int second, int r) { return r * static_cast<int>(second ? v_stride : k_stride) * 2; });
+    }
+    __device__ __forceinline__ int tiles() const { return (len + TL::kRows - 1) / TL::kRows; }
+    __device__ __forceinline__ void request(int t, uint32_t tile, int wave) const {
+        const int64_t first = static_cast<int64_t>(t) * TL::kRows;
+        ring.request(rows_rsrc(kp, first, len - first, k_stride, dh), rows_rsrc(vp, first, len - first, v_stride, dh), tile, wave);
+    }
+    // which of tile t's keys count; with a mask it waits for memory
+    __device__ __forceinline__ uint64_t valid(int t, int lane) const {
+        const int key = t * TL::kRows + lane;
+        return mask ? __ballot(key < len && mask[key] != 0) : keys_below(len - t * TL::kRows);
+    }
+    // rows of keys that do not count are replaced, in LDS, where they are multiplied by zeros and may be NaN: the keys' (second 0) or the values'
+    static __device__ __forceinline__ void drop(char* tile, int second, uint64_t valid, int wave, int lane) {
+        if (valid == ~0ull) return;
+        for (int r = wave; r < TL::kRows; r += kRingWaves)
+            if (!(valid >> r & 1) && lane < TL::CHP) *reinterpret_cast<xu32x4_t*>(tile + second * Ring::kSecond + r * TL::kPitch + lane * 16) = xu32x4_t{0, 0, 0, 0};
+    }
+};
+
+// Resident keys: all tiles to LDS, masks[t] their bits; whether any key counts.  Ends with a barrier.
+template <int DP>
+__device__ __forceinline__ bool bring_keys(const RingKeys<DP>& keys, char* lds, uint64_t (&masks)[kMaxTiles], int drop_second, int wave, int lane) {
+    using Ring = typename RingKeys<DP>::Ring;
+    const int tiles = keys.tiles();
+    bool any = tiles > 0;
+    if (keys.mask) {
+        for (int t = wave; t < tiles; t += kRingWaves) {
+            const uint64_t bits = keys.valid(t, lane);
+            if (lane == 0) masks[t] = bits;
+        }
+    }
+    wait_vm_barrier<0>();
+    if (keys.mask) {
+        any = false;
+        for (int t = 0; t < tiles; ++t) {
+            const uint64_t valid = masks[t];
+            any |= valid != 0;
+            keys.drop(lds + t * Ring::kTileBytes, drop_second, valid, wave, lane);
+        }
+        __syncthreads();
+    }
+    return any;
+}
+
+template <int DP>
+constexpr int ring_tiles() { return (kLdsBytes - 128) / PairRing<DP, kRingWaves>::kTileBytes; }
+inline int tiles_that_fit(int32_t dh) {
+    return std::min(kMaxTiles, dh <= 32 ? ring_tiles<32>() : dh <= 64 ? ring_tiles<64>() : dh <= 80 ? ring_tiles<80>() : dh <= 96 ? ring_tiles<96>() : ring_tiles<128>());
+}
+
+// (sample, key head) and place in it of a workgroup: an XCD has heads that are next to each other, and the same place of them at a time - rows of 144 bytes
+// share lines
+struct WorkPlace {
+    int pair, place;
+    __device__ __forceinline__ WorkPlace(int id, int pairs) {
+        const bool by_xcd = pairs % kXcds == 0;
+        const int per = by_xcd ? pairs / kXcds : pairs, at = by_xcd ? id / kXcds : id;
+        pair = (by_xcd ? id % kXcds * per : 0) + at % per;
+        place = at / per;
+    }
+};
 
 // Keys and values of a (sample, key head), tile by tile, and which of a tile's keys count.  The mask of a tile is requested a tile ahead of its rows.
 template <typename T, int DP, bool kVec>

@@ -241,53 +241,24 @@ __global__ __launch_bounds__(kThreads, (kThreeWaves<T, DP, KS, kVec> ? 3 : 2)) v
 
 // bf16 of whole chunks, eight wavefronts of 32 queries at a time.
 // kResident: all keys and values of a (sample, key head) fit in LDS.  They are brought there once, and each wavefront takes one block of queries after
-// the other, without a barrier, the next block's queries requested ahead.  Otherwise tiles pass through a ring of kRing, two of them under way
-// while one is multiplied: requested one ahead, a tile arrives later than the products of another take.
-constexpr int kRing = 3, kRingWaves = 8, kMaxTiles = 16;
-constexpr int kLdsBytes = 160 * 1024 - 256;
-
-template <int DP>
-constexpr int ring_tiles() { return (kLdsBytes - 128) / PairRing<DP, kRingWaves>::kTileBytes; }
-
+// the other, without a barrier, the next block's queries requested ahead.  Otherwise tiles pass through a ring.
 template <int DP, bool kResident>
 __global__ __launch_bounds__(kRingWaves * 64, 2) void cross_ring_kernel(CrossArgs a, Parts pt, int32_t chunks, int32_t blocks_per_chunk) {
     using T = bf16_t;
     using H = HeadShape<T, DP>;
-    using TL = Tile<T, DP>;
     using Ring = PairRing<DP, kRingWaves>;
-    constexpr int KSTEPS = H::KSTEPS, DT = H::DT, BKV = TL::kRows;
+    constexpr int KSTEPS = H::KSTEPS, DT = H::DT;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     __shared__ uint64_t masks[kMaxTiles];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, g = lane >> 5;
-    const int pairs = a.B * a.kv_heads, group = a.heads / a.kv_heads, per_part = pairs * chunks;
-    const int part = blockIdx.x / per_part, id = blockIdx.x % per_part;
-    // An XCD has heads that are next to each other, and the same queries of them at a time: rows of 144 bytes share lines.
-    const bool by_xcd = pairs % kXcds == 0;
-    const int per_xcd = by_xcd ? pairs / kXcds : pairs, place = by_xcd ? id / kXcds : id;
-    const int pair = (by_xcd ? id % kXcds * per_xcd : 0) + place % per_xcd, chunk = place / per_xcd;
-    const int kvh = pair % a.kv_heads, b = pair / a.kv_heads;
+    const int pairs = a.B * a.kv_heads, group = a.heads / a.kv_heads, part = blockIdx.x / (pairs * chunks);
+    const WorkPlace at(blockIdx.x % (pairs * chunks), pairs);
+    const int pair = at.pair, chunk = at.place, kvh = pair % a.kv_heads, b = pair / a.kv_heads;
     const int rows = a.Nq * group, blocks = (rows + 31) / 32;
-    const int len = attended(a, b), tiles = (len + BKV - 1) / BKV, t0 = part * pt.tiles, t1 = min(t0 + pt.tiles, tiles);
-    const bf16_t* const kp = static_cast<const T*>(a.k) + static_cast<int64_t>(b) * a.Nk * a.k_stride + static_cast<int64_t>(kvh) * a.dh;
-    const bf16_t* const vp = static_cast<const T*>(a.v) + static_cast<int64_t>(b) * a.Nk * a.v_stride + static_cast<int64_t>(kvh) * a.dh;
-    const uint8_t* const mask = a.key_mask ? a.key_mask + static_cast<int64_t>(b) * a.Nk : nullptr;
+    RingKeys<DP> keys(a, b, kvh, wave, lane);
+    const int tiles = keys.tiles(), t0 = part * pt.tiles, t1 = min(t0 + pt.tiles, tiles);
     const uint32_t lds_base = lds_address(lds);
-    Ring ring;
-    ring.aim(wave, lane, a.dh, [&](int second, int r) { return r * static_cast<int>(second ? a.v_stride : a.k_stride) * 2; });
-    const auto request = [&](int t, int slot) {
-        const int64_t first = static_cast<int64_t>(t) * BKV;
-        ring.request(rows_rsrc(kp, first, len - first, a.k_stride, a.dh), rows_rsrc(vp, first, len - first, a.v_stride, a.dh), lds_base + slot * Ring::kTileBytes, wave);
-    };
-    const auto mask_bits = [&](int t) {              // of tile t's keys; waits for memory
-        const int key = t * BKV + lane;
-        return __ballot(key < len && mask[key] != 0);
-    };
-    // the values of keys that do not count are replaced, in LDS: they are multiplied by zeros, and may be NaN
-    const auto drop_values = [&](char* tile, uint64_t valid) {
-        if (valid == ~0ull) return;
-        for (int r = wave; r < BKV; r += kRingWaves)
-            if (!(valid >> r & 1) && lane < TL::CHP) *reinterpret_cast<xu32x4_t*>(tile + Ring::kSecond + r * TL::kPitch + lane * 16) = xu32x4_t{0, 0, 0, 0};
-    };
+    const auto request = [&](int t, int slot) { keys.request(t, lds_base + slot * Ring::kTileBytes, wave); };
     const auto load_queries = [&](int block, xu32x4_t (&f)[KSTEPS]) {
         const int r = min(block * 32 + l32, rows - 1), token = over_group(r, group), head = kvh * group + r - token * group;
         const T* const p = static_cast<const T*>(a.q) + (static_cast<int64_t>(b) * a.Nq + token) * a.q_stride + static_cast<int64_t>(head) * a.dh;
@@ -343,30 +314,14 @@ __global__ __launch_bounds__(kRingWaves * 64, 2) void cross_ring_kernel(CrossArg
         for (int t = 0; t < tiles; ++t) request(t, t);
         const int first = chunk * blocks_per_chunk, last = min(first + blocks_per_chunk, blocks);
         if (first + wave < last) load_queries(first + wave, qf);
-        bool any = tiles > 0;
-        if (mask) {
-            for (int t = wave; t < tiles; t += kRingWaves) {
-                const uint64_t bits = mask_bits(t);
-                if (lane == 0) masks[t] = bits;
-            }
-        }
-        wait_vm_barrier<0>();
-        if (mask) {
-            any = false;
-            for (int t = 0; t < tiles; ++t) {
-                const uint64_t valid = masks[t];
-                any |= valid != 0;
-                drop_values(lds + t * Ring::kTileBytes, valid);
-            }
-            __syncthreads();
-        }
+        const bool any = bring_keys(keys, lds, masks, 1, wave, lane);
         for (int block = first + wave; block < last; block += kRingWaves) {
             xu32x4_t next[KSTEPS];
             arrived(qf);
             if (block + kRingWaves < last) load_queries(block + kRingWaves, next);
             begin();
             for (int t = 0; t < tiles; ++t) {
-                const uint64_t valid = mask ? masks[t] : keys_below(len - t * BKV);
+                const uint64_t valid = keys.mask ? masks[t] : keys_below(keys.len - t * Tile<T, DP>::kRows);
                 multiply(lds + t * Ring::kTileBytes, valid);
             }
             finish(block, any);
@@ -385,14 +340,14 @@ __global__ __launch_bounds__(kRingWaves * 64, 2) void cross_ring_kernel(CrossArg
         arrived(qf);
         int slot = 0, free_slot = kRing - 1;
         for (int t = t0; t < t1; ++t) {
-            const uint64_t valid = mask ? mask_bits(t) : keys_below(len - t * BKV);
+            const uint64_t valid = keys.valid(t, lane);
             any |= valid != 0;
             // tile t has arrived, and everybody is done with the one before it
             if (t + kRing - 1 <= t1) wait_vm_barrier<(kRing - 2) * Ring::N>();
             else wait_vm_barrier<0>();
             char* const tile = lds + slot * Ring::kTileBytes;
-            if (mask && valid != ~0ull) {
-                drop_values(tile, valid);
+            if (keys.mask && valid != ~0ull) {
+                keys.drop(tile, 1, valid, wave, lane);
                 __syncthreads();
             }
             if (t + kRing - 1 < t1) request(t + kRing - 1, free_slot);
@@ -583,10 +538,6 @@ struct Plan {
 };
 constexpr int kUnits = 256;
 
-int tiles_that_fit(int32_t dh) {
-    return dh <= 32 ? ring_tiles<32>() : dh <= 64 ? ring_tiles<64>() : dh <= 80 ? ring_tiles<80>() : dh <= 96 ? ring_tiles<96>() : ring_tiles<128>();
-}
-
 Plan plan_of(int32_t B, int32_t Nq, int32_t Nk, int32_t heads, int32_t kv_heads, int32_t dh, int32_t dtype, bool ring_covers) {
     const int64_t pairs = static_cast<int64_t>(B) * kv_heads, rows = static_cast<int64_t>(Nq) * (heads / kv_heads);
     Plan p{};
@@ -598,7 +549,7 @@ Plan plan_of(int32_t B, int32_t Nq, int32_t Nk, int32_t heads, int32_t kv_heads,
     const int64_t blocks = (rows + 31) / 32;
     if (!p.few && dtype == FREE_BF16 && ring_covers && pairs * blocks >= kUnits * kRingWaves) {
         p.ring = true;
-        p.resident = tiles <= std::min(tiles_that_fit(dh), kMaxTiles);
+        p.resident = tiles <= tiles_that_fit(dh);
         p.parts = 1;
         p.tiles = static_cast<int32_t>(tiles);
         p.q_tiles = (blocks + kRingWaves - 1) / kRingWaves;

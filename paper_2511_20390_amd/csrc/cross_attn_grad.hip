@@ -2,8 +2,9 @@
 //   P = exp(scale q k^T - lse) on the keys that count,  delta = sum dout out,  dS = P (dout v^T - delta)
 //   dq = scale dS k,   dk = scale dS^T q,   dv = P^T dout      (dk, dv: summed over the queries of all heads that share them)
 // Nothing of the size of the scores is kept between the passes: both kernels compute their tiles of scores again.
-//  * dq: a workgroup has 128 rows (query and head of a group) and passes tiles of K and V through LDS; it also leaves delta for
-//  * dk, dv: a workgroup has 128 or 64 keys and passes tiles of q and dout through LDS, so that both sums stay in registers.
+//  * dq: a wavefront has 32 rows (query and head of a group), and K and V stay in LDS or pass through it in tiles; it also leaves -lse / scale and
+//    -delta of its rows for
+//  * dk, dv: a wavefront has 32 keys, and tiles of q and dout pass through LDS, so that both sums stay in registers.
 // The score tile's rows are the streamed tensor's rows and its columns the workgroup's own (cross_attn.h), in both.
 // Where a launch would have few workgroups the streamed axis is cut in parts, whose fp32 results a second launch adds in order: no
 // atomics, equal inputs give equal bits.
@@ -24,9 +25,100 @@ struct GradParts {
     float *sum0, *sum1;
 };
 
+// what a row of queries is to the keys' gradient: -lse / scale and -delta, each [B, heads, Nq]
+struct RowStats {
+    float *lse, *delta;
+};
+
+// dq += over one 32-key block; bits: which of its keys count, from this half-wave's first on
+template <typename T, int DP>
+__device__ __forceinline__ void dq_block(const char* tile_k, const char* tile_v, int row0, int lane, uint32_t bits, const xu32x4_t (&qf)[HeadShape<T, DP>::KSTEPS],
+                                         const xu32x4_t (&gf)[HeadShape<T, DP>::KSTEPS], float dl, float lse2, float scale_log2,
+                                         xf32x16_t (&dq)[HeadShape<T, DP>::DT]) {
+    xu32x4_t fk[kRowGroup<T, DP>], fv[kRowGroup<T, DP>];
+    Columns<T, DP> ck;
+    xf32x16_t st, dp;
+    clear_tile(st);
+#pragma unroll
+    for (int e = 0; e < 16; ++e) dp[e] = -dl;
+    read_rows<T, DP>(tile_k, row0, lane, 0, fk);
+    read_rows<T, DP>(tile_v, row0, lane, 0, fv);
+    fence();
+    row_products<T, DP>(tile_k, row0, lane, fk, qf, st);
+    ck.read(tile_k, row0, lane, 0);
+    fence();
+    row_products<T, DP>(tile_v, row0, lane, fv, gf, dp);
+#pragma unroll
+    for (int e = 0; e < 16; ++e) st[e] = __builtin_amdgcn_exp2f(fmaf(st[e], scale_log2, -lse2)) * dp[e];
+    if (__builtin_amdgcn_readfirstlane(bits) != ~0u) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) st[e] = bits >> register_row<T>(e, 0) & 1 ? st[e] : 0.f;
+    }
+    column_products<T, DP>(tile_k, row0, lane, ck, st, dq);
+}
+
+// dk, dv += over one block of 32 rows, whose -lse / scale and -delta are at `lse` and `delta`: the sums of scores begin with them
+template <typename T, int DP>
+__device__ __forceinline__ void dkv_block(const char* tile_q, const char* tile_g, int row0, int lane, const float* lse, const float* delta,
+                                          const xu32x4_t (&kf)[HeadShape<T, DP>::KSTEPS], const xu32x4_t (&vf)[HeadShape<T, DP>::KSTEPS], float scale_log2,
+                                          xf32x16_t (&dk)[HeadShape<T, DP>::DT], xf32x16_t (&dv)[HeadShape<T, DP>::DT]) {
+    xu32x4_t fq[kRowGroup<T, DP>], fg[kRowGroup<T, DP>];
+    Columns<T, DP> cg, cq;
+    xf32x16_t st, dp;
+#pragma unroll
+    for (int e4 = 0; e4 < 4; ++e4) {
+        const int at = row0 + register_row<T>(4 * e4, lane >> 5);
+        const xf32x4_t l = *reinterpret_cast<const xf32x4_t*>(lse + at), d = *reinterpret_cast<const xf32x4_t*>(delta + at);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            st[4 * e4 + i] = l[i];
+            dp[4 * e4 + i] = d[i];
+        }
+    }
+    read_rows<T, DP>(tile_q, row0, lane, 0, fq);
+    read_rows<T, DP>(tile_g, row0, lane, 0, fg);
+    fence();
+    row_products<T, DP>(tile_q, row0, lane, fq, kf, st);
+    cg.read(tile_g, row0, lane, 0);
+    fence();
+    row_products<T, DP>(tile_g, row0, lane, fg, vf, dp);
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+        st[e] = __builtin_amdgcn_exp2f(st[e] * scale_log2);
+        dp[e] *= st[e];
+    }
+    cq.read(tile_q, row0, lane, 0);
+    fence();
+    column_products<T, DP>(tile_g, row0, lane, cg, st, dv);
+    column_products<T, DP>(tile_q, row0, lane, cq, dp, dk);
+}
+
+// a row's q and dout as operands, and sum dout out
+template <typename T, int DP, bool kVec>
+__device__ __forceinline__ float load_row(const CrossArgs& a, int64_t q_at, int64_t h_at, int g, xu32x4_t (&qf)[HeadShape<T, DP>::KSTEPS],
+                                          xu32x4_t (&gf)[HeadShape<T, DP>::KSTEPS]) {
+    float dl = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < HeadShape<T, DP>::KSTEPS; ++ks) {
+        qf[ks] = row_chunk<T, kVec>(static_cast<const T*>(a.q) + q_at * a.q_stride + h_at, 2 * ks + g, a.dh);
+        gf[ks] = row_chunk<T, kVec>(static_cast<const T*>(a.dout) + q_at * a.dout_stride + h_at, 2 * ks + g, a.dh);
+        const xu32x4_t of = row_chunk<T, kVec>(static_cast<const T*>(a.out) + q_at * a.out_stride + h_at, 2 * ks + g, a.dh);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if constexpr (sizeof(T) == 2) {
+                dl = fmaf(__uint_as_float(gf[ks][e] << 16), __uint_as_float(of[e] << 16), dl);
+                dl = fmaf(__uint_as_float(gf[ks][e] & 0xffff0000u), __uint_as_float(of[e] & 0xffff0000u), dl);
+            } else {
+                dl = fmaf(__uint_as_float(gf[ks][e]), __uint_as_float(of[e]), dl);
+            }
+        }
+    }
+    return add_lane_xor<32>(dl);
+}
+
 // ---- dq and delta
 template <typename T, int DP, bool kVec>
-__global__ __launch_bounds__(kThreads, (sizeof(T) == 2 || DP <= 64) ? 2 : 1) void cross_dq_kernel(CrossArgs a, float* delta, GradParts pt, int32_t q_tiles) {
+__global__ __launch_bounds__(kThreads, (sizeof(T) == 2 || DP <= 64) ? 2 : 1) void cross_dq_kernel(CrossArgs a, RowStats stats, GradParts pt, int32_t q_tiles) {
     using H = HeadShape<T, DP>;
     using TL = Tile<T, DP>;
     constexpr int KSTEPS = H::KSTEPS, DT = H::DT, BKV = TL::kRows;
@@ -53,25 +145,12 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 || DP <= 64) ? 2 : 1) voi
     const int64_t q_at = static_cast<int64_t>(b) * a.Nq + token, h_at = static_cast<int64_t>(head) * a.dh;
     const int64_t stat = (static_cast<int64_t>(b) * a.heads + head) * a.Nq + token;
     xu32x4_t qf[KSTEPS], gf[KSTEPS];
-    float dl = 0.f;
-#pragma unroll
-    for (int ks = 0; ks < KSTEPS; ++ks) {
-        qf[ks] = row_chunk<T, kVec>(static_cast<const T*>(a.q) + q_at * a.q_stride + h_at, 2 * ks + g, a.dh);
-        gf[ks] = row_chunk<T, kVec>(static_cast<const T*>(a.dout) + q_at * a.dout_stride + h_at, 2 * ks + g, a.dh);
-        const xu32x4_t of = row_chunk<T, kVec>(static_cast<const T*>(a.out) + q_at * a.out_stride + h_at, 2 * ks + g, a.dh);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            if constexpr (sizeof(T) == 2) {
-                dl = fmaf(__uint_as_float(gf[ks][e] << 16), __uint_as_float(of[e] << 16), dl);
-                dl = fmaf(__uint_as_float(gf[ks][e] & 0xffff0000u), __uint_as_float(of[e] & 0xffff0000u), dl);
-            } else {
-                dl = fmaf(__uint_as_float(gf[ks][e]), __uint_as_float(of[e]), dl);
-            }
-        }
+    const float dl = load_row<T, DP, kVec>(a, q_at, h_at, g, qf, gf);
+    const float lse = a.lse[stat], lse2 = lse * kLog2e, scale_log2 = a.scale * kLog2e;
+    if (part == 0 && g == 0 && row < rows) {
+        stats.lse[stat] = -lse / a.scale;
+        stats.delta[stat] = -dl;
     }
-    dl = add_lane_xor<32>(dl);
-    const float lse2 = a.lse[stat] * kLog2e, scale_log2 = a.scale * kLog2e;
-    if (part == 0 && g == 0 && row < rows) delta[stat] = dl;
 
     xf32x16_t dq[DT];
 #pragma unroll
@@ -90,26 +169,9 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 || DP <= 64) ? 2 : 1) voi
         }
 #pragma unroll
         for (int kb = 0; kb < BKV / 32; ++kb) {
-            xu32x4_t fk[kRowGroup<T, DP>], fv[kRowGroup<T, DP>];
-            Columns<T, DP> ck;
-            xf32x16_t st, dp;
-            clear_tile(st);
-#pragma unroll
-            for (int e = 0; e < 16; ++e) dp[e] = -dl;
-            read_rows<T, DP>(sK, kb * 32, lane, 0, fk);
-            read_rows<T, DP>(sK + TL::kBytes, kb * 32, lane, 0, fv);
-            fence();
-            row_products<T, DP>(sK, kb * 32, lane, fk, qf, st);
-            ck.read(sK, kb * 32, lane, 0);
-            fence();
-            row_products<T, DP>(sK + TL::kBytes, kb * 32, lane, fv, gf, dp);
-            const uint32_t bits = static_cast<uint32_t>(valid >> (32 * kb)) >> (sizeof(T) == 2 ? 8 * g : 4 * g);
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                const float ds = __builtin_amdgcn_exp2f(fmaf(st[e], scale_log2, -lse2)) * dp[e];
-                st[e] = bits >> register_row<T>(e, 0) & 1 ? ds : 0.f;
-            }
-            column_products<T, DP>(sK, kb * 32, lane, ck, st, dq);
+            // (fp32 has 32 keys to a tile, and a full mask of them)
+            const uint32_t bits = static_cast<uint32_t>(valid >> (32 * kb));
+            dq_block<T, DP>(sK, sK + TL::kBytes, kb * 32, lane, bits == ~0u ? bits : bits >> (sizeof(T) == 2 ? 8 * g : 4 * g), qf, gf, dl, lse2, scale_log2, dq);
         }
         if (t + 1 < t1) keys.deliver(lds + other, lds + other + TL::kBytes, tid, valid_next);
         valid = valid_next;
@@ -122,7 +184,7 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 || DP <= 64) ? 2 : 1) voi
 // ---- dk and dv.  KW wavefronts have 32 keys each; with KW 2 the two halves of a tile's rows go to two wavefronts, whose sums are parts of
 // their own.
 template <typename T, int DP, int KW, bool kVec>
-__global__ __launch_bounds__(kThreads, (sizeof(T) == 2 && DP <= 80) || DP <= 32 ? 2 : 1) void cross_dkv_kernel(CrossArgs a, const float* delta, GradParts pt, int32_t k_tiles) {
+__global__ __launch_bounds__(kThreads, (sizeof(T) == 2 && DP <= 80) || DP <= 32 ? 2 : 1) void cross_dkv_kernel(CrossArgs a, RowStats row_stats, GradParts pt, int32_t k_tiles) {
     using H = HeadShape<T, DP>;
     using TL = Tile<T, DP>;
     constexpr int KSTEPS = H::KSTEPS, DT = H::DT, BR = TL::kRows, QW = 4 / KW, RB = BR / 32 / QW;
@@ -150,7 +212,6 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 && DP <= 80) || DP <= 32 
     const int q_row = static_cast<int>(a.q_stride) * static_cast<int>(sizeof(T)), g_row = static_cast<int>(a.dout_stride) * static_cast<int>(sizeof(T));
     const int head_bytes = a.dh * static_cast<int>(sizeof(T));
     const int64_t first_row = static_cast<int64_t>(b) * a.Nq, h0 = static_cast<int64_t>(kvh) * group * a.dh;
-    const float inv_scale = 1.0f / a.scale;
     TileStream<T, DP, kVec> queries, grads;
     float lse_next = 0.f, delta_next = 0.f;
     const uint32_t lds_base = lds_address(lds);
@@ -172,8 +233,8 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 && DP <= 80) || DP <= 32 
             const int token = over_group(rest + tid, group), h = rest + tid - token * group;
             const int64_t at = (static_cast<int64_t>(b) * a.heads + kvh * group + h) * a.Nq + token0 + token;
             const bool on = r0 + tid < rows;
-            lse_next = on ? a.lse[at] : INFINITY;                       // (rows past the end: probabilities of zero)
-            delta_next = on ? delta[at] : 0.f;
+            lse_next = on ? row_stats.lse[at] : 0.f;                    // (rows past the end are zero, and add nothing)
+            delta_next = on ? row_stats.delta[at] : 0.f;
         }
     };
     const auto deliver = [&](int stage) {
@@ -181,8 +242,8 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 && DP <= 80) || DP <= 32 
         queries.deliver(sQ, tid, false, 0);
         grads.deliver(sQ + TL::kBytes, tid, false, 0);
         if (tid < BR) {
-            stats[stage * 2 * BR + tid] = -lse_next * inv_scale;
-            stats[stage * 2 * BR + BR + tid] = -delta_next;
+            stats[stage * 2 * BR + tid] = lse_next;
+            stats[stage * 2 * BR + BR + tid] = delta_next;
         }
     };
     if (t0 < t1) request(t0, 0);
@@ -215,36 +276,8 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 && DP <= 80) || DP <= 32 
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb) {
             const int row0 = (qw * RB + rb) * 32;
-            xu32x4_t fq[kRowGroup<T, DP>], fg[kRowGroup<T, DP>];
-            Columns<T, DP> cg, cq;
-            xf32x16_t st, dp;
-            // the sums begin with -lse / scale and -delta of their row
-#pragma unroll
-            for (int e4 = 0; e4 < 4; ++e4) {
-                const float* const at = stats + stage * 2 * BR + row0 + register_row<T>(4 * e4, g);
-                const xf32x4_t lse = *reinterpret_cast<const xf32x4_t*>(at), dl = *reinterpret_cast<const xf32x4_t*>(at + BR);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    st[4 * e4 + i] = lse[i];
-                    dp[4 * e4 + i] = dl[i];
-                }
-            }
-            read_rows<T, DP>(sQ, row0, lane, 0, fq);
-            read_rows<T, DP>(sQ + TL::kBytes, row0, lane, 0, fg);
-            fence();
-            row_products<T, DP>(sQ, row0, lane, fq, kf, st);
-            cg.read(sQ + TL::kBytes, row0, lane, 0);
-            fence();
-            row_products<T, DP>(sQ + TL::kBytes, row0, lane, fg, vf, dp);
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                st[e] = __builtin_amdgcn_exp2f(st[e] * scale_log2);
-                dp[e] *= st[e];
-            }
-            cq.read(sQ, row0, lane, 0);
-            fence();
-            column_products<T, DP>(sQ + TL::kBytes, row0, lane, cg, st, dv);
-            column_products<T, DP>(sQ, row0, lane, cq, dp, dk);
+            const float* const at = stats + stage * 2 * BR;
+            dkv_block<T, DP>(sQ, sQ + TL::kBytes, row0, lane, at, at + BR, kf, vf, scale_log2, dk, dv);
         }
         if (t + 1 < t1) deliver(stage ^ 1);
         queries.settle();
@@ -265,6 +298,219 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 && DP <= 80) || DP <= 32 
     } else {
         store_column<T, kVec, DT>(static_cast<T*>(a.dk) + kv_at * a.dk_stride + h_at, a.dh, g, dk, a.scale, on);
         store_column<T, kVec, DT>(static_cast<T*>(a.dv) + kv_at * a.dv_stride + h_at, a.dh, g, dv, 1.0f, on);
+    }
+}
+
+// ---- the same for bf16 of whole chunks and many rows (cross_ring_kernel of cross_attn.hip)
+template <int DP, bool kResident>
+__global__ __launch_bounds__(kRingWaves * 64, 2) void cross_dq_ring_kernel(CrossArgs a, RowStats stats, int32_t chunks, int32_t blocks_per_chunk) {
+    using T = bf16_t;
+    using H = HeadShape<T, DP>;
+    using Ring = PairRing<DP, kRingWaves>;
+    constexpr int KSTEPS = H::KSTEPS, DT = H::DT;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    __shared__ uint64_t masks[kMaxTiles];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, g = lane >> 5;
+    const int pairs = a.B * a.kv_heads, group = a.heads / a.kv_heads;
+    const WorkPlace at(blockIdx.x, pairs);
+    const int pair = at.pair, chunk = at.place, kvh = pair % a.kv_heads, b = pair / a.kv_heads;
+    const int rows = a.Nq * group, blocks = (rows + 31) / 32;
+    RingKeys<DP> keys(a, b, kvh, wave, lane);
+    const int tiles = keys.tiles();
+    const uint32_t lds_base = lds_address(lds);
+    const auto request = [&](int t, int slot) { keys.request(t, lds_base + slot * Ring::kTileBytes, wave); };
+    const float scale_log2 = a.scale * kLog2e;
+    xu32x4_t qf[KSTEPS], gf[KSTEPS];
+    xf32x16_t dq[DT];
+    float dl = 0.f, lse = 0.f;
+    int64_t q_at = 0, h_at = 0;
+    const auto begin = [&](int block) {
+        const int r = min(block * 32 + l32, rows - 1), token = over_group(r, group), head = kvh * group + r - token * group;
+        q_at = static_cast<int64_t>(b) * a.Nq + token;
+        h_at = static_cast<int64_t>(head) * a.dh;
+        const int64_t stat = (static_cast<int64_t>(b) * a.heads + head) * a.Nq + token;
+        dl = load_row<T, DP, true>(a, q_at, h_at, g, qf, gf);
+        lse = a.lse[stat];
+        if (g == 0 && block * 32 + l32 < rows) {
+            stats.lse[stat] = -lse / a.scale;
+            stats.delta[stat] = -dl;
+        }
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) clear_tile(dq[dt]);
+        arrived(qf);
+        arrived(gf);
+    };
+    const auto multiply = [&](const char* tile, uint64_t valid) {
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+            const uint32_t bits = static_cast<uint32_t>(valid >> (32 * kb));
+            dq_block<T, DP>(tile, tile + Ring::kSecond, kb * 32, lane, bits == ~0u ? bits : bits >> (8 * g), qf, gf, dl, lse * kLog2e, scale_log2, dq);
+        }
+    };
+    const auto finish = [&](bool on) { store_column<T, true, DT>(static_cast<T*>(a.dq) + q_at * a.dq_stride + h_at, a.dh, g, dq, a.scale, on); };
+    if constexpr (kResident) {
+        for (int t = 0; t < tiles; ++t) request(t, t);
+        bring_keys(keys, lds, masks, 0, wave, lane);
+        const int first = chunk * blocks_per_chunk, last = min(first + blocks_per_chunk, blocks);
+        for (int block = first + wave; block < last; block += kRingWaves) {
+            begin(block);
+            for (int t = 0; t < tiles; ++t)
+                multiply(lds + t * Ring::kTileBytes, keys.mask ? masks[t] : keys_below(keys.len - t * Tile<T, DP>::kRows));
+            finish(block * 32 + l32 < rows);
+        }
+    } else {
+        const int block = chunk * kRingWaves + wave;
+#pragma unroll
+        for (int s = 0; s < kRing - 1; ++s)
+            if (s < tiles) request(s, s);
+        begin(block);
+        int slot = 0, free_slot = kRing - 1;
+        for (int t = 0; t < tiles; ++t) {
+            const uint64_t valid = keys.valid(t, lane);
+            if (t + kRing - 1 <= tiles) wait_vm_barrier<(kRing - 2) * Ring::N>();
+            else wait_vm_barrier<0>();
+            char* const tile = lds + slot * Ring::kTileBytes;
+            if (keys.mask && valid != ~0ull) {
+                keys.drop(tile, 0, valid, wave, lane);
+                __syncthreads();
+            }
+            if (t + kRing - 1 < tiles) request(t + kRing - 1, free_slot);
+            multiply(tile, valid);
+            free_slot = slot;
+            slot = slot + 1 == kRing ? 0 : slot + 1;
+        }
+        finish(block * 32 + l32 < rows);
+    }
+}
+
+// NW wavefronts: KW of them have 32 keys each, and with KW < NW the blocks of a tile's rows go to two, whose sums are added at the end
+template <int DP, int NW, int KW>
+__global__ __launch_bounds__(NW * 64, NW / 4) void cross_dkv_ring_kernel(CrossArgs a, RowStats row_stats, GradParts pt, int32_t k_tiles) {
+    using T = bf16_t;
+    using H = HeadShape<T, DP>;
+    using TL = Tile<T, DP>;
+    using Ring = PairRing<DP, NW>;
+    constexpr int KSTEPS = H::KSTEPS, DT = H::DT, BR = TL::kRows, QW = NW / KW, RB = 2 / QW;
+    constexpr int kSlot = Ring::kTileBytes + NW * 256;                   // a tile, then -lse / scale and -delta of its rows (and room for the other wavefronts' loads)
+    static_assert(QW == 1 || QW == 2, "blocks of a tile");
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, g = lane >> 5;
+    const int kw = wave % KW, qw = wave / KW;
+    const int pairs = a.B * a.kv_heads, group = a.heads / a.kv_heads;
+    const WorkPlace at(blockIdx.x, pairs);
+    const int pair = at.pair, k_tile = at.place % k_tiles, part = at.place / k_tiles;
+    const int kvh = pair % a.kv_heads, b = pair / a.kv_heads;
+    const int rows = a.Nq * group, first_key = (k_tile * KW + kw) * 32, key = first_key + l32;
+    const int len = attended(a, b);
+    const int t0 = part * pt.tiles, t1 = k_tile * 32 * KW < len ? min(t0 + pt.tiles, (rows + BR - 1) / BR) : t0;
+    const bool there = key < len && (!a.key_mask || a.key_mask[static_cast<int64_t>(b) * a.Nk + key] != 0);
+    const bool busy = first_key < len;                                   // (a wavefront without keys takes part in the loads alone)
+
+    const int64_t first_row = static_cast<int64_t>(b) * a.Nq, h0 = static_cast<int64_t>(kvh) * group * a.dh;
+    const bf16_t* const qp = static_cast<const T*>(a.q) + first_row * a.q_stride + h0;
+    const bf16_t* const gp = static_cast<const T*>(a.dout) + first_row * a.dout_stride + h0;
+    const int64_t stat0 = (static_cast<int64_t>(b) * a.heads + kvh * group) * a.Nq;
+    const uint32_t lds_base = lds_address(lds);
+    Ring ring;
+    const auto aim = [&](int rest) {                                     // row r of a tile is token (rest + r) / group of it
+        ring.aim(wave, lane, a.dh, [&](int second, int r) {
+            const int token = over_group(rest + r, group);
+            return (token * static_cast<int>(second ? a.dout_stride : a.q_stride) + (rest + r - token * group) * a.dh) * 2;
+        });
+    };
+    aim(0);
+    const bool turn = BR % group != 0;                                   // tiles begin at other heads of the group
+    const auto request = [&](int t, int slot) {
+        const int r0 = t * BR, token0 = over_group(r0, group), rest = r0 - token0 * group;
+        if (turn) aim(rest);
+        const uint32_t to = lds_base + slot * kSlot;
+        ring.request(rows_rsrc(qp, token0, a.Nq - token0, a.q_stride, group * a.dh), rows_rsrc(gp, token0, a.Nq - token0, a.dout_stride, group * a.dh), to, wave);
+        const int token = over_group(rest + lane, group), head = rest + lane - token * group;
+        const int off = wave < 2 && r0 + lane < rows ? (head * a.Nq + token) * 4 : kNowhere;         // (rows past the end are zero, and add nothing)
+        const float* const from = (wave == 0 ? row_stats.lse : row_stats.delta) + stat0 + token0;
+        dma_floats(to + Ring::kTileBytes + wave * 256, off, make_rsrc(from, (static_cast<int64_t>(rows) - token0) * 4));
+    };
+#pragma unroll
+    for (int s = 0; s < kRing - 1; ++s)
+        if (t0 + s < t1) request(t0 + s, s);
+
+    const int64_t kv_at = static_cast<int64_t>(b) * a.Nk + (key < a.Nk ? key : 0), h_at = static_cast<int64_t>(kvh) * a.dh;
+    xu32x4_t kf[KSTEPS], vf[KSTEPS];
+#pragma unroll
+    for (int ks = 0; ks < KSTEPS; ++ks) {
+        kf[ks] = vf[ks] = xu32x4_t{0, 0, 0, 0};
+        if (there) {
+            kf[ks] = row_chunk<T, true>(static_cast<const T*>(a.k) + kv_at * a.k_stride + h_at, 2 * ks + g, a.dh);
+            vf[ks] = row_chunk<T, true>(static_cast<const T*>(a.v) + kv_at * a.v_stride + h_at, 2 * ks + g, a.dh);
+        }
+    }
+    const float scale_log2 = a.scale * kLog2e;
+    xf32x16_t dk[DT], dv[DT];
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) {
+        clear_tile(dk[dt]);
+        clear_tile(dv[dt]);
+    }
+    arrived(kf);
+    arrived(vf);
+    int slot = 0, free_slot = kRing - 1;
+    for (int t = t0; t < t1; ++t) {
+        if (t + kRing - 1 <= t1) wait_vm_barrier<(kRing - 2) * (Ring::N + 1)>();
+        else wait_vm_barrier<0>();
+        if (t + kRing - 1 < t1) request(t + kRing - 1, free_slot);
+        const char* const tile = lds + slot * kSlot;
+        const float* const lse = reinterpret_cast<const float*>(tile + Ring::kTileBytes);
+        if (busy) {
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb) dkv_block<T, DP>(tile, tile + Ring::kSecond, (qw * RB + rb) * 32, lane, lse, lse + 64, kf, vf, scale_log2, dk, dv);
+        }
+        free_slot = slot;
+        slot = slot + 1 == kRing ? 0 : slot + 1;
+    }
+    if constexpr (QW == 2) {
+        // the second blocks' sums to the first's wavefronts, dk and dv in turn
+        static_assert(KW * DT * 4096 <= kRing * kSlot, "the sums of half the wavefronts fit in the ring");
+        char* const to = lds + kw * DT * 4096 + lane * 16;
+        const auto add = [&](xf32x16_t (&v)[DT]) {
+            __syncthreads();
+            if (qw > 0) {
+#pragma unroll
+                for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+                    for (int e4 = 0; e4 < 4; ++e4)
+                        *reinterpret_cast<xf32x4_t*>(to + (dt * 4 + e4) * 1024) = xf32x4_t{v[dt][4 * e4], v[dt][4 * e4 + 1], v[dt][4 * e4 + 2], v[dt][4 * e4 + 3]};
+            }
+            __syncthreads();
+            if (qw == 0) {
+#pragma unroll
+                for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+                    for (int e4 = 0; e4 < 4; ++e4) {
+                        const xf32x4_t o = *reinterpret_cast<const xf32x4_t*>(to + (dt * 4 + e4) * 1024);
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) v[dt][4 * e4 + c] += o[c];
+                    }
+            }
+        };
+        add(dk);
+        add(dv);
+        if (qw > 0) return;
+    }
+    const bool on = key < a.Nk;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            dk[dt][e] = there ? dk[dt][e] : 0.f;
+            dv[dt][e] = there ? dv[dt][e] : 0.f;
+        }
+    if (pt.parts > 1) {
+        const int64_t to = ((part * static_cast<int64_t>(pairs) + pair) * a.Nk + key) * a.dh;
+        store_column<float, true, DT>(pt.sum0 + to, a.dh, g, dk, 1.0f, on);
+        store_column<float, true, DT>(pt.sum1 + to, a.dh, g, dv, 1.0f, on);
+    } else {
+        store_column<T, true, DT>(static_cast<T*>(a.dk) + kv_at * a.dk_stride + h_at, a.dh, g, dk, a.scale, on);
+        store_column<T, true, DT>(static_cast<T*>(a.dv) + kv_at * a.dv_stride + h_at, a.dh, g, dv, 1.0f, on);
     }
 }
 
@@ -313,32 +559,65 @@ int32_t launch_sum(const SumJobs& a, int jobs, hipStream_t s) {
 
 // How the two launches are cut; by the sizes alone
 struct Plan {
-    int32_t q_parts, q_part_tiles;
-    int64_t q_tiles;
-    int kw;
-    int32_t k_parts, k_part_tiles;                // (parts: those of the wavefronts counted)
-    int64_t k_tiles;
+    bool q_ring, resident;
+    int32_t q_parts, q_part_tiles, q_blocks;      // q_blocks: resident, 32-row blocks of a workgroup
+    int64_t q_tiles;                              // workgroups of a (sample, key head) and part
+    bool k_ring;
+    int kw;                                       // wavefronts with keys of their own
+    int32_t k_parts, k_part_tiles;                // (parts: where two wavefronts have the same keys and keep their sums, those counted)
+    int64_t k_tiles, k_units;                     // workgroups of a (sample, key head) and part; parts that a workgroup has
 };
 constexpr int kUnits = 256;
 
-Plan plan_of(int32_t B, int32_t Nq, int32_t Nk, int32_t heads, int32_t kv_heads, int32_t dtype) {
-    const int64_t pairs = static_cast<int64_t>(B) * kv_heads, rows = static_cast<int64_t>(Nq) * (heads / kv_heads);
+// wavefronts of cross_dkv_ring_kernel: head dimensions over 80 need the registers of two
+template <int DP>
+constexpr int kKeyWaves = DP <= 80 ? 8 : 4;
+
+Plan plan_of(int32_t B, int32_t Nq, int32_t Nk, int32_t heads, int32_t kv_heads, int32_t dh, int32_t dtype, bool whole_chunks) {
+    const int64_t pairs = static_cast<int64_t>(B) * kv_heads, rows = static_cast<int64_t>(Nq) * (heads / kv_heads), units = std::max<int64_t>(pairs, 1);
     const int tile = dtype == FREE_BF16 ? 64 : 32;
-    const auto cut = [](int64_t work, int64_t tiles, int64_t least, int64_t* parts, int64_t* per) {
-        *parts = std::min<int64_t>(std::max<int64_t>(1, std::min(2 * kUnits / std::max<int64_t>(work, 1), tiles / least)), 64);
+    const auto cut = [](int64_t work, int64_t want, int64_t tiles, int64_t least, int64_t* parts, int64_t* per) {
+        *parts = std::min<int64_t>(std::max<int64_t>(1, std::min(want / std::max<int64_t>(work, 1), tiles / least)), 64);
         *per = (tiles + *parts - 1) / *parts;
         *parts = (tiles + *per - 1) / *per;
     };
+    const bool ring = dtype == FREE_BF16 && whole_chunks && rows < 1 << 29;       // (32-bit offsets of a row's floats)
+    const int64_t key_tiles = std::max<int64_t>(1, (static_cast<int64_t>(Nk) + tile - 1) / tile), row_tiles = std::max<int64_t>(1, (rows + tile - 1) / tile);
     Plan p{};
     int64_t parts, per;
-    p.q_tiles = std::max<int64_t>(1, (rows + 127) / 128);
-    cut(pairs * p.q_tiles, std::max<int64_t>(1, (static_cast<int64_t>(Nk) + tile - 1) / tile), 4, &parts, &per);
-    p.q_parts = static_cast<int32_t>(parts);
-    p.q_part_tiles = static_cast<int32_t>(per);
-    p.kw = dtype == FREE_BF16 && Nk <= 64 ? 2 : 4;
-    p.k_tiles = std::max<int64_t>(1, (static_cast<int64_t>(Nk) + 32 * p.kw - 1) / (32 * p.kw));
-    cut(pairs * p.k_tiles, std::max<int64_t>(1, (rows + tile - 1) / tile), 4, &parts, &per);
-    p.k_parts = static_cast<int32_t>(parts * (4 / p.kw));
+    const int64_t blocks = (rows + 31) / 32;
+    if (ring && pairs * blocks >= kUnits * kRingWaves) {
+        p.q_ring = true;
+        p.resident = key_tiles <= tiles_that_fit(dh);
+        p.q_parts = 1;
+        p.q_part_tiles = static_cast<int32_t>(key_tiles);
+        p.q_tiles = (blocks + kRingWaves - 1) / kRingWaves;
+        if (p.resident) {
+            const int64_t want = std::max<int64_t>(1, kUnits / units), rounds = std::max<int64_t>(1, (p.q_tiles + want - 1) / want);
+            p.q_blocks = static_cast<int32_t>(rounds * kRingWaves);
+            p.q_tiles = (blocks + p.q_blocks - 1) / p.q_blocks;
+        }
+    } else {
+        p.q_tiles = std::max<int64_t>(1, (rows + 127) / 128);
+        cut(pairs * p.q_tiles, 2 * kUnits, key_tiles, 4, &parts, &per);
+        p.q_parts = static_cast<int32_t>(parts);
+        p.q_part_tiles = static_cast<int32_t>(per);
+    }
+    // (fewer rows leave the ring without a tile to be ahead of)
+    if (ring && pairs * row_tiles >= kUnits * 4) {
+        p.k_ring = true;
+        p.kw = dh <= 80 && Nk > 128 ? 8 : 4;
+        p.k_tiles = std::max<int64_t>(1, (static_cast<int64_t>(Nk) + 32 * p.kw - 1) / (32 * p.kw));
+        cut(pairs * p.k_tiles, kUnits, row_tiles, 4, &parts, &per);
+        p.k_parts = static_cast<int32_t>(parts);
+        p.k_units = 1;
+    } else {
+        p.kw = dtype == FREE_BF16 && Nk <= 64 ? 2 : 4;
+        p.k_tiles = std::max<int64_t>(1, (static_cast<int64_t>(Nk) + 32 * p.kw - 1) / (32 * p.kw));
+        cut(pairs * p.k_tiles, 2 * kUnits, row_tiles, 4, &parts, &per);
+        p.k_units = 4 / p.kw;
+        p.k_parts = static_cast<int32_t>(parts * p.k_units);
+    }
     p.k_part_tiles = static_cast<int32_t>(per);
     return p;
 }
@@ -346,11 +625,12 @@ Plan plan_of(int32_t B, int32_t Nq, int32_t Nk, int32_t heads, int32_t kv_heads,
 size_t up256(size_t n) { return (n + 255) / 256 * 256; }
 
 struct Space {
-    size_t delta, dq, dk, dv, bytes;              // offsets
+    size_t lse, delta, dq, dk, dv, bytes;         // offsets
     Space(const Plan& p, int32_t B, int32_t Nq, int32_t Nk, int32_t heads, int32_t kv_heads, int32_t dh) {
-        delta = 0;
+        lse = 0;
+        delta = up256(static_cast<size_t>(B) * heads * Nq * sizeof(float));
         // the parts of dq and those of dk, dv take turns
-        dq = dk = up256(static_cast<size_t>(B) * heads * Nq * sizeof(float));
+        dq = dk = 2 * delta;
         const size_t q = p.q_parts > 1 ? static_cast<size_t>(p.q_parts) * B * Nq * heads * dh * sizeof(float) : 0;
         const size_t kv = p.k_parts > 1 ? up256(static_cast<size_t>(p.k_parts) * B * Nk * kv_heads * dh * sizeof(float)) : 0;
         dv = dk + kv;
@@ -358,39 +638,82 @@ struct Space {
     }
 };
 
+template <typename K>
+bool allow(K kern, LdsLimit& limit, size_t lds) { return limit.allow(reinterpret_cast<const void*>(kern), lds); }
+
 template <typename T, int DP, bool kVec>
-int32_t launch_shape(const CrossArgs& a, const Plan& p, const Space& w, char* ws, hipStream_t s) {
+int32_t launch_dq(const CrossArgs& a, const Plan& p, const RowStats& stats, const GradParts& pt, hipStream_t s) {
     using TL = Tile<T, DP>;
-    const int64_t pairs = static_cast<int64_t>(a.B) * a.kv_heads;
-    const int64_t q_blocks = pairs * p.q_tiles * p.q_parts, k_blocks = pairs * p.k_tiles * (p.k_parts / (4 / p.kw));
-    if (q_blocks > 0x7fffffff || k_blocks > 0x7fffffff) return FREE_ERR_LIMIT;
-    float* const delta = reinterpret_cast<float*>(ws + w.delta);
-    {
-        const GradParts pt{p.q_parts, p.q_part_tiles, reinterpret_cast<float*>(ws + w.dq), nullptr};
-        auto kern = cross_dq_kernel<T, DP, kVec>;
-        const size_t lds = 4 * TL::kBytes;
-        static LdsLimit limit;
-        if (!limit.allow(reinterpret_cast<const void*>(kern), lds)) return FREE_ERR_HIP;
-        hipLaunchKernelGGL(kern, dim3(static_cast<uint32_t>(q_blocks)), dim3(kThreads), lds, s, a, delta, pt, static_cast<int32_t>(p.q_tiles));
-        if (!launch_ok()) return FREE_ERR_HIP;
-        if (p.q_parts > 1) {
-            const SumJobs sum{{{pt.sum0, a.dq, a.dq_stride, a.scale}, {}}, p.q_parts, a.kv_heads, a.Nq, a.heads / a.kv_heads, a.dh, pairs};
-            const int32_t st = launch_sum<T, kVec>(sum, 1, s);
-            if (st != FREE_OK) return st;
+    const dim3 grid(static_cast<uint32_t>(static_cast<int64_t>(a.B) * a.kv_heads * p.q_tiles * p.q_parts));
+    if constexpr (sizeof(T) == 2 && kVec) {
+        if (p.q_ring) {
+            const size_t lds = static_cast<size_t>(p.resident ? p.q_part_tiles : kRing) * PairRing<DP, kRingWaves>::kTileBytes + 128;
+            const auto launch = [&](auto resident) {
+                auto kern = cross_dq_ring_kernel<DP, decltype(resident)::value>;
+                static LdsLimit limit;
+                if (!allow(kern, limit, kLdsBytes)) return FREE_ERR_HIP;
+                hipLaunchKernelGGL(kern, grid, dim3(kRingWaves * 64), lds, s, a, stats, static_cast<int32_t>(p.q_tiles), p.q_blocks);
+                return launch_ok() ? FREE_OK : FREE_ERR_HIP;
+            };
+            return p.resident ? launch(std::true_type{}) : launch(std::false_type{});
         }
     }
-    const GradParts pt{p.k_parts, p.k_part_tiles, reinterpret_cast<float*>(ws + w.dk), reinterpret_cast<float*>(ws + w.dv)};
+    auto kern = cross_dq_kernel<T, DP, kVec>;
+    static LdsLimit limit;
+    if (!allow(kern, limit, 4 * TL::kBytes)) return FREE_ERR_HIP;
+    hipLaunchKernelGGL(kern, grid, dim3(kThreads), 4 * TL::kBytes, s, a, stats, pt, static_cast<int32_t>(p.q_tiles));
+    return launch_ok() ? FREE_OK : FREE_ERR_HIP;
+}
+
+template <typename T, int DP, bool kVec>
+int32_t launch_dkv(const CrossArgs& a, const Plan& p, const RowStats& stats, const GradParts& pt, hipStream_t s) {
+    using TL = Tile<T, DP>;
+    const dim3 grid(static_cast<uint32_t>(static_cast<int64_t>(a.B) * a.kv_heads * p.k_tiles * (p.k_parts / p.k_units)));
+    if constexpr (sizeof(T) == 2 && kVec) {
+        if (p.k_ring) {
+            constexpr int NW = kKeyWaves<DP>;
+            const size_t lds = kRing * (PairRing<DP, NW>::kTileBytes + NW * 256) + 128;
+            const auto launch = [&](auto kw) {
+                auto kern = cross_dkv_ring_kernel<DP, NW, decltype(kw)::value>;
+                static LdsLimit limit;
+                if (!allow(kern, limit, lds)) return FREE_ERR_HIP;
+                hipLaunchKernelGGL(kern, grid, dim3(NW * 64), lds, s, a, stats, pt, static_cast<int32_t>(p.k_tiles));
+                return launch_ok() ? FREE_OK : FREE_ERR_HIP;
+            };
+            return p.kw == NW ? launch(std::integral_constant<int, NW>{}) : launch(std::integral_constant<int, 4>{});
+        }
+    }
     const size_t lds = 4 * TL::kBytes + 4 * TL::kRows * sizeof(float);
     const auto launch = [&](auto kw) {
         auto kern = cross_dkv_kernel<T, DP, decltype(kw)::value, kVec>;
         static LdsLimit limit;
-        if (!limit.allow(reinterpret_cast<const void*>(kern), lds)) return FREE_ERR_HIP;
-        hipLaunchKernelGGL(kern, dim3(static_cast<uint32_t>(k_blocks)), dim3(kThreads), lds, s, a, delta, pt, static_cast<int32_t>(p.k_tiles));
+        if (!allow(kern, limit, lds)) return FREE_ERR_HIP;
+        hipLaunchKernelGGL(kern, grid, dim3(kThreads), lds, s, a, stats, pt, static_cast<int32_t>(p.k_tiles));
         return launch_ok() ? FREE_OK : FREE_ERR_HIP;
     };
-    int32_t st = FREE_OK;
-    if constexpr (sizeof(T) == 2) st = p.kw == 2 ? launch(std::integral_constant<int, 2>{}) : launch(std::integral_constant<int, 4>{});
-    else st = launch(std::integral_constant<int, 4>{});
+    if constexpr (sizeof(T) == 2) {
+        if (p.kw == 2) return launch(std::integral_constant<int, 2>{});
+    }
+    return launch(std::integral_constant<int, 4>{});
+}
+
+template <typename T, int DP, bool kVec>
+int32_t launch_shape(const CrossArgs& a, const Plan& p, const Space& w, char* ws, hipStream_t s) {
+    const int64_t pairs = static_cast<int64_t>(a.B) * a.kv_heads;
+    if (pairs * p.q_tiles * p.q_parts > 0x7fffffff || pairs * p.k_tiles * p.k_parts > 0x7fffffff) return FREE_ERR_LIMIT;
+    const RowStats stats{reinterpret_cast<float*>(ws + w.lse), reinterpret_cast<float*>(ws + w.delta)};
+    if (a.Nq > 0) {
+        const GradParts pt{p.q_parts, p.q_part_tiles, reinterpret_cast<float*>(ws + w.dq), nullptr};
+        int32_t st = launch_dq<T, DP, kVec>(a, p, stats, pt, s);
+        if (st == FREE_OK && p.q_parts > 1) {
+            const SumJobs sum{{{pt.sum0, a.dq, a.dq_stride, a.scale}, {}}, p.q_parts, a.kv_heads, a.Nq, a.heads / a.kv_heads, a.dh, pairs};
+            st = launch_sum<T, kVec>(sum, 1, s);
+        }
+        if (st != FREE_OK) return st;
+    }
+    if (a.Nk == 0) return FREE_OK;
+    const GradParts pt{p.k_parts, p.k_part_tiles, reinterpret_cast<float*>(ws + w.dk), reinterpret_cast<float*>(ws + w.dv)};
+    const int32_t st = launch_dkv<T, DP, kVec>(a, p, stats, pt, s);
     if (st != FREE_OK || p.k_parts == 1) return st;
     const SumJobs sum{{{pt.sum0, a.dk, a.dk_stride, a.scale}, {pt.sum1, a.dv, a.dv_stride, 1.0f}}, p.k_parts, a.kv_heads, a.Nk, 1, a.dh, pairs};
     return launch_sum<T, kVec>(sum, 2, s);
@@ -407,11 +730,11 @@ int32_t launch_width(const CrossArgs& a, const Plan& p, const Space& w, char* ws
 
 template <typename T>
 int32_t launch_type(const CrossArgs& a, void* ws, hipStream_t s) {
-    const Plan p = plan_of(a.B, a.Nq, a.Nk, a.heads, a.kv_heads, sizeof(T) == 2 ? FREE_BF16 : FREE_FP32);
-    const Space w(p, a.B, a.Nq, a.Nk, a.heads, a.kv_heads, a.dh);
     const auto al = [](const void* x, int64_t stride) { return (reinterpret_cast<uintptr_t>(x) & 15u) == 0 && stride % static_cast<int64_t>(16 / sizeof(T)) == 0; };
     const bool vec = a.dh % static_cast<int>(16 / sizeof(T)) == 0 && al(a.q, a.q_stride) && al(a.k, a.k_stride) && al(a.v, a.v_stride) && al(a.out, a.out_stride) &&
                      al(a.dout, a.dout_stride) && al(a.dq, a.dq_stride) && al(a.dk, a.dk_stride) && al(a.dv, a.dv_stride);
+    const Plan p = plan_of(a.B, a.Nq, a.Nk, a.heads, a.kv_heads, a.dh, sizeof(T) == 2 ? FREE_BF16 : FREE_FP32, vec);
+    const Space w(p, a.B, a.Nq, a.Nk, a.heads, a.kv_heads, a.dh);
     char* const base = static_cast<char*>(ws);
     return vec ? launch_width<T, true>(a, p, w, base, s) : launch_width<T, false>(a, p, w, base, s);
 }
@@ -419,7 +742,9 @@ int32_t launch_type(const CrossArgs& a, void* ws, hipStream_t s) {
 }  // namespace
 
 size_t cross_backward_bytes(int32_t B, int32_t Nq, int32_t Nk, int32_t heads, int32_t kv_heads, int32_t dh, int32_t dtype) {
-    return Space(plan_of(B, Nq, Nk, heads, kv_heads, dtype), B, Nq, Nk, heads, kv_heads, dh).bytes;
+    // (whichever way the tensors' alignment leaves)
+    const auto bytes = [&](bool whole) { return Space(plan_of(B, Nq, Nk, heads, kv_heads, dh, dtype, whole), B, Nq, Nk, heads, kv_heads, dh).bytes; };
+    return std::max(bytes(true), bytes(false));
 }
 
 int32_t launch_cross_backward(const CrossArgs& a, int32_t dtype, void* ws, hipStream_t s) {

@@ -100,3 +100,19 @@ def test_sums_in_parts(dtype, B, Nq, Nk, heads, kv, dh):
 ])
 def test_many_queries(keys, B, Nq, Nk, heads, kv, dh):
     compare(*problem(5, B, Nq, Nk, heads, kv, dh, torch.bfloat16, keys), B, heads, kv, dh)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_no_queries_and_no_keys(dtype):
+    q, k, v, g, _, _ = problem(6, 2, 5, 9, 4, 2, 24, dtype, "all")
+    how = dict(B=2, heads=4, dh=24, kv_heads=2)
+    none = q[:0]
+    lse = torch.empty(2, 4, 0, device=DEV)
+    assert b.op_cross_attention(none, k, v, lse=lse, **how).shape == (0, 96)
+    dq, dk, dv = b.op_cross_attention_backward(none, none, k, v, none, lse, **how)
+    assert dq.shape == (0, 96) and torch.equal(dk, torch.zeros_like(k)) and torch.equal(dv, torch.zeros_like(v))
+    lse = torch.empty(2, 4, 5, device=DEV)
+    out = b.op_cross_attention(q, k[:0], v[:0], lse=lse, **how)
+    assert torch.equal(out, torch.zeros_like(q)) and torch.equal(lse, torch.full_like(lse, -math.inf))
+    dq, dk, dv = b.op_cross_attention_backward(g, q, k[:0], v[:0], out, lse, **how)
+    assert torch.equal(dq, torch.zeros_like(q)) and dk.shape == dv.shape == (0, 48)
