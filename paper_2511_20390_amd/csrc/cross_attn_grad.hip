@@ -41,13 +41,17 @@ __device__ __forceinline__ void dq_block(const char* tile_k, const char* tile_v,
     clear_tile(st);
 #pragma unroll
     for (int e = 0; e < 16; ++e) dp[e] = -dl;
+    // (wide heads have no registers for operands further ahead)
+    constexpr bool kFar = DP <= 64;
     read_rows<T, DP>(tile_k, row0, lane, 0, fk);
-    read_rows<T, DP>(tile_v, row0, lane, 0, fv);
+    if constexpr (kFar) read_rows<T, DP>(tile_v, row0, lane, 0, fv);
     fence();
     row_products<T, DP>(tile_k, row0, lane, fk, qf, st);
-    ck.read(tile_k, row0, lane, 0);
+    if constexpr (kFar) ck.read(tile_k, row0, lane, 0);
+    else read_rows<T, DP>(tile_v, row0, lane, 0, fv);
     fence();
     row_products<T, DP>(tile_v, row0, lane, fv, gf, dp);
+    if constexpr (!kFar) ck.read(tile_k, row0, lane, 0);
 #pragma unroll
     for (int e = 0; e < 16; ++e) st[e] = __builtin_amdgcn_exp2f(fmaf(st[e], scale_log2, -lse2)) * dp[e];
     if (__builtin_amdgcn_readfirstlane(bits) != ~0u) {
@@ -93,28 +97,46 @@ __device__ __forceinline__ void dkv_block(const char* tile_q, const char* tile_g
     column_products<T, DP>(tile_q, row0, lane, cq, dp, dk);
 }
 
-// a row's q and dout as operands, and sum dout out
+// A row's chunks of q, dout and out, and sum dout out of them
 template <typename T, int DP, bool kVec>
-__device__ __forceinline__ float load_row(const CrossArgs& a, int64_t q_at, int64_t h_at, int g, xu32x4_t (&qf)[HeadShape<T, DP>::KSTEPS],
-                                          xu32x4_t (&gf)[HeadShape<T, DP>::KSTEPS]) {
-    float dl = 0.f;
+struct RowOperands {
+    static constexpr int KSTEPS = HeadShape<T, DP>::KSTEPS;
+    xu32x4_t q[KSTEPS], g[KSTEPS];
+    int64_t q_at, h_at, stat;        // its row, its head's first value in it, and its place among [B, heads, Nq]
+    float lse;
+    __device__ __forceinline__ void load(const CrossArgs& a, int b, int kvh, int row, int half, xu32x4_t (&o)[KSTEPS]) {
+        const int group = a.heads / a.kv_heads, r = min(row, a.Nq * group - 1), token = over_group(r, group), head = kvh * group + r - token * group;
+        q_at = static_cast<int64_t>(b) * a.Nq + token;
+        h_at = static_cast<int64_t>(head) * a.dh;
+        stat = (static_cast<int64_t>(b) * a.heads + head) * a.Nq + token;
+        lse = a.lse[stat];
 #pragma unroll
-    for (int ks = 0; ks < HeadShape<T, DP>::KSTEPS; ++ks) {
-        qf[ks] = row_chunk<T, kVec>(static_cast<const T*>(a.q) + q_at * a.q_stride + h_at, 2 * ks + g, a.dh);
-        gf[ks] = row_chunk<T, kVec>(static_cast<const T*>(a.dout) + q_at * a.dout_stride + h_at, 2 * ks + g, a.dh);
-        const xu32x4_t of = row_chunk<T, kVec>(static_cast<const T*>(a.out) + q_at * a.out_stride + h_at, 2 * ks + g, a.dh);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            if constexpr (sizeof(T) == 2) {
-                dl = fmaf(__uint_as_float(gf[ks][e] << 16), __uint_as_float(of[e] << 16), dl);
-                dl = fmaf(__uint_as_float(gf[ks][e] & 0xffff0000u), __uint_as_float(of[e] & 0xffff0000u), dl);
-            } else {
-                dl = fmaf(__uint_as_float(gf[ks][e]), __uint_as_float(of[e]), dl);
-            }
+        for (int ks = 0; ks < KSTEPS; ++ks) {
+            g[ks] = row_chunk<T, kVec>(static_cast<const T*>(a.dout) + q_at * a.dout_stride + h_at, 2 * ks + half, a.dh);
+            o[ks] = row_chunk<T, kVec>(static_cast<const T*>(a.out) + q_at * a.out_stride + h_at, 2 * ks + half, a.dh);
+            q[ks] = row_chunk<T, kVec>(static_cast<const T*>(a.q) + q_at * a.q_stride + h_at, 2 * ks + half, a.dh);
         }
     }
-    return add_lane_xor<32>(dl);
-}
+    __device__ __forceinline__ float delta(const xu32x4_t (&o)[KSTEPS]) const {
+        float dl = 0.f;
+#pragma unroll
+        for (int ks = 0; ks < KSTEPS; ++ks)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                if constexpr (sizeof(T) == 2) {
+                    dl = fmaf(__uint_as_float(g[ks][e] << 16), __uint_as_float(o[ks][e] << 16), dl);
+                    dl = fmaf(__uint_as_float(g[ks][e] & 0xffff0000u), __uint_as_float(o[ks][e] & 0xffff0000u), dl);
+                } else {
+                    dl = fmaf(__uint_as_float(g[ks][e]), __uint_as_float(o[ks][e]), dl);
+                }
+            }
+        return add_lane_xor<32>(dl);
+    }
+    __device__ __forceinline__ void leave(const RowStats& stats, float dl, float scale) const {
+        stats.lse[stat] = -lse / scale;
+        stats.delta[stat] = -dl;
+    }
+};
 
 // ---- dq and delta
 template <typename T, int DP, bool kVec>
@@ -141,23 +163,18 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 || DP <= 64) ? 2 : 1) voi
     if (t0 < t1) keys.request(t0, lds_base, lds_base + TL::kBytes, wave, lane, valid);
     keys.request_mask(t0 + 1, lane);
 
-    const int q_row = row < rows ? row : rows - 1, token = over_group(q_row, group), head = kvh * group + q_row - token * group;
-    const int64_t q_at = static_cast<int64_t>(b) * a.Nq + token, h_at = static_cast<int64_t>(head) * a.dh;
-    const int64_t stat = (static_cast<int64_t>(b) * a.heads + head) * a.Nq + token;
-    xu32x4_t qf[KSTEPS], gf[KSTEPS];
-    const float dl = load_row<T, DP, kVec>(a, q_at, h_at, g, qf, gf);
-    const float lse = a.lse[stat], lse2 = lse * kLog2e, scale_log2 = a.scale * kLog2e;
-    if (part == 0 && g == 0 && row < rows) {
-        stats.lse[stat] = -lse / a.scale;
-        stats.delta[stat] = -dl;
-    }
+    RowOperands<T, DP, kVec> own;
+    xu32x4_t of[KSTEPS];
+    own.load(a, b, kvh, row, g, of);
+    const float dl = own.delta(of), lse2 = own.lse * kLog2e, scale_log2 = a.scale * kLog2e;
+    if (part == 0 && g == 0 && row < rows) own.leave(stats, dl, a.scale);
 
     xf32x16_t dq[DT];
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) clear_tile(dq[dt]);
     if (t0 < t1) keys.deliver(lds, lds + TL::kBytes, tid, valid);
-    arrived(qf);
-    arrived(gf);
+    arrived(own.q);
+    arrived(own.g);
     keys.k.settle();
     for (int t = t0; t < t1; ++t) {
         const int stage = (t - t0) & 1, other = (stage ^ 1) * 2 * TL::kBytes;
@@ -171,14 +188,14 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 || DP <= 64) ? 2 : 1) voi
         for (int kb = 0; kb < BKV / 32; ++kb) {
             // (fp32 has 32 keys to a tile, and a full mask of them)
             const uint32_t bits = static_cast<uint32_t>(valid >> (32 * kb));
-            dq_block<T, DP>(sK, sK + TL::kBytes, kb * 32, lane, bits == ~0u ? bits : bits >> (sizeof(T) == 2 ? 8 * g : 4 * g), qf, gf, dl, lse2, scale_log2, dq);
+            dq_block<T, DP>(sK, sK + TL::kBytes, kb * 32, lane, bits == ~0u ? bits : bits >> (sizeof(T) == 2 ? 8 * g : 4 * g), own.q, own.g, dl, lse2, scale_log2, dq);
         }
         if (t + 1 < t1) keys.deliver(lds + other, lds + other + TL::kBytes, tid, valid_next);
         valid = valid_next;
         keys.k.settle();
     }
     if (pt.parts > 1) store_column<float, kVec, DT>(pt.sum0 + ((part * static_cast<int64_t>(pairs) + pair) * rows + row) * a.dh, a.dh, g, dq, 1.0f, row < rows);
-    else store_column<T, kVec, DT>(static_cast<T*>(a.dq) + q_at * a.dq_stride + h_at, a.dh, g, dq, a.scale, row < rows);
+    else store_column<T, kVec, DT>(static_cast<T*>(a.dq) + own.q_at * a.dq_stride + own.h_at, a.dh, g, dq, a.scale, row < rows);
 }
 
 // ---- dk and dv.  KW wavefronts have 32 keys each; with KW 2 the two halves of a tile's rows go to two wavefronts, whose sums are parts of
@@ -320,49 +337,56 @@ __global__ __launch_bounds__(kRingWaves * 64, 2) void cross_dq_ring_kernel(Cross
     const uint32_t lds_base = lds_address(lds);
     const auto request = [&](int t, int slot) { keys.request(t, lds_base + slot * Ring::kTileBytes, wave); };
     const float scale_log2 = a.scale * kLog2e;
-    xu32x4_t qf[KSTEPS], gf[KSTEPS];
+    RowOperands<T, DP, true> own;
     xf32x16_t dq[DT];
-    float dl = 0.f, lse = 0.f;
-    int64_t q_at = 0, h_at = 0;
+    float dl = 0.f;
     const auto begin = [&](int block) {
-        const int r = min(block * 32 + l32, rows - 1), token = over_group(r, group), head = kvh * group + r - token * group;
-        q_at = static_cast<int64_t>(b) * a.Nq + token;
-        h_at = static_cast<int64_t>(head) * a.dh;
-        const int64_t stat = (static_cast<int64_t>(b) * a.heads + head) * a.Nq + token;
-        dl = load_row<T, DP, true>(a, q_at, h_at, g, qf, gf);
-        lse = a.lse[stat];
-        if (g == 0 && block * 32 + l32 < rows) {
-            stats.lse[stat] = -lse / a.scale;
-            stats.delta[stat] = -dl;
-        }
+        if (g == 0 && block * 32 + l32 < rows) own.leave(stats, dl, a.scale);
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt) clear_tile(dq[dt]);
-        arrived(qf);
-        arrived(gf);
+        arrived(own.q);
+        arrived(own.g);
     };
     const auto multiply = [&](const char* tile, uint64_t valid) {
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb) {
             const uint32_t bits = static_cast<uint32_t>(valid >> (32 * kb));
-            dq_block<T, DP>(tile, tile + Ring::kSecond, kb * 32, lane, bits == ~0u ? bits : bits >> (8 * g), qf, gf, dl, lse * kLog2e, scale_log2, dq);
+            dq_block<T, DP>(tile, tile + Ring::kSecond, kb * 32, lane, bits == ~0u ? bits : bits >> (8 * g), own.q, own.g, dl, own.lse * kLog2e, scale_log2, dq);
         }
     };
-    const auto finish = [&](bool on) { store_column<T, true, DT>(static_cast<T*>(a.dq) + q_at * a.dq_stride + h_at, a.dh, g, dq, a.scale, on); };
+    const auto finish = [&](int block) {
+        store_column<T, true, DT>(static_cast<T*>(a.dq) + own.q_at * a.dq_stride + own.h_at, a.dh, g, dq, a.scale, block * 32 + l32 < rows);
+    };
     if constexpr (kResident) {
+        // the next block's rows are requested ahead of this one's products where there are registers for them
+        constexpr bool kNext = DP <= 80;
         for (int t = 0; t < tiles; ++t) request(t, t);
-        bring_keys(keys, lds, masks, 0, wave, lane);
         const int first = chunk * blocks_per_chunk, last = min(first + blocks_per_chunk, blocks);
+        xu32x4_t of[KSTEPS];
+        if (first + wave < last) own.load(a, b, kvh, (first + wave) * 32 + l32, g, of);
+        bring_keys(keys, lds, masks, 0, wave, lane);
         for (int block = first + wave; block < last; block += kRingWaves) {
+            dl = own.delta(of);
             begin(block);
+            RowOperands<T, DP, true> next = own;
+            const bool more = block + kRingWaves < last;
+            if (kNext && more) next.load(a, b, kvh, (block + kRingWaves) * 32 + l32, g, of);
             for (int t = 0; t < tiles; ++t)
                 multiply(lds + t * Ring::kTileBytes, keys.mask ? masks[t] : keys_below(keys.len - t * Tile<T, DP>::kRows));
-            finish(block * 32 + l32 < rows);
+            finish(block);
+            own = next;
+            if (!kNext && more) own.load(a, b, kvh, (block + kRingWaves) * 32 + l32, g, of);
         }
     } else {
         const int block = chunk * kRingWaves + wave;
 #pragma unroll
         for (int s = 0; s < kRing - 1; ++s)
             if (s < tiles) request(s, s);
+        {
+            xu32x4_t of[KSTEPS];
+            own.load(a, b, kvh, block * 32 + l32, g, of);
+            dl = own.delta(of);
+        }
         begin(block);
         int slot = 0, free_slot = kRing - 1;
         for (int t = 0; t < tiles; ++t) {
@@ -379,7 +403,7 @@ __global__ __launch_bounds__(kRingWaves * 64, 2) void cross_dq_ring_kernel(Cross
             free_slot = slot;
             slot = slot + 1 == kRing ? 0 : slot + 1;
         }
-        finish(block * 32 + l32 < rows);
+        finish(block);
     }
 }
 
@@ -606,7 +630,7 @@ Plan plan_of(int32_t B, int32_t Nq, int32_t Nk, int32_t heads, int32_t kv_heads,
     // (fewer rows leave the ring without a tile to be ahead of)
     if (ring && pairs * row_tiles >= kUnits * 4) {
         p.k_ring = true;
-        p.kw = dh <= 80 && Nk > 128 ? 8 : 4;
+        p.kw = 4;                    // (eight, with both blocks of a tile each, leave twice the parts to add)
         p.k_tiles = std::max<int64_t>(1, (static_cast<int64_t>(Nk) + 32 * p.kw - 1) / (32 * p.kw));
         cut(pairs * p.k_tiles, kUnits, row_tiles, 4, &parts, &per);
         p.k_parts = static_cast<int32_t>(parts);
@@ -673,14 +697,11 @@ int32_t launch_dkv(const CrossArgs& a, const Plan& p, const RowStats& stats, con
         if (p.k_ring) {
             constexpr int NW = kKeyWaves<DP>;
             const size_t lds = kRing * (PairRing<DP, NW>::kTileBytes + NW * 256) + 128;
-            const auto launch = [&](auto kw) {
-                auto kern = cross_dkv_ring_kernel<DP, NW, decltype(kw)::value>;
-                static LdsLimit limit;
-                if (!allow(kern, limit, lds)) return FREE_ERR_HIP;
-                hipLaunchKernelGGL(kern, grid, dim3(NW * 64), lds, s, a, stats, pt, static_cast<int32_t>(p.k_tiles));
-                return launch_ok() ? FREE_OK : FREE_ERR_HIP;
-            };
-            return p.kw == NW ? launch(std::integral_constant<int, NW>{}) : launch(std::integral_constant<int, 4>{});
+            auto kern = cross_dkv_ring_kernel<DP, NW, 4>;
+            static LdsLimit limit;
+            if (!allow(kern, limit, lds)) return FREE_ERR_HIP;
+            hipLaunchKernelGGL(kern, grid, dim3(NW * 64), lds, s, a, stats, pt, static_cast<int32_t>(p.k_tiles));
+            return launch_ok() ? FREE_OK : FREE_ERR_HIP;
         }
     }
     const size_t lds = 4 * TL::kBytes + 4 * TL::kRows * sizeof(float);
