@@ -11,7 +11,7 @@
 //  * dA and dB: 128 columns of x or dout by all ranks per workgroup, over the rows of one adapter, in parts that a second launch adds in
 //    order.  Rows of other adapters are not read.
 // For the gradient W, B and A are needed the other way round ([K][N], [rank][N], [K][rank]): copies of that layout go into the workspace, filled
-// up with zeros to whole slices. 
+// up with zeros to whole slices.
 #include <algorithm>
 
 #include "adapter_term.h"
@@ -77,8 +77,8 @@ __global__ __launch_bounds__(kDownWaves * 64) void adapter_down_kernel(DownArgs 
     const T* x[MT];
 #pragma unroll
     for (int t = 0; t < MT; ++t) {
-        const int m = m0 + t * 16 + r16;
-        x[t] = static_cast<const T*>(a.x) + static_cast<int64_t>(m < a.M ? m : a.M - 1) * a.K + at;
+        const int row = mine >> (t * 16 + r16) & 1 ? t * 16 + r16 : __builtin_ctzll(mine);      // (other adapters' rows are not read)
+        x[t] = static_cast<const T*>(a.x) + static_cast<int64_t>(m0 + row) * a.K + at;
     }
     f32x4a_t acc[RT][MT];
 #pragma unroll
@@ -361,20 +361,32 @@ __global__ __launch_bounds__(kThreads) void adapter_sum_kernel(SumArgs a) {
                 stage ^= 1;
             }
         } else {
-            constexpr int kPairs = RB == 1 ? 32 : 16;            // row pairs whose loads are in flight together
-            const int col = c0 + wave * 32 + l32;
+            constexpr int kPairs = RB == 1 ? 32 : RB == 2 ? 16 : 8;        // row pairs whose loads are in flight together
+            const int col = min(c0 + wave * 32 + l32, cols - 1);
+            int rank[RB];
+#pragma unroll
+            for (int b = 0; b < RB; ++b) rank[b] = min(b * 32 + l32, a.t_row - 1);
             for (int i = next(0); i < count; i = next(i + 1)) {
                 const uint64_t bits = masks[i];
+                const int own = __builtin_ctzll(bits);
                 const int64_t m0 = static_cast<int64_t>(base + i) * kTileRows;
-#pragma unroll kPairs
-                for (int k = 0; k < kTileRows / 2; ++k) {
-                    const int row = 2 * k + g;
-                    const bool on = bits >> row & 1;
-                    const float w = on && col < cols ? wide[(m0 + row) * ld + col] : 0.f;
+                // (rows of other adapters: one of this adapter's is read again and zeros multiply)
 #pragma unroll
-                    for (int b = 0; b < RB; ++b) {
-                        const float t = on && b * 32 + l32 < a.t_row ? thin[(m0 + row) * a.t_row + b * 32 + l32] : 0.f;
-                        acc[b] = __builtin_amdgcn_mfma_f32_32x32x2f32(w, t, acc[b], 0, 0, 0);
+                for (int k0 = 0; k0 < kTileRows / 2; k0 += kPairs) {
+                    float wv[kPairs], tv[RB][kPairs];
+#pragma unroll
+                    for (int k = 0; k < kPairs; ++k) {
+                        const int row = 2 * (k0 + k) + g, from = bits >> row & 1 ? row : own;
+                        wv[k] = wide[(m0 + from) * ld + col];
+#pragma unroll
+                        for (int b = 0; b < RB; ++b) tv[b][k] = thin[(m0 + from) * a.t_row + rank[b]];
+                    }
+#pragma unroll
+                    for (int k = 0; k < kPairs; ++k) {
+                        const bool on = bits >> (2 * (k0 + k) + g) & 1;
+#pragma unroll
+                        for (int b = 0; b < RB; ++b)
+                            acc[b] = __builtin_amdgcn_mfma_f32_32x32x2f32(on ? wv[k] : 0.f, on ? tv[b][k] : 0.f, acc[b], 0, 0, 0);
                     }
                 }
             }
@@ -465,13 +477,13 @@ struct ForwardSpace {
     }
 };
 
-// Parts of the rows of the weights' gradients: workgroups for the chip, at least 4 tiles of 64 rows each.
+// Parts of the rows of the weights' gradients: workgroups for the chip, at least 4 tiles of 64 rows each (fp32, whose rows take longer: 2).
 struct SumPlan {
     int32_t parts, part_tiles;
     explicit SumPlan(const Sizes& z) {
         const int64_t tiles = std::max<int64_t>(1, (static_cast<int64_t>(z.M) + kTileRows - 1) / kTileRows);
         const int64_t groups = (static_cast<int64_t>(z.K + 127) / 128 + (z.N + 127) / 128) * z.n;
-        const int64_t want = std::max<int64_t>(1, std::min({(1024 + groups - 1) / groups, tiles / 4, static_cast<int64_t>(32)}));
+        const int64_t want = std::max<int64_t>(1, std::min({(1024 + groups - 1) / groups, tiles / (z.es == 2 ? 4 : 2), static_cast<int64_t>(32)}));
         part_tiles = static_cast<int32_t>((tiles + want - 1) / want);
         parts = static_cast<int32_t>((tiles + part_tiles - 1) / part_tiles);
     }
@@ -607,6 +619,7 @@ int32_t backward_of(const Sizes& z, const AdapterArgs& a, char* ws, hipStream_t 
 // 32-bit byte offsets inside a tile of 384 rows, grids of less than 2^32 threads
 bool adapters_cover(int32_t M, int32_t K, int32_t N, int32_t r, int32_t n, int32_t dtype) {
     if (K > 1 << 20 || N > 1 << 20 || r > 128 || n > 16384) return false;
+    if (static_cast<int64_t>(K) * N > int64_t{1} << 34 || (static_cast<int64_t>(K) + N + 128) * n > 1 << 28) return false;
     const int64_t m = (static_cast<int64_t>(M) + 127) / 128, k = (K + 127) / 128, c = (N + 127) / 128;
     return std::max(m * k, m * c) <= (dtype == FREE_FP32 ? 1 << 20 : 1 << 22) && (static_cast<int64_t>(K) + N) * r * n <= int64_t{1} << 36;
 }

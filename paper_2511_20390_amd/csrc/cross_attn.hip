@@ -580,7 +580,7 @@ Plan plan_of(int32_t B, int32_t Nq, int32_t Nk, int32_t heads, int32_t kv_heads,
 template <typename T, int DP, bool kVec>
 int32_t launch_shape(const CrossArgs& a, const Plan& p, const Parts& pt, hipStream_t s) {
     const int64_t blocks = static_cast<int64_t>(a.B) * a.kv_heads * p.q_tiles * p.parts;
-    if (blocks > 0x7fffffff) return FREE_ERR_LIMIT;
+    if (blocks >= 1 << 23) return FREE_ERR_LIMIT;
     constexpr int DT = HeadShape<T, DP>::DT;
     if (p.few) {
         const size_t lds = 4 * std::max<size_t>(32 * kValueRow<T, DP> + (sizeof(T) == 4 ? 128 : 0), DT * 4096 + 512);

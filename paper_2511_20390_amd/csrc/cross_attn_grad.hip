@@ -556,28 +556,30 @@ template <typename T, int V>
 __global__ __launch_bounds__(kThreads) void cross_sum_kernel(SumJobs a) {
     const SumJob& j = blockIdx.y ? a.job[1] : a.job[0];
     const uint32_t rows = static_cast<uint32_t>(a.tokens) * a.group, per_row = a.dh / V;
-    const int64_t all = a.pairs * rows * per_row, i = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x;
-    if (i >= all) return;
-    float s[V];
-    __builtin_memcpy(s, j.parts + i * V, sizeof(s));
-    for (int p = 1; p < a.n; ++p) {
-        float v[V];
-        __builtin_memcpy(v, j.parts + (p * all + i) * V, sizeof(v));
+    const int64_t all = a.pairs * rows * per_row;
+    for (int64_t i = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x; i < all; i += static_cast<int64_t>(gridDim.x) * kThreads) {
+        float s[V];
+        __builtin_memcpy(s, j.parts + i * V, sizeof(s));
+        for (int p = 1; p < a.n; ++p) {
+            float v[V];
+            __builtin_memcpy(v, j.parts + (p * all + i) * V, sizeof(v));
 #pragma unroll
-        for (int e = 0; e < V; ++e) s[e] += v[e];
+            for (int e = 0; e < V; ++e) s[e] += v[e];
+        }
+        const int64_t at = i / per_row, pair = at / rows;
+        const int r = static_cast<int>(at - pair * rows), token = over_group(r, a.group), head = static_cast<int>(pair % a.kv_heads) * a.group + r - token * a.group;
+        T* const out = static_cast<T*>(j.out) + (pair / a.kv_heads * a.tokens + token) * j.stride + static_cast<int64_t>(head) * a.dh + (i - at * per_row) * V;
+        if constexpr (V == 4) store4<T, true>(out, 0, 4, s[0] * j.factor, s[1] * j.factor, s[2] * j.factor, s[3] * j.factor);
+        else store_f(out, s[0] * j.factor);
     }
-    const int64_t at = i / per_row, pair = at / rows;
-    const int r = static_cast<int>(at - pair * rows), token = over_group(r, a.group), head = static_cast<int>(pair % a.kv_heads) * a.group + r - token * a.group;
-    T* const out = static_cast<T*>(j.out) + (pair / a.kv_heads * a.tokens + token) * j.stride + static_cast<int64_t>(head) * a.dh + (i - at * per_row) * V;
-    if constexpr (V == 4) store4<T, true>(out, 0, 4, s[0] * j.factor, s[1] * j.factor, s[2] * j.factor, s[3] * j.factor);
-    else store_f(out, s[0] * j.factor);
 }
 
 template <typename T, bool kVec>
 int32_t launch_sum(const SumJobs& a, int jobs, hipStream_t s) {
     constexpr int V = kVec ? 4 : 1;
     const int64_t all = a.pairs * a.tokens * a.group * (a.dh / V);
-    hipLaunchKernelGGL((cross_sum_kernel<T, V>), dim3(static_cast<uint32_t>((all + kThreads - 1) / kThreads), jobs), dim3(kThreads), 0, s, a);
+    const int64_t blocks = std::min<int64_t>((all + kThreads - 1) / kThreads, 1 << 20);
+    hipLaunchKernelGGL((cross_sum_kernel<T, V>), dim3(static_cast<uint32_t>(blocks), jobs), dim3(kThreads), 0, s, a);
     return launch_ok() ? FREE_OK : FREE_ERR_HIP;
 }
 
@@ -721,7 +723,7 @@ int32_t launch_dkv(const CrossArgs& a, const Plan& p, const RowStats& stats, con
 template <typename T, int DP, bool kVec>
 int32_t launch_shape(const CrossArgs& a, const Plan& p, const Space& w, char* ws, hipStream_t s) {
     const int64_t pairs = static_cast<int64_t>(a.B) * a.kv_heads;
-    if (pairs * p.q_tiles * p.q_parts > 0x7fffffff || pairs * p.k_tiles * p.k_parts > 0x7fffffff) return FREE_ERR_LIMIT;
+    if (pairs * p.q_tiles * p.q_parts >= 1 << 23 || pairs * p.k_tiles * (p.k_parts / p.k_units) >= 1 << 23) return FREE_ERR_LIMIT;
     const RowStats stats{reinterpret_cast<float*>(ws + w.lse), reinterpret_cast<float*>(ws + w.delta)};
     if (a.Nq > 0) {
         const GradParts pt{p.q_parts, p.q_part_tiles, reinterpret_cast<float*>(ws + w.dq), nullptr};
