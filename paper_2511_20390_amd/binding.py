@@ -972,16 +972,17 @@ def cross_attention_workspace_bytes(B: int, Nq: int, Nk: int, heads: int, kv_hea
 
 def _rows(t, name, rows, width, dtype):
     """Address and row distance of [rows, width], values of a row next to each other, rows any distance apart."""
+    if t.is_cuda and t.dtype == dtype and t.shape == (rows, width):
+        step, inner = t.stride()
+        if inner == 1 or width == 1:
+            return t.data_ptr(), step
     if not t.is_cuda:
         raise FreeError(FREE_ERR_NULL, f"{name}: not a device tensor")
     if t.dtype != dtype:
         raise FreeError(FREE_ERR_DTYPE, f"{name}: element type {t.dtype}, expected {dtype}")
     if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != width:
         raise FreeError(FREE_ERR_SHAPE, f"{name}: shape {tuple(t.shape)}, expected {(rows, width)}")
-    step, inner = t.stride()
-    if width > 1 and inner != 1:
-        raise FreeError(FREE_ERR_SHAPE, f"{name}: values of a row are not next to each other")
-    return t.data_ptr(), step
+    raise FreeError(FREE_ERR_SHAPE, f"{name}: values of a row are not next to each other")
 
 
 def _cross_sizes(q, k, B, heads, kv_heads, dh, scale):
@@ -1017,7 +1018,7 @@ def op_cross_attention(q, k, v, B: int, heads: int, dh: int, kv_heads: int = Non
     keys = _keys(key_len, key_mask, B, Nk)
     lse_at = _addr(lse, torch.float32, "lse", (B, heads, Nq), optional=True)
     if out is None:
-        out = torch.empty(B * Nq, width, dtype=dt, device=q.device)
+        out = q.new_empty(B * Nq, width)
     if workspace is None:
         workspace = torch.empty(load().free_cross_attention_workspace_bytes(B, Nq, Nk, heads, kv_heads, dh, mode, 0), dtype=torch.uint8, device=q.device)
     dev = _same_device(q, k, v, key_len, key_mask, lse, out, workspace)
@@ -1085,7 +1086,7 @@ def op_linear_adapters(x, W, bias, A, B, adapter, scale=None, rows_per_sample: i
     M, K, N, r, n, rows, mode, xw, ab = _adapter_sizes(x, W, A, B, adapter, rows_per_sample)
     u8 = torch.uint8
     if out is None:
-        out = torch.empty(M, N, dtype=x.dtype, device=x.device)
+        out = x.new_empty(M, N)
     if workspace is None:
         workspace = torch.empty(load().free_linear_adapters_workspace_bytes(M, K, N, r, n, mode, 0), dtype=u8, device=x.device)
     dev = _same_device(x, W, bias, A, B, adapter, scale, saved, out, workspace)
