@@ -32,9 +32,11 @@ using AdaptersOf = std::conditional_t<EPI == FREE_EPI_ADAPT, AdapterTerm, NoAdap
 namespace {
 
 // acc[i][j] += the term, for rows gm + 32 i and columns gn + 32 j of a wavefront whose lane has row and column lane % 32 (bf16, the
-// accumulators' order of v_mfma_f32_32x32x16_bf16 with W's rows first).  The adapters of the wavefront's rows come one after the other - one where
-// they are of one request - as k-steps of 16 ranks, the rows of others at zero.  Operands come straight from memory behind the loads of the first
-// slices; a launch of its own over the finished result would read and write it once more, and round it twice.
+// accumulators' order of v_mfma_f32_32x32x16_bf16 with W's rows first).  The adapters of the wavefront's rows come one after the other as
+// k-steps of 16 ranks.  Operands come straight from memory behind the loads of the first slices; a launch of its own over the finished result
+// would read and write it once more, and round it twice.
+// Zeros in the operands of rows with another adapter would not keep an infinite or NaN one out of them: where a wavefront's rows differ, such values
+// of B count as zero, and the rows that have the adapter get NaN in their columns.
 template <int TM, int TN, typename Acc>
 __device__ __forceinline__ void add_adapters(const AdapterTerm& ad, int gm, int gn, int lhi, int M, Acc (&acc)[TM][TN]) {
     typedef uint32_t chunk_t __attribute__((ext_vector_type(4)));
@@ -51,12 +53,15 @@ __device__ __forceinline__ void add_adapters(const AdapterTerm& ad, int gm, int 
             which = left != 0 ? __builtin_amdgcn_readlane(of[i], __builtin_ctzll(left)) : which;
         }
         if (which < 0) break;
-        bool on[TM];
+        bool on[TM], all = true;     // (rows past the end do as the others do)
 #pragma unroll
         for (int i = 0; i < TM; ++i) {
             on[i] = of[i] == which;
+            all = all && (on[i] || gm + 32 * i >= M);
             of[i] = on[i] ? -1 : of[i];
         }
+        const bool mixed = __ballot(all) != ~0ull;
+        uint32_t bad = 0;            // columns gn + 32 j with such values in this lane's ranks
         const bf16_t* const b = static_cast<const bf16_t*>(ad.b) + static_cast<int64_t>(which) * ad.cols * ad.b_row;
         for (int k0 = 0; k0 < ad.r; k0 += 16) {
             const int k = k0 + lhi * 8;
@@ -80,11 +85,33 @@ __device__ __forceinline__ void add_adapters(const AdapterTerm& ad, int gm, int 
                 tv[i] = chunk_t{0, 0, 0, 0};
                 if (on[i]) tv[i] = *reinterpret_cast<const chunk_t*>(static_cast<const bf16_t*>(ad.t) + static_cast<int64_t>(gm + 32 * i) * ad.t_row + k);
             }
+            if (mixed) {
+#pragma unroll
+                for (int j = 0; j < TN; ++j)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const bool lo = (bv[j][e] & 0x7f80u) == 0x7f80u, hi = (bv[j][e] & 0x7f800000u) == 0x7f800000u;
+                        bv[j][e] &= (lo ? 0xffff0000u : ~0u) & (hi ? 0xffffu : ~0u);
+                        bad |= static_cast<uint32_t>(lo || hi) << j;
+                    }
+            }
 #pragma unroll
             for (int i = 0; i < TM; ++i)
 #pragma unroll
                 for (int j = 0; j < TN; ++j)
                     acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(operand_t, bv[j]), __builtin_bit_cast(operand_t, tv[i]), acc[i][j], 0, 0, 0);
+        }
+        if (__builtin_expect(__ballot(bad != 0) != 0, 0)) {
+#pragma unroll
+            for (int j = 0; j < TN; ++j) {
+                const uint64_t halves = __ballot(bad >> j & 1);
+                const uint32_t columns = static_cast<uint32_t>(halves | halves >> 32) >> (4 * lhi);
+#pragma unroll
+                for (int i = 0; i < TM; ++i)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e)
+                        acc[i][j][e] = on[i] && (columns >> (8 * (e >> 2) + (e & 3)) & 1) ? __builtin_nanf("") : acc[i][j][e];
+            }
         }
     }
 }

@@ -228,6 +228,8 @@ __global__ __launch_bounds__(kThreads) void adapter_up_kernel(AdapterTerm ad, in
             const int n = n0 + l32 < N ? n0 + l32 : N - 1;
             const float* const b = static_cast<const float*>(ad.b) + (static_cast<int64_t>(which) * N + n) * ad.b_row;
             const float* const t = static_cast<const float*>(ad.t) + static_cast<int64_t>(m < M ? m : M - 1) * ad.t_row;
+            xf32x16_t sum;               // (of its own: an infinite or NaN adapter stays out of the other rows)
+            clear_tile(sum);
             for (int k0 = 0; k0 < ad.r; k0 += 8) {
                 const int k = k0 + 4 * g;
                 xu32x4_t tv = {0, 0, 0, 0}, bv = {0, 0, 0, 0};
@@ -238,8 +240,10 @@ __global__ __launch_bounds__(kThreads) void adapter_up_kernel(AdapterTerm ad, in
 #pragma unroll
                     for (int e = 0; e < 4; ++e) bv[e] = k + e < ad.r ? __float_as_uint(b[k + e]) : 0u;
                 }
-                chunk_product<float>(bv, tv, acc);
+                chunk_product<float>(bv, tv, sum);
             }
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[e] += of == which ? sum[e] : 0.f;
             of = of == which ? -1 : of;
         }
         if (m < M) {

@@ -41,7 +41,10 @@ def cross_reference(q, k, v, B, heads, kv, dh, scale, keys, dout=None):
     out = p @ V
     pv = p @ V.abs()
     e_l = (p * e_p).sum(3, keepdim=True) + chain(Nk)
-    e_out = (p * (h + (1 + h) * e_p)) @ V.abs() + pv * (e_l + h) + chain(Nk) * pv
+    # A probability (before the division by a sum of at least one) or a score's gradient below the smallest normal number of fp32 and bf16 may count as
+    # zero, as it does where an instruction flushes subnormal results or operands: it is off by itself, less than 2^-126.
+    least = torch.where(there, torch.full_like(p, 2.0 ** -126), torch.zeros_like(p))
+    e_out = (p * (h + (1 + h) * e_p) + least) @ V.abs() + pv * (e_l + h) + chain(Nk) * pv
     e_lse = torch.where(some, 1.1 * e_l + 8 * U * (lse.abs() + size + 1), torch.zeros_like(lse))
     res = [(rows(out), rows(e_out)), (torch.where(some, lse, torch.full_like(lse, -math.inf))[..., 0], e_lse[..., 0])]
     if dout is None:
@@ -54,13 +57,13 @@ def cross_reference(q, k, v, B, heads, kv, dh, scale, keys, dout=None):
     e_delta = (G.abs() * (e_out * (1 + half_step(kind)) + (half_step(kind) + (dh + 8) * U) * out.abs())).sum(3, keepdim=True)
     ds = p * (dp - delta)
     e_ds = (p * e_p) * (dp - delta).abs() + p * (1 + e_p) * (e_dp + e_delta + 2 * U * (dp.abs() + delta.abs()))
-    e_ds = (1 + h) * e_ds + h * ds.abs()
+    e_ds = (1 + h) * e_ds + h * ds.abs() + least * (1 + (dp - delta).abs())
     dq, e_dq = scale * (ds @ K), scale * ((e_ds + chain(Nk) * (ds.abs() + e_ds)) @ K.abs())
     n = chain(Nq * group)
     by_key = lambda t: t.reshape(B, kv, group, Nk, dh).sum(2)
     T = lambda t: t.transpose(2, 3)
     dk, e_dk = scale * (T(ds) @ Q), scale * (T(e_ds + n * (ds.abs() + e_ds)) @ Q.abs())
-    e_pr = p * (h + (1 + h) * e_p)
+    e_pr = p * (h + (1 + h) * e_p) + least
     dv, e_dv = T(p) @ G, T(e_pr + n * (p + e_pr)) @ G.abs()
     return res + [(rows(dq), rows(e_dq)), (rows(by_key(dk)), rows(by_key(e_dk))), (rows(by_key(dv)), rows(by_key(e_dv)))]
 
