@@ -18,6 +18,7 @@ namespace freemi {
 namespace {
 
 constexpr int kThreads = kStreamThreads;
+constexpr int kTwiceKeys = 256;                   // bf16: up to as many keys are passed over twice for delta, where they do not stay in LDS
 
 // parts of the streamed axis: tiles of each; fp32 results [part][pair][row][dh]
 struct GradParts {
@@ -30,10 +31,35 @@ struct RowStats {
     float *lse, *delta;
 };
 
-// dq += over one 32-key block; bits: which of its keys count, from this half-wave's first on
+// delta += sum P dP over one 32-key block; bits: which of its keys count, from this half-wave's first on
 template <typename T, int DP>
+__device__ __forceinline__ void delta_block(const char* tile_k, const char* tile_v, int row0, int lane, uint32_t bits, const xu32x4_t (&qf)[HeadShape<T, DP>::KSTEPS],
+                                            const xu32x4_t (&gf)[HeadShape<T, DP>::KSTEPS], float lse2, float scale_log2, float& delta) {
+    xu32x4_t fk[kRowGroup<T, DP>], fv[kRowGroup<T, DP>];
+    xf32x16_t st, dp;
+    clear_tile(st);
+    clear_tile(dp);
+    read_rows<T, DP>(tile_k, row0, lane, 0, fk);
+    read_rows<T, DP>(tile_v, row0, lane, 0, fv);
+    fence();
+    row_products<T, DP>(tile_k, row0, lane, fk, qf, st);
+    row_products<T, DP>(tile_v, row0, lane, fv, gf, dp);
+    float sum = 0.f;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) st[e] = __builtin_amdgcn_exp2f(fmaf(st[e], scale_log2, -lse2)) * dp[e];
+    if (__builtin_amdgcn_readfirstlane(bits) != ~0u) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) st[e] = bits >> register_row<T>(e, 0) & 1 ? st[e] : 0.f;
+    }
+#pragma unroll
+    for (int e = 0; e < 16; ++e) sum += st[e];
+    delta += sum;
+}
+
+// dq += over one 32-key block; rest += the sum of its dS, which is zero over all keys but for what delta is off by
+template <typename T, int DP, bool kRest>
 __device__ __forceinline__ void dq_block(const char* tile_k, const char* tile_v, int row0, int lane, uint32_t bits, const xu32x4_t (&qf)[HeadShape<T, DP>::KSTEPS],
-                                         const xu32x4_t (&gf)[HeadShape<T, DP>::KSTEPS], float dl, float lse2, float scale_log2,
+                                         const xu32x4_t (&gf)[HeadShape<T, DP>::KSTEPS], float dl, float lse2, float scale_log2, float& rest,
                                          xf32x16_t (&dq)[HeadShape<T, DP>::DT]) {
     xu32x4_t fk[kRowGroup<T, DP>], fv[kRowGroup<T, DP>];
     Columns<T, DP> ck;
@@ -57,6 +83,12 @@ __device__ __forceinline__ void dq_block(const char* tile_k, const char* tile_v,
     if (__builtin_amdgcn_readfirstlane(bits) != ~0u) {
 #pragma unroll
         for (int e = 0; e < 16; ++e) st[e] = bits >> register_row<T>(e, 0) & 1 ? st[e] : 0.f;
+    }
+    if constexpr (kRest) {
+        float sum = 0.f;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) sum += st[e];
+        rest += sum;
     }
     column_products<T, DP>(tile_k, row0, lane, ck, st, dq);
 }
@@ -97,14 +129,14 @@ __device__ __forceinline__ void dkv_block(const char* tile_q, const char* tile_g
     column_products<T, DP>(tile_q, row0, lane, cq, dp, dk);
 }
 
-// A row's chunks of q, dout and out, and sum dout out of them
+// A row's chunks of q and dout; delta of its chunks of out, too
 template <typename T, int DP, bool kVec>
 struct RowOperands {
     static constexpr int KSTEPS = HeadShape<T, DP>::KSTEPS;
     xu32x4_t q[KSTEPS], g[KSTEPS];
     int64_t q_at, h_at, stat;        // its row, its head's first value in it, and its place among [B, heads, Nq]
     float lse;
-    __device__ __forceinline__ void load(const CrossArgs& a, int b, int kvh, int row, int half, xu32x4_t (&o)[KSTEPS]) {
+    __device__ __forceinline__ void load(const CrossArgs& a, int b, int kvh, int row, int half) {
         const int group = a.heads / a.kv_heads, r = min(row, a.Nq * group - 1), token = over_group(r, group), head = kvh * group + r - token * group;
         q_at = static_cast<int64_t>(b) * a.Nq + token;
         h_at = static_cast<int64_t>(head) * a.dh;
@@ -113,11 +145,13 @@ struct RowOperands {
 #pragma unroll
         for (int ks = 0; ks < KSTEPS; ++ks) {
             g[ks] = row_chunk<T, kVec>(static_cast<const T*>(a.dout) + q_at * a.dout_stride + h_at, 2 * ks + half, a.dh);
-            o[ks] = row_chunk<T, kVec>(static_cast<const T*>(a.out) + q_at * a.out_stride + h_at, 2 * ks + half, a.dh);
             q[ks] = row_chunk<T, kVec>(static_cast<const T*>(a.q) + q_at * a.q_stride + h_at, 2 * ks + half, a.dh);
         }
     }
-    __device__ __forceinline__ float delta(const xu32x4_t (&o)[KSTEPS]) const {
+    __device__ __forceinline__ float delta(const CrossArgs& a, int half) const {
+        xu32x4_t o[KSTEPS];
+#pragma unroll
+        for (int ks = 0; ks < KSTEPS; ++ks) o[ks] = row_chunk<T, kVec>(static_cast<const T*>(a.out) + q_at * a.out_stride + h_at, 2 * ks + half, a.dh);
         float dl = 0.f;
 #pragma unroll
         for (int ks = 0; ks < KSTEPS; ++ks)
@@ -158,42 +192,52 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 || DP <= 64) ? 2 : 1) voi
     KeyStream<T, DP, kVec> keys(a, b, kvh);
     const int t0 = part * pt.tiles, t1 = min(t0 + pt.tiles, keys.tiles());
     const uint32_t lds_base = lds_address(lds);
+    const int n = max(t1 - t0, 0);
+    const bool twice = sizeof(T) == 2 && a.Nk <= kTwiceKeys;
+    const int passes = twice ? 2 * n : n;
+    const auto tile_of = [&](int u) { return t0 + (u >= n ? u - n : u); };
     keys.request_mask(t0, lane);
     uint64_t valid = keys.valid_of(t0);
-    if (t0 < t1) keys.request(t0, lds_base, lds_base + TL::kBytes, wave, lane, valid);
-    keys.request_mask(t0 + 1, lane);
+    if (n > 0) keys.request(t0, lds_base, lds_base + TL::kBytes, wave, lane, valid);
+    keys.request_mask(tile_of(1), lane);
 
     RowOperands<T, DP, kVec> own;
-    xu32x4_t of[KSTEPS];
-    own.load(a, b, kvh, row, g, of);
-    const float dl = own.delta(of), lse2 = own.lse * kLog2e, scale_log2 = a.scale * kLog2e;
-    if (part == 0 && g == 0 && row < rows) own.leave(stats, dl, a.scale);
+    own.load(a, b, kvh, row, g);
+    const float lse2 = own.lse * kLog2e, scale_log2 = a.scale * kLog2e;
+    float dl = 0.f, rest = 0.f;
+    if (!twice) dl = own.delta(a, g);
 
     xf32x16_t dq[DT];
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) clear_tile(dq[dt]);
-    if (t0 < t1) keys.deliver(lds, lds + TL::kBytes, tid, valid);
+    if (n > 0) keys.deliver(lds, lds + TL::kBytes, tid, valid);
     arrived(own.q);
     arrived(own.g);
     keys.k.settle();
-    for (int t = t0; t < t1; ++t) {
-        const int stage = (t - t0) & 1, other = (stage ^ 1) * 2 * TL::kBytes;
+    for (int u = 0; u < passes; ++u) {
+        const int stage = u & 1, other = (stage ^ 1) * 2 * TL::kBytes;
         const char* const sK = lds + stage * 2 * TL::kBytes;
-        const uint64_t valid_next = keys.valid_of(t + 1);
-        if (t + 1 < t1) {
-            keys.request(t + 1, lds_base + other, lds_base + other + TL::kBytes, wave, lane, valid_next);
-            keys.request_mask(t + 2, lane);
+        const uint64_t valid_next = keys.valid_of(tile_of(u + 1));
+        if (u + 1 < passes) {
+            keys.request(tile_of(u + 1), lds_base + other, lds_base + other + TL::kBytes, wave, lane, valid_next);
+            keys.request_mask(tile_of(u + 2), lane);
         }
+        if (twice && u == n) dl = add_lane_xor<32>(dl);
 #pragma unroll
         for (int kb = 0; kb < BKV / 32; ++kb) {
             // (fp32 has 32 keys to a tile, and a full mask of them)
             const uint32_t bits = static_cast<uint32_t>(valid >> (32 * kb));
-            dq_block<T, DP>(sK, sK + TL::kBytes, kb * 32, lane, bits == ~0u ? bits : bits >> (sizeof(T) == 2 ? 8 * g : 4 * g), own.q, own.g, dl, lse2, scale_log2, dq);
+            const uint32_t mine = bits == ~0u ? bits : bits >> (sizeof(T) == 2 ? 8 * g : 4 * g);
+            if (twice && u < n) delta_block<T, DP>(sK, sK + TL::kBytes, kb * 32, lane, mine, own.q, own.g, lse2, scale_log2, dl);
+            else dq_block<T, DP, true>(sK, sK + TL::kBytes, kb * 32, lane, mine, own.q, own.g, dl, lse2, scale_log2, rest, dq);
         }
-        if (t + 1 < t1) keys.deliver(lds + other, lds + other + TL::kBytes, tid, valid_next);
+        if (u + 1 < passes) keys.deliver(lds + other, lds + other + TL::kBytes, tid, valid_next);
         valid = valid_next;
         keys.k.settle();
     }
+    // (a part has not all keys; with both passes the rest is what rounding leaves)
+    rest = pt.parts > 1 ? 0.f : add_lane_xor<32>(rest);
+    if (part == 0 && g == 0 && row < rows) own.leave(stats, dl + rest, a.scale);
     if (pt.parts > 1) store_column<float, kVec, DT>(pt.sum0 + ((part * static_cast<int64_t>(pairs) + pair) * rows + row) * a.dh, a.dh, g, dq, 1.0f, row < rows);
     else store_column<T, kVec, DT>(static_cast<T*>(a.dq) + own.q_at * a.dq_stride + own.h_at, a.dh, g, dq, a.scale, row < rows);
 }
@@ -339,9 +383,8 @@ __global__ __launch_bounds__(kRingWaves * 64, 2) void cross_dq_ring_kernel(Cross
     const float scale_log2 = a.scale * kLog2e;
     RowOperands<T, DP, true> own;
     xf32x16_t dq[DT];
-    float dl = 0.f;
-    const auto begin = [&](int block) {
-        if (g == 0 && block * 32 + l32 < rows) own.leave(stats, dl, a.scale);
+    float dl = 0.f, rest = 0.f;
+    const auto begin = [&] {
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt) clear_tile(dq[dt]);
         arrived(own.q);
@@ -351,10 +394,12 @@ __global__ __launch_bounds__(kRingWaves * 64, 2) void cross_dq_ring_kernel(Cross
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb) {
             const uint32_t bits = static_cast<uint32_t>(valid >> (32 * kb));
-            dq_block<T, DP>(tile, tile + Ring::kSecond, kb * 32, lane, bits == ~0u ? bits : bits >> (8 * g), own.q, own.g, dl, own.lse * kLog2e, scale_log2, dq);
+            dq_block<T, DP, !kResident>(tile, tile + Ring::kSecond, kb * 32, lane, bits == ~0u ? bits : bits >> (8 * g), own.q, own.g, dl, own.lse * kLog2e, scale_log2, rest, dq);
         }
     };
     const auto finish = [&](int block) {
+        if (!kResident) dl += add_lane_xor<32>(rest);
+        if (g == 0 && block * 32 + l32 < rows) own.leave(stats, dl, a.scale);
         store_column<T, true, DT>(static_cast<T*>(a.dq) + own.q_at * a.dq_stride + own.h_at, a.dh, g, dq, a.scale, block * 32 + l32 < rows);
     };
     if constexpr (kResident) {
@@ -362,32 +407,38 @@ __global__ __launch_bounds__(kRingWaves * 64, 2) void cross_dq_ring_kernel(Cross
         constexpr bool kNext = DP <= 80;
         for (int t = 0; t < tiles; ++t) request(t, t);
         const int first = chunk * blocks_per_chunk, last = min(first + blocks_per_chunk, blocks);
-        xu32x4_t of[KSTEPS];
-        if (first + wave < last) own.load(a, b, kvh, (first + wave) * 32 + l32, g, of);
+        if (first + wave < last) own.load(a, b, kvh, (first + wave) * 32 + l32, g);
         bring_keys(keys, lds, masks, 0, wave, lane);
         for (int block = first + wave; block < last; block += kRingWaves) {
-            dl = own.delta(of);
-            begin(block);
+            begin();
             RowOperands<T, DP, true> next = own;
             const bool more = block + kRingWaves < last;
-            if (kNext && more) next.load(a, b, kvh, (block + kRingWaves) * 32 + l32, g, of);
-            for (int t = 0; t < tiles; ++t)
-                multiply(lds + t * Ring::kTileBytes, keys.mask ? masks[t] : keys_below(keys.len - t * Tile<T, DP>::kRows));
+            if (kNext && more) next.load(a, b, kvh, (block + kRingWaves) * 32 + l32, g);
+            const auto bits_of = [&](int t) { return keys.mask ? masks[t] : keys_below(keys.len - t * Tile<T, DP>::kRows); };
+            dl = 0.f;
+            for (int t = 0; t < tiles; ++t) {
+                const uint64_t valid = bits_of(t);
+                const char* const tile = lds + t * Ring::kTileBytes;
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb) {
+                    const uint32_t bits = static_cast<uint32_t>(valid >> (32 * kb));
+                    delta_block<T, DP>(tile, tile + Ring::kSecond, kb * 32, lane, bits == ~0u ? bits : bits >> (8 * g), own.q, own.g, own.lse * kLog2e, scale_log2, dl);
+                }
+            }
+            dl = add_lane_xor<32>(dl);
+            for (int t = 0; t < tiles; ++t) multiply(lds + t * Ring::kTileBytes, bits_of(t));
             finish(block);
             own = next;
-            if (!kNext && more) own.load(a, b, kvh, (block + kRingWaves) * 32 + l32, g, of);
+            if (!kNext && more) own.load(a, b, kvh, (block + kRingWaves) * 32 + l32, g);
         }
     } else {
         const int block = chunk * kRingWaves + wave;
 #pragma unroll
         for (int s = 0; s < kRing - 1; ++s)
             if (s < tiles) request(s, s);
-        {
-            xu32x4_t of[KSTEPS];
-            own.load(a, b, kvh, block * 32 + l32, g, of);
-            dl = own.delta(of);
-        }
-        begin(block);
+        own.load(a, b, kvh, block * 32 + l32, g);
+        dl = own.delta(a, g);
+        begin();
         int slot = 0, free_slot = kRing - 1;
         for (int t = 0; t < tiles; ++t) {
             const uint64_t valid = keys.valid(t, lane);
