@@ -420,10 +420,10 @@ __device__ __forceinline__ int attended(const CrossArgs& a, int b) {
 }
 
 // Keys and values of a (sample, key head) for the kernels with a PairRing
-template <int DP>
+template <int DP, int NW = kRingWaves>
 struct RingKeys {
     using TL = Tile<bf16_t, DP>;
-    using Ring = PairRing<DP, kRingWaves>;
+    using Ring = PairRing<DP, NW>;
     const bf16_t *kp, *vp;
     const uint8_t* mask;
     int64_t k_stride, v_stride;
@@ -448,7 +448,7 @@ struct RingKeys {
     // rows of keys that do not count are replaced, in LDS, where they are multiplied by zeros and may be NaN: the keys' (second 0) or the values'
     static __device__ __forceinline__ void drop(char* tile, int second, uint64_t valid, int wave, int lane) {
         if (valid == ~0ull) return;
-        for (int r = wave; r < TL::kRows; r += kRingWaves)
+        for (int r = wave; r < TL::kRows; r += NW)
             if (!(valid >> r & 1) && lane < TL::CHP) *reinterpret_cast<xu32x4_t*>(tile + second * Ring::kSecond + r * TL::kPitch + lane * 16) = xu32x4_t{0, 0, 0, 0};
     }
 };

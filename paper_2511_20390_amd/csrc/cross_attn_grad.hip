@@ -31,29 +31,57 @@ struct RowStats {
     float *lse, *delta;
 };
 
-// delta += sum P dP over one 32-key block; bits: which of its keys count, from this half-wave's first on
+// A block of 32 keys by a wavefront's rows: the scores in st, dout v^T on top of what is in dp.  Operands are read a group of chunks ahead of the
+// products, through both tensors.
 template <typename T, int DP>
-__device__ __forceinline__ void delta_block(const char* tile_k, const char* tile_v, int row0, int lane, uint32_t bits, const xu32x4_t (&qf)[HeadShape<T, DP>::KSTEPS],
-                                            const xu32x4_t (&gf)[HeadShape<T, DP>::KSTEPS], float lse2, float scale_log2, float& delta) {
-    xu32x4_t fk[kRowGroup<T, DP>], fv[kRowGroup<T, DP>];
-    xf32x16_t st, dp;
+__device__ __forceinline__ void score_products(const char* tile_k, const char* tile_v, int row0, int lane, const xu32x4_t (&qf)[HeadShape<T, DP>::KSTEPS],
+                                               const xu32x4_t (&gf)[HeadShape<T, DP>::KSTEPS], xf32x16_t& st, xf32x16_t& dp) {
+    constexpr int KSTEPS = HeadShape<T, DP>::KSTEPS, G = kRowGroup<T, DP>, kGroups = (KSTEPS + G - 1) / G;
+    constexpr bool kOrder = DP <= 96;
+    xu32x4_t f[2][G];
     clear_tile(st);
-    clear_tile(dp);
-    read_rows<T, DP>(tile_k, row0, lane, 0, fk);
-    read_rows<T, DP>(tile_v, row0, lane, 0, fv);
-    fence();
-    row_products<T, DP>(tile_k, row0, lane, fk, qf, st);
-    row_products<T, DP>(tile_v, row0, lane, fv, gf, dp);
-    float sum = 0.f;
+    read_rows<T, DP>(tile_k, row0, lane, 0, f[0]);
+#pragma unroll
+    for (int i = 0; i < 2 * kGroups; ++i) {
+        const int first = i % kGroups * G;
+        if (i + 1 < 2 * kGroups) read_rows<T, DP>(i + 1 < kGroups ? tile_k : tile_v, row0, lane, (i + 1) % kGroups * G, f[(i + 1) & 1]);
+        if constexpr (kOrder) fence();
+#pragma unroll
+        for (int k = 0; k < G; ++k)
+            if (first + k < KSTEPS) {
+                if (i < kGroups) chunk_product<T>(f[i & 1][k], qf[first + k], st);
+                else chunk_product<T>(f[i & 1][k], gf[first + k], dp);
+            }
+    }
+}
+
+// P times what stands in dp, for the keys that count
+template <typename T>
+__device__ __forceinline__ void weigh(xf32x16_t& st, const xf32x16_t& dp, uint32_t bits, float lse2, float scale_log2) {
 #pragma unroll
     for (int e = 0; e < 16; ++e) st[e] = __builtin_amdgcn_exp2f(fmaf(st[e], scale_log2, -lse2)) * dp[e];
     if (__builtin_amdgcn_readfirstlane(bits) != ~0u) {
 #pragma unroll
         for (int e = 0; e < 16; ++e) st[e] = bits >> register_row<T>(e, 0) & 1 ? st[e] : 0.f;
     }
+}
+
+__device__ __forceinline__ float sum_of(const xf32x16_t& v) {
+    float s = 0.f;
 #pragma unroll
-    for (int e = 0; e < 16; ++e) sum += st[e];
-    delta += sum;
+    for (int e = 0; e < 16; ++e) s += v[e];
+    return s;
+}
+
+// delta += sum P dP over one 32-key block; bits: which of its keys count, from this half-wave's first on
+template <typename T, int DP>
+__device__ __forceinline__ void delta_block(const char* tile_k, const char* tile_v, int row0, int lane, uint32_t bits, const xu32x4_t (&qf)[HeadShape<T, DP>::KSTEPS],
+                                            const xu32x4_t (&gf)[HeadShape<T, DP>::KSTEPS], float lse2, float scale_log2, float& delta) {
+    xf32x16_t st, dp;
+    clear_tile(dp);
+    score_products<T, DP>(tile_k, tile_v, row0, lane, qf, gf, st, dp);
+    weigh<T>(st, dp, bits, lse2, scale_log2);
+    delta += sum_of(st);
 }
 
 // dq += over one 32-key block; rest += the sum of its dS, which is zero over all keys but for what delta is off by
@@ -61,36 +89,15 @@ template <typename T, int DP, bool kRest>
 __device__ __forceinline__ void dq_block(const char* tile_k, const char* tile_v, int row0, int lane, uint32_t bits, const xu32x4_t (&qf)[HeadShape<T, DP>::KSTEPS],
                                          const xu32x4_t (&gf)[HeadShape<T, DP>::KSTEPS], float dl, float lse2, float scale_log2, float& rest,
                                          xf32x16_t (&dq)[HeadShape<T, DP>::DT]) {
-    xu32x4_t fk[kRowGroup<T, DP>], fv[kRowGroup<T, DP>];
     Columns<T, DP> ck;
     xf32x16_t st, dp;
-    clear_tile(st);
 #pragma unroll
     for (int e = 0; e < 16; ++e) dp[e] = -dl;
-    // (wide heads have no registers for operands further ahead)
-    constexpr bool kFar = DP <= 64;
-    read_rows<T, DP>(tile_k, row0, lane, 0, fk);
-    if constexpr (kFar) read_rows<T, DP>(tile_v, row0, lane, 0, fv);
-    fence();
-    row_products<T, DP>(tile_k, row0, lane, fk, qf, st);
-    if constexpr (kFar) ck.read(tile_k, row0, lane, 0);
-    else read_rows<T, DP>(tile_v, row0, lane, 0, fv);
-    fence();
-    row_products<T, DP>(tile_v, row0, lane, fv, gf, dp);
-    if constexpr (!kFar) ck.read(tile_k, row0, lane, 0);
-#pragma unroll
-    for (int e = 0; e < 16; ++e) st[e] = __builtin_amdgcn_exp2f(fmaf(st[e], scale_log2, -lse2)) * dp[e];
-    if (__builtin_amdgcn_readfirstlane(bits) != ~0u) {
-#pragma unroll
-        for (int e = 0; e < 16; ++e) st[e] = bits >> register_row<T>(e, 0) & 1 ? st[e] : 0.f;
-    }
-    if constexpr (kRest) {
-        float sum = 0.f;
-#pragma unroll
-        for (int e = 0; e < 16; ++e) sum += st[e];
-        rest += sum;
-    }
-    column_products<T, DP>(tile_k, row0, lane, ck, st, dq);
+    score_products<T, DP>(tile_k, tile_v, row0, lane, qf, gf, st, dp);
+    ck.read(tile_k, row0, lane, 0);
+    weigh<T>(st, dp, bits, lse2, scale_log2);
+    if constexpr (kRest) rest += sum_of(st);
+    column_products<T, DP, (DP <= 96)>(tile_k, row0, lane, ck, st, dq);
 }
 
 // dk, dv += over one block of 32 rows, whose -lse / scale and -delta are at `lse` and `delta`: the sums of scores begin with them
@@ -193,7 +200,7 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 || DP <= 64) ? 2 : 1) voi
     const int t0 = part * pt.tiles, t1 = min(t0 + pt.tiles, keys.tiles());
     const uint32_t lds_base = lds_address(lds);
     const int n = max(t1 - t0, 0);
-    const bool twice = sizeof(T) == 2 && a.Nk <= kTwiceKeys;
+    const bool twice = sizeof(T) == 2 && keys.len <= kTwiceKeys;         // (which are all in the first part then)
     const int passes = twice ? 2 * n : n;
     const auto tile_of = [&](int u) { return t0 + (u >= n ? u - n : u); };
     keys.request_mask(t0, lane);
@@ -397,6 +404,13 @@ __global__ __launch_bounds__(kRingWaves * 64, 2) void cross_dq_ring_kernel(Cross
             dq_block<T, DP, !kResident>(tile, tile + Ring::kSecond, kb * 32, lane, bits == ~0u ? bits : bits >> (8 * g), own.q, own.g, dl, own.lse * kLog2e, scale_log2, rest, dq);
         }
     };
+    const auto measure = [&](const char* tile, uint64_t valid) {
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+            const uint32_t bits = static_cast<uint32_t>(valid >> (32 * kb));
+            delta_block<T, DP>(tile, tile + Ring::kSecond, kb * 32, lane, bits == ~0u ? bits : bits >> (8 * g), own.q, own.g, own.lse * kLog2e, scale_log2, dl);
+        }
+    };
     const auto finish = [&](int block) {
         if (!kResident) dl += add_lane_xor<32>(rest);
         if (g == 0 && block * 32 + l32 < rows) own.leave(stats, dl, a.scale);
@@ -416,15 +430,7 @@ __global__ __launch_bounds__(kRingWaves * 64, 2) void cross_dq_ring_kernel(Cross
             if (kNext && more) next.load(a, b, kvh, (block + kRingWaves) * 32 + l32, g);
             const auto bits_of = [&](int t) { return keys.mask ? masks[t] : keys_below(keys.len - t * Tile<T, DP>::kRows); };
             dl = 0.f;
-            for (int t = 0; t < tiles; ++t) {
-                const uint64_t valid = bits_of(t);
-                const char* const tile = lds + t * Ring::kTileBytes;
-#pragma unroll
-                for (int kb = 0; kb < 2; ++kb) {
-                    const uint32_t bits = static_cast<uint32_t>(valid >> (32 * kb));
-                    delta_block<T, DP>(tile, tile + Ring::kSecond, kb * 32, lane, bits == ~0u ? bits : bits >> (8 * g), own.q, own.g, own.lse * kLog2e, scale_log2, dl);
-                }
-            }
+            for (int t = 0; t < tiles; ++t) measure(lds + t * Ring::kTileBytes, bits_of(t));
             dl = add_lane_xor<32>(dl);
             for (int t = 0; t < tiles; ++t) multiply(lds + t * Ring::kTileBytes, bits_of(t));
             finish(block);
@@ -433,27 +439,41 @@ __global__ __launch_bounds__(kRingWaves * 64, 2) void cross_dq_ring_kernel(Cross
         }
     } else {
         const int block = chunk * kRingWaves + wave;
+        const auto begin_tiles = [&] {
 #pragma unroll
-        for (int s = 0; s < kRing - 1; ++s)
-            if (s < tiles) request(s, s);
-        own.load(a, b, kvh, block * 32 + l32, g);
-        dl = own.delta(a, g);
-        begin();
-        int slot = 0, free_slot = kRing - 1;
-        for (int t = 0; t < tiles; ++t) {
-            const uint64_t valid = keys.valid(t, lane);
-            if (t + kRing - 1 <= tiles) wait_vm_barrier<(kRing - 2) * Ring::N>();
-            else wait_vm_barrier<0>();
-            char* const tile = lds + slot * Ring::kTileBytes;
-            if (keys.mask && valid != ~0ull) {
-                keys.drop(tile, 0, valid, wave, lane);
-                __syncthreads();
+            for (int s = 0; s < kRing - 1; ++s)
+                if (s < tiles) request(s, s);
+        };
+        const auto each_tile = [&](auto&& use) {
+            int slot = 0, free_slot = kRing - 1;
+            for (int t = 0; t < tiles; ++t) {
+                const uint64_t valid = keys.valid(t, lane);
+                if (t + kRing - 1 <= tiles) wait_vm_barrier<(kRing - 2) * Ring::N>();
+                else wait_vm_barrier<0>();
+                char* const tile = lds + slot * Ring::kTileBytes;
+                if (keys.mask && valid != ~0ull) {
+                    keys.drop(tile, 0, valid, wave, lane);
+                    __syncthreads();
+                }
+                if (t + kRing - 1 < tiles) request(t + kRing - 1, free_slot);
+                use(tile, valid);
+                free_slot = slot;
+                slot = slot + 1 == kRing ? 0 : slot + 1;
             }
-            if (t + kRing - 1 < tiles) request(t + kRing - 1, free_slot);
-            multiply(tile, valid);
-            free_slot = slot;
-            slot = slot + 1 == kRing ? 0 : slot + 1;
+        };
+        begin_tiles();
+        own.load(a, b, kvh, block * 32 + l32, g);
+        if (keys.len <= kTwiceKeys) {
+            begin();
+            each_tile(measure);
+            dl = add_lane_xor<32>(dl);
+            __syncthreads();
+            begin_tiles();
+        } else {
+            dl = own.delta(a, g);
+            begin();
         }
+        each_tile(multiply);
         finish(block);
     }
 }
