@@ -401,6 +401,11 @@ struct PairRing {
 // another take.
 constexpr int kRing = 3, kRingWaves = 8, kMaxTiles = 16;
 constexpr int kLdsBytes = 160 * 1024 - 256;
+// Two workgroups of kPassWaves share a compute unit where tiles pass through: one is busy while the other brings or stores its rows.  Tiles of each in LDS
+// (with two, one is under way while one is multiplied).
+constexpr int kPassWaves = 4;
+template <int DP>
+constexpr int kPassTiles = kLdsBytes / 2 / PairRing<DP, kPassWaves>::kTileBytes >= 3 ? 3 : 2;
 
 // 64 floats, one per lane, to LDS (dma_1k's comment)
 __device__ __forceinline__ void dma_floats(uint32_t lds_addr, int voff, u32x4_t rsrc) {

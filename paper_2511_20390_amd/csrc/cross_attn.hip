@@ -239,15 +239,15 @@ __global__ __launch_bounds__(kThreads, (kThreeWaves<T, DP, KS, kVec> ? 3 : 2)) v
     write_row<T, kVec, DT>(a, pt, part, pair, b, kvh, row, g, m_ref * scale_log2, l, any, o, row < rows);
 }
 
-// bf16 of whole chunks, eight wavefronts of 32 queries at a time.
+// bf16 of whole chunks, wavefronts of 32 queries at a time.
 // kResident: all keys and values of a (sample, key head) fit in LDS.  They are brought there once, and each wavefront takes one block of queries after
 // the other, without a barrier, the next block's queries requested ahead.  Otherwise tiles pass through a ring.
 template <int DP, bool kResident>
-__global__ __launch_bounds__(kRingWaves * 64, 2) void cross_ring_kernel(CrossArgs a, Parts pt, int32_t chunks, int32_t blocks_per_chunk) {
+__global__ __launch_bounds__((kResident ? kRingWaves : kPassWaves) * 64, 2) void cross_ring_kernel(CrossArgs a, Parts pt, int32_t chunks, int32_t blocks_per_chunk) {
     using T = bf16_t;
     using H = HeadShape<T, DP>;
-    using Ring = PairRing<DP, kRingWaves>;
-    constexpr int KSTEPS = H::KSTEPS, DT = H::DT;
+    constexpr int KSTEPS = H::KSTEPS, DT = H::DT, NW = kResident ? kRingWaves : kPassWaves, kSlots = kPassTiles<DP>;
+    using Ring = PairRing<DP, NW>;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     __shared__ uint64_t masks[kMaxTiles];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, g = lane >> 5;
@@ -255,7 +255,7 @@ __global__ __launch_bounds__(kRingWaves * 64, 2) void cross_ring_kernel(CrossArg
     const WorkPlace at(blockIdx.x % (pairs * chunks), pairs);
     const int pair = at.pair, chunk = at.place, kvh = pair % a.kv_heads, b = pair / a.kv_heads;
     const int rows = a.Nq * group, blocks = (rows + 31) / 32;
-    RingKeys<DP> keys(a, b, kvh, wave, lane);
+    RingKeys<DP, NW> keys(a, b, kvh, wave, lane);
     const int tiles = keys.tiles(), t0 = part * pt.tiles, t1 = min(t0 + pt.tiles, tiles);
     const uint32_t lds_base = lds_address(lds);
     const auto request = [&](int t, int slot) { keys.request(t, lds_base + slot * Ring::kTileBytes, wave); };
@@ -315,10 +315,10 @@ __global__ __launch_bounds__(kRingWaves * 64, 2) void cross_ring_kernel(CrossArg
         const int first = chunk * blocks_per_chunk, last = min(first + blocks_per_chunk, blocks);
         if (first + wave < last) load_queries(first + wave, qf);
         const bool any = bring_keys(keys, lds, masks, 1, wave, lane);
-        for (int block = first + wave; block < last; block += kRingWaves) {
+        for (int block = first + wave; block < last; block += NW) {
             xu32x4_t next[KSTEPS];
             arrived(qf);
-            if (block + kRingWaves < last) load_queries(block + kRingWaves, next);
+            if (block + NW < last) load_queries(block + NW, next);
             begin();
             for (int t = 0; t < tiles; ++t) {
                 const uint64_t valid = keys.mask ? masks[t] : keys_below(keys.len - t * Tile<T, DP>::kRows);
@@ -329,31 +329,31 @@ __global__ __launch_bounds__(kRingWaves * 64, 2) void cross_ring_kernel(CrossArg
             for (int ks = 0; ks < KSTEPS; ++ks) qf[ks] = next[ks];
         }
     } else {
-        const int block = min(chunk * kRingWaves + wave, blocks - 1);
-        const bool mine = chunk * kRingWaves + wave < blocks;
+        const int block = min(chunk * NW + wave, blocks - 1);
+        const bool mine = chunk * NW + wave < blocks;
 #pragma unroll
-        for (int s = 0; s < kRing - 1; ++s)
+        for (int s = 0; s < kSlots - 1; ++s)
             if (t0 + s < t1) request(t0 + s, s);
         load_queries(block, qf);
         begin();
         bool any = false;
         arrived(qf);
-        int slot = 0, free_slot = kRing - 1;
+        int slot = 0, free_slot = kSlots - 1;
         for (int t = t0; t < t1; ++t) {
             const uint64_t valid = keys.valid(t, lane);
             any |= valid != 0;
             // tile t has arrived, and everybody is done with the one before it
-            if (t + kRing - 1 <= t1) wait_vm_barrier<(kRing - 2) * Ring::N>();
+            if (t + kSlots - 1 <= t1) wait_vm_barrier<(kSlots - 2) * Ring::N>();
             else wait_vm_barrier<0>();
             char* const tile = lds + slot * Ring::kTileBytes;
             if (keys.mask && valid != ~0ull) {
                 keys.drop(tile, 1, valid, wave, lane);
                 __syncthreads();
             }
-            if (t + kRing - 1 < t1) request(t + kRing - 1, free_slot);
+            if (t + kSlots - 1 < t1) request(t + kSlots - 1, free_slot);
             multiply(tile, valid);
             free_slot = slot;
-            slot = slot + 1 == kRing ? 0 : slot + 1;
+            slot = slot + 1 == kSlots ? 0 : slot + 1;
         }
         finish(mine ? block : rows, any);
     }
@@ -552,8 +552,9 @@ Plan plan_of(int32_t B, int32_t Nq, int32_t Nk, int32_t heads, int32_t kv_heads,
         p.resident = tiles <= tiles_that_fit(dh);
         p.parts = 1;
         p.tiles = static_cast<int32_t>(tiles);
-        p.q_tiles = (blocks + kRingWaves - 1) / kRingWaves;
+        p.q_tiles = (blocks + kPassWaves - 1) / kPassWaves;
         if (p.resident) {
+            p.q_tiles = (blocks + kRingWaves - 1) / kRingWaves;
             // one workgroup per compute unit
             const int64_t want = std::max<int64_t>(1, kUnits / std::max<int64_t>(pairs, 1)), rounds = std::max<int64_t>(1, (p.q_tiles + want - 1) / want);
             p.blocks = static_cast<int32_t>(rounds * kRingWaves);
@@ -592,12 +593,13 @@ int32_t launch_shape(const CrossArgs& a, const Plan& p, const Parts& pt, hipStre
     }
     if constexpr (sizeof(T) == 2 && kVec) {
         if (p.ring) {
-            const size_t lds = static_cast<size_t>(p.resident ? p.tiles : kRing) * PairRing<DP, kRingWaves>::kTileBytes + 128;
+            const size_t lds = p.resident ? static_cast<size_t>(p.tiles) * PairRing<DP, kRingWaves>::kTileBytes : kPassTiles<DP> * PairRing<DP, kPassWaves>::kTileBytes;
             const auto launch = [&](auto resident) {
                 auto kern = cross_ring_kernel<DP, decltype(resident)::value>;
                 static LdsLimit limit;
                 if (!limit.allow(reinterpret_cast<const void*>(kern), kLdsBytes)) return FREE_ERR_HIP;
-                hipLaunchKernelGGL(kern, dim3(static_cast<uint32_t>(blocks)), dim3(kRingWaves * 64), lds, s, a, pt, static_cast<int32_t>(p.q_tiles), p.blocks);
+                hipLaunchKernelGGL(kern, dim3(static_cast<uint32_t>(blocks)), dim3((p.resident ? kRingWaves : kPassWaves) * 64), lds, s, a, pt, static_cast<int32_t>(p.q_tiles),
+                                   p.blocks);
                 return launch_ok() ? FREE_OK : FREE_ERR_HIP;
             };
             return p.resident ? launch(std::true_type{}) : launch(std::false_type{});

@@ -371,11 +371,11 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 && DP <= 80) || DP <= 32 
 
 // ---- the same for bf16 of whole chunks and many rows (cross_ring_kernel of cross_attn.hip)
 template <int DP, bool kResident>
-__global__ __launch_bounds__(kRingWaves * 64, 2) void cross_dq_ring_kernel(CrossArgs a, RowStats stats, int32_t chunks, int32_t blocks_per_chunk) {
+__global__ __launch_bounds__((kResident ? kRingWaves : kPassWaves) * 64, 2) void cross_dq_ring_kernel(CrossArgs a, RowStats stats, int32_t chunks, int32_t blocks_per_chunk) {
     using T = bf16_t;
     using H = HeadShape<T, DP>;
-    using Ring = PairRing<DP, kRingWaves>;
-    constexpr int KSTEPS = H::KSTEPS, DT = H::DT;
+    constexpr int KSTEPS = H::KSTEPS, DT = H::DT, NW = kResident ? kRingWaves : kPassWaves, kSlots = kPassTiles<DP>;
+    using Ring = PairRing<DP, NW>;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     __shared__ uint64_t masks[kMaxTiles];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, g = lane >> 5;
@@ -383,7 +383,7 @@ __global__ __launch_bounds__(kRingWaves * 64, 2) void cross_dq_ring_kernel(Cross
     const WorkPlace at(blockIdx.x, pairs);
     const int pair = at.pair, chunk = at.place, kvh = pair % a.kv_heads, b = pair / a.kv_heads;
     const int rows = a.Nq * group, blocks = (rows + 31) / 32;
-    RingKeys<DP> keys(a, b, kvh, wave, lane);
+    RingKeys<DP, NW> keys(a, b, kvh, wave, lane);
     const int tiles = keys.tiles();
     const uint32_t lds_base = lds_address(lds);
     const auto request = [&](int t, int slot) { keys.request(t, lds_base + slot * Ring::kTileBytes, wave); };
@@ -423,11 +423,11 @@ __global__ __launch_bounds__(kRingWaves * 64, 2) void cross_dq_ring_kernel(Cross
         const int first = chunk * blocks_per_chunk, last = min(first + blocks_per_chunk, blocks);
         if (first + wave < last) own.load(a, b, kvh, (first + wave) * 32 + l32, g);
         bring_keys(keys, lds, masks, 0, wave, lane);
-        for (int block = first + wave; block < last; block += kRingWaves) {
+        for (int block = first + wave; block < last; block += NW) {
             begin();
             RowOperands<T, DP, true> next = own;
-            const bool more = block + kRingWaves < last;
-            if (kNext && more) next.load(a, b, kvh, (block + kRingWaves) * 32 + l32, g);
+            const bool more = block + NW < last;
+            if (kNext && more) next.load(a, b, kvh, (block + NW) * 32 + l32, g);
             const auto bits_of = [&](int t) { return keys.mask ? masks[t] : keys_below(keys.len - t * Tile<T, DP>::kRows); };
             dl = 0.f;
             for (int t = 0; t < tiles; ++t) measure(lds + t * Ring::kTileBytes, bits_of(t));
@@ -435,30 +435,30 @@ __global__ __launch_bounds__(kRingWaves * 64, 2) void cross_dq_ring_kernel(Cross
             for (int t = 0; t < tiles; ++t) multiply(lds + t * Ring::kTileBytes, bits_of(t));
             finish(block);
             own = next;
-            if (!kNext && more) own.load(a, b, kvh, (block + kRingWaves) * 32 + l32, g);
+            if (!kNext && more) own.load(a, b, kvh, (block + NW) * 32 + l32, g);
         }
     } else {
-        const int block = chunk * kRingWaves + wave;
+        const int block = chunk * NW + wave;
         const auto begin_tiles = [&] {
 #pragma unroll
-            for (int s = 0; s < kRing - 1; ++s)
+            for (int s = 0; s < kSlots - 1; ++s)
                 if (s < tiles) request(s, s);
         };
         const auto each_tile = [&](auto&& use) {
-            int slot = 0, free_slot = kRing - 1;
+            int slot = 0, free_slot = kSlots - 1;
             for (int t = 0; t < tiles; ++t) {
                 const uint64_t valid = keys.valid(t, lane);
-                if (t + kRing - 1 <= tiles) wait_vm_barrier<(kRing - 2) * Ring::N>();
+                if (t + kSlots - 1 <= tiles) wait_vm_barrier<(kSlots - 2) * Ring::N>();
                 else wait_vm_barrier<0>();
                 char* const tile = lds + slot * Ring::kTileBytes;
                 if (keys.mask && valid != ~0ull) {
                     keys.drop(tile, 0, valid, wave, lane);
                     __syncthreads();
                 }
-                if (t + kRing - 1 < tiles) request(t + kRing - 1, free_slot);
+                if (t + kSlots - 1 < tiles) request(t + kSlots - 1, free_slot);
                 use(tile, valid);
                 free_slot = slot;
-                slot = slot + 1 == kRing ? 0 : slot + 1;
+                slot = slot + 1 == kSlots ? 0 : slot + 1;
             }
         };
         begin_tiles();
@@ -475,6 +475,165 @@ __global__ __launch_bounds__(kRingWaves * 64, 2) void cross_dq_ring_kernel(Cross
         }
         each_tile(multiply);
         finish(block);
+    }
+}
+
+// Head dimensions over 96: a wavefront has two blocks of 32 rows and the registers of two wavefronts, so that what it reads from LDS is multiplied twice.
+// delta += sum P dP over one 32-key block, or dq += of it
+template <int DP, bool kDelta>
+__device__ __forceinline__ void dq_wide_block(const char* tile_k, const char* tile_v, int row0, int lane, uint32_t bits, const RowOperands<bf16_t, DP, true> (&own)[2],
+                                              float scale_log2, float (&dl)[2], float (&rest)[2], xf32x16_t (&dq)[2][HeadShape<bf16_t, DP>::DT]) {
+    using T = bf16_t;
+    constexpr int KSTEPS = HeadShape<T, DP>::KSTEPS, G = 2, kGroups = KSTEPS / G, DT = HeadShape<T, DP>::DT;
+    static_assert(KSTEPS % G == 0, "whole groups");
+    xu32x4_t f[2][G];                // the operands multiplied and those read ahead
+    xf32x16_t st[2], dp[2];
+    const auto read = [&](int i) {
+        const int row = block_row<T>(lane & 31), g = lane >> 5;
+        const char* const base = (i < kGroups ? tile_k : tile_v) + row0 * Tile<T, DP>::kPitch;
+#pragma unroll
+        for (int k = 0; k < G; ++k) f[i & 1][k] = *reinterpret_cast<const xu32x4_t*>(base + Tile<T, DP>::at(row, 2 * (i % kGroups * G + k) + g));
+    };
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+        clear_tile(st[r]);
+        clear_tile(dp[r]);
+    }
+    const float nlse[2] = {-own[0].lse * kLog2e, -own[1].lse * kLog2e};
+    Columns<T, DP> c;
+    read(0);
+#pragma unroll
+    for (int i = 0; i < 2 * kGroups; ++i) {
+        if (i + 1 < 2 * kGroups) read(i + 1);
+        else if (!kDelta) c.read(tile_k, row0, lane, 0);
+        fence();
+#pragma unroll
+        for (int k = 0; k < G; ++k)
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+                if (i < kGroups) chunk_product<T>(f[i & 1][k], own[r].q[i * G + k], st[r]);
+                else chunk_product<T>(f[i & 1][k], own[r].g[(i - kGroups) * G + k], dp[r]);
+            }
+        if (i >= kGroups) {                              // (exponentials between the products of the second tensor)
+            const int r = (i - kGroups) / (kGroups / 2), e0 = (i - kGroups) % (kGroups / 2) * (32 / kGroups);
+#pragma unroll
+            for (int e = e0; e < e0 + 32 / kGroups; ++e) st[r][e] = __builtin_amdgcn_exp2f(fmaf(st[r][e], scale_log2, nlse[r]));
+#pragma unroll
+            for (int k = 0; k < 2 * G; ++k) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x002, 4, 0);
+                __builtin_amdgcn_sched_group_barrier(0x400, 2, 0);
+            }
+        }
+    }
+    const auto weigh_row = [&](int r) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) st[r][e] *= kDelta ? dp[r][e] : dp[r][e] - dl[r];
+        if (__builtin_amdgcn_readfirstlane(bits) != ~0u) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) st[r][e] = bits >> register_row<T>(e, 0) & 1 ? st[r][e] : 0.f;
+        }
+        if (kDelta) dl[r] += sum_of(st[r]);
+        else rest[r] += sum_of(st[r]);
+    };
+    weigh_row(0);
+    if constexpr (kDelta) {
+        weigh_row(1);
+    } else {
+        Columns<T, DP> next;
+        next.read(tile_k, row0, lane, 1);
+        fence();
+        c.multiply(st[0], 0, dq[0]);
+        next.multiply(st[0], 1, dq[0]);
+        weigh_row(1);
+#pragma unroll
+        for (int k = 0; k < 2 * DT; ++k) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x002, 8, 0);
+        }
+        c.multiply(st[1], 0, dq[1]);
+        next.multiply(st[1], 1, dq[1]);
+    }
+}
+
+constexpr int kWideWaves = 4;
+
+template <int DP>
+__global__ __launch_bounds__(kWideWaves * 64, 1) void cross_dq_wide_kernel(CrossArgs a, RowStats stats) {
+    using T = bf16_t;
+    using H = HeadShape<T, DP>;
+    using Ring = PairRing<DP, kWideWaves>;
+    constexpr int DT = H::DT;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, g = lane >> 5;
+    const int pairs = a.B * a.kv_heads, group = a.heads / a.kv_heads;
+    const WorkPlace at(blockIdx.x, pairs);
+    const int pair = at.pair, kvh = pair % a.kv_heads, b = pair / a.kv_heads;
+    const int rows = a.Nq * group, row0 = (at.place * kWideWaves + wave) * 64 + l32;
+    RingKeys<DP, kWideWaves> keys(a, b, kvh, wave, lane);
+    const int tiles = keys.tiles();
+    const uint32_t lds_base = lds_address(lds);
+    const auto request = [&](int t, int slot) { keys.request(t, lds_base + slot * Ring::kTileBytes, wave); };
+    const auto begin_tiles = [&] {
+#pragma unroll
+        for (int s = 0; s < kRing - 1; ++s)
+            if (s < tiles) request(s, s);
+    };
+    begin_tiles();
+    const float scale_log2 = a.scale * kLog2e;
+    RowOperands<T, DP, true> own[2];
+    xf32x16_t dq[2][DT];
+    float dl[2] = {0.f, 0.f}, rest[2] = {0.f, 0.f};
+#pragma unroll
+    for (int r = 0; r < 2; ++r) own[r].load(a, b, kvh, row0 + 32 * r, g);
+    const auto each_tile = [&](auto delta) {
+        int slot = 0, free_slot = kRing - 1;
+        for (int t = 0; t < tiles; ++t) {
+            const uint64_t valid = keys.valid(t, lane);
+            if (t + kRing - 1 <= tiles) wait_vm_barrier<(kRing - 2) * Ring::N>();
+            else wait_vm_barrier<0>();
+            char* const tile = lds + slot * Ring::kTileBytes;
+            if (keys.mask && valid != ~0ull) {
+                keys.drop(tile, 0, valid, wave, lane);
+                __syncthreads();
+            }
+            if (t + kRing - 1 < tiles) request(t + kRing - 1, free_slot);
+#pragma unroll 1
+            for (int kb = 0; kb < 2; ++kb) {
+                const uint32_t bits = static_cast<uint32_t>(valid >> (32 * kb));
+                dq_wide_block<DP, decltype(delta)::value>(tile, tile + Ring::kSecond, kb * 32, lane, bits == ~0u ? bits : bits >> (8 * g), own, scale_log2, dl, rest, dq);
+            }
+            free_slot = slot;
+            slot = slot + 1 == kRing ? 0 : slot + 1;
+        }
+    };
+    if (keys.len > kTwiceKeys) {
+#pragma unroll
+        for (int r = 0; r < 2; ++r) dl[r] = own[r].delta(a, g);
+    }
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+        arrived(own[r].q);
+        arrived(own[r].g);
+    }
+    if (keys.len <= kTwiceKeys) {
+        each_tile(std::true_type{});
+#pragma unroll
+        for (int r = 0; r < 2; ++r) dl[r] = add_lane_xor<32>(dl[r]);
+        __syncthreads();
+        begin_tiles();
+    }
+#pragma unroll
+    for (int r = 0; r < 2; ++r)
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) clear_tile(dq[r][dt]);
+    each_tile(std::false_type{});
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+        const bool on = row0 + 32 * r < rows;
+        const float sum = add_lane_xor<32>(rest[r]);
+        if (g == 0 && on) own[r].leave(stats, dl[r] + sum, a.scale);
+        store_column<T, true, DT>(static_cast<T*>(a.dq) + own[r].q_at * a.dq_stride + own[r].h_at, a.dh, g, dq[r], a.scale, on);
     }
 }
 
@@ -685,11 +844,13 @@ Plan plan_of(int32_t B, int32_t Nq, int32_t Nk, int32_t heads, int32_t kv_heads,
     const int64_t blocks = (rows + 31) / 32;
     if (ring && pairs * blocks >= kUnits * kRingWaves) {
         p.q_ring = true;
-        p.resident = key_tiles <= tiles_that_fit(dh);
+        p.resident = dh <= 96 && key_tiles <= tiles_that_fit(dh);
         p.q_parts = 1;
         p.q_part_tiles = static_cast<int32_t>(key_tiles);
-        p.q_tiles = (blocks + kRingWaves - 1) / kRingWaves;
+        const int64_t per_group = dh > 96 ? 2 * kWideWaves : kPassWaves;
+        p.q_tiles = (blocks + per_group - 1) / per_group;
         if (p.resident) {
+            p.q_tiles = (blocks + kRingWaves - 1) / kRingWaves;
             const int64_t want = std::max<int64_t>(1, kUnits / units), rounds = std::max<int64_t>(1, (p.q_tiles + want - 1) / want);
             p.q_blocks = static_cast<int32_t>(rounds * kRingWaves);
             p.q_tiles = (blocks + p.q_blocks - 1) / p.q_blocks;
@@ -743,13 +904,22 @@ int32_t launch_dq(const CrossArgs& a, const Plan& p, const RowStats& stats, cons
     using TL = Tile<T, DP>;
     const dim3 grid(static_cast<uint32_t>(static_cast<int64_t>(a.B) * a.kv_heads * p.q_tiles * p.q_parts));
     if constexpr (sizeof(T) == 2 && kVec) {
-        if (p.q_ring) {
-            const size_t lds = static_cast<size_t>(p.resident ? p.q_part_tiles : kRing) * PairRing<DP, kRingWaves>::kTileBytes + 128;
+        if constexpr (DP > 96) {
+            if (p.q_ring) {
+                auto kern = cross_dq_wide_kernel<DP>;
+                static LdsLimit limit;
+                constexpr size_t lds = kRing * PairRing<DP, kWideWaves>::kTileBytes;
+                if (!allow(kern, limit, lds)) return FREE_ERR_HIP;
+                hipLaunchKernelGGL(kern, grid, dim3(kWideWaves * 64), lds, s, a, stats);
+                return launch_ok() ? FREE_OK : FREE_ERR_HIP;
+            }
+        } else if (p.q_ring) {
+            const size_t lds = p.resident ? static_cast<size_t>(p.q_part_tiles) * PairRing<DP, kRingWaves>::kTileBytes : kPassTiles<DP> * PairRing<DP, kPassWaves>::kTileBytes;
             const auto launch = [&](auto resident) {
                 auto kern = cross_dq_ring_kernel<DP, decltype(resident)::value>;
                 static LdsLimit limit;
                 if (!allow(kern, limit, kLdsBytes)) return FREE_ERR_HIP;
-                hipLaunchKernelGGL(kern, grid, dim3(kRingWaves * 64), lds, s, a, stats, static_cast<int32_t>(p.q_tiles), p.q_blocks);
+                hipLaunchKernelGGL(kern, grid, dim3((p.resident ? kRingWaves : kPassWaves) * 64), lds, s, a, stats, static_cast<int32_t>(p.q_tiles), p.q_blocks);
                 return launch_ok() ? FREE_OK : FREE_ERR_HIP;
             };
             return p.resident ? launch(std::true_type{}) : launch(std::false_type{});
