@@ -146,8 +146,10 @@ int32_t launch_down_shape(const DownArgs& a, hipStream_t s) {
 
 template <typename T, int MT>
 int32_t launch_down_ranks(const DownArgs& a, hipStream_t s) {
-    if (a.t_row <= 16) return launch_down_shape<T, MT, 1>(a, s);
-    if (a.t_row <= 32) return launch_down_shape<T, MT, 2>(a, s);
+    // more ranks per workgroup read x less often, but few workgroups leave compute units without work
+    const int32_t blocks = (a.M + 16 * MT - 1) / (16 * MT);
+    if (a.t_row <= 16 || blocks < 64) return launch_down_shape<T, MT, 1>(a, s);
+    if (a.t_row <= 32 || blocks < 128) return launch_down_shape<T, MT, 2>(a, s);
     return launch_down_shape<T, MT, 4>(a, s);
 }
 
@@ -449,6 +451,7 @@ struct Sizes {
         Np = up_to(nn, slice);
     }
     bool few() const { return ffn_rows_pay(M, K, N, K != Kp); }
+    bool few_back() const { return ffn_rows_pay(M, Np, K, false); }
     size_t thin_bytes() const { return static_cast<size_t>(M) * t_row * es; }
 };
 
@@ -609,7 +612,8 @@ int32_t backward_of(const Sizes& z, const AdapterArgs& a, char* ws, hipStream_t 
     DownArgs down{dout, w.bt, a.adapter, a.scale, w.u, z.M, z.Np, z.n, z.t_row, z.r, z.t_row, a.rows_per_sample, w.zeros, z.K};
     FREE_STEP(launch_down<T>(down, s));
     const AdapterTerm term{w.u, w.at, a.adapter, nullptr, z.n, z.t_row, z.t_row, z.t_row, z.K, a.rows_per_sample};
-    FREE_STEP(linear_with<T>(dout, w.wt, w.zeros, z.M, z.Np, term, static_cast<T*>(a.dx), s));
+    if (z.few_back()) FREE_STEP(launch_adapter_rows<T>(dout, w.wt, z.M, z.K, z.Np, term, static_cast<T*>(a.dx), s));
+    else FREE_STEP(linear_with<T>(dout, w.wt, w.zeros, z.M, z.Np, term, static_cast<T*>(a.dx), s));
     const SumPlan plan(z);
     const SumArgs sum{{x, dout}, {w.u, a.saved}, {w.x ? z.Kp : z.K, z.Np}, {z.K, z.N}, {(z.K + 127) / 128, (z.N + 127) / 128}, {a.da, a.db}, w.part, a.adapter, z.M,
                       z.n, z.r, z.t_row, a.rows_per_sample, plan.parts, plan.part_tiles};

@@ -181,7 +181,7 @@ struct RowOperands {
 
 // ---- dq and delta
 template <typename T, int DP, bool kVec>
-__global__ __launch_bounds__(kThreads, (sizeof(T) == 2 || DP <= 64) ? 2 : 1) void cross_dq_kernel(CrossArgs a, RowStats stats, GradParts pt, int32_t q_tiles) {
+__global__ __launch_bounds__(kThreads, (sizeof(T) == 2 && kVec) || DP <= 64 ? 2 : 1) void cross_dq_kernel(CrossArgs a, RowStats stats, GradParts pt, int32_t q_tiles) {
     using H = HeadShape<T, DP>;
     using TL = Tile<T, DP>;
     constexpr int KSTEPS = H::KSTEPS, DT = H::DT, BKV = TL::kRows;
@@ -199,15 +199,37 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 || DP <= 64) ? 2 : 1) voi
     KeyStream<T, DP, kVec> keys(a, b, kvh);
     const int t0 = part * pt.tiles, t1 = min(t0 + pt.tiles, keys.tiles());
     const uint32_t lds_base = lds_address(lds);
-    const int n = max(t1 - t0, 0);
     const bool twice = sizeof(T) == 2 && keys.len <= kTwiceKeys;         // (which are all in the first part then)
-    const int passes = twice ? 2 * n : n;
-    const auto tile_of = [&](int u) { return t0 + (u >= n ? u - n : u); };
-    keys.request_mask(t0, lane);
-    uint64_t valid = keys.valid_of(t0);
-    if (n > 0) keys.request(t0, lds_base, lds_base + TL::kBytes, wave, lane, valid);
-    keys.request_mask(tile_of(1), lane);
-
+    uint64_t valid;
+    const auto begin_tiles = [&] {
+        keys.request_mask(t0, lane);
+        valid = keys.valid_of(t0);
+        if (t0 < t1) keys.request(t0, lds_base, lds_base + TL::kBytes, wave, lane, valid);
+        keys.request_mask(t0 + 1, lane);
+    };
+    const auto each_block = [&](auto&& use) {
+        if (t0 < t1) keys.deliver(lds, lds + TL::kBytes, tid, valid);
+        keys.k.settle();
+        for (int t = t0; t < t1; ++t) {
+            const int stage = (t - t0) & 1, other = (stage ^ 1) * 2 * TL::kBytes;
+            const char* const sK = lds + stage * 2 * TL::kBytes;
+            const uint64_t valid_next = keys.valid_of(t + 1);
+            if (t + 1 < t1) {
+                keys.request(t + 1, lds_base + other, lds_base + other + TL::kBytes, wave, lane, valid_next);
+                keys.request_mask(t + 2, lane);
+            }
+#pragma unroll
+            for (int kb = 0; kb < BKV / 32; ++kb) {
+                // (fp32 has 32 keys to a tile, and a full mask of them)
+                const uint32_t bits = static_cast<uint32_t>(valid >> (32 * kb));
+                use(sK, kb * 32, bits == ~0u ? bits : bits >> (sizeof(T) == 2 ? 8 * g : 4 * g));
+            }
+            if (t + 1 < t1) keys.deliver(lds + other, lds + other + TL::kBytes, tid, valid_next);
+            valid = valid_next;
+            keys.k.settle();
+        }
+    };
+    begin_tiles();
     RowOperands<T, DP, kVec> own;
     own.load(a, b, kvh, row, g);
     const float lse2 = own.lse * kLog2e, scale_log2 = a.scale * kLog2e;
@@ -217,31 +239,20 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 || DP <= 64) ? 2 : 1) voi
     xf32x16_t dq[DT];
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) clear_tile(dq[dt]);
-    if (n > 0) keys.deliver(lds, lds + TL::kBytes, tid, valid);
     arrived(own.q);
     arrived(own.g);
-    keys.k.settle();
-    for (int u = 0; u < passes; ++u) {
-        const int stage = u & 1, other = (stage ^ 1) * 2 * TL::kBytes;
-        const char* const sK = lds + stage * 2 * TL::kBytes;
-        const uint64_t valid_next = keys.valid_of(tile_of(u + 1));
-        if (u + 1 < passes) {
-            keys.request(tile_of(u + 1), lds_base + other, lds_base + other + TL::kBytes, wave, lane, valid_next);
-            keys.request_mask(tile_of(u + 2), lane);
+    if constexpr (sizeof(T) == 2) {
+        if (twice) {
+            each_block([&](const char* tile, int row0, uint32_t bits) {
+                delta_block<T, DP>(tile, tile + TL::kBytes, row0, lane, bits, own.q, own.g, lse2, scale_log2, dl);
+            });
+            dl = add_lane_xor<32>(dl);
+            begin_tiles();
         }
-        if (twice && u == n) dl = add_lane_xor<32>(dl);
-#pragma unroll
-        for (int kb = 0; kb < BKV / 32; ++kb) {
-            // (fp32 has 32 keys to a tile, and a full mask of them)
-            const uint32_t bits = static_cast<uint32_t>(valid >> (32 * kb));
-            const uint32_t mine = bits == ~0u ? bits : bits >> (sizeof(T) == 2 ? 8 * g : 4 * g);
-            if (twice && u < n) delta_block<T, DP>(sK, sK + TL::kBytes, kb * 32, lane, mine, own.q, own.g, lse2, scale_log2, dl);
-            else dq_block<T, DP, true>(sK, sK + TL::kBytes, kb * 32, lane, mine, own.q, own.g, dl, lse2, scale_log2, rest, dq);
-        }
-        if (u + 1 < passes) keys.deliver(lds + other, lds + other + TL::kBytes, tid, valid_next);
-        valid = valid_next;
-        keys.k.settle();
     }
+    each_block([&](const char* tile, int row0, uint32_t bits) {
+        dq_block<T, DP, true>(tile, tile + TL::kBytes, row0, lane, bits, own.q, own.g, dl, lse2, scale_log2, rest, dq);
+    });
     // (a part has not all keys; with both passes the rest is what rounding leaves)
     rest = pt.parts > 1 ? 0.f : add_lane_xor<32>(rest);
     if (part == 0 && g == 0 && row < rows) own.leave(stats, dl + rest, a.scale);
@@ -249,16 +260,21 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 || DP <= 64) ? 2 : 1) voi
     else store_column<T, kVec, DT>(static_cast<T*>(a.dq) + own.q_at * a.dq_stride + own.h_at, a.dh, g, dq, a.scale, row < rows);
 }
 
-// ---- dk and dv.  KW wavefronts have 32 keys each; with KW 2 the two halves of a tile's rows go to two wavefronts, whose sums are parts of
-// their own.
+// ---- dk and dv.  KW wavefronts have 32 keys each; where the keys leave some without, the rows of a step are shared out among QW, whose sums are
+// parts of their own: the two halves of a tile (bf16), or a tile for each (fp32, whose products take eight times as long; 7 x 5303 queries to one key, 16
+// heads of 64: 452 -> 165 us).  With four tiles to a step there is one stage.
+template <typename T, int KW>
+constexpr int kStepTiles = sizeof(T) == 4 ? 4 / KW : 1;
+
 template <typename T, int DP, int KW, bool kVec>
 __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 && DP <= 80) || DP <= 32 ? 2 : 1) void cross_dkv_kernel(CrossArgs a, RowStats row_stats, GradParts pt, int32_t k_tiles) {
     using H = HeadShape<T, DP>;
     using TL = Tile<T, DP>;
-    constexpr int KSTEPS = H::KSTEPS, DT = H::DT, BR = TL::kRows, QW = 4 / KW, RB = BR / 32 / QW;
+    constexpr int KSTEPS = H::KSTEPS, DT = H::DT, BR = TL::kRows, QW = 4 / KW;
+    constexpr int SUB = kStepTiles<T, KW>, STAGES = SUB == 4 ? 1 : 2, MR = BR * SUB, RB = SUB > 1 ? 1 : BR / 32 / QW;
     static_assert(RB >= 1, "a block of rows for each wavefront");
-    extern __shared__ __attribute__((aligned(16))) char lds[];          // [stage][q, dout], then [stage][lse, delta][BR]
-    float* const stats = reinterpret_cast<float*>(lds + 4 * TL::kBytes);
+    extern __shared__ __attribute__((aligned(16))) char lds[];          // [stage][tile][q, dout], then [stage][lse, delta][MR]
+    float* const stats = reinterpret_cast<float*>(lds + STAGES * SUB * 2 * TL::kBytes);
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int l32 = lane & 31, g = lane >> 5;
     const int kw = wave % KW, qw = wave / KW;
@@ -272,32 +288,36 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 && DP <= 80) || DP <= 32 
     const int kvh = pair % a.kv_heads, b = pair / a.kv_heads;
     const int rows = a.Nq * group, key = k_tile * 32 * KW + kw * 32 + l32;
     const int len = attended(a, b);
-    const int tiles = (rows + BR - 1) / BR, t0 = part * pt.tiles;
+    const int steps = (rows + MR - 1) / MR, t0 = part * pt.tiles;
     // keys that do not count have no gradient: a workgroup without others has nothing to sum
-    const int t1 = k_tile * 32 * KW < len ? min(t0 + pt.tiles, tiles) : t0;
+    const int t1 = k_tile * 32 * KW < len ? min(t0 + pt.tiles, steps) : t0;
     const bool there = key < len && (!a.key_mask || a.key_mask[static_cast<int64_t>(b) * a.Nk + key] != 0);
 
     const int q_row = static_cast<int>(a.q_stride) * static_cast<int>(sizeof(T)), g_row = static_cast<int>(a.dout_stride) * static_cast<int>(sizeof(T));
     const int head_bytes = a.dh * static_cast<int>(sizeof(T));
     const int64_t first_row = static_cast<int64_t>(b) * a.Nq, h0 = static_cast<int64_t>(kvh) * group * a.dh;
-    TileStream<T, DP, kVec> queries, grads;
+    TileStream<T, DP, kVec> queries[SUB], grads[SUB];
     float lse_next = 0.f, delta_next = 0.f;
     const uint32_t lds_base = lds_address(lds);
     const auto request = [&](int t, int stage) {
-        const int r0 = t * BR, token0 = over_group(r0, group), rest = r0 - token0 * group;         // of the group's heads: row r0 + r is token0 + (rest + r) / group
-        const int64_t left = a.Nq - token0;
-        const auto place = [&](int stride) {
-            return [=](int r) {
-                const int token = over_group(rest + r, group);
-                return token * stride + (rest + r - token * group) * head_bytes;
+#pragma unroll
+        for (int j = 0; j < SUB; ++j) {
+            const int r0 = t * MR + j * BR, token0 = over_group(r0, group), rest = r0 - token0 * group;      // of the group's heads: row r0 + r is token0 + (rest + r) / group
+            const int64_t left = a.Nq - token0;
+            const auto place = [&](int stride) {
+                return [=](int r) {
+                    const int token = over_group(rest + r, group);
+                    return token * stride + (rest + r - token * group) * head_bytes;
+                };
             };
-        };
-        const uint32_t to = lds_base + stage * 2 * TL::kBytes;
-        queries.request(static_cast<const T*>(a.q) + (first_row + token0) * a.q_stride + h0, (left - 1) * q_row + group * head_bytes, to, wave, lane, a.dh, false, 0,
-                        place(q_row));
-        grads.request(static_cast<const T*>(a.dout) + (first_row + token0) * a.dout_stride + h0, (left - 1) * g_row + group * head_bytes, to + TL::kBytes, wave, lane,
-                      a.dh, false, 0, place(g_row));
-        if (tid < BR) {
+            const uint32_t to = lds_base + (stage * SUB + j) * 2 * TL::kBytes;
+            queries[j].request(static_cast<const T*>(a.q) + (first_row + token0) * a.q_stride + h0, (left - 1) * q_row + group * head_bytes, to, wave, lane, a.dh, false, 0,
+                               place(q_row));
+            grads[j].request(static_cast<const T*>(a.dout) + (first_row + token0) * a.dout_stride + h0, (left - 1) * g_row + group * head_bytes, to + TL::kBytes, wave,
+                             lane, a.dh, false, 0, place(g_row));
+        }
+        const int r0 = t * MR, token0 = over_group(r0, group), rest = r0 - token0 * group;
+        if (tid < MR) {
             const int token = over_group(rest + tid, group), h = rest + tid - token * group;
             const int64_t at = (static_cast<int64_t>(b) * a.heads + kvh * group + h) * a.Nq + token0 + token;
             const bool on = r0 + tid < rows;
@@ -306,12 +326,15 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 && DP <= 80) || DP <= 32 
         }
     };
     const auto deliver = [&](int stage) {
-        char* const sQ = lds + stage * 2 * TL::kBytes;
-        queries.deliver(sQ, tid, false, 0);
-        grads.deliver(sQ + TL::kBytes, tid, false, 0);
-        if (tid < BR) {
-            stats[stage * 2 * BR + tid] = lse_next;
-            stats[stage * 2 * BR + BR + tid] = delta_next;
+#pragma unroll
+        for (int j = 0; j < SUB; ++j) {
+            char* const sQ = lds + (stage * SUB + j) * 2 * TL::kBytes;
+            queries[j].deliver(sQ, tid, false, 0);
+            grads[j].deliver(sQ + TL::kBytes, tid, false, 0);
+        }
+        if (tid < MR) {
+            stats[stage * 2 * MR + tid] = lse_next;
+            stats[stage * 2 * MR + MR + tid] = delta_next;
         }
     };
     if (t0 < t1) request(t0, 0);
@@ -336,19 +359,20 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 && DP <= 80) || DP <= 32 
     if (t0 < t1) deliver(0);
     arrived(kf);
     arrived(vf);
-    queries.settle();
+    TileStream<T, DP, kVec>::settle();
     for (int t = t0; t < t1; ++t) {
-        const int stage = (t - t0) & 1;
-        const char* const sQ = lds + stage * 2 * TL::kBytes;
-        if (t + 1 < t1) request(t + 1, stage ^ 1);
+        const int stage = STAGES == 2 ? (t - t0) & 1 : 0, other = STAGES == 2 ? stage ^ 1 : 0, sub = SUB > 1 ? qw : 0;
+        const char* const sQ = lds + (stage * SUB + sub) * 2 * TL::kBytes;
+        if (t + 1 < t1) request(t + 1, other);
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb) {
-            const int row0 = (qw * RB + rb) * 32;
-            const float* const at = stats + stage * 2 * BR;
-            dkv_block<T, DP>(sQ, sQ + TL::kBytes, row0, lane, at, at + BR, kf, vf, scale_log2, dk, dv);
+            const int row0 = SUB > 1 ? 0 : (qw * RB + rb) * 32;
+            const float* const at = stats + stage * 2 * MR + sub * BR;
+            dkv_block<T, DP>(sQ, sQ + TL::kBytes, row0, lane, at, at + MR, kf, vf, scale_log2, dk, dv);
         }
-        if (t + 1 < t1) deliver(stage ^ 1);
-        queries.settle();
+        if (STAGES == 1) __syncthreads();
+        if (t + 1 < t1) deliver(other);
+        TileStream<T, DP, kVec>::settle();
     }
     const bool on = key < a.Nk;
     // (what a key that does not count has got are sums over zeros in place of it, not a gradient)
@@ -790,6 +814,7 @@ __global__ __launch_bounds__(kThreads) void cross_sum_kernel(SumJobs a) {
     for (int64_t i = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x; i < all; i += static_cast<int64_t>(gridDim.x) * kThreads) {
         float s[V];
         __builtin_memcpy(s, j.parts + i * V, sizeof(s));
+#pragma unroll 8
         for (int p = 1; p < a.n; ++p) {
             float v[V];
             __builtin_memcpy(v, j.parts + (p * all + i) * V, sizeof(v));
@@ -870,9 +895,10 @@ Plan plan_of(int32_t B, int32_t Nq, int32_t Nk, int32_t heads, int32_t kv_heads,
         p.k_parts = static_cast<int32_t>(parts);
         p.k_units = 1;
     } else {
-        p.kw = dtype == FREE_BF16 && Nk <= 64 ? 2 : 4;
+        p.kw = dtype == FREE_FP32 && Nk <= 32 ? 1 : Nk <= 64 ? 2 : 4;
         p.k_tiles = std::max<int64_t>(1, (static_cast<int64_t>(Nk) + 32 * p.kw - 1) / (32 * p.kw));
-        cut(pairs * p.k_tiles, 2 * kUnits, row_tiles, 4, &parts, &per);
+        const int64_t steps = dtype == FREE_FP32 ? (row_tiles * p.kw + 3) / 4 : row_tiles;       // (kStepTiles)
+        cut(pairs * p.k_tiles, 2 * kUnits, steps, dtype == FREE_FP32 ? p.kw : 4, &parts, &per);
         p.k_units = 4 / p.kw;
         p.k_parts = static_cast<int32_t>(parts * p.k_units);
     }
@@ -947,17 +973,19 @@ int32_t launch_dkv(const CrossArgs& a, const Plan& p, const RowStats& stats, con
             return launch_ok() ? FREE_OK : FREE_ERR_HIP;
         }
     }
-    const size_t lds = 4 * TL::kBytes + 4 * TL::kRows * sizeof(float);
     const auto launch = [&](auto kw) {
+        constexpr int SUB = kStepTiles<T, decltype(kw)::value>, STAGES = SUB == 4 ? 1 : 2;
+        constexpr size_t lds = STAGES * SUB * 2 * (TL::kBytes + TL::kRows * sizeof(float));
         auto kern = cross_dkv_kernel<T, DP, decltype(kw)::value, kVec>;
         static LdsLimit limit;
         if (!allow(kern, limit, lds)) return FREE_ERR_HIP;
         hipLaunchKernelGGL(kern, grid, dim3(kThreads), lds, s, a, stats, pt, static_cast<int32_t>(p.k_tiles));
         return launch_ok() ? FREE_OK : FREE_ERR_HIP;
     };
-    if constexpr (sizeof(T) == 2) {
-        if (p.kw == 2) return launch(std::integral_constant<int, 2>{});
+    if constexpr (sizeof(T) == 4) {
+        if (p.kw == 1) return launch(std::integral_constant<int, 1>{});
     }
+    if (p.kw == 2) return launch(std::integral_constant<int, 2>{});
     return launch(std::integral_constant<int, 4>{});
 }
 

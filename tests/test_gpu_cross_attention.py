@@ -84,6 +84,9 @@ def test_odd_head_dimensions(dtype, dh):
     (2, 1100, 40, 2, 2, 72),             # queries in parts
     (1, 700, 200, 4, 1, 128),
     (1, 2000, 130, 8, 8, 64),
+    (2, 2500, 4, 8, 1, 72),              # queries in parts and shared out among the wavefronts
+    (1, 3000, 1, 2, 2, 128),
+    (2, 1700, 64, 3, 3, 96),
 ])
 def test_sums_in_parts(dtype, B, Nq, Nk, heads, kv, dh):
     for keys in ("all", "holes"):

@@ -48,7 +48,7 @@ def compare(x, w, bias, a, bb, adapter, scale, g, rows):
 
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("M,K,N,r,n,rows", [
-    (1, 64, 64, 4, 1, 1), (8, 128, 192, 16, 8, 1), (17, 64, 320, 8, 3, 5), (33, 192, 64, 16, 2, 7), (100, 64, 128, 32, 3, 100), (130, 320, 192, 64, 4, 33),
+    (1, 64, 64, 4, 1, 1), (8, 128, 192, 16, 8, 1), (17, 64, 320, 8, 3, 5), (33, 192, 64, 16, 2, 7), (20, 2112, 2112, 24, 3, 6), (12, 1024, 512, 64, 4, 3), (1100, 64, 192, 40, 3, 300), (100, 64, 128, 32, 3, 100), (130, 320, 192, 64, 4, 33),
     (257, 128, 256, 100, 2, 64), (300, 64, 64, 128, 5, 1), (512, 384, 640, 16, 3, 256),
 ])
 def test_whole_widths(dtype, M, K, N, r, n, rows):
