@@ -616,7 +616,7 @@ int32_t free_op_cross_attention_backward(const void* dout, int64_t dout_stride, 
  * NULL; scale fp32 [n] or NULL (ones); adapter int32 [samples], in any order.  Adapters of lower rank are filled up with zeros.  Sums are fp32,
  * t is rounded to dtype as operand of the second product.  Any K and N; those that are not multiples of 8 (bf16) or 64 (fp32) go through
  * padded copies in the workspace, but for forward calls of at most 32 rows.  r <= 128, n <= 16384, M K and M N at most 2^36 (bf16) or 2^34 (fp32),
- * (K + N) r n at most 2^36, (K + N + 128) n at most 2^28, K N at most 2^34, K and N at most 2^20 (FREE_ERR_LIMIT).
+ * (K + N) r n at most 2^36, (K + N + 128) n at most 2^28, K N at most 2^34, K and N at most 2^20, M at most 2^27 (FREE_ERR_LIMIT).
  * saved (NULL: none): free_linear_adapters_saved_bytes bytes, 256-byte aligned, that keep t for the gradient.
  * The gradient, W, bias and scale being fixed:
  *   dx = dout W + u A_a,   u = scale_a dout B_a,   dA_a = sum over the adapter's rows of u^T x,   dB_a = sum of dout^T t

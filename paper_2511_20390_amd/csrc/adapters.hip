@@ -5,13 +5,17 @@
 // (s: a scale per adapter; W is shared and keeps still).  Requests come in any order: wherever a kernel has a block of rows, it takes the
 // adapters of these rows one after the other, with the other rows masked.
 //  * t and u: x (dout) is read once, 16 or 32 rows per workgroup whose wavefronts share K; rounded to the type of the product they are
-//    operands of, like the hidden values of the gated block.
-//  * out and dx: the kernels and tiles of the linear layers, whose sums begin with the adapters' (bf16, adapter_term.h), or a second pass over
-//    the result (fp32, where the product takes ten times as long); up to 32 rows of out ffn_rows.hip.
+//    operands of, like the hidden values of the gated block.  Bound by reading x and, for each block of rows, its adapter again from the L2: 12288 x 1152,
+//    rank 16, 8.6 us (3.3 TB/s); 4100 x 4096, rank 64, 26.
+//  * out and dx: the kernels and tiles of the linear layers, whose sums begin with the adapters' (bf16, adapter_term.h: 12288 rows of 1152 to 1152, 34 us; 8192
+//    of 1152 to 4608, 86 and back 95, 1.01 and 0.92 PFLOP/s; what bounds them is in gemm_pipe.hip), or a second pass over the result (fp32, where the
+//    product takes ten times as long: 1000 rows of 384 to 1536, 16 and 9 us); few rows ffn_rows.hip (8 rows of 4096 to 4096: 7.6, 4.4 TB/s).  The tiles
+//    of the gated block, which read W by its columns as well, took 489 against 345 for both passes of 4100 rows of 4096 to 4096.
 //  * dA and dB: 128 columns of x or dout by all ranks per workgroup, over the rows of one adapter, in parts that a second launch adds in
-//    order.  Rows of other adapters are not read.
+//    order.  Rows of other adapters are not read.  Bound by reading x and dout once: 8192 rows of 1152 and 4608, rank 32, 27 and 5.6 us for the parts
+//    (3.5 TB/s), 4100 of 4096 and 4096, rank 64, 34 and 10.
 // For the gradient W, B and A are needed the other way round ([K][N], [rank][N], [K][rank]): copies of that layout go into the workspace, filled
-// up with zeros to whole slices.
+// up with zeros to whole slices (4096 x 4096 of 6 adapters of rank 64: 17 us).
 #include <algorithm>
 
 #include "adapter_term.h"
@@ -42,7 +46,8 @@ struct DownArgs {
     int32_t zero_n = 0;
 };
 
-// Workgroup (block of 16 MT rows, j, 16 RT ranks): the j-th adapter of the block's rows, in the order they come
+// Workgroup (block of 16 MT rows, j, 16 RT ranks): the j-th adapter of the block's rows, in the order they come.  A workgroup more than the block has
+// adapters ends at once: how many it has is on the device.
 template <typename T, int MT, int RT, bool kEdge>
 __global__ __launch_bounds__(kDownWaves * 64) void adapter_down_kernel(DownArgs a) {
     constexpr int P = 2, E = 16 / sizeof(T), kStep = 4 * P * E, U = MT * RT == 1 ? 8 : MT * RT == 2 ? 4 : 2;      // steps in flight
@@ -146,7 +151,8 @@ int32_t launch_down_shape(const DownArgs& a, hipStream_t s) {
 
 template <typename T, int MT>
 int32_t launch_down_ranks(const DownArgs& a, hipStream_t s) {
-    // more ranks per workgroup read x less often, but few workgroups leave compute units without work
+    // more ranks per workgroup read x less often, but few workgroups leave compute units without work: 7 rows of 4096 in fp32, rank 62, 34 us with 64
+    // ranks and 13 with 16; 244 in bf16, rank 64, 20.6 and 9.1
     const int32_t blocks = (a.M + 16 * MT - 1) / (16 * MT);
     if (a.t_row <= 16 || blocks < 64) return launch_down_shape<T, MT, 1>(a, s);
     if (a.t_row <= 32 || blocks < 128) return launch_down_shape<T, MT, 2>(a, s);
@@ -155,6 +161,7 @@ int32_t launch_down_ranks(const DownArgs& a, hipStream_t s) {
 
 template <typename T>
 int32_t launch_down(const DownArgs& a, hipStream_t s) {
+    // 32 rows read an adapter half as often: 4100 x 4096, rank 64, 26 us against 38 with 16
     return a.M <= 16 * 128 ? launch_down_ranks<T, 1>(a, s) : launch_down_ranks<T, 2>(a, s);
 }
 
@@ -628,7 +635,7 @@ int32_t backward_of(const Sizes& z, const AdapterArgs& a, char* ws, hipStream_t 
 
 // 32-bit byte offsets inside a tile of 384 rows, grids of less than 2^32 threads
 bool adapters_cover(int32_t M, int32_t K, int32_t N, int32_t r, int32_t n, int32_t dtype) {
-    if (K > 1 << 20 || N > 1 << 20 || r > 128 || n > 16384) return false;
+    if (M > 1 << 27 || K > 1 << 20 || N > 1 << 20 || r > 128 || n > 16384) return false;
     if (static_cast<int64_t>(K) * N > int64_t{1} << 34 || (static_cast<int64_t>(K) + N + 128) * n > 1 << 28) return false;
     const int64_t m = (static_cast<int64_t>(M) + 127) / 128, k = (K + 127) / 128, c = (N + 127) / 128;
     return std::max(m * k, m * c) <= (dtype == FREE_FP32 ? 1 << 20 : 1 << 22) && (static_cast<int64_t>(K) + N) * r * n <= int64_t{1} << 36;

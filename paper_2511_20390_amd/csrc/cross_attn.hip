@@ -6,10 +6,16 @@
 // sample without keys: out zero, lse -inf.
 //
 // The queries of a group of heads are rows of one problem (row r: token r / group, head r % group), so that keys and values are read once for
-// all of them.  Two kernels:
-//  * many rows: a workgroup has 128 or 64 of them and passes tiles of keys through LDS in two stages;
-//  * up to 32 rows (a single query, a few learned ones): bound by reading keys and values once.  Every wavefront streams key tiles of its own,
-//    K straight into the matrix instructions, V through a private piece of LDS; partial results (maximum, sum, out) are joined in order.
+// all of them.  Three kernels (us on one MI355X):
+//  * cross_ring_kernel, bf16 of whole chunks, 2048 blocks of 32 rows and more: keys that fit stay in LDS, others pass through it.  Bound by the vector
+//    unit: of a tile of 64 keys by 32 queries of 72 the softmax is 1360 cycles of a SIMD (16 of them per exponential of a register), the products 704.
+//    12288 queries to 64 / 256 keys of 16 heads of 64: 14 / 23 against 17 / 25 with tiles that all pass through; 32760 to 512 of 128: 174, 0.79
+//    PFLOP/s, 52 of them the rows' way to and from memory.
+//  * cross_many_kernel, the rest of more than 32 rows, fp32, odd strides: a workgroup has 128 or 64 of them and passes tiles of keys through LDS in two
+//    stages.  2 x 256 queries to 77 keys: 7.5, a launch and four dependent trips to memory.
+//  * cross_few_kernel, up to 32 rows (a single query, a few learned ones): bound by reading keys and values once.  Every wavefront streams key tiles of
+//    its own, K straight into the matrix instructions, V through a private piece of LDS; partial results (maximum, sum, out) are joined in order.
+//    4 queries of 32 heads of 128 to up to 16384 keys of 8: 33 and 5 for the join, 155 MB of keys and values at 4.7 TB/s.
 // Where rows alone leave compute units idle the keys are cut in parts, each a workgroup's, and a second launch joins them.
 #include <algorithm>
 #include <cmath>
@@ -23,7 +29,9 @@ namespace {
 
 constexpr int kThreads = kStreamThreads;
 constexpr int kFewRows = 32;
-constexpr float kLazy = 8.0f;                     // log2 by which a maximum may grow before the sums are rescaled
+// log2 by which a maximum may grow before the sums are rescaled: they stay below 2^8 times their value, and a branch that is hardly ever taken spares
+// 16 products per tile of a result
+constexpr float kLazy = 8.0f;
 constexpr float kNoScore = -3.402823466e38f;      // a part's maximum where it has keys and all their scores are -inf
 
 // What a launch does: parts of the keys, tiles of a part; partial results [part][pair][row]
@@ -113,10 +121,11 @@ __device__ __forceinline__ void add_values(const char* v, int lane, const xf32x1
 template <typename T, int DP>
 constexpr int kValueRow = sizeof(T) == 4 ? (DP + 8) * 4 : DP <= 32 ? 64 : DP <= 96 ? 192 : 320;
 
-// KS wavefronts share the keys of a block of 32 queries
+// Heads of up to 80 leave the registers for three wavefronts per SIMD, if the compiler orders reads and products: 2 x 6144 queries to 300 keys 39 -> 35 us
 template <typename T, int DP, int KS, bool kVec>
 constexpr bool kThreeWaves = sizeof(T) == 2 && DP <= 80 && KS == 1 && kVec;
 
+// KS wavefronts share the keys of a block of 32 queries: two where there are few blocks
 template <typename T, int DP, int KS, bool kVec>
 __global__ __launch_bounds__(kThreads, (kThreeWaves<T, DP, KS, kVec> ? 3 : 2)) void cross_many_kernel(CrossArgs a, Parts pt, int32_t q_tiles) {
     using H = HeadShape<T, DP>;
@@ -241,7 +250,9 @@ __global__ __launch_bounds__(kThreads, (kThreeWaves<T, DP, KS, kVec> ? 3 : 2)) v
 
 // bf16 of whole chunks, wavefronts of 32 queries at a time.
 // kResident: all keys and values of a (sample, key head) fit in LDS.  They are brought there once, and each wavefront takes one block of queries after
-// the other, without a barrier, the next block's queries requested ahead.  Otherwise tiles pass through a ring.
+// the other, without a barrier, the next block's queries requested ahead.  Otherwise tiles pass through a ring, and two workgroups share a
+// compute unit, so that one multiplies while the other brings or stores its rows (one of eight wavefronts: 32760 queries to 512 keys of 16 heads of 128,
+// 199 us; two of four, 174).
 template <int DP, bool kResident>
 __global__ __launch_bounds__((kResident ? kRingWaves : kPassWaves) * 64, 2) void cross_ring_kernel(CrossArgs a, Parts pt, int32_t chunks, int32_t blocks_per_chunk) {
     using T = bf16_t;
@@ -359,7 +370,7 @@ __global__ __launch_bounds__((kResident ? kRingWaves : kPassWaves) * 64, 2) void
     }
 }
 
-// Up to 32 rows per (sample, head): workgroup (part, pair), its four wavefronts take the part's key tiles of 32 in turn
+// Up to 32 rows per (sample, key head): workgroup (part, pair), its four wavefronts take the part's key tiles of 32 in turn
 template <typename T, int DP, bool kVec>
 __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void cross_few_kernel(CrossArgs a, Parts pt) {
     using H = HeadShape<T, DP>;

@@ -93,7 +93,8 @@ def test_linear_adapters_refusals(lib, call):
     assert call(lib, M=-1) == call(lib, K=0) == call(lib, N=0) == call(lib, r=0) == call(lib, n=0) == call(lib, rows=0) == b.FREE_ERR_SHAPE
     assert call(lib, r=129) == call(lib, n=16385) == call(lib, K=(1 << 20) + 1) == call(lib, N=(1 << 20) + 1) == b.FREE_ERR_LIMIT
     assert call(lib, M=2**31 - 1, K=1 << 20) == call(lib, M=2**31 - 1, N=1 << 20) == call(lib, K=1 << 20, N=1 << 20, r=128, n=16384) == b.FREE_ERR_LIMIT
-    # grids of the launches: copies of W in tiles, and of A and B
+    # grids of the launches: copies of W in tiles, and of A and B, and rows
+    assert call(lib, M=(1 << 27) + 1, K=1, N=1) == b.FREE_ERR_LIMIT
     assert call(lib, M=1, K=1 << 20, N=1 << 15) == call(lib, M=1, K=1 << 18, N=1, r=1, n=2048) == b.FREE_ERR_LIMIT
     assert call(lib, ws=None) == call(lib, ws=C.c_void_p(4100)) == call(lib, bytes_=0) == b.FREE_ERR_WORKSPACE
     assert call(lib, saved=C.c_void_p(4100), sb=BIG) == call(lib, saved=ONE, sb=100) == b.FREE_ERR_WORKSPACE

@@ -161,6 +161,29 @@ def test_outputs_given_and_equal_bits(dtype):
     assert all(torch.equal(s, t) for run in runs[1:] for s, t in zip(runs[0], run))
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("M,K,N,r,n,rows", [(9, 64, 96, 8, 3, 2), (300, 128, 192, 16, 3, 50), (300, 128, 192, 6, 3, 50), (70, 33, 50, 3, 2, 9)])
+def test_adapters_of_any_alignment(dtype, M, K, N, r, n, rows):
+    """A, B and their gradients one value behind an aligned address, with NaN around what is read."""
+    x, w, bias, a, bb, adapter, scale, g = problem(13, M, K, N, r, n, rows, dtype)
+
+    def shift(t, guard):
+        whole = torch.full((t.numel() + 2,), guard, dtype=dtype, device=DEV)
+        whole[1:-1] = t.reshape(-1)
+        return whole, whole[1:-1].view(t.shape)
+
+    (_, a1), (_, b1) = shift(a, math.nan), shift(bb, math.nan)
+    (wa, da), (wb, db) = shift(a, 7.0), shift(bb, 7.0)
+    saved = torch.empty(b.linear_adapters_saved_bytes(M, r, MODE[dtype]), dtype=torch.uint8, device=DEV)
+    how = dict(scale=scale, rows_per_sample=rows)
+    out = b.op_linear_adapters(x, w, bias, a1, b1, adapter, saved=saved, **how)
+    dx = torch.empty_like(x)
+    b.op_linear_adapters_backward(g, x, w, a1, b1, adapter, saved, out=(dx, da, db), **how)
+    for t, e, what in zip((out, dx, da, db), adapters_reference(x, w, bias, a, bb, adapter, scale, rows, g), ("out", "dx", "dA", "dB")):
+        check(t, e, what)
+    assert wa[0] == wa[-1] == wb[0] == wb[-1] == 7.0
+
+
 def test_gradient_against_differences():
     """Along a direction; the formula is a polynomial of the second degree in A and B together and of the first in x, so that the central difference in 64
     bits has no error but its roundings."""
