@@ -12,7 +12,7 @@
 // delta from out 1.86 / 1.58 / 1.52 at 16 / 64 / 256 keys, so 1.42 / 1.43 / 1.44 (1.41 is dS's rounding and the result's); the second pass costs 32 -> 37 us
 // at 8 x 1024 queries to 256 keys of 16 heads of 72.
 // What bounds them: bf16 dk and dv the reads of tiles from LDS, 22 KB for 704 cycles of products of a block of 32 by 32 of 72 (8 x 1024 queries to 256 keys
-// of 16 heads: 35 us; 32760 to 512 of 128: 371, 0.74 PFLOP/s); dq a third its rows' way to and from memory (37 and 345 us there), the rest the same
+// of 16 heads: 35 us; 32760 to 512 of 128: 367, 0.75 PFLOP/s); dq a third its rows' way to and from memory (37 and 345 us there), the rest the same
 // reads.  fp32 the matrix instructions, an eighth as fast (3 x 333 to 141 of 6 heads of 64: 25 and 38).
 // Where a launch would have few workgroups the streamed axis is cut in parts, whose fp32 results a second launch adds in order: no
 // atomics, equal inputs give equal bits.
@@ -108,6 +108,17 @@ __device__ __forceinline__ void dq_block(const char* tile_k, const char* tile_v,
     column_products<T, DP, (DP <= 96)>(tile_k, row0, lane, ck, st, dq);
 }
 
+// of the instructions since the last fence: N times a product, then `valu` and `trans` others
+template <int N, int valu, int trans>
+__device__ __forceinline__ void between_products() {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        if (valu > 0) __builtin_amdgcn_sched_group_barrier(0x002, valu, 0);
+        if (trans > 0) __builtin_amdgcn_sched_group_barrier(0x400, trans, 0);
+    }
+}
+
 // dk, dv += over one block of 32 rows, whose -lse / scale and -delta are at `lse` and `delta`: the sums of scores begin with them
 template <typename T, int DP>
 __device__ __forceinline__ void dkv_block(const char* tile_q, const char* tile_g, int row0, int lane, const float* lse, const float* delta,
@@ -125,6 +136,48 @@ __device__ __forceinline__ void dkv_block(const char* tile_q, const char* tile_g
             st[4 * e4 + i] = l[i];
             dp[4 * e4 + i] = d[i];
         }
+    }
+    if constexpr (sizeof(T) == 2) {
+        // A wavefront's matrix instructions run on while it issues others: the exponentials stand between the products of the second tensor, and what is
+        // left of dS between those of dv.
+        constexpr int KSTEPS = HeadShape<T, DP>::KSTEPS, G = kRowGroup<T, DP>, kGroups = (KSTEPS + G - 1) / G, DT = HeadShape<T, DP>::DT, kPer = 16 / kGroups;
+        xu32x4_t f[2][G];
+        read_rows<T, DP>(tile_q, row0, lane, 0, f[0]);
+#pragma unroll
+        for (int i = 0; i < 2 * kGroups; ++i) {
+            const int first = i % kGroups * G;
+            if (i + 1 < 2 * kGroups) read_rows<T, DP>(i + 1 < kGroups ? tile_q : tile_g, row0, lane, (i + 1) % kGroups * G, f[(i + 1) & 1]);
+            else cg.read(tile_g, row0, lane, 0);
+            fence();
+#pragma unroll
+            for (int k = 0; k < G; ++k)
+                if (first + k < KSTEPS) {
+                    if (i < kGroups) chunk_product<T>(f[i & 1][k], kf[first + k], st);
+                    else chunk_product<T>(f[i & 1][k], vf[first + k], dp);
+                }
+            if (i >= kGroups) {
+#pragma unroll
+                for (int e = (i - kGroups) * kPer; e < (i - kGroups + 1) * kPer; ++e) st[e] = __builtin_amdgcn_exp2f(st[e] * scale_log2);
+                between_products<G, (2 * kPer + G - 1) / G, (kPer + G - 1) / G>();
+            }
+        }
+        cq.read(tile_g, row0, lane, 1);
+        fence();
+        cg.multiply(st, 0, dv);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) dp[e] *= st[e];
+        between_products<DT, (16 + DT - 1) / DT, 0>();
+        cg.read(tile_q, row0, lane, 0);
+        fence();
+        cq.multiply(st, 1, dv);
+#pragma unroll
+        for (int e = 8; e < 16; ++e) dp[e] *= st[e];
+        between_products<DT, (16 + DT - 1) / DT, 0>();
+        cq.read(tile_q, row0, lane, 1);
+        fence();
+        cg.multiply(dp, 0, dk);
+        cq.multiply(dp, 1, dk);
+        return;
     }
     read_rows<T, DP>(tile_q, row0, lane, 0, fq);
     read_rows<T, DP>(tile_g, row0, lane, 0, fg);
