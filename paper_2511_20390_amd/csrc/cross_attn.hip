@@ -580,7 +580,7 @@ Plan plan_of(int32_t B, int32_t Nq, int32_t Nk, int32_t heads, int32_t kv_heads,
             p.q_tiles = (rows + 63) / 64;
         }
     }
-    const int64_t work = pairs * p.q_tiles, least = p.few ? 8 : 4, want = 2 * kUnits;      // tiles of a part; workgroups
+    const int64_t work = pairs * p.q_tiles, least = p.few ? 8 : dtype == FREE_BF16 ? 4 : 2, want = 2 * kUnits;      // tiles of a part; workgroups
     int64_t parts = 1;
     if (work < want) parts = std::max<int64_t>(1, std::min(want / std::max<int64_t>(work, 1), tiles / least));
     parts = std::min<int64_t>(parts, 64);

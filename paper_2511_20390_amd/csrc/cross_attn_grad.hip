@@ -927,6 +927,7 @@ Plan plan_of(int32_t B, int32_t Nq, int32_t Nk, int32_t heads, int32_t kv_heads,
     const int64_t key_tiles = std::max<int64_t>(1, (static_cast<int64_t>(Nk) + tile - 1) / tile), row_tiles = std::max<int64_t>(1, (rows + tile - 1) / tile);
     Plan p{};
     int64_t parts, per;
+    const int least = dtype == FREE_BF16 ? 4 : 2;        // tiles of a part: an fp32 one is 6 us of a workgroup
     const int64_t blocks = (rows + 31) / 32;
     if (ring && pairs * blocks >= kUnits * kRingWaves) {
         p.q_ring = true;
@@ -943,7 +944,7 @@ Plan plan_of(int32_t B, int32_t Nq, int32_t Nk, int32_t heads, int32_t kv_heads,
         }
     } else {
         p.q_tiles = std::max<int64_t>(1, (rows + 127) / 128);
-        cut(pairs * p.q_tiles, 2 * kUnits, key_tiles, 4, &parts, &per);
+        cut(pairs * p.q_tiles, 2 * kUnits, key_tiles, least, &parts, &per);
         p.q_parts = static_cast<int32_t>(parts);
         p.q_part_tiles = static_cast<int32_t>(per);
     }
@@ -959,7 +960,7 @@ Plan plan_of(int32_t B, int32_t Nq, int32_t Nk, int32_t heads, int32_t kv_heads,
         p.kw = dtype == FREE_FP32 && Nk <= 32 ? 1 : Nk <= 64 ? 2 : 4;
         p.k_tiles = std::max<int64_t>(1, (static_cast<int64_t>(Nk) + 32 * p.kw - 1) / (32 * p.kw));
         const int64_t steps = dtype == FREE_FP32 ? (row_tiles * p.kw + 3) / 4 : row_tiles;       // (kStepTiles)
-        cut(pairs * p.k_tiles, 2 * kUnits, steps, dtype == FREE_FP32 ? p.kw : 4, &parts, &per);
+        cut(pairs * p.k_tiles, 2 * kUnits, steps, dtype == FREE_FP32 ? std::min(p.kw, least) : least, &parts, &per);
         p.k_units = 4 / p.kw;
         p.k_parts = static_cast<int32_t>(parts * p.k_units);
     }
