@@ -927,7 +927,8 @@ Plan plan_of(int32_t B, int32_t Nq, int32_t Nk, int32_t heads, int32_t kv_heads,
     const int64_t key_tiles = std::max<int64_t>(1, (static_cast<int64_t>(Nk) + tile - 1) / tile), row_tiles = std::max<int64_t>(1, (rows + tile - 1) / tile);
     Plan p{};
     int64_t parts, per;
-    const int least = dtype == FREE_BF16 ? 4 : 2;        // tiles of a part: an fp32 one is 6 us of a workgroup
+    // Tiles of a part: fewer cost more in sums than they spare, bf16 (2 x 300 queries to 400 keys of 8 heads of 64, dq and dk, dv 25 us with 4 and 28 with 2);
+    // an fp32 tile is some 5 us of a workgroup (3 x 333 to 141 of 6 heads, dq 25, 20 + 4, 15 + 4 with 4, 2, 1; dk and dv 38, 26, 29).
     const int64_t blocks = (rows + 31) / 32;
     if (ring && pairs * blocks >= kUnits * kRingWaves) {
         p.q_ring = true;
@@ -944,7 +945,7 @@ Plan plan_of(int32_t B, int32_t Nq, int32_t Nk, int32_t heads, int32_t kv_heads,
         }
     } else {
         p.q_tiles = std::max<int64_t>(1, (rows + 127) / 128);
-        cut(pairs * p.q_tiles, 2 * kUnits, key_tiles, least, &parts, &per);
+        cut(pairs * p.q_tiles, 2 * kUnits, key_tiles, dtype == FREE_BF16 ? 4 : 1, &parts, &per);
         p.q_parts = static_cast<int32_t>(parts);
         p.q_part_tiles = static_cast<int32_t>(per);
     }
@@ -960,7 +961,7 @@ Plan plan_of(int32_t B, int32_t Nq, int32_t Nk, int32_t heads, int32_t kv_heads,
         p.kw = dtype == FREE_FP32 && Nk <= 32 ? 1 : Nk <= 64 ? 2 : 4;
         p.k_tiles = std::max<int64_t>(1, (static_cast<int64_t>(Nk) + 32 * p.kw - 1) / (32 * p.kw));
         const int64_t steps = dtype == FREE_FP32 ? (row_tiles * p.kw + 3) / 4 : row_tiles;       // (kStepTiles)
-        cut(pairs * p.k_tiles, 2 * kUnits, steps, dtype == FREE_FP32 ? std::min(p.kw, least) : least, &parts, &per);
+        cut(pairs * p.k_tiles, 2 * kUnits, steps, dtype == FREE_BF16 ? 4 : std::min(p.kw, 2), &parts, &per);
         p.k_units = 4 / p.kw;
         p.k_parts = static_cast<int32_t>(parts * p.k_units);
     }
