@@ -66,7 +66,7 @@ def test_ragged_widths(dtype, M, K, N, r, n, rows):
 
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("M,K,N,r,n,rows", [
-    (4200, 128, 192, 24, 3, 512), (6000, 256, 128, 16, 12, 60), (200, 2048, 384, 16, 2, 50), (5000, 64, 64, 64, 2, 5000), (700, 1152, 2304, 16, 4, 350),
+    (4200, 128, 192, 24, 3, 512), (6000, 256, 128, 16, 12, 60), (200, 2048, 384, 16, 2, 50), (5000, 64, 64, 64, 2, 5000), (2100, 4160, 2304, 40, 3, 700), (40, 5000, 5008, 16, 3, 7), (700, 1152, 2304, 16, 4, 350),
 ])
 def test_sums_in_parts_and_large_tiles(dtype, M, K, N, r, n, rows):
     compare(*problem(3, M, K, N, r, n, rows, dtype), rows)
