@@ -164,8 +164,10 @@ def test_outputs_given_and_equal_bits(dtype):
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("M,K,N,r,n,rows", [(9, 64, 96, 8, 3, 2), (300, 128, 192, 16, 3, 50), (300, 128, 192, 6, 3, 50), (70, 33, 50, 3, 2, 9)])
 def test_adapters_of_any_alignment(dtype, M, K, N, r, n, rows):
-    """A, B and their gradients one value behind an aligned address, with NaN around what is read."""
+    """A, B, their gradients, bias and scale one value behind an aligned address, with NaN around what is read."""
     x, w, bias, a, bb, adapter, scale, g = problem(13, M, K, N, r, n, rows, dtype)
+    behind = lambda t: torch.cat([torch.full((1,), math.nan, device=DEV), t, torch.full((1,), math.nan, device=DEV)])[1:-1]
+    bias, scale = behind(bias), behind(scale)
 
     def shift(t, guard):
         whole = torch.full((t.numel() + 2,), guard, dtype=dtype, device=DEV)
