@@ -11,9 +11,10 @@
 // the sum of a row's dS shows it to be off by (over all keys dS is zero).  In bf16, error of dq relative to that of a result computed in 64 bits and rounded: with
 // delta from out 1.86 / 1.58 / 1.52 at 16 / 64 / 256 keys, so 1.42 / 1.43 / 1.44 (1.41 is dS's rounding and the result's); the second pass costs 32 -> 37 us
 // at 8 x 1024 queries to 256 keys of 16 heads of 72.
-// What bounds them: bf16 dk and dv the reads of tiles from LDS, 22 KB for 704 cycles of products of a block of 32 by 32 of 72 (8 x 1024 queries to 256 keys
-// of 16 heads: 35 us; 32760 to 512 of 128: 367, 0.75 PFLOP/s); dq a third its rows' way to and from memory (37 and 345 us there), the rest the same
-// reads.  fp32 the matrix instructions, an eighth as fast (3 x 333 to 141 of 6 heads of 64: 25 and 38).
+// What bounds them: heads of 72, the latency of a block's chain (LDS, products, exponentials, products) with two wavefronts per SIMD, which wait 43 % of their
+// time in dk and dv and 27 in dq, the matrix pipe busy 26 and 33 % (8 x 1024 queries to 256 keys of 16 heads: 35 and 37 us).  Heads of 128, one
+// wavefront per SIMD whose vector and matrix instructions take turns, the pipe busy 35 and 28 % (32760 to 512: 367 us, 0.75 PFLOP/s, and 346, of which 170 are
+// the rows' way to and from memory).  fp32 the matrix instructions, an eighth as fast (3 x 333 to 141 of 6 heads of 64: 25 and 15).
 // Where a launch would have few workgroups the streamed axis is cut in parts, whose fp32 results a second launch adds in order: no
 // atomics, equal inputs give equal bits.
 #include <algorithm>
