@@ -22,6 +22,7 @@
 #include <type_traits>
 
 #include "cross_attn.h"
+#include "wave_rows.h"
 
 namespace freemi {
 
@@ -271,7 +272,7 @@ __global__ __launch_bounds__((kResident ? kRingWaves : kPassWaves) * 64, 2) void
     const uint32_t lds_base = lds_address(lds);
     const auto request = [&](int t, int slot) { keys.request(t, lds_base + slot * Ring::kTileBytes, wave); };
     const auto load_queries = [&](int block, xu32x4_t (&f)[KSTEPS]) {
-        const int r = min(block * 32 + l32, rows - 1), token = over_group(r, group), head = kvh * group + r - token * group;
+        const int r = min(lane_row(block, l32), rows - 1), token = over_group(r, group), head = kvh * group + r - token * group;
         const T* const p = static_cast<const T*>(a.q) + (static_cast<int64_t>(b) * a.Nq + token) * a.q_stride + static_cast<int64_t>(head) * a.dh;
 #pragma unroll
         for (int ks = 0; ks < KSTEPS; ++ks) f[ks] = row_chunk<T, true>(p, 2 * ks + g, a.dh);
@@ -317,7 +318,7 @@ __global__ __launch_bounds__((kResident ? kRingWaves : kPassWaves) * 64, 2) void
     };
     const auto finish = [&](int block, bool any) {
         l = add_lane_xor<32>(l);
-        const int r = block * 32 + l32;
+        const int r = lane_row(block, l32);
         write_row<T, true, DT>(a, pt, part, pair, b, kvh, r, g, m_ref * scale_log2, l, any, o, r < rows);
     };
 
@@ -340,8 +341,7 @@ __global__ __launch_bounds__((kResident ? kRingWaves : kPassWaves) * 64, 2) void
             for (int ks = 0; ks < KSTEPS; ++ks) qf[ks] = next[ks];
         }
     } else {
-        const int block = min(chunk * NW + wave, blocks - 1);
-        const bool mine = chunk * NW + wave < blocks;
+        const int block = wave_block(chunk, NW, wave);       // (past the last one: it takes part in the loads, and has no row)
 #pragma unroll
         for (int s = 0; s < kSlots - 1; ++s)
             if (t0 + s < t1) request(t0 + s, s);
@@ -366,7 +366,7 @@ __global__ __launch_bounds__((kResident ? kRingWaves : kPassWaves) * 64, 2) void
             free_slot = slot;
             slot = slot + 1 == kSlots ? 0 : slot + 1;
         }
-        finish(mine ? block : rows, any);
+        finish(block, any);
     }
 }
 
