@@ -508,15 +508,19 @@ __global__ __launch_bounds__(kThreads) void cross_join_kernel(CrossArgs a, Parts
     float m = max_lane_xor32(mp);
 #pragma unroll
     for (int x = 16; x > 0; x >>= 1) m = fmaxf(m, __shfl_xor(m, x, 64));
-    const float w = mp == -INFINITY ? 0.f : mp == m ? 1.0f : __builtin_amdgcn_exp2f(mp - m);
-    const float l = wave_sum(w == 0.f ? 0.f : w * lp);
+    // (parts without keys are left out; one with keys counts however small its weight is: its sums may be NaN)
+    const bool keyed = mp != -INFINITY;
+    const uint64_t keyed_parts = __ballot(keyed);
+    const float w = !keyed ? 0.f : mp == m ? 1.0f : __builtin_amdgcn_exp2f(mp - m);
+    const float l = wave_sum(keyed ? w * lp : 0.f);
     float o[2] = {0.f, 0.f};
     for (int p = first; p < pt.parts; p += WPR) {
+        if (!(keyed_parts >> p & 1)) continue;
         const float wp = __shfl(w, p, 64);
         const float* const from = pt.o + (p * all + at) * a.dh;
 #pragma unroll
         for (int k = 0; k < 2; ++k)
-            if (lane + 64 * k < a.dh && wp != 0.f) o[k] = fmaf(wp, from[lane + 64 * k], o[k]);
+            if (lane + 64 * k < a.dh) o[k] = fmaf(wp, from[lane + 64 * k], o[k]);
     }
     if constexpr (WPR > 1) {
 #pragma unroll

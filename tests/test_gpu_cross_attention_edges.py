@@ -41,3 +41,58 @@ def test_rows_past_26_bits(Nq, heads):
         ref = cross_reference(q[at], k, v, 1, heads, 1, dh, dh ** -0.5, keys)
         check(out[at], ref[0], f"out of rows from {first} on")
         check(lse[:, :, at], ref[1], f"lse of rows from {first} on")
+
+
+@pytest.mark.parametrize("B,Nq,Nk,heads,kv,dh,dtype", [
+    (1, 1, 4096, 4, 2, 64, torch.bfloat16), (2, 3, 3000, 4, 4, 72, torch.bfloat16), (1, 150, 2050, 2, 2, 72, torch.bfloat16), (2, 40, 3000, 2, 2, 33, torch.bfloat16),
+    (1, 1, 3000, 4, 2, 64, torch.float32), (1, 150, 2050, 2, 2, 72, torch.float32), (2, 9, 100, 4, 2, 64, torch.bfloat16), (2, 2100, 130, 16, 16, 72, torch.bfloat16),
+    (2, 1100, 700, 32, 32, 64, torch.bfloat16),
+])
+@pytest.mark.parametrize("what", ["key alone", "key beside a small score", "value of a small weight"])
+def test_nan_in_a_key_that_counts(B, Nq, Nk, heads, kv, dh, dtype, what):
+    """NaN in one key (or value) of the last sample's second key head: everything that depends on it is NaN, however the keys are cut and whatever the
+    weight of the part that it is in, and nothing else."""
+    gen = generator(2)
+    q, g = normal(gen, (B * Nq, heads * dh), 1.0, dtype).abs() + 1, normal(gen, (B * Nq, heads * dh), 1.0, dtype)
+    k, v = normal(gen, (B * Nk, kv * dh), 1.0, dtype), normal(gen, (B * Nk, kv * dh), 1.0, dtype)
+    group = heads // kv
+    mask = torch.zeros(B, Nk, dtype=torch.uint8, device=DEV)
+    mask[:, :Nk // 4] = 1
+    # of the other keys, in parts of their own where there are parts: one or two
+    at = Nk * 4 // 5 // 64 * 64
+    mask[:, at] = 1
+    row = (B - 1) * Nk + at
+    head = slice(dh, 2 * dh)
+    if what == "key alone":
+        k[row, dh + 3] = math.nan
+    else:
+        k[row, head] = -80.0             # a score of -80 sqrt(dh) and less, 300 binary orders under the others where dh is 33 and more
+        if what == "value of a small weight":
+            v[row, dh + 3] = math.nan
+        else:
+            mask[:, at + 1] = 1
+            k[row + 1, dh + 3] = math.nan
+    keys = keys_that_count(B, Nk, None, mask, DEV)
+    lse = torch.empty(B, heads, Nq, device=DEV)
+    how = dict(B=B, heads=heads, dh=dh, kv_heads=kv, key_mask=mask)
+    out = b.op_cross_attention(q, k, v, lse=lse, **how)
+    ref = cross_reference(q, k, v, B, heads, kv, dh, dh ** -0.5, keys, g)
+    assert ref[0][0].isnan().any()
+    check(out, ref[0], "out")
+    check(lse, ref[1], "lse")
+    dq, dk, dv = b.op_cross_attention_backward(g, q, k, v, out, lse, **how)
+    hit = torch.zeros_like(q, dtype=torch.bool)
+    hit[(B - 1) * Nq:, group * dh:2 * group * dh] = True
+    assert dq[hit].isnan().all()
+    check(torch.where(hit, ref[2][0].to(dtype), dq), ref[2], "dq")
+    theirs = torch.zeros_like(k, dtype=torch.bool)
+    theirs[(B - 1) * Nk:, head] = True
+    hit = theirs & keys.reshape(-1, 1)
+    unkeyed = ~keys.reshape(-1)
+    for t, r, name in ((dk, ref[3], "dk"), (dv, ref[4], "dv")):
+        assert not t[unkeyed].any(), name
+        if name == "dv" and what == "value of a small weight":
+            check(t, r, name)            # (depends on keys and queries alone)
+            continue
+        assert t[hit].isnan().all(), name
+        check(torch.where(theirs, r[0].to(dtype), t), r, name)
