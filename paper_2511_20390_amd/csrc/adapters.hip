@@ -55,8 +55,8 @@ __global__ __launch_bounds__(kDownWaves * 64) void adapter_down_kernel(DownArgs 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     // blocks of rows next to each other on one XCD: its L2 has the adapters of few requests to hold
     const int m0 = xcd_tile(blockIdx.x, gridDim.x) * 16 * MT, rank0 = blockIdx.z * 16 * RT, quad = lane >> 4, r16 = lane & 15;
-    if (a.zeros && blockIdx.y == 0 && blockIdx.z == 0)
-        for (int i = blockIdx.x * kDownWaves * 64 + threadIdx.x; i < a.zero_n; i += gridDim.x * kDownWaves * 64) a.zeros[i] = 0.f;
+    if (a.zeros && blockIdx.y == 0 && blockIdx.z == 0)       // (a grid of 2^22 workgroups has 2^31 threads)
+        for (int64_t i = static_cast<int64_t>(blockIdx.x) * kDownWaves * 64 + threadIdx.x; i < a.zero_n; i += static_cast<int64_t>(gridDim.x) * kDownWaves * 64) a.zeros[i] = 0.f;
     int of = -1;                                 // lane: row m0 + lane's adapter
     if (lane < 16 * MT && m0 + lane < a.M) {
         const int id = a.adapter[(m0 + lane) / a.rows_per_sample];
