@@ -200,22 +200,32 @@ __device__ __forceinline__ uint64_t keys_below(int left) { return left >= 64 ? ~
 //   rows of 10: every second place, eight rows of them -> c ^ (row / 8 % 2)      rows of 8 and 16: likewise, and the four rows of a
 //   transposing read, which start at the same bank, on different groups of four places
 // fp32: rows of an odd number of chunks.
+constexpr int kOverRead = 128;                   // bytes behind a tile that its last rows' columns may reach (they are read, and dropped)
+
 template <typename T, int DP>
 struct Tile {
     using H = HeadShape<T, DP>;
     static constexpr int kRows = sizeof(T) == 2 ? 64 : 32;
     static constexpr int CHP = sizeof(T) == 2 ? H::CH : H::CH | 1;                // chunks from row to row
     static constexpr int kPitch = CHP * 16;
-    static constexpr int kBytes = kRows * kPitch + 128;  // (columns past a row's end are read, and dropped)
+    static constexpr int kBytes = kRows * kPitch + kOverRead;
     static_assert(sizeof(T) == 4 || CHP == 4 || CHP == 8 || CHP == 10 || CHP == 12 || CHP == 16, "a place for every chunk");
-    static __device__ __forceinline__ int turn(int row) {
+    static __host__ __device__ __forceinline__ constexpr int turn(int row) {
         if constexpr (sizeof(T) == 4) return 0;
         else if constexpr (CHP == 16) return (row & 3) << 2 | (row >> 2 & 3);
         else if constexpr (CHP == 8) return (row >> 1 & 1) << 2 | (row >> 2 & 3);
         else if constexpr (CHP == 10) return row >> 3 & 1;
         else return row >> 2 & 3;
     }
-    static __device__ __forceinline__ int at(int row, int c) { return row * kPitch + ((c ^ turn(row)) << 4); }
+    static __host__ __device__ __forceinline__ constexpr int at(int row, int c) { return row * kPitch + ((c ^ turn(row)) << 4); }
+    // behind the last byte that reading the tile's columns touches: all 32 of the last block of them
+    static constexpr int columns_end() {
+        if (sizeof(T) == 4) return (kRows - 1) * kPitch + H::DT * 128;
+        int end = 0;
+        for (int row = 0; row < kRows; ++row)
+            for (int c = 0; c < 4 * H::DT; ++c) end = std::max(end, at(row, c) + 16);
+        return end;
+    }
 };
 
 constexpr int kStreamThreads = 256, kNowhere = 0x7fffffff;       // a byte offset behind every buffer: reads as zero
@@ -405,7 +415,7 @@ constexpr int kLdsBytes = 160 * 1024 - 256;
 // (with two, one is under way while one is multiplied).
 constexpr int kPassWaves = 4;
 template <int DP>
-constexpr int kPassTiles = kLdsBytes / 2 / PairRing<DP, kPassWaves>::kTileBytes >= 3 ? 3 : 2;
+constexpr int kPassTiles = (kLdsBytes / 2 - kOverRead) / PairRing<DP, kPassWaves>::kTileBytes >= 3 ? 3 : 2;
 
 // 64 floats, one per lane, to LDS (dma_1k's comment)
 __device__ __forceinline__ void dma_floats(uint32_t lds_addr, int voff, u32x4_t rsrc) {
@@ -484,7 +494,15 @@ __device__ __forceinline__ bool bring_keys(const RingKeys<DP>& keys, char* lds, 
 }
 
 template <int DP>
-constexpr int ring_tiles() { return (kLdsBytes - 128) / PairRing<DP, kRingWaves>::kTileBytes; }
+constexpr int ring_tiles() { return (kLdsBytes - kOverRead) / PairRing<DP, kRingWaves>::kTileBytes; }
+
+// LDS of a kernel with `tiles` tiles of a PairRing, whose last one ends with the second tensor's rows
+template <int DP, int NW>
+constexpr size_t ring_bytes(int tiles) {
+    using Ring = PairRing<DP, NW>;
+    static_assert(Ring::kSecond + Tile<bf16_t, DP>::columns_end() <= Ring::kTileBytes + kOverRead, "columns of the last tile's second tensor");
+    return static_cast<size_t>(tiles) * Ring::kTileBytes + kOverRead;
+}
 inline int tiles_that_fit(int32_t dh) {
     return std::min(kMaxTiles, dh <= 32 ? ring_tiles<32>() : dh <= 64 ? ring_tiles<64>() : dh <= 80 ? ring_tiles<80>() : dh <= 96 ? ring_tiles<96>() : ring_tiles<128>());
 }

@@ -608,7 +608,7 @@ int32_t launch_shape(const CrossArgs& a, const Plan& p, const Parts& pt, hipStre
     }
     if constexpr (sizeof(T) == 2 && kVec) {
         if (p.ring) {
-            const size_t lds = p.resident ? static_cast<size_t>(p.tiles) * PairRing<DP, kRingWaves>::kTileBytes : kPassTiles<DP> * PairRing<DP, kPassWaves>::kTileBytes;
+            const size_t lds = p.resident ? ring_bytes<DP, kRingWaves>(p.tiles) : ring_bytes<DP, kPassWaves>(kPassTiles<DP>);
             const auto launch = [&](auto resident) {
                 auto kern = cross_ring_kernel<DP, decltype(resident)::value>;
                 static LdsLimit limit;

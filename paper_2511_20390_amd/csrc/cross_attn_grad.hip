@@ -1019,13 +1019,13 @@ int32_t launch_dq(const CrossArgs& a, const Plan& p, const RowStats& stats, cons
             if (p.q_ring) {
                 auto kern = cross_dq_wide_kernel<DP>;
                 static LdsLimit limit;
-                constexpr size_t lds = kRing * PairRing<DP, kWideWaves>::kTileBytes;
+                constexpr size_t lds = ring_bytes<DP, kWideWaves>(kRing);
                 if (!allow(kern, limit, lds)) return FREE_ERR_HIP;
                 hipLaunchKernelGGL(kern, grid, dim3(kWideWaves * 64), lds, s, a, stats);
                 return launch_ok() ? FREE_OK : FREE_ERR_HIP;
             }
         } else if (p.q_ring) {
-            const size_t lds = p.resident ? static_cast<size_t>(p.q_part_tiles) * PairRing<DP, kRingWaves>::kTileBytes : kPassTiles<DP> * PairRing<DP, kPassWaves>::kTileBytes;
+            const size_t lds = p.resident ? ring_bytes<DP, kRingWaves>(p.q_part_tiles) : ring_bytes<DP, kPassWaves>(kPassTiles<DP>);
             const auto launch = [&](auto resident) {
                 auto kern = cross_dq_ring_kernel<DP, decltype(resident)::value>;
                 static LdsLimit limit;
@@ -1050,7 +1050,7 @@ int32_t launch_dkv(const CrossArgs& a, const Plan& p, const RowStats& stats, con
     if constexpr (sizeof(T) == 2 && kVec) {
         if (p.k_ring) {
             constexpr int NW = kKeyWaves<DP>;
-            const size_t lds = kRing * (PairRing<DP, NW>::kTileBytes + NW * 256) + 128;
+            const size_t lds = ring_bytes<DP, NW>(kRing) + kRing * NW * 256;
             auto kern = cross_dkv_ring_kernel<DP, NW, 4>;
             static LdsLimit limit;
             if (!allow(kern, limit, lds)) return FREE_ERR_HIP;
