@@ -24,9 +24,9 @@ int32_t check_cross_sizes(int32_t B, int32_t Nq, int32_t Nk, int32_t heads, int3
     if (B < 0 || Nq < 0 || Nk < 0 || heads < 1 || kv_heads < 1 || heads % kv_heads != 0 || dh < 1) return FREE_ERR_SHAPE;
     const int64_t pairs = static_cast<int64_t>(B) * kv_heads, rows = static_cast<int64_t>(Nq) * (heads / kv_heads);
     if (dh > 128 || static_cast<int64_t>(heads) * dh > kMaxStride || rows > 0x7fffffff - 128 || Nk > 0x7fffffff - 128) return FREE_ERR_LIMIT;
-    // (workgroups of 512 threads, 2^32 threads to a launch)
+    // (workgroups of 512 threads, 2^32 threads to a launch; blocks alone are up to 2^26)
     const int64_t most = std::max({rows, static_cast<int64_t>(Nk), int64_t{1}});
-    return pairs * ((most + 31) / 32) >= 1 << 23 ? FREE_ERR_LIMIT : FREE_OK;
+    return pairs >= 1 << 23 || pairs * ((most + 31) / 32) >= 1 << 23 ? FREE_ERR_LIMIT : FREE_OK;
 }
 
 bool element_aligned(const void* p, int32_t dtype) { return aligned(p, dtype == FREE_BF16 ? 2 : 4); }
