@@ -96,3 +96,47 @@ def test_nan_in_a_key_that_counts(B, Nq, Nk, heads, kv, dh, dtype, what):
             continue
         assert t[hit].isnan().all(), name
         check(torch.where(theirs, r[0].to(dtype), t), r, name)
+
+
+def ragged(seed, lens, Nq, Nk, heads, kv, dh, dtype, masked):
+    """Both passes on samples whose keys end anywhere, NaN in those that do not count."""
+    B, gen = len(lens), generator(seed)
+    q, g = normal(gen, (B * Nq, heads * dh), 1.5, dtype), normal(gen, (B * Nq, heads * dh), 1.0, dtype)
+    k, v = normal(gen, (B * Nk, kv * dh), 1.0, dtype), normal(gen, (B * Nk, kv * dh), 1.0, dtype)
+    key_len = torch.tensor(lens, device=DEV, dtype=torch.int32)
+    mask = (torch.rand(B, Nk, device=DEV, generator=gen) < 0.6).to(torch.uint8) if masked else None
+    keys = keys_that_count(B, Nk, key_len, mask, DEV)
+    ref = cross_reference(q, k, v, B, heads, kv, dh, dh ** -0.5, keys, g)
+    for t in (k, v):
+        t[~keys.reshape(-1)] = math.nan
+    lse = torch.full((B, heads, Nq), 7.0, device=DEV)
+    how = dict(B=B, heads=heads, dh=dh, kv_heads=kv, key_len=key_len, key_mask=mask)
+    out = b.op_cross_attention(q, k, v, lse=lse, **how)
+    got = (out, lse, *b.op_cross_attention_backward(g, q, k, v, out, lse, **how))
+    for t, r, what in zip(got, ref, ("out", "lse", "dq", "dk", "dv")):
+        check(t, r, what)
+
+
+@pytest.mark.parametrize("masked", [False, True])
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("Nq,Nk,heads,kv,dh,lens", [
+    (1, 3000, 4, 2, 64, [3000, 0, 1, 287, 288, 289, 1500, 2999]),            # few rows: parts of 288 keys
+    (3, 3000, 8, 2, 72, [3000, 0, 1, 31, 33, 288, 577, 2999]),
+    (5, 1100, 3, 3, 33, [1100, 0, 1, 256, 512, 513, 7]),
+    (150, 2050, 4, 2, 72, [2050, 0, 1, 100, 255, 256, 257, 320, 321, 1999]), # many rows: parts of 320 keys, delta by one pass and by two
+    (150, 2050, 2, 2, 128, [2050, 0, 1, 64, 256, 257]),
+    (40, 700, 6, 2, 40, [700, 1, 100, 256, 257, 640]),
+])
+def test_lengths_that_end_in_any_part(Nq, Nk, heads, kv, dh, lens, dtype, masked):
+    ragged(3, lens, Nq, Nk, heads, kv, dh, dtype, masked)
+
+
+@pytest.mark.parametrize("masked", [False, True])
+@pytest.mark.parametrize("Nq,Nk,heads,kv,dh", [
+    (1500, 700, 16, 16, 72), (1500, 700, 16, 16, 96), (1500, 700, 16, 16, 128), (1500, 900, 16, 16, 64),      # keys pass through LDS
+    (1500, 250, 16, 16, 72), (1500, 200, 16, 16, 40),                                                         # keys stay in it
+    (500, 700, 48, 16, 72), (500, 130, 48, 16, 64), (250, 700, 96, 16, 128), (250, 300, 112, 16, 96),         # groups that no tile of rows is a multiple of
+])
+@pytest.mark.parametrize("lens", [[1.0, 100, 256], [257, 0, 1], [1.0, 63, 64]])
+def test_many_queries_of_ragged_samples(Nq, Nk, heads, kv, dh, lens, masked):
+    ragged(4, [int(n * Nk) if isinstance(n, float) else min(n, Nk) for n in lens], Nq, Nk, heads, kv, dh, torch.bfloat16, masked)
