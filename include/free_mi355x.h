@@ -594,8 +594,9 @@ int32_t free_op_gated_ffn_backward(const void* dout, const void* x, const void* 
  * Scores, probabilities' sums and results are summed in fp32; probabilities are rounded to dtype as operands of the second product.
  * The gradient, of the same inputs, out and lse: dq like q, dk and dv like k and v (each with its distance from row to row), written, not
  * added to, zero for keys that do not count; probabilities and the scores' gradient are rounded to dtype as operands of the products.
- * How sums are cut depends on the sizes alone.  2^-64 <= scale <= 2^64 (FREE_ERR_RANGE); 1 <= dh <= 128, strides up to 2^22 values, Nq heads / kv_heads below 2^31 - 128,
- * B kv_heads times the blocks of 32 query rows (or keys) of a sample and key head below 2^23 (FREE_ERR_LIMIT). */
+ * How sums are cut depends on the sizes and on whether all rows are 16-byte aligned pieces (see above), so equal values at another alignment may
+ * differ in their last bits, as may a query row beside other rows.  2^-64 <= scale <= 2^64 (FREE_ERR_RANGE); 1 <= dh <= 128, heads dh and strides up to
+ * 2^22 values, B kv_heads times the blocks of 32 query rows (or keys) of a sample and key head below 2^23 (FREE_ERR_LIMIT). */
 size_t free_cross_attention_workspace_bytes(int32_t B, int32_t Nq, int32_t Nk, int32_t heads, int32_t kv_heads, int32_t dh, int32_t dtype,
                                             int32_t backward);
 int32_t free_op_cross_attention(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
@@ -614,9 +615,10 @@ int32_t free_op_cross_attention_backward(const void* dout, int64_t dout_stride, 
  *   out = x W^T + bias + t B_a^T,   t = scale_a x A_a^T
  * x [M, K], W [N, K], A [n, r, K], B [n, N, r], out [M, N], all of type dtype, contiguous; x, W, out (dout, dx) 16-byte aligned; bias fp32 [N] or
  * NULL; scale fp32 [n] or NULL (ones); adapter int32 [samples], in any order.  Adapters of lower rank are filled up with zeros.  Sums are fp32,
- * t is rounded to dtype as operand of the second product.  Any K and N; those that are not multiples of 8 (bf16) or 64 (fp32) go through
- * padded copies in the workspace, but for forward calls of at most 32 rows.  r <= 128, n <= 16384, M K and M N at most 2^36 (bf16) or 2^34 (fp32),
- * (K + N) r n at most 2^36, (K + N + 128) n at most 2^28, K N at most 2^34, K and N at most 2^20, M at most 2^27 (FREE_ERR_LIMIT).
+ * t is rounded to dtype as operand of the second product.  Any K and N.  A K that is not a multiple of 64 (bf16) or 32 (fp32) costs a padded copy of x and
+ * W per forward call of more than 32 rows; the gradient copies W, A and B the other way round in every call, dout where N is not such a multiple, and x where
+ * K is not one of 8 (bf16) or 4 (fp32).  r <= 128, n <= 16384, tiles of 128 x 128 of M x K and of M x N at most 2^22 (bf16) or 2^20 (fp32), (K + N) r n
+ * at most 2^36, (K + N + 128) n at most 2^28, K N at most 2^34, K and N at most 2^20, M at most 2^27 (FREE_ERR_LIMIT).
  * saved (NULL: none): free_linear_adapters_saved_bytes bytes, 256-byte aligned, that keep t for the gradient.
  * The gradient, W, bias and scale being fixed:
  *   dx = dout W + u A_a,   u = scale_a dout B_a,   dA_a = sum over the adapter's rows of u^T x,   dB_a = sum of dout^T t

@@ -8,12 +8,13 @@
 //    operands of, like the hidden values of the gated block.  Bound by reading x and, for each block of rows, its adapter again from the L2: 12288 x 1152,
 //    rank 16, 8.6 us (3.3 TB/s); 4100 x 4096, rank 64, 26.
 //  * out and dx: the kernels and tiles of the linear layers, whose sums begin with the adapters' (bf16, adapter_term.h: 12288 rows of 1152 to 1152, 34 us; 8192
-//    of 1152 to 4608, 86 and back 95, 1.01 and 0.92 PFLOP/s; what bounds them is in gemm_pipe.hip), or a second pass over the result (fp32, where the
-//    product takes ten times as long: 1000 rows of 384 to 1536, 16 and 9 us); few rows ffn_rows.hip (8 rows of 4096 to 4096: 7.6, 4.4 TB/s).  The tiles
+//    of 1152 to 4608, 86 and back 95, 1.01 and 0.92 PFLOP/s; what bounds them is in gemm_pipe.hip), or a second pass over the result (fp32: 1000 rows of
+//    384 to 1536, 17 and 8.4 us); few rows ffn_rows.hip (8 rows of 4096 to 4096: 7.6, 4.4 TB/s).  The tiles
 //    of the gated block, which read W by its columns as well, took 489 against 345 for both passes of 4100 rows of 4096 to 4096.
 //  * dA and dB: 128 columns of x or dout by all ranks per workgroup, over the rows of one adapter, in parts that a second launch adds in
-//    order.  Rows of other adapters are not read.  Bound by reading x and dout once: 8192 rows of 1152 and 4608, rank 32, 27 and 5.6 us for the parts
-//    (3.5 TB/s), 4100 of 4096 and 4096, rank 64, 34 and 10.
+//    order.  Rows of other adapters are not read, but every (columns, adapter, part) stores its part, zeros where no row is the adapter's.  8192 rows of
+//    1152 and 4608, rank 32, 3 adapters: 27 us, the reading of x and dout at 3.5 TB/s, and 5.6 for the parts; 4100 of 4096 and 4096, rank 64, 6 adapters: 34
+//    and 10, 67 MB read at 2 TB/s beside 38 MB of parts.
 // For the gradient W, B and A are needed the other way round ([K][N], [rank][N], [K][rank]): copies of that layout go into the workspace, filled
 // up with zeros to whole slices (4096 x 4096 of 6 adapters of rank 64: 17 us).
 #include <algorithm>
@@ -152,7 +153,7 @@ int32_t launch_down_shape(const DownArgs& a, hipStream_t s) {
 template <typename T, int MT>
 int32_t launch_down_ranks(const DownArgs& a, hipStream_t s) {
     // more ranks per workgroup read x less often, but few workgroups leave compute units without work: 7 rows of 4096 in fp32, rank 62, 34 us with 64
-    // ranks and 13 with 16; 244 in bf16, rank 64, 20.6 and 9.1
+    // ranks and 13 with 16; 244 in bf16, rank 64, 20.6 and 9.1 (1 and 16 blocks; from where on 32 and 64 ranks pay is not measured closer)
     const int32_t blocks = (a.M + 16 * MT - 1) / (16 * MT);
     if (a.t_row <= 16 || blocks < 64) return launch_down_shape<T, MT, 1>(a, s);
     if (a.t_row <= 32 || blocks < 128) return launch_down_shape<T, MT, 2>(a, s);

@@ -556,7 +556,7 @@ struct KeyStream {
 
 }  // namespace
 
-// cross_attn.hip, cross_attn_grad.hip; arguments checked in cross_abi.hip
+// cross_attn.hip, cross_attn_grad.hip; arguments checked in cond_abi.hip
 size_t cross_forward_bytes(int32_t B, int32_t Nq, int32_t Nk, int32_t heads, int32_t kv_heads, int32_t dh, int32_t dtype);
 size_t cross_backward_bytes(int32_t B, int32_t Nq, int32_t Nk, int32_t heads, int32_t kv_heads, int32_t dh, int32_t dtype);
 int32_t launch_cross_forward(const CrossArgs& a, int32_t dtype, void* ws, hipStream_t s);

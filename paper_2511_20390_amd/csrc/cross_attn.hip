@@ -31,7 +31,7 @@ namespace {
 constexpr int kThreads = kStreamThreads;
 constexpr int kFewRows = 32;
 // log2 by which a maximum may grow before the sums are rescaled: they stay below 2^8 times their value, and a branch that is hardly ever taken spares
-// 16 products per tile of a result
+// 16 products per tile of a result.  It is taken for a wavefront: a row's last bits may depend on the rows beside it.
 constexpr float kLazy = 8.0f;
 constexpr float kNoScore = -3.402823466e38f;      // a part's maximum where it has keys and all their scores are -inf
 
@@ -543,7 +543,7 @@ __global__ __launch_bounds__(kThreads) void cross_join_kernel(CrossArgs a, Parts
     if (a.lse && lane == 0) a.lse[(static_cast<int64_t>(b) * a.heads + head) * a.Nq + token] = m == -INFINITY ? m : (m + __builtin_log2f(l)) * kLn2;
 }
 
-// How a problem is cut; by its sizes alone (a workspace's size must not depend on the device)
+// How a problem is cut; by its sizes and by whether rows are whole aligned chunks, not by the device (a workspace is as large as either way needs)
 struct Plan {
     bool few, ring, resident;
     int ks;                                       // wavefronts that share a query block's keys (many rows)

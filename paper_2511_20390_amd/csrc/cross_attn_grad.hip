@@ -8,7 +8,7 @@
 // The score tile's rows are the streamed tensor's rows and its columns the workgroup's own (cross_attn.h), in both.
 // delta: out is rounded to its type, and dS is a difference that is small where few keys share the weight.  A sample of up to 256 keys (kTwiceKeys), and
 // one whose keys stay in LDS, is passed over twice, first for sum P dP in fp32; of more keys delta is sum dout out, and the keys' gradient is given what
-// the sum of a row's dS shows it to be off by (over all keys dS is zero).  In bf16, error of dq relative to that of a result computed in 64 bits and rounded: with
+// the sum of a row's dS shows it to be off by (over all keys dS is zero; not where the keys are cut in parts).  In bf16, error of dq relative to that of a result computed in 64 bits and rounded: with
 // delta from out 1.86 / 1.58 / 1.52 at 16 / 64 / 256 keys, so 1.42 / 1.43 / 1.44 (1.41 is dS's rounding and the result's); the second pass costs 32 -> 37 us
 // at 8 x 1024 queries to 256 keys of 16 heads of 72.
 // What bounds them: heads of 72, the latency of a block's chain (LDS, products, exponentials, products) with two wavefronts per SIMD, which wait 43 % of their
@@ -921,7 +921,7 @@ int32_t launch_sum(const SumJobs& a, int jobs, hipStream_t s) {
     return launch_ok() ? FREE_OK : FREE_ERR_HIP;
 }
 
-// How the two launches are cut; by the sizes alone
+// How the two launches are cut; by the sizes and by whether rows are whole aligned chunks
 struct Plan {
     bool q_ring, resident;
     int32_t q_parts, q_part_tiles, q_blocks;      // q_blocks: resident, 32-row blocks of a workgroup

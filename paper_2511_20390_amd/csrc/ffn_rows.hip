@@ -37,7 +37,7 @@ __device__ __forceinline__ float gate_of(float g, int act) {
     return 0.5f * g * (1.0f + tanhf(0.7978845608028654f * (g + 0.044715f * g * g * g)));
 }
 
-// kEdge: rows' last steps may not be whole.  kAdapt: a bias and the rows' adapters are added, summed before the weights arrive: a thread has
+// kEdge: rows' last steps may not be whole.  kAdapt: a bias and the rows' adapters are added; they are summed in front of the weights' first loads, a thread having
 // at most two values.
 template <typename T, int R, int MT, bool kGated, bool kEdge, bool kAdapt>
 __global__ __launch_bounds__(kWaves * 64) void ffn_rows_kernel(RowArgs a) {
