@@ -140,3 +140,22 @@ def test_lengths_that_end_in_any_part(Nq, Nk, heads, kv, dh, lens, dtype, masked
 @pytest.mark.parametrize("lens", [[1.0, 100, 256], [257, 0, 1], [1.0, 63, 64]])
 def test_many_queries_of_ragged_samples(Nq, Nk, heads, kv, dh, lens, masked):
     ragged(4, [int(n * Nk) if isinstance(n, float) else min(n, Nk) for n in lens], Nq, Nk, heads, kv, dh, torch.bfloat16, masked)
+
+
+@pytest.mark.parametrize("Nq,heads,Nk,dtype", [((1 << 20) + 1, 64, 1100, torch.bfloat16), ((1 << 26) + 33, 1, 1100, torch.bfloat16), ((1 << 20) + 1, 65, 77, torch.float32)])
+def test_gradient_of_rows_past_26_bits(Nq, heads, Nk, dtype):
+    """The last rows alone have a gradient."""
+    dh, gen, few = 8, generator(5), 3000 // heads
+    q = torch.empty(Nq, heads * dh, device=DEV, dtype=dtype).normal_(0, 1.5, generator=gen)
+    k, v = normal(gen, (Nk, dh), 1.0, dtype), normal(gen, (Nk, dh), 1.0, dtype)
+    last = slice(Nq - few, Nq)
+    g = torch.zeros_like(q)
+    g[last] = normal(gen, (few, heads * dh), 1.0, dtype)
+    lse = torch.empty(1, heads, Nq, device=DEV)
+    how = dict(B=1, heads=heads, dh=dh, kv_heads=1)
+    out = b.op_cross_attention(q, k, v, lse=lse, **how)
+    dq, dk, dv = b.op_cross_attention_backward(g, q, k, v, out, lse, **how)
+    ref = cross_reference(q[last], k, v, 1, heads, 1, dh, dh ** -0.5, torch.ones(1, Nk, dtype=torch.bool, device=DEV), g[last])
+    for t, r, what in ((out[last], ref[0], "out"), (lse[:, :, last], ref[1], "lse"), (dq[last], ref[2], "dq"), (dk, ref[3], "dk"), (dv, ref[4], "dv")):
+        check(t, r, what)
+    assert not dq[:Nq - few].any()
