@@ -591,7 +591,8 @@ int32_t free_op_gated_ffn_backward(const void* dout, const void* x, const void* 
  * [B, Nk] bytes, zero for a key that does not count.  What stands in keys that do not count, NaN included, has no influence.  A sample
  * without keys has out zero.
  * lse (NULL: not wanted): fp32 [B, heads, Nq], the logarithm of the sum of exp(scale q k^T), -inf without keys; the gradient reads it.
- * Scores, probabilities' sums and results are summed in fp32; probabilities are rounded to dtype as operands of the second product.
+ * Scores, probabilities' sums and results are summed in fp32; probabilities are rounded to dtype as operands of the second product.  They are divided by
+ * their sum at the end and may be 2^8 before: values of v of 2^120 / Nk and more can make a result infinite.
  * The gradient, of the same inputs, out and lse: dq like q, dk and dv like k and v (each with its distance from row to row), written, not
  * added to, zero for keys that do not count; probabilities and the scores' gradient are rounded to dtype as operands of the products.
  * How sums are cut depends on the sizes and on whether all rows are 16-byte aligned pieces (see above), so equal values at another alignment may
